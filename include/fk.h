@@ -56,8 +56,10 @@ typedef enum fk_status {
   FK_ERR_ARG = 2,      /* null or misaligned pointer, layer/head out of range, short buffer */
   FK_ERR_STATE = 3,    /* call out of order: attend before compress, no current chunk,
                           layers out of step under layer-0 pooled scoring               */
-  FK_ERR_FULL = 4,     /* unbounded window and max_history_frames would be exceeded      */
-  FK_ERR_RANGE = 5,    /* scoring precondition violated: a token's squared key norm > 2^23 */
+  FK_ERR_FULL = 4,     /* unbounded window and max_history_frames would be exceeded; paged cache:
+                          too few free pages, or a sequence beyond max_seq_tokens           */
+  FK_ERR_RANGE = 5,    /* scoring precondition violated: a token's squared key norm > 2^23;
+                          paged cache: see fk_paged_sync_status                             */
   FK_ERR_TIMEOUT = 6,  /* a bounded wait inside a kernel expired; outputs are undefined   */
   FK_ERR_CUDA = 7,     /* a CUDA runtime/driver call failed (no device, launch failure)   */
   FK_ERR_NOMEM = 8     /* device memory for the cache could not be allocated             */
@@ -346,6 +348,124 @@ FK_API fk_status fk_classify_heads(const double* mass, int n_heads, int alpha_pe
  * Asynchronous on `stream`; allocates nothing; uses the current device. */
 FK_API fk_status fk_quantize_e4m3(const void* X, int64_t rows, int dim, int row_scaled,
                                   void* q8, int8_t* exps, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Paged 8-bit cache: keys and values of many sequences in pages, held as OCP FP8 E4M3 codes with one
+ * power-of-two scale for each page and head, and the attention that reads it (no counterpart in the
+ * paper, whose cache holds one video).  For the parts of a generator that are language models: prompt
+ * encoding and rewriting, token-by-token decoding, several streams at once, cross attention.
+ *
+ * Use: fk_paged_step names the sequences of a step, how many tokens each appends and how many queries it
+ * asks; then, layer by layer, fk_paged_append and fk_paged_attend on [tokens][heads][head_dim] bf16
+ * tensors that hold the sequences' tokens one after the other in the step's order.  The next step
+ * (or a drop) ends it: its tokens belong to their sequences from then on.  Until then an append may be repeated
+ * and replaces what it wrote.  A step that no layer was appended to is withdrawn.
+ *
+ * Held values: a block is one page of page_tokens tokens of one kv head.  Its exponent e is the
+ * smallest integer in [-120, 120] with |x| <= 448 * 2^e for the block's finite values (-120 for zeros alone); a
+ * value x is held as E4M3(x * 2^-e) * 2^e, to nearest, ties to even.  The open page's tokens are kept unrounded beside it
+ * and rounded again when e changes, so what a block holds depends on its tokens only.  Infinities are
+ * held as the block's largest magnitude, NaN as 0, and fk_paged_sync_status reports FK_ERR_RANGE.
+ *
+ * All calls: device tensors only (FK_ERR_ARG for host memory or memory of another device), 16-byte aligned, tokens
+ * `stride` elements apart (a multiple of 8, at least heads * head_dim; heads and channels contiguous).  Asynchronous on
+ * `stream`; nothing is allocated or waited for after fk_paged_create (calls can be captured in a
+ * graph, which then stands for this step).  Calls that use different streams are ordered by the
+ * caller, as is the work of one handle's attentions among themselves (they share a workspace).  The current
+ * device is left as it was.
+ * --------------------------------------------------------------------------------------------- */
+enum {
+  FK_ROPE_HALF = 0,        /* channel pairs (i, i + dim/2)  */
+  FK_ROPE_INTERLEAVED = 1  /* channel pairs (2i, 2i + 1)    */
+};
+
+typedef struct fk_paged_config {
+  int32_t n_layers;        /* 1..256; pages are taken for all layers at once                       */
+  int32_t n_q_heads;       /* a multiple of n_kv_heads, at most 1024: head h reads kv head
+                              h / (n_q_heads / n_kv_heads)                                       */
+  int32_t n_kv_heads;      /* 1..128                                                             */
+  int32_t head_dim;        /* 64 or 128                                                          */
+  int32_t page_tokens;     /* 32, 64 or 128                                                      */
+  int32_t n_pages;         /* pages per layer, all sequences (n_pages * n_kv_heads * page_tokens
+                              below 2^31)                                                        */
+  int32_t max_seqs;        /* sequences 0..max_seqs-1, at most 65536                             */
+  int32_t max_seq_tokens;  /* of one sequence                                                    */
+  int32_t rope_style;      /* FK_ROPE_*                                                          */
+  int32_t device;          /* CUDA device ordinal                                                */
+} fk_paged_config;
+
+/* Rotation applied by fk_paged_append: y_i = x_i cos_i - x_j sin_i, y_j = x_j cos_i + x_i sin_i for the
+ * pairs (i, j) of the first `dim` channels, in fp32 with every product and sum rounded by itself. */
+typedef struct fk_rope {
+  const float* cos;        /* device [rows][dim / 2], 16-byte aligned                            */
+  const float* sin;
+  const int32_t* positions;/* device [tokens]: table row of each token; NULL: its place in its
+                              sequence                                                           */
+  int32_t rows;            /* a position outside 0..rows-1 leaves its token unrotated and is reported by
+                              fk_paged_sync_status (FK_ERR_RANGE); places are checked by the call (FK_ERR_ARG) */
+  int32_t dim;             /* rotated channels: a multiple of 16, at most head_dim               */
+} fk_rope;
+
+typedef struct fk_paged fk_paged;
+
+/* Host-only validation (no CUDA call): FK_OK, FK_ERR_CONFIG or FK_ERR_ARG. */
+FK_API fk_status fk_paged_validate_config(const fk_paged_config* cfg);
+
+/* Create a cache on cfg->device and allocate all of its device memory: per layer 2 * n_kv_heads *
+ * head_dim bytes for each token of its pages, and 12 of them for each token of two pages of each of the
+ * max_seqs sequences (their open pages).  Errors as fk_create. */
+FK_API fk_status fk_paged_create(const fk_paged_config* cfg, fk_paged** out);
+
+/* Release the handle and its device memory (synchronizes the device first).  NULL is a no-op. */
+FK_API void fk_paged_destroy(fk_paged* h);
+
+/* Begin a step of n_seqs different sequences (host arrays): sequence seqs[i] appends n_new[i] >= 0 tokens and asks
+ * n_query[i] >= 0 queries (n_query NULL: as many as new tokens), which stand at its last positions.
+ * Takes the pages that the new tokens need.  FK_ERR_FULL when too few are free or a sequence would exceed
+ * max_seq_tokens, FK_ERR_STATE when the step before was appended to some layers and not to others; a
+ * refused step leaves the one before current. */
+FK_API fk_status fk_paged_step(fk_paged* h, int n_seqs, const int32_t* seqs, const int32_t* n_new,
+                               const int32_t* n_query, void* stream);
+
+/* Append the step's keys and values K, V [tokens][n_kv_heads][head_dim] to `layer`, the keys rotated (rope
+ * NULL: as they are).  With Q [tokens][n_q_heads][head_dim], the queries of the same tokens, their
+ * rotation is rounded to bf16 into Q_out (which may be Q) by the same launch; Q needs a rope. */
+FK_API fk_status fk_paged_append(fk_paged* h, int layer, const void* K, int64_t k_stride, const void* V,
+                                 int64_t v_stride, const fk_rope* rope, const void* Q, int64_t q_stride,
+                                 void* Q_out, int64_t q_out_stride, void* stream);
+
+/* O = softmax(scale Q K^T) V over the held keys and values: Q, O [queries][n_q_heads][head_dim].  Query i of
+ * n_query stands at position p = n_keys - n_query + i and sees key j when j <= p (causal = 1) or any j
+ * (causal = 0), and under window > 0 only j > p - window or j < sinks.  A query that sees no key gives 0.  scale = 0:
+ * 1 / sqrt(head_dim).  Logits, softmax and sums are in fp32; products are of the held values and the bf16
+ * queries, exact but for query elements below 2^-10 of their row's largest, which may be rounded to 2^-19 of it;
+ * softmax numerators are rounded to f16 before they multiply the values.
+ * FK_ERR_STATE without a step, or when the layer was not appended to in it. */
+FK_API fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_stride, void* O,
+                                 int64_t o_stride, int causal, int window, int sinks, float scale, void* stream);
+
+/* The held keys and values as bf16 (exact), K, V [*n_tokens][n_kv_heads][head_dim] contiguous: of every
+ * sequence of the step, in its order, all tokens (whole = 1) or those from the start of the page that its
+ * first new token is in (whole = 0).  FK_ERR_ARG when `capacity` tokens are too few (then *n_tokens holds
+ * the count). */
+FK_API fk_status fk_paged_read(fk_paged* h, int layer, int whole, void* K, void* V, int64_t capacity,
+                               int64_t* n_tokens, void* stream);
+
+/* End the current step and empty sequence `seq`: its pages are free for the next step.  FK_ERR_STATE as
+ * fk_paged_step.  Host only; steps that take the pages again come after the work queued on them. */
+FK_API fk_status fk_paged_drop(fk_paged* h, int seq);
+
+/* Tokens of a sequence, the current step's included (-1: no such sequence), and pages not taken. */
+FK_API int64_t fk_paged_length(const fk_paged* h, int seq);
+FK_API int64_t fk_paged_free_pages(const fk_paged* h);
+
+/* Device memory that the handle allocated, kernels launched so far. */
+FK_API size_t fk_paged_reserved_bytes(const fk_paged* h);
+FK_API int64_t fk_paged_launch_count(const fk_paged* h);
+
+/* Synchronize `stream` and report (then clear) device-side conditions: FK_ERR_TIMEOUT (a bounded wait
+ * expired), FK_ERR_RANGE (an appended key or value that was not finite, a position outside the tables), FK_OK. */
+FK_API fk_status fk_paged_sync_status(fk_paged* h, void* stream);
 
 /* Static text for a status code. */
 FK_API const char* fk_status_str(fk_status s);

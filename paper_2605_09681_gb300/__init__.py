@@ -1,5 +1,6 @@
 """Forcing-KV hot path on GB300: hybrid KV-cache compression (static structural pruning,
-segment-similarity pruning) and chunk attention over the compressed cache.
+segment-similarity pruning) and chunk attention over the compressed cache; and a paged 8-bit cache of
+many sequences (PagedKVCache) with the attention that reads it.
 
 Every step runs in the CUDA kernels of libfk.so behind the C ABI of include/fk.h; this
 module only marshals arguments (torch tensors for device memory and streams).
@@ -13,7 +14,7 @@ import numpy as np
 from . import _lib as L
 from ._lib import FkError, KERNEL_KINDS, STATUS_NAMES
 
-__all__ = ["ForcingKVCache", "FkError", "KERNEL_KINDS", "STATUS_NAMES", "load_library",
+__all__ = ["ForcingKVCache", "PagedKVCache", "FkError", "KERNEL_KINDS", "STATUS_NAMES", "load_library",
            "head_profile", "classify_heads", "quantize_e4m3", "stream_read"]
 
 
@@ -292,3 +293,177 @@ class ForcingKVCache:
 
     def launch_count(self) -> int:
         return int(self._lib.fk_launch_count(self._h))
+
+
+def _ints(values, n=None):
+    """A ctypes array of 32-bit whole numbers."""
+    v = [int(x) for x in values]
+    if n is not None and len(v) != n:
+        raise ValueError("expected %d numbers, got %d" % (n, len(v)))
+    if any(not -2 ** 31 <= x < 2 ** 31 for x in v):
+        raise ValueError("numbers must fit 32 bits")
+    return (ctypes.c_int32 * len(v))(*v)
+
+
+class PagedKVCache:
+    """Keys and values of many sequences in pages of E4M3 codes, one power-of-two scale for each page and
+    head (fk_paged_*), on one GPU.
+
+        cache.step(seqs, n_new)                      # which sequences append how many tokens
+        for layer in range(n_layers):
+            Q = cache.append(layer, K, V, cos, sin, Q=Q)   # keys and queries rotated, keys and values held
+            O = cache.attend(layer, Q)
+
+    Tensors are bf16 CUDA tensors [tokens, heads, head_dim], the step's sequences one after the other in its order;
+    they may be slices of wider rows (a fused projection's output).  Calls are asynchronous on `stream`
+    (default: torch's current stream of the cache's device).  The step's tokens belong to their sequences from the
+    next step on; until then append may be called again with other keys and values, which take their place."""
+
+    def __init__(self, *, n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
+                 max_seq_tokens, rope="half", device=0):
+        self._lib = L.load()
+        self._h = ctypes.c_void_p()
+        self.cfg = L.FkPagedConfig(n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
+                                   max_seq_tokens, L.FK_ROPE[rope], device)
+        self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
+        self.page_tokens, self.device = page_tokens, device
+        self._new = self._queries = 0
+        _check(self._lib.fk_paged_create(ctypes.byref(self.cfg), ctypes.byref(self._h)), "fk_paged_create")
+
+    # ---- lifetime
+    def close(self):
+        if getattr(self, "_h", None) and self._h.value:
+            self._lib.fk_paged_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _on(self, stream):
+        if stream is None:
+            import torch
+            try:                                     # as _stream, of the cache's device
+                return torch._C._cuda_getCurrentRawStream(self.device)
+            except AttributeError:
+                return torch.cuda.current_stream(self.device).cuda_stream
+        return getattr(stream, "cuda_stream", stream)
+
+    def _rows(self, x, tokens, heads, name):
+        """(address, elements from token to token) of a [tokens, heads, head_dim] tensor."""
+        import torch
+        D = self.head_dim
+        if x.dtype != torch.bfloat16 or not x.is_cuda or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != D:
+            raise ValueError("%s: expected a bf16 CUDA tensor [tokens, %d, %d]" % (name, heads, D))
+        if x.shape[0] != tokens:
+            raise ValueError("%s: the step has %d tokens, the tensor %d" % (name, tokens, x.shape[0]))
+        if tokens and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != D)):
+            raise ValueError("%s: the heads of a token must lie contiguously" % name)
+        return x.data_ptr(), x.stride(0) if tokens > 1 else heads * D
+
+    # ---- steps
+    def step(self, seqs, n_new, n_query=None, stream=None):
+        """Begin a step: sequence seqs[i] appends n_new[i] tokens and asks n_query[i] queries (default: as
+        many), which stand at its last positions."""
+        s = _ints(seqs)
+        n = _ints(n_new, len(s))
+        q = None if n_query is None else _ints(n_query, len(s))
+        _check(self._lib.fk_paged_step(self._h, len(s), s, n, q, self._on(stream)), "fk_paged_step")
+        self._new = sum(n)
+        self._queries = self._new if q is None else sum(q)
+
+    def append(self, layer, K, V, cos=None, sin=None, positions=None, Q=None, Q_out=None, stream=None):
+        """Append the step's keys and values to a layer, the keys rotated by the tables cos, sin [rows, dim / 2]
+        (fp32) at rows `positions` (int32 [tokens]; default: each token's place in its sequence); without
+        tables as they are.  With Q, the queries of the same tokens, returns them rotated (in Q_out, which
+        may be Q)."""
+        import torch
+        k, ks = self._rows(K, self._new, self.n_kv_heads, "K")
+        v, vs = self._rows(V, self._new, self.n_kv_heads, "V")
+        rope = q = o = None
+        qs = os = 0
+        if cos is not None:
+            if sin is None or cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or \
+                    cos.shape != sin.shape or not cos.is_contiguous() or not sin.is_contiguous():
+                raise ValueError("cos, sin: expected contiguous fp32 tensors [rows, dim / 2]")
+            if positions is not None and (positions.dtype != torch.int32 or positions.dim() != 1 or
+                                          positions.shape[0] != self._new or not positions.is_contiguous()):
+                raise ValueError("positions: expected a contiguous int32 tensor [%d]" % self._new)
+            rope = ctypes.byref(L.FkRope(cos.data_ptr(), sin.data_ptr(), positions.data_ptr() if positions is not None else None,
+                                         cos.shape[0], 2 * cos.shape[1]))
+        elif sin is not None or positions is not None:
+            raise ValueError("sin and positions need cos")
+        if Q is not None:
+            if Q_out is None:
+                Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+            q, qs = self._rows(Q, self._new, self.n_q_heads, "Q")
+            o, os = self._rows(Q_out, self._new, self.n_q_heads, "Q_out")
+        _check(self._lib.fk_paged_append(self._h, layer, k, ks, v, vs, rope, q, qs, o, os, self._on(stream)),
+               "fk_paged_append")
+        return Q_out
+
+    def attend(self, layer, Q, O=None, causal=True, window=0, sinks=0, scale=None, stream=None):
+        """Attention of the step's queries over what their sequences hold: query at position p sees key j when
+        j <= p (causal) or any j, and under window > 0 only j > p - window or j < sinks; a query that sees
+        none gives 0.  scale: default 1 / sqrt(head_dim)."""
+        if O is None:
+            import torch
+            O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+        if scale is not None and not scale > 0:
+            raise ValueError("scale must be positive")
+        q, qs = self._rows(Q, self._queries, self.n_q_heads, "Q")
+        o, os = self._rows(O, self._queries, self.n_q_heads, "O")
+        _check(self._lib.fk_paged_attend(self._h, layer, q, qs, o, os, 1 if causal else 0, window, sinks,
+                                         0.0 if scale is None else scale, self._on(stream)), "fk_paged_attend")
+        return O
+
+    def read(self, layer, whole=False, K=None, V=None, stream=None):
+        """The held keys and values of the step's sequences as bf16 [tokens, n_kv_heads, head_dim]: all their
+        tokens, or those from the start of the page that a sequence's first new token is in."""
+        import torch
+        n = ctypes.c_int64(0)
+        st = self._lib.fk_paged_read(self._h, layer, 1 if whole else 0, None, None, 0, ctypes.byref(n), None)
+        if st != L.FK_OK and n.value == 0:
+            _check(st, "fk_paged_read")
+        shape = (n.value, self.n_kv_heads, self.head_dim)
+        if K is None:
+            K = torch.empty(shape, dtype=torch.bfloat16, device="cuda:%d" % self.device)
+        if V is None:
+            V = torch.empty(shape, dtype=torch.bfloat16, device="cuda:%d" % self.device)
+        for x, name in ((K, "K"), (V, "V")):
+            self._rows(x, n.value, self.n_kv_heads, name)
+            if not x.is_contiguous():
+                raise ValueError("%s: expected a contiguous tensor" % name)
+        _check(self._lib.fk_paged_read(self._h, layer, 1 if whole else 0, K.data_ptr(), V.data_ptr(), n.value,
+                                       ctypes.byref(n), self._on(stream)), "fk_paged_read")
+        return K, V
+
+    def drop(self, seq):
+        """End the current step and empty a sequence: its pages are free for the next step."""
+        _check(self._lib.fk_paged_drop(self._h, seq), "fk_paged_drop")
+        self._new = self._queries = 0
+
+    # ---- inspection
+    def length(self, seq) -> int:
+        return int(self._lib.fk_paged_length(self._h, seq))
+
+    def free_pages(self) -> int:
+        return int(self._lib.fk_paged_free_pages(self._h))
+
+    def reserved_bytes(self) -> int:
+        return int(self._lib.fk_paged_reserved_bytes(self._h))
+
+    def launch_count(self) -> int:
+        return int(self._lib.fk_paged_launch_count(self._h))
+
+    def sync_status(self, stream=None) -> int:
+        """Synchronize and return the device status (FK_OK, FK_ERR_RANGE, FK_ERR_TIMEOUT)."""
+        return int(self._lib.fk_paged_sync_status(self._h, self._on(stream)))

@@ -17,6 +17,7 @@ FK_SCOPE_PER_FRAME, FK_SCOPE_POOLED = 0, 1
 FK_SCORE_PER_HEAD, FK_SCORE_LAYER0_POOLED = 0, 1
 FK_SELECT = {"similarity": 0, "all": 1, "uniform": 2, "random": 3}
 FK_ATTN = {"bf16": 0, "fp8_qk": 1, "fp8": 2}
+FK_ROPE = {"half": 0, "interleaved": 1}
 KERNEL_KINDS = {"append": 0, "score": 1, "select": 2, "compact": 3, "attend": 4}
 
 EXPORTS = [
@@ -26,6 +27,9 @@ EXPORTS = [
     "fk_profile_read", "fk_profile_reset", "fk_launch_count", "fk_status_str", "fk_abi_version",
     "fk_segment_scores_noalloc", "fk_head_profile", "fk_classify_heads", "fk_set_host_overlap",
     "fk_wait_selftest", "fk_wait_outputs", "fk_quantize_e4m3", "fk_stream_read", "fk_force_attention_plan",
+    "fk_paged_validate_config", "fk_paged_create", "fk_paged_destroy", "fk_paged_step", "fk_paged_append",
+    "fk_paged_attend", "fk_paged_read", "fk_paged_drop", "fk_paged_length", "fk_paged_free_pages",
+    "fk_paged_reserved_bytes", "fk_paged_launch_count", "fk_paged_sync_status",
 ]
 
 
@@ -41,6 +45,17 @@ class FkConfig(ctypes.Structure):
         ("selection", ctypes.c_int32), ("select_seed", ctypes.c_uint32),
         ("static_drop_anchor", ctypes.c_int32), ("attn_precision", ctypes.c_int32),
     ]
+
+
+class FkPagedConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "max_seqs",
+                 "max_seq_tokens", "rope_style", "device")]
+
+
+class FkRope(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("rows", ctypes.c_int32), ("dim", ctypes.c_int32)]
 
 
 class FkError(RuntimeError):
@@ -63,7 +78,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
         raise ImportError("libfk.so not built (%s); run paper_2605_09681_gb300.build.build()" % path)
     lib = ctypes.CDLL(path)
     vp, i32, cp = ctypes.c_void_p, ctypes.c_int, ctypes.c_char_p
-    st = ctypes.c_int
+    st, i64 = ctypes.c_int, ctypes.c_int64
     sig = {
         "fk_validate_config": (st, [ctypes.POINTER(FkConfig)]),
         "fk_create": (st, [ctypes.POINTER(FkConfig), ctypes.POINTER(vp)]),
@@ -96,6 +111,19 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                    ctypes.POINTER(ctypes.c_uint8)]),
         "fk_quantize_e4m3": (st, [vp, ctypes.c_int64, i32, i32, vp, vp, vp]),
         "fk_stream_read": (st, [vp, ctypes.c_size_t, vp]),
+        "fk_paged_validate_config": (st, [ctypes.POINTER(FkPagedConfig)]),
+        "fk_paged_create": (st, [ctypes.POINTER(FkPagedConfig), ctypes.POINTER(vp)]),
+        "fk_paged_destroy": (None, [vp]),
+        "fk_paged_step": (st, [vp, i32, vp, vp, vp, vp]),
+        "fk_paged_append": (st, [vp, i32, vp, i64, vp, i64, ctypes.POINTER(FkRope), vp, i64, vp, i64, vp]),
+        "fk_paged_attend": (st, [vp, i32, vp, i64, vp, i64, i32, i32, i32, ctypes.c_float, vp]),
+        "fk_paged_read": (st, [vp, i32, i32, vp, vp, i64, ctypes.POINTER(i64), vp]),
+        "fk_paged_drop": (st, [vp, i32]),
+        "fk_paged_length": (i64, [vp, i32]),
+        "fk_paged_free_pages": (i64, [vp]),
+        "fk_paged_reserved_bytes": (ctypes.c_size_t, [vp]),
+        "fk_paged_launch_count": (i64, [vp]),
+        "fk_paged_sync_status": (st, [vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

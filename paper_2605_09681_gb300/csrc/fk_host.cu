@@ -555,6 +555,19 @@ fk_status update_current(fk_handle* h, int layer, bool retire, const void* K, co
 
 }  // namespace
 
+namespace fk {
+bool encode_byte_rows(CUtensorMap* m, void* base, int64_t rows, int row_bytes, int box_rows) {
+  if (!get_encode()) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)row_bytes, (cuuint32_t)box_rows};
+  const cuuint32_t es[2] = {1, 1};
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+}  // namespace fk
+
 extern "C" {
 
 fk_status fk_head_profile(const void* Q, const void* K, int n_queries, int n_keys, int n_heads,

@@ -95,6 +95,10 @@ __device__ __forceinline__ void fixed24_split(float v, int& hi, int& lo) {
 }
 #endif
 
+// 2D TMA map over [rows][row_bytes] bytes of device memory, boxes of box_rows whole rows, swizzled by the row
+// length (64 or 128 bytes).  False when the driver refuses it.
+bool encode_byte_rows(CUtensorMap* m, void* base, int64_t rows, int row_bytes, int box_rows);
+
 // ------------------------------------------------------------------ copy kernels
 // Current chunk update in one pass: each 16-byte granule of the previous current chunk (in
 // the view fronts) is first copied to its history location, then overwritten by the new

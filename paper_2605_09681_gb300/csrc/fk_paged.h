@@ -1,0 +1,140 @@
+// Internal declarations of the paged 8-bit cache: argument blocks and launchers of its kernels.
+#pragma once
+
+#include "fk_internal.h"
+
+namespace fk {
+
+constexpr int kStepSeqs = 256;        // sequences of one launch (their numbers travel by value)
+constexpr int kPagedFewRows = 16;     // query rows of one warp-level MMA tile
+constexpr int kPagedFewTile = 64;     // keys per tile of the few-row kernel
+
+constexpr int kPartSlots = 1024;      // CTAs of a launch that share their rows with other key splits, at most
+
+constexpr int kStatusNonFinite = 4;   // device status: an appended key or value was not finite
+constexpr int kStatusPosition = 8;    // device status: a position outside the rotation tables
+
+// One layer's pages.  A page of P tokens of kv head h is one block: P rows of D codes, contiguous, and
+// one exponent e (held value = E4M3 code * 2^e) for keys and one for values.
+struct PagedPool {
+  uint8_t* k;                         // [n_pages][Hkv][P][D]
+  uint8_t* v;
+  int8_t* ke;                         // [n_pages][Hkv]
+  int8_t* ve;
+  // the open (last, unfilled) page of each sequence as it was before the rounding, in two slots that
+  // take turns (a step reads the old open page's while it writes the new one's)
+  float* tail_k;                      // [max_seqs][2][Hkv][P][D], rotated
+  bf16* tail_v;
+  float* tail_kmax;                   // [max_seqs][2][Hkv][P]: a token's largest finite magnitude
+  float* tail_vmax;
+};
+
+// Sequences of one append or read-back launch.
+struct PagedSeqs {
+  int n;
+  int slot[kStepSeqs];
+  int old_len[kStepSeqs];
+  int new_len[kStepSeqs];
+  int tok0[kStepSeqs];                // first token of the sequence in the caller's tensors
+  int page0[kStepSeqs + 1];           // pages before the sequence's first one in this launch
+  uint8_t buf[kStepSeqs];             // bit 0: tail slot read, bit 1: tail slot written
+};
+
+struct AppendArgs {
+  PagedPool pool;
+  const int* table;                   // [max_seqs][max_pages]
+  int max_pages, Hkv, G, P, n_pages;
+  const bf16* K;                      // [T][Hkv][D], rows of a token contiguous, kstride from token to token
+  const bf16* V;
+  const bf16* Q;                      // [T][Hkv G][D] or nullptr
+  bf16* Qr;                           // [T][Hkv G][D]
+  int64_t kstride, vstride, qstride, qrstride;
+  const float* cos;                   // [rope_rows][R / 2] or nullptr: no rotation
+  const float* sin;
+  const int* positions;               // table row of each token (nullptr: its place in the sequence)
+  int rope_rows, R, interleaved;
+  int* status;
+  PagedSeqs seqs;
+};
+cudaError_t launch_paged_append(int D, const AppendArgs& a, cudaStream_t s);
+
+// Held keys and values of tokens first(s) .. new_len - 1 of each sequence as bf16, first(s) = the first token of
+// the first page that the step writes (or 0): page0 counts from that page, tok0 its place in the output.
+struct ReadArgs {
+  PagedPool pool;
+  const int* table;
+  int max_pages, Hkv, P;
+  int whole;                          // 1: from token 0
+  bf16* K;                            // [tokens][Hkv][D]
+  bf16* V;
+  PagedSeqs seqs;
+};
+cudaError_t launch_paged_read(int D, const ReadArgs& a, cudaStream_t s);
+
+constexpr int kTableEntries = 480;
+struct TableArgs {                    // table[index[i]] = page[i]
+  int* table;
+  int n;
+  int index[kTableEntries];
+  int page[kTableEntries];
+};
+cudaError_t launch_paged_table(const TableArgs& a, cudaStream_t s);
+
+// Visible keys of the query at position p of a sequence of n keys: j < (causal ? p + 1 : n), and under a window W
+// also j > p - W or j < sinks.
+struct PagedMask {
+  int causal, window, sinks;
+};
+// Key tiles of `tile` keys that hold a visible key of some query at positions p0 .. p1: tiles
+// [0, n_sink) and [first, last).
+struct TileRange {
+  int n_sink, first, last;
+  __host__ __device__ int count() const { return n_sink + (last > first ? last - first : 0); }
+  // the i-th of them
+  __host__ __device__ int at(int i) const { return i < n_sink ? i : first + (i - n_sink); }
+};
+__host__ __device__ inline TileRange paged_tiles(int n_keys, int p0, int p1, const PagedMask& m, int tile) {
+  int end = m.causal ? (p1 + 1 < n_keys ? p1 + 1 : n_keys) : n_keys;
+  if (end < 0) end = 0;               // queries before the first key
+  TileRange r{0, 0, end > 0 ? (end + tile - 1) / tile : 0};
+  if (m.window > 0) {
+    const int lo = p0 - m.window + 1;
+    r.first = lo > 0 ? lo / tile : 0;
+    if (r.first > r.last) r.first = r.last;
+    const int s = ((m.sinks < end ? m.sinks : end) + tile - 1) / tile;
+    r.n_sink = s < r.first ? s : r.first;
+  }
+  return r;
+}
+
+struct PagedAttnSeqs {
+  int n;
+  int slot[kStepSeqs];
+  int n_keys[kStepSeqs];
+  int q0[kStepSeqs];                  // first query of the sequence in Q and O
+  int n_q[kStepSeqs];
+  int item0[kStepSeqs + 1];           // work items before the sequence's first one
+  int part0[kStepSeqs];               // workspace slots before the sequence's first one (key splits)
+};
+
+struct PagedAttnArgs {
+  const int* table;
+  const int8_t* ke;
+  const int8_t* ve;
+  int max_pages, Hkv, G, P;
+  const bf16* Q;                      // [T][Hkv G][D]
+  bf16* O;
+  int64_t qstride, ostride;
+  float scale_log2;                   // log2(e) * scale
+  PagedMask mask;
+  float* part;                        // partial O of the key splits [kPartSlots][16][D], then (m, l, r, -) of their rows
+  int* arrived;                       // [kPartSlots]: splits of a group that are done (0 between launches)
+  int* status;
+  PagedAttnSeqs seqs;
+};
+// At most kPagedFewRows query rows (query, head of the group) per CTA, any number of keys.
+cudaError_t launch_paged_few(int D, const CUtensorMap& tmK, const CUtensorMap& tmV, const PagedAttnArgs& a,
+                             cudaStream_t s);
+cudaError_t paged_attention_prepare(int D);
+
+}  // namespace fk
