@@ -102,41 +102,6 @@ struct Layout {
   static constexpr int kSmem = (kUsed + 1024) > 118 * 1024 ? (kUsed + 1024) : 118 * 1024;
 };
 
-// 32-column chunks `first` .. `first` + `count` - 1 of a key tile
-template <int kFirst, int kCount>
-struct Chunks {
-  static constexpr int first = kFirst, count = kCount;
-};
-
-// 32 logits -> numerators exp2(s * sc + nm): their sums in four chains, and P words (bf16 pairs, or
-// four E4M3 codes; `ov` then collects the bits of the overflow test).  The sums and roundings of a
-// pair come kSkew pairs after its exponentials, so that they do not wait for them.
-constexpr int kSkew = 4;
-template <bool kE4m3>
-__device__ __forceinline__ void exp_chunk(const uint32_t* s, float2 sc2, float2 nm2, float2* ah,
-                                          uint32_t* pk, uint32_t& ov) {
-  float2 e[16];
-#pragma unroll
-  for (int q = 0; q < 16 + kSkew; ++q) {
-    if (q < 16) {
-      const float2 x = ffma2(make_float2(__uint_as_float(s[2 * q]), __uint_as_float(s[2 * q + 1])), sc2, nm2);
-      e[q] = make_float2(fast_exp2(x.x), fast_exp2(x.y));
-    }
-    if (q >= kSkew) {
-      const int p = q - kSkew;
-      ah[p & 3] = fadd2(ah[p & 3], e[p]);
-      if constexpr (kE4m3) {
-        if (p & 1) {
-          pk[p >> 1] = e4m3x4(e[p - 1], e[p]);
-          ov |= pk[p >> 1] + 0x02020202u;
-        }
-      } else {
-        pk[p] = pack_bf16(e[p].x, e[p].y);
-      }
-    }
-  }
-}
-
 // 32 logits -> the sums of exp2(s * sc + nm) in four chains
 __device__ __forceinline__ void exp_sum(const uint32_t* s, float2 sc2, float2 nm2, float2* ah) {
   float2 e[16];
@@ -148,17 +113,6 @@ __device__ __forceinline__ void exp_sum(const uint32_t* s, float2 sc2, float2 nm
     }
     if (q >= kSkew) ah[q & 3] = fadd2(ah[q & 3], e[q - kSkew]);
   }
-}
-
-// Whether a numerator of these columns may exceed the bound in any lane (warp-uniform).  bf16, 2^8: no more
-// than their sum does.  E4M3 (the bound is then 432, the values that round above 416 or saturate):
-// exactly when a code is 0x7E; codes are non-negative and at most 0x7E, so adding 2 to each byte sets
-// its top bit then, without carries between bytes.
-template <bool kE4m3>
-__device__ __forceinline__ bool exceeds(const float2* ah, uint32_t ov) {
-  if constexpr (kE4m3) return __any_sync(0xffffffffu, (ov & 0x80808080u) != 0);
-  const float2 hs2 = fadd2(fadd2(ah[0], ah[1]), fadd2(ah[2], ah[3]));
-  return __any_sync(0xffffffffu, hs2.x + hs2.y > 256.0f);
 }
 
 // Rows [g0, g0 + rows) of the key splits' merge by one of 8 warps: with M = max_s m_s (log2 domain),
@@ -244,6 +198,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   using Lay = Layout<D, kFp8, kFp8PV>;
   constexpr float kThr = kFp8PV ? kRescaleThresholdFp8 : kRescaleThreshold;
   constexpr float kPShift = kFp8PV ? kPShiftFp8 : 0.0f;
+  constexpr PFormat kP = kFp8PV ? PFormat::kE4m3 : PFormat::kBf16;
   constexpr int kHalves = D / 64;                 // 64-column (128-byte) swizzle atoms
   // S_t(j + kAhead) follows P_t V_j; a query tile's (kOne: key set's) first key tile is below kAhead
   constexpr int kAhead = kOne ? 2 : 1;
@@ -561,7 +516,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
 #pragma unroll
         for (int c = 0; c < kN; ++c) {
           uint32_t pk[16], ov = 0;
-          exp_chunk<kFp8PV>(sv[c], sc2, nm2, ac, pk, ov);
+          exp_chunk<kP>(sv[c], sc2, nm2, ac, pk, ov);
           if constexpr (kFp8PV) FK_TMEM_ST8(tS + (c0 + c) * 8, pk);
           else FK_TMEM_ST16(tS + (c0 + c) * 16, pk);
         }
@@ -608,15 +563,15 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         FK_TMEM_LD32(tS, ca);
         FK_TMEM_WAIT_LD32(ca);
         FK_TMEM_LD32(tS + 32, cb);
-        exp_chunk<kFp8PV>(ca, sc2, nm2, ah, pk, ov);
+        exp_chunk<kP>(ca, sc2, nm2, ah, pk, ov);
         FK_TMEM_WAIT_LD32(cb);
         FK_TMEM_LD32(tS + 64, ca);
-        exp_chunk<kFp8PV>(cb, sc2, nm2, ah, pk + kW, ov);
+        exp_chunk<kP>(cb, sc2, nm2, ah, pk + kW, ov);
         FK_TMEM_WAIT_LD32(ca);
         FK_TMEM_LD32(tS + 96, cb);
-        exp_chunk<kFp8PV>(ca, sc2, nm2, ah, pk + 2 * kW, ov);
+        exp_chunk<kP>(ca, sc2, nm2, ah, pk + 2 * kW, ov);
         FK_TMEM_WAIT_LD32(cb);
-        general = exceeds<kFp8PV>(ah, ov);           // warp-uniform
+        general = exceeds<kP>(ah, ov);           // warp-uniform
         if (!general) {
           if constexpr (kFp8PV) {
             FK_TMEM_ST16(tS, pk);
@@ -644,8 +599,8 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
 #pragma unroll
         for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
         ov = 0;
-        exp_chunk<kFp8PV>(cb, sc2, nm2, ah, pk, ov);
-        general = exceeds<kFp8PV>(ah, ov);
+        exp_chunk<kP>(cb, sc2, nm2, ah, pk, ov);
+        general = exceeds<kP>(ah, ov);
         if (!general) {
           if constexpr (kFp8PV) FK_TMEM_ST8(tS + 24, pk);
           else FK_TMEM_ST16(tS + 48, pk);

@@ -11,6 +11,13 @@ constexpr int kPagedFewTile = 64;     // keys per tile of the few-row kernel
 
 constexpr int kPartSlots = 1024;      // CTAs of a launch that share their rows with other key splits, at most
 
+// Stored exponent of a block of zeros (others are at least -120).
+constexpr int kZeroExp = -126;
+// The attention folds a value block's 2^e into the softmax numerators, w = p 2^(e - r), as f16, relative to a
+// reference r that O (fp32) is kept to: e - r stays in [-kRefWindow, 0], so that no weight loses bits to a
+// block of another size, seen or not.  A block outside moves r to e + kRefRoom and rescales O by a power of two.
+constexpr int kRefWindow = 16, kRefRoom = 2;
+
 constexpr int kStatusNonFinite = 4;   // device status: an appended key or value was not finite
 constexpr int kStatusPosition = 8;    // device status: a position outside the rotation tables
 
@@ -115,6 +122,8 @@ struct PagedAttnSeqs {
   int n_q[kStepSeqs];
   int item0[kStepSeqs + 1];           // work items before the sequence's first one
   int part0[kStepSeqs];               // workspace slots before the sequence's first one (key splits)
+  int splits[kStepSeqs];              // key splits of an item
+  int whole[kStepSeqs];               // chunk kernel: items that are not split, the first ones
 };
 
 struct PagedAttnArgs {
@@ -127,7 +136,10 @@ struct PagedAttnArgs {
   int64_t qstride, ostride;
   float scale_log2;                   // log2(e) * scale
   PagedMask mask;
-  float* part;                        // partial O of the key splits [kPartSlots][16][D], then (m, l, r, -) of their rows
+  // partial O of the key splits and then (m, l, r, -) of their rows: [kPartSlots][16][D] and [..][16][4] (few
+  // rows), [part_tiles][128][D] and [..][128][4] (chunks)
+  float* part;
+  int part_tiles;
   int* arrived;                       // [kPartSlots]: splits of a group that are done (0 between launches)
   int* status;
   PagedAttnSeqs seqs;
@@ -135,6 +147,10 @@ struct PagedAttnArgs {
 // At most kPagedFewRows query rows (query, head of the group) per CTA, any number of keys.
 cudaError_t launch_paged_few(int D, const CUtensorMap& tmK, const CUtensorMap& tmV, const PagedAttnArgs& a,
                              cudaStream_t s);
-cudaError_t paged_attention_prepare(int D);
+cudaError_t paged_few_prepare(int D);
+// Any number of query rows, 256 per CTA (one_tile: 128).
+cudaError_t launch_paged_chunk(int D, bool one_tile, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                               const PagedAttnArgs& a, cudaStream_t s);
+cudaError_t paged_chunk_prepare(int D);
 
 }  // namespace fk

@@ -5,7 +5,7 @@
 //   rotation  y_i = x_i c_i - x_j s_i, y_j = x_j c_i + x_i s_i on channel pairs (i, j) of the first R channels,
 //             (i, i + R/2) or (2i, 2i + 1), in fp32 with every product and sum rounded by itself;
 //   block     a = largest finite |y| of the page's tokens so far (those of this step and those already there),
-//             e = smallest integer >= -120 with a <= 448 2^e, code = E4M3(y 2^-e) (exact scaling, one rounding
+//             e = smallest integer >= -120 with a <= 448 2^e (kZeroExp for zeros), code = E4M3(y 2^-e) (exact scaling, one rounding
 //             to nearest even).  Infinities saturate, NaN becomes 0: the cache holds finite values only, so that a
 //             masked key or value can never reach a row that does not see it; the status word tells.
 // A block's codes depend on its tokens only and not on how they came in steps: the open page's tokens are kept as they
@@ -19,8 +19,8 @@
 namespace fk {
 namespace {
 
-// exponent of a block whose largest finite magnitude is `amax`; a block of zeros takes the least one
-__device__ __forceinline__ int block_exponent(float amax) { return amax == 0.0f ? -120 : e4m3_row_exponent(amax); }
+// exponent of a block whose largest finite magnitude is `amax`
+__device__ __forceinline__ int block_exponent(float amax) { return amax == 0.0f ? kZeroExp : e4m3_row_exponent(amax); }
 
 __device__ __forceinline__ void unpack8(uint4 v, float* x) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(2 * D) append_kernel(const __grid_constant__ A
   __syncthreads();
   for (int w = 0; w < (int)(blockDim.x >> 5); ++w) m = fmaxf(m, red[w]);
   const int e = block_exponent(m);
-  const float inv = pow2f(-e);
+  const float inv = pow2f(-e);                 // (2^126 for zeros)
   if (threadIdx.x == 0) exps[block] = (int8_t)e;
   const bool again = lo > 0 && e != e_old;     // the older tokens' codes have another exponent
   const bool open = hi < P;                    // the page stays open: keep its new tokens unrounded

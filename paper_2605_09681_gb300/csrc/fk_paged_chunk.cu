@@ -1,0 +1,783 @@
+// Attention of many queries over the paged 8-bit cache (chunks, prompts): 5th-generation tensor cores.
+//   S = q k^T 2^(e_q + e_k) log2(e) scale,  p = 2^(S - m),  l = sum p,  O = 2^r sum p 2^(e_v - r) v / l
+// with v the codes' values.
+// CTA = (sequence, kv head, two tiles of 128 query rows, key split); a query row is (query, head of the group), so
+// that a group's heads share every key tile.  Small grids: one tile of 128 rows per CTA over two sets of key
+// tiles (kOne).  Keys come in tiles of 128, from 1 to 4 pages each:
+//   warps 0-3 / 4-7    softmax of query tile 0 / 1 (kOne: of key tiles 0, 2, .. / 1, 3, ..), thread = row;
+//   warp 8             page numbers, exponents, and TMA of K and V codes into two-stage rings;
+//   warp 9             tcgen05.mma, in the order PV_0(j), S_0(j+1), PV_1(j), S_1(j+1);
+//   warps 10-11        V codes -> f16 values (exact).
+// Q K^T needs no conversion of the keys: with q 2^-e_q = hi + lo, both E4M3 (a bf16 element of at least 2^-10 of its
+// row's largest is the sum exactly, smaller ones to 2^-19 of the largest), S = hi K^T + lo K^T is two E4M3 products
+// at twice the bf16 rate, on the codes as the cache holds them.  P V needs P in more than 4 bits, and P split the
+// same way would cost each of the 256 x 128 numerators of a key tile five more instructions; the tile's 128 x D values
+// cost six instructions per 16 instead, in warps of their own, and P goes as f16 (11 bits).  The block exponents come
+// for free: e_k and e_v - r of each 32 keys in the factor and the summand of the softmax's fused multiply-add.
+// r (see kRefWindow) is chosen per key tile by the loading warp.  A tile whose own pages differ by more than the
+// window allows ("wild") is handed over 32 keys at a time, O rescaled in between.
+// The pipeline, its barriers and the lazily raised running maximum are those of the chunk attention over packed views.
+#include "fk_paged.h"
+#include "fk_tc.h"
+
+namespace fk {
+namespace {
+
+constexpr float kRescaleThreshold = 1.0f;          // log2 units by which a part must exceed m to raise it
+constexpr int kNoRef = -1000;                      // r before any block but zeros
+constexpr float kNoMax = -3.402823466e38f;         // m before any key: finite, so that 2^(-inf - m) is 0
+constexpr int kWarpTma = 8, kWarpMma = 9, kWarpConv = 10;
+constexpr int kChunkThreads = 384;
+constexpr int kBM = kAttnBM, kBN = kAttnBN;
+constexpr float kShiftP = 7.0f;                    // P is stored times 2^7: at most 2^15 in f16
+constexpr int kInfo = 64;                          // key tiles whose pages and exponents are at hand
+
+struct ChunkInfo {                                 // of a key tile
+  int y[4];                                        // row of each box in the layer's pages
+  uint32_t ke, ve;                                 // exponents of each 32 keys, one byte each
+  int r;                                           // reference of O after the tile
+  int wild;
+};
+struct ChunkBarriers {
+  uint64_t q_ready;
+  uint64_t k0_full, k0_empty;       // key tile 0 (kOne: 0 and 1)
+  uint64_t vk_full[2], vk_empty[2]; // b = j mod 2: V codes of tile j (stage b) with K_{j+1} (kOne: K_{j+2})
+  uint64_t vf_full[2], vf_empty[2]; // f16 values of tile j
+  uint64_t s_full[2], p_full[2], pa_full[2], pva_done[2];
+  uint64_t o_done, fin;
+  uint32_t tmem_base;
+  int last;
+  volatile int abort;
+};
+
+template <int D>
+struct ChunkLayout {
+  static constexpr int kQ = kBM * D;              // one E4M3 query tile (hi or lo)
+  static constexpr int kK = kBN * D;              // one tile of codes
+  static constexpr int kV = kBN * D * 2;          // one tile of f16 values
+  static constexpr int kOffQ = 0;                 // hi, lo of tile 0, hi, lo of tile 1
+  static constexpr int kOffK = kOffQ + 4 * kQ;
+  static constexpr int kOffV8 = kOffK + 2 * kK;
+  static constexpr int kOffV = kOffV8 + 2 * kK;
+  static constexpr int kOffInfo = kOffV + 2 * kV;
+  static constexpr int kOffBar = kOffInfo + kInfo * (int)sizeof(ChunkInfo);
+  static constexpr int kUsed = kOffBar + 320;
+  static_assert(sizeof(ChunkBarriers) <= 320, "barriers");
+  // the epilogue's rows of O in fp32 (256) and their (m, l, r)
+  static_assert(2 * kBM * D * 4 + 2 * kBM * 16 <= kOffInfo, "O over the operand tiles");
+  // at least ~116 KB so that one CTA occupies an SM (its 512 TMEM columns are then free)
+  static constexpr int kSmem = (kUsed + 1024) > 118 * 1024 ? (kUsed + 1024) : 118 * 1024;
+};
+
+// exponent of chunk c (32 keys) of four packed ones
+__device__ __forceinline__ int chunk_exp(uint32_t packed, int c) { return (int)(int8_t)(packed >> (8 * c)); }
+
+// hi = E4M3(x), lo = E4M3(x - hi) of 16 scaled query elements
+__device__ __forceinline__ void split16(const float* x, uint4& hi, uint4& lo) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = e4m3x2(x[4 * i], x[4 * i + 1]), b = e4m3x2(x[4 * i + 2], x[4 * i + 3]);
+    const uint32_t fa = f16x2_of_e4m3x2((uint16_t)a), fb = f16x2_of_e4m3x2((uint16_t)b);
+    const float2 ya = __half22float2(*reinterpret_cast<const __half2*>(&fa));
+    const float2 yb = __half22float2(*reinterpret_cast<const __half2*>(&fb));
+    h[i] = a | (b << 16);
+    l[i] = e4m3x2(x[4 * i] - ya.x, x[4 * i + 1] - ya.y) | (e4m3x2(x[4 * i + 2] - yb.x, x[4 * i + 3] - yb.y) << 16);
+  }
+  hi = make_uint4(h[0], h[1], h[2], h[3]);
+  lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+// byte offset of 16-byte run c of row `row` in a tile of D-byte rows (the TMA's and the MMA's swizzle)
+template <int D>
+__device__ __forceinline__ int code_run(int row, int c) {
+  return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+}
+template <int D, bool kOne>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+             const __grid_constant__ PagedAttnArgs a) {
+  using Lay = ChunkLayout<D>;
+  constexpr int kAhead = kOne ? 2 : 1;            // S_t(j + kAhead) follows P_t V_j
+  constexpr int kTiles = kOne ? 1 : 2;            // query tiles
+  constexpr uint32_t kTmemCols = 512;
+  constexpr uint32_t kColO = 2 * kBN;             // S0 = cols 0..127, S1 = 128..255, O0, O1 after
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = smem + Lay::kOffQ;
+  uint8_t* sK = smem + Lay::kOffK;
+  uint8_t* sV8 = smem + Lay::kOffV8;
+  uint8_t* sV = smem + Lay::kOffV;
+  ChunkInfo* info = reinterpret_cast<ChunkInfo*>(smem + Lay::kOffInfo);
+  ChunkBarriers* bar = reinterpret_cast<ChunkBarriers*>(smem + Lay::kOffBar);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // ---- this CTA's rows and key tiles
+  int s = 0;
+  {
+    int hi = a.seqs.n - 1;
+    while (s < hi) {
+      const int mid = (s + hi + 1) >> 1;
+      if (a.seqs.item0[mid] <= (int)blockIdx.x) s = mid;
+      else hi = mid - 1;
+    }
+  }
+  const int n_keys = a.seqs.n_keys[s], n_q = a.seqs.n_q[s], n_rows = n_q * a.G;
+  // items: (rows, kv head) pairs, the longest rows first; the first `whole` of them unsplit
+  const int groups = (n_rows + kTiles * kBM - 1) / (kTiles * kBM), whole = a.seqs.whole[s];
+  const int item = (int)blockIdx.x - a.seqs.item0[s];
+  const int n_splits = item < whole ? 1 : a.seqs.splits[s];
+  const int split = item < whole ? 0 : (item - whole) % n_splits;
+  const int pair = item < whole ? item : whole + (item - whole) / n_splits;
+  const int kvh = pair % a.Hkv, row0 = (groups - 1 - pair / a.Hkv) * (kTiles * kBM);
+  const int rows = min(kTiles * kBM, n_rows - row0);
+  const int p_first = n_keys - n_q;
+  const TileRange tr = paged_tiles(n_keys, p_first + row0 / a.G, p_first + (row0 + rows - 1) / a.G, a.mask, kBN);
+  const int n_tiles = tr.count();
+  const int i0 = (int)((int64_t)n_tiles * split / n_splits);
+  const int nt = (int)((int64_t)n_tiles * (split + 1) / n_splits) - i0;        // may be 0
+
+  const int box = min(a.P, kPagedFewTile), boxes = kBN / box;   // rows of a TMA box, boxes of a tile
+  auto load = [&](const CUtensorMap* map, uint8_t* dst, int j, uint64_t* b) {   // lanes < boxes
+    if (lane < boxes) tma_load_2d(dst + lane * box * D, map, b, 0, info[j & (kInfo - 1)].y[lane]);
+  };
+  // pages, exponents and references of key tiles j0 + lane (a warp)
+  int ref[2] = {kNoRef, kNoRef};                    // of the last tile (kOne: of each key set)
+  auto fetch_info = [&](int j0) {
+    const int j = j0 + lane;
+    int lo = 127, hi = -127, last = kNoRef;         // of the tile's blocks that are not zeros
+    ChunkInfo x;
+    x.ke = x.ve = 0;
+    if (j < nt) {
+      const int* table = a.table + (int64_t)a.seqs.slot[s] * a.max_pages;
+      const int last_page = max(n_keys - 1, 0) / a.P, key0 = tr.at(i0 + j) * kBN;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {                 // 32 keys each
+        const int key = key0 + 32 * c, page = __ldg(table + min(key / a.P, last_page));
+        const int64_t block = (int64_t)page * a.Hkv + kvh;
+        x.ke |= (uint32_t)(uint8_t)a.ke[block] << (8 * c);
+        const int ev = a.ve[block];
+        x.ve |= (uint32_t)(uint8_t)ev << (8 * c);
+        if (ev != kZeroExp) {
+          lo = min(lo, ev);
+          hi = max(hi, ev);
+          last = ev;
+        }
+        const int y = (page * a.Hkv + kvh) * a.P + key % a.P;
+        if (boxes == 4) x.y[c] = y;
+        else if ((c & 1) == 0) x.y[c >> 1] = y;
+      }
+    }
+    x.wild = hi - lo > kRefWindow - kRefRoom;
+    x.r = 0;
+    for (int i = 0; i < min(32, nt - j0); ++i) {    // the references, tile by tile
+      int r = kOne && (i & 1) ? ref[1] : ref[0];
+      const int thi = __shfl_sync(0xffffffffu, hi, i), tlo = __shfl_sync(0xffffffffu, lo, i);
+      const int tlast = __shfl_sync(0xffffffffu, last, i), tw = __shfl_sync(0xffffffffu, x.wild, i);
+      if (tlast != kNoRef && (tw || thi > r || tlo < r - kRefWindow)) r = (tw ? tlast : thi) + kRefRoom;
+      (kOne && (i & 1) ? ref[1] : ref[0]) = r;
+      if (lane == i) x.r = r;
+    }
+    if (j < nt) info[j & (kInfo - 1)] = x;
+    __syncwarp();
+  };
+
+  if (warp == kWarpTma) {
+    if (lane == 0) {
+      mbar_init(&bar->q_ready, kTiles * kBM);
+      mbar_init(&bar->k0_full, 1);
+      mbar_init(&bar->k0_empty, 1);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&bar->vk_full[i], 1);
+        mbar_init(&bar->vk_empty[i], 3);            // the MMAs, and both converting warps
+        mbar_init(&bar->vf_full[i], 2);
+        mbar_init(&bar->vf_empty[i], 1);
+        mbar_init(&bar->s_full[i], 1);
+        mbar_init(&bar->p_full[i], 4);
+        mbar_init(&bar->pa_full[i], 4);
+        mbar_init(&bar->pva_done[i], 1);
+      }
+      mbar_init(&bar->o_done, 1);
+      mbar_init(&bar->fin, 1);
+      bar->abort = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    fetch_info(0);
+    if (nt > 0) {
+      const bool k1 = kOne && nt > 1;               // kOne: key tiles 0 and 1
+      if (lane == 0) mbar_expect_tx(&bar->k0_full, (k1 ? 2 : 1) * Lay::kK);
+      __syncwarp();
+      load(&tmK, sK, 0, &bar->k0_full);
+      if (k1) load(&tmK, sK + Lay::kK, 1, &bar->k0_full);
+    }
+  }
+  __syncwarp();
+  if (warp == kWarpMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 :: "r"(su32(&bar->tmem_base)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bar->tmem_base;
+
+  // softmax state (warps 0-7)
+  const int t = warp >> 2;                          // query tile (kOne: key set) of this warpgroup
+  const int wq = warp & 3, row = wq * 32 + lane;
+  float m = kNoMax, l = 0.0f;
+  int r = kNoRef;                                   // reference of O
+  uint32_t n_pa = 0;                                // parts handed over on pa_full
+  bool ok = true;
+
+  if (warp == kWarpTma) {
+    // ------------------------------------------------------------------ TMA producer
+    int lastVK[2] = {-1, -1};
+    // per key tile j: V codes of j together with K_{j+1} on one barrier (b = j mod 2).  Their stages were last
+    // used by V_{j-2} (converted) and K_{j-1} (multiplied), released by vk_empty[b]; K_2 reuses K_0's stage: k0_empty.
+    // kOne: V_j with K_{j+2}, whose stage K_j leaves with iteration j-2 (tiles 0 and 1: k0_empty).
+    for (int j = 0; j < nt; ++j) {
+      const int b = j & 1, u = j >> 1, jk = j + kAhead;
+      const bool more = jk < nt;
+      if (j >= 2 && !warp_wait(&bar->vk_empty[b], (u - 1) & 1, bar, a.status)) { ok = false; break; }
+      if (!kOne && j == 1 && more && !warp_wait(&bar->k0_empty, 0, bar, a.status)) { ok = false; break; }
+      if (lane == 0) mbar_expect_tx(&bar->vk_full[b], Lay::kK + (more ? Lay::kK : 0));
+      __syncwarp();
+      load(&tmV, sV8 + b * Lay::kK, j, &bar->vk_full[b]);
+      (b ? lastVK[1] : lastVK[0]) = u;
+      if (kOne && j < 2 && more && !warp_wait(&bar->k0_empty, 0, bar, a.status)) { ok = false; break; }
+      if (more) load(&tmK, sK + (jk & 1) * Lay::kK, jk, &bar->vk_full[b]);
+      if (((jk + 1) & 31) == 0) fetch_info(jk + 1);   // the next 32 tiles', before they are wanted
+    }
+    // On expiry: what was issued lands before the CTA ends.  (A barrier whose K was not issued does not complete:
+    // its V has had the wait's 2 s to land.)
+    if (!ok) {
+      if (nt > 0) wait_phase(&bar->k0_full, 0, bar, a.status, false);
+      for (int b = 0; b < 2; ++b)
+        if (lastVK[b] >= 0) wait_phase(&bar->vk_full[b], lastVK[b] & 1, bar, a.status, false);
+    }
+    __syncwarp();
+  } else if (warp == kWarpMma) {
+    // ------------------------------------------------------------------ MMA issuer
+    // Tensor-core operations of one thread complete in issue order: when S_t(j+1) is complete, so is PV_t(j).
+    constexpr uint32_t kIdQK = idesc_e4m3(kBM, kBN), kIdPV = idesc_f16(kBM, D, 1);
+    constexpr uint32_t kLayout = D == 128 ? 2 : 4, kSbo = 8 * D;
+    const uint64_t dQ = sdesc(su32(sQ), 16, kSbo, kLayout), dK = sdesc(su32(sK), 16, kSbo, kLayout);
+    const uint64_t dV = sdesc(su32(sV), 16384, 1024);
+    auto qk = [&](int j, int tt) {
+      const uint64_t da = dQ + (uint32_t)((kOne ? 0 : tt) * (2 * Lay::kQ >> 4)), db = dK + (uint32_t)((j & 1) * (Lay::kK >> 4));
+      const uint32_t d = tmem + (uint32_t)(tt * kBN);
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) umma_f8(d, da + kk * 2, db + kk * 2, kIdQK, kk > 0 ? 1u : 0u);
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) umma_f8(d, da + (Lay::kQ >> 4) + kk * 2, db + kk * 2, kIdQK, 1u);
+      umma_commit(&bar->s_full[tt]);
+    };
+    // PV of a tile's keys 32 c0 .. 32 c1 - 1
+    auto pv = [&](int j, int tt, int c0, int c1) {
+      const uint64_t db = dV + (uint32_t)((j & 1) * (Lay::kV >> 4));
+      const uint32_t d = tmem + kColO + (uint32_t)(tt * D), p = tmem + (uint32_t)(tt * kBN);
+#pragma unroll
+      for (int kk = 2 * c0; kk < 2 * c1; ++kk)
+        umma_ts(d, p + kk * 8, db + kk * 128, kIdPV, (j >= kAhead || kk > 0) ? 1u : 0u);
+    };
+    auto pv1 = [&](int j, int tt, int c) {          // 32 keys
+      const uint64_t db = dV + (uint32_t)((j & 1) * (Lay::kV >> 4) + c * 256);
+      const uint32_t d = tmem + kColO + (uint32_t)(tt * D), p = tmem + (uint32_t)(tt * kBN + c * 16);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        umma_ts(d, p + kk * 8, db + kk * 128, kIdPV, (j >= kAhead || c > 0 || kk > 0) ? 1u : 0u);
+    };
+    auto wait = [&](uint64_t* b, uint32_t parity) { return warp_wait(b, parity, bar, a.status); };
+    uint32_t n_pa[2] = {0, 0};                      // parts of P taken on pa_full
+    if (nt > 0) {
+      ok = wait(&bar->q_ready, 0) && wait(&bar->k0_full, 0);
+      if (ok) {
+        tc_fence_after();
+        if (elect_one()) {
+          qk(0, 0);
+          if (!kOne) qk(0, 1);
+          else if (nt > 1) qk(1, 1);
+          umma_commit(&bar->k0_empty);
+        }
+      }
+    }
+    for (int j = 0; j < nt && ok; ++j) {
+      const int b = j & 1;
+      const bool more = j + kAhead < nt;
+      const uint32_t ph = kOne ? (j >> 1) & 1 : j & 1;   // of a query tile's (kOne: key set's) barriers
+      if (!wait(&bar->vk_full[b], (j >> 1) & 1) || !wait(&bar->vf_full[b], (j >> 1) & 1)) { ok = false; break; }
+      const bool wild = info[j & (kInfo - 1)].wild != 0;
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        const int tt = kOne ? b : i;
+        uint32_t& np = tt ? n_pa[1] : n_pa[0];
+        if (!wild) {
+          if (!wait(&bar->pa_full[tt], np++ & 1)) { ok = false; break; }
+          tc_fence_after();
+          if (elect_one()) {
+            pv(j, tt, 0, 3);
+            umma_commit(&bar->pva_done[tt]);
+          }
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < 4 && ok; ++c) {
+            ok = wait(&bar->pa_full[tt], np++ & 1);
+            tc_fence_after();
+            if (ok && elect_one()) {
+              pv1(j, tt, c);
+              umma_commit(&bar->pva_done[tt]);
+            }
+          }
+          if (!ok) break;
+        }
+        if (!wait(&bar->p_full[tt], ph)) { ok = false; break; }
+        tc_fence_after();
+        if (elect_one()) {
+          if (!wild) pv(j, tt, 3, 4);
+          if (more) qk(j + kAhead, tt);
+          if (i == kTiles - 1) {
+            umma_commit(&bar->vf_empty[b]);
+            umma_commit(&bar->vk_empty[b]);
+          }
+        }
+      }
+    }
+    if (elect_one()) {
+      if (ok) umma_commit(&bar->o_done);
+      umma_commit(&bar->fin);                       // completes once every MMA above is done
+    }
+    wait_phase(&bar->fin, 0, bar, a.status, false);
+    __syncwarp();
+  } else if (warp >= kWarpConv) {
+    // ------------------------------------------------------------------ V codes -> f16 values
+    constexpr int kRuns = D / 16, kStepRows = 64 / kRuns;   // 16-byte runs of a row; rows per pass
+    const int x = threadIdx.x - kWarpConv * 32, prow = x / kRuns;
+    // the run at physical place x % kRuns of rows prow + kStepRows k: its channels do not depend on k
+    const int c = D == 128 ? (x & 7) ^ (prow & 7) : (x & 3) ^ ((prow >> 1) & 3);
+    const int half = c >> 2, flip = D == 128 ? half : 0;     // (the other half's lanes start with their second unit)
+    const int u0 = ((c & 3) * 2 + flip) ^ (prow & 7), u1 = u0 ^ 1;
+    for (int j = 0; j < nt && ok; ++j) {
+      const int b = j & 1, u = j >> 1;
+      if (!warp_wait(&bar->vk_full[b], u & 1, bar, a.status) ||
+          (j >= 2 && !warp_wait(&bar->vf_empty[b], (u - 1) & 1, bar, a.status))) { ok = false; break; }
+      const uint8_t* src = sV8 + b * Lay::kK + x * 16;
+      uint8_t* dst = sV + b * Lay::kV + half * 16384 + prow * 128;
+#pragma unroll 8
+      for (int k = 0; k < kBN / kStepRows; ++k) {
+        const uint4 v = *reinterpret_cast<const uint4*>(src + k * kStepRows * D);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t y[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[2 * e] = f16x2_of_e4m3x2((uint16_t)w[e]);
+          y[2 * e + 1] = f16x2_of_e4m3x2((uint16_t)(w[e] >> 16));
+        }
+        const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
+        *reinterpret_cast<uint4*>(dst + k * kStepRows * 128 + (u0 << 4)) = flip ? hi : lo;
+        *reinterpret_cast<uint4*>(dst + k * kStepRows * 128 + (u1 << 4)) = flip ? lo : hi;
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor core reads them through it
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&bar->vf_full[b]);
+        mbar_arrive(&bar->vk_empty[b]);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------------ softmax warpgroups
+    const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
+    const uint32_t tS = tmem + lane_base + (uint32_t)(t * kBN);
+    const uint32_t tO = tmem + lane_base + kColO + (uint32_t)(t * D);
+    const int crow = (kOne ? 0 : t * kBM) + row;    // row of the CTA
+    const bool in = crow < rows;
+    const int rr = row0 + (in ? crow : 0), pos = p_first + rr / a.G;
+    float sl2 = a.scale_log2;
+    // this row of Q: scaled to E4M3's range, hi and lo in the MMA's layout (kOne: both key sets want the scale)
+    {
+      const uint4* src = reinterpret_cast<const uint4*>(a.Q + ((int64_t)a.seqs.q0[s] + rr / a.G) * a.qstride +
+                                                        (int64_t)(kvh * a.G + rr % a.G) * D);
+      uint4 v[D / 8];
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) v[j] = in ? __ldg(src + j) : make_uint4(0, 0, 0, 0);
+      float amax = 0.0f;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) amax = fmaxf(amax, absmax8(v[j]));
+      const int e = e4m3_row_exponent(amax);
+      const float inv = pow2f(-e);
+      uint8_t* hi = sQ + (kOne ? 0 : t) * (2 * Lay::kQ);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t w[4] = {v[2 * c + i].x, v[2 * c + i].y, v[2 * c + i].z, v[2 * c + i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            x[8 * i + 2 * k] = __uint_as_float(w[k] << 16) * inv;
+            x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u) * inv;
+          }
+        }
+        if (!kOne || t == 0) {
+          uint4 h4, l4;
+          split16(x, h4, l4);
+          *reinterpret_cast<uint4*>(hi + code_run<D>(row, c)) = h4;
+          *reinterpret_cast<uint4*>(hi + Lay::kQ + code_run<D>(row, c)) = l4;
+        }
+      }
+      sl2 *= pow2f(e);
+      if (!kOne || t == 0) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(&bar->q_ready);
+      }
+    }
+    // visible keys: [lower, limit) and those below the sinks; tiles without a masked key for any of the tile's rows
+    const int limit = a.mask.causal ? min(pos + 1, n_keys) : n_keys;
+    const int lower = a.mask.window > 0 ? pos - a.mask.window + 1 : 0;
+    const int trow1 = min(kOne ? rows : rows - t * kBM, kBM) - 1;   // last row of this query tile
+    const int pa = p_first + (row0 + (kOne ? 0 : t * kBM)) / a.G, pb = p_first + (row0 + (kOne ? 0 : t * kBM) + max(trow1, 0)) / a.G;
+    const int full_hi = a.mask.causal ? min(pa + 1, n_keys) : n_keys;
+    const int full_lo = a.mask.window > 0 ? pb - a.mask.window + 1 : 0;
+
+    for (int it = 0; ok; ++it) {
+      const int j = kOne ? 2 * it + t : it;         // kOne: this warpgroup's key set is every other tile
+      if (j >= nt) break;
+      if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
+      tc_fence_after();
+      const ChunkInfo& ti = info[j & (kInfo - 1)];
+      const uint32_t ke = ti.ke, ve = ti.ve;
+      const bool wild = ti.wild != 0;
+      float rs = 1.0f;                              // what O has to be scaled by for the tile's reference
+      if (!wild && ti.r != r) {
+        rs = pow2_any(r - ti.r);
+        r = ti.r;
+      }
+      // of 32 keys: factor and summand of the exponent S + e_v - r + 7 - m, and 2^(r - e_v) for the row sum
+      auto factor = [&](int c) {
+        // (neither 0 nor infinite: masked logits are -inf, and codes may all be 0)
+        const float f = fminf(fmaxf(sl2 * pow2f(chunk_exp(ke, c)), 1e-37f), 3e38f);
+        return make_float2(f, f);
+      };
+      auto below = [&](int c) {                     // r - e_v
+        const int e = chunk_exp(ve, c);
+        return e == kZeroExp ? 0 : r - e;
+      };
+      auto summand = [&](int c) {
+        const float x = kShiftP - (float)below(c) - m;
+        return make_float2(x, x);
+      };
+      auto weighted = [&](const float2* ah, int c, float& plain) {   // 32 numerators' sum, and its share of l
+        const float2 x = fadd2(fadd2(ah[0], ah[1]), fadd2(ah[2], ah[3]));
+        plain += x.x + x.y;
+        return (x.x + x.y) * pow2f(below(c));
+      };
+      const int key0 = tr.at(i0 + j) * kBN;
+      const bool full = trow1 < 0 || (key0 + kBN <= full_hi && (key0 >= full_lo || key0 + kBN <= a.mask.sinks));
+      // A tile goes in two parts, keys 0-95 and 96-127.  On full tiles after the first, P is computed with the running
+      // max m straight away; a part with a weight beyond 2^8 (2^15 as stored) is done again by general_part, which raises m.
+      // (O holds every key before part c0 once pva_done says so; rs: O's factor for a moved reference.)
+      auto general_part = [&](auto count, int c0, float rs) -> bool {
+        constexpr int kN = decltype(count)::count;
+        uint32_t sv[kN][32];
+#pragma unroll
+        for (int c = 0; c < kN; ++c) FK_TMEM_LD32(tS + (c0 + c) * 32, sv[c]);
+#pragma unroll
+        for (int c = 0; c < kN; ++c) FK_TMEM_WAIT_LD32(sv[c]);
+        if (!full) {                                 // masked keys give 0
+#pragma unroll
+          for (int c = 0; c < kN; ++c) {
+            const int k0 = key0 + (c0 + c) * 32, hi = limit - k0, lo = lower - k0, si = a.mask.sinks - k0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i >= hi || (i < lo && i >= si)) sv[c][i] = __float_as_uint(-INFINITY);
+          }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < kN; ++c) {
+          float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 32; ++i) mxa[i & 3] = fmaxf(mxa[i & 3], __uint_as_float(sv[c][i]));
+          mx = fmaxf(mx, fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * factor(c0 + c).x);
+        }
+        const float m_new = fmaxf(m, mx);
+        const bool raise = __any_sync(0xffffffffu, m_new > m + kRescaleThreshold);   // warp-uniform
+        float alpha = rs;                            // 0 when m = kNoMax
+        if (raise) {
+          const float al = fast_exp2(m - m_new);
+          l *= al;
+          alpha *= al;
+          m = m_new;
+        }
+#pragma unroll
+        for (int c = 0; c < kN; ++c) {
+          uint32_t pk[16], ov = 0;
+          float2 ac[4];
+          float plain = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ac[i] = make_float2(0.0f, 0.0f);
+          exp_chunk<PFormat::kF16>(sv[c], factor(c0 + c), summand(c0 + c), ac, pk, ov);
+          FK_TMEM_ST16(tS + (c0 + c) * 16, pk);
+          l += weighted(ac, c0 + c, plain);
+        }
+        if ((raise || rs != 1.0f) && (it > 0 || c0 > 0)) {
+          if (c0 > 0) {
+            if (!warp_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) return false;
+            tc_fence_after();
+          }
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            FK_TMEM_LD32(tO + c * 32, o);
+            FK_TMEM_WAIT_LD32(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            FK_TMEM_ST32(tO + c * 32, o);
+          }
+        }
+        return true;
+      };
+      auto hand_over = [&](uint64_t* b) {            // P in TMEM -> the MMA warp
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b);
+      };
+      if (wild) {                                    // 32 keys at a time, each at its own reference
+#pragma unroll 1
+        for (int c = 0; c < 4 && ok; ++c) {
+          const int e = chunk_exp(ve, c), rn = e == kZeroExp ? r : e + kRefRoom;
+          const float f = pow2_any(r - rn);
+          r = rn;
+          ok = general_part(Chunks<0, 1>{}, c, f);
+          if (ok) hand_over(&bar->pa_full[t]);
+          ++n_pa;
+        }
+        if (!ok) break;
+        hand_over(&bar->p_full[t]);
+        continue;
+      }
+      const bool direct = full && it > 0 && rs == 1.0f;   // uniform over the warpgroup
+      uint32_t cb[32], ov = 0;
+      bool general = true;
+      if (direct) {
+        uint32_t ca[32], pk[48];
+        float plain = 0.0f, dl = 0.0f;
+        auto part = [&](const uint32_t* x, int c) {
+          float2 ah[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
+          exp_chunk<PFormat::kF16>(x, factor(c), summand(c), ah, pk + 16 * c, ov);
+          dl += weighted(ah, c, plain);
+        };
+        FK_TMEM_LD32(tS, ca);
+        FK_TMEM_WAIT_LD32(ca);
+        FK_TMEM_LD32(tS + 32, cb);
+        part(ca, 0);
+        FK_TMEM_WAIT_LD32(cb);
+        FK_TMEM_LD32(tS + 64, ca);
+        part(cb, 1);
+        FK_TMEM_WAIT_LD32(ca);
+        FK_TMEM_LD32(tS + 96, cb);
+        part(ca, 2);
+        FK_TMEM_WAIT_LD32(cb);
+        general = __any_sync(0xffffffffu, plain > 32768.0f);   // (no numerator exceeds the sum) warp-uniform
+        if (!general) {
+          FK_TMEM_ST32(tS, pk);
+          FK_TMEM_ST16(tS + 32, (pk + 32));
+          l += dl;
+        }
+      }
+      if (general) {
+        if (!general_part(Chunks<0, 3>{}, 0, rs)) { ok = false; break; }
+        if (direct) {                                // (not kept across the general path)
+          FK_TMEM_LD32(tS + 96, cb);
+          FK_TMEM_WAIT_LD32(cb);
+        }
+      }
+      hand_over(&bar->pa_full[t]);
+      ++n_pa;
+      general = true;
+      if (direct) {
+        uint32_t pk[16];
+        float2 ah[4];
+        float plain = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
+        exp_chunk<PFormat::kF16>(cb, factor(3), summand(3), ah, pk, ov);
+        const float dl = weighted(ah, 3, plain);
+        general = __any_sync(0xffffffffu, plain > 32768.0f);
+        if (!general) {
+          FK_TMEM_ST16(tS + 48, pk);
+          l += dl;
+        }
+      }
+      if (general && !general_part(Chunks<0, 1>{}, 3, 1.0f)) { ok = false; break; }
+      hand_over(&bar->p_full[t]);
+    }
+    // ---------------------------------------------------------------- epilogue
+    // every MMA is done, so the operand tiles' shared memory is free
+    ok = ok && warp_wait(&bar->o_done, 0, bar, a.status);
+    tc_fence_after();
+    const bool has = kOne ? t < nt : nt > 0;        // this accumulator was written
+    auto out_row = [&](int r) {                      // row r of the CTA
+      const int q = row0 + r;
+      return a.O + ((int64_t)a.seqs.q0[s] + q / a.G) * a.ostride + (int64_t)(kvh * a.G + q % a.G) * D;
+    };
+    // (r is that of the last tile, or of the tile's last block: the same for all threads of an accumulator)
+    if (!kOne && n_splits == 1) {
+      // normalise, and through the warp's own 32 rows of shared memory (16-byte chunk c of row r at
+      // chunk c ^ (r mod D/8)) to whole rows of O
+      const float inv = l > 0.0f || l != l ? pow2_any(r) / l : 0.0f;    // no visible key: 0
+      uint8_t* stage = smem + warp * (32 * D * 2);
+      if (ok) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          FK_TMEM_LD32(tO + c * 32, o);
+          FK_TMEM_WAIT_LD32(o);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (has) {
+              v.x = pack_bf16(__uint_as_float(o[e + 0]) * inv, __uint_as_float(o[e + 1]) * inv);
+              v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+              v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+              v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+            }
+            *reinterpret_cast<uint4*>(stage + lane * (D * 2) + (((c * 4 + e / 8) ^ (lane & (D / 8 - 1))) << 4)) = v;
+          }
+        }
+        __syncwarp();
+        constexpr int kLanes = D / 8;               // lanes of one row
+        const int cl = lane % kLanes;
+#pragma unroll
+        for (int r0 = 0; r0 < 32; r0 += 32 / kLanes) {
+          const int r = r0 + lane / kLanes, cr = t * kBM + wq * 32 + r;
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + r * (D * 2) + ((cl ^ (r & (D / 8 - 1))) << 4));
+          if (cr < rows) *reinterpret_cast<uint4*>(out_row(cr) + cl * 8) = v;
+        }
+      }
+    } else {
+      // both accumulators to shared memory, [t][row][D] with 16-byte run c of a row at c ^ (row & 7), and their (m, l, r)
+      float* so = reinterpret_cast<float*>(smem) + (t * kBM + row) * D;
+      float4* ml = reinterpret_cast<float4*>(smem + 2 * kBM * D * 4);
+      if (ok) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          FK_TMEM_LD32(tO + c * 32, o);
+          FK_TMEM_WAIT_LD32(o);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<uint4*>(so + (((c * 8 + e) ^ (row & 7)) << 2)) =
+                has ? make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]) : make_uint4(0, 0, 0, 0);
+        }
+      }
+      ml[t * kBM + row] = make_float4(m, l, (float)r, 0.0f);
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      constexpr int kRuns = D / 4;
+      const float* base = reinterpret_cast<const float*>(smem);
+      const int slot0 = a.seqs.part0[s] + (item - whole) * kTiles;          // workspace tiles of this CTA
+      float4* part = reinterpret_cast<float4*>(a.part);
+      float4* mls = part + (int64_t)a.part_tiles * kBM * kRuns;
+      for (int i = threadIdx.x; i < rows * kRuns; i += 256) {
+        const int r = i / kRuns, c = i % kRuns;
+        float4 x = *reinterpret_cast<const float4*>(base + r * D + ((c ^ (r & 7)) << 2));
+        float M = ml[r].x, L = ml[r].y, R = ml[r].z;
+        if constexpr (kOne) {                        // the two key sets
+          const float4 o = ml[kBM + r];
+          const float4 y = *reinterpret_cast<const float4*>(base + (kBM + r) * D + ((c ^ (r & 7)) << 2));
+          const float M2 = fmaxf(M, o.x), R2 = fmaxf(R, o.z), w0 = fast_exp2(M - M2), w1 = fast_exp2(o.x - M2);
+          const float v0 = w0 * pow2_any((int)(R - R2)), v1 = w1 * pow2_any((int)(o.z - R2));
+          x = make_float4(fmaf(x.x, v0, y.x * v1), fmaf(x.y, v0, y.y * v1), fmaf(x.z, v0, y.z * v1), fmaf(x.w, v0, y.w * v1));
+          L = fmaf(L, w0, o.y * w1);
+          M = M2;
+          R = R2;
+        }
+        if (n_splits == 1) {
+          const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;
+          *reinterpret_cast<uint2*>(out_row(r) + 4 * c) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+        } else {
+          part[((int64_t)slot0 * kBM + r) * kRuns + c] = x;
+          if (c == 0) mls[(int64_t)slot0 * kBM + r] = make_float4(M, L, R, 0.0f);
+        }
+      }
+      if (n_splits > 1) {
+        // the last split of the group joins them all, in their order
+        __threadfence();
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const int first = slot0 - split * kTiles;
+        if (threadIdx.x == 0)
+          bar->last = atomicInc(reinterpret_cast<unsigned*>(a.arrived + first), n_splits - 1) == (unsigned)(n_splits - 1);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (bar->last) {
+          __threadfence();
+          for (int i = threadIdx.x; i < rows * kRuns; i += 256) {
+            const int r = i / kRuns, c = i % kRuns;
+            float M = kNoMax, R = kNoRef, L = 0.0f;
+            for (int sp = 0; sp < n_splits; ++sp) {
+              const float4 e = __ldcg(mls + (int64_t)(first + sp * kTiles) * kBM + r);
+              M = fmaxf(M, e.x);
+              R = fmaxf(R, e.z);
+            }
+            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+            for (int sp = 0; sp < n_splits; ++sp) {
+              const float4 e = __ldcg(mls + (int64_t)(first + sp * kTiles) * kBM + r);
+              const float4 x = __ldcg(part + ((int64_t)(first + sp * kTiles) * kBM + r) * kRuns + c);
+              const float f = fast_exp2(e.x - M), fo = f * pow2_any((int)(e.z - R));
+              L = fmaf(f, e.y, L);
+              acc.x = fmaf(fo, x.x, acc.x);
+              acc.y = fmaf(fo, x.y, acc.y);
+              acc.z = fmaf(fo, x.z, acc.z);
+              acc.w = fmaf(fo, x.w, acc.w);
+            }
+            const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;
+            *reinterpret_cast<uint2*>(out_row(r) + 4 * c) =
+                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+          }
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kWarpMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+}  // namespace
+
+cudaError_t paged_chunk_prepare(int D) {
+  cudaError_t e = cudaSuccess;
+  for (int one = 0; one < 2 && e == cudaSuccess; ++one) {
+    if (D == 128)
+      e = cudaFuncSetAttribute(one ? chunk_kernel<128, true> : chunk_kernel<128, false>,
+                               cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkLayout<128>::kSmem);
+    else
+      e = cudaFuncSetAttribute(one ? chunk_kernel<64, true> : chunk_kernel<64, false>,
+                               cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkLayout<64>::kSmem);
+  }
+  return e;
+}
+
+cudaError_t launch_paged_chunk(int D, bool one_tile, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                               const PagedAttnArgs& a, cudaStream_t s) {
+  const unsigned grid = (unsigned)a.seqs.item0[a.seqs.n];
+  if (grid == 0) return cudaSuccess;
+  if (D == 128) {
+    if (one_tile) chunk_kernel<128, true><<<grid, kChunkThreads, ChunkLayout<128>::kSmem, s>>>(tmK, tmV, a);
+    else chunk_kernel<128, false><<<grid, kChunkThreads, ChunkLayout<128>::kSmem, s>>>(tmK, tmV, a);
+  } else {
+    if (one_tile) chunk_kernel<64, true><<<grid, kChunkThreads, ChunkLayout<64>::kSmem, s>>>(tmK, tmV, a);
+    else chunk_kernel<64, false><<<grid, kChunkThreads, ChunkLayout<64>::kSmem, s>>>(tmK, tmV, a);
+  }
+  return cudaGetLastError();
+}
+
+}  // namespace fk

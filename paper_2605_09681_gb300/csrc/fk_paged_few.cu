@@ -1,25 +1,23 @@
 // Attention of a few queries over the paged 8-bit cache (single tokens, drafted tokens): the bytes of the cache
 // bound it, so the keys are split over as many CTAs as the device holds and every byte is loaded once.
-//   S = q k^T 2^(e_q + e_k) log2(e) scale,  p = 2^(S - m),  l = sum p,  O = sum p 2^(e_v - r) v / (2^-r l)
+//   S = q k^T 2^(e_q + e_k) log2(e) scale,  p = 2^(S - m),  l = sum p,  O = 2^r sum p 2^(e_v - r) v / l
+// with v the codes' values.
 // CTA = (sequence, up to 16 query rows of one kv head's group, key split): warp 4 streams tiles of 64 keys and
 // values into a ring (TMA, 2 boxes of a page's rows where pages are smaller); warps 0-3 take 16 keys of
 // each tile by themselves, with their own running maximum m, sum l and O, and meet only at the end.
 //   products  mma.m16n8k16 in f16: E4M3 codes are f16 values exactly, and a query row scaled by 2^-e_q (bf16 has
-//             fewer bits than f16) is too, so that S is exact up to fp32 sums; p is rounded to f16 (11 bits).  The
+//             fewer bits than f16) is too, so that S is exact up to fp32 sums; p 2^(e_v - r) is rounded to f16 (11 bits).  The
 //             tensor memory path would need 128 query rows to be worth its hand-overs.
 //   layout    an MMA's inner index and its columns may be permuted at will, so that each lane reads whole 16-byte
 //             runs of a row from shared memory and converts them in place: key column n of a 16-key group is key
 //             tok(n) = n (n even) or ((n - 1) ^ 4) + 1 (n odd), and with the 128-byte swizzle no two lanes of a
 //             quarter warp then meet in a bank, neither for keys (4 lanes on a row) nor for values (2 runs of 4 rows).
-//   scales    e_k goes into S.  O is kept relative to r, the largest e_v that the warp has seen (values of a block
-//             with a smaller one count 2^(e_v - r) of it, exact unless that is below 2^-22): a growing r rescales O by
-//             an exact power of two.  m is raised only when a row outgrows it by 2^4, so that O is seldom rescaled.
-// Splits leave (m, l, O) in a workspace; the last one to arrive joins them in the order of the splits (no atomics on
+//   scales    e_k is in the factor of the exponent and e_v - r in its summand (r: see kRefWindow), so no key or value
+//             is scaled.  m is raised only when a row outgrows it by 2^4, so that O is seldom rescaled.
+// Splits leave (m, l, r, O) in a workspace; the last one to arrive joins them in the order of the splits (no atomics on
 // values: results do not change from run to run).
 #include "fk_paged.h"
 #include "fk_tc.h"
-
-#include <cuda_fp16.h>
 
 namespace fk {
 namespace {
@@ -48,15 +46,6 @@ struct FewBarriers {
   volatile int abort;
 };
 
-__device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint16_t c) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
-  return h;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 // D += A B, A 16 x 16 (row), B 16 x 8 (column), f16 in, f32 out
 __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -68,9 +57,6 @@ template <int D>
 __device__ __forceinline__ int run_at(int row, int c) {
   return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
 }
-// 2^k for any integer k (0 below the float range)
-__device__ __forceinline__ float pow2_any(int k) { return k < -126 ? 0.0f : pow2f(min(k, 127)); }
-
 // Sequence of work item b: the last s with first[s] <= b.
 __device__ __forceinline__ int find_item(const int* first, int n, int b) {
   int lo = 0, hi = n - 1;
@@ -102,8 +88,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const int s = find_item(a.seqs.item0, a.seqs.n, blockIdx.x);
   const int n_keys = a.seqs.n_keys[s], n_q = a.seqs.n_q[s];
   const int n_rows = n_q * a.G;
-  const int row_tiles = (n_rows + kRows - 1) / kRows;
-  const int n_splits = (a.seqs.item0[s + 1] - a.seqs.item0[s]) / row_tiles;
+  const int n_splits = a.seqs.splits[s];
   const int item = blockIdx.x - a.seqs.item0[s];
   const int split = item % n_splits, row0 = (item / n_splits) * kRows;
   const int rows = min(kRows, n_rows - row0);
@@ -129,7 +114,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   for (int c = 0; c < kCols; ++c)
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[c][i] = 0.0f;
-  int r = -1000;                                        // reference exponent of O (none yet)
+  int r = -1000;                                        // reference of O (none yet)
   const int g = lane >> 2, t = lane & 3;
 
   if (warp == kWarps) {
@@ -255,7 +240,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       const int ja = j0 + va, jb = j0 + vb;             // keys of columns 2 t and 2 t + 1
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float c = sc[h] * ske;
+        const float c = fminf(sc[h] * ske, 3e38f);      // (codes may all be 0)
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           sv[n][2 * h] *= c;
@@ -267,7 +252,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           }
         }
       }
-      // running maximum and reference exponent
+      // running maximum and reference
       float mx[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -275,9 +260,10 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
         mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
       }
-      if (__any_sync(0xffffffffu, mx[0] > m[0] + kRaise || mx[1] > m[1] + kRaise || ev > r)) {
-        const float fr = pow2_any(r - max(r, ev));
-        r = max(r, ev);
+      const bool move = ev != kZeroExp && (ev > r || ev < r - kRefWindow);   // warp-uniform
+      if (__any_sync(0xffffffffu, move || mx[0] > m[0] + kRaise || mx[1] > m[1] + kRaise)) {
+        const float fr = move ? pow2_any(r - (ev + kRefRoom)) : 1.0f;
+        if (move) r = ev + kRefRoom;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float mn = fmaxf(m[h], mx[h]), al = fast_exp2(m[h] - mn);
@@ -290,15 +276,15 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           }
         }
       }
-      const float fv = pow2_any(ev - r);                // of the values' block
+      const float we = ev == kZeroExp ? 0.0f : (float)(ev - r), fl = ev == kZeroExp ? 1.0f : pow2f(r - ev);
       uint32_t p[4];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-          const float x = fast_exp2(sv[n][2 * h] - m[h] + kShiftP), y = fast_exp2(sv[n][2 * h + 1] - m[h] + kShiftP);
-          l[h] += x + y;
-          p[2 * n + h] = pack_f16(x * fv, y * fv);
+          const float z = we + kShiftP - m[h], x = fast_exp2(sv[n][2 * h] + z), y = fast_exp2(sv[n][2 * h + 1] + z);
+          l[h] = fmaf(x + y, fl, l[h]);
+          p[2 * n + h] = pack_f16(x, y);
         }
       // O += P V
       uint4 w[4];
@@ -337,7 +323,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
   __syncthreads();                                      // every tile has been read: the stages are free
 
-  // ---- the warps' (m, r, l) and O
+  // ---- the warps' (m, l, r) and O
   float* sO = reinterpret_cast<float*>(smem);           // [warp][row][D], 16-byte run c of row at c ^ (row & 7)
   __shared__ float sm[kWarps][kRows], sl[kWarps][kRows];
   __shared__ int sr[kWarps];
@@ -370,7 +356,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     return a.O + ((int64_t)a.seqs.q0[s] + rr / a.G) * a.ostride + (int64_t)(kvh * a.G + rr % a.G) * D;
   };
   float* part = a.part + (int64_t)cta * kRows * D;
-  float* ml = a.part + (int64_t)kPartSlots * kRows * D + (int64_t)cta * kRows * 4;   // m, l, r
+  float4* mls = reinterpret_cast<float4*>(a.part + (int64_t)kPartSlots * kRows * D);   // m, l, r
   for (int i = threadIdx.x; i < rows * kRuns; i += kFewThreads) {
     const int row = i / kRuns, c = i % kRuns;
     float M = kLowest, L = 0.0f;
@@ -393,7 +379,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
     } else {
       *reinterpret_cast<float4*>(part + row * D + 4 * c) = acc;
-      if (c == 0) *reinterpret_cast<float4*>(ml + row * 4) = make_float4(M, L, (float)R, 0.0f);
+      if (c == 0) mls[cta * kRows + row] = make_float4(M, L, (float)R, 0.0f);
     }
   }
   if (n_splits == 1) return;
@@ -407,19 +393,18 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   if (!bar->last) return;
   __threadfence();
   const float* parts = a.part + (int64_t)first * kRows * D;
-  const float* mls = a.part + (int64_t)kPartSlots * kRows * D + (int64_t)first * kRows * 4;
   for (int i = threadIdx.x; i < rows * kRuns; i += kFewThreads) {
     const int row = i / kRuns, c = i % kRuns;
     float M = kLowest, RR = -1000.0f, L = 0.0f;
     for (int sp = 0; sp < n_splits; ++sp) {
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(mls + (sp * kRows + row) * 4));
-      M = fmaxf(M, x.x);
-      RR = fmaxf(RR, x.z);
+      const float4 e = __ldcg(mls + (first + sp) * kRows + row);
+      M = fmaxf(M, e.x);
+      RR = fmaxf(RR, e.z);
     }
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
     for (int sp = 0; sp < n_splits; ++sp) {
-      const float4 e = __ldcg(reinterpret_cast<const float4*>(mls + (sp * kRows + row) * 4));
+      const float4 e = __ldcg(mls + (first + sp) * kRows + row);
       const float4 x = __ldcg(reinterpret_cast<const float4*>(parts + ((int64_t)sp * kRows + row) * D + 4 * c));
       const float f = fast_exp2(e.x - M), fo = f * pow2_any((int)(e.z - RR));
       L = fmaf(f, e.y, L);
@@ -436,7 +421,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 
 }  // namespace
 
-cudaError_t paged_attention_prepare(int D) {
+cudaError_t paged_few_prepare(int D) {
   return D == 128 ? cudaFuncSetAttribute(few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewLayout<128>::kSmem)
                   : cudaFuncSetAttribute(few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewLayout<64>::kSmem);
 }

@@ -52,7 +52,9 @@ struct fk_paged {
   std::vector<PagedPool> pools;
   std::vector<CUtensorMap> tmK, tmV;
   int* table = nullptr;
-  float* part = nullptr;
+  float* part_few = nullptr;          // key splits' partial results
+  float* part_chunk = nullptr;
+  int part_tiles = 0;                 // query tiles that part_chunk holds
   int* arrived = nullptr;
   int* status = nullptr;
   int sms = 0;
@@ -175,6 +177,64 @@ void fill_seqs(const fk_paged* h, size_t i0, size_t i1, bool whole, bool read, i
   out->page0[out->n] = page0;
 }
 
+// Work items of the few-row kernel: row tiles of 16, and key splits where they do not fill the device.
+void plan_few(const fk_paged* h, PagedAttnArgs* a) {
+  PagedAttnSeqs& s = a->seqs;
+  int tiles[kStepSeqs], row_tiles[kStepSeqs];
+  int64_t work = 0;                   // key tiles of all CTAs, unsplit
+  for (int k = 0; k < s.n; ++k) {
+    row_tiles[k] = (s.n_q[k] * a->G + kPagedFewRows - 1) / kPagedFewRows;
+    tiles[k] = paged_tiles(s.n_keys[k], s.n_keys[k] - s.n_q[k], s.n_keys[k] - 1, a->mask, kPagedFewTile).count();
+    work += (int64_t)tiles[k] * row_tiles[k] * a->Hkv;
+  }
+  // two CTAs fit an SM; a split takes at least 4 tiles
+  const int64_t per = std::max<int64_t>(4, (work + 2 * h->sms - 1) / (2 * h->sms));
+  int item = 0, part = 0;
+  for (int k = 0; k < s.n; ++k) {
+    int splits = (int)std::max<int64_t>(1, (tiles[k] + per - 1) / per);
+    if (splits > 1 && part + (int64_t)splits * row_tiles[k] * a->Hkv > kPartSlots) splits = 1;
+    s.item0[k] = item;
+    s.part0[k] = part;
+    s.splits[k] = splits;
+    s.whole[k] = 0;
+    item += row_tiles[k] * splits;
+    if (splits > 1) part += splits * row_tiles[k] * a->Hkv;
+  }
+  s.item0[s.n] = item;
+}
+
+// Work items of the chunk kernel; true: one query tile per CTA.
+bool plan_chunk(const fk_paged* h, PagedAttnArgs* a) {
+  PagedAttnSeqs& s = a->seqs;
+  int64_t pairs = 0;
+  for (int k = 0; k < s.n; ++k) pairs += ((int64_t)s.n_q[k] * a->G + 2 * kAttnBM - 1) / (2 * kAttnBM) * a->Hkv;
+  const bool one = pairs < h->sms;
+  const int rows = (one ? 1 : 2) * kAttnBM;
+  int tiles[kStepSeqs], items[kStepSeqs];
+  int64_t work = 0, total = 0;
+  for (int k = 0; k < s.n; ++k) {
+    items[k] = (int)(((int64_t)s.n_q[k] * a->G + rows - 1) / rows * a->Hkv);
+    tiles[k] = paged_tiles(s.n_keys[k], s.n_keys[k] - s.n_q[k], s.n_keys[k] - 1, a->mask, kAttnBN).count();
+    work += (int64_t)tiles[k] * items[k];
+    total += items[k];
+  }
+  const int64_t per = total >= h->sms ? INT32_MAX : std::max<int64_t>(2, (work + h->sms - 1) / h->sms);
+  int item = 0, part = 0;
+  for (int k = 0; k < s.n; ++k) {
+    int splits = (int)std::max<int64_t>(1, (tiles[k] + per - 1) / per);
+    const int64_t slots = (int64_t)splits * items[k] * (rows / kAttnBM);
+    if (splits > 1 && part + slots > h->part_tiles) splits = 1;
+    s.item0[k] = item;
+    s.part0[k] = part;
+    s.splits[k] = splits;
+    s.whole[k] = splits > 1 ? 0 : items[k];
+    item += items[k] * splits;
+    if (splits > 1) part += (int)slots;
+  }
+  s.item0[s.n] = item;
+  return one;
+}
+
 int64_t read_tokens(const fk_paged* h, bool whole) {
   int64_t n = 0;
   const int P = h->cfg.page_tokens;
@@ -255,11 +315,13 @@ fk_status fk_paged_create(const fk_paged_config* cfg, fk_paged** out) {
         e = FK_ERR_CUDA;
     }
     get(S * h->max_pages * sizeof(int), &h->table);
-    get((size_t)kPartSlots * kPagedFewRows * (D + 4) * sizeof(float), &h->part);
+    get((size_t)kPartSlots * kPagedFewRows * (D + 4) * sizeof(float), &h->part_few);
+    h->part_tiles = std::min(4 * h->sms, kPartSlots);
+    get((size_t)h->part_tiles * kAttnBM * (D + 4) * sizeof(float), &h->part_chunk);
     get(kPartSlots * sizeof(int), &h->arrived);
     get(sizeof(int), &h->status);
     if (e != FK_OK) return e;
-    if (paged_attention_prepare((int)D) != cudaSuccess) return FK_ERR_CUDA;
+    if (paged_few_prepare((int)D) != cudaSuccess || paged_chunk_prepare((int)D) != cudaSuccess) return FK_ERR_CUDA;
     if (cudaDeviceSynchronize() != cudaSuccess) return FK_ERR_CUDA;
     *out = h.release();
     return FK_OK;
@@ -287,7 +349,7 @@ fk_status fk_paged_step(fk_paged* h, int n_seqs, const int32_t* seqs, const int3
       total += n_new[i];
       queries += n_query ? n_query[i] : n_new[i];
     }
-    if (total >= ((int64_t)1 << 31) || queries * (h->cfg.n_q_heads / h->cfg.n_kv_heads) >= ((int64_t)1 << 31)) return FK_ERR_ARG;
+    if (total >= ((int64_t)1 << 31) || queries * h->cfg.n_q_heads >= ((int64_t)1 << 31)) return FK_ERR_ARG;
     DeviceGuard dev(h->cfg.device);
     if (dev.err != cudaSuccess) return FK_ERR_CUDA;
     // lengths and pages as they are once the current step has ended: a refusal leaves it as it is
@@ -430,48 +492,36 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
     a->ostride = o_stride;
     a->scale_log2 = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)c.head_dim)));
     a->mask = {causal, window, window > 0 ? sinks : 0};
-    a->part = h->part;
+    a->part_tiles = h->part_tiles;
     a->arrived = h->arrived;
     a->status = h->status;
     int64_t q0 = 0;
     for (size_t i = 0; i < h->step.size(); i += kStepSeqs) {
       const size_t i1 = std::min(h->step.size(), i + kStepSeqs);
-      PagedAttnSeqs& s = a->seqs;
-      s.n = 0;
-      int64_t work = 0;               // key tiles of all CTAs, unsplit
-      int tiles[kStepSeqs], row_tiles[kStepSeqs];
-      for (size_t j = i; j < i1; ++j) {
-        const StepSeq& st = h->step[j];
-        const int n = h->seqs[st.seq].len + st.n_new;
-        if (st.n_query > 0) {
-          const int k = s.n++;
-          s.slot[k] = st.seq;
-          s.n_keys[k] = n;
-          s.q0[k] = (int)q0;
-          s.n_q[k] = st.n_query;
-          row_tiles[k] = (int)(((int64_t)st.n_query * a->G + kPagedFewRows - 1) / kPagedFewRows);
-          tiles[k] = paged_tiles(n, n - st.n_query, n - 1, a->mask, kPagedFewTile).count();
-          work += (int64_t)tiles[k] * row_tiles[k] * c.n_kv_heads;
+      for (const bool chunk : {false, true}) {
+        int64_t q = q0;
+        a->seqs.n = 0;
+        for (size_t j = i; j < i1; ++j) {
+          const StepSeq& st = h->step[j];
+          if (st.n_query > 0 && ((int64_t)st.n_query * a->G > kPagedFewRows) == chunk) {
+            const int k = a->seqs.n++;
+            a->seqs.slot[k] = st.seq;
+            a->seqs.n_keys[k] = h->seqs[st.seq].len + st.n_new;
+            a->seqs.q0[k] = (int)q;
+            a->seqs.n_q[k] = st.n_query;
+          }
+          q += st.n_query;
         }
-        q0 += st.n_query;
+        if (chunk) q0 = q;
+        if (a->seqs.n == 0) continue;
+        const bool one = chunk && plan_chunk(h, a.get());
+        if (!chunk) plan_few(h, a.get());
+        a->part = chunk ? h->part_chunk : h->part_few;
+        const cudaStream_t s = static_cast<cudaStream_t>(stream);
+        const fk_status st = done(h, chunk ? launch_paged_chunk(c.head_dim, one, h->tmK[layer], h->tmV[layer], *a, s)
+                                           : launch_paged_few(c.head_dim, h->tmK[layer], h->tmV[layer], *a, s));
+        if (st != FK_OK) return st;
       }
-      if (s.n == 0) continue;
-      // Key splits: two CTAs fit an SM; a split takes at least 4 tiles.
-      const int64_t per = std::max<int64_t>(4, (work + 2 * h->sms - 1) / (2 * h->sms));
-      int64_t item = 0, part = 0;
-      for (int k = 0; k < s.n; ++k) {
-        int splits = (int)std::max<int64_t>(1, (tiles[k] + per - 1) / per);
-        const int64_t slots = (int64_t)splits * row_tiles[k] * c.n_kv_heads;
-        if (splits > 1 && part + slots > kPartSlots) splits = 1;
-        s.item0[k] = (int)item;
-        s.part0[k] = (int)part;
-        item += (int64_t)row_tiles[k] * splits;
-        if (splits > 1) part += slots;
-      }
-      if (item >= ((int64_t)1 << 31)) return FK_ERR_ARG;
-      s.item0[s.n] = (int)item;
-      const fk_status st = done(h, launch_paged_few(c.head_dim, h->tmK[layer], h->tmV[layer], *a, static_cast<cudaStream_t>(stream)));
-      if (st != FK_OK) return st;
     }
     return FK_OK;
   });

@@ -3,6 +3,8 @@
 // attention kernels only (each has its own copies: everything is inlined).
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "fk_internal.h"
 
 namespace fk {
@@ -103,10 +105,10 @@ __device__ __forceinline__ void tc_fence_after() {
 }
 
 // Shared-memory matrix descriptor (tcgen05): start, leading/stride byte offsets (16-byte
-// units), descriptor version 1, 128-byte swizzle.
-__device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+// units), descriptor version 1, 128-byte swizzle (layout 2) or 64-byte swizzle (layout 4).
+__device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo, uint32_t sbo, uint32_t layout = 2) {
   return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
-         ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (2ull << 61);
+         ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) | (1ull << 46) | ((uint64_t)layout << 61);
 }
 
 // Instruction descriptor, kind::f16: f32 accumulate, bf16 A and B, A K-major,
@@ -114,6 +116,10 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo, uint32_t
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn << 16) |
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// The same for f16 A and B.
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int b_mn) {
+  return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 // Instruction descriptor, kind::f8f6f4: f32 accumulate, A and B E4M3 (type code 0 at bits
 // 7 and 10), A K-major, B K-major (b_mn = 0) or MN-major (b_mn = 1).
@@ -207,6 +213,9 @@ __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
+// 2^k for any integer k (0 below the float range, 2^127 above)
+__device__ __forceinline__ float pow2_any(int k) { return k < -126 ? 0.0f : pow2f(min(k, 127)); }
+
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -270,6 +279,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 p = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+// two E4M3 codes -> two f16 values (exact)
+__device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint16_t c) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
+  return h;
+}
+
 // tcgen05.wait::ld that also names the registers of the loads it completes, so that no use of
 // them can be scheduled before it
 #define FK_TMEM_WAIT_LD32(v)                                                                \
@@ -281,6 +301,57 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
                  "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]),           \
                  "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])            \
                :: "memory")
+
+// 32-column chunks `first` .. `first` + `count` - 1 of a key tile
+template <int kFirst, int kCount>
+struct Chunks {
+  static constexpr int first = kFirst, count = kCount;
+};
+
+// how P goes to the tensor core
+enum class PFormat { kBf16, kF16, kE4m3 };
+
+// 32 logits -> numerators exp2(s * sc + nm): their sums in four chains, and P words (bf16 or f16 pairs, or
+// four E4M3 codes; `ov` then collects the bits of the overflow test).  The sums and roundings of a
+// pair come kSkew pairs after its exponentials, so that they do not wait for them.
+constexpr int kSkew = 4;
+template <PFormat kP>
+__device__ __forceinline__ void exp_chunk(const uint32_t* s, float2 sc2, float2 nm2, float2* ah,
+                                          uint32_t* pk, uint32_t& ov) {
+  float2 e[16];
+#pragma unroll
+  for (int q = 0; q < 16 + kSkew; ++q) {
+    if (q < 16) {
+      const float2 x = ffma2(make_float2(__uint_as_float(s[2 * q]), __uint_as_float(s[2 * q + 1])), sc2, nm2);
+      e[q] = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+    }
+    if (q >= kSkew) {
+      const int p = q - kSkew;
+      ah[p & 3] = fadd2(ah[p & 3], e[p]);
+      if constexpr (kP == PFormat::kE4m3) {
+        if (p & 1) {
+          pk[p >> 1] = e4m3x4(e[p - 1], e[p]);
+          ov |= pk[p >> 1] + 0x02020202u;
+        }
+      } else if constexpr (kP == PFormat::kF16) {
+        pk[p] = pack_f16(e[p].x, e[p].y);
+      } else {
+        pk[p] = pack_bf16(e[p].x, e[p].y);
+      }
+    }
+  }
+}
+
+// Whether a numerator of these columns may exceed the bound in any lane (warp-uniform).  bf16 and f16, 2^8: no more
+// than their sum does.  E4M3 (the bound is then 432, the values that round above 416 or saturate):
+// exactly when a code is 0x7E; codes are non-negative and at most 0x7E, so adding 2 to each byte sets
+// its top bit then, without carries between bytes.
+template <PFormat kP>
+__device__ __forceinline__ bool exceeds(const float2* ah, uint32_t ov) {
+  if constexpr (kP == PFormat::kE4m3) return __any_sync(0xffffffffu, (ov & 0x80808080u) != 0);
+  const float2 hs2 = fadd2(fadd2(ah[0], ah[1]), fadd2(ah[2], ah[3]));
+  return __any_sync(0xffffffffu, hs2.x + hs2.y > 256.0f);
+}
 
 }  // namespace
 }  // namespace fk

@@ -226,6 +226,22 @@ def test_value_blocks_of_very_different_size(D, nq):
     _attend(dict(head_dim=D, page_tokens=32), [330, 90], [nq, nq], [dict(), dict(causal=False)], spread=5.0)
 
 
+def test_tiny_and_huge_magnitudes():
+    r = np.random.default_rng(22)
+    for nq in (1, 70):
+        for kq, vv in ((1e-12, 1e-20), (1e12, 1e20), (1e-30, 1.0)):
+            K, V, Q = (_normal(r, (n, h, 128), 0.2) for n, h in ((150, 2), (150, 2), (nq, 4)))
+            K, V, Q = P.to_bf16(K * np.float32(1 / kq)), P.to_bf16(V * np.float32(vv)), P.to_bf16(Q * np.float32(kq))
+            K[30:70], V[60:100] = 0, 0                     # blocks of zeros among them
+            with _cache(page_tokens=32) as cache:
+                cache.step([0], [150], [nq])
+                cache.append(0, _bf16(K), _bf16(V))
+                o = _np(cache.attend(0, _bf16(Q)))
+            hk, hv = P.held(K, 32), P.held(V, 32)
+            want = P.attention(Q, hk, hv, True, 0, 0)
+            assert (np.abs(o - want) <= _bound(want, hv)).all(), (nq, kq, vv)
+
+
 @pytest.mark.parametrize("scale", [0.02, 0.5])
 def test_scale(scale):
     _attend({}, [200, 70], [3, 70], [dict(), dict(causal=False)], scale=scale)
