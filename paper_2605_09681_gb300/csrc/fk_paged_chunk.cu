@@ -5,14 +5,14 @@
 // that a group's heads share every key tile.  Small grids: one tile of 128 rows per CTA over two sets of key
 // tiles (kOne).  Keys come in tiles of 128, from 1 to 4 pages each:
 //   warps 0-3 / 4-7    softmax of query tile 0 / 1 (kOne: of key tiles 0, 2, .. / 1, 3, ..), thread = row;
-//   warp 8             page numbers, exponents, and TMA of K and V codes into two-stage rings;
+//   warp 8             page numbers, exponents, and TMA of K and V codes into rings of three and two stages;
 //   warp 9             tcgen05.mma, in the order PV_0(j), S_0(j+1), PV_1(j), S_1(j+1);
-//   warps 10-11        V codes -> f16 values (exact).
+//   warps 10-11        V codes -> f16 values (exact), two stages.
 // Q K^T needs no conversion of the keys: with q 2^-e_q = hi + lo, both E4M3 (a bf16 element of at least 2^-10 of its
 // row's largest is the sum exactly, smaller ones to 2^-19 of the largest), S = hi K^T + lo K^T is two E4M3 products
 // at twice the bf16 rate, on the codes as the cache holds them.  P V needs P in more than 4 bits, and P split the
 // same way would cost each of the 256 x 128 numerators of a key tile five more instructions; the tile's 128 x D values
-// cost six instructions per 16 instead, in warps of their own, and P goes as f16 (11 bits).  The block exponents come
+// cost twelve instructions per 16 instead, in warps of their own, and P goes as f16 (11 bits).  The block exponents come
 // for free: e_k and e_v - r of each 32 keys in the factor and the summand of the softmax's fused multiply-add.
 // r (see kRefWindow) is chosen per key tile by the loading warp.  A tile whose own pages differ by more than the
 // window allows ("wild") is handed over 32 keys at a time, O rescaled in between.
@@ -28,26 +28,34 @@ constexpr int kNoRef = -1000;                      // r before any block but zer
 constexpr float kNoMax = -3.402823466e38f;         // m before any key: finite, so that 2^(-inf - m) is 0
 constexpr int kWarpTma = 8, kWarpMma = 9, kWarpConv = 10;
 constexpr int kChunkThreads = 384;
+constexpr int kKStages = 3;
 constexpr int kBM = kAttnBM, kBN = kAttnBN;
 constexpr float kShiftP = 7.0f;                    // P is stored times 2^7: at most 2^15 in f16
 constexpr int kInfo = 64;                          // key tiles whose pages and exponents are at hand
 
 struct ChunkInfo {                                 // of a key tile
   int y[4];                                        // row of each box in the layer's pages
-  uint32_t ke, ve;                                 // exponents of each 32 keys, one byte each
+  uint32_t ve;                                     // e_v of each 32 keys, one byte each
   int r;                                           // reference of O after the tile
   int wild;
+  int key0;                                        // first key
+  // of each 32 keys: 2^e_k, the exponent's summand e_v - r + 7, and 2^(r - e_v) for the row sum (r the
+  // tile's reference, or the 32 keys' own in a wild tile; blocks of zeros count as e_v = r)
+  float fk[4], add[4], mul[4];
 };
 struct ChunkBarriers {
   uint64_t q_ready;
-  uint64_t k0_full, k0_empty;       // key tile 0 (kOne: 0 and 1)
-  uint64_t vk_full[2], vk_empty[2]; // b = j mod 2: V codes of tile j (stage b) with K_{j+1} (kOne: K_{j+2})
-  uint64_t vf_full[2], vf_empty[2]; // f16 values of tile j
+  uint64_t k_full[kKStages], k_empty[kKStages];
+  uint64_t v8_full[2], v8_empty[2]; // V codes
+  uint64_t vf_full[2], vf_empty[2]; // f16 values
   uint64_t s_full[2], p_full[2], pa_full[2], pva_done[2];
   uint64_t o_done, fin;
   uint32_t tmem_base;
   int last;
+  int n_info;                       // key tiles whose ChunkInfo has been written
   volatile int abort;
+  // what the epilogue needs of the CTA's place (kept here and not in registers across the key tiles)
+  volatile int seq, kvh, row0, rows, split, n_splits, slot0;
 };
 
 template <int D>
@@ -57,12 +65,12 @@ struct ChunkLayout {
   static constexpr int kV = kBN * D * 2;          // one tile of f16 values
   static constexpr int kOffQ = 0;                 // hi, lo of tile 0, hi, lo of tile 1
   static constexpr int kOffK = kOffQ + 4 * kQ;
-  static constexpr int kOffV8 = kOffK + 2 * kK;
+  static constexpr int kOffV8 = kOffK + kKStages * kK;
   static constexpr int kOffV = kOffV8 + 2 * kK;
   static constexpr int kOffInfo = kOffV + 2 * kV;
   static constexpr int kOffBar = kOffInfo + kInfo * (int)sizeof(ChunkInfo);
-  static constexpr int kUsed = kOffBar + 320;
-  static_assert(sizeof(ChunkBarriers) <= 320, "barriers");
+  static constexpr int kUsed = kOffBar + 384;
+  static_assert(sizeof(ChunkBarriers) <= 384, "barriers");
   // the epilogue's rows of O in fp32 (256) and their (m, l, r)
   static_assert(2 * kBM * D * 4 + 2 * kBM * 16 <= kOffInfo, "O over the operand tiles");
   // at least ~116 KB so that one CTA occupies an SM (its 512 TMEM columns are then free)
@@ -140,13 +148,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   auto load = [&](const CUtensorMap* map, uint8_t* dst, int j, uint64_t* b) {   // lanes < boxes
     if (lane < boxes) tma_load_2d(dst + lane * box * D, map, b, 0, info[j & (kInfo - 1)].y[lane]);
   };
+  auto load_k = [&](int j) {
+    const int st = j % kKStages;
+    if (lane == 0) mbar_expect_tx(&bar->k_full[st], Lay::kK);
+    __syncwarp();
+    load(&tmK, sK + st * Lay::kK, j, &bar->k_full[st]);
+  };
   // pages, exponents and references of key tiles j0 + lane (a warp)
   int ref[2] = {kNoRef, kNoRef};                    // of the last tile (kOne: of each key set)
   auto fetch_info = [&](int j0) {
     const int j = j0 + lane;
     int lo = 127, hi = -127, last = kNoRef;         // of the tile's blocks that are not zeros
     ChunkInfo x;
-    x.ke = x.ve = 0;
+    x.ve = 0;
+    float fk[4] = {1.0f, 1.0f, 1.0f, 1.0f};
     if (j < nt) {
       const int* table = a.table + (int64_t)a.seqs.slot[s] * a.max_pages;
       const int last_page = max(n_keys - 1, 0) / a.P, key0 = tr.at(i0 + j) * kBN;
@@ -154,7 +169,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       for (int c = 0; c < 4; ++c) {                 // 32 keys each
         const int key = key0 + 32 * c, page = __ldg(table + min(key / a.P, last_page));
         const int64_t block = (int64_t)page * a.Hkv + kvh;
-        x.ke |= (uint32_t)(uint8_t)a.ke[block] << (8 * c);
+        fk[c] = pow2f(a.ke[block]);
         const int ev = a.ve[block];
         x.ve |= (uint32_t)(uint8_t)ev << (8 * c);
         if (ev != kZeroExp) {
@@ -177,18 +192,29 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       (kOne && (i & 1) ? ref[1] : ref[0]) = r;
       if (lane == i) x.r = r;
     }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int e = chunk_exp(x.ve, c), below = e == kZeroExp ? 0 : x.wild ? kRefRoom : x.r - e;
+      x.fk[c] = fk[c];
+      x.add[c] = kShiftP - (float)below;
+      x.mul[c] = pow2_any(below);
+    }
+    x.key0 = j < nt ? tr.at(i0 + j) * kBN : 0;
     if (j < nt) info[j & (kInfo - 1)] = x;
     __syncwarp();
+    if (lane == 0) asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" :: "r"(su32(&bar->n_info)), "r"(j0 + 32) : "memory");
   };
 
   if (warp == kWarpTma) {
     if (lane == 0) {
       mbar_init(&bar->q_ready, kTiles * kBM);
-      mbar_init(&bar->k0_full, 1);
-      mbar_init(&bar->k0_empty, 1);
+      for (int i = 0; i < kKStages; ++i) {
+        mbar_init(&bar->k_full[i], 1);
+        mbar_init(&bar->k_empty[i], 1);
+      }
       for (int i = 0; i < 2; ++i) {
-        mbar_init(&bar->vk_full[i], 1);
-        mbar_init(&bar->vk_empty[i], 3);            // the MMAs, and both converting warps
+        mbar_init(&bar->v8_full[i], 1);
+        mbar_init(&bar->v8_empty[i], 2);            // both converting warps
         mbar_init(&bar->vf_full[i], 2);
         mbar_init(&bar->vf_empty[i], 1);
         mbar_init(&bar->s_full[i], 1);
@@ -199,17 +225,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       mbar_init(&bar->o_done, 1);
       mbar_init(&bar->fin, 1);
       bar->abort = 0;
+      bar->n_info = 0;
+      bar->seq = s;
+      bar->kvh = kvh;
+      bar->row0 = row0;
+      bar->rows = rows;
+      bar->split = split;
+      bar->n_splits = n_splits;
+      bar->slot0 = a.seqs.part0[s] + (item - whole) * kTiles;   // workspace tiles of this CTA
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
     fetch_info(0);
-    if (nt > 0) {
-      const bool k1 = kOne && nt > 1;               // kOne: key tiles 0 and 1
-      if (lane == 0) mbar_expect_tx(&bar->k0_full, (k1 ? 2 : 1) * Lay::kK);
-      __syncwarp();
-      load(&tmK, sK, 0, &bar->k0_full);
-      if (k1) load(&tmK, sK + Lay::kK, 1, &bar->k0_full);
-    }
+    for (int j = 0; j < min(2, nt); ++j) load_k(j);
   }
   __syncwarp();
   if (warp == kWarpMma) {
@@ -232,29 +260,24 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
 
   if (warp == kWarpTma) {
     // ------------------------------------------------------------------ TMA producer
-    int lastVK[2] = {-1, -1};
-    // per key tile j: V codes of j together with K_{j+1} on one barrier (b = j mod 2).  Their stages were last
-    // used by V_{j-2} (converted) and K_{j-1} (multiplied), released by vk_empty[b]; K_2 reuses K_0's stage: k0_empty.
-    // kOne: V_j with K_{j+2}, whose stage K_j leaves with iteration j-2 (tiles 0 and 1: k0_empty).
+    // V_j, then K_{j+2} (K_0 and K_1 are under way)
+    int jv = -1, jk = min(2, nt) - 1;               // last tiles issued
     for (int j = 0; j < nt; ++j) {
-      const int b = j & 1, u = j >> 1, jk = j + kAhead;
-      const bool more = jk < nt;
-      if (j >= 2 && !warp_wait(&bar->vk_empty[b], (u - 1) & 1, bar, a.status)) { ok = false; break; }
-      if (!kOne && j == 1 && more && !warp_wait(&bar->k0_empty, 0, bar, a.status)) { ok = false; break; }
-      if (lane == 0) mbar_expect_tx(&bar->vk_full[b], Lay::kK + (more ? Lay::kK : 0));
+      const int b = j & 1;
+      if (j >= 2 && !warp_wait(&bar->v8_empty[b], ((j >> 1) - 1) & 1, bar, a.status)) { ok = false; break; }
+      if (lane == 0) mbar_expect_tx(&bar->v8_full[b], Lay::kK);
       __syncwarp();
-      load(&tmV, sV8 + b * Lay::kK, j, &bar->vk_full[b]);
-      (b ? lastVK[1] : lastVK[0]) = u;
-      if (kOne && j < 2 && more && !warp_wait(&bar->k0_empty, 0, bar, a.status)) { ok = false; break; }
-      if (more) load(&tmK, sK + (jk & 1) * Lay::kK, jk, &bar->vk_full[b]);
-      if (((jk + 1) & 31) == 0) fetch_info(jk + 1);   // the next 32 tiles', before they are wanted
+      load(&tmV, sV8 + b * Lay::kK, j, &bar->v8_full[b]);
+      jv = j;
+      if (j + 2 >= nt) continue;
+      if (((j + 2) & 31) == 0) fetch_info(j + 2);
+      if (j + 2 >= kKStages && !warp_wait(&bar->k_empty[(j + 2) % kKStages], ((j + 2) / kKStages - 1) & 1, bar, a.status)) { ok = false; break; }
+      load_k(j + 2);
+      jk = j + 2;
     }
-    // On expiry: what was issued lands before the CTA ends.  (A barrier whose K was not issued does not complete:
-    // its V has had the wait's 2 s to land.)
-    if (!ok) {
-      if (nt > 0) wait_phase(&bar->k0_full, 0, bar, a.status, false);
-      for (int b = 0; b < 2; ++b)
-        if (lastVK[b] >= 0) wait_phase(&bar->vk_full[b], lastVK[b] & 1, bar, a.status, false);
+    if (!ok) {                                      // what was issued lands before the CTA ends
+      for (int j = max(0, jk - kKStages + 1); j <= jk; ++j) wait_phase(&bar->k_full[j % kKStages], (j / kKStages) & 1, bar, a.status, false);
+      for (int j = max(0, jv - 1); j <= jv; ++j) wait_phase(&bar->v8_full[j & 1], (j >> 1) & 1, bar, a.status, false);
     }
     __syncwarp();
   } else if (warp == kWarpMma) {
@@ -265,7 +288,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const uint64_t dQ = sdesc(su32(sQ), 16, kSbo, kLayout), dK = sdesc(su32(sK), 16, kSbo, kLayout);
     const uint64_t dV = sdesc(su32(sV), 16384, 1024);
     auto qk = [&](int j, int tt) {
-      const uint64_t da = dQ + (uint32_t)((kOne ? 0 : tt) * (2 * Lay::kQ >> 4)), db = dK + (uint32_t)((j & 1) * (Lay::kK >> 4));
+      const uint64_t da = dQ + (uint32_t)((kOne ? 0 : tt) * (2 * Lay::kQ >> 4)), db = dK + (uint32_t)((j % kKStages) * (Lay::kK >> 4));
       const uint32_t d = tmem + (uint32_t)(tt * kBN);
 #pragma unroll
       for (int kk = 0; kk < D / 32; ++kk) umma_f8(d, da + kk * 2, db + kk * 2, kIdQK, kk > 0 ? 1u : 0u);
@@ -290,15 +313,23 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     };
     auto wait = [&](uint64_t* b, uint32_t parity) { return warp_wait(b, parity, bar, a.status); };
     uint32_t n_pa[2] = {0, 0};                      // parts of P taken on pa_full
+    auto k_ready = [&](int j) { return wait(&bar->k_full[j % kKStages], (j / kKStages) & 1); };
     if (nt > 0) {
-      ok = wait(&bar->q_ready, 0) && wait(&bar->k0_full, 0);
+      ok = wait(&bar->q_ready, 0) && k_ready(0);
       if (ok) {
         tc_fence_after();
         if (elect_one()) {
           qk(0, 0);
           if (!kOne) qk(0, 1);
-          else if (nt > 1) qk(1, 1);
-          umma_commit(&bar->k0_empty);
+          umma_commit(&bar->k_empty[0]);
+        }
+      }
+      ok = ok && wait(&bar->vf_full[0], 0);
+      if (kOne && nt > 1 && ok) {
+        ok = k_ready(1);
+        if (ok && elect_one()) {
+          qk(1, 1);
+          umma_commit(&bar->k_empty[1]);
         }
       }
     }
@@ -306,7 +337,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       const int b = j & 1;
       const bool more = j + kAhead < nt;
       const uint32_t ph = kOne ? (j >> 1) & 1 : j & 1;   // of a query tile's (kOne: key set's) barriers
-      if (!wait(&bar->vk_full[b], (j >> 1) & 1) || !wait(&bar->vf_full[b], (j >> 1) & 1)) { ok = false; break; }
       const bool wild = info[j & (kInfo - 1)].wild != 0;
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
@@ -331,6 +361,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           }
           if (!ok) break;
         }
+        // K for the tile's S before the second part, the next V before the last one: neither has anything left to
+        // hide behind between a tile's S and the next tile's P (a wait takes ~100 cycles when there is nothing to wait for)
+        if (i == 0 && more && !k_ready(j + kAhead)) { ok = false; break; }
+        if (i == kTiles - 1 && j + 1 < nt && !wait(&bar->vf_full[b ^ 1], ((j + 1) >> 1) & 1)) { ok = false; break; }
         if (!wait(&bar->p_full[tt], ph)) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
@@ -338,7 +372,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           if (more) qk(j + kAhead, tt);
           if (i == kTiles - 1) {
             umma_commit(&bar->vf_empty[b]);
-            umma_commit(&bar->vk_empty[b]);
+            if (more) umma_commit(&bar->k_empty[(j + kAhead) % kKStages]);
           }
         }
       }
@@ -351,37 +385,36 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     __syncwarp();
   } else if (warp >= kWarpConv) {
     // ------------------------------------------------------------------ V codes -> f16 values
-    constexpr int kRuns = D / 16, kStepRows = 64 / kRuns;   // 16-byte runs of a row; rows per pass
-    const int x = threadIdx.x - kWarpConv * 32, prow = x / kRuns;
-    // the run at physical place x % kRuns of rows prow + kStepRows k: its channels do not depend on k
-    const int c = D == 128 ? (x & 7) ^ (prow & 7) : (x & 3) ^ ((prow >> 1) & 3);
-    const int half = c >> 2, flip = D == 128 ? half : 0;     // (the other half's lanes start with their second unit)
-    const int u0 = ((c & 3) * 2 + flip) ^ (prow & 7), u1 = u0 ^ 1;
+    // A thread takes 8 codes of a row at a time: half a 16-byte run, one 16-byte unit of the f16 row.
+    constexpr int kOct = D / 8, kStepRows = 64 / kOct, kFly = 8;   // units of a row; rows per pass; loads in flight
+    const int x = threadIdx.x - kWarpConv * 32, prow = x / kOct, unit = x % kOct;
     for (int j = 0; j < nt && ok; ++j) {
       const int b = j & 1, u = j >> 1;
-      if (!warp_wait(&bar->vk_full[b], u & 1, bar, a.status) ||
+      if (!warp_wait(&bar->v8_full[b], u & 1, bar, a.status) ||
           (j >= 2 && !warp_wait(&bar->vf_empty[b], (u - 1) & 1, bar, a.status))) { ok = false; break; }
-      const uint8_t* src = sV8 + b * Lay::kK + x * 16;
-      uint8_t* dst = sV + b * Lay::kV + half * 16384 + prow * 128;
-#pragma unroll 8
-      for (int k = 0; k < kBN / kStepRows; ++k) {
-        const uint4 v = *reinterpret_cast<const uint4*>(src + k * kStepRows * D);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        uint32_t y[8];
+      const uint8_t* src = sV8 + b * Lay::kK;
+      uint8_t* dst = sV + b * Lay::kV;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          y[2 * e] = f16x2_of_e4m3x2((uint16_t)w[e]);
-          y[2 * e + 1] = f16x2_of_e4m3x2((uint16_t)(w[e] >> 16));
+      for (int k0 = 0; k0 < kBN / kStepRows; k0 += kFly) {   // (loads would not pass the stores by themselves)
+        uint2 v[kFly];
+#pragma unroll
+        for (int k = 0; k < kFly; ++k) {
+          const int r = prow + (k0 + k) * kStepRows;
+          v[k] = *reinterpret_cast<const uint2*>(src + code_run<D>(r, unit >> 1) + (unit & 1) * 8);
         }
-        const uint4 lo = make_uint4(y[0], y[1], y[2], y[3]), hi = make_uint4(y[4], y[5], y[6], y[7]);
-        *reinterpret_cast<uint4*>(dst + k * kStepRows * 128 + (u0 << 4)) = flip ? hi : lo;
-        *reinterpret_cast<uint4*>(dst + k * kStepRows * 128 + (u1 << 4)) = flip ? lo : hi;
+#pragma unroll
+        for (int k = 0; k < kFly; ++k) {
+          const int r = prow + (k0 + k) * kStepRows;
+          *reinterpret_cast<uint4*>(dst + (unit >> 3) * 16384 + r * 128 + (((unit & 7) ^ (r & 7)) << 4)) =
+              make_uint4(f16x2_of_e4m3x2((uint16_t)v[k].x), f16x2_of_e4m3x2((uint16_t)(v[k].x >> 16)),
+                         f16x2_of_e4m3x2((uint16_t)v[k].y), f16x2_of_e4m3x2((uint16_t)(v[k].y >> 16)));
+        }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor core reads them through it
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(&bar->vf_full[b]);
-        mbar_arrive(&bar->vk_empty[b]);
+        mbar_arrive(&bar->v8_empty[b]);
       }
     }
     __syncwarp();
@@ -440,190 +473,195 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const int full_hi = a.mask.causal ? min(pa + 1, n_keys) : n_keys;
     const int full_lo = a.mask.window > 0 ? pb - a.mask.window + 1 : 0;
 
+    auto known = [&] {
+      int n;
+      asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(n) : "r"(su32(&bar->n_info)) : "memory");
+      return n;
+    };
+    int n_info = 0;                                 // tiles whose numbers are known to be there
     for (int it = 0; ok; ++it) {
       const int j = kOne ? 2 * it + t : it;         // kOne: this warpgroup's key set is every other tile
       if (j >= nt) break;
-      if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
-      tc_fence_after();
+      // The tile's numbers, before its S is complete: they are mostly written many tiles ahead, at the latest with its K.
+      if (j >= n_info) {
+        n_info = known();
+        if (j >= n_info) {
+          if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
+          n_info = known();
+        }
+      }
       const ChunkInfo& ti = info[j & (kInfo - 1)];
-      const uint32_t ke = ti.ke, ve = ti.ve;
       const bool wild = ti.wild != 0;
       float rs = 1.0f;                              // what O has to be scaled by for the tile's reference
       if (!wild && ti.r != r) {
         rs = pow2_any(r - ti.r);
         r = ti.r;
       }
-      // of 32 keys: factor and summand of the exponent S + e_v - r + 7 - m, and 2^(r - e_v) for the row sum
-      auto factor = [&](int c) {
-        // (neither 0 nor infinite: masked logits are -inf, and codes may all be 0)
-        const float f = fminf(fmaxf(sl2 * pow2f(chunk_exp(ke, c)), 1e-37f), 3e38f);
-        return make_float2(f, f);
-      };
-      auto below = [&](int c) {                     // r - e_v
-        const int e = chunk_exp(ve, c);
-        return e == kZeroExp ? 0 : r - e;
-      };
+      // of 32 keys: factor and summand of the exponent S + e_v - r + 7 - m, and what the row sum takes of theirs
+      float fc[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c)                   // neither 0 nor infinite: masked logits are -inf, codes may all be 0
+        fc[c] = fminf(fmaxf(sl2 * ti.fk[c], 1e-37f), 3e38f);
+      auto factor = [&](int c) { return make_float2(fc[c], fc[c]); };
+      auto factor_at = [&](int c) { return fminf(fmaxf(sl2 * ti.fk[c], 1e-37f), 3e38f); };   // (c not a constant)
       auto summand = [&](int c) {
-        const float x = kShiftP - (float)below(c) - m;
+        const float x = ti.add[c] - m;
         return make_float2(x, x);
       };
       auto weighted = [&](const float2* ah, int c, float& plain) {   // 32 numerators' sum, and its share of l
         const float2 x = fadd2(fadd2(ah[0], ah[1]), fadd2(ah[2], ah[3]));
         plain += x.x + x.y;
-        return (x.x + x.y) * pow2f(below(c));
+        return (x.x + x.y) * ti.mul[c];
       };
-      const int key0 = tr.at(i0 + j) * kBN;
+      const int key0 = ti.key0;
       const bool full = trow1 < 0 || (key0 + kBN <= full_hi && (key0 >= full_lo || key0 + kBN <= a.mask.sinks));
-      // A tile goes in two parts, keys 0-95 and 96-127.  On full tiles after the first, P is computed with the running
-      // max m straight away; a part with a weight beyond 2^8 (2^15 as stored) is done again by general_part, which raises m.
-      // (O holds every key before part c0 once pva_done says so; rs: O's factor for a moved reference.)
-      auto general_part = [&](auto count, int c0, float rs) -> bool {
-        constexpr int kN = decltype(count)::count;
-        uint32_t sv[kN][32];
+      const bool direct = full && it > 0 && rs == 1.0f && !wild;   // uniform over the warpgroup
+      if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
+      tc_fence_after();
+      uint32_t ca[32], cb[32], ov = 0;
+      // A tile goes in two parts, keys 0-95 and 96-127 (a wild one 32 keys at a time).  On full tiles after the first, P is
+      // computed with the running max m straight away; a part with a weight beyond 2^8 (2^15 as stored) is
+      // done again with a max pass, which raises m.  One copy of that general path serves all parts: with one for each,
+      // the loop outgrew the instruction cache (480P chunk 716 -> 604 us without the wild tiles' copy).
+      const int parts = wild ? 4 : 2;
+#pragma unroll 1
+      for (int part = 0; part < parts; ++part) {
+        bool general = true;
+        if (direct) {
+          if (part == 0) {
+            uint32_t pk[48];
+            float plain = 0.0f, dl = 0.0f;
+            auto chunk = [&](const uint32_t* x, int c) {
+              float2 ah[4];
 #pragma unroll
-        for (int c = 0; c < kN; ++c) FK_TMEM_LD32(tS + (c0 + c) * 32, sv[c]);
+              for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
+              exp_chunk<PFormat::kF16>(x, factor(c), summand(c), ah, pk + 16 * c, ov);
+              dl += weighted(ah, c, plain);
+            };
+            FK_TMEM_LD32(tS, ca);
+            FK_TMEM_WAIT_LD32(ca);
+            FK_TMEM_LD32(tS + 32, cb);
+            chunk(ca, 0);
+            FK_TMEM_WAIT_LD32(cb);
+            FK_TMEM_LD32(tS + 64, ca);
+            chunk(cb, 1);
+            FK_TMEM_WAIT_LD32(ca);
+            FK_TMEM_LD32(tS + 96, cb);
+            chunk(ca, 2);
+            FK_TMEM_WAIT_LD32(cb);
+            general = __any_sync(0xffffffffu, plain > 32768.0f);   // (no numerator exceeds the sum) warp-uniform
+            if (!general) {
+              FK_TMEM_ST32(tS, pk);
+              FK_TMEM_ST16(tS + 32, (pk + 32));
+              l += dl;
+            }
+          } else {
+            uint32_t pk[16];
+            float2 ah[4];
+            float plain = 0.0f;
 #pragma unroll
-        for (int c = 0; c < kN; ++c) FK_TMEM_WAIT_LD32(sv[c]);
-        if (!full) {                                 // masked keys give 0
-#pragma unroll
-          for (int c = 0; c < kN; ++c) {
-            const int k0 = key0 + (c0 + c) * 32, hi = limit - k0, lo = lower - k0, si = a.mask.sinks - k0;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i >= hi || (i < lo && i >= si)) sv[c][i] = __float_as_uint(-INFINITY);
+            for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
+            exp_chunk<PFormat::kF16>(cb, factor(3), summand(3), ah, pk, ov);
+            const float dl = weighted(ah, 3, plain);
+            general = __any_sync(0xffffffffu, plain > 32768.0f);
+            if (!general) {
+              FK_TMEM_ST16(tS + 48, pk);
+              l += dl;
+            }
           }
         }
-        float mx = -INFINITY;
+        if (general) {
+          const int c0 = wild ? part : 3 * part, c1 = wild ? part + 1 : 3 + part;   // chunks of 32 keys
+          if (wild) {                                // at their own reference
+            const int e = chunk_exp(ti.ve, part), rn = e == kZeroExp ? r : e + kRefRoom;
+            rs = pow2_any(r - rn);
+            r = rn;
+          } else if (part > 0) {
+            rs = 1.0f;
+          }
+          auto load_chunk = [&](int c) {             // logits of a chunk, masked keys -inf
+            FK_TMEM_LD32(tS + c * 32, ca);
+            FK_TMEM_WAIT_LD32(ca);
+            if (!full) {
+              const int k0 = key0 + c * 32, hi = limit - k0, lo = lower - k0, si = a.mask.sinks - k0;
 #pragma unroll
-        for (int c = 0; c < kN; ++c) {
-          float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+              for (int i = 0; i < 32; ++i)
+                if (i >= hi || (i < lo && i >= si)) ca[i] = __float_as_uint(-INFINITY);
+            }
+          };
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int c = c0; c < c1; ++c) {
+            load_chunk(c);
+            float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 32; ++i) mxa[i & 3] = fmaxf(mxa[i & 3], __uint_as_float(sv[c][i]));
-          mx = fmaxf(mx, fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * factor(c0 + c).x);
-        }
-        const float m_new = fmaxf(m, mx);
-        const bool raise = __any_sync(0xffffffffu, m_new > m + kRescaleThreshold);   // warp-uniform
-        float alpha = rs;                            // 0 when m = kNoMax
-        if (raise) {
-          const float al = fast_exp2(m - m_new);
-          l *= al;
-          alpha *= al;
-          m = m_new;
-        }
-#pragma unroll
-        for (int c = 0; c < kN; ++c) {
-          uint32_t pk[16], ov = 0;
-          float2 ac[4];
-          float plain = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) ac[i] = make_float2(0.0f, 0.0f);
-          exp_chunk<PFormat::kF16>(sv[c], factor(c0 + c), summand(c0 + c), ac, pk, ov);
-          FK_TMEM_ST16(tS + (c0 + c) * 16, pk);
-          l += weighted(ac, c0 + c, plain);
-        }
-        if ((raise || rs != 1.0f) && (it > 0 || c0 > 0)) {
-          if (c0 > 0) {
-            if (!warp_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) return false;
-            tc_fence_after();
+            for (int i = 0; i < 32; ++i) mxa[i & 3] = fmaxf(mxa[i & 3], __uint_as_float(ca[i]));
+            mx = fmaxf(mx, fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * factor_at(c));
+          }
+          const float m_new = fmaxf(m, mx);
+          const bool raise = __any_sync(0xffffffffu, m_new > m + kRescaleThreshold);   // warp-uniform
+          if (raise) {
+            const float al = fast_exp2(m - m_new);   // 0 when m = kNoMax
+            l *= al;
+            rs *= al;
+            m = m_new;
           }
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            FK_TMEM_LD32(tO + c * 32, o);
-            FK_TMEM_WAIT_LD32(o);
+          for (int c = c0; c < c1; ++c) {            // (P's columns lie over logits already read)
+            load_chunk(c);
+            uint32_t pk[16];
+            float2 ac[4];
+            float plain = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-            FK_TMEM_ST32(tO + c * 32, o);
+            for (int i = 0; i < 4; ++i) ac[i] = make_float2(0.0f, 0.0f);
+            const float f = factor_at(c);
+            exp_chunk<PFormat::kF16>(ca, make_float2(f, f), summand(c), ac, pk, ov);
+            FK_TMEM_ST16(tS + c * 16, pk);
+            l += weighted(ac, c, plain);
+          }
+          if (__any_sync(0xffffffffu, rs != 1.0f) && (it > 0 || c0 > 0)) {   // O holds every key before chunk c0 ...
+            if (c0 > 0) {                            // ... once pva_done says so
+              if (!warp_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) { ok = false; break; }
+              tc_fence_after();
+            }
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              FK_TMEM_LD32(tO + c * 32, ca);
+              FK_TMEM_WAIT_LD32(ca);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) ca[e] = __float_as_uint(__uint_as_float(ca[e]) * rs);
+              FK_TMEM_ST32(tO + c * 32, ca);
+            }
+          }
+          if (direct && part == 0) {                 // (not kept across the general path)
+            FK_TMEM_LD32(tS + 96, cb);
+            FK_TMEM_WAIT_LD32(cb);
           }
         }
-        return true;
-      };
-      auto hand_over = [&](uint64_t* b) {            // P in TMEM -> the MMA warp
+        // P in TMEM -> the MMA warp
+        const bool more = wild || part == 0;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(b);
-      };
-      if (wild) {                                    // 32 keys at a time, each at its own reference
-#pragma unroll 1
-        for (int c = 0; c < 4 && ok; ++c) {
-          const int e = chunk_exp(ve, c), rn = e == kZeroExp ? r : e + kRefRoom;
-          const float f = pow2_any(r - rn);
-          r = rn;
-          ok = general_part(Chunks<0, 1>{}, c, f);
-          if (ok) hand_over(&bar->pa_full[t]);
-          ++n_pa;
-        }
-        if (!ok) break;
-        hand_over(&bar->p_full[t]);
-        continue;
+        if (lane == 0) mbar_arrive(more ? &bar->pa_full[t] : &bar->p_full[t]);
+        n_pa += more;
       }
-      const bool direct = full && it > 0 && rs == 1.0f;   // uniform over the warpgroup
-      uint32_t cb[32], ov = 0;
-      bool general = true;
-      if (direct) {
-        uint32_t ca[32], pk[48];
-        float plain = 0.0f, dl = 0.0f;
-        auto part = [&](const uint32_t* x, int c) {
-          float2 ah[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
-          exp_chunk<PFormat::kF16>(x, factor(c), summand(c), ah, pk + 16 * c, ov);
-          dl += weighted(ah, c, plain);
-        };
-        FK_TMEM_LD32(tS, ca);
-        FK_TMEM_WAIT_LD32(ca);
-        FK_TMEM_LD32(tS + 32, cb);
-        part(ca, 0);
-        FK_TMEM_WAIT_LD32(cb);
-        FK_TMEM_LD32(tS + 64, ca);
-        part(cb, 1);
-        FK_TMEM_WAIT_LD32(ca);
-        FK_TMEM_LD32(tS + 96, cb);
-        part(ca, 2);
-        FK_TMEM_WAIT_LD32(cb);
-        general = __any_sync(0xffffffffu, plain > 32768.0f);   // (no numerator exceeds the sum) warp-uniform
-        if (!general) {
-          FK_TMEM_ST32(tS, pk);
-          FK_TMEM_ST16(tS + 32, (pk + 32));
-          l += dl;
-        }
+      if (!ok) break;
+      if (wild) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar->p_full[t]);
       }
-      if (general) {
-        if (!general_part(Chunks<0, 3>{}, 0, rs)) { ok = false; break; }
-        if (direct) {                                // (not kept across the general path)
-          FK_TMEM_LD32(tS + 96, cb);
-          FK_TMEM_WAIT_LD32(cb);
-        }
-      }
-      hand_over(&bar->pa_full[t]);
-      ++n_pa;
-      general = true;
-      if (direct) {
-        uint32_t pk[16];
-        float2 ah[4];
-        float plain = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
-        exp_chunk<PFormat::kF16>(cb, factor(3), summand(3), ah, pk, ov);
-        const float dl = weighted(ah, 3, plain);
-        general = __any_sync(0xffffffffu, plain > 32768.0f);
-        if (!general) {
-          FK_TMEM_ST16(tS + 48, pk);
-          l += dl;
-        }
-      }
-      if (general && !general_part(Chunks<0, 1>{}, 3, 1.0f)) { ok = false; break; }
-      hand_over(&bar->p_full[t]);
     }
     // ---------------------------------------------------------------- epilogue
     // every MMA is done, so the operand tiles' shared memory is free
     ok = ok && warp_wait(&bar->o_done, 0, bar, a.status);
     tc_fence_after();
     const bool has = kOne ? t < nt : nt > 0;        // this accumulator was written
+    const int row0 = bar->row0, rows = bar->rows, kvh = bar->kvh, n_splits = bar->n_splits;
+    const int64_t q0 = a.seqs.q0[bar->seq];
     auto out_row = [&](int r) {                      // row r of the CTA
       const int q = row0 + r;
-      return a.O + ((int64_t)a.seqs.q0[s] + q / a.G) * a.ostride + (int64_t)(kvh * a.G + q % a.G) * D;
+      return a.O + (q0 + q / a.G) * a.ostride + (int64_t)(kvh * a.G + q % a.G) * D;
     };
     // (r is that of the last tile, or of the tile's last block: the same for all threads of an accumulator)
     if (!kOne && n_splits == 1) {
@@ -679,7 +717,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       asm volatile("bar.sync 1, 256;" ::: "memory");
       constexpr int kRuns = D / 4;
       const float* base = reinterpret_cast<const float*>(smem);
-      const int slot0 = a.seqs.part0[s] + (item - whole) * kTiles;          // workspace tiles of this CTA
+      const int slot0 = bar->slot0, split = bar->split;
       float4* part = reinterpret_cast<float4*>(a.part);
       float4* mls = part + (int64_t)a.part_tiles * kBM * kRuns;
       for (int i = threadIdx.x; i < rows * kRuns; i += 256) {
@@ -714,29 +752,46 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         asm volatile("bar.sync 1, 256;" ::: "memory");
         if (bar->last) {
           __threadfence();
-          for (int i = threadIdx.x; i < rows * kRuns; i += 256) {
-            const int r = i / kRuns, c = i % kRuns;
-            float M = kNoMax, R = kNoRef, L = 0.0f;
-            for (int sp = 0; sp < n_splits; ++sp) {
-              const float4 e = __ldcg(mls + (int64_t)(first + sp * kTiles) * kBM + r);
-              M = fmaxf(M, e.x);
-              R = fmaxf(R, e.z);
+          // a thread's places are 256 apart: the same run of every (256 / kRuns)-th row, four rows in flight
+          constexpr int kStep = 256 / kRuns, kFly = 4;
+          const int c = threadIdx.x % kRuns;
+          for (int r0 = threadIdx.x / kRuns; r0 < rows; r0 += kStep * kFly) {
+            float M[kFly], R[kFly], L[kFly];
+            float4 acc[kFly];
+#pragma unroll
+            for (int k = 0; k < kFly; ++k) {
+              M[k] = kNoMax;
+              R[k] = kNoRef;
+              L[k] = 0.0f;
+              acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
-            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
             for (int sp = 0; sp < n_splits; ++sp) {
-              const float4 e = __ldcg(mls + (int64_t)(first + sp * kTiles) * kBM + r);
-              const float4 x = __ldcg(part + ((int64_t)(first + sp * kTiles) * kBM + r) * kRuns + c);
-              const float f = fast_exp2(e.x - M), fo = f * pow2_any((int)(e.z - R));
-              L = fmaf(f, e.y, L);
-              acc.x = fmaf(fo, x.x, acc.x);
-              acc.y = fmaf(fo, x.y, acc.y);
-              acc.z = fmaf(fo, x.z, acc.z);
-              acc.w = fmaf(fo, x.w, acc.w);
+              float4 e[kFly], x[kFly];
+#pragma unroll
+              for (int k = 0; k < kFly; ++k) {
+                const int64_t at = (int64_t)(first + sp * kTiles) * kBM + min(r0 + k * kStep, rows - 1);
+                e[k] = __ldcg(mls + at);
+                x[k] = __ldcg(part + at * kRuns + c);
+              }
+#pragma unroll
+              for (int k = 0; k < kFly; ++k) {        // joined one by one, as the key sets above
+                const float M2 = fmaxf(M[k], e[k].x), R2 = fmaxf(R[k], e[k].z), w0 = fast_exp2(M[k] - M2), w1 = fast_exp2(e[k].x - M2);
+                const float v0 = w0 * pow2_any((int)(R[k] - R2)), v1 = w1 * pow2_any((int)(e[k].z - R2));
+                L[k] = fmaf(L[k], w0, e[k].y * w1);
+                acc[k] = make_float4(fmaf(acc[k].x, v0, x[k].x * v1), fmaf(acc[k].y, v0, x[k].y * v1),
+                                     fmaf(acc[k].z, v0, x[k].z * v1), fmaf(acc[k].w, v0, x[k].w * v1));
+                M[k] = M2;
+                R[k] = R2;
+              }
             }
-            const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;
-            *reinterpret_cast<uint2*>(out_row(r) + 4 * c) =
-                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+#pragma unroll
+            for (int k = 0; k < kFly; ++k) {
+              const int r = r0 + k * kStep;
+              const float inv = L[k] > 0.0f || L[k] != L[k] ? pow2_any((int)R[k]) / L[k] : 0.0f;
+              if (r < rows)
+                *reinterpret_cast<uint2*>(out_row(r) + 4 * c) =
+                    make_uint2(pack_bf16(acc[k].x * inv, acc[k].y * inv), pack_bf16(acc[k].z * inv, acc[k].w * inv));
+            }
           }
         }
       }

@@ -218,7 +218,21 @@ bool plan_chunk(const fk_paged* h, PagedAttnArgs* a) {
     work += (int64_t)tiles[k] * items[k];
     total += items[k];
   }
-  const int64_t per = total >= h->sms ? INT32_MAX : std::max<int64_t>(2, (work + h->sms - 1) / h->sms);
+  // Key splits, one CTA to an SM: of everything where the items do not fill the device; else, with one sequence
+  // whose items take about as long, of those left over after the last whole wave.
+  int64_t per = INT32_MAX;
+  if (total < h->sms) {
+    per = std::max<int64_t>(2, (work + h->sms - 1) / h->sms);
+  } else if (s.n == 1 && !a->mask.causal && total % h->sms && total < 8 * h->sms) {
+    const int rest = (int)(total % h->sms), splits = std::min<int>(tiles[0] / 2, std::max(1, h->sms / rest));
+    if (splits > 1 && (int64_t)splits * rest * (rows / kAttnBM) <= h->part_tiles) {
+      s.item0[0] = s.part0[0] = 0;
+      s.splits[0] = splits;
+      s.whole[0] = items[0] - rest;
+      s.item0[1] = s.whole[0] + rest * splits;
+      return one;
+    }
+  }
   int item = 0, part = 0;
   for (int k = 0; k < s.n; ++k) {
     int splits = (int)std::max<int64_t>(1, (tiles[k] + per - 1) / per);
