@@ -114,6 +114,18 @@ __host__ __device__ inline TileRange paged_tiles(int n_keys, int p0, int p1, con
   return r;
 }
 
+// Division of 0 .. 2^31 - 1 by a number that the host knows: q = (umulhi(n, mul) + n) >> shift.
+struct FastDiv {
+  uint32_t d, mul, shift;
+  explicit FastDiv(uint32_t div = 1) : d(div), mul(0), shift(0) {
+    while (((uint64_t)1 << shift) < d) ++shift;
+    mul = (uint32_t)(((((uint64_t)1 << shift) - d) << 32) / d + 1);
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+#endif
+};
+
 struct PagedAttnSeqs {
   int n;
   int slot[kStepSeqs];
@@ -131,6 +143,7 @@ struct PagedAttnArgs {
   const int8_t* ke;
   const int8_t* ve;
   int max_pages, Hkv, G, P;
+  FastDiv by_g;                       // query row -> query (row = query * G + head of the group)
   const bf16* Q;                      // [T][Hkv G][D]
   bf16* O;
   int64_t qstride, ostride;

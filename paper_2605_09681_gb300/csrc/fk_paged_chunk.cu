@@ -44,7 +44,8 @@ struct ChunkInfo {                                 // of a key tile
   float fk[4], add[4], mul[4];
 };
 struct ChunkBarriers {
-  uint64_t q_ready;
+  uint64_t q_full, q_ready;         // query rows staged (where f16 values go later); their codes written
+  uint64_t info_ready;              // the first 32 tiles' numbers
   uint64_t k_full[kKStages], k_empty[kKStages];
   uint64_t v8_full[2], v8_empty[2]; // V codes
   uint64_t vf_full[2], vf_empty[2]; // f16 values
@@ -80,20 +81,19 @@ struct ChunkLayout {
 // exponent of chunk c (32 keys) of four packed ones
 __device__ __forceinline__ int chunk_exp(uint32_t packed, int c) { return (int)(int8_t)(packed >> (8 * c)); }
 
-// hi = E4M3(x), lo = E4M3(x - hi) of 16 scaled query elements
-__device__ __forceinline__ void split16(const float* x, uint4& hi, uint4& lo) {
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = e4m3x2(x[4 * i], x[4 * i + 1]), b = e4m3x2(x[4 * i + 2], x[4 * i + 3]);
-    const uint32_t fa = f16x2_of_e4m3x2((uint16_t)a), fb = f16x2_of_e4m3x2((uint16_t)b);
-    const float2 ya = __half22float2(*reinterpret_cast<const __half2*>(&fa));
-    const float2 yb = __half22float2(*reinterpret_cast<const __half2*>(&fb));
-    h[i] = a | (b << 16);
-    l[i] = e4m3x2(x[4 * i] - ya.x, x[4 * i + 1] - ya.y) | (e4m3x2(x[4 * i + 2] - yb.x, x[4 * i + 3] - yb.y) << 16);
-  }
-  hi = make_uint4(h[0], h[1], h[2], h[3]);
-  lo = make_uint4(l[0], l[1], l[2], l[3]);
+// Two bf16 query elements times `scale` (at most 448) as f16, x = hi + lo: E4M3 codes of both parts.  hi has the leading
+// four bits of each element and lo the rest (a bf16 has eight).
+__device__ __forceinline__ uint16_t e4m3x2_of_f16x2(uint32_t x) {
+  uint16_t c;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
+  return c;
+}
+__device__ __forceinline__ void split2(uint32_t w, float scale, uint16_t& hi, uint16_t& lo) {
+  const uint32_t x = pack_f16(__uint_as_float(w << 16) * scale, __uint_as_float(w & 0xFFFF0000u) * scale);
+  hi = e4m3x2_of_f16x2(x);
+  const uint32_t h = f16x2_of_e4m3x2(hi);
+  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&h));
+  lo = e4m3x2_of_f16x2(*reinterpret_cast<const uint32_t*>(&d));
 }
 // byte offset of 16-byte run c of row `row` in a tile of D-byte rows (the TMA's and the MMA's swizzle)
 template <int D>
@@ -139,7 +139,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   const int kvh = pair % a.Hkv, row0 = (groups - 1 - pair / a.Hkv) * (kTiles * kBM);
   const int rows = min(kTiles * kBM, n_rows - row0);
   const int p_first = n_keys - n_q;
-  const TileRange tr = paged_tiles(n_keys, p_first + row0 / a.G, p_first + (row0 + rows - 1) / a.G, a.mask, kBN);
+  const TileRange tr = paged_tiles(n_keys, p_first + a.by_g.div(row0), p_first + a.by_g.div(row0 + rows - 1), a.mask, kBN);
   const int n_tiles = tr.count();
   const int i0 = (int)((int64_t)n_tiles * split / n_splits);
   const int nt = (int)((int64_t)n_tiles * (split + 1) / n_splits) - i0;        // may be 0
@@ -154,60 +154,83 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     __syncwarp();
     load(&tmK, sK + st * Lay::kK, j, &bar->k_full[st]);
   };
-  // pages, exponents and references of key tiles j0 + lane (a warp)
-  int ref[2] = {kNoRef, kNoRef};                    // of the last tile (kOne: of each key set)
-  auto fetch_info = [&](int j0) {
+  // Key tiles j0 + lane (a warp): their pages, and then, which the loads need not wait for, exponents and references.
+  int pages[4] = {0, 0, 0, 0};                      // of each 32 keys
+  auto fetch_pages = [&](int j0) {
     const int j = j0 + lane;
-    int lo = 127, hi = -127, last = kNoRef;         // of the tile's blocks that are not zeros
-    ChunkInfo x;
-    x.ve = 0;
-    float fk[4] = {1.0f, 1.0f, 1.0f, 1.0f};
     if (j < nt) {
       const int* table = a.table + (int64_t)a.seqs.slot[s] * a.max_pages;
       const int last_page = max(n_keys - 1, 0) / a.P, key0 = tr.at(i0 + j) * kBN;
+      ChunkInfo& x = info[j & (kInfo - 1)];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {                 // 32 keys each
-        const int key = key0 + 32 * c, page = __ldg(table + min(key / a.P, last_page));
-        const int64_t block = (int64_t)page * a.Hkv + kvh;
-        fk[c] = pow2f(a.ke[block]);
-        const int ev = a.ve[block];
-        x.ve |= (uint32_t)(uint8_t)ev << (8 * c);
-        if (ev != kZeroExp) {
-          lo = min(lo, ev);
-          hi = max(hi, ev);
-          last = ev;
-        }
-        const int y = (page * a.Hkv + kvh) * a.P + key % a.P;
+      for (int c = 0; c < 4; ++c) pages[c] = __ldg(table + min((key0 + 32 * c) / a.P, last_page));
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int y = (pages[c] * a.Hkv + kvh) * a.P + (key0 + 32 * c) % a.P;
         if (boxes == 4) x.y[c] = y;
         else if ((c & 1) == 0) x.y[c >> 1] = y;
       }
     }
-    x.wild = hi - lo > kRefWindow - kRefRoom;
-    x.r = 0;
+    __syncwarp();
+  };
+  int ref[2] = {kNoRef, kNoRef};                    // of the last tile (kOne: of each key set)
+  auto fetch_exps = [&](int j0) {
+    const int j = j0 + lane;
+    int lo = 127, hi = -127, last = kNoRef, ev[4];  // of the tile's blocks that are not zeros
+    float fk[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    bool wild = false;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) ev[c] = kZeroExp;
+    if (j < nt) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int64_t block = (int64_t)pages[c] * a.Hkv + kvh;
+        fk[c] = pow2f(a.ke[block]);
+        ev[c] = a.ve[block];
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (ev[c] != kZeroExp) {
+          lo = min(lo, ev[c]);
+          hi = max(hi, ev[c]);
+          last = ev[c];
+        }
+      wild = hi - lo > kRefWindow - kRefRoom;
+    }
+    int mine = kNoRef;
     for (int i = 0; i < min(32, nt - j0); ++i) {    // the references, tile by tile
       int r = kOne && (i & 1) ? ref[1] : ref[0];
       const int thi = __shfl_sync(0xffffffffu, hi, i), tlo = __shfl_sync(0xffffffffu, lo, i);
-      const int tlast = __shfl_sync(0xffffffffu, last, i), tw = __shfl_sync(0xffffffffu, x.wild, i);
+      const int tlast = __shfl_sync(0xffffffffu, last, i), tw = __shfl_sync(0xffffffffu, (int)wild, i);
       if (tlast != kNoRef && (tw || thi > r || tlo < r - kRefWindow)) r = (tw ? tlast : thi) + kRefRoom;
       (kOne && (i & 1) ? ref[1] : ref[0]) = r;
-      if (lane == i) x.r = r;
+      if (lane == i) mine = r;
     }
+    if (j < nt) {
+      ChunkInfo& x = info[j & (kInfo - 1)];
+      x.r = mine;
+      x.wild = wild;
+      x.key0 = tr.at(i0 + j) * kBN;
+      uint32_t ve = 0;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int e = chunk_exp(x.ve, c), below = e == kZeroExp ? 0 : x.wild ? kRefRoom : x.r - e;
-      x.fk[c] = fk[c];
-      x.add[c] = kShiftP - (float)below;
-      x.mul[c] = pow2_any(below);
+      for (int c = 0; c < 4; ++c) {
+        const int below = ev[c] == kZeroExp ? 0 : wild ? kRefRoom : mine - ev[c];
+        ve |= (uint32_t)(uint8_t)ev[c] << (8 * c);
+        x.fk[c] = fk[c];
+        x.add[c] = kShiftP - (float)below;
+        x.mul[c] = pow2_any(below);
+      }
+      x.ve = ve;
     }
-    x.key0 = j < nt ? tr.at(i0 + j) * kBN : 0;
-    if (j < nt) info[j & (kInfo - 1)] = x;
     __syncwarp();
     if (lane == 0) asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" :: "r"(su32(&bar->n_info)), "r"(j0 + 32) : "memory");
   };
 
   if (warp == kWarpTma) {
     if (lane == 0) {
-      mbar_init(&bar->q_ready, kTiles * kBM);
+      mbar_init(&bar->q_full, 1);
+      mbar_init(&bar->q_ready, 8);
+      mbar_init(&bar->info_ready, 1);
       for (int i = 0; i < kKStages; ++i) {
         mbar_init(&bar->k_full[i], 1);
         mbar_init(&bar->k_empty[i], 1);
@@ -236,8 +259,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    fetch_info(0);
-    for (int j = 0; j < min(2, nt); ++j) load_k(j);
+    if (nt > 0) {
+      // the query rows, bf16, as they lie: a run of rows for each query (the group's heads lie together)
+      if (lane == 0) mbar_expect_tx(&bar->q_full, (uint32_t)rows * D * 2);
+      __syncwarp();
+      const int tok0 = a.by_g.div(row0), tok1 = a.by_g.div(row0 + rows - 1);
+      for (int tok = tok0 + lane; tok <= tok1; tok += 32) {
+        const int ra = max(tok * a.G, row0), rb = min((tok + 1) * a.G, row0 + rows);
+        bulk_load(sV + (ra - row0) * (D * 2), a.Q + ((int64_t)a.seqs.q0[s] + tok) * a.qstride + (int64_t)(kvh * a.G + ra - tok * a.G) * D,
+                  (uint32_t)(rb - ra) * D * 2, &bar->q_full);
+      }
+      __syncwarp();
+    }
   }
   __syncwarp();
   if (warp == kWarpMma) {
@@ -261,6 +294,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   if (warp == kWarpTma) {
     // ------------------------------------------------------------------ TMA producer
     // V_j, then K_{j+2} (K_0 and K_1 are under way)
+    fetch_pages(0);
+    for (int j = 0; j < min(2, nt); ++j) load_k(j);
     int jv = -1, jk = min(2, nt) - 1;               // last tiles issued
     for (int j = 0; j < nt; ++j) {
       const int b = j & 1;
@@ -269,13 +304,21 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       __syncwarp();
       load(&tmV, sV8 + b * Lay::kK, j, &bar->v8_full[b]);
       jv = j;
+      if (j == 0) {
+        fetch_exps(0);
+        if (lane == 0) mbar_arrive(&bar->info_ready);
+      }
       if (j + 2 >= nt) continue;
-      if (((j + 2) & 31) == 0) fetch_info(j + 2);
+      if (((j + 2) & 31) == 0) {
+        fetch_pages(j + 2);
+        fetch_exps(j + 2);
+      }
       if (j + 2 >= kKStages && !warp_wait(&bar->k_empty[(j + 2) % kKStages], ((j + 2) / kKStages - 1) & 1, bar, a.status)) { ok = false; break; }
       load_k(j + 2);
       jk = j + 2;
     }
     if (!ok) {                                      // what was issued lands before the CTA ends
+      wait_phase(&bar->q_full, 0, bar, a.status, false);
       for (int j = max(0, jk - kKStages + 1); j <= jk; ++j) wait_phase(&bar->k_full[j % kKStages], (j / kKStages) & 1, bar, a.status, false);
       for (int j = max(0, jv - 1); j <= jv; ++j) wait_phase(&bar->v8_full[j & 1], (j >> 1) & 1, bar, a.status, false);
     }
@@ -324,7 +367,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           umma_commit(&bar->k_empty[0]);
         }
       }
-      ok = ok && wait(&bar->vf_full[0], 0);
+      ok = ok && wait(&bar->info_ready, 0) && wait(&bar->vf_full[0], 0);
       if (kOne && nt > 1 && ok) {
         ok = k_ready(1);
         if (ok && elect_one()) {
@@ -387,6 +430,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     // ------------------------------------------------------------------ V codes -> f16 values
     // A thread takes 8 codes of a row at a time: half a 16-byte run, one 16-byte unit of the f16 row.
     constexpr int kOct = D / 8, kStepRows = 64 / kOct, kFly = 8;   // units of a row; rows per pass; loads in flight
+    ok = nt == 0 || warp_wait(&bar->q_ready, 0, bar, a.status);   // (the query rows were staged where the values go)
     const int x = threadIdx.x - kWarpConv * 32, prow = x / kOct, unit = x % kOct;
     for (int j = 0; j < nt && ok; ++j) {
       const int b = j & 1, u = j >> 1;
@@ -425,51 +469,52 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const uint32_t tO = tmem + lane_base + kColO + (uint32_t)(t * D);
     const int crow = (kOne ? 0 : t * kBM) + row;    // row of the CTA
     const bool in = crow < rows;
-    const int rr = row0 + (in ? crow : 0), pos = p_first + rr / a.G;
+    const int pos = p_first + a.by_g.div(row0 + (in ? crow : 0));
     float sl2 = a.scale_log2;
-    // this row of Q: scaled to E4M3's range, hi and lo in the MMA's layout (kOne: both key sets want the scale)
-    {
-      const uint4* src = reinterpret_cast<const uint4*>(a.Q + ((int64_t)a.seqs.q0[s] + rr / a.G) * a.qstride +
-                                                        (int64_t)(kvh * a.G + rr % a.G) * D);
-      uint4 v[D / 8];
-#pragma unroll
-      for (int j = 0; j < D / 8; ++j) v[j] = in ? __ldg(src + j) : make_uint4(0, 0, 0, 0);
-      float amax = 0.0f;
-#pragma unroll
-      for (int j = 0; j < D / 8; ++j) amax = fmaxf(amax, absmax8(v[j]));
-      const int e = e4m3_row_exponent(amax);
-      const float inv = pow2f(-e);
-      uint8_t* hi = sQ + (kOne ? 0 : t) * (2 * Lay::kQ);
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t w[4] = {v[2 * c + i].x, v[2 * c + i].y, v[2 * c + i].z, v[2 * c + i].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            x[8 * i + 2 * k] = __uint_as_float(w[k] << 16) * inv;
-            x[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u) * inv;
-          }
-        }
-        if (!kOne || t == 0) {
-          uint4 h4, l4;
-          split16(x, h4, l4);
-          *reinterpret_cast<uint4*>(hi + code_run<D>(row, c)) = h4;
-          *reinterpret_cast<uint4*>(hi + Lay::kQ + code_run<D>(row, c)) = l4;
-        }
+    // The thread's row of Q from the staged rows: scaled to E4M3's range, hi and lo in the MMA's layout.  16-byte chunks in
+    // an order of the row's own (j ^ row), so that the rows of a warp meet few banks.  (kOne: both key sets
+    // want the scale.)  Loading rows from global memory a warp at a time, with the maximum by shuffles, took
+    // 12000-58000 cycles: the shuffles waited for the loads in flight.
+    if (nt > 0) {
+      ok = warp_wait(&bar->q_full, 0, bar, a.status);
+      const uint8_t* src = sV + crow * (D * 2);
+      uint32_t top = 0;
+#pragma unroll 4
+      for (int j = 0; j < D / 8; ++j) {
+        const uint4 v = *reinterpret_cast<const uint4*>(src + ((j ^ (row & 7)) << 4));
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
       }
-      sl2 *= pow2f(e);
+      top = in ? max(top & 0xFFFFu, top >> 16) : 0;        // as bf16 bits; rows past the end were not loaded
+      const bool fine = top < 0x7F80u;
+      const int e = fine ? e4m3_row_exponent(__uint_as_float(top << 16)) : 0;
       if (!kOne || t == 0) {
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(&bar->q_ready);
+        const float scale = in ? pow2f(-e) : 0.0f;
+        uint8_t* dst = sQ + (kOne ? 0 : t) * (2 * Lay::kQ);
+#pragma unroll 2
+        for (int j = 0; j < D / 8; ++j) {
+          const int c = j ^ (row & 7);
+          const uint4 v = in ? *reinterpret_cast<const uint4*>(src + (c << 4)) : make_uint4(0, 0, 0, 0);
+          uint16_t h[4], g[4];
+          split2(v.x, scale, h[0], g[0]);
+          split2(v.y, scale, h[1], g[1]);
+          split2(v.z, scale, h[2], g[2]);
+          split2(v.w, scale, h[3], g[3]);
+          uint8_t* to = dst + code_run<D>(row, c >> 1) + (c & 1) * 8;
+          *reinterpret_cast<uint2*>(to) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+          *reinterpret_cast<uint2*>(to + Lay::kQ) = make_uint2(g[0] | (uint32_t)g[1] << 16, g[2] | (uint32_t)g[3] << 16);
+        }
       }
+      if (fine) sl2 *= pow2f(e);
+      else l = NAN;                                 // infinities or NaN: the row's O is NaN
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar->q_ready);
     }
     // visible keys: [lower, limit) and those below the sinks; tiles without a masked key for any of the tile's rows
     const int limit = a.mask.causal ? min(pos + 1, n_keys) : n_keys;
     const int lower = a.mask.window > 0 ? pos - a.mask.window + 1 : 0;
     const int trow1 = min(kOne ? rows : rows - t * kBM, kBM) - 1;   // last row of this query tile
-    const int pa = p_first + (row0 + (kOne ? 0 : t * kBM)) / a.G, pb = p_first + (row0 + (kOne ? 0 : t * kBM) + max(trow1, 0)) / a.G;
+    const int trow0 = row0 + (kOne ? 0 : t * kBM), pa = p_first + a.by_g.div(trow0), pb = p_first + a.by_g.div(trow0 + max(trow1, 0));
     const int full_hi = a.mask.causal ? min(pa + 1, n_keys) : n_keys;
     const int full_lo = a.mask.window > 0 ? pb - a.mask.window + 1 : 0;
 
@@ -479,10 +524,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       return n;
     };
     int n_info = 0;                                 // tiles whose numbers are known to be there
+    if (nt > 0) ok = warp_wait(&bar->info_ready, 0, bar, a.status);
     for (int it = 0; ok; ++it) {
       const int j = kOne ? 2 * it + t : it;         // kOne: this warpgroup's key set is every other tile
       if (j >= nt) break;
-      // The tile's numbers, before its S is complete: they are mostly written many tiles ahead, at the latest with its K.
+      // The tile's numbers, before its S is complete: they are mostly written many tiles ahead, at the latest before its K is
+      // loaded (the first 32 tiles': info_ready).
       if (j >= n_info) {
         n_info = known();
         if (j >= n_info) {
@@ -494,7 +541,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       const bool wild = ti.wild != 0;
       float rs = 1.0f;                              // what O has to be scaled by for the tile's reference
       if (!wild && ti.r != r) {
-        rs = pow2_any(r - ti.r);
+        if (it > 0) rs = pow2_any(r - ti.r);
         r = ti.r;
       }
       // of 32 keys: factor and summand of the exponent S + e_v - r + 7 - m, and what the row sum takes of theirs
@@ -515,11 +562,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       };
       const int key0 = ti.key0;
       const bool full = trow1 < 0 || (key0 + kBN <= full_hi && (key0 >= full_lo || key0 + kBN <= a.mask.sinks));
-      const bool direct = full && it > 0 && rs == 1.0f && !wild;   // uniform over the warpgroup
+      bool direct = full && it > 0 && rs == 1.0f && !wild;   // uniform over the warpgroup
       if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
       tc_fence_after();
       uint32_t ca[32], cb[32], ov = 0;
-      // A tile goes in two parts, keys 0-95 and 96-127 (a wild one 32 keys at a time).  On full tiles after the first, P is
+      if (it == 0 && full && !wild) {               // the first tile: m from its first 32 keys
+        FK_TMEM_LD32(tS, ca);
+        FK_TMEM_WAIT_LD32(ca);
+        float mxa[4] = {kNoMax, kNoMax, kNoMax, kNoMax};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mxa[i & 3] = fmaxf(mxa[i & 3], __uint_as_float(ca[i]));
+        m = fmaxf(fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * fc[0], kNoMax);
+        direct = true;
+      }
+      // A tile goes in two parts, keys 0-95 and 96-127 (a wild one 32 keys at a time).  On full tiles, P is
       // computed with the running max m straight away; a part with a weight beyond 2^8 (2^15 as stored) is
       // done again with a max pass, which raises m.  One copy of that general path serves all parts: with one for each,
       // the loop outgrew the instruction cache (480P chunk 716 -> 604 us without the wild tiles' copy).
@@ -660,8 +716,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const int row0 = bar->row0, rows = bar->rows, kvh = bar->kvh, n_splits = bar->n_splits;
     const int64_t q0 = a.seqs.q0[bar->seq];
     auto out_row = [&](int r) {                      // row r of the CTA
-      const int q = row0 + r;
-      return a.O + (q0 + q / a.G) * a.ostride + (int64_t)(kvh * a.G + q % a.G) * D;
+      const int q = row0 + r, tok = a.by_g.div(q);
+      return a.O + (q0 + tok) * a.ostride + (int64_t)(kvh * a.G + q - tok * a.G) * D;
     };
     // (r is that of the last tile, or of the tile's last block: the same for all threads of an accumulator)
     if (!kOne && n_splits == 1) {
@@ -690,7 +746,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         __syncwarp();
         constexpr int kLanes = D / 8;               // lanes of one row
         const int cl = lane % kLanes;
-#pragma unroll
+#pragma unroll 2
         for (int r0 = 0; r0 < 32; r0 += 32 / kLanes) {
           const int r = r0 + lane / kLanes, cr = t * kBM + wq * 32 + r;
           const uint4 v = *reinterpret_cast<const uint4*>(stage + r * (D * 2) + ((cl ^ (r & (D / 8 - 1))) << 4));

@@ -93,7 +93,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const int split = item % n_splits, row0 = (item / n_splits) * kRows;
   const int rows = min(kRows, n_rows - row0);
   const int p_first = n_keys - n_q;                    // position of query 0
-  const int pos0 = p_first + row0 / a.G, pos1 = p_first + (row0 + rows - 1) / a.G;
+  const int pos0 = p_first + a.by_g.div(row0), pos1 = p_first + a.by_g.div(row0 + rows - 1);
   const TileRange tr = paged_tiles(n_keys, pos0, pos1, a.mask, kT);
   const int n_tiles = tr.count();
   const int i0 = (int)((int64_t)n_tiles * split / n_splits), i1 = (int)((int64_t)n_tiles * (split + 1) / n_splits);
@@ -177,10 +177,10 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     for (int h = 0; h < 2; ++h) {
       const int row = g + 8 * h;
       const bool in = row < rows;
-      const int rr = row0 + (in ? row : 0), pos = p_first + rr / a.G;
+      const int rr = row0 + (in ? row : 0), tok = a.by_g.div(rr), pos = p_first + tok;
       limit[h] = !in ? 0 : a.mask.causal ? min(pos + 1, n_keys) : n_keys;
       lower[h] = a.mask.window > 0 ? pos - a.mask.window + 1 : 0;
-      const bf16* src = a.Q + ((int64_t)a.seqs.q0[s] + rr / a.G) * a.qstride + (int64_t)(kvh * a.G + rr % a.G) * D;
+      const bf16* src = a.Q + ((int64_t)a.seqs.q0[s] + tok) * a.qstride + (int64_t)(kvh * a.G + rr - tok * a.G) * D;
       uint4 v[D / 32];
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
@@ -192,6 +192,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       for (int c = 0; c < D / 32; ++c) amax = fmaxf(amax, absmax8(v[c]));
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      if (!(amax <= 3.402823466e38f)) l[h] = NAN;       // infinities (NaN makes its own way)
       const int e = e4m3_row_exponent(amax);
       const float inv = pow2f(-e);
       sc[h] = a.scale_log2 * pow2f(e);
@@ -352,8 +353,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const int cta = a.seqs.part0[s] + kvh * (a.seqs.item0[s + 1] - a.seqs.item0[s]) + item;   // workspace slot
   constexpr int kRuns = D / 4;
   auto out_row = [&](int row) {
-    const int rr = row0 + row;
-    return a.O + ((int64_t)a.seqs.q0[s] + rr / a.G) * a.ostride + (int64_t)(kvh * a.G + rr % a.G) * D;
+    const int rr = row0 + row, tok = a.by_g.div(rr);
+    return a.O + ((int64_t)a.seqs.q0[s] + tok) * a.ostride + (int64_t)(kvh * a.G + rr - tok * a.G) * D;
   };
   float* part = a.part + (int64_t)cta * kRows * D;
   float4* mls = reinterpret_cast<float4*>(a.part + (int64_t)kPartSlots * kRows * D);   // m, l, r

@@ -500,6 +500,7 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
     a->Hkv = c.n_kv_heads;
     a->G = c.n_q_heads / c.n_kv_heads;
     a->P = c.page_tokens;
+    a->by_g = FastDiv((uint32_t)a->G);
     a->Q = static_cast<const bf16*>(Q);
     a->O = static_cast<bf16*>(O);
     a->qstride = q_stride;
