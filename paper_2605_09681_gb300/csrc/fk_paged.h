@@ -6,9 +6,10 @@
 namespace fk {
 
 constexpr int kStepSeqs = 256;        // sequences of one launch (their numbers travel by value)
-constexpr int kPagedFewRows = 16;     // query rows of one warp-level MMA tile
+constexpr int kPagedFewRows = 16;     // query rows of a CTA of the few-row kernel, at most
 constexpr int kPagedFewTile = 64;     // keys per tile of the few-row kernel
 
+constexpr int kMaxFewSplits = 480;    // key splits of a row of the few-row kernel
 constexpr int kPartSlots = 1024;      // CTAs of a launch that share their rows with other key splits, at most
 
 // Stored exponent of a block of zeros (others are at least -120).
@@ -157,8 +158,8 @@ struct PagedAttnArgs {
   int* status;
   PagedAttnSeqs seqs;
 };
-// At most kPagedFewRows query rows (query, head of the group) per CTA, any number of keys.
-cudaError_t launch_paged_few(int D, const CUtensorMap& tmK, const CUtensorMap& tmV, const PagedAttnArgs& a,
+// 8 row_tiles (1 or 2) query rows (query, head of the group) per CTA, any number of keys.
+cudaError_t launch_paged_few(int D, int row_tiles, const CUtensorMap& tmK, const CUtensorMap& tmV, const PagedAttnArgs& a,
                              cudaStream_t s);
 cudaError_t paged_few_prepare(int D);
 // Any number of query rows, 256 per CTA (one_tile: 128).

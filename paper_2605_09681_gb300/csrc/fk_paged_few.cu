@@ -2,18 +2,22 @@
 // bound it, so the keys are split over as many CTAs as the device holds and every byte is loaded once.
 //   S = q k^T 2^(e_q + e_k) log2(e) scale,  p = 2^(S - m),  l = sum p,  O = 2^r sum p 2^(e_v - r) v / l
 // with v the codes' values.
-// CTA = (sequence, up to 16 query rows of one kv head's group, key split): warp 4 streams tiles of 64 keys and
+// CTA = (sequence, up to 8 kN query rows of one kv head's group, key split): warp 4 streams tiles of 64 keys and
 // values into a ring (TMA, 2 boxes of a page's rows where pages are smaller); warps 0-3 take 16 keys of
 // each tile by themselves, with their own running maximum m, sum l and O, and meet only at the end.
-//   products  mma.m16n8k16 in f16: E4M3 codes are f16 values exactly, and a query row scaled by 2^-e_q (bf16 has
-//             fewer bits than f16) is too, so that S is exact up to fp32 sums; p 2^(e_v - r) is rounded to f16 (11 bits).  The
-//             tensor memory path would need 128 query rows to be worth its hand-overs.
-//   layout    an MMA's inner index and its columns may be permuted at will, so that each lane reads whole 16-byte
-//             runs of a row from shared memory and converts them in place: key column n of a 16-key group is key
+//   products  mma.m16n8k16 in f16, keys and values as the 16-row operand (S^T = K Q^T, O^T = V^T P^T), so that 8 query rows
+//             fill an instruction and half the accumulators do (16 query rows as the 16-row operand: 168 registers, two
+//             CTAs to an SM).  E4M3 codes are f16 values exactly, and a query row scaled by 2^-e_q (bf16 has fewer bits
+//             than f16) is too, so that S is exact up to fp32 sums; p 2^(e_v - r) is rounded to f16 (11 bits) and
+//             turned into the other operand's layout by movmatrix.  The tensor-memory path would need 128 query rows
+//             to be worth its hand-overs.
+//   layout    an MMA's inner index and its rows may be permuted at will, so that each lane reads whole 16-byte
+//             runs of a row from shared memory and converts them in place: row n of a 16-key group is key
 //             tok(n) = n (n even) or ((n - 1) ^ 4) + 1 (n odd), and with the 128-byte swizzle no two lanes of a
 //             quarter warp then meet in a bank, neither for keys (4 lanes on a row) nor for values (2 runs of 4 rows).
 //   scales    e_k is in the factor of the exponent and e_v - r in its summand (r: see kRefWindow), so no key or value
-//             is scaled.  m is raised only when a row outgrows it by 2^4, so that O is seldom rescaled.
+//             is scaled.  m is raised only when a row outgrows it by 2^4: a vote finds that no row does, without a maximum
+//             over lanes, and O is seldom rescaled.
 // Splits leave (m, l, r, O) in a workspace; the last one to arrive joins them in the order of the splits (no atomics on
 // values: results do not change from run to run).
 #include "fk_paged.h"
@@ -28,6 +32,7 @@ constexpr int kStages = 4;
 constexpr float kLowest = -3.402823466e38f;           // m before any key: finite, so that 2^(-inf - m) is 0
 constexpr float kRaise = 4.0f;                        // log2 units by which a row may outgrow m
 constexpr float kShiftP = 8.0f;                       // p is stored times 2^8: at most 2^12 in f16
+constexpr int kNoRef = -1000;                         // r before any block but zeros
 
 template <int D>
 struct FewLayout {
@@ -37,45 +42,41 @@ struct FewLayout {
   static constexpr int kOffBar = kOffV + kStages * kTile;
   static constexpr int kSmem = kOffBar + 256 + 1024;
   static_assert(kWarps * kPagedFewRows * D * 4 <= kOffBar, "the warps' O over the stages");
+  static_assert(kMaxFewSplits * kPagedFewRows * 4 <= kOffBar, "the splits' weights over the stages");
 };
 
 struct FewBarriers {
   uint64_t full[kStages], empty[kStages];
-  int8_t ke[kStages][2], ve[kStages][2];              // exponents of the tile's halves (pages)
   int last;
   volatile int abort;
 };
 
 // D += A B, A 16 x 16 (row), B 16 x 8 (column), f16 in, f32 out
-__device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the transpose of an 8 x 8 matrix of 16-bit elements, two of a row to a lane
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 // byte offset of 16-byte run c of row `row` in a tile (TMA swizzle of the row length)
 template <int D>
 __device__ __forceinline__ int run_at(int row, int c) {
   return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
 }
-// Sequence of work item b: the last s with first[s] <= b.
-__device__ __forceinline__ int find_item(const int* first, int n, int b) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= b) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
 
-template <int D>
-__global__ void __launch_bounds__(kFewThreads, 2)
+template <int D, int kN>
+__global__ void __launch_bounds__(kFewThreads, kN == 1 ? 3 : 2)
 few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
            const __grid_constant__ PagedAttnArgs a) {
   using Lay = FewLayout<D>;
-  constexpr int kRows = kPagedFewRows, kT = kPagedFewTile;
-  constexpr int kSteps = D / 16;                      // inner steps of S
-  constexpr int kCols = D / 8;                        // column tiles of O
+  constexpr int kRows = 8 * kN, kT = kPagedFewTile;
+  constexpr int kSteps = D / 16;                      // inner steps of S^T
+  constexpr int kRowTiles = D / 16;                   // row tiles of O^T
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sK = smem + Lay::kOffK;
@@ -85,10 +86,14 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const int kvh = blockIdx.y;
 
   // ---- this CTA's rows and key tiles
-  const int s = find_item(a.seqs.item0, a.seqs.n, blockIdx.x);
-  const int n_keys = a.seqs.n_keys[s], n_q = a.seqs.n_q[s];
+  int s = 0;
+  for (int hi = a.seqs.n - 1; s < hi;) {              // the last one whose items begin at or before this one
+    const int mid = (s + hi + 1) >> 1;
+    if (a.seqs.item0[mid] <= (int)blockIdx.x) s = mid;
+    else hi = mid - 1;
+  }
+  const int n_keys = a.seqs.n_keys[s], n_q = a.seqs.n_q[s], n_splits = a.seqs.splits[s];
   const int n_rows = n_q * a.G;
-  const int n_splits = a.seqs.splits[s];
   const int item = blockIdx.x - a.seqs.item0[s];
   const int split = item % n_splits, row0 = (item / n_splits) * kRows;
   const int rows = min(kRows, n_rows - row0);
@@ -97,8 +102,10 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const TileRange tr = paged_tiles(n_keys, pos0, pos1, a.mask, kT);
   const int n_tiles = tr.count();
   const int i0 = (int)((int64_t)n_tiles * split / n_splits), i1 = (int)((int64_t)n_tiles * (split + 1) / n_splits);
+  const int* table = a.table + (int64_t)a.seqs.slot[s] * a.max_pages;
+  const int last_page = max(n_keys - 1, 0) / a.P;
 
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == kWarps * 32) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&bar->full[i], 1);
       mbar_init(&bar->empty[i], kWarps);
@@ -108,186 +115,152 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
   __syncthreads();
 
-  float m[2] = {kLowest, kLowest}, l[2] = {0.0f, 0.0f};
-  float o[kCols][4];
+  float m[kN][2], l[kN][2];                             // of rows 8 j + 2 t, + 1 (l: this lane's keys only)
+  float o[kN][kRowTiles][4];
 #pragma unroll
-  for (int c = 0; c < kCols; ++c)
+  for (int j = 0; j < kN; ++j) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[c][i] = 0.0f;
-  int r = -1000;                                        // reference of O (none yet)
+    for (int c = 0; c < kRowTiles; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][c][i] = 0.0f;
+    m[j][0] = m[j][1] = kLowest;
+    l[j][0] = l[j][1] = 0.0f;
+  }
+  int r = kNoRef;
   const int g = lane >> 2, t = lane & 3;
 
   if (warp == kWarps) {
     // ------------------------------------------------------------------ loads
     const int box = min(a.P, kT), boxes = kT / box;     // rows of a page in a tile
-    const int* table = a.table + (int64_t)a.seqs.slot[s] * a.max_pages;
-    const int last_page = max(n_keys - 1, 0) / a.P;
-    int pg[2] = {0, 0}, ek[2] = {0, 0}, ev[2] = {0, 0}, tile = 0;
+    int y0 = 0, y1 = 0;                                 // lane: rows of the boxes of tile i0 + 32 n + lane
     bool ok = true;
-    int lastU[kStages];
-#pragma unroll
-    for (int i = 0; i < kStages; ++i) lastU[i] = -1;
-    for (int i = i0; i < i1 && ok; ++i) {
+    int i = i0;
+    for (; i < i1; ++i) {
       const int k = i - i0;
-      if ((k & 31) == 0) {                              // lane: pages and exponents of tile i + lane
-        if (i + lane < i1) {
-          tile = tr.at(i + lane);
-          for (int b = 0; b < boxes; ++b) {
-            pg[b] = __ldg(table + min((tile * kT + b * box) / a.P, last_page));
-            ek[b] = a.ke[(int64_t)pg[b] * a.Hkv + kvh];
-            ev[b] = a.ve[(int64_t)pg[b] * a.Hkv + kvh];
-          }
-        }
-        __syncwarp();
+      if ((k & 31) == 0) {
+        const int key = tr.at(min(i + lane, i1 - 1)) * kT;
+        y0 = (__ldg(table + min(key / a.P, last_page)) * a.Hkv + kvh) * a.P + key % a.P;
+        if (boxes == 2) y1 = (__ldg(table + min((key + box) / a.P, last_page)) * a.Hkv + kvh) * a.P;
       }
       const int st = k % kStages, u = k / kStages;
       if (u > 0 && !warp_wait(&bar->empty[st], (u - 1) & 1, bar, a.status)) { ok = false; break; }
-      const int from = k & 31;
-      const int tl = __shfl_sync(0xffffffffu, tile, from);
-      if (lane == from) {
-        for (int b = 0; b < 2; ++b) {
-          bar->ke[st][b] = (int8_t)ek[boxes == 2 ? b : 0];
-          bar->ve[st][b] = (int8_t)ev[boxes == 2 ? b : 0];
-        }
+      const int ya = __shfl_sync(0xffffffffu, y0, k & 31), yb = __shfl_sync(0xffffffffu, y1, k & 31);
+      if (elect_one()) {
         mbar_expect_tx(&bar->full[st], 2 * Lay::kTile);
-        for (int b = 0; b < boxes; ++b) {
-          const int y = (pg[b] * a.Hkv + kvh) * a.P + (boxes == 1 ? (tl * kT) % a.P : 0);
-          tma_load_2d(sK + st * Lay::kTile + b * box * D, &tmK, &bar->full[st], 0, y);
-          tma_load_2d(sV + st * Lay::kTile + b * box * D, &tmV, &bar->full[st], 0, y);
+        tma_load_2d(sK + st * Lay::kTile, &tmK, &bar->full[st], 0, ya);
+        tma_load_2d(sV + st * Lay::kTile, &tmV, &bar->full[st], 0, ya);
+        if (boxes == 2) {
+          tma_load_2d(sK + st * Lay::kTile + box * D, &tmK, &bar->full[st], 0, yb);
+          tma_load_2d(sV + st * Lay::kTile + box * D, &tmV, &bar->full[st], 0, yb);
         }
       }
       __syncwarp();
-#pragma unroll
-      for (int q = 0; q < kStages; ++q)
-        if (q == st) lastU[q] = u;
     }
     if (!ok)                                            // loads in flight land before the CTA ends
-#pragma unroll
-      for (int q = 0; q < kStages; ++q)
-        if (lastU[q] >= 0) wait_phase(&bar->full[q], lastU[q] & 1, bar, a.status, false);
+      for (int k = max(0, i - i0 - kStages); k < i - i0; ++k)
+        wait_phase(&bar->full[k % kStages], (k / kStages) & 1, bar, a.status, false);
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ this lane's part of the queries
-    // A fragment: rows g and g + 8, inner step st: channels base + 4 w + {0, 1} and + {2, 3}, base and w as the
-    // lane's runs of a key row: run t (16 t ..) for the first four steps, run t + 4 (64 + 16 t ..) for the others
-    uint32_t q[kSteps][4];
-    float sc[2];
-    int limit[2], lower[2];                             // visible keys: [lower, limit) and those below `sinks`
+    // B fragment: row 8 j + g, inner step st: channels base + 4 w + {0, 1} and + {2, 3}, base and w as the lane's runs
+    // of a key row: run t (16 t ..) for the first four steps, run t + 4 (64 + 16 t ..) for the others
+    uint32_t q[kN][kSteps][2];
+    float sc[kN][2];                                    // of rows 8 j + 2 t, + 1
+    int limit[kN][2], lower[kN][2];                     // visible keys: [lower, limit) and those below `sinks`
+    const bf16* qbase = a.Q + (int64_t)a.seqs.q0[s] * a.qstride + (int64_t)kvh * a.G * D;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int row = g + 8 * h;
-      const bool in = row < rows;
-      const int rr = row0 + (in ? row : 0), tok = a.by_g.div(rr), pos = p_first + tok;
-      limit[h] = !in ? 0 : a.mask.causal ? min(pos + 1, n_keys) : n_keys;
-      lower[h] = a.mask.window > 0 ? pos - a.mask.window + 1 : 0;
-      const bf16* src = a.Q + ((int64_t)a.seqs.q0[s] + tok) * a.qstride + (int64_t)(kvh * a.G + rr - tok * a.G) * D;
+    for (int j = 0; j < kN; ++j) {
+      const int row = 8 * j + g, rr = row0 + min(row, rows - 1), tok = a.by_g.div(rr);
+      const bf16* src = qbase + (int64_t)tok * a.qstride + (int64_t)(rr - tok * a.G) * D + 16 * t;
       uint4 v[D / 32];
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
-        v[2 * c] = __ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t));
-        v[2 * c + 1] = __ldg(reinterpret_cast<const uint4*>(src + 64 * c + 16 * t) + 1);
+        v[2 * c] = __ldg(reinterpret_cast<const uint4*>(src + 64 * c));
+        v[2 * c + 1] = __ldg(reinterpret_cast<const uint4*>(src + 64 * c) + 1);
       }
-      float amax = 0.0f;
+      uint32_t top = 0;                                 // largest magnitude as bf16 bits
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) amax = fmaxf(amax, absmax8(v[c]));
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-      if (!(amax <= 3.402823466e38f)) l[h] = NAN;       // infinities (NaN makes its own way)
-      const int e = e4m3_row_exponent(amax);
+      for (int c = 0; c < D / 32; ++c)
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[c].x & 0x7FFF7FFFu, v[c].y & 0x7FFF7FFFu), __vmaxu2(v[c].z & 0x7FFF7FFFu, v[c].w & 0x7FFF7FFFu)));
+      top = max(top & 0xFFFFu, top >> 16);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const bool fine = top < 0x7F80u;
+      const int e = fine ? e4m3_row_exponent(__uint_as_float(top << 16)) : 0;
       const float inv = pow2f(-e);
-      sc[h] = a.scale_log2 * pow2f(e);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {                   // channels 8 c' + 2 i, + 1
-          const uint32_t p = pack_f16(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xFFFF0000u) * inv);
-          q[2 * c + (i >> 1)][(i & 1) * 2 + h] = p;
+        for (int i = 0; i < 4; ++i)                     // channels 8 c' + 2 i, + 1
+          q[j][2 * c + (i >> 1)][i & 1] = pack_f16(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xFFFF0000u) * inv);
+      }
+      // what belongs to row 8 j + g, to the lanes that hold its sums
+      const float scale = fine ? a.scale_log2 * pow2f(e) : NAN;
+      const int pos = p_first + tok, lim = row >= rows ? 0 : a.mask.causal ? min(pos + 1, n_keys) : n_keys;
+      const int low = a.mask.window > 0 ? pos - a.mask.window + 1 : 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int from = (2 * t + h) * 4;
+        sc[j][h] = __shfl_sync(0xffffffffu, scale, from);
+        limit[j][h] = __shfl_sync(0xffffffffu, lim, from);
+        lower[j][h] = __shfl_sync(0xffffffffu, low, from);
+        if (sc[j][h] != sc[j][h]) {                     // infinities or NaN: the row's O is NaN
+          l[j][h] = NAN;
+          sc[j][h] = 0.0f;
         }
       }
     }
     // a tile without a masked key for any row of the CTA: [full_lo, full_hi), or all below the sinks
     const int full_hi = a.mask.causal ? min(pos0 + 1, n_keys) : n_keys;
     const int full_lo = a.mask.window > 0 ? pos1 - a.mask.window + 1 : 0;
-    const int krow = warp * 16 + ((g & 1) ? ((g ^ 1) ^ 4) + 1 : g);   // key row of column g, first 8 columns
+    const int krow = warp * 16 + ((g & 1) ? ((g ^ 1) ^ 4) + 1 : g);   // key row of MMA row g
     const int va = warp * 16 + 2 * t, vb = warp * 16 + ((2 * t) ^ 4) + 1;
 
-    bool ok = true;
+    int packed = 0;                                     // lane: exponents of this warp's block of tile i0 + 32 n + lane
     for (int i = i0; i < i1; ++i) {
       const int k = i - i0, st = k % kStages;
-      if (!warp_wait(&bar->full[st], (k / kStages) & 1, bar, a.status)) { ok = false; break; }
+      if ((k & 31) == 0) {
+        const int key = tr.at(min(i + lane, i1 - 1)) * kT + warp * 16;
+        const int64_t block = (int64_t)__ldg(table + min(key / a.P, last_page)) * a.Hkv + kvh;
+        packed = (int)(uint8_t)a.ke[block] | (int)a.ve[block] << 8;
+      }
+      const int both = __shfl_sync(0xffffffffu, packed, k & 31), ek = (int)(int8_t)both, ev = both >> 8;
+      if (!warp_wait(&bar->full[st], (k / kStages) & 1, bar, a.status)) break;
       const uint8_t* kt = sK + st * Lay::kTile;
       const uint8_t* vt = sV + st * Lay::kTile;
-      const int ek = bar->ke[st][warp >> 1], ev = bar->ve[st][warp >> 1];
-      // S of the warp's 16 keys
-      float sv[2][4];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) sv[n][c] = 0.0f;
+      // S^T of the warp's 16 keys (rows g and g + 8), in two chains
+      float sv[kN][4];
+      {
+        uint4 ka[D / 64], kb[D / 64];
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
-          const uint4 kv = *reinterpret_cast<const uint4*>(kt + run_at<D>(krow + 8 * n, t + 4 * c));
-          const uint32_t w[4] = {kv.x, kv.y, kv.z, kv.w};
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            mma16816(sv[n], q[4 * c + x], f16x2_of_e4m3x2((uint16_t)w[x]), f16x2_of_e4m3x2((uint16_t)(w[x] >> 16)));
+          ka[c] = *reinterpret_cast<const uint4*>(kt + run_at<D>(krow, t + 4 * c));
+          kb[c] = *reinterpret_cast<const uint4*>(kt + run_at<D>(krow + 8, t + 4 * c));
         }
-      }
-      // scale and mask
-      const float ske = pow2f(ek);
-      const int j0 = tr.at(i) * kT;
-      const bool full = j0 + kT <= full_hi && (j0 >= full_lo || j0 + kT <= a.mask.sinks);
-      const int ja = j0 + va, jb = j0 + vb;             // keys of columns 2 t and 2 t + 1
+        float s2[kN][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float c = fminf(sc[h] * ske, 3e38f);      // (codes may all be 0)
+        for (int j = 0; j < kN; ++j)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          sv[n][2 * h] *= c;
-          sv[n][2 * h + 1] *= c;
-          if (!full) {
-            const int x = ja + 8 * n, y = jb + 8 * n;
-            if (x >= limit[h] || (x < lower[h] && x >= a.mask.sinks)) sv[n][2 * h] = -INFINITY;
-            if (y >= limit[h] || (y < lower[h] && y >= a.mask.sinks)) sv[n][2 * h + 1] = -INFINITY;
+          for (int x = 0; x < 4; ++x) sv[j][x] = s2[j][x] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          const uint32_t wa[4] = {ka[c].x, ka[c].y, ka[c].z, ka[c].w}, wb[4] = {kb[c].x, kb[c].y, kb[c].z, kb[c].w};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t a0 = f16x2_of_e4m3x2((uint16_t)wa[x]), a2 = f16x2_of_e4m3x2((uint16_t)(wa[x] >> 16));
+            const uint32_t a1 = f16x2_of_e4m3x2((uint16_t)wb[x]), a3 = f16x2_of_e4m3x2((uint16_t)(wb[x] >> 16));
+#pragma unroll
+            for (int j = 0; j < kN; ++j)
+              mma16816(x & 1 ? s2[j] : sv[j], a0, a1, a2, a3, q[j][4 * c + x][0], q[j][4 * c + x][1]);
           }
         }
+#pragma unroll
+        for (int j = 0; j < kN; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) sv[j][x] += s2[j][x];
       }
-      // running maximum and reference
-      float mx[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        mx[h] = fmaxf(fmaxf(sv[0][2 * h], sv[0][2 * h + 1]), fmaxf(sv[1][2 * h], sv[1][2 * h + 1]));
-        mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-        mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
-      }
-      const bool move = ev != kZeroExp && (ev > r || ev < r - kRefWindow);   // warp-uniform
-      if (__any_sync(0xffffffffu, move || mx[0] > m[0] + kRaise || mx[1] > m[1] + kRaise)) {
-        const float fr = move ? pow2_any(r - (ev + kRefRoom)) : 1.0f;
-        if (move) r = ev + kRefRoom;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float mn = fmaxf(m[h], mx[h]), al = fast_exp2(m[h] - mn);
-          m[h] = mn;
-          l[h] *= al;
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) {
-            o[c][2 * h] *= al * fr;
-            o[c][2 * h + 1] *= al * fr;
-          }
-        }
-      }
-      const float we = ev == kZeroExp ? 0.0f : (float)(ev - r), fl = ev == kZeroExp ? 1.0f : pow2f(r - ev);
-      uint32_t p[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const float z = we + kShiftP - m[h], x = fast_exp2(sv[n][2 * h] + z), y = fast_exp2(sv[n][2 * h + 1] + z);
-          l[h] = fmaf(x + y, fl, l[h]);
-          p[2 * n + h] = pack_f16(x, y);
-        }
-      // O += P V
+      // the values' loads are under way meanwhile
       uint4 w[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -299,28 +272,83 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           w[x] = make_uint4(y.x, y.y, 0, 0);
         }
       }
+      // scale and mask: keys krow (x = 0, 1) and krow + 8 (2, 3), rows 2 t (0, 2) and 2 t + 1 (1, 3)
+      const float ske = pow2f(ek);
+      const int j0 = tr.at(i) * kT;
+      const bool full = j0 + kT <= full_hi && (j0 >= full_lo || j0 + kT <= a.mask.sinks);
+      bool grows = false;
 #pragma unroll
-      for (int x = 0; x < kCols / 4; ++x) {
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float c = fminf(sc[j][h] * ske, 3e38f);  // (codes may all be 0)
+          sv[j][h] *= c;
+          sv[j][2 + h] *= c;
+          if (!full) {
+            const int x = j0 + krow, y = x + 8;
+            if (x >= limit[j][h] || (x < lower[j][h] && x >= a.mask.sinks)) sv[j][h] = -INFINITY;
+            if (y >= limit[j][h] || (y < lower[j][h] && y >= a.mask.sinks)) sv[j][2 + h] = -INFINITY;
+          }
+          grows |= fmaxf(sv[j][h], sv[j][2 + h]) > m[j][h] + kRaise;
+        }
+      const bool move = ev != kZeroExp && (ev > r || ev < r - kRefWindow);   // warp-uniform
+      if (__any_sync(0xffffffffu, grows || move)) {
+        const float fr = move ? pow2_any(r - (ev + kRefRoom)) : 1.0f;
+        if (move) r = ev + kRefRoom;
+#pragma unroll
+        for (int j = 0; j < kN; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float mx = fmaxf(sv[j][h], sv[j][2 + h]);    // over the 16 keys
+#pragma unroll
+            for (int off = 4; off <= 16; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+            const float mn = fmaxf(m[j][h], mx), al = fast_exp2(m[j][h] - mn);
+            m[j][h] = mn;
+            l[j][h] *= al;
+#pragma unroll
+            for (int c = 0; c < kRowTiles; ++c) {
+              o[j][c][h] *= al * fr;
+              o[j][c][2 + h] *= al * fr;
+            }
+          }
+      }
+      const float we = kShiftP + (ev == kZeroExp ? 0.0f : (float)(ev - r)), fl = ev == kZeroExp ? 1.0f : pow2f(r - ev);
+      uint32_t p0[kN], p1[kN];
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const float za = we - m[j][0], zb = we - m[j][1];
+        const float x0 = fast_exp2(sv[j][0] + za), x1 = fast_exp2(sv[j][1] + zb);
+        const float x2 = fast_exp2(sv[j][2] + za), x3 = fast_exp2(sv[j][3] + zb);
+        l[j][0] = fmaf(x0 + x2, fl, l[j][0]);
+        l[j][1] = fmaf(x1 + x3, fl, l[j][1]);
+        p0[j] = transpose8(pack_f16(x0, x1));            // lane: row g, keys of MMA rows 2 t, 2 t + 1
+        p1[j] = transpose8(pack_f16(x2, x3));            // and 2 t + 8, 2 t + 9
+      }
+      // O^T += V^T P^T: row tile 2 x + y: channels of the lane's run, 4 x + 2 y (rows g) and + 1 (rows g + 8)
+#pragma unroll
+      for (int x = 0; x < kRowTiles / 2; ++x) {
         const uint32_t wa[2] = {x == 0 ? w[0].x : x == 1 ? w[0].y : x == 2 ? w[0].z : w[0].w,
                                 x == 0 ? w[2].x : x == 1 ? w[2].y : x == 2 ? w[2].z : w[2].w};
         const uint32_t wb[2] = {x == 0 ? w[1].x : x == 1 ? w[1].y : x == 2 ? w[1].z : w[1].w,
                                 x == 0 ? w[3].x : x == 1 ? w[3].y : x == 2 ? w[3].z : w[3].w};
-        const uint32_t lo0 = __byte_perm(wa[0], wb[0], 0x5140), hi0 = __byte_perm(wa[0], wb[0], 0x7362);
-        const uint32_t lo1 = __byte_perm(wa[1], wb[1], 0x5140), hi1 = __byte_perm(wa[1], wb[1], 0x7362);
-        mma16816(o[4 * x], p, f16x2_of_e4m3x2((uint16_t)lo0), f16x2_of_e4m3x2((uint16_t)lo1));
-        mma16816(o[4 * x + 1], p, f16x2_of_e4m3x2((uint16_t)(lo0 >> 16)), f16x2_of_e4m3x2((uint16_t)(lo1 >> 16)));
-        mma16816(o[4 * x + 2], p, f16x2_of_e4m3x2((uint16_t)hi0), f16x2_of_e4m3x2((uint16_t)hi1));
-        mma16816(o[4 * x + 3], p, f16x2_of_e4m3x2((uint16_t)(hi0 >> 16)), f16x2_of_e4m3x2((uint16_t)(hi1 >> 16)));
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t lo = __byte_perm(wa[0], wb[0], y ? 0x7362 : 0x5140), hi = __byte_perm(wa[1], wb[1], y ? 0x7362 : 0x5140);
+          const uint32_t a0 = f16x2_of_e4m3x2((uint16_t)lo), a1 = f16x2_of_e4m3x2((uint16_t)(lo >> 16));
+          const uint32_t a2 = f16x2_of_e4m3x2((uint16_t)hi), a3 = f16x2_of_e4m3x2((uint16_t)(hi >> 16));
+#pragma unroll
+          for (int j = 0; j < kN; ++j) mma16816(o[j][2 * x + y], a0, a1, a2, a3, p0[j], p1[j]);
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar->empty[st]);
     }
-    (void)ok;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-    }
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int off = 4; off <= 16; off <<= 1) l[j][h] += __shfl_xor_sync(0xffffffffu, l[j][h], off);
   }
   __syncthreads();                                      // every tile has been read: the stages are free
 
@@ -330,21 +358,22 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   __shared__ int sr[kWarps];
   if (warp < kWarps) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int row = g + 8 * h;
-      float* dst = sO + (warp * kRows + row) * D;
-      // lane t holds channels 2 kCols t + c (even columns) and 2 kCols t + kCols + c (odd columns)
+    for (int j = 0; j < kN; ++j)
 #pragma unroll
-      for (int c = 0; c < kCols; c += 4) {
-        const int ca = (2 * kCols * t + c) / 4, cb = ca + kCols / 4;
-        *reinterpret_cast<float4*>(dst + ((ca ^ (row & 7)) << 2)) = make_float4(o[c][2 * h], o[c + 1][2 * h], o[c + 2][2 * h], o[c + 3][2 * h]);
-        *reinterpret_cast<float4*>(dst + ((cb ^ (row & 7)) << 2)) = make_float4(o[c][2 * h + 1], o[c + 1][2 * h + 1], o[c + 2][2 * h + 1], o[c + 3][2 * h + 1]);
+      for (int h = 0; h < 2; ++h) {
+        const int row = 8 * j + 2 * t + h;
+        float* dst = sO + (warp * kRows + row) * D;
+        // channels D/8 g .. + D/8 - 1
+#pragma unroll
+        for (int c = 0; c < kRowTiles; c += 2) {
+          const int run = D / 32 * g + c / 2;
+          *reinterpret_cast<float4*>(dst + ((run ^ (row & 7)) << 2)) = make_float4(o[j][c][h], o[j][c][2 + h], o[j][c + 1][h], o[j][c + 1][2 + h]);
+        }
+        if (g == 0) {
+          sm[warp][row] = m[j][h];
+          sl[warp][row] = l[j][h];
+        }
       }
-      if (t == 0) {
-        sm[warp][row] = m[h];
-        sl[warp][row] = l[h];
-      }
-    }
     if (lane == 0) sr[warp] = r;
   }
   __syncthreads();
@@ -356,8 +385,9 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     const int rr = row0 + row, tok = a.by_g.div(rr);
     return a.O + ((int64_t)a.seqs.q0[s] + tok) * a.ostride + (int64_t)(kvh * a.G + rr - tok * a.G) * D;
   };
-  float* part = a.part + (int64_t)cta * kRows * D;
-  float4* mls = reinterpret_cast<float4*>(a.part + (int64_t)kPartSlots * kRows * D);   // m, l, r
+  float4* part = reinterpret_cast<float4*>(a.part);                     // [slot][row][run]
+  float4* mls = part + (int64_t)kPartSlots * kPagedFewRows * kRuns;     // [slot][row]: m, l, r
+#pragma unroll 1
   for (int i = threadIdx.x; i < rows * kRuns; i += kFewThreads) {
     const int row = i / kRuns, c = i % kRuns;
     float M = kLowest, L = 0.0f;
@@ -379,60 +409,89 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       *reinterpret_cast<uint2*>(out_row(row) + 4 * c) =
           make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
     } else {
-      *reinterpret_cast<float4*>(part + row * D + 4 * c) = acc;
-      if (c == 0) mls[cta * kRows + row] = make_float4(M, L, (float)R, 0.0f);
+      part[((int64_t)cta * kPagedFewRows + row) * kRuns + c] = acc;
+      if (c == 0) mls[cta * kPagedFewRows + row] = make_float4(M, L, (float)R, 0.0f);
     }
   }
   if (n_splits == 1) return;
 
-  // ---- the last split of the group joins them all
-  __threadfence();
+  // ---- the last split of the group joins them all.  The CTA's writes come before thread 0's release (barrier, then
+  // an atomic of acquire and release at device scope), the others' before its acquire.
   __syncthreads();
   const int first = cta - split;                        // slot of split 0
-  if (threadIdx.x == 0) bar->last = atomicInc(reinterpret_cast<unsigned*>(a.arrived + first), n_splits - 1) == (unsigned)(n_splits - 1);
+  if (threadIdx.x == 0) {
+    unsigned before;
+    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;"
+                 : "=r"(before) : "l"(a.arrived + first), "r"((unsigned)(n_splits - 1)) : "memory");
+    bar->last = before == (unsigned)(n_splits - 1);
+  }
   __syncthreads();
   if (!bar->last) return;
-  __threadfence();
-  const float* parts = a.part + (int64_t)first * kRows * D;
-  for (int i = threadIdx.x; i < rows * kRuns; i += kFewThreads) {
-    const int row = i / kRuns, c = i % kRuns;
-    float M = kLowest, RR = -1000.0f, L = 0.0f;
-    for (int sp = 0; sp < n_splits; ++sp) {
-      const float4 e = __ldcg(mls + (first + sp) * kRows + row);
+  // each row's weights 2^(m - M) 2^(r - RR), first (row by row, a warp each), then the sums, eight loads in flight
+  float* wts = reinterpret_cast<float*>(smem);          // [row][split]
+  for (int row = warp; row < rows; row += kWarps + 1) {
+    float M = kLowest, RR = (float)kNoRef, L = 0.0f;
+    for (int sp = lane; sp < n_splits; sp += 32) {
+      const float4 e = __ldcg(mls + (first + sp) * kPagedFewRows + row);
       M = fmaxf(M, e.x);
       RR = fmaxf(RR, e.z);
     }
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (int sp = 0; sp < n_splits; ++sp) {
-      const float4 e = __ldcg(mls + (first + sp) * kRows + row);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(parts + ((int64_t)sp * kRows + row) * D + 4 * c));
-      const float f = fast_exp2(e.x - M), fo = f * pow2_any((int)(e.z - RR));
-      L = fmaf(f, e.y, L);
-      acc.x = fmaf(fo, x.x, acc.x);
-      acc.y = fmaf(fo, x.y, acc.y);
-      acc.z = fmaf(fo, x.z, acc.z);
-      acc.w = fmaf(fo, x.w, acc.w);
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) {
+      M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+      RR = fmaxf(RR, __shfl_xor_sync(0xffffffffu, RR, off));
     }
-    const float inv = L > 0.0f || L != L ? pow2_any((int)RR) / L : 0.0f;
+    for (int sp = lane; sp < n_splits; sp += 32) {
+      const float4 e = __ldcg(mls + (first + sp) * kPagedFewRows + row);
+      const float f = fast_exp2(e.x - M);
+      L = fmaf(f, e.y, L);
+      wts[row * n_splits + sp] = f * pow2_any((int)(e.z - RR));
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
+    if (lane == 0) sl[0][row] = L > 0.0f || L != L ? pow2_any((int)RR) / L : 0.0f;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = threadIdx.x; i < rows * kRuns; i += kFewThreads) {
+    const int row = i / kRuns, c = i % kRuns;
+    const float4* src = part + ((int64_t)first * kPagedFewRows + row) * kRuns + c;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+    for (int sp = 0; sp < n_splits; ++sp) {
+      const float4 x = __ldcg(src + (int64_t)sp * kPagedFewRows * kRuns);
+      const float f = wts[row * n_splits + sp];
+      acc.x = fmaf(f, x.x, acc.x);
+      acc.y = fmaf(f, x.y, acc.y);
+      acc.z = fmaf(f, x.z, acc.z);
+      acc.w = fmaf(f, x.w, acc.w);
+    }
+    const float inv = sl[0][row];
     *reinterpret_cast<uint2*>(out_row(row) + 4 * c) =
         make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
   }
 }
 
+using FewKern = void (*)(const CUtensorMap, const CUtensorMap, const PagedAttnArgs);
+FewKern few_of(int D, int row_tiles) {
+  if (D == 128) return row_tiles == 1 ? few_kernel<128, 1> : few_kernel<128, 2>;
+  return row_tiles == 1 ? few_kernel<64, 1> : few_kernel<64, 2>;
+}
+
 }  // namespace
 
 cudaError_t paged_few_prepare(int D) {
-  return D == 128 ? cudaFuncSetAttribute(few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewLayout<128>::kSmem)
-                  : cudaFuncSetAttribute(few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewLayout<64>::kSmem);
+  cudaError_t e = cudaSuccess;
+  for (int n = 1; n <= 2 && e == cudaSuccess; ++n)
+    e = cudaFuncSetAttribute(few_of(D, n), cudaFuncAttributeMaxDynamicSharedMemorySize, D == 128 ? FewLayout<128>::kSmem : FewLayout<64>::kSmem);
+  return e;
 }
 
-cudaError_t launch_paged_few(int D, const CUtensorMap& tmK, const CUtensorMap& tmV, const PagedAttnArgs& a,
+cudaError_t launch_paged_few(int D, int row_tiles, const CUtensorMap& tmK, const CUtensorMap& tmV, const PagedAttnArgs& a,
                              cudaStream_t s) {
   const dim3 grid((unsigned)a.seqs.item0[a.seqs.n], (unsigned)a.Hkv);
   if (grid.x == 0) return cudaSuccess;
-  if (D == 128) few_kernel<128><<<grid, kFewThreads, FewLayout<128>::kSmem, s>>>(tmK, tmV, a);
-  else few_kernel<64><<<grid, kFewThreads, FewLayout<64>::kSmem, s>>>(tmK, tmV, a);
+  few_of(D, row_tiles)<<<grid, kFewThreads, D == 128 ? FewLayout<128>::kSmem : FewLayout<64>::kSmem, s>>>(tmK, tmV, a);
   return cudaGetLastError();
 }
 

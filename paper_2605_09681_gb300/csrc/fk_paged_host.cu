@@ -177,21 +177,38 @@ void fill_seqs(const fk_paged* h, size_t i0, size_t i1, bool whole, bool read, i
   out->page0[out->n] = page0;
 }
 
-// Work items of the few-row kernel: row tiles of 16, and key splits where they do not fill the device.
-void plan_few(const fk_paged* h, PagedAttnArgs* a) {
+// Sequences in the order of `key`, the largest first (their items then start first).
+void sort_seqs(PagedAttnSeqs& s, const int* key) {
+  int order[kStepSeqs], old[kStepSeqs];
+  for (int k = 0; k < s.n; ++k) order[k] = k;
+  std::stable_sort(order, order + s.n, [&](int x, int y) { return key[x] > key[y]; });
+  for (int* v : {s.slot, s.n_keys, s.q0, s.n_q}) {
+    std::copy(v, v + s.n, old);
+    for (int k = 0; k < s.n; ++k) v[k] = old[order[k]];
+  }
+}
+
+// Work items of the few-row kernel: 8 or 16 rows to a CTA (returned, in eights), and key splits where they do not fill
+// the device.
+int plan_few(const fk_paged* h, PagedAttnArgs* a) {
   PagedAttnSeqs& s = a->seqs;
-  int tiles[kStepSeqs], row_tiles[kStepSeqs];
+  int tiles[kStepSeqs], row_tiles[kStepSeqs], eights = 1;
+  for (int k = 0; k < s.n; ++k)
+    if (s.n_q[k] * a->G > 8) eights = 2;
+  auto count = [&](int k) { return paged_tiles(s.n_keys[k], s.n_keys[k] - s.n_q[k], s.n_keys[k] - 1, a->mask, kPagedFewTile).count(); };
+  for (int k = 0; k < s.n; ++k) tiles[k] = count(k);
+  sort_seqs(s, tiles);
   int64_t work = 0;                   // key tiles of all CTAs, unsplit
   for (int k = 0; k < s.n; ++k) {
-    row_tiles[k] = (s.n_q[k] * a->G + kPagedFewRows - 1) / kPagedFewRows;
-    tiles[k] = paged_tiles(s.n_keys[k], s.n_keys[k] - s.n_q[k], s.n_keys[k] - 1, a->mask, kPagedFewTile).count();
+    row_tiles[k] = (s.n_q[k] * a->G + 8 * eights - 1) / (8 * eights);
+    tiles[k] = count(k);
     work += (int64_t)tiles[k] * row_tiles[k] * a->Hkv;
   }
-  // two CTAs fit an SM; a split takes at least 4 tiles
-  const int64_t per = std::max<int64_t>(4, (work + 2 * h->sms - 1) / (2 * h->sms));
+  // three CTAs fit an SM (two of 16 rows); a split takes at least 4 tiles
+  const int64_t slots = (eights == 1 ? 3 : 2) * h->sms, per = std::max<int64_t>(4, (work + slots - 1) / slots);
   int item = 0, part = 0;
   for (int k = 0; k < s.n; ++k) {
-    int splits = (int)std::max<int64_t>(1, (tiles[k] + per - 1) / per);
+    int splits = (int)std::min<int64_t>(kMaxFewSplits, std::max<int64_t>(1, (tiles[k] + per - 1) / per));
     if (splits > 1 && part + (int64_t)splits * row_tiles[k] * a->Hkv > kPartSlots) splits = 1;
     s.item0[k] = item;
     s.part0[k] = part;
@@ -201,6 +218,7 @@ void plan_few(const fk_paged* h, PagedAttnArgs* a) {
     if (splits > 1) part += splits * row_tiles[k] * a->Hkv;
   }
   s.item0[s.n] = item;
+  return eights;
 }
 
 // Work items of the chunk kernel; true: one query tile per CTA.
@@ -529,12 +547,11 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
         }
         if (chunk) q0 = q;
         if (a->seqs.n == 0) continue;
-        const bool one = chunk && plan_chunk(h, a.get());
-        if (!chunk) plan_few(h, a.get());
+        const int shape = chunk ? (plan_chunk(h, a.get()) ? 1 : 2) : plan_few(h, a.get());
         a->part = chunk ? h->part_chunk : h->part_few;
         const cudaStream_t s = static_cast<cudaStream_t>(stream);
-        const fk_status st = done(h, chunk ? launch_paged_chunk(c.head_dim, one, h->tmK[layer], h->tmV[layer], *a, s)
-                                           : launch_paged_few(c.head_dim, h->tmK[layer], h->tmV[layer], *a, s));
+        const fk_status st = done(h, chunk ? launch_paged_chunk(c.head_dim, shape == 1, h->tmK[layer], h->tmV[layer], *a, s)
+                                           : launch_paged_few(c.head_dim, shape, h->tmK[layer], h->tmV[layer], *a, s));
         if (st != FK_OK) return st;
       }
     }
