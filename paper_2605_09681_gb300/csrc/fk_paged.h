@@ -9,8 +9,8 @@ constexpr int kStepSeqs = 256;        // sequences of one launch (their numbers 
 constexpr int kPagedFewRows = 16;     // query rows of a CTA of the few-row kernel, at most
 constexpr int kPagedFewTile = 64;     // keys per tile of the few-row kernel
 
-constexpr int kMaxFewSplits = 480;    // key splits of a row of the few-row kernel
-constexpr int kPartSlots = 1024;      // CTAs of a launch that share their rows with other key splits, at most
+constexpr int kMaxFewSplits = 460;    // key splits of a row of the few-row kernel
+constexpr int kPartSlots = 4096;      // CTAs of a launch that share their rows with other key splits, at most
 
 // Stored exponent of a block of zeros (others are at least -120).
 constexpr int kZeroExp = -126;
@@ -18,6 +18,8 @@ constexpr int kZeroExp = -126;
 // reference r that O (fp32) is kept to: e - r stays in [-kRefWindow, 0], so that no weight loses bits to a
 // block of another size, seen or not.  A block outside moves r to e + kRefRoom and rescales O by a power of two.
 constexpr int kRefWindow = 16, kRefRoom = 2;
+
+constexpr int kAppendFewRows = 8;     // new tokens on a page that one warp takes
 
 constexpr int kStatusNonFinite = 4;   // device status: an appended key or value was not finite
 constexpr int kStatusPosition = 8;    // device status: a position outside the rotation tables
@@ -37,6 +39,18 @@ struct PagedPool {
   float* tail_vmax;
 };
 
+// Division of 0 .. 2^31 - 1 by a number that the host knows: q = (umulhi(n, mul) + n) >> shift.
+struct FastDiv {
+  uint32_t d, mul, shift;
+  explicit FastDiv(uint32_t div = 1) : d(div), mul(0), shift(0) {
+    while (((uint64_t)1 << shift) < d) ++shift;
+    mul = (uint32_t)(((((uint64_t)1 << shift) - d) << 32) / d + 1);
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+#endif
+};
+
 // Sequences of one append or read-back launch.
 struct PagedSeqs {
   int n;
@@ -51,7 +65,9 @@ struct PagedSeqs {
 struct AppendArgs {
   PagedPool pool;
   const int* table;                   // [max_seqs][max_pages]
-  int max_pages, Hkv, G, P, n_pages;
+  int max_pages, Hkv, G, P;
+  int most;                           // new tokens on a page, at most
+  FastDiv by_g;                       // row of a page's queries -> token
   const bf16* K;                      // [T][Hkv][D], rows of a token contiguous, kstride from token to token
   const bf16* V;
   const bf16* Q;                      // [T][Hkv G][D] or nullptr
@@ -114,18 +130,6 @@ __host__ __device__ inline TileRange paged_tiles(int n_keys, int p0, int p1, con
   }
   return r;
 }
-
-// Division of 0 .. 2^31 - 1 by a number that the host knows: q = (umulhi(n, mul) + n) >> shift.
-struct FastDiv {
-  uint32_t d, mul, shift;
-  explicit FastDiv(uint32_t div = 1) : d(div), mul(0), shift(0) {
-    while (((uint64_t)1 << shift) < d) ++shift;
-    mul = (uint32_t)(((((uint64_t)1 << shift) - d) << 32) / d + 1);
-  }
-#ifdef __CUDACC__
-  __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
-#endif
-};
 
 struct PagedAttnSeqs {
   int n;

@@ -12,8 +12,8 @@
 // were before the rounding (rotated keys in fp32, values in bf16: both exact) with each token's largest magnitude, and
 // where e moves, its older tokens are rounded again from there.  Most steps leave e alone, and then only the new
 // tokens are touched.  A step's append may be repeated with other keys and values: nothing it reads is what it wrote.
-// Threads: P D / 64, in rows of D / 16; a thread holds 16 channels (two runs of 8, the two halves of its pairs) of
-// 4 tokens, so that a page is loaded at once and never read again.
+// Threads: P D / 32, in rows of D / 16; a thread holds 16 channels (two runs of 8, the two halves of its pairs) of
+// 2 tokens, so that a page is loaded at once and never read again.  Steps of a few tokens: append_few_kernel.
 #include "fk_paged.h"
 
 namespace fk {
@@ -44,7 +44,7 @@ __device__ __forceinline__ uint2 codes8(const float* x, float scale) {
   uint32_t c[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) c[i] = e4m3x2(x[2 * i] * scale, x[2 * i + 1] * scale);
-  return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+  return make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
 }
 
 // Sequence of page (or item) b: the last s with first[s] <= b.
@@ -70,7 +70,7 @@ __device__ __forceinline__ Cols cols_of(int j, int R, int interleaved) {
   return {8 * (2 * half + 2 * (j - half)), 8 * (2 * half + 2 * (j - half) + 1), false};
 }
 
-// Rotate the 16 channels x (two runs) by table row `pos`; c, s: 8 factors each.
+// Rotate the 16 channels x (two runs); cs, sn: 8 factors each.  (Packed products and sums would be contracted.)
 __device__ __forceinline__ void rotate16(float* x, const float* cs, const float* sn, int interleaved) {
   if (interleaved) {
 #pragma unroll
@@ -95,104 +95,186 @@ __device__ __forceinline__ void load8(const float* p, float* x) {
   x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
 }
 
+// What an append CTA or warp knows of its page.
+struct PageOf {
+  int slot, pi, base, lo, hi;         // sequence's slot, page of the sequence, its first token, this step's rows of it
+  int64_t tok;                        // caller's token of row 0
+  int64_t tail_old, tail_new;         // tail rows of row 0
+};
+__device__ __forceinline__ PageOf page_of(const AppendArgs& a, int b, int h) {
+  const int s = find_seq(a.seqs.page0, a.seqs.n, b), P = a.P;
+  const int old_len = a.seqs.old_len[s], new_len = a.seqs.new_len[s], buf = a.seqs.buf[s];
+  PageOf g;
+  g.slot = a.seqs.slot[s];
+  g.pi = old_len / P + (b - a.seqs.page0[s]);
+  g.base = g.pi * P;
+  g.lo = max(old_len - g.base, 0);
+  g.hi = min(new_len - g.base, P);
+  g.tok = (int64_t)a.seqs.tok0[s] + (g.base - old_len);
+  g.tail_old = (((int64_t)g.slot * 2 + (buf & 1)) * a.Hkv + h) * P;
+  g.tail_new = (((int64_t)g.slot * 2 + (buf >> 1)) * a.Hkv + h) * P;
+  return g;
+}
+
+// Table row of caller's token t, row `row` of the page (asked for early: the factors' address hangs on it).
+__device__ __forceinline__ int position_of(const AppendArgs& a, const PageOf& g, int64_t t, int row) {
+  return a.positions ? __ldg(a.positions + t) : g.base + row;
+}
+// Rotate 16 channels x by table row `pos`.
+__device__ __forceinline__ void rotate_row(const AppendArgs& a, int pos, int j, float* x) {
+  if ((unsigned)pos >= (unsigned)a.rope_rows) {
+    atomicOr(a.status, kStatusPosition);
+    return;
+  }
+  float cs[8], sn[8];
+  const int64_t at = (int64_t)pos * (a.R / 2) + 8 * j;
+  load8(a.cos + at, cs);
+  load8(a.sin + at, sn);
+  rotate16(x, cs, sn, a.interleaved);
+}
+
+// Largest finite magnitude of 16 values; `bad` when one is not finite.
+__device__ __forceinline__ float largest16(const float* x, bool& bad) {
+  float m = 0.0f, z = 0.0f;
+#pragma unroll
+  for (int c = 0; c < 16; ++c) {
+    m = fmaxf(m, fabsf(x[c]));
+    z = fmaf(x[c], 0.0f, z);                   // NaN from infinities and NaN
+  }
+  if (z != z) {
+    bad = true;
+    m = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 16; ++c)
+      if (fabsf(x[c]) <= 3.402823466e38f) m = fmaxf(m, fabsf(x[c]));
+  }
+  return m;
+}
+__device__ __forceinline__ void no_nan16(float* x) {
+#pragma unroll
+  for (int c = 0; c < 16; ++c)
+    if (x[c] != x[c]) x[c] = 0.0f;
+}
+
+// Codes of a row's 16 channels, and their unrounded copy in the tail (`keep`: the row's place there, -1: none).
 template <int D>
-__global__ void __launch_bounds__(2 * D) append_kernel(const __grid_constant__ AppendArgs a) {
-  constexpr int kCols = D / 16;       // threads of one token
-  __shared__ float red[8];
-  const int s = find_seq(a.seqs.page0, a.seqs.n, blockIdx.x);
-  const int h = blockIdx.y, P = a.P;
-  const int slot = a.seqs.slot[s], old_len = a.seqs.old_len[s], new_len = a.seqs.new_len[s];
-  const int pi = old_len / P + (blockIdx.x - a.seqs.page0[s]);     // page of the sequence
-  const int base = pi * P;                                           // its first token
-  const int lo = max(old_len - base, 0), hi = min(new_len - base, P);   // this step's rows of the page
-  const int64_t tok = (int64_t)a.seqs.tok0[s] + (base - old_len);    // caller's token of row 0
-  const int j = threadIdx.x % kCols, r0 = threadIdx.x / kCols, step = P / 4;
-  const Cols cl = cols_of(j, a.cos ? a.R : 0, a.interleaved);
-
-  auto factors = [&](int64_t t, int row, float* cs, float* sn) -> bool {   // of caller's token t, row of the page
-    const int pos = a.positions ? __ldg(a.positions + t) : base + row;
-    if ((unsigned)pos >= (unsigned)a.rope_rows) {
-      atomicOr(a.status, kStatusPosition);
-      return false;
+__device__ __forceinline__ void put16(const AppendArgs& a, bool is_v, uint8_t* dst, int row, const Cols& cl, const float* x, float inv,
+                                      int64_t keep) {
+  *reinterpret_cast<uint2*>(dst + row * D + cl.c0) = codes8(x, inv);
+  *reinterpret_cast<uint2*>(dst + row * D + cl.c1) = codes8(x + 8, inv);
+  if (keep < 0) return;
+  if (is_v) {
+    bf16* p = a.pool.tail_v + keep * D;
+    *reinterpret_cast<uint4*>(p + cl.c0) = pack8(x);
+    *reinterpret_cast<uint4*>(p + cl.c1) = pack8(x + 8);
+  } else {
+    float* p = a.pool.tail_k + keep * D;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      *reinterpret_cast<float4*>(p + cl.c0 + 4 * q) = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+      *reinterpret_cast<float4*>(p + cl.c1 + 4 * q) = make_float4(x[8 + 4 * q], x[9 + 4 * q], x[10 + 4 * q], x[11 + 4 * q]);
     }
-    const int64_t at = (int64_t)pos * (a.R / 2) + 8 * j;
-    load8(a.cos + at, cs);
-    load8(a.sin + at, sn);
-    return true;
-  };
+  }
+}
+// A tail row's 16 channels.
+template <int D>
+__device__ __forceinline__ void tail16(const AppendArgs& a, bool is_v, int64_t row, const Cols& cl, float* x) {
+  if (is_v) {
+    const bf16* p = a.pool.tail_v + row * D;
+    unpack8(*reinterpret_cast<const uint4*>(p + cl.c0), x);
+    unpack8(*reinterpret_cast<const uint4*>(p + cl.c1), x + 8);
+  } else {
+    const float* p = a.pool.tail_k + row * D;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      x[c] = p[cl.c0 + c];
+      x[8 + c] = p[cl.c1 + c];
+    }
+  }
+}
 
-  if (blockIdx.z == 2) {              // queries of the page's new tokens, heads of the group
-    const int n = (hi - lo) * a.G;
+// Queries of the page's new tokens, heads of group h: rows (token, head) first, first + step, ..
+template <int D>
+__device__ __forceinline__ void rotate_queries(const AppendArgs& a, const PageOf& g, int h, int first, int step, int j, const Cols& cl) {
+  const int n = (g.hi - g.lo) * a.G;
 #pragma unroll 2
-    for (int i = r0; i < n; i += step) {
-      const int row = lo + i / a.G;
-      const int64_t t = tok + row, hd = h * a.G + i % a.G;
-      float x[16], cs[8], sn[8];
-      const bf16* q = a.Q + t * a.qstride + hd * D;
-      unpack8(__ldg(reinterpret_cast<const uint4*>(q + cl.c0)), x);
-      unpack8(__ldg(reinterpret_cast<const uint4*>(q + cl.c1)), x + 8);
-      if (cl.rot && factors(t, row, cs, sn)) rotate16(x, cs, sn, a.interleaved);
-      bf16* o = a.Qr + t * a.qrstride + hd * D;
+  for (int i = first; i < n; i += step) {
+    const int row = g.lo + a.by_g.div(i);
+    const int64_t t = g.tok + row, hd = h * a.G + i - (row - g.lo) * a.G;
+    const int pos = cl.rot ? position_of(a, g, t, row) : 0;
+    float x[16];
+    const bf16* q = a.Q + t * a.qstride + hd * D;
+    unpack8(__ldg(reinterpret_cast<const uint4*>(q + cl.c0)), x);
+    unpack8(__ldg(reinterpret_cast<const uint4*>(q + cl.c1)), x + 8);
+    if (cl.rot) rotate_row(a, pos, j, x);
+    bf16* o = a.Qr + t * a.qrstride + hd * D;
+    *reinterpret_cast<uint4*>(o + cl.c0) = pack8(x);
+    *reinterpret_cast<uint4*>(o + cl.c1) = pack8(x + 8);
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(4 * D, 2) append_kernel(const __grid_constant__ AppendArgs a) {
+  constexpr int kCols = D / 16;       // threads of one token
+  __shared__ float red[16];
+  const int h = blockIdx.y, P = a.P;
+  const PageOf g = page_of(a, blockIdx.x, h);
+  const int j = threadIdx.x % kCols, r0 = threadIdx.x / kCols, step = P / 2;
+  const Cols cl = cols_of(j, a.cos ? a.R : 0, a.interleaved);
+  // z: keys, values, then the heads of the group's queries
+  const bool is_q = blockIdx.z >= 2, is_v = blockIdx.z == 1, turn = !is_v && cl.rot;
+  const bf16* src = is_q ? a.Q + (int64_t)(h * a.G + (int)blockIdx.z - 2) * D : (is_v ? a.V : a.K) + h * D;
+  const int64_t stride = is_q ? a.qstride : is_v ? a.vstride : a.kstride;
+  uint4 v[2][2];
+  int pos[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = r0 + i * step;
+    v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
+    if (row >= g.lo && row < g.hi) {
+      if (turn) pos[i] = position_of(a, g, g.tok + row, row);
+      const bf16* p = src + (g.tok + row) * stride;
+      v[i][0] = __ldg(reinterpret_cast<const uint4*>(p + cl.c0));
+      v[i][1] = __ldg(reinterpret_cast<const uint4*>(p + cl.c1));
+    }
+  }
+  if (is_q) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = r0 + i * step;
+      if (row < g.lo || row >= g.hi) continue;
+      float x[16];
+      unpack8(v[i][0], x);
+      unpack8(v[i][1], x + 8);
+      if (turn) rotate_row(a, pos[i], j, x);
+      bf16* o = a.Qr + (g.tok + row) * a.qrstride + (int64_t)(h * a.G + (int)blockIdx.z - 2) * D;
       *reinterpret_cast<uint4*>(o + cl.c0) = pack8(x);
       *reinterpret_cast<uint4*>(o + cl.c1) = pack8(x + 8);
     }
     return;
   }
-
-  const bool is_v = blockIdx.z == 1;
-  const bf16* src = is_v ? a.V : a.K;
-  const int64_t stride = is_v ? a.vstride : a.kstride;
-  const int page = __ldg(a.table + (int64_t)slot * a.max_pages + pi);
-  const int64_t block = (int64_t)page * a.Hkv + h;
+  const int64_t block = (int64_t)__ldg(a.table + (int64_t)g.slot * a.max_pages + g.pi) * a.Hkv + h;
   uint8_t* dst = (is_v ? a.pool.v : a.pool.k) + block * P * D;
   int8_t* exps = is_v ? a.pool.ve : a.pool.ke;
-  const int64_t tail_old = (((int64_t)slot * 2 + (a.seqs.buf[s] & 1)) * a.Hkv + h) * P;      // rows
-  const int64_t tail_new = (((int64_t)slot * 2 + (a.seqs.buf[s] >> 1)) * a.Hkv + h) * P;
   float* tmax = is_v ? a.pool.tail_vmax : a.pool.tail_kmax;
-  const int e_old = lo > 0 ? (int)exps[block] : 0;
-
-  // the new tokens, rotated, and the largest finite magnitude
-  float x[4][16], rmax[4];
+  const int e_old = g.lo > 0 ? (int)exps[block] : 0;
+  const bool open = g.hi < P;                  // the page stays open: its new tokens are kept unrounded
+  float m = 0.0f, x[2][16];
   bool bad = false;
-  {
-    uint4 v[4][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = r0 + i * step;
-      v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
-      if (row >= lo && row < hi) {
-        const bf16* p = src + (tok + row) * stride + h * D;
-        v[i][0] = __ldg(reinterpret_cast<const uint4*>(p + cl.c0));
-        v[i][1] = __ldg(reinterpret_cast<const uint4*>(p + cl.c1));
-      }
-    }
+  for (int i = 0; i < 2; ++i) {
+    const int row = r0 + i * step;
+    unpack8(v[i][0], x[i]);
+    unpack8(v[i][1], x[i] + 8);
+    if (turn && row >= g.lo && row < g.hi) rotate_row(a, pos[i], j, x[i]);
+    float rmax = largest16(x[i], bad);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = r0 + i * step;
-      unpack8(v[i][0], x[i]);
-      unpack8(v[i][1], x[i] + 8);
-      if (!is_v && cl.rot && row >= lo && row < hi) {
-        float cs[8], sn[8];
-        if (factors(tok + row, row, cs, sn)) rotate16(x[i], cs, sn, a.interleaved);
-      }
-      rmax[i] = 0.0f;
-#pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        const float m = fabsf(x[i][c]);
-        const bool fine = m <= 3.402823466e38f;
-        bad |= !fine;
-        if (fine) rmax[i] = fmaxf(rmax[i], m);
-        if (x[i][c] != x[i][c]) x[i][c] = 0.0f;
-      }
-    }
+    for (int off = kCols / 2; off >= 1; off >>= 1) rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, off));
+    if (open && j == 0 && row >= g.lo && row < g.hi) tmax[g.tail_new + row] = rmax;
+    m = fmaxf(m, rmax);
   }
   if (bad) atomicOr(a.status, kStatusNonFinite);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int off = kCols / 2; off >= 1; off >>= 1) rmax[i] = fmaxf(rmax[i], __shfl_xor_sync(0xffffffffu, rmax[i], off));
-  float m = fmaxf(fmaxf(rmax[0], rmax[1]), fmaxf(rmax[2], rmax[3]));
-  for (int r = threadIdx.x; r < lo; r += blockDim.x) m = fmaxf(m, tmax[tail_old + r]);
+  for (int r = threadIdx.x; r < g.lo; r += blockDim.x) m = fmaxf(m, tmax[g.tail_old + r]);
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
@@ -201,45 +283,92 @@ __global__ void __launch_bounds__(2 * D) append_kernel(const __grid_constant__ A
   const int e = block_exponent(m);
   const float inv = pow2f(-e);                 // (2^126 for zeros)
   if (threadIdx.x == 0) exps[block] = (int8_t)e;
-  const bool again = lo > 0 && e != e_old;     // the older tokens' codes have another exponent
-  const bool open = hi < P;                    // the page stays open: keep its new tokens unrounded
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     const int row = r0 + i * step;
-    if (row < lo && again) {
-      if (is_v) {
-        const bf16* p = a.pool.tail_v + (tail_old + row) * D;
-        unpack8(*reinterpret_cast<const uint4*>(p + cl.c0), x[i]);
-        unpack8(*reinterpret_cast<const uint4*>(p + cl.c1), x[i] + 8);
-      } else {
-        const float* p = a.pool.tail_k + (tail_old + row) * D;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          x[i][c] = p[cl.c0 + c];
-          x[i][8 + c] = p[cl.c1 + c];
-        }
-      }
+    if (row < g.lo || row >= g.hi) continue;
+    if (bad) no_nan16(x[i]);
+    put16<D>(a, is_v, dst, row, cl, x[i], inv, open ? g.tail_new + row : -1);
+  }
+  if (g.lo > 0 && e != e_old)                  // the older tokens' codes have another exponent
+    for (int row = r0; row < g.lo; row += step) {
+      float x[16];
+      tail16<D>(a, is_v, g.tail_old + row, cl, x);
+      put16<D>(a, is_v, dst, row, cl, x, inv, -1);
     }
-    if (row < hi && (row >= lo || again)) {
-      *reinterpret_cast<uint2*>(dst + row * D + cl.c0) = codes8(x[i], inv);
-      *reinterpret_cast<uint2*>(dst + row * D + cl.c1) = codes8(x[i] + 8, inv);
-    }
-    if (open && row >= lo && row < hi) {
-      if (is_v) {
-        bf16* p = a.pool.tail_v + (tail_new + row) * D;
-        *reinterpret_cast<uint4*>(p + cl.c0) = pack8(x[i]);
-        *reinterpret_cast<uint4*>(p + cl.c1) = pack8(x[i] + 8);
-      } else {
-        float* p = a.pool.tail_k + (tail_new + row) * D;
+}
+
+// A few new tokens to a page (decoding): a warp each for a page's keys, values and queries, so that nothing waits for a CTA;
+// up to kPass passes of 32 / (D / 16) rows.
+template <int D>
+__global__ void __launch_bounds__(96) append_few_kernel(const __grid_constant__ AppendArgs a) {
+  constexpr int kCols = D / 16, kRows = 32 / kCols, kPass = kAppendFewRows / kRows;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y, P = a.P;
+  const PageOf g = page_of(a, blockIdx.x, h);
+  const int j = lane % kCols, r0 = lane / kCols;
+  const Cols cl = cols_of(j, a.cos ? a.R : 0, a.interleaved);
+  if (warp == 2) {
+    rotate_queries<D>(a, g, h, r0, kRows, j, cl);
+    return;
+  }
+  const bool is_v = warp == 1, turn = !is_v && cl.rot;
+  const bf16* src = is_v ? a.V : a.K;
+  const int64_t stride = is_v ? a.vstride : a.kstride;
+  uint4 v[kPass][2];
+  int pos[kPass];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          *reinterpret_cast<float4*>(p + cl.c0 + 4 * q) = make_float4(x[i][4 * q], x[i][4 * q + 1], x[i][4 * q + 2], x[i][4 * q + 3]);
-          *reinterpret_cast<float4*>(p + cl.c1 + 4 * q) = make_float4(x[i][8 + 4 * q], x[i][9 + 4 * q], x[i][10 + 4 * q], x[i][11 + 4 * q]);
-        }
-      }
-      if (j == 0) tmax[tail_new + row] = rmax[i];
+  for (int i = 0; i < kPass; ++i) {
+    const int row = g.lo + r0 + i * kRows;
+    v[i][0] = v[i][1] = make_uint4(0, 0, 0, 0);
+    pos[i] = 0;
+    if (row < g.hi) {
+      if (turn) pos[i] = position_of(a, g, g.tok + row, row);
+      const bf16* p = src + (g.tok + row) * stride + h * D;
+      v[i][0] = __ldg(reinterpret_cast<const uint4*>(p + cl.c0));
+      v[i][1] = __ldg(reinterpret_cast<const uint4*>(p + cl.c1));
     }
   }
+  const int64_t block = (int64_t)__ldg(a.table + (int64_t)g.slot * a.max_pages + g.pi) * a.Hkv + h;
+  uint8_t* dst = (is_v ? a.pool.v : a.pool.k) + block * P * D;
+  int8_t* exps = is_v ? a.pool.ve : a.pool.ke;
+  float* tmax = is_v ? a.pool.tail_vmax : a.pool.tail_kmax;
+  float m = 0.0f;                              // of the older tokens, under way while the new ones load
+  for (int r = lane; r < g.lo; r += 32) m = fmaxf(m, tmax[g.tail_old + r]);
+  const int e_old = g.lo > 0 ? (int)exps[block] : 0;
+  const bool open = g.hi < P;
+  bool bad = false;
+  float x[kPass][16];
+#pragma unroll
+  for (int i = 0; i < kPass; ++i) {
+    const int row = g.lo + r0 + i * kRows;
+    unpack8(v[i][0], x[i]);
+    unpack8(v[i][1], x[i] + 8);
+    if (turn && row < g.hi) rotate_row(a, pos[i], j, x[i]);
+    float rmax = largest16(x[i], bad);
+#pragma unroll
+    for (int off = kCols / 2; off >= 1; off >>= 1) rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, off));
+    if (open && j == 0 && row < g.hi) tmax[g.tail_new + row] = rmax;
+    m = fmaxf(m, rmax);
+  }
+  if (bad) atomicOr(a.status, kStatusNonFinite);
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  const int e = block_exponent(m);
+  const float inv = pow2f(-e);
+  if (lane == 0) exps[block] = (int8_t)e;
+#pragma unroll
+  for (int i = 0; i < kPass; ++i) {
+    const int row = g.lo + r0 + i * kRows;
+    if (row >= g.hi) continue;
+    if (bad) no_nan16(x[i]);
+    put16<D>(a, is_v, dst, row, cl, x[i], inv, open ? g.tail_new + row : -1);
+  }
+  if (g.lo > 0 && e != e_old)
+    for (int row = r0; row < g.lo; row += kRows) {
+      float y[16];
+      tail16<D>(a, is_v, g.tail_old + row, cl, y);
+      put16<D>(a, is_v, dst, row, cl, y, inv, -1);
+    }
 }
 
 // eight codes -> eight values times 2^e as bf16 (exact; beyond bf16's range the largest finite value)
@@ -286,10 +415,18 @@ __global__ void table_kernel(const __grid_constant__ TableArgs a) {
 }  // namespace
 
 cudaError_t launch_paged_append(int D, const AppendArgs& a, cudaStream_t s) {
-  const dim3 grid((unsigned)a.seqs.page0[a.seqs.n], (unsigned)a.Hkv, a.Q ? 3 : 2);
+  const dim3 grid((unsigned)a.seqs.page0[a.seqs.n], (unsigned)a.Hkv, a.Q ? 2 + a.G : 2);
   if (grid.x == 0) return cudaSuccess;
-  if (D == 128) append_kernel<128><<<grid, a.P * 2, 0, s>>>(a);
-  else append_kernel<64><<<grid, a.P, 0, s>>>(a);
+  // at most kAppendFewRows new tokens on any page: a warp takes a page's (batch of 64 streams, a token each: MEASURE)
+  if (a.most <= kAppendFewRows) {
+    const dim3 few(grid.x, grid.y, 1);
+    const int threads = a.Q ? 96 : 64;
+    if (D == 128) append_few_kernel<128><<<few, threads, 0, s>>>(a);
+    else append_few_kernel<64><<<few, threads, 0, s>>>(a);
+    return cudaGetLastError();
+  }
+  if (D == 128) append_kernel<128><<<grid, a.P * 4, 0, s>>>(a);
+  else append_kernel<64><<<grid, a.P * 2, 0, s>>>(a);
   return cudaGetLastError();
 }
 

@@ -42,7 +42,7 @@ struct FewLayout {
   static constexpr int kOffBar = kOffV + kStages * kTile;
   static constexpr int kSmem = kOffBar + 256 + 1024;
   static_assert(kWarps * kPagedFewRows * D * 4 <= kOffBar, "the warps' O over the stages");
-  static_assert(kMaxFewSplits * kPagedFewRows * 4 <= kOffBar, "the splits' weights over the stages");
+  static_assert(kMaxFewSplits * kPagedFewRows * 4 + kFewThreads * 16 <= 8 * kPagedFewTile * D, "the join's numbers over the stages");
 };
 
 struct FewBarriers {
@@ -427,7 +427,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
   __syncthreads();
   if (!bar->last) return;
-  // each row's weights 2^(m - M) 2^(r - RR), first (row by row, a warp each), then the sums, eight loads in flight
+  // each row's weights 2^(m - M) 2^(r - RR), first (row by row, a warp each), then the sums
   float* wts = reinterpret_cast<float*>(smem);          // [row][split]
   for (int row = warp; row < rows; row += kWarps + 1) {
     float M = kLowest, RR = (float)kNoRef, L = 0.0f;
@@ -452,23 +452,48 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     if (lane == 0) sl[0][row] = L > 0.0f || L != L ? pow2_any((int)RR) / L : 0.0f;
   }
   __syncthreads();
+  // A place (row, run) is summed by `sets` threads, each over every sets-th split, sixteen loads in flight.
+  const int places = rows * kRuns, sets = max(1, kFewThreads / places);
+  float4* sums = reinterpret_cast<float4*>(smem + kMaxFewSplits * kPagedFewRows * 4);     // [set][place]
 #pragma unroll 1
-  for (int i = threadIdx.x; i < rows * kRuns; i += kFewThreads) {
+  for (int i0 = 0; i0 < places; i0 += kFewThreads) {
+    const int i = i0 + (sets > 1 ? (int)threadIdx.x % places : (int)threadIdx.x), set = sets > 1 ? (int)threadIdx.x / places : 0;
+    const bool mine = i < places && set < sets;
     const int row = i / kRuns, c = i % kRuns;
-    const float4* src = part + ((int64_t)first * kPagedFewRows + row) * kRuns + c;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-    for (int sp = 0; sp < n_splits; ++sp) {
-      const float4 x = __ldcg(src + (int64_t)sp * kPagedFewRows * kRuns);
-      const float f = wts[row * n_splits + sp];
-      acc.x = fmaf(f, x.x, acc.x);
-      acc.y = fmaf(f, x.y, acc.y);
-      acc.z = fmaf(f, x.z, acc.z);
-      acc.w = fmaf(f, x.w, acc.w);
+    if (mine) {
+      const float4* src = part + ((int64_t)first * kPagedFewRows + row) * kRuns + c;
+#pragma unroll 1
+      for (int sp = set; sp < n_splits; sp += 16 * sets) {
+        float4 x[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (sp + k * sets < n_splits) x[k] = __ldcg(src + (int64_t)(sp + k * sets) * kPagedFewRows * kRuns);
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (sp + k * sets < n_splits) {
+            const float f = wts[row * n_splits + sp + k * sets];
+            acc.x = fmaf(f, x[k].x, acc.x);
+            acc.y = fmaf(f, x[k].y, acc.y);
+            acc.z = fmaf(f, x[k].z, acc.z);
+            acc.w = fmaf(f, x[k].w, acc.w);
+          }
+      }
     }
-    const float inv = sl[0][row];
-    *reinterpret_cast<uint2*>(out_row(row) + 4 * c) =
-        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    if (sets > 1) {
+      if (mine) sums[threadIdx.x] = acc;
+      __syncthreads();
+      if (mine && set == 0)
+        for (int k = 1; k < sets; ++k) {
+          const float4 x = sums[k * places + i];
+          acc = make_float4(acc.x + x.x, acc.y + x.y, acc.z + x.z, acc.w + x.w);
+        }
+    }
+    if (mine && set == 0) {
+      const float inv = sl[0][row];
+      *reinterpret_cast<uint2*>(out_row(row) + 4 * c) =
+          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    }
   }
 }
 

@@ -204,8 +204,14 @@ int plan_few(const fk_paged* h, PagedAttnArgs* a) {
     tiles[k] = count(k);
     work += (int64_t)tiles[k] * row_tiles[k] * a->Hkv;
   }
-  // three CTAs fit an SM (two of 16 rows); a split takes at least 4 tiles
-  const int64_t slots = (eights == 1 ? 3 : 2) * h->sms, per = std::max<int64_t>(4, (work + slots - 1) / slots);
+  // Three CTAs fit an SM (two of 16 rows); a split takes at least 4 tiles.  Where whole sequences already make many
+  // CTAs, of lengths of their own, pieces of half a CTA's share even out the end (64 ragged streams: 92 us with
+  // pieces of a share, 84 half, 86 a third, 87 a quarter); where the keys of a few are split, each further split costs
+  // the one that joins them (one stream of 131072 keys: 51 us, halves 62).
+  int64_t base = 0;
+  for (int k = 0; k < s.n; ++k) base += (int64_t)row_tiles[k] * a->Hkv;
+  const int64_t slots = (eights == 1 ? 3 : 2) * h->sms, pieces = 2 * base > slots ? 2 * slots : slots;
+  const int64_t per = std::max<int64_t>(4, (work + pieces - 1) / pieces);
   int item = 0, part = 0;
   for (int k = 0; k < s.n; ++k) {
     int splits = (int)std::min<int64_t>(kMaxFewSplits, std::max<int64_t>(1, (tiles[k] + per - 1) / per));
@@ -468,6 +474,7 @@ fk_status fk_paged_append(fk_paged* h, int layer, const void* K, int64_t k_strid
     a->Hkv = c.n_kv_heads;
     a->G = c.n_q_heads / c.n_kv_heads;
     a->P = c.page_tokens;
+    a->by_g = FastDiv((uint32_t)a->G);
     a->K = static_cast<const bf16*>(K);
     a->V = static_cast<const bf16*>(V);
     a->Q = static_cast<const bf16*>(Q);
@@ -489,6 +496,8 @@ fk_status fk_paged_append(fk_paged* h, int layer, const void* K, int64_t k_strid
     for (size_t i = 0; i < h->step.size(); i += kStepSeqs) {
       fill_seqs(h, i, std::min(h->step.size(), i + kStepSeqs), false, false, &tok, &a->seqs);
       if (a->seqs.n == 0) continue;
+      a->most = 0;
+      for (int k = 0; k < a->seqs.n; ++k) a->most = std::max(a->most, a->seqs.new_len[k] - a->seqs.old_len[k]);
       const fk_status st = done(h, launch_paged_append(c.head_dim, *a, static_cast<cudaStream_t>(stream)));
       if (st != FK_OK) return st;
     }
