@@ -140,7 +140,8 @@ struct PagedAttnSeqs {
   int item0[kStepSeqs + 1];           // work items before the sequence's first one
   int part0[kStepSeqs];               // workspace slots before the sequence's first one (key splits)
   int splits[kStepSeqs];              // key splits of an item
-  int whole[kStepSeqs];               // chunk kernel: items that are not split, the first ones
+  int whole[kStepSeqs];               // chunk kernel: (rows, kv head) pairs that are not split, the first ones
+  int join0[kStepSeqs + 1];           // chunk kernel: split pairs before the sequence's first one
 };
 
 struct PagedAttnArgs {

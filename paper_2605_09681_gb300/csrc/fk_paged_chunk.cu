@@ -16,6 +16,7 @@
 // for free: e_k and e_v - r of each 32 keys in the factor and the summand of the softmax's fused multiply-add.
 // r (see kRefWindow) is chosen per key tile by the loading warp.  A tile whose own pages differ by more than the
 // window allows ("wild") is handed over 32 keys at a time, O rescaled in between.
+// Key splits leave (m, l, r, O) in a workspace; join_kernel joins them.
 // The pipeline, its barriers and the lazily raised running maximum are those of the chunk attention over packed views.
 #include "fk_paged.h"
 #include "fk_tc.h"
@@ -52,7 +53,6 @@ struct ChunkBarriers {
   uint64_t s_full[2], p_full[2], pa_full[2], pva_done[2];
   uint64_t o_done, fin;
   uint32_t tmem_base;
-  int last;
   int n_info;                       // key tiles whose ChunkInfo has been written
   volatile int abort;
   // what the epilogue needs of the CTA's place (kept here and not in registers across the key tiles)
@@ -798,59 +798,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           if (c == 0) mls[(int64_t)slot0 * kBM + r] = make_float4(M, L, R, 0.0f);
         }
       }
-      if (n_splits > 1) {
-        // the last split of the group joins them all, in their order
-        __threadfence();
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        const int first = slot0 - split * kTiles;
-        if (threadIdx.x == 0)
-          bar->last = atomicInc(reinterpret_cast<unsigned*>(a.arrived + first), n_splits - 1) == (unsigned)(n_splits - 1);
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (bar->last) {
-          __threadfence();
-          // a thread's places are 256 apart: the same run of every (256 / kRuns)-th row, four rows in flight
-          constexpr int kStep = 256 / kRuns, kFly = 4;
-          const int c = threadIdx.x % kRuns;
-          for (int r0 = threadIdx.x / kRuns; r0 < rows; r0 += kStep * kFly) {
-            float M[kFly], R[kFly], L[kFly];
-            float4 acc[kFly];
-#pragma unroll
-            for (int k = 0; k < kFly; ++k) {
-              M[k] = kNoMax;
-              R[k] = kNoRef;
-              L[k] = 0.0f;
-              acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            }
-            for (int sp = 0; sp < n_splits; ++sp) {
-              float4 e[kFly], x[kFly];
-#pragma unroll
-              for (int k = 0; k < kFly; ++k) {
-                const int64_t at = (int64_t)(first + sp * kTiles) * kBM + min(r0 + k * kStep, rows - 1);
-                e[k] = __ldcg(mls + at);
-                x[k] = __ldcg(part + at * kRuns + c);
-              }
-#pragma unroll
-              for (int k = 0; k < kFly; ++k) {        // joined one by one, as the key sets above
-                const float M2 = fmaxf(M[k], e[k].x), R2 = fmaxf(R[k], e[k].z), w0 = fast_exp2(M[k] - M2), w1 = fast_exp2(e[k].x - M2);
-                const float v0 = w0 * pow2_any((int)(R[k] - R2)), v1 = w1 * pow2_any((int)(e[k].z - R2));
-                L[k] = fmaf(L[k], w0, e[k].y * w1);
-                acc[k] = make_float4(fmaf(acc[k].x, v0, x[k].x * v1), fmaf(acc[k].y, v0, x[k].y * v1),
-                                     fmaf(acc[k].z, v0, x[k].z * v1), fmaf(acc[k].w, v0, x[k].w * v1));
-                M[k] = M2;
-                R[k] = R2;
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < kFly; ++k) {
-              const int r = r0 + k * kStep;
-              const float inv = L[k] > 0.0f || L[k] != L[k] ? pow2_any((int)R[k]) / L[k] : 0.0f;
-              if (r < rows)
-                *reinterpret_cast<uint2*>(out_row(r) + 4 * c) =
-                    make_uint2(pack_bf16(acc[k].x * inv, acc[k].y * inv), pack_bf16(acc[k].z * inv, acc[k].w * inv));
-            }
-          }
-        }
-      }
     }
   }
 
@@ -860,6 +807,71 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
   }
+}
+
+// Joins the key splits of the chunk kernel: a warp for a row.  (A kernel of its own: the last of 18 splits took 27 us to join
+// 128 rows by itself.)  With M = max m, R = max r: O = 2^R sum 2^(m - M) 2^(r - R) O_s / sum 2^(m - M) l_s.
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ PagedAttnArgs a, int tiles) {
+  constexpr int kRuns = D / 4, kFly = 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t place = (int64_t)blockIdx.x * 8 + warp;          // row of the split items' rows
+  int s = 0;
+  for (int hi = a.seqs.n - 1; s < hi;) {
+    const int mid = (s + hi + 1) >> 1;
+    if (a.seqs.join0[mid] <= (int)(place / (tiles * kBM))) s = mid;
+    else hi = mid - 1;
+  }
+  // `pair` counts the (rows, kv head) pairs of the sequence as the chunk kernel does, unsplit ones first
+  const int n_splits = a.seqs.splits[s], whole = a.seqs.whole[s], n_rows = a.seqs.n_q[s] * a.G;
+  const int groups = (n_rows + tiles * kBM - 1) / (tiles * kBM);
+  const int split_pair = (int)(place / (tiles * kBM)) - a.seqs.join0[s], r = (int)(place % (tiles * kBM));
+  const int pair = whole + split_pair, kvh = pair % a.Hkv, row = (groups - 1 - pair / a.Hkv) * (tiles * kBM) + r;
+  if (s >= a.seqs.n || pair >= groups * a.Hkv || row >= n_rows) return;
+  const float4* part = reinterpret_cast<const float4*>(a.part);
+  const float4* mls = part + (int64_t)a.part_tiles * kBM * kRuns;
+  const int64_t first = ((int64_t)a.seqs.part0[s] + (int64_t)split_pair * n_splits * tiles) * kBM + r;   // split 0's row
+  const int64_t next = (int64_t)tiles * kBM;
+  float M = kNoMax, R = (float)kNoRef, L = 0.0f;
+  for (int sp = lane; sp < n_splits; sp += 32) {
+    const float4 e = __ldcg(mls + first + sp * next);
+    M = fmaxf(M, e.x);
+    R = fmaxf(R, e.z);
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) {
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, off));
+  }
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s0 = 0; s0 < n_splits; s0 += 32) {        // weights of 32 splits, a lane each
+    float w = 0.0f;
+    if (s0 + lane < n_splits) {
+      const float4 e = __ldcg(mls + first + (s0 + lane) * next);
+      const float f = fast_exp2(e.x - M);
+      L = fmaf(f, e.y, L);
+      w = f * pow2_any((int)(e.z - R));
+    }
+    const int n = min(32, n_splits - s0);
+    for (int k0 = 0; k0 < n; k0 += kFly) {
+      float4 x[kFly];
+#pragma unroll
+      for (int k = 0; k < kFly; ++k)
+        x[k] = k0 + k < n && lane < kRuns ? __ldcg(part + (first + (s0 + k0 + k) * next) * kRuns + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int k = 0; k < kFly; ++k) {
+        const float f = __shfl_sync(0xffffffffu, w, (k0 + k) & 31);
+        acc = make_float4(fmaf(f, x[k].x, acc.x), fmaf(f, x[k].y, acc.y), fmaf(f, x[k].z, acc.z), fmaf(f, x[k].w, acc.w));
+      }
+    }
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
+  const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;      // no visible key: 0
+  const int tok = a.by_g.div(row);
+  bf16* o = a.O + ((int64_t)a.seqs.q0[s] + tok) * a.ostride + (int64_t)(kvh * a.G + row - tok * a.G) * D;
+  if (lane < kRuns)
+    *reinterpret_cast<uint2*>(o + 4 * lane) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
 }
 
 }  // namespace
@@ -887,6 +899,11 @@ cudaError_t launch_paged_chunk(int D, bool one_tile, const CUtensorMap& tmK, con
   } else {
     if (one_tile) chunk_kernel<64, true><<<grid, kChunkThreads, ChunkLayout<64>::kSmem, s>>>(tmK, tmV, a);
     else chunk_kernel<64, false><<<grid, kChunkThreads, ChunkLayout<64>::kSmem, s>>>(tmK, tmV, a);
+  }
+  const int tiles = one_tile ? 1 : 2;
+  if (const unsigned pairs = (unsigned)a.seqs.join0[a.seqs.n]) {       // 8 rows to a CTA
+    if (D == 128) join_kernel<128><<<pairs * (tiles * kBM / 8), 256, 0, s>>>(a, tiles);
+    else join_kernel<64><<<pairs * (tiles * kBM / 8), 256, 0, s>>>(a, tiles);
   }
   return cudaGetLastError();
 }

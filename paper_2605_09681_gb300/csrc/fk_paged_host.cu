@@ -24,6 +24,17 @@ struct StepSeq {
   int seq, n_new, n_query, old_pages;
 };
 
+// One launch of an attention: rows of a CTA in eights (few) or tiles of 128 (chunk).
+struct AttnLaunch {
+  bool chunk;
+  int shape;
+  PagedAttnSeqs seqs;
+};
+struct AttnPlan {
+  PagedMask mask;
+  std::vector<AttnLaunch> launches;
+};
+
 // the caller's current device comes back when a call ends
 struct DeviceGuard {
   int before = -1;
@@ -48,6 +59,7 @@ struct fk_paged {
   std::vector<StepSeq> step;
   bool in_step = false;
   int64_t step_new = 0;               // tokens of the step, all sequences
+  std::vector<AttnPlan> plans;        // of the step
   std::vector<uint8_t> appended;      // per layer: this step's append was made
   std::vector<PagedPool> pools;
   std::vector<CUtensorMap> tmK, tmV;
@@ -144,6 +156,7 @@ fk_status end_step(fk_paged* h) {
     }
   }
   h->in_step = false;
+  h->plans.clear();
   h->step.clear();
   h->step_new = 0;
   return FK_OK;
@@ -177,100 +190,218 @@ void fill_seqs(const fk_paged* h, size_t i0, size_t i1, bool whole, bool read, i
   out->page0[out->n] = page0;
 }
 
-// Sequences in the order of `key`, the largest first (their items then start first).
-void sort_seqs(PagedAttnSeqs& s, const int* key) {
+// ---- plans of an attention
+// Estimated times, in us, of what a CTA takes for a key tile (D = 128) with the device full of such CTAs, and of its start and end;
+// `slots` such CTAs fit an SM.  Measured back to back over grids of rows, keys and sequences (MEASURE).
+struct Shape {
+  int rows, tile, slots;
+  double per_tile, fixed;
+};
+constexpr Shape kFew8{8, kPagedFewTile, 3, 1.2, 4.0}, kFew16{16, kPagedFewTile, 2, 1.0, 5.0};
+constexpr Shape kChunk1{kAttnBM, kAttnBN, 1, 1.1, 9.0}, kChunk2{2 * kAttnBM, kAttnBN, 1, 1.55, 10.0};
+
+struct Candidate {
+  double us = 1e30;
+  int per = INT32_MAX;                // key tiles of a split, at most
+};
+
+// Sequences of one launch: key tiles and items (row tiles times kv heads) under a shape.
+struct Load {
+  int n = 0;
+  int tiles[kStepSeqs];
+  int64_t items[kStepSeqs];
+};
+Load load_of(const PagedAttnArgs& a, const PagedAttnSeqs& s, const Shape& sh) {
+  Load w;
+  w.n = s.n;
+  for (int k = 0; k < s.n; ++k) {
+    w.tiles[k] = paged_tiles(s.n_keys[k], s.n_keys[k] - s.n_q[k], s.n_keys[k] - 1, a.mask, sh.tile).count();
+    w.items[k] = ((int64_t)s.n_q[k] * a.G + sh.rows - 1) / sh.rows * a.Hkv;
+  }
+  return w;
+}
+int splits_of(int tiles, int per) { return per >= tiles ? 1 : (int)(((int64_t)tiles + per - 1) / per); }
+
+// How the keys are best split: the time of the device's slots filled with the pieces, longest first, and what a join adds.
+Candidate best_split(const fk_paged* h, const Load& w, const Shape& sh, int min_tiles, int max_splits, int64_t max_slots, double join) {
+  const double per_tile = sh.per_tile * (sh.slots == 1 ? (h->cfg.head_dim == 128 ? 1.0 : 0.75) : h->cfg.head_dim == 128 ? 1.0 : 0.7);
+  const int slots = sh.slots * h->sms;
+  int most = 0;
+  for (int k = 0; k < w.n; ++k) most = std::max(most, w.tiles[k]);
+  Candidate best;
+  std::pair<float, int64_t> piece[kStepSeqs];
+  std::vector<float> room(2 * (size_t)slots);
+  float *busy = room.data(), *other = busy + slots;
+  for (int s = 1; s <= max_splits; s += std::max(1, s / 6)) {
+    const int per = std::max(min_tiles, (most + s - 1) / s);
+    double total = 0, longest = 0, shortest = 1e30;
+    int64_t ctas = 0, split = 0;
+    for (int k = 0; k < w.n; ++k) {
+      const int n = splits_of(w.tiles[k], per);
+      piece[k] = {(float)((w.tiles[k] + n - 1) / n * per_tile + sh.fixed), w.items[k] * n};
+      total += (double)piece[k].first * (double)piece[k].second;
+      longest = std::max(longest, (double)piece[k].first);
+      shortest = std::min(shortest, (double)piece[k].first);
+      ctas += piece[k].second;
+      if (n > 1) split += piece[k].second;
+    }
+    if (split > max_slots || (s > 1 && ctas > 6 * slots)) break;
+    // Pieces of one length come in whole waves; of several, the longest first, each goes to the slot that is free first.
+    double us;
+    if (longest <= 1.2 * shortest) {
+      us = (double)((ctas + slots - 1) / slots) * longest;
+    } else if (ctas > 6 * slots) {
+      us = std::max(longest, total / slots + 0.5 * shortest);
+    } else {
+      std::sort(piece, piece + w.n, [](const auto& x, const auto& y) { return x.first > y.first; });
+      const int q = std::min(8, h->cfg.n_kv_heads & -h->cfg.n_kv_heads), m = slots / q;   // pieces come q at a time
+      std::fill(busy, busy + m, 0.0f);                     // ascending
+      for (int k = 0; k < w.n; ++k)
+        for (int64_t left = piece[k].second / q; left > 0;) {
+          const int n = (int)std::min<int64_t>(left, m);
+          for (int i = 0; i < n; ++i) busy[i] += piece[k].first;
+          std::merge(busy, busy + n, busy + n, busy + m, other);
+          std::swap(busy, other);
+          left -= n;
+        }
+      us = busy[m - 1];
+    }
+    if (split > 0) us += join + 0.02 * splits_of(most, per);
+    if (us < best.us - 0.2) best = {us, per};
+    if (per <= min_tiles) break;
+  }
+  return best;
+}
+
+// Sequences in the order of their pieces' lengths, the longest first (their items then start first).
+void sort_seqs(PagedAttnSeqs& s, const Load& w, int per) {
   int order[kStepSeqs], old[kStepSeqs];
+  auto len = [&](int k) { return (w.tiles[k] + splits_of(w.tiles[k], per) - 1) / splits_of(w.tiles[k], per); };
   for (int k = 0; k < s.n; ++k) order[k] = k;
-  std::stable_sort(order, order + s.n, [&](int x, int y) { return key[x] > key[y]; });
+  std::stable_sort(order, order + s.n, [&](int x, int y) { return len(x) > len(y); });
   for (int* v : {s.slot, s.n_keys, s.q0, s.n_q}) {
     std::copy(v, v + s.n, old);
     for (int k = 0; k < s.n; ++k) v[k] = old[order[k]];
   }
 }
 
-// Work items of the few-row kernel: 8 or 16 rows to a CTA (returned, in eights), and key splits where they do not fill
-// the device.
-int plan_few(const fk_paged* h, PagedAttnArgs* a) {
-  PagedAttnSeqs& s = a->seqs;
-  int tiles[kStepSeqs], row_tiles[kStepSeqs], eights = 1;
-  for (int k = 0; k < s.n; ++k)
-    if (s.n_q[k] * a->G > 8) eights = 2;
-  auto count = [&](int k) { return paged_tiles(s.n_keys[k], s.n_keys[k] - s.n_q[k], s.n_keys[k] - 1, a->mask, kPagedFewTile).count(); };
-  for (int k = 0; k < s.n; ++k) tiles[k] = count(k);
-  sort_seqs(s, tiles);
-  int64_t work = 0;                   // key tiles of all CTAs, unsplit
+// The launch of a plan: work items, workspace places and joins.
+void lay_out(const PagedAttnArgs& a, PagedAttnSeqs& s, const Shape& sh, int per) {
+  sort_seqs(s, load_of(a, s, sh), per);
+  const Load w = load_of(a, s, sh);
+  const bool few = sh.tile == kPagedFewTile;
+  const int tiles = std::max(1, sh.rows / kAttnBM);        // workspace places of a CTA
+  int item = 0, part = 0, pair = 0;
   for (int k = 0; k < s.n; ++k) {
-    row_tiles[k] = (s.n_q[k] * a->G + 8 * eights - 1) / (8 * eights);
-    tiles[k] = count(k);
-    work += (int64_t)tiles[k] * row_tiles[k] * a->Hkv;
-  }
-  // Three CTAs fit an SM (two of 16 rows); a split takes at least 4 tiles.  Where whole sequences already make many
-  // CTAs, of lengths of their own, pieces of half a CTA's share even out the end (64 ragged streams: 92 us with
-  // pieces of a share, 84 half, 86 a third, 87 a quarter); where the keys of a few are split, each further split costs
-  // the one that joins them (one stream of 131072 keys: 51 us, halves 62).
-  int64_t base = 0;
-  for (int k = 0; k < s.n; ++k) base += (int64_t)row_tiles[k] * a->Hkv;
-  const int64_t slots = (eights == 1 ? 3 : 2) * h->sms, pieces = 2 * base > slots ? 2 * slots : slots;
-  const int64_t per = std::max<int64_t>(4, (work + pieces - 1) / pieces);
-  int item = 0, part = 0;
-  for (int k = 0; k < s.n; ++k) {
-    int splits = (int)std::min<int64_t>(kMaxFewSplits, std::max<int64_t>(1, (tiles[k] + per - 1) / per));
-    if (splits > 1 && part + (int64_t)splits * row_tiles[k] * a->Hkv > kPartSlots) splits = 1;
+    const int n = splits_of(w.tiles[k], per);
     s.item0[k] = item;
     s.part0[k] = part;
-    s.splits[k] = splits;
-    s.whole[k] = 0;
-    item += row_tiles[k] * splits;
-    if (splits > 1) part += splits * row_tiles[k] * a->Hkv;
-  }
-  s.item0[s.n] = item;
-  return eights;
-}
-
-// Work items of the chunk kernel; true: one query tile per CTA.
-bool plan_chunk(const fk_paged* h, PagedAttnArgs* a) {
-  PagedAttnSeqs& s = a->seqs;
-  int64_t pairs = 0;
-  for (int k = 0; k < s.n; ++k) pairs += ((int64_t)s.n_q[k] * a->G + 2 * kAttnBM - 1) / (2 * kAttnBM) * a->Hkv;
-  const bool one = pairs < h->sms;
-  const int rows = (one ? 1 : 2) * kAttnBM;
-  int tiles[kStepSeqs], items[kStepSeqs];
-  int64_t work = 0, total = 0;
-  for (int k = 0; k < s.n; ++k) {
-    items[k] = (int)(((int64_t)s.n_q[k] * a->G + rows - 1) / rows * a->Hkv);
-    tiles[k] = paged_tiles(s.n_keys[k], s.n_keys[k] - s.n_q[k], s.n_keys[k] - 1, a->mask, kAttnBN).count();
-    work += (int64_t)tiles[k] * items[k];
-    total += items[k];
-  }
-  // Key splits, one CTA to an SM: of everything where the items do not fill the device; else, with one sequence
-  // whose items take about as long, of those left over after the last whole wave.
-  int64_t per = INT32_MAX;
-  if (total < h->sms) {
-    per = std::max<int64_t>(2, (work + h->sms - 1) / h->sms);
-  } else if (s.n == 1 && !a->mask.causal && total % h->sms && total < 8 * h->sms) {
-    const int rest = (int)(total % h->sms), splits = std::min<int>(tiles[0] / 2, std::max(1, h->sms / rest));
-    if (splits > 1 && (int64_t)splits * rest * (rows / kAttnBM) <= h->part_tiles) {
-      s.item0[0] = s.part0[0] = 0;
-      s.splits[0] = splits;
-      s.whole[0] = items[0] - rest;
-      s.item0[1] = s.whole[0] + rest * splits;
-      return one;
+    s.splits[k] = n;
+    s.join0[k] = pair;
+    s.whole[k] = n > 1 ? 0 : (int)w.items[k];
+    item += (int)(few ? w.items[k] / a.Hkv : w.items[k]) * n;
+    if (n > 1) {
+      part += (int)w.items[k] * n * tiles;
+      if (!few) pair += (int)w.items[k];
     }
   }
-  int item = 0, part = 0;
-  for (int k = 0; k < s.n; ++k) {
-    int splits = (int)std::max<int64_t>(1, (tiles[k] + per - 1) / per);
-    const int64_t slots = (int64_t)splits * items[k] * (rows / kAttnBM);
-    if (splits > 1 && part + slots > h->part_tiles) splits = 1;
-    s.item0[k] = item;
-    s.part0[k] = part;
-    s.splits[k] = splits;
-    s.whole[k] = splits > 1 ? 0 : items[k];
-    item += items[k] * splits;
-    if (splits > 1) part += (int)slots;
-  }
   s.item0[s.n] = item;
-  return one;
+  s.join0[s.n] = pair;
+}
+
+// One sequence of equally long items that fill the device more than once: only those left over after the last whole wave are split.
+bool split_the_rest(const fk_paged* h, const PagedAttnArgs& a, PagedAttnSeqs& s, const Shape& sh) {
+  if (s.n != 1 || a.mask.causal) return false;
+  const Load w = load_of(a, s, sh);
+  const int64_t items = w.items[0], rest = items % h->sms;
+  const int tiles = sh.rows / kAttnBM, n = rest ? (int)std::min<int64_t>(w.tiles[0] / 2, h->sms / rest) : 0;
+  if (items < h->sms || n < 2 || rest * n * tiles > h->part_tiles) return false;
+  s.item0[0] = s.part0[0] = s.join0[0] = 0;
+  s.splits[0] = n;
+  s.whole[0] = (int)(items - rest);
+  s.item0[1] = (int)(items - rest + rest * n);
+  s.join0[1] = (int)rest;
+  return true;
+}
+
+// The launches of an attention over the step's sequences i .. i1 - 1 (at most kStepSeqs): those of few rows and the others.  Up to
+// which row count the few-row kernel is the better one depends on how much there is to fill the device with (it takes a
+// sequence's keys once for every 16 rows): the estimates decide.
+void plan_group(const fk_paged* h, const PagedAttnArgs& a, size_t i, size_t i1, int64_t* q0, std::vector<AttnLaunch>* out) {
+  PagedAttnSeqs all;
+  all.n = 0;
+  int most = 0;
+  for (size_t j = i; j < i1; ++j) {
+    const StepSeq& st = h->step[j];
+    if (st.n_query > 0) {
+      const int k = all.n++;
+      all.slot[k] = st.seq;
+      all.n_keys[k] = h->seqs[st.seq].len + st.n_new;
+      all.q0[k] = (int)*q0;
+      all.n_q[k] = st.n_query;
+      most = std::max(most, st.n_query * a.G);
+    }
+    *q0 += st.n_query;
+  }
+  if (all.n == 0) return;
+  auto take = [&](int above, int upto, PagedAttnSeqs& s) {     // sequences of above + 1 .. upto rows
+    s.n = 0;
+    for (int k = 0; k < all.n; ++k) {
+      const int rows = all.n_q[k] * a.G;
+      if (rows <= above || rows > upto) continue;
+      s.slot[s.n] = all.slot[k];
+      s.n_keys[s.n] = all.n_keys[k];
+      s.q0[s.n] = all.q0[k];
+      s.n_q[s.n++] = all.n_q[k];
+    }
+  };
+  auto few_of = [&](const PagedAttnSeqs& s) {
+    for (int k = 0; k < s.n; ++k)
+      if (s.n_q[k] * a.G > kFew8.rows) return kFew16;
+    return kFew8;
+  };
+  auto few_plan = [&](const PagedAttnSeqs& s) {
+    const Shape sh = few_of(s);
+    return best_split(h, load_of(a, s, sh), sh, 4, kMaxFewSplits, kPartSlots, 2.0);
+  };
+  auto chunk_plan = [&](const PagedAttnSeqs& s, Shape* sh) {
+    Candidate best;
+    for (const Shape& x : {kChunk2, kChunk1}) {
+      const Candidate c = best_split(h, load_of(a, s, x), x, 2, 64, h->part_tiles / (x.rows / kAttnBM), 4.0);
+      if (c.us < best.us) {
+        best = c;
+        *sh = x;
+      }
+    }
+    return best;
+  };
+  PagedAttnSeqs part[2];
+  int upto = 0;
+  double us = 1e30;
+  for (int t : {16, 32, 64, 128}) {                           // the few-row kernel's (16 rows it always takes)
+    Shape sh = kChunk2;
+    take(0, t, part[0]);
+    take(t, INT32_MAX, part[1]);
+    const double x = (part[0].n ? few_plan(part[0]).us : 0.0) + (part[1].n ? chunk_plan(part[1], &sh).us : 0.0);
+    if (x < us) {
+      us = x;
+      upto = t;
+    }
+    if (t >= most) break;
+  }
+  take(0, upto, part[0]);
+  take(upto, INT32_MAX, part[1]);
+  if (part[0].n) {
+    const Shape sh = few_of(part[0]);
+    lay_out(a, part[0], sh, few_plan(part[0]).per);
+    out->push_back({false, sh.rows / 8, part[0]});
+  }
+  if (part[1].n) {
+    Shape sh = kChunk2;
+    const Candidate c = chunk_plan(part[1], &sh);
+    if (!split_the_rest(h, a, part[1], sh)) lay_out(a, part[1], sh, c.per);
+    out->push_back({true, sh.rows / kAttnBM, part[1]});
+  }
 }
 
 int64_t read_tokens(const fk_paged* h, bool whole) {
@@ -519,7 +650,7 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
     DeviceGuard dev(c.device);
     if (dev.err != cudaSuccess) return FK_ERR_CUDA;
     if (!rows_ok(h, Q, q_stride, c.n_q_heads) || !rows_ok(h, O, o_stride, c.n_q_heads)) return FK_ERR_ARG;
-    auto a = std::make_unique<PagedAttnArgs>();
+    std::unique_ptr<PagedAttnArgs> a(new PagedAttnArgs);
     a->table = h->table;
     a->ke = h->pools[layer].ke;
     a->ve = h->pools[layer].ve;
@@ -537,32 +668,27 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
     a->part_tiles = h->part_tiles;
     a->arrived = h->arrived;
     a->status = h->status;
-    int64_t q0 = 0;
-    for (size_t i = 0; i < h->step.size(); i += kStepSeqs) {
-      const size_t i1 = std::min(h->step.size(), i + kStepSeqs);
-      for (const bool chunk : {false, true}) {
-        int64_t q = q0;
-        a->seqs.n = 0;
-        for (size_t j = i; j < i1; ++j) {
-          const StepSeq& st = h->step[j];
-          if (st.n_query > 0 && ((int64_t)st.n_query * a->G > kPagedFewRows) == chunk) {
-            const int k = a->seqs.n++;
-            a->seqs.slot[k] = st.seq;
-            a->seqs.n_keys[k] = h->seqs[st.seq].len + st.n_new;
-            a->seqs.q0[k] = (int)q;
-            a->seqs.n_q[k] = st.n_query;
-          }
-          q += st.n_query;
-        }
-        if (chunk) q0 = q;
-        if (a->seqs.n == 0) continue;
-        const int shape = chunk ? (plan_chunk(h, a.get()) ? 1 : 2) : plan_few(h, a.get());
-        a->part = chunk ? h->part_chunk : h->part_few;
-        const cudaStream_t s = static_cast<cudaStream_t>(stream);
-        const fk_status st = done(h, chunk ? launch_paged_chunk(c.head_dim, shape == 1, h->tmK[layer], h->tmV[layer], *a, s)
-                                           : launch_paged_few(c.head_dim, shape, h->tmK[layer], h->tmV[layer], *a, s));
-        if (st != FK_OK) return st;
-      }
+    // The launches are planned once for a step and mask: every layer of a model takes the same ones.
+    AttnPlan* plan = nullptr;
+    for (AttnPlan& p : h->plans)
+      if (p.mask.causal == a->mask.causal && p.mask.window == a->mask.window && p.mask.sinks == a->mask.sinks) plan = &p;
+    if (!plan) {
+      AttnPlan p;
+      p.mask = a->mask;
+      int64_t q0 = 0;
+      for (size_t i = 0; i < h->step.size(); i += kStepSeqs)
+        plan_group(h, *a, i, std::min(h->step.size(), i + kStepSeqs), &q0, &p.launches);
+      if (h->plans.size() >= 8) h->plans.clear();
+      h->plans.push_back(std::move(p));
+      plan = &h->plans.back();
+    }
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    for (const AttnLaunch& l : plan->launches) {
+      a->seqs = l.seqs;
+      a->part = l.chunk ? h->part_chunk : h->part_few;
+      const fk_status st = done(h, l.chunk ? launch_paged_chunk(c.head_dim, l.shape == 1, h->tmK[layer], h->tmV[layer], *a, s)
+                                           : launch_paged_few(c.head_dim, l.shape, h->tmK[layer], h->tmV[layer], *a, s));
+      if (st != FK_OK) return st;
     }
     return FK_OK;
   });
