@@ -47,12 +47,13 @@ struct ChunkInfo {                                 // of a key tile
 struct ChunkBarriers {
   uint64_t q_full, q_ready;         // query rows staged (where f16 values go later); their codes written
   uint64_t info_ready;              // the first 32 tiles' numbers
+  uint64_t tmem_ready;              // the tensor memory's address
   uint64_t k_full[kKStages], k_empty[kKStages];
   uint64_t v8_full[2], v8_empty[2]; // V codes
   uint64_t vf_full[2], vf_empty[2]; // f16 values
   uint64_t s_full[2], p_full[2], pa_full[2], pva_done[2];
   uint64_t o_done, fin;
-  uint32_t tmem_base;
+  volatile uint32_t tmem_base;
   int n_info;                       // key tiles whose ChunkInfo has been written
   volatile int abort;
   // what the epilogue needs of the CTA's place (kept here and not in registers across the key tiles)
@@ -231,6 +232,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       mbar_init(&bar->q_full, 1);
       mbar_init(&bar->q_ready, 8);
       mbar_init(&bar->info_ready, 1);
+      mbar_init(&bar->tmem_ready, 1);
       for (int i = 0; i < kKStages; ++i) {
         mbar_init(&bar->k_full[i], 1);
         mbar_init(&bar->k_empty[i], 1);
@@ -258,7 +260,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       bar->slot0 = a.seqs.part0[s] + (item - whole) * kTiles;   // workspace tiles of this CTA
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncwarp();
+  }
+  __syncthreads();
+
+  // softmax state (warps 0-7)
+  const int t = warp >> 2;                          // query tile (kOne: key set) of this warpgroup
+  const int wq = warp & 3, row = wq * 32 + lane;
+  float m = kNoMax, l = 0.0f;
+  int r = kNoRef;                                   // reference of O
+  uint32_t n_pa = 0;                                // parts handed over on pa_full
+  bool ok = true;
+
+  if (warp == kWarpTma) {
+    // ------------------------------------------------------------------ TMA producer
     if (nt > 0) {
       // the query rows, bf16, as they lie: a run of rows for each query (the group's heads lie together)
       if (lane == 0) mbar_expect_tx(&bar->q_full, (uint32_t)rows * D * 2);
@@ -271,28 +285,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       }
       __syncwarp();
     }
-  }
-  __syncwarp();
-  if (warp == kWarpMma) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 :: "r"(su32(&bar->tmem_base)), "r"(kTmemCols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = bar->tmem_base;
-
-  // softmax state (warps 0-7)
-  const int t = warp >> 2;                          // query tile (kOne: key set) of this warpgroup
-  const int wq = warp & 3, row = wq * 32 + lane;
-  float m = kNoMax, l = 0.0f;
-  int r = kNoRef;                                   // reference of O
-  uint32_t n_pa = 0;                                // parts handed over on pa_full
-  bool ok = true;
-
-  if (warp == kWarpTma) {
-    // ------------------------------------------------------------------ TMA producer
     // V_j, then K_{j+2} (K_0 and K_1 are under way)
     fetch_pages(0);
     for (int j = 0; j < min(2, nt); ++j) load_k(j);
@@ -326,6 +318,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   } else if (warp == kWarpMma) {
     // ------------------------------------------------------------------ MMA issuer
     // Tensor-core operations of one thread complete in issue order: when S_t(j+1) is complete, so is PV_t(j).
+    // (The allocation takes ~1000 cycles: nobody waits for it at the start.)
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 :: "r"(su32(const_cast<uint32_t*>(&bar->tmem_base))), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (lane == 0) mbar_arrive(&bar->tmem_ready);
+    const uint32_t tmem = bar->tmem_base;
     constexpr uint32_t kIdQK = idesc_e4m3(kBM, kBN), kIdPV = idesc_f16(kBM, D, 1);
     constexpr uint32_t kLayout = D == 128 ? 2 : 4, kSbo = 8 * D;
     const uint64_t dQ = sdesc(su32(sQ), 16, kSbo, kLayout), dK = sdesc(su32(sK), 16, kSbo, kLayout);
@@ -464,9 +462,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ softmax warpgroups
-    const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
-    const uint32_t tS = tmem + lane_base + (uint32_t)(t * kBN);
-    const uint32_t tO = tmem + lane_base + kColO + (uint32_t)(t * D);
     const int crow = (kOne ? 0 : t * kBM) + row;    // row of the CTA
     const bool in = crow < rows;
     const int pos = p_first + a.by_g.div(row0 + (in ? crow : 0));
@@ -518,13 +513,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const int full_hi = a.mask.causal ? min(pa + 1, n_keys) : n_keys;
     const int full_lo = a.mask.window > 0 ? pb - a.mask.window + 1 : 0;
 
+    ok = warp_wait(&bar->tmem_ready, 0, bar, a.status) && ok;
+    const uint32_t lanes = bar->tmem_base + ((uint32_t)(wq * 32) << 16);
+    const uint32_t tS = lanes + (uint32_t)(t * kBN), tO = lanes + kColO + (uint32_t)(t * D);
     auto known = [&] {
       int n;
       asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(n) : "r"(su32(&bar->n_info)) : "memory");
       return n;
     };
     int n_info = 0;                                 // tiles whose numbers are known to be there
-    if (nt > 0) ok = warp_wait(&bar->info_ready, 0, bar, a.status);
+    if (nt > 0) ok = warp_wait(&bar->info_ready, 0, bar, a.status) && ok;
     for (int it = 0; ok; ++it) {
       const int j = kOne ? 2 * it + t : it;         // kOne: this warpgroup's key set is every other tile
       if (j >= nt) break;
@@ -746,7 +744,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         __syncwarp();
         constexpr int kLanes = D / 8;               // lanes of one row
         const int cl = lane % kLanes;
-#pragma unroll 2
+#pragma unroll 8
         for (int r0 = 0; r0 < 32; r0 += 32 / kLanes) {
           const int r = r0 + lane / kLanes, cr = t * kBM + wq * 32 + r;
           const uint4 v = *reinterpret_cast<const uint4*>(stage + r * (D * 2) + ((cl ^ (r & (D / 8 - 1))) << 4));
@@ -805,7 +803,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   __syncthreads();
   if (warp == kWarpMma) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(bar->tmem_base), "r"(kTmemCols) : "memory");
   }
 }
 

@@ -362,7 +362,7 @@ void plan_group(const fk_paged* h, const PagedAttnArgs& a, size_t i, size_t i1, 
   };
   auto few_plan = [&](const PagedAttnSeqs& s) {
     const Shape sh = few_of(s);
-    return best_split(h, load_of(a, s, sh), sh, 4, kMaxFewSplits, kPartSlots, 2.0);
+    return best_split(h, load_of(a, s, sh), sh, 1, kMaxFewSplits, kPartSlots, 2.0);
   };
   auto chunk_plan = [&](const PagedAttnSeqs& s, Shape* sh) {
     Candidate best;
