@@ -420,209 +420,6 @@ class PagedKVCache:
                "fk_paged_append")
         return Q_out
 
-    def attend(self, layer, Q, O=None, stream=None):
-        if O is None:
-            import torch
-            O = torch.empty_like(Q)
-        _check(self._lib.fk_attend(self._h, layer, _ptr(Q), _ptr(O), _stream(stream)), "fk_attend")
-        return O
-
-    # ---- inspection
-    def kept(self, layer, head, stream=None) -> list:
-        n = ctypes.c_int(0)
-        st = self._lib.fk_get_kept(self._h, layer, head, None, 0, ctypes.byref(n), _stream(stream))
-        if n.value == 0:
-            _check(st, "fk_get_kept")
-            return []
-        buf = (ctypes.c_int32 * n.value)()
-        _check(self._lib.fk_get_kept(self._h, layer, head, buf, n.value, ctypes.byref(n),
-                                     _stream(stream)), "fk_get_kept")
-        return list(buf)
-
-    def scores(self, layer, head, stream=None):
-        """(first_frame, fp32 array [n_frames, n_segments]) of the scoreable frames."""
-        first, nfr = ctypes.c_int(0), ctypes.c_int(0)
-        cap = 1 << 16
-        buf = np.zeros(cap, dtype=np.float32)
-        _check(self._lib.fk_get_scores(self._h, layer, head,
-                                       buf.ctypes.data_as(ctypes.POINTER(ctypes.c_float)), cap,
-                                       ctypes.byref(first), ctypes.byref(nfr), _stream(stream)),
-               "fk_get_scores")
-        return first.value, buf[: nfr.value * self.n_segments].reshape(nfr.value, self.n_segments).copy()
-
-    def key_count(self, layer, head) -> int:
-        n = ctypes.c_int(0)
-        _check(self._lib.fk_key_count(self._h, layer, head, ctypes.byref(n)), "fk_key_count")
-        return n.value
-
-    def cache_bytes(self) -> int:
-        return int(self._lib.fk_cache_bytes(self._h))
-
-    def reserved_bytes(self) -> int:
-        return int(self._lib.fk_reserved_bytes(self._h))
-
-    def sync_status(self, stream=None) -> int:
-        """Synchronize and return the device status (FK_OK, FK_ERR_RANGE, FK_ERR_TIMEOUT)."""
-        return int(self._lib.fk_sync_status(self._h, _stream(stream)))
-
-    # ---- timing
-    def profile_enable(self, on=True):
-        _check(self._lib.fk_profile_enable(self._h, 1 if on else 0), "fk_profile_enable")
-
-    def profile_reset(self):
-        _check(self._lib.fk_profile_reset(self._h), "fk_profile_reset")
-
-    def profile_read(self, kind: str):
-        ms, n = ctypes.c_double(0), ctypes.c_int64(0)
-        _check(self._lib.fk_profile_read(self._h, KERNEL_KINDS[kind], ctypes.byref(ms),
-                                         ctypes.byref(n)), "fk_profile_read")
-        return ms.value, n.value
-
-    def wait_selftest(self, limit_us: int = 20000, stream=None) -> None:
-        """Run the bounded-wait self-test (fk_wait_selftest): the next sync_status() reports
-        FK_ERR_TIMEOUT."""
-        _check(self._lib.fk_wait_selftest(self._h, int(limit_us), _stream(stream)), "fk_wait_selftest")
-
-    def force_attention_plan(self, query_tiles: int = 0, kv_splits: int = 0) -> None:
-        """Fix the attention's query tiles per CTA and key splits, for tests and measurements
-        (fk_force_attention_plan); 0, 0: chosen by the key counts."""
-        _check(self._lib.fk_force_attention_plan(self._h, int(query_tiles), int(kv_splits)),
-               "fk_force_attention_plan")
-
-    def set_host_overlap(self, on: bool = True) -> None:
-        """Overlap host transfers with queued work (see fk_set_host_overlap): host inputs must
-        be final at call time; host outputs are complete after wait_outputs() (or
-        sync_status()) and a synchronization of the stream."""
-        _check(self._lib.fk_set_host_overlap(self._h, 1 if on else 0), "fk_set_host_overlap")
-
-    def wait_outputs(self, stream=None) -> None:
-        """Make the stream wait for pending host-output copies (fk_wait_outputs)."""
-        _check(self._lib.fk_wait_outputs(self._h, _stream(stream)), "fk_wait_outputs")
-
-    def launch_count(self) -> int:
-        return int(self._lib.fk_launch_count(self._h))
-
-
-def _ints(values, n=None):
-    """A ctypes array of 32-bit whole numbers."""
-    v = [int(x) for x in values]
-    if n is not None and len(v) != n:
-        raise ValueError("expected %d numbers, got %d" % (n, len(v)))
-    if any(not -2 ** 31 <= x < 2 ** 31 for x in v):
-        raise ValueError("numbers must fit 32 bits")
-    return (ctypes.c_int32 * len(v))(*v)
-
-
-class PagedKVCache:
-    """Keys and values of many sequences in pages of E4M3 codes, one power-of-two scale for each page and
-    head (fk_paged_*), on one GPU.
-
-        cache.step(seqs, n_new)                      # which sequences append how many tokens
-        for layer in range(n_layers):
-            Q = cache.append(layer, K, V, cos, sin, Q=Q)   # keys and queries rotated, keys and values held
-            O = cache.attend(layer, Q)
-
-    Tensors are bf16 CUDA tensors [tokens, heads, head_dim], the step's sequences one after the other in its order;
-    they may be slices of wider rows (a fused projection's output).  Calls are asynchronous on `stream`
-    (default: torch's current stream of the cache's device).  The step's tokens belong to their sequences from the
-    next step on; until then append may be called again with other keys and values, which take their place."""
-
-    def __init__(self, *, n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
-                 max_seq_tokens, rope="half", device=0):
-        self._lib = L.load()
-        self._h = ctypes.c_void_p()
-        self.cfg = L.FkPagedConfig(n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
-                                   max_seq_tokens, L.FK_ROPE[rope], device)
-        self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
-        self.page_tokens, self.device = page_tokens, device
-        import torch
-        self._bf16, self._f32, self._rope = torch.bfloat16, torch.float32, L.FkRope()
-        self._new = self._queries = 0
-        self._count, self._dev = ctypes.byref(ctypes.c_int64(0)), torch.device("cuda", device)
-        self._held = {}                              # tokens that a read of the current step gives
-        _check(self._lib.fk_paged_create(ctypes.byref(self.cfg), ctypes.byref(self._h)), "fk_paged_create")
-
-    # ---- lifetime
-    def close(self):
-        if getattr(self, "_h", None) and self._h.value:
-            self._lib.fk_paged_destroy(self._h)
-            self._h = ctypes.c_void_p()
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
-
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        self.close()
-
-    def _on(self, stream):
-        if stream is None:
-            import torch
-            try:                                     # as _stream, of the cache's device
-                return torch._C._cuda_getCurrentRawStream(self.device)
-            except AttributeError:
-                return torch.cuda.current_stream(self.device).cuda_stream
-        return getattr(stream, "cuda_stream", stream)
-
-    def _rows(self, x, tokens, heads, name):
-        """(address, elements from token to token) of a [tokens, heads, head_dim] tensor.  (Few tensor properties are
-        asked for: a small call is paced by the host.)"""
-        D = self.head_dim
-        if x.dtype is not self._bf16 or x.shape != (tokens, heads, D) or not x.is_cuda:
-            raise ValueError("%s: expected a bf16 CUDA tensor of %d tokens (the step's) [%d, %d, %d], not %s %s"
-                             % (name, tokens, tokens, heads, D, x.dtype, list(x.shape)))
-        row, head, channel = x.stride()
-        if tokens and (channel != 1 or (heads > 1 and head != D)):
-            raise ValueError("%s: the heads of a token must lie contiguously" % name)
-        return x.data_ptr(), row if tokens > 1 else heads * D
-
-    # ---- steps
-    def step(self, seqs, n_new, n_query=None, stream=None):
-        """Begin a step: sequence seqs[i] appends n_new[i] tokens and asks n_query[i] queries (default: as
-        many), which stand at its last positions."""
-        s = _ints(seqs)
-        n = _ints(n_new, len(s))
-        q = None if n_query is None else _ints(n_query, len(s))
-        _check(self._lib.fk_paged_step(self._h, len(s), s, n, q, self._on(stream)), "fk_paged_step")
-        self._new = sum(n)
-        self._queries = self._new if q is None else sum(q)
-        self._held = {}
-
-    def append(self, layer, K, V, cos=None, sin=None, positions=None, Q=None, Q_out=None, stream=None):
-        """Append the step's keys and values to a layer, the keys rotated by the tables cos, sin [rows, dim / 2]
-        (fp32) at rows `positions` (int32 [tokens]; default: each token's place in its sequence); without
-        tables as they are.  With Q, the queries of the same tokens, returns them rotated (in Q_out, which
-        may be Q)."""
-        import torch
-        k, ks = self._rows(K, self._new, self.n_kv_heads, "K")
-        v, vs = self._rows(V, self._new, self.n_kv_heads, "V")
-        rope = q = o = None
-        qs = os = 0
-        if cos is not None:
-            if sin is None or cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or \
-                    cos.shape != sin.shape or not cos.is_contiguous() or not sin.is_contiguous():
-                raise ValueError("cos, sin: expected contiguous fp32 tensors [rows, dim / 2]")
-            if positions is not None and (positions.dtype != torch.int32 or positions.dim() != 1 or
-                                          positions.shape[0] != self._new or not positions.is_contiguous()):
-                raise ValueError("positions: expected a contiguous int32 tensor [%d]" % self._new)
-            rope = ctypes.byref(L.FkRope(cos.data_ptr(), sin.data_ptr(), positions.data_ptr() if positions is not None else None,
-                                         cos.shape[0], 2 * cos.shape[1]))
-        elif sin is not None or positions is not None:
-            raise ValueError("sin and positions need cos")
-        if Q is not None:
-            if Q_out is None:
-                Q_out = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
-            q, qs = self._rows(Q, self._new, self.n_q_heads, "Q")
-            o, os = self._rows(Q_out, self._new, self.n_q_heads, "Q_out")
-        _check(self._lib.fk_paged_append(self._h, layer, k, ks, v, vs, rope, q, qs, o, os, self._on(stream)),
-               "fk_paged_append")
-        return Q_out
-
     def attend(self, layer, Q, O=None, causal=True, window=0, sinks=0, scale=None, stream=None):
         """Attention of the step's queries over what their sequences hold: query at position p sees key j when
         j <= p (causal) or any j, and under window > 0 only j > p - window or j < sinks; a query that sees
