@@ -16,6 +16,8 @@
 // 2 tokens, so that a page is loaded at once and never read again.  Steps of a few tokens: append_few_kernel.
 #include "fk_paged.h"
 
+#include <algorithm>
+
 namespace fk {
 namespace {
 
@@ -214,7 +216,7 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, const PageOf
 }
 
 template <int D>
-__global__ void __launch_bounds__(4 * D, 2) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(4 * D, D == 64 ? 5 : 2) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int kCols = D / 16;       // threads of one token
   __shared__ float red[16];
   const int h = blockIdx.y, P = a.P;
@@ -399,11 +401,19 @@ __global__ void __launch_bounds__(256) read_kernel(const __grid_constant__ ReadA
   const uint8_t* src = (blockIdx.z ? a.pool.v : a.pool.k) + block * P * D;
   bf16* dst = (blockIdx.z ? a.V : a.K) + ((int64_t)a.seqs.tok0[s] + (int64_t)(pi - first) * P) * a.Hkv * D + h * D;
   const float scale = pow2f(blockIdx.z ? a.pool.ve[block] : a.pool.ke[block]);
-  constexpr int kCols = D / 8;
-  for (int i = threadIdx.x; i < rows * kCols; i += blockDim.x) {
-    const int row = i / kCols, c = (i % kCols) * 8;
-    *reinterpret_cast<uint4*>(dst + (int64_t)row * a.Hkv * D + c) =
-        values8(*reinterpret_cast<const uint2*>(src + row * D + c), scale);
+  constexpr int kCols = D / 8, kFly = 4;
+  for (int i0 = threadIdx.x; i0 < rows * kCols; i0 += blockDim.x * kFly) {
+    uint2 v[kFly];
+#pragma unroll
+    for (int k = 0; k < kFly; ++k) {
+      const int i = i0 + k * blockDim.x;
+      if (i < rows * kCols) v[k] = *reinterpret_cast<const uint2*>(src + i * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < kFly; ++k) {
+      const int i = i0 + k * blockDim.x;
+      if (i < rows * kCols) *reinterpret_cast<uint4*>(dst + (int64_t)(i / kCols) * a.Hkv * D + (i % kCols) * 8) = values8(v[k], scale);
+    }
   }
 }
 
@@ -433,8 +443,9 @@ cudaError_t launch_paged_append(int D, const AppendArgs& a, cudaStream_t s) {
 cudaError_t launch_paged_read(int D, const ReadArgs& a, cudaStream_t s) {
   const dim3 grid((unsigned)a.seqs.page0[a.seqs.n], (unsigned)a.Hkv, 2);
   if (grid.x == 0) return cudaSuccess;
-  if (D == 128) read_kernel<128><<<grid, 256, 0, s>>>(a);
-  else read_kernel<64><<<grid, 256, 0, s>>>(a);
+  const int threads = std::min(256, a.P * D / 32);
+  if (D == 128) read_kernel<128><<<grid, threads, 0, s>>>(a);
+  else read_kernel<64><<<grid, threads, 0, s>>>(a);
   return cudaGetLastError();
 }
 
