@@ -15,6 +15,7 @@
 // Threads: P D / 32, in rows of D / 16; a thread holds 16 channels (two runs of 8, the two halves of its pairs) of
 // 2 tokens, so that a page is loaded at once and never read again.  Steps of a few tokens: append_few_kernel.
 #include "fk_paged.h"
+#include "fk_tc.h"
 
 #include <algorithm>
 
@@ -104,12 +105,12 @@ struct PageOf {
   int64_t tail_old, tail_new;         // tail rows of row 0
 };
 __device__ __forceinline__ PageOf page_of(const AppendArgs& a, int b, int h) {
-  const int s = find_seq(a.seqs.page0, a.seqs.n, b), P = a.P;
+  const int s = find_seq(a.seqs.page0, a.seqs.n, b), P = a.P, shift = 31 - __clz(P);   // (a power of two)
   const int old_len = a.seqs.old_len[s], new_len = a.seqs.new_len[s], buf = a.seqs.buf[s];
   PageOf g;
   g.slot = a.seqs.slot[s];
-  g.pi = old_len / P + (b - a.seqs.page0[s]);
-  g.base = g.pi * P;
+  g.pi = (old_len >> shift) + (b - a.seqs.page0[s]);
+  g.base = g.pi << shift;
   g.lo = max(old_len - g.base, 0);
   g.hi = min(new_len - g.base, P);
   g.tok = (int64_t)a.seqs.tok0[s] + (g.base - old_len);
@@ -137,13 +138,13 @@ __device__ __forceinline__ void rotate_row(const AppendArgs& a, int pos, int j, 
 
 // Largest finite magnitude of 16 values; `bad` when one is not finite.
 __device__ __forceinline__ float largest16(const float* x, bool& bad) {
-  float m = 0.0f, z = 0.0f;
+  float m = 0.0f;
+  float2 z = make_float2(0.0f, 0.0f);
 #pragma unroll
-  for (int c = 0; c < 16; ++c) {
-    m = fmaxf(m, fabsf(x[c]));
-    z = fmaf(x[c], 0.0f, z);                   // NaN from infinities and NaN
-  }
-  if (z != z) {
+  for (int c = 0; c < 16; ++c) m = fmaxf(m, fabsf(x[c]));
+#pragma unroll
+  for (int c = 0; c < 16; c += 2) z = ffma2(make_float2(x[c], x[c + 1]), make_float2(0.0f, 0.0f), z);   // NaN from infinities and NaN
+  if (z.x + z.y != 0.0f) {
     bad = true;
     m = 0.0f;
 #pragma unroll
@@ -157,6 +158,9 @@ __device__ __forceinline__ void no_nan16(float* x) {
   for (int c = 0; c < 16; ++c)
     if (x[c] != x[c]) x[c] = 0.0f;
 }
+
+// Largest of a warp's non-negative floats (their bits are ordered as they are).
+__device__ __forceinline__ float warp_max(float m) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m))); }
 
 // Codes of a row's 16 channels, and their unrounded copy in the tail (`keep`: the row's place there, -1: none).
 template <int D>
@@ -216,7 +220,7 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, const PageOf
 }
 
 template <int D>
-__global__ void __launch_bounds__(4 * D, D == 64 ? 5 : 2) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(4 * D, 256 / D) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int kCols = D / 16;       // threads of one token
   __shared__ float red[16];
   const int h = blockIdx.y, P = a.P;
@@ -270,18 +274,20 @@ __global__ void __launch_bounds__(4 * D, D == 64 ? 5 : 2) append_kernel(const __
     unpack8(v[i][1], x[i] + 8);
     if (turn && row >= g.lo && row < g.hi) rotate_row(a, pos[i], j, x[i]);
     float rmax = largest16(x[i], bad);
-#pragma unroll
-    for (int off = kCols / 2; off >= 1; off >>= 1) rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, off));
-    if (open && j == 0 && row >= g.lo && row < g.hi) tmax[g.tail_new + row] = rmax;
     m = fmaxf(m, rmax);
+    if (open) {
+#pragma unroll
+      for (int off = kCols / 2; off >= 1; off >>= 1) rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, off));
+      if (j == 0 && row >= g.lo && row < g.hi) tmax[g.tail_new + row] = rmax;
+    }
   }
   if (bad) atomicOr(a.status, kStatusNonFinite);
   for (int r = threadIdx.x; r < g.lo; r += blockDim.x) m = fmaxf(m, tmax[g.tail_old + r]);
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
+  m = warp_max(m);
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) red[threadIdx.x >> 5] = m;
   __syncthreads();
-  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) m = fmaxf(m, red[w]);
+  m = warp_max(lane < (int)(blockDim.x >> 5) ? red[lane] : 0.0f);
   const int e = block_exponent(m);
   const float inv = pow2f(-e);                 // (2^126 for zeros)
   if (threadIdx.x == 0) exps[block] = (int8_t)e;
@@ -347,14 +353,15 @@ __global__ void __launch_bounds__(96) append_few_kernel(const __grid_constant__ 
     unpack8(v[i][1], x[i] + 8);
     if (turn && row < g.hi) rotate_row(a, pos[i], j, x[i]);
     float rmax = largest16(x[i], bad);
-#pragma unroll
-    for (int off = kCols / 2; off >= 1; off >>= 1) rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, off));
-    if (open && j == 0 && row < g.hi) tmax[g.tail_new + row] = rmax;
     m = fmaxf(m, rmax);
+    if (open) {
+#pragma unroll
+      for (int off = kCols / 2; off >= 1; off >>= 1) rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, off));
+      if (j == 0 && row < g.hi) tmax[g.tail_new + row] = rmax;
+    }
   }
   if (bad) atomicOr(a.status, kStatusNonFinite);
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+  m = warp_max(m);
   const int e = block_exponent(m);
   const float inv = pow2f(-e);
   if (lane == 0) exps[block] = (int8_t)e;
