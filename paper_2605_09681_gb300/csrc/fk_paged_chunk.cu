@@ -45,7 +45,7 @@ struct ChunkInfo {                                 // of a key tile
   float fk[4], add[4], mul[4];
 };
 struct ChunkBarriers {
-  uint64_t q_full, q_ready;         // query rows staged (where f16 values go later); their codes written
+  uint64_t q_ready;                 // the queries' codes written
   uint64_t info_ready;              // the first 32 tiles' numbers
   uint64_t tmem_ready;              // the tensor memory's address
   uint64_t k_full[kKStages], k_empty[kKStages];
@@ -229,7 +229,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
 
   if (warp == kWarpTma) {
     if (lane == 0) {
-      mbar_init(&bar->q_full, 1);
       mbar_init(&bar->q_ready, 8);
       mbar_init(&bar->info_ready, 1);
       mbar_init(&bar->tmem_ready, 1);
@@ -261,11 +260,23 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
   }
+  const int t = warp >> 2;                          // query tile (kOne: key set) of a softmax warpgroup
+  const int wq = warp & 3, row = wq * 32 + lane;
+  if (warp < 8 && nt > 0) {
+    // a softmax warp's query rows, bf16, on their way to where the values go later
+    constexpr int kRuns = D / 8;                    // 16-byte runs of a row
+    const int q0 = a.seqs.q0[s];
+#pragma unroll 4
+    for (int i = lane / kRuns; i < 32; i += 32 / kRuns) {
+      const int rr = wq * 32 + i, at = row0 + (kOne ? 0 : t * kBM) + rr, tok = a.by_g.div(at), c = lane % kRuns;
+      if (at < row0 + rows)
+        cp_async16(sV + (t * kBM + rr) * (D * 2) + c * 16,
+                   a.Q + ((int64_t)q0 + tok) * a.qstride + (int64_t)(kvh * a.G + at - tok * a.G) * D + c * 8);
+    }
+  }
   __syncthreads();
 
   // softmax state (warps 0-7)
-  const int t = warp >> 2;                          // query tile (kOne: key set) of this warpgroup
-  const int wq = warp & 3, row = wq * 32 + lane;
   float m = kNoMax, l = 0.0f;
   int r = kNoRef;                                   // reference of O
   uint32_t n_pa = 0;                                // parts handed over on pa_full
@@ -273,18 +284,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
 
   if (warp == kWarpTma) {
     // ------------------------------------------------------------------ TMA producer
-    if (nt > 0) {
-      // the query rows, bf16, as they lie: a run of rows for each query (the group's heads lie together)
-      if (lane == 0) mbar_expect_tx(&bar->q_full, (uint32_t)rows * D * 2);
-      __syncwarp();
-      const int tok0 = a.by_g.div(row0), tok1 = a.by_g.div(row0 + rows - 1);
-      for (int tok = tok0 + lane; tok <= tok1; tok += 32) {
-        const int ra = max(tok * a.G, row0), rb = min((tok + 1) * a.G, row0 + rows);
-        bulk_load(sV + (ra - row0) * (D * 2), a.Q + ((int64_t)a.seqs.q0[s] + tok) * a.qstride + (int64_t)(kvh * a.G + ra - tok * a.G) * D,
-                  (uint32_t)(rb - ra) * D * 2, &bar->q_full);
-      }
-      __syncwarp();
-    }
     // V_j, then K_{j+2} (K_0 and K_1 are under way)
     fetch_pages(0);
     for (int j = 0; j < min(2, nt); ++j) load_k(j);
@@ -310,7 +309,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       jk = j + 2;
     }
     if (!ok) {                                      // what was issued lands before the CTA ends
-      wait_phase(&bar->q_full, 0, bar, a.status, false);
       for (int j = max(0, jk - kKStages + 1); j <= jk; ++j) wait_phase(&bar->k_full[j % kKStages], (j / kKStages) & 1, bar, a.status, false);
       for (int j = max(0, jv - 1); j <= jv; ++j) wait_phase(&bar->v8_full[j & 1], (j >> 1) & 1, bar, a.status, false);
     }
@@ -471,8 +469,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     // want the scale.)  Loading rows from global memory a warp at a time, with the maximum by shuffles, took
     // 12000-58000 cycles: the shuffles waited for the loads in flight.
     if (nt > 0) {
-      ok = warp_wait(&bar->q_full, 0, bar, a.status);
-      const uint8_t* src = sV + crow * (D * 2);
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+      const uint8_t* src = sV + (t * kBM + row) * (D * 2);
       uint32_t top = 0;
 #pragma unroll 4
       for (int j = 0; j < D / 8; ++j) {

@@ -97,10 +97,9 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, u
       :: "r"(su32(dst)), "l"(map), "r"(su32(b)), "r"(x), "r"(y), "r"(z) : "memory");
 }
 
-// `bytes` (a multiple of 16) from global to shared memory, both 16-byte aligned
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* b) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               :: "r"(su32(dst)), "l"(src), "r"(bytes), "r"(su32(b)) : "memory");
+// 16 bytes from global to shared memory (complete after this thread's cp.async.wait_all)
+__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(su32(dst)), "l"(src) : "memory");
 }
 
 __device__ __forceinline__ void tc_fence_before() {
