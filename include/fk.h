@@ -412,8 +412,9 @@ typedef struct fk_paged fk_paged;
 FK_API fk_status fk_paged_validate_config(const fk_paged_config* cfg);
 
 /* Create a cache on cfg->device and allocate all of its device memory: per layer 2 * n_kv_heads *
- * head_dim bytes for each token of its pages, and 12 of them for each token of two pages of each of the
- * max_seqs sequences (their open pages).  Errors as fk_create. */
+ * head_dim bytes for each token of its pages and 6 * n_kv_heads * head_dim for each token of two pages of
+ * each of the max_seqs sequences (their open pages, unrounded), and up to 80 MB of workspace for key splits, one for
+ * all layers.  Errors as fk_create. */
 FK_API fk_status fk_paged_create(const fk_paged_config* cfg, fk_paged** out);
 
 /* Release the handle and its device memory (synchronizes the device first).  NULL is a no-op. */
@@ -438,8 +439,9 @@ FK_API fk_status fk_paged_append(fk_paged* h, int layer, const void* K, int64_t 
  * n_query stands at position p = n_keys - n_query + i and sees key j when j <= p (causal = 1) or any j
  * (causal = 0), and under window > 0 only j > p - window or j < sinks.  A query that sees no key gives 0.  scale = 0:
  * 1 / sqrt(head_dim).  Logits, softmax and sums are in fp32; products are of the held values and the bf16
- * queries, exact but for query elements below 2^-10 of their row's largest, which may be rounded to 2^-19 of it;
- * softmax numerators are rounded to f16 before they multiply the values.
+ * queries, exact but for query elements below 2^-9 of their row's largest, which may be rounded to 2^-17 of it;
+ * softmax numerators are rounded to f16 before they multiply the values.  A query with an infinity or NaN gives NaN
+ * in that head and nowhere else.
  * FK_ERR_STATE without a step, or when the layer was not appended to in it. */
 FK_API fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_stride, void* O,
                                  int64_t o_stride, int causal, int window, int sinks, float scale, void* stream);

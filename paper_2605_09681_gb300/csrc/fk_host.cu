@@ -698,8 +698,8 @@ const char* fk_status_str(fk_status s) {
     case FK_ERR_CONFIG: return "invalid configuration";
     case FK_ERR_ARG: return "invalid argument";
     case FK_ERR_STATE: return "call out of order";
-    case FK_ERR_FULL: return "history capacity exceeded";
-    case FK_ERR_RANGE: return "scoring precondition violated (token squared key norm > 2^23)";
+    case FK_ERR_FULL: return "capacity exceeded (history, pages or tokens of a sequence)";
+    case FK_ERR_RANGE: return "values out of range (scoring: token squared key norm > 2^23; paged cache: not finite, or a position outside the tables)";
     case FK_ERR_TIMEOUT: return "bounded device wait expired";
     case FK_ERR_CUDA: return "CUDA error";
     case FK_ERR_NOMEM: return "out of device memory";

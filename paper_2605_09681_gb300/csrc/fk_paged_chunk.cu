@@ -8,8 +8,8 @@
 //   warp 8             page numbers, exponents, and TMA of K and V codes into rings of three and two stages;
 //   warp 9             tcgen05.mma, in the order PV_0(j), S_0(j+1), PV_1(j), S_1(j+1);
 //   warps 10-11        V codes -> f16 values (exact), two stages.
-// Q K^T needs no conversion of the keys: with q 2^-e_q = hi + lo, both E4M3 (a bf16 element of at least 2^-10 of its
-// row's largest is the sum exactly, smaller ones to 2^-19 of the largest), S = hi K^T + lo K^T is two E4M3 products
+// Q K^T needs no conversion of the keys: with q 2^-e_q = hi + lo, both E4M3 (a bf16 element of at least 2^-9 of its
+// row's largest is the sum exactly, smaller ones to 2^-17 of the largest), S = hi K^T + lo K^T is two E4M3 products
 // at twice the bf16 rate, on the codes as the cache holds them.  P V needs P in more than 4 bits, and P split the
 // same way would cost each of the 256 x 128 numerators of a key tile five more instructions; the tile's 128 x D values
 // cost twelve instructions per 16 instead, in warps of their own, and P goes as f16 (11 bits).  The block exponents come
@@ -17,6 +17,12 @@
 // r (see kRefWindow) is chosen per key tile by the loading warp.  A tile whose own pages differ by more than the
 // window allows ("wild") is handed over 32 keys at a time, O rescaled in between.
 // Key splits leave (m, l, r, O) in a workspace; join_kernel joins them.
+// What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 641 us, 1470 TFLOP/s.  A key tile takes the two query tiles
+// 2950 cycles, 2048 of them products: a query tile's softmax (1600) and the wait for its next S take turns, since P lies over S
+// and tensor memory is full (S, O of two tiles).  A CTA starts and ends in ~16000 cycles, which is what causal prompts
+// (6 of 63 to 4001 tokens, 32 heads: 245 us) and windows pay for.
+// Measured and left: an MMA warp for each query tile (their products then interleave: 821 us), looking for the next hand-over
+// between products (712), four converting warps at 88 registers (677), keys handed over as 112 + 16 (701).
 // The pipeline, its barriers and the lazily raised running maximum are those of the chunk attention over packed views.
 #include "fk_paged.h"
 #include "fk_tc.h"
@@ -575,7 +581,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       // A tile goes in two parts, keys 0-95 and 96-127 (a wild one 32 keys at a time).  On full tiles, P is
       // computed with the running max m straight away; a part with a weight beyond 2^8 (2^15 as stored) is
       // done again with a max pass, which raises m.  One copy of that general path serves all parts: with one for each,
-      // the loop outgrew the instruction cache (480P chunk 716 -> 604 us without the wild tiles' copy).
+      // the loop outgrew the instruction cache (a copy for wild tiles alone cost a sixth).
       const int parts = wild ? 4 : 2;
 #pragma unroll 1
       for (int part = 0; part < parts; ++part) {
