@@ -872,9 +872,9 @@ def run_stack(local_rank, attn_precision="bf16"):
 # removed) the capture was taken on: a figure is reported only while that code is unchanged.
 NCU_TRAFFIC = {
     "480p_layer": {
-        "attend": ("fk_attn.cu", "90b07b56a988", 118980000),
-        "attend_fp8": ("fk_attn.cu", "90b07b56a988", 92110000),
-        "attend_fp8pv": ("fk_attn.cu", "90b07b56a988", 65890000),
+        "attend": ("fk_attn.cu+fk_tc.h", "357086293c20+a7e18a81f3ae", 118980000),
+        "attend_fp8": ("fk_attn.cu+fk_tc.h", "357086293c20+a7e18a81f3ae", 92110000),
+        "attend_fp8pv": ("fk_attn.cu+fk_tc.h", "357086293c20+a7e18a81f3ae", 65890000),
         "append": ("fk_copy.cu", "e3a1045fec8c", 54790000),
         "compact": ("fk_copy.cu", "e3a1045fec8c", 58560000),
         "score": ("fk_score.cu", "1bc903628fd4", 35970000),
@@ -901,8 +901,8 @@ def _code_hash(path):
 def _traffic(workload):
     out = {}
     for kind, (src, sha, nbytes) in NCU_TRAFFIC.get(workload, {}).items():
-        path = os.path.join(ROOT, "paper_2605_09681_gb300", "csrc", src)
-        cur = _code_hash(path) if os.path.exists(path) else ""
+        paths = [os.path.join(ROOT, "paper_2605_09681_gb300", "csrc", f) for f in src.split("+")]
+        cur = "+".join(_code_hash(p) if os.path.exists(p) else "" for p in paths)
         out[kind] = nbytes if cur == sha else None
     return out
 
