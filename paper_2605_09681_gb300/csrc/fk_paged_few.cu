@@ -431,11 +431,35 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
   __syncthreads();
   if (!bar->last) return;
-  // each row's weights 2^(m - M) 2^(r - RR), first (row by row, a warp each), then the sums
+  // each row's weights 2^(m - M) 2^(r - RR), first (row by row, a warp each), then the sums.  What both need of the workspace
+  // is asked for at once: its numbers of the first 32 splits, and the first twelve runs of a thread's sum.
   float* wts = reinterpret_cast<float*>(smem);          // [row][split]
-  for (int row = warp; row < rows; row += kWarps + 1) {
-    float M = kLowest, RR = (float)kNoRef, L = 0.0f;
-    for (int sp = lane; sp < n_splits; sp += 32) {
+  constexpr int kRowsEach = (kRows + kWarps) / (kWarps + 1), kFly = 12;
+  float4 e0[kRowsEach];
+#pragma unroll
+  for (int k = 0; k < kRowsEach; ++k) {
+    const int row = warp + k * (kWarps + 1);
+    e0[k] = row < rows && lane < n_splits ? __ldcg(mls + (first + lane) * kPagedFewRows + row) : make_float4(kLowest, 0.0f, (float)kNoRef, 0.0f);
+  }
+  // A place (row, run) is summed by `sets` threads, each over every sets-th split, twelve loads in flight.
+  const int places = rows * kRuns, sets = max(1, kFewThreads / places);
+  const int set = sets > 1 ? (int)threadIdx.x / places : 0, i_first = sets > 1 ? (int)threadIdx.x % places : (int)threadIdx.x;
+  float4 x[kFly];
+  auto ask = [&](int i, int sp0) {
+    const float4* src = part + ((int64_t)first * kPagedFewRows + i / kRuns) * kRuns + i % kRuns;
+#pragma unroll
+    for (int k = 0; k < kFly; ++k) {
+      const int sp = sp0 + k * sets;
+      if (sp < n_splits) x[k] = __ldcg(src + (int64_t)sp * kPagedFewRows * kRuns);
+    }
+  };
+  if (i_first < places && set < sets) ask(i_first, set);
+#pragma unroll
+  for (int k = 0; k < kRowsEach; ++k) {
+    const int row = warp + k * (kWarps + 1);
+    if (row >= rows) break;
+    float M = e0[k].x, RR = e0[k].z, L = 0.0f;
+    for (int sp = lane + 32; sp < n_splits; sp += 32) {
       const float4 e = __ldcg(mls + (first + sp) * kPagedFewRows + row);
       M = fmaxf(M, e.x);
       RR = fmaxf(RR, e.z);
@@ -446,7 +470,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       RR = fmaxf(RR, __shfl_xor_sync(0xffffffffu, RR, off));
     }
     for (int sp = lane; sp < n_splits; sp += 32) {
-      const float4 e = __ldcg(mls + (first + sp) * kPagedFewRows + row);
+      const float4 e = sp == lane ? e0[k] : __ldcg(mls + (first + sp) * kPagedFewRows + row);
       const float f = fast_exp2(e.x - M);
       L = fmaf(f, e.y, L);
       wts[row * n_splits + sp] = f * pow2_any((int)(e.z - RR));
@@ -456,25 +480,19 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     if (lane == 0) sl[0][row] = L > 0.0f || L != L ? pow2_any((int)RR) / L : 0.0f;
   }
   __syncthreads();
-  // A place (row, run) is summed by `sets` threads, each over every sets-th split, sixteen loads in flight.
-  const int places = rows * kRuns, sets = max(1, kFewThreads / places);
   float4* sums = reinterpret_cast<float4*>(smem + kMaxFewSplits * kPagedFewRows * 4);     // [set][place]
 #pragma unroll 1
   for (int i0 = 0; i0 < places; i0 += kFewThreads) {
-    const int i = i0 + (sets > 1 ? (int)threadIdx.x % places : (int)threadIdx.x), set = sets > 1 ? (int)threadIdx.x / places : 0;
+    const int i = i0 + i_first;
     const bool mine = i < places && set < sets;
     const int row = i / kRuns, c = i % kRuns;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (mine) {
-      const float4* src = part + ((int64_t)first * kPagedFewRows + row) * kRuns + c;
 #pragma unroll 1
-      for (int sp = set; sp < n_splits; sp += 16 * sets) {
-        float4 x[16];
+      for (int sp = set; sp < n_splits; sp += kFly * sets) {
+        if (i0 > 0 || sp > set) ask(i, sp);
 #pragma unroll
-        for (int k = 0; k < 16; ++k)
-          if (sp + k * sets < n_splits) x[k] = __ldcg(src + (int64_t)(sp + k * sets) * kPagedFewRows * kRuns);
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
+        for (int k = 0; k < kFly; ++k)
           if (sp + k * sets < n_splits) {
             const float f = wts[row * n_splits + sp + k * sets];
             acc.x = fmaf(f, x[k].x, acc.x);
@@ -489,8 +507,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       __syncthreads();
       if (mine && set == 0)
         for (int k = 1; k < sets; ++k) {
-          const float4 x = sums[k * places + i];
-          acc = make_float4(acc.x + x.x, acc.y + x.y, acc.z + x.z, acc.w + x.w);
+          const float4 y = sums[k * places + i];
+          acc = make_float4(acc.x + y.x, acc.y + y.y, acc.z + y.z, acc.w + y.w);
         }
     }
     if (mine && set == 0) {
