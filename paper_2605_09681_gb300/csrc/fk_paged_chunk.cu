@@ -58,7 +58,7 @@ struct ChunkBarriers {
   uint64_t v8_full[2], v8_empty[2]; // V codes
   uint64_t vf_full[2], vf_empty[2]; // f16 values
   uint64_t s_full[2], p_full[2], pa_full[2], pva_done[2];
-  uint64_t o_done, fin;
+  uint64_t o_done[2], fin;
   volatile uint32_t tmem_base;
   int n_info;                       // key tiles whose ChunkInfo has been written
   volatile int abort;
@@ -252,7 +252,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         mbar_init(&bar->pa_full[i], 4);
         mbar_init(&bar->pva_done[i], 1);
       }
-      mbar_init(&bar->o_done, 1);
+      mbar_init(&bar->o_done[0], 1);
+      mbar_init(&bar->o_done[1], 1);
       mbar_init(&bar->fin, 1);
       bar->abort = 0;
       bar->n_info = 0;
@@ -280,7 +281,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                    a.Q + ((int64_t)q0 + tok) * a.qstride + (int64_t)(kvh * a.G + at - tok * a.G) * D + c * 8);
     }
   }
-  __syncthreads();
+  // The loading warp, which has set the barriers up, goes on at once; the others come when the copies are on their way.
+  if (warp == kWarpTma) {
+    __syncwarp();
+    asm volatile("bar.arrive 2, %0;" :: "n"(kChunkThreads) : "memory");
+  } else {
+    asm volatile("bar.sync 2, %0;" :: "n"(kChunkThreads) : "memory");
+  }
 
   // softmax state (warps 0-7)
   float m = kNoMax, l = 0.0f;
@@ -415,6 +422,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         if (elect_one()) {
           if (!wild) pv(j, tt, 3, 4);
           if (more) qk(j + kAhead, tt);
+          else umma_commit(&bar->o_done[tt]);
           if (i == kTiles - 1) {
             umma_commit(&bar->vf_empty[b]);
             if (more) umma_commit(&bar->k_empty[(j + kAhead) % kKStages]);
@@ -423,7 +431,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       }
     }
     if (elect_one()) {
-      if (ok) umma_commit(&bar->o_done);
+      if (nt == 0) umma_commit(&bar->o_done[0]);
+      if (nt <= (kOne ? 1 : 0)) umma_commit(&bar->o_done[1]);
       umma_commit(&bar->fin);                       // completes once every MMA above is done
     }
     wait_phase(&bar->fin, 0, bar, a.status, false);
@@ -479,7 +488,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       __syncwarp();
       const uint8_t* src = sV + (t * kBM + row) * (D * 2);
       uint32_t top = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (int j = 0; j < D / 8; ++j) {
         const uint4 v = *reinterpret_cast<const uint4*>(src + ((j ^ (row & 7)) << 4));
         top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
@@ -490,18 +499,31 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       if (!kOne || t == 0) {
         const float scale = in ? pow2f(-e) : 0.0f;
         uint8_t* dst = sQ + (kOne ? 0 : t) * (2 * Lay::kQ);
-#pragma unroll 2
-        for (int j = 0; j < D / 8; ++j) {
-          const int c = j ^ (row & 7);
-          const uint4 v = in ? *reinterpret_cast<const uint4*>(src + (c << 4)) : make_uint4(0, 0, 0, 0);
-          uint16_t h[4], g[4];
-          split2(v.x, scale, h[0], g[0]);
-          split2(v.y, scale, h[1], g[1]);
-          split2(v.z, scale, h[2], g[2]);
-          split2(v.w, scale, h[3], g[3]);
-          uint8_t* to = dst + code_run<D>(row, c >> 1) + (c & 1) * 8;
-          *reinterpret_cast<uint2*>(to) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-          *reinterpret_cast<uint2*>(to + Lay::kQ) = make_uint2(g[0] | (uint32_t)g[1] << 16, g[2] | (uint32_t)g[3] << 16);
+        constexpr int kFly = 4;                      // (loads would not pass the stores by themselves)
+#pragma unroll 1
+        for (int j0 = 0; j0 < D / 8; j0 += kFly) {
+          uint4 v[kFly];
+          uint2 hi[kFly], lo[kFly];
+#pragma unroll
+          for (int k = 0; k < kFly; ++k)
+            v[k] = in ? *reinterpret_cast<const uint4*>(src + (((j0 + k) ^ (row & 7)) << 4)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int k = 0; k < kFly; ++k) {
+            uint16_t h[4], g[4];
+            split2(v[k].x, scale, h[0], g[0]);
+            split2(v[k].y, scale, h[1], g[1]);
+            split2(v[k].z, scale, h[2], g[2]);
+            split2(v[k].w, scale, h[3], g[3]);
+            hi[k] = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+            lo[k] = make_uint2(g[0] | (uint32_t)g[1] << 16, g[2] | (uint32_t)g[3] << 16);
+          }
+#pragma unroll
+          for (int k = 0; k < kFly; ++k) {
+            const int c = (j0 + k) ^ (row & 7);
+            uint8_t* to = dst + code_run<D>(row, c >> 1) + (c & 1) * 8;
+            *reinterpret_cast<uint2*>(to) = hi[k];
+            *reinterpret_cast<uint2*>(to + Lay::kQ) = lo[k];
+          }
         }
       }
       if (fine) sl2 *= pow2f(e);
@@ -712,8 +734,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       }
     }
     // ---------------------------------------------------------------- epilogue
-    // every MMA is done, so the operand tiles' shared memory is free
-    ok = ok && warp_wait(&bar->o_done, 0, bar, a.status);
+    // This accumulator's last MMA is done, and with it every MMA that reads Q: that shared memory is free.
+    ok = ok && warp_wait(&bar->o_done[t], 0, bar, a.status);
     tc_fence_after();
     const bool has = kOne ? t < nt : nt > 0;        // this accumulator was written
     const int row0 = bar->row0, rows = bar->rows, kvh = bar->kvh, n_splits = bar->n_splits;
@@ -757,6 +779,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         }
       }
     } else {
+      ok = ok && warp_wait(&bar->o_done[t ^ 1], 0, bar, a.status);   // all operand tiles are free
       // both accumulators to shared memory, [t][row][D] with 16-byte run c of a row at c ^ (row & 7), and their (m, l, r)
       float* so = reinterpret_cast<float*>(smem) + (t * kBM + row) * D;
       float4* ml = reinterpret_cast<float4*>(smem + 2 * kBM * D * 4);
