@@ -587,20 +587,39 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       };
       const int key0 = ti.key0;
       const bool full = trow1 < 0 || (key0 + kBN <= full_hi && (key0 >= full_lo || key0 + kBN <= a.mask.sinks));
-      bool direct = full && it > 0 && rs == 1.0f && !wild;   // uniform over the warpgroup
+      const bool keeps = it > 0 && rs == 1.0f && !wild;   // uniform over the warpgroup
+      bool direct = full && keeps;
       if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
       tc_fence_after();
       uint32_t ca[32], cb[32], ov = 0;
-      if (it == 0 && full && !wild) {               // the first tile: m from its first 32 keys
-        FK_TMEM_LD32(tS, ca);
+      if (!full) {                                  // masked keys' logits become -inf, in place
+        auto below = [](int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; };
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          const int k0 = key0 + 32 * c;
+          const uint32_t seen = below(limit - k0) & (~below(lower - k0) | below(a.mask.sinks - k0));
+          if (__all_sync(0xffffffffu, seen == ~0u)) continue;
+          FK_TMEM_LD32(tS + c * 32, ca);
+          FK_TMEM_WAIT_LD32(ca);
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (!(seen >> i & 1u)) ca[i] = __float_as_uint(-INFINITY);
+          FK_TMEM_ST32(tS + c * 32, ca);
+        }
+        tmem_wait_st();
+        direct = keeps;
+      }
+      if (it == 0 && !wild) {                       // the first tile: m from 32 of its keys, at its end where a window begins in it
+        const int c = key0 >= full_lo || key0 < a.mask.sinks ? 0 : 3;
+        FK_TMEM_LD32(tS + c * 32, ca);
         FK_TMEM_WAIT_LD32(ca);
         float mxa[4] = {kNoMax, kNoMax, kNoMax, kNoMax};
 #pragma unroll
         for (int i = 0; i < 32; ++i) mxa[i & 3] = fmaxf(mxa[i & 3], __uint_as_float(ca[i]));
-        m = fmaxf(fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * fc[0], kNoMax);
+        m = fmaxf(fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * factor_at(c), kNoMax);
         direct = true;
       }
-      // A tile goes in two parts, keys 0-95 and 96-127 (a wild one 32 keys at a time).  On full tiles, P is
+      // A tile goes in two parts, keys 0-95 and 96-127 (a wild one 32 keys at a time).  P is
       // computed with the running max m straight away; a part with a weight beyond 2^8 (2^15 as stored) is
       // done again with a max pass, which raises m.  One copy of that general path serves all parts: with one for each,
       // the loop outgrew the instruction cache (a copy for wild tiles alone cost a sixth).
@@ -660,15 +679,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           } else if (part > 0) {
             rs = 1.0f;
           }
-          auto load_chunk = [&](int c) {             // logits of a chunk, masked keys -inf
+          auto load_chunk = [&](int c) {             // logits of a chunk
             FK_TMEM_LD32(tS + c * 32, ca);
             FK_TMEM_WAIT_LD32(ca);
-            if (!full) {
-              const int k0 = key0 + c * 32, hi = limit - k0, lo = lower - k0, si = a.mask.sinks - k0;
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (i >= hi || (i < lo && i >= si)) ca[i] = __float_as_uint(-INFINITY);
-            }
           };
           float mx = -INFINITY;
 #pragma unroll 1
