@@ -394,6 +394,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       for (int i = 0; i < kTiles; ++i) {
         const int tt = kOne ? b : i;
         uint32_t& np = tt ? n_pa[1] : n_pa[0];
+        if (kOne && j > 0 && !wait(&bar->vf_full[b], (j >> 1) & 1)) { ok = false; break; }
         if (!wild) {
           if (!wait(&bar->pa_full[tt], np++ & 1)) { ok = false; break; }
           tc_fence_after();
@@ -416,7 +417,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         // K for the tile's S before the second part, the next V before the last one: neither has anything left to
         // hide behind between a tile's S and the next tile's P (a wait takes ~100 cycles when there is nothing to wait for)
         if (i == 0 && more && !k_ready(j + kAhead)) { ok = false; break; }
-        if (i == kTiles - 1 && j + 1 < nt && !wait(&bar->vf_full[b ^ 1], ((j + 1) >> 1) & 1)) { ok = false; break; }
+        // (kOne: its values are not there yet, and cannot be while this tile's products wait: it is looked for later.)
+        if (!kOne && i == kTiles - 1 && j + 1 < nt && !wait(&bar->vf_full[b ^ 1], ((j + 1) >> 1) & 1)) { ok = false; break; }
         if (!wait(&bar->p_full[tt], ph)) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
@@ -440,7 +442,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   } else if (warp >= kWarpConv) {
     // ------------------------------------------------------------------ V codes -> f16 values
     // A thread takes 8 codes of a row at a time: half a 16-byte run, one 16-byte unit of the f16 row.
-    constexpr int kOct = D / 8, kStepRows = 64 / kOct, kFly = 8;   // units of a row; rows per pass; loads in flight
+    constexpr int kOct = D / 8, kStepRows = 64 / kOct, kFly = 16;   // units of a row; rows per pass; loads in flight
     ok = nt == 0 || warp_wait(&bar->q_ready, 0, bar, a.status);   // (the query rows were staged where the values go)
     const int x = threadIdx.x - kWarpConv * 32, prow = x / kOct, unit = x % kOct;
     for (int j = 0; j < nt && ok; ++j) {
