@@ -193,7 +193,8 @@ void fill_seqs(const fk_paged* h, size_t i0, size_t i1, bool whole, bool read, i
 // ---- plans of an attention
 // Estimated times, in us, of what a CTA takes for a key tile (D = 128) with the device full of such CTAs, and of its start and end;
 // `slots` such CTAs fit an SM.  Measured back to back with 16 to 256 rows, 1000 to 16000 keys, 1 to 64 sequences and 2 to 8 kv heads;
-// the plans barely depend on them (`fixed` of the chunks a third lower: the same times).
+// the plans barely depend on them (`fixed` of the chunks a sixth or a third lower: one of 36 drawn steps changed by more than 5%,
+// for the worse).
 struct Shape {
   int rows, tile, slots;
   double per_tile, fixed;
@@ -377,31 +378,39 @@ void plan_group(const fk_paged* h, const PagedAttnArgs& a, size_t i, size_t i1, 
     return best;
   };
   PagedAttnSeqs part[2];
-  int upto = 0;
+  struct {
+    int upto = 0;
+    Candidate few, chunk;
+    Shape shape = kChunk2;
+  } best;
   double us = 1e30;
   for (int t : {16, 32, 64, 128}) {                           // the few-row kernel's (16 rows it always takes)
     Shape sh = kChunk2;
+    Candidate few, chunk;
     take(0, t, part[0]);
     take(t, INT32_MAX, part[1]);
-    const double x = (part[0].n ? few_plan(part[0]).us : 0.0) + (part[1].n ? chunk_plan(part[1], &sh).us : 0.0);
+    if (part[0].n) few = few_plan(part[0]);
+    if (part[1].n) chunk = chunk_plan(part[1], &sh);
+    const double x = (part[0].n ? few.us : 0.0) + (part[1].n ? chunk.us : 0.0);
     if (x < us) {
       us = x;
-      upto = t;
+      best.upto = t;
+      best.few = few;
+      best.chunk = chunk;
+      best.shape = sh;
     }
     if (t >= most) break;
   }
-  take(0, upto, part[0]);
-  take(upto, INT32_MAX, part[1]);
+  take(0, best.upto, part[0]);
+  take(best.upto, INT32_MAX, part[1]);
   if (part[0].n) {
     const Shape sh = few_of(part[0]);
-    lay_out(a, part[0], sh, few_plan(part[0]).per);
+    lay_out(a, part[0], sh, best.few.per);
     out->push_back({false, sh.rows / 8, part[0]});
   }
   if (part[1].n) {
-    Shape sh = kChunk2;
-    const Candidate c = chunk_plan(part[1], &sh);
-    if (!split_the_rest(h, a, part[1], sh)) lay_out(a, part[1], sh, c.per);
-    out->push_back({true, sh.rows / kAttnBM, part[1]});
+    if (!split_the_rest(h, a, part[1], best.shape)) lay_out(a, part[1], best.shape, best.chunk.per);
+    out->push_back({true, best.shape.rows / kAttnBM, part[1]});
   }
 }
 
