@@ -854,27 +854,30 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
 // 128 rows by itself.)  With M = max m, R = max r: O = 2^R sum 2^(m - M) 2^(r - R) O_s / sum 2^(m - M) l_s.
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ PagedAttnArgs a, int tiles) {
-  constexpr int kRuns = D / 4, kFly = 8;
+  constexpr int kRuns = D / 4, kFly = 4;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t place = (int64_t)blockIdx.x * 8 + warp;          // row of the split items' rows
+  const int place = (int)blockIdx.x * 8 + warp, shift = tiles == 2 ? 8 : 7;   // row of the split items' rows; tiles 128 = 2^shift
+  static_assert(kBM == 128, "shift");
   int s = 0;
   for (int hi = a.seqs.n - 1; s < hi;) {
     const int mid = (s + hi + 1) >> 1;
-    if (a.seqs.join0[mid] <= (int)(place / (tiles * kBM))) s = mid;
+    if (a.seqs.join0[mid] <= place >> shift) s = mid;
     else hi = mid - 1;
   }
   // `pair` counts the (rows, kv head) pairs of the sequence as the chunk kernel does, unsplit ones first
   const int n_splits = a.seqs.splits[s], whole = a.seqs.whole[s], n_rows = a.seqs.n_q[s] * a.G;
-  const int groups = (n_rows + tiles * kBM - 1) / (tiles * kBM);
-  const int split_pair = (int)(place / (tiles * kBM)) - a.seqs.join0[s], r = (int)(place % (tiles * kBM));
+  const int groups = (n_rows + tiles * kBM - 1) >> shift;
+  const int split_pair = (place >> shift) - a.seqs.join0[s], r = place & (tiles * kBM - 1);
   const int pair = whole + split_pair, kvh = pair % a.Hkv, row = (groups - 1 - pair / a.Hkv) * (tiles * kBM) + r;
   if (s >= a.seqs.n || pair >= groups * a.Hkv || row >= n_rows) return;
   const float4* part = reinterpret_cast<const float4*>(a.part);
   const float4* mls = part + (int64_t)a.part_tiles * kBM * kRuns;
   const int64_t first = ((int64_t)a.seqs.part0[s] + (int64_t)split_pair * n_splits * tiles) * kBM + r;   // split 0's row
   const int64_t next = (int64_t)tiles * kBM;
-  float M = kNoMax, R = (float)kNoRef, L = 0.0f;
-  for (int sp = lane; sp < n_splits; sp += 32) {
+  // (m, l, r) of the first 32 splits are asked for once
+  const float4 e0 = lane < n_splits ? __ldcg(mls + first + lane * next) : make_float4(kNoMax, 0.0f, (float)kNoRef, 0.0f);
+  float M = e0.x, R = e0.z, L = 0.0f;
+  for (int sp = lane + 32; sp < n_splits; sp += 32) {
     const float4 e = __ldcg(mls + first + sp * next);
     M = fmaxf(M, e.x);
     R = fmaxf(R, e.z);
@@ -888,7 +891,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Paged
   for (int s0 = 0; s0 < n_splits; s0 += 32) {        // weights of 32 splits, a lane each
     float w = 0.0f;
     if (s0 + lane < n_splits) {
-      const float4 e = __ldcg(mls + first + (s0 + lane) * next);
+      const float4 e = s0 == 0 ? e0 : __ldcg(mls + first + (s0 + lane) * next);
       const float f = fast_exp2(e.x - M);
       L = fmaf(f, e.y, L);
       w = f * pow2_any((int)(e.z - R));
