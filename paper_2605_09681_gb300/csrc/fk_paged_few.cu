@@ -18,10 +18,10 @@
 //   scales    e_k is in the factor of the exponent and e_v - r in its summand (r: see kRefWindow), so no key or value
 //             is scaled.  m is raised only when a row outgrows it by 2^4: a vote finds that no row does, without a maximum
 //             over lanes, and O is seldom rescaled.
-// What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 52 us, 5.1 TB/s, where
-// reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 82.5 us, 5.9 TB/s (76.4).  With
-// little to read the launch and the join do: one token of 12 heads over 1561 keys 6.9 us.  At 16 rows its products and
-// conversions bound it: 4 warps issue every cycle that they can.
+// What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 50 us, 5.3 TB/s, where
+// reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 82.3 us, 5.9 TB/s (76.4).  With
+// little to read the launch and the join do: one token of 12 heads over 1561 keys 6.7 us.  At 16 rows its products and
+// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 15.0 us).
 // Splits leave (m, l, r, O) in a workspace; the last one to arrive joins them in the order of the splits (no atomics on
 // values: results do not change from run to run).
 #include "fk_paged.h"
