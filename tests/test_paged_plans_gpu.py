@@ -138,3 +138,31 @@ def test_a_query_that_is_not_finite_stays_in_its_head(bad, nq):
     o[at, 1] = plain[at, 1]
     assert np.isfinite(o).all()
     assert (np.abs(o - plain) <= 2 * T._bound(plain, held[0][1])).all()
+
+
+def test_pages_beyond_four_gigabytes():
+    """A page's codes whose offset does not fit 32 bits: 2 MB a page (128 heads of 128, 128 tokens), 2112 pages taken before."""
+    H, D, page, fill = 128, 128, 128, 8192
+    r = np.random.default_rng(78)
+    some = T._normal(r, (64, H, D), 0.3)
+    lens = [300, 40]
+    K, V = T._normal(r, (300, H, D), 0.3), T._normal(r, (300, H, D))
+    with T._cache(n_q_heads=H, n_kv_heads=H, head_dim=D, page_tokens=page, max_seqs=3, n_pages=2112 + 4,
+                  max_seq_tokens=33 * fill) as cache:
+        x = T._bf16(some).repeat(fill // 64, 1, 1)
+        for _ in range(33):
+            cache.step([0], [fill])
+            cache.append(0, x, x)
+        for seq, nq in ((1, 300), (2, 1)):
+            n = lens[seq - 1]
+            cache.step([seq], [n], [nq])
+            cache.append(0, T._bf16(K[:n]), T._bf16(V[:n]))
+            hk, hv = cache.read(0, whole=True)
+            k, v = P.held(K[:n], page), P.held(V[:n], page)
+            assert np.array_equal(T._np(hk), k) and np.array_equal(T._np(hv), v)
+            Q = T._normal(r, (nq, H, D), 0.5)
+            out = T._np(cache.attend(0, T._bf16(Q)))
+            for h in (0, 57, 127):
+                want = P.attention(Q[:, h: h + 1], k[:, h: h + 1], v[:, h: h + 1], True, 0, 0)
+                assert (np.abs(out[:, h: h + 1] - want) <= T._bound(want, v)).all(), (seq, h)
+        assert cache.free_pages() == 0 and cache.sync_status() == 0
