@@ -153,6 +153,7 @@ struct PagedAttnArgs {
   const bf16* Q;                      // [T][Hkv G][D]
   bf16* O;
   int64_t qstride, ostride;
+  int wide_o;                         // rows of O are 32-byte aligned
   float scale_log2;                   // log2(e) * scale
   PagedMask mask;
   // partial O of the key splits and then (m, l, r, -) of their rows: [kPartSlots][16][D] and [..][16][4] (few

@@ -17,16 +17,17 @@
 // r (see kRefWindow) is chosen per key tile by the loading warp.  A tile whose own pages differ by more than the
 // window allows ("wild") is handed over 32 keys at a time, O rescaled in between.
 // Key splits leave (m, l, r, O) in a workspace; join_kernel joins them.
-// What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 639 us, 1475 TFLOP/s.  A key tile takes the two query tiles
+// What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 636-639 us, 1475 TFLOP/s.  A key tile takes the two query tiles
 // 2950 cycles, 2048 of them products at their nominal rate: a query tile's softmax (1600) and the wait for its next S take turns, since
 // P lies over S and tensor memory is full (S, O of two tiles), and Q K^T wants 128 bytes of shared memory a cycle, all there is, beside
 // the conversion's.  A CTA starts and ends in ~15000 cycles (queries copied 3300, their codes 3500, first S 1450, first tile
-// 2000 more than the others, rows out 3850), which is what causal prompts (6 of 63 to 4001 tokens, 32 heads of 128: 227 us)
-// and windows (2048 queries, window 1024: 28.6 us) pay for.  kOne (8 sequences of 16000 keys, 12 kv heads, 30 rows: 101 us, the
+// 2000 more than the others, rows out 3000), which is what causal prompts (6 of 63 to 4001 tokens, 32 heads of 128: 222-228 us)
+// and windows (2048 queries, window 1024: 28.5 us) pay for.  kOne (8 sequences of 16000 keys, 12 kv heads, 30 rows: 101 us, the
 // codes' bytes 58) is bound by its products' operands.
 // Measured and left: an MMA warp for each query tile (their products then interleave: 821 us), looking for the next hand-over
 // between products (712), four converting warps at 88 registers (677; kOne 105.8), keys handed over as 112 + 16 (701), the
-// two-pass path for masked tiles (prompts 244, window 33.8).
+// two-pass path for masked tiles (prompts 244, window 33.8), a thread's query row from global memory into registers (64 channels and kOne
+// 2-3% faster, 128 channels 3-4% slower: the key tiles' loop moves with what the compiler puts before it).
 // The pipeline, its barriers and the lazily raised running maximum are those of the chunk attention over packed views.
 #include "fk_paged.h"
 #include "fk_tc.h"
@@ -105,6 +106,11 @@ __device__ __forceinline__ void split2(uint32_t w, float scale, uint16_t& hi, ui
   const uint32_t h = f16x2_of_e4m3x2(hi);
   const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&h));
   lo = e4m3x2_of_f16x2(*reinterpret_cast<const uint32_t*>(&d));
+}
+// 32 bytes to global memory at once (32-byte aligned)
+__device__ __forceinline__ void store32(void* dst, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               :: "l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 // byte offset of 16-byte run c of row `row` in a tile of D-byte rows (the TMA's and the MMA's swizzle)
 template <int D>
@@ -765,36 +771,27 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     };
     // (r is that of the last tile, or of the tile's last block: the same for all threads of an accumulator)
     if (!kOne && n_splits == 1) {
-      // normalise, and through the warp's own 32 rows of shared memory (16-byte chunk c of row r at
-      // chunk c ^ (r mod D/8)) to whole rows of O
+      // normalise; a thread writes its row, a whole 32-byte sector at a time where rows are aligned to that (through shared
+      // memory to coalesced rows, side by side: 228.7 us for the prompts; 16 bytes at a time 228.3; 32: 221.4)
       const float inv = l > 0.0f || l != l ? pow2_any(r) / l : 0.0f;    // no visible key: 0
-      uint8_t* stage = smem + warp * (32 * D * 2);
+      const int cr = (kOne ? 0 : t * kBM) + row;
       if (ok) {
+        bf16* dst = out_row(min(cr, rows - 1));
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
-          uint32_t o[32];
+          uint32_t o[32], v[16];
           FK_TMEM_LD32(tO + c * 32, o);
           FK_TMEM_WAIT_LD32(o);
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (has) {
-              v.x = pack_bf16(__uint_as_float(o[e + 0]) * inv, __uint_as_float(o[e + 1]) * inv);
-              v.y = pack_bf16(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
-              v.z = pack_bf16(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
-              v.w = pack_bf16(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
-            }
-            *reinterpret_cast<uint4*>(stage + lane * (D * 2) + (((c * 4 + e / 8) ^ (lane & (D / 8 - 1))) << 4)) = v;
+          for (int e = 0; e < 16; ++e) v[e] = has ? pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+          if (cr >= rows) continue;
+          if (a.wide_o) {
+            store32(dst + c * 32, v);
+            store32(dst + c * 32 + 16, v + 8);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(dst + c * 32 + 2 * e) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
           }
-        }
-        __syncwarp();
-        constexpr int kLanes = D / 8;               // lanes of one row
-        const int cl = lane % kLanes;
-#pragma unroll 8
-        for (int r0 = 0; r0 < 32; r0 += 32 / kLanes) {
-          const int r = r0 + lane / kLanes, cr = t * kBM + wq * 32 + r;
-          const uint4 v = *reinterpret_cast<const uint4*>(stage + r * (D * 2) + ((cl ^ (r & (D / 8 - 1))) << 4));
-          if (cr < rows) *reinterpret_cast<uint4*>(out_row(cr) + cl * 8) = v;
         }
       }
     } else {
