@@ -415,7 +415,9 @@ class PagedKVCache:
             if Q_out is None:
                 import torch
                 Q_out = torch.empty_like(Q)          # (dense: rows of a wider tensor are not kept apart)
-            o, os = self._rows(Q_out, self._new, self.n_q_heads, "Q_out")
+                o, os = Q_out.data_ptr(), self.n_q_heads * self.head_dim
+            else:
+                o, os = self._rows(Q_out, self._new, self.n_q_heads, "Q_out")
         _check(self._lib.fk_paged_append(self._h, layer, k, ks, v, vs, rope, q, qs, o, os, self._on(stream)),
                "fk_paged_append")
         return Q_out
@@ -426,11 +428,15 @@ class PagedKVCache:
         none gives 0.  scale: default 1 / sqrt(head_dim)."""
         if scale is not None and not scale > 0:
             raise ValueError("scale must be positive")
+        if window >= 2 ** 31 or sinks >= 2 ** 31:
+            raise ValueError("window, sinks: at most 2^31 - 1")
         q, qs = self._rows(Q, self._queries, self.n_q_heads, "Q")
         if O is None:
             import torch
             O = torch.empty_like(Q)
-        o, os = self._rows(O, self._queries, self.n_q_heads, "O")
+            o, os = O.data_ptr(), self.n_q_heads * self.head_dim
+        else:
+            o, os = self._rows(O, self._queries, self.n_q_heads, "O")
         _check(self._lib.fk_paged_attend(self._h, layer, q, qs, o, os, 1 if causal else 0, window, sinks,
                                          0.0 if scale is None else scale, self._on(stream)), "fk_paged_attend")
         return O
@@ -445,15 +451,17 @@ class PagedKVCache:
             if st != L.FK_OK and count.value == 0:
                 _check(st, "fk_paged_read")
             n = self._held[whole] = count.value
+        for x in (K, V):
+            if x is not None:
+                self._rows(x, n, self.n_kv_heads, "K, V")
+                if not x.is_contiguous():
+                    raise ValueError("K, V: expected contiguous tensors")
         if K is None or V is None:
             import torch
             shape = (n, self.n_kv_heads, self.head_dim)
             K = torch.empty(shape, dtype=self._bf16, device=self._dev) if K is None else K
             V = torch.empty(shape, dtype=self._bf16, device=self._dev) if V is None else V
-        k, _ = self._rows(K, n, self.n_kv_heads, "K")
-        v, _ = self._rows(V, n, self.n_kv_heads, "V")
-        if not K.is_contiguous() or not V.is_contiguous():
-            raise ValueError("K, V: expected contiguous tensors")
+        k, v = K.data_ptr(), V.data_ptr()
         _check(self._lib.fk_paged_read(self._h, layer, 1 if whole else 0, k, v, n, self._count, self._on(stream)),
                "fk_paged_read")
         return K, V

@@ -675,7 +675,8 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
     a->ostride = o_stride;
     a->wide_o = aligned(O, 32) && o_stride % 16 == 0;
     a->scale_log2 = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)c.head_dim)));
-    a->mask = {causal, window, window > 0 ? sinks : 0};
+    // (no sequence is longer than 2^30, and a position before the first key less a wider window would not fit)
+    a->mask = {causal, std::min(window, 1 << 30), window > 0 ? sinks : 0};
     a->part_tiles = h->part_tiles;
     a->arrived = h->arrived;
     a->status = h->status;

@@ -166,3 +166,41 @@ def test_pages_beyond_four_gigabytes():
                 want = P.attention(Q[:, h: h + 1], k[:, h: h + 1], v[:, h: h + 1], True, 0, 0)
                 assert (np.abs(out[:, h: h + 1] - want) <= T._bound(want, v)).all(), (seq, h)
         assert cache.free_pages() == 0 and cache.sync_status() == 0
+
+
+@pytest.mark.parametrize("nq", [3, 200])
+def test_the_widest_window_is_none(nq):
+    """Queries before the first key: their position less the window would not fit 32 bits."""
+    lens = [2]
+    cache, Q, held = _filled(np.random.default_rng(79), (4, 2), 128, 64, lens, [nq])
+    with cache:
+        q = T._bf16(Q)
+        plain = cache.attend(0, q)
+        for window, sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 30, 5)):
+            assert torch.equal(cache.attend(0, q, window=window, sinks=sinks), plain), window
+        _check(T._np(plain), Q, held, lens, [nq], dict())
+        for bad in (dict(window=2 ** 31), dict(window=2 ** 32 + 5), dict(window=4, sinks=2 ** 31)):
+            with pytest.raises(ValueError):
+                cache.attend(0, q, **bad)
+
+
+def test_outputs_made_for_slices_of_one_and_more_tokens():
+    """Outputs that the binding makes are dense whatever the rows of Q lie in, also where a dimension is one."""
+    r = np.random.default_rng(80)
+    for Hq, Hkv, n in ((4, 2, 1), (1, 1, 7), (1, 1, 1), (4, 2, 9)):
+        K, V, Q = T._normal(r, (n, Hkv, 64), 0.3), T._normal(r, (n, Hkv, 64)), T._normal(r, (n, Hq, 64))
+        wide = torch.zeros((n, Hq + 3, 64), dtype=torch.bfloat16, device="cuda")
+        wide[:, 2: 2 + Hq] = T._bf16(Q)
+        c, s = (torch.from_numpy(t).cuda() for t in T._tables(16, 64))
+        with T._cache(n_q_heads=Hq, n_kv_heads=Hkv, head_dim=64) as cache:
+            cache.step([0], [n])
+            a = cache.append(0, T._bf16(K), T._bf16(V), c, s, Q=T._bf16(Q))
+            b = cache.append(0, T._bf16(K), T._bf16(V), c, s, Q=wide[:, 2: 2 + Hq])
+            assert torch.equal(a, b) and b.is_contiguous()
+            assert torch.equal(cache.attend(0, a), cache.attend(0, torch.cat((a, a), 1)[:, Hq:]))
+            hk, hv = cache.read(0)
+            out = torch.empty_like(hk), torch.empty_like(hv)
+            assert cache.read(0, K=out[0], V=out[1])[0] is out[0]
+            assert torch.equal(hk, out[0]) and torch.equal(hv, out[1])
+            with pytest.raises(ValueError):
+                cache.read(0, K=torch.empty((n, Hkv + 1, 64), dtype=torch.bfloat16, device="cuda")[:, :Hkv] if n > 1 else hk.float())
