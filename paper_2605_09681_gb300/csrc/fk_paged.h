@@ -154,6 +154,7 @@ struct PagedAttnArgs {
   bf16* O;
   int64_t qstride, ostride;
   int wide_o;                         // rows of O are 32-byte aligned
+  int join;                           // 16-row CTAs: there are splits to join
   float scale_log2;                   // log2(e) * scale
   PagedMask mask;
   // partial O of the key splits and then (m, l, r, -) of their rows: [kPartSlots][16][D] and [..][16][4] (few

@@ -21,9 +21,9 @@
 // What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 50 us, 5.3 TB/s, where
 // reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 82.3 us, 5.9 TB/s (76.4).  With
 // little to read the launch and the join do: one token of 12 heads over 1561 keys 6.7 us.  At 16 rows its products and
-// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 15.0 us).
-// Splits leave (m, l, r, O) in a workspace; the last one to arrive joins them in the order of the splits (no atomics on
-// values: results do not change from run to run).
+// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.6 us).
+// Splits leave (m, l, r, O) in a workspace; the last one to arrive (8 rows) or a kernel of its own (16) joins them in the order of
+// the splits (no atomics on values: results do not change from run to run).
 #include "fk_paged.h"
 #include "fk_tc.h"
 
@@ -417,7 +417,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       if (c == 0) mls[cta * kPagedFewRows + row] = make_float4(M, L, (float)R, 0.0f);
     }
   }
-  if (n_splits == 1) return;
+  if (n_splits == 1 || kN == 2) return;
 
   // ---- the last split of the group joins them all.  The CTA's writes come before thread 0's release (barrier, then
   // an atomic of acquire and release at device scope), the others' before its acquire.
@@ -519,6 +519,66 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
 }
 
+// The same join by a kernel of its own, a warp for a row, for 16-row CTAs: one CTA would take long over the rows of many splits
+// (two queries of 64 heads over 20000 keys of 8: 27.2 us, this 20.4; 16 streams' drafts 14.9, 14.6).  For 8 rows or fewer the last
+// CTA is as good or better (two rows: 9.9 us, a kernel of its own 15.1).
+template <int D>
+__global__ void __launch_bounds__(512) few_join_kernel(const __grid_constant__ PagedAttnArgs a) {
+  constexpr int kRuns = D / 4, kFly = 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kvh = blockIdx.y;
+  int s = 0;
+  for (int hi = a.seqs.n - 1; s < hi;) {
+    const int mid = (s + hi + 1) >> 1;
+    if (a.seqs.item0[mid] <= (int)blockIdx.x) s = mid;
+    else hi = mid - 1;
+  }
+  const int n_splits = a.seqs.splits[s], item = blockIdx.x - a.seqs.item0[s];
+  const int row = item / n_splits * kPagedFewRows + warp;   // of the sequence's rows of this kv head
+  if (n_splits == 1 || item % n_splits != 0 || row >= a.seqs.n_q[s] * a.G) return;
+  const int first = a.seqs.part0[s] + kvh * (a.seqs.item0[s + 1] - a.seqs.item0[s]) + item;
+  const float4* part = reinterpret_cast<const float4*>(a.part);
+  const float4* mls = part + (int64_t)kPartSlots * kPagedFewRows * kRuns + (int64_t)first * kPagedFewRows + warp;
+  part += ((int64_t)first * kPagedFewRows + warp) * kRuns + lane;
+  const float4 none = make_float4(kLowest, 0.0f, (float)kNoRef, 0.0f);
+  const float4 e0 = lane < n_splits ? __ldcg(mls + lane * kPagedFewRows) : none;
+  float M = e0.x, R = e0.z, L = 0.0f;
+  for (int sp = lane + 32; sp < n_splits; sp += 32) {
+    const float4 e = __ldcg(mls + sp * kPagedFewRows);
+    M = fmaxf(M, e.x);
+    R = fmaxf(R, e.z);
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) {
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, off));
+  }
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s0 = 0; s0 < n_splits; s0 += 32) {           // weights of 32 splits, a lane each
+    const float4 e = s0 == 0 ? e0 : s0 + lane < n_splits ? __ldcg(mls + (s0 + lane) * kPagedFewRows) : none;
+    const float f = s0 + lane < n_splits ? fast_exp2(e.x - M) : 0.0f, w = f * pow2_any((int)(e.z - R));
+    L = fmaf(f, e.y, L);
+    const int n = min(32, n_splits - s0);
+    for (int k0 = 0; k0 < n; k0 += kFly) {
+      float4 x[kFly];
+#pragma unroll
+      for (int k = 0; k < kFly; ++k)
+        x[k] = k0 + k < n && lane < kRuns ? __ldcg(part + (int64_t)(s0 + k0 + k) * kPagedFewRows * kRuns) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int k = 0; k < kFly; ++k) {
+        const float g = __shfl_sync(0xffffffffu, w, (k0 + k) & 31);
+        acc = make_float4(fmaf(g, x[k].x, acc.x), fmaf(g, x[k].y, acc.y), fmaf(g, x[k].z, acc.z), fmaf(g, x[k].w, acc.w));
+      }
+    }
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
+  const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;      // no visible key: 0
+  const int tok = a.by_g.div(row);
+  bf16* o = a.O + ((int64_t)a.seqs.q0[s] + tok) * a.ostride + (int64_t)(kvh * a.G + row - tok * a.G) * D;
+  if (lane < kRuns)
+    *reinterpret_cast<uint2*>(o + 4 * lane) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+}
+
 using FewKern = void (*)(const CUtensorMap, const CUtensorMap, const PagedAttnArgs);
 FewKern few_of(int D, int row_tiles) {
   if (D == 128) return row_tiles == 1 ? few_kernel<128, 1> : few_kernel<128, 2>;
@@ -539,6 +599,10 @@ cudaError_t launch_paged_few(int D, int row_tiles, const CUtensorMap& tmK, const
   const dim3 grid((unsigned)a.seqs.item0[a.seqs.n], (unsigned)a.Hkv);
   if (grid.x == 0) return cudaSuccess;
   few_of(D, row_tiles)<<<grid, kFewThreads, D == 128 ? FewLayout<128>::kSmem : FewLayout<64>::kSmem, s>>>(tmK, tmV, a);
+  if (a.join) {
+    if (D == 128) few_join_kernel<128><<<grid, 32 * kPagedFewRows, 0, s>>>(a);
+    else few_join_kernel<64><<<grid, 32 * kPagedFewRows, 0, s>>>(a);
+  }
   return cudaGetLastError();
 }
 

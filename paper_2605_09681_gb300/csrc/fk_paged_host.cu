@@ -28,6 +28,7 @@ struct StepSeq {
 struct AttnLaunch {
   bool chunk;
   int shape;
+  bool join;                          // a second kernel joins the splits
   PagedAttnSeqs seqs;
 };
 struct AttnPlan {
@@ -406,11 +407,12 @@ void plan_group(const fk_paged* h, const PagedAttnArgs& a, size_t i, size_t i1, 
   if (part[0].n) {
     const Shape sh = few_of(part[0]);
     lay_out(a, part[0], sh, best.few.per);
-    out->push_back({false, sh.rows / 8, part[0]});
+    const bool split = std::any_of(part[0].splits, part[0].splits + part[0].n, [](int n) { return n > 1; });
+    out->push_back({false, sh.rows / 8, split && sh.rows == kPagedFewRows, part[0]});
   }
   if (part[1].n) {
     if (!split_the_rest(h, a, part[1], best.shape)) lay_out(a, part[1], best.shape, best.chunk.per);
-    out->push_back({true, best.shape.rows / kAttnBM, part[1]});
+    out->push_back({true, best.shape.rows / kAttnBM, part[1].join0[part[1].n] > 0, part[1]});
   }
 }
 
@@ -698,6 +700,8 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
     for (const AttnLaunch& l : plan->launches) {
       a->seqs = l.seqs;
       a->part = l.chunk ? h->part_chunk : h->part_few;
+      a->join = !l.chunk && l.join;
+      h->launches += l.join;
       const fk_status st = done(h, l.chunk ? launch_paged_chunk(c.head_dim, l.shape == 1, h->tmK[layer], h->tmV[layer], *a, s)
                                            : launch_paged_few(c.head_dim, l.shape, h->tmK[layer], h->tmV[layer], *a, s));
       if (st != FK_OK) return st;
