@@ -3,6 +3,8 @@
 
 #include "fk_internal.h"
 
+#include <utility>
+
 namespace fk {
 
 constexpr int kStepSeqs = 256;        // sequences of one launch (their numbers travel by value)
@@ -173,5 +175,25 @@ cudaError_t paged_few_prepare(int D);
 cudaError_t launch_paged_chunk(int D, bool one_tile, const CUtensorMap& tmK, const CUtensorMap& tmV,
                                const PagedAttnArgs& a, cudaStream_t s);
 cudaError_t paged_chunk_prepare(int D);
+
+#ifdef __CUDACC__
+// A join's launch may come while the kernel before it in the stream still runs (that one allows it, once all its CTAs have
+// started): the join waits for its end, and its writes, before it reads anything.
+__device__ __forceinline__ void allow_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_parts() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <class... Params, class... Args>
+cudaError_t launch_join(void (*kernel)(Params...), dim3 grid, unsigned threads, cudaStream_t s, Args&&... args) {
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = s;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+#endif
 
 }  // namespace fk

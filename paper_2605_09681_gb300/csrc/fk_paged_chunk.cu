@@ -17,7 +17,7 @@
 // r (see kRefWindow) is chosen per key tile by the loading warp.  A tile whose own pages differ by more than the
 // window allows ("wild") is handed over 32 keys at a time, O rescaled in between.
 // Key splits leave (m, l, r, O) in a workspace; join_kernel joins them.
-// What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 636-639 us, 1475 TFLOP/s.  A key tile takes the two query tiles
+// What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 627-639 us, 1475-1500 TFLOP/s.  A key tile takes the two query tiles
 // 2950 cycles, 2048 of them products at their nominal rate: a query tile's softmax (1600) and the wait for its next S take turns, since
 // P lies over S and tensor memory is full (S, O of two tiles), and Q K^T wants 128 bytes of shared memory a cycle, all there is, beside
 // the conversion's.  A CTA starts and ends in ~15000 cycles (queries copied 3300, their codes 3500, first S 1450, first tile
@@ -331,6 +331,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       load_k(j + 2);
       jk = j + 2;
     }
+    if constexpr (kOne) allow_join();               // (16 x 2000 keys, 48 rows: 21.7 -> 18.5 us; two tiles, whose join is short: slower)
     if (!ok) {                                      // what was issued lands before the CTA ends
       for (int j = max(0, jk - kKStages + 1); j <= jk; ++j) wait_phase(&bar->k_full[j % kKStages], (j / kKStages) & 1, bar, a.status, false);
       for (int j = max(0, jv - 1); j <= jv; ++j) wait_phase(&bar->v8_full[j & 1], (j >> 1) & 1, bar, a.status, false);
@@ -875,6 +876,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Paged
   const float4* mls = part + (int64_t)a.part_tiles * kBM * kRuns;
   const int64_t first = ((int64_t)a.seqs.part0[s] + (int64_t)split_pair * n_splits * tiles) * kBM + r;   // split 0's row
   const int64_t next = (int64_t)tiles * kBM;
+  wait_for_parts();
   // (m, l, r) of the first 32 splits are asked for once
   const float4 e0 = lane < n_splits ? __ldcg(mls + first + lane * next) : make_float4(kNoMax, 0.0f, (float)kNoRef, 0.0f);
   float M = e0.x, R = e0.z, L = 0.0f;
@@ -947,8 +949,9 @@ cudaError_t launch_paged_chunk(int D, bool one_tile, const CUtensorMap& tmK, con
   }
   const int tiles = one_tile ? 1 : 2;
   if (const unsigned pairs = (unsigned)a.seqs.join0[a.seqs.n]) {       // 8 rows to a CTA
-    if (D == 128) join_kernel<128><<<pairs * (tiles * kBM / 8), 256, 0, s>>>(a, tiles);
-    else join_kernel<64><<<pairs * (tiles * kBM / 8), 256, 0, s>>>(a, tiles);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    return launch_join(D == 128 ? join_kernel<128> : join_kernel<64>, dim3(pairs * (tiles * kBM / 8)), 256, s, a, tiles);
   }
   return cudaGetLastError();
 }

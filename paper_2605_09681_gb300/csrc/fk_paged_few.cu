@@ -21,7 +21,7 @@
 // What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 50 us, 5.3 TB/s, where
 // reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 82.3 us, 5.9 TB/s (76.4).  With
 // little to read the launch and the join do: one token of 12 heads over 1561 keys 6.7 us.  At 16 rows its products and
-// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.6 us).
+// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.1 us).
 // Splits leave (m, l, r, O) in a workspace; the last one to arrive (8 rows) or a kernel of its own (16) joins them in the order of
 // the splits (no atomics on values: results do not change from run to run).
 #include "fk_paged.h"
@@ -354,6 +354,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 #pragma unroll
         for (int off = 4; off <= 16; off <<= 1) l[j][h] += __shfl_xor_sync(0xffffffffu, l[j][h], off);
   }
+  if constexpr (kN == 2) allow_join();
   __syncthreads();                                      // every tile has been read: the stages are free
 
   // ---- the warps' (m, l, r) and O
@@ -520,7 +521,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 }
 
 // The same join by a kernel of its own, a warp for a row, for 16-row CTAs: one CTA would take long over the rows of many splits
-// (two queries of 64 heads over 20000 keys of 8: 27.2 us, this 20.4; 16 streams' drafts 14.9, 14.6).  For 8 rows or fewer the last
+// (two queries of 64 heads over 20000 keys of 8: 30.3 us, this 22.6; 16 streams' drafts 17.1, 16.4; without the early
+// launch 24.6 and 18.6: launched one after the other).  For 8 rows or fewer the last
 // CTA is as good or better (two rows: 9.9 us, a kernel of its own 15.1).
 template <int D>
 __global__ void __launch_bounds__(512) few_join_kernel(const __grid_constant__ PagedAttnArgs a) {
@@ -533,6 +535,7 @@ __global__ void __launch_bounds__(512) few_join_kernel(const __grid_constant__ P
     else hi = mid - 1;
   }
   const int n_splits = a.seqs.splits[s], item = blockIdx.x - a.seqs.item0[s];
+  wait_for_parts();
   const int row = item / n_splits * kPagedFewRows + warp;   // of the sequence's rows of this kv head
   if (n_splits == 1 || item % n_splits != 0 || row >= a.seqs.n_q[s] * a.G) return;
   const int first = a.seqs.part0[s] + kvh * (a.seqs.item0[s + 1] - a.seqs.item0[s]) + item;
@@ -599,11 +602,9 @@ cudaError_t launch_paged_few(int D, int row_tiles, const CUtensorMap& tmK, const
   const dim3 grid((unsigned)a.seqs.item0[a.seqs.n], (unsigned)a.Hkv);
   if (grid.x == 0) return cudaSuccess;
   few_of(D, row_tiles)<<<grid, kFewThreads, D == 128 ? FewLayout<128>::kSmem : FewLayout<64>::kSmem, s>>>(tmK, tmV, a);
-  if (a.join) {
-    if (D == 128) few_join_kernel<128><<<grid, 32 * kPagedFewRows, 0, s>>>(a);
-    else few_join_kernel<64><<<grid, 32 * kPagedFewRows, 0, s>>>(a);
-  }
-  return cudaGetLastError();
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || !a.join) return e;
+  return launch_join(D == 128 ? few_join_kernel<128> : few_join_kernel<64>, grid, 32 * kPagedFewRows, s, a);
 }
 
 }  // namespace fk
