@@ -726,11 +726,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
             FK_TMEM_ST16(tS + c * 16, pk);
             l += weighted(ac, c, plain);
           }
-          if (__any_sync(0xffffffffu, rs != 1.0f) && (it > 0 || c0 > 0)) {   // O holds every key before chunk c0 ...
-            if (c0 > 0) {                            // ... once pva_done says so
-              if (!warp_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) { ok = false; break; }
-              tc_fence_after();
-            }
+          const bool rescale = __any_sync(0xffffffffu, rs != 1.0f) && (it > 0 || c0 > 0);   // O holds every key before chunk c0 ...
+          if (c0 > 0 && (rescale || wild)) {         // ... once pva_done says so
+            // (A wild tile's parts all go over pa_full: no warp hands one over before all four have handed over the one before,
+            // or a fast warp's arrival would stand for a slow one's.)
+            if (!warp_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) { ok = false; break; }
+            tc_fence_after();
+          }
+          if (rescale) {
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
               FK_TMEM_LD32(tO + c * 32, ca);
