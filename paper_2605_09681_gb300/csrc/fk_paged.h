@@ -17,9 +17,11 @@ constexpr int kPartSlots = 4096;      // CTAs of a launch that share their rows 
 // Stored exponent of a block of zeros (others are at least -120).
 constexpr int kZeroExp = -126;
 // The attention folds a value block's 2^e into the softmax numerators, w = p 2^(e - r), as f16, relative to a
-// reference r that O (fp32) is kept to: e - r stays in [-kRefWindow, 0], so that no weight loses bits to a
-// block of another size, seen or not.  A block outside moves r to e + kRefRoom and rescales O by a power of two.
+// reference r that O (fp32) is kept to: e - r stays in [-kRefWindow, 0] where the rows go together, and a block outside asks for
+// r = e + kRefRoom: O moves by a power of two, as far as what it holds allows.
 constexpr int kRefWindow = 16, kRefRoom = 2;
+constexpr int kNoRef = -1000;         // r before any block but zeros
+constexpr int kAskPast = -8;          // log2 of a block's largest p from which on a row simply takes a larger block's reference
 
 constexpr int kAppendFewRows = 8;     // new tokens on a page that one warp takes
 
@@ -148,6 +150,8 @@ struct PagedAttnSeqs {
 
 struct PagedAttnArgs {
   const int* table;
+  const uint8_t* k;                   // as in PagedPool
+  const uint8_t* v;
   const int8_t* ke;
   const int8_t* ve;
   int max_pages, Hkv, G, P;
@@ -177,6 +181,33 @@ cudaError_t launch_paged_chunk(int D, bool one_tile, const CUtensorMap& tmK, con
 cudaError_t paged_chunk_prepare(int D);
 
 #ifdef __CUDACC__
+// exponent e of x > 0, 2^e > x (below 2^-126: -126)
+__device__ __forceinline__ int above2(float x) { return (int)(__float_as_uint(x) >> 23) - 126; }
+
+// Where a row's reference r goes when a block that it sees asks for `to`.  p: log2 of the row's largest numerator in the block; 2^top > |O|
+// relative to r (a numerator of 1 in a block of reference r is 2^kRowTop there at most).  Not lower than leaves O room, which then grows, and
+// no higher above what the row holds or the block adds than leaves the bits of both.
+constexpr int kRowTop = 16, kRoom = 110, kAbove = 8;
+__device__ __forceinline__ int follow(int r, int to, float p, int top) {
+  const int most = max(r + top - kRowTop, to + (int)fmaxf(p, -1000.0f));
+  return max(min(to, most + kAbove), max(r + top - kRoom, r - 127));
+}
+
+// Parts of a row's keys, each with its maximum m, its l and its reference r, joined by a warp: weights 2^(m - M) of l, M = max m, and
+// 2^((m - M) + (r - R)) of O.  R: the largest r, unless no part holds nearly 2^R (then that of what they hold).  e0: part `lane`.
+template <class Part>
+__device__ __forceinline__ float join_ref(float M, float R, const float4& e0, int n, Part part) {
+  float most = (e0.x - M) + e0.z;
+  if (__any_sync(0xffffffffu, most >= R - 40.0f)) return R;
+  for (int i = (threadIdx.x & 31) + 32; i < n; i += 32) {
+    const float4 e = part(i);
+    most = fmaxf(most, (e.x - M) + e.z);
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+  return floorf(most);
+}
+
 // A join's launch may come while the kernel before it in the stream still runs (that one allows it, once all its CTAs have
 // started): the join waits for its end, and its writes, before it reads anything.
 __device__ __forceinline__ void allow_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

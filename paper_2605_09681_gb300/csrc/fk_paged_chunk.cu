@@ -14,8 +14,9 @@
 // same way would cost each of the 256 x 128 numerators of a key tile five more instructions; the tile's 128 x D values
 // cost twelve instructions per 16 instead, in warps of their own, and P goes as f16 (11 bits).  The block exponents come
 // for free: e_k and e_v - r of each 32 keys in the factor and the summand of the softmax's fused multiply-add.
-// r (see kRefWindow) is chosen per key tile by the loading warp.  A tile whose own pages differ by more than the
-// window allows ("wild") is handed over 32 keys at a time, O rescaled in between.
+// The loading warp says which r (see kRefWindow) a key tile asks for, and each row goes there as far as what it holds allows (follow).  A
+// tile whose own pages differ by more than the window allows, or has one of zeros ("wild"), is handed over 32 keys at a time,
+// which ask for their own, O rescaled in between.
 // Key splits leave (m, l, r, O) in a workspace; join_kernel joins them.
 // What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 627-639 us, 1475-1500 TFLOP/s.  A key tile takes the two query tiles
 // 2950 cycles, 2048 of them products at their nominal rate: a query tile's softmax (1600) and the wait for its next S take turns, since
@@ -36,7 +37,6 @@ namespace fk {
 namespace {
 
 constexpr float kRescaleThreshold = 1.0f;          // log2 units by which a part must exceed m to raise it
-constexpr int kNoRef = -1000;                      // r before any block but zeros
 constexpr float kNoMax = -3.402823466e38f;         // m before any key: finite, so that 2^(-inf - m) is 0
 constexpr int kWarpTma = 8, kWarpMma = 9, kWarpConv = 10;
 constexpr int kChunkThreads = 384;
@@ -48,11 +48,11 @@ constexpr int kInfo = 64;                          // key tiles whose pages and 
 struct ChunkInfo {                                 // of a key tile
   int y[4];                                        // row of each box in the layer's pages
   uint32_t ve;                                     // e_v of each 32 keys, one byte each
-  int r;                                           // reference of O after the tile
+  int r;                                           // reference that the tile asks for (a wild one's 32 keys ask for their own)
   int wild;
   int key0;                                        // first key
-  // of each 32 keys: 2^e_k, the exponent's summand e_v - r + 7, and 2^(r - e_v) for the row sum (r the
-  // tile's reference, or the 32 keys' own in a wild tile; blocks of zeros count as e_v = r)
+  // of each 32 keys: 2^e_k, and where the tile is not wild the exponent's summand e_v - r + 7, and 2^(r - e_v) for the
+  // row sum
   float fk[4], add[4], mul[4];
 };
 struct ChunkBarriers {
@@ -82,7 +82,8 @@ struct ChunkLayout {
   static constexpr int kOffV = kOffV8 + 2 * kK;
   static constexpr int kOffInfo = kOffV + 2 * kV;
   static constexpr int kOffBar = kOffInfo + kInfo * (int)sizeof(ChunkInfo);
-  static constexpr int kUsed = kOffBar + 384;
+  static constexpr int kOffHeld = kOffBar + 384;
+  static constexpr int kUsed = kOffHeld + 256 * 4;
   static_assert(sizeof(ChunkBarriers) <= 384, "barriers");
   // the epilogue's rows of O in fp32 (256) and their (m, l, r)
   static_assert(2 * kBM * D * 4 + 2 * kBM * 16 <= kOffInfo, "O over the operand tiles");
@@ -117,6 +118,24 @@ template <int D>
 __device__ __forceinline__ int code_run(int row, int c) {
   return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
 }
+// warp_wait whose polling is out of line (a copy of it for each of the kernel's waits outgrows the instruction cache).
+__device__ __noinline__ bool poll(uint64_t* b, uint32_t parity, ChunkBarriers* bar, int* status) { return warp_wait(b, parity, bar, status); }
+__device__ __forceinline__ bool tile_wait(uint64_t* b, uint32_t parity, ChunkBarriers* bar, int* status) {
+  return __all_sync(0xffffffffu, mbar_test(b, parity)) || poll(b, parity, bar, status);
+}
+// 16 columns of tensor memory, awaited
+#define FK_TMEM_LD16(taddr, v)                                                              \
+  asm volatile(                                                                             \
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,"  \
+      "%13,%14,%15}, [%16];"                                                                \
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),  \
+        "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]),           \
+        "=r"(v[13]), "=r"(v[14]), "=r"(v[15])                                               \
+      : "r"(taddr));                                                                        \
+  asm volatile("tcgen05.wait::ld.sync.aligned;"                                             \
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]),    \
+                 "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]),  \
+                 "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]) :: "memory")
 template <int D, bool kOne>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -134,6 +153,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   uint8_t* sV = smem + Lay::kOffV;
   ChunkInfo* info = reinterpret_cast<ChunkInfo*>(smem + Lay::kOffInfo);
   ChunkBarriers* bar = reinterpret_cast<ChunkBarriers*>(smem + Lay::kOffBar);
+  float* held = reinterpret_cast<float*>(smem + Lay::kOffHeld);   // of a softmax thread's row: see less
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // ---- this CTA's rows and key tiles
@@ -195,7 +215,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const int j = j0 + lane;
     int lo = 127, hi = -127, last = kNoRef, ev[4];  // of the tile's blocks that are not zeros
     float fk[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-    bool wild = false;
+    bool wild = false, zeros = false;
 #pragma unroll
     for (int c = 0; c < 4; ++c) ev[c] = kZeroExp;
     if (j < nt) {
@@ -211,8 +231,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           lo = min(lo, ev[c]);
           hi = max(hi, ev[c]);
           last = ev[c];
+        } else {
+          zeros = true;
         }
-      wild = hi - lo > kRefWindow - kRefRoom;
+      wild = zeros || hi - lo > kRefWindow - kRefRoom;
     }
     int mine = kNoRef;
     for (int i = 0; i < min(32, nt - j0); ++i) {    // the references, tile by tile
@@ -231,7 +253,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       uint32_t ve = 0;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const int below = ev[c] == kZeroExp ? 0 : wild ? kRefRoom : mine - ev[c];
+        const int below = wild ? 0 : mine - ev[c];
         ve |= (uint32_t)(uint8_t)ev[c] << (8 * c);
         x.fk[c] = fk[c];
         x.add[c] = kShiftP - (float)below;
@@ -302,6 +324,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   // softmax state (warps 0-7)
   float m = kNoMax, l = 0.0f;
   int r = kNoRef;                                   // reference of O
+  if (warp < 8) held[threadIdx.x] = 0.0f;
   uint32_t n_pa = 0;                                // parts handed over on pa_full
   bool ok = true;
 
@@ -313,7 +336,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     int jv = -1, jk = min(2, nt) - 1;               // last tiles issued
     for (int j = 0; j < nt; ++j) {
       const int b = j & 1;
-      if (j >= 2 && !warp_wait(&bar->v8_empty[b], ((j >> 1) - 1) & 1, bar, a.status)) { ok = false; break; }
+      if (j >= 2 && !tile_wait(&bar->v8_empty[b], ((j >> 1) - 1) & 1, bar, a.status)) { ok = false; break; }
       if (lane == 0) mbar_expect_tx(&bar->v8_full[b], Lay::kK);
       __syncwarp();
       load(&tmV, sV8 + b * Lay::kK, j, &bar->v8_full[b]);
@@ -327,7 +350,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         fetch_pages(j + 2);
         fetch_exps(j + 2);
       }
-      if (j + 2 >= kKStages && !warp_wait(&bar->k_empty[(j + 2) % kKStages], ((j + 2) / kKStages - 1) & 1, bar, a.status)) { ok = false; break; }
+      if (j + 2 >= kKStages && !tile_wait(&bar->k_empty[(j + 2) % kKStages], ((j + 2) / kKStages - 1) & 1, bar, a.status)) { ok = false; break; }
       load_k(j + 2);
       jk = j + 2;
     }
@@ -374,7 +397,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       for (int kk = 0; kk < 2; ++kk)
         umma_ts(d, p + kk * 8, db + kk * 128, kIdPV, (j >= kAhead || c > 0 || kk > 0) ? 1u : 0u);
     };
-    auto wait = [&](uint64_t* b, uint32_t parity) { return warp_wait(b, parity, bar, a.status); };
+    auto wait = [&](uint64_t* b, uint32_t parity) { return tile_wait(b, parity, bar, a.status); };
     uint32_t n_pa[2] = {0, 0};                      // parts of P taken on pa_full
     auto k_ready = [&](int j) { return wait(&bar->k_full[j % kKStages], (j / kKStages) & 1); };
     if (nt > 0) {
@@ -454,12 +477,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     // ------------------------------------------------------------------ V codes -> f16 values
     // A thread takes 8 codes of a row at a time: half a 16-byte run, one 16-byte unit of the f16 row.
     constexpr int kOct = D / 8, kStepRows = 64 / kOct, kFly = 16;   // units of a row; rows per pass; loads in flight
-    ok = nt == 0 || warp_wait(&bar->q_ready, 0, bar, a.status);   // (the query rows were staged where the values go)
+    ok = nt == 0 || tile_wait(&bar->q_ready, 0, bar, a.status);   // (the query rows were staged where the values go)
     const int x = threadIdx.x - kWarpConv * 32, prow = x / kOct, unit = x % kOct;
     for (int j = 0; j < nt && ok; ++j) {
       const int b = j & 1, u = j >> 1;
-      if (!warp_wait(&bar->v8_full[b], u & 1, bar, a.status) ||
-          (j >= 2 && !warp_wait(&bar->vf_empty[b], (u - 1) & 1, bar, a.status))) { ok = false; break; }
+      if (!tile_wait(&bar->v8_full[b], u & 1, bar, a.status) ||
+          (j >= 2 && !tile_wait(&bar->vf_empty[b], (u - 1) & 1, bar, a.status))) { ok = false; break; }
       const uint8_t* src = sV8 + b * Lay::kK;
       uint8_t* dst = sV + b * Lay::kV;
 #pragma unroll
@@ -553,7 +576,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const int full_hi = a.mask.causal ? min(pa + 1, n_keys) : n_keys;
     const int full_lo = a.mask.window > 0 ? pb - a.mask.window + 1 : 0;
 
-    ok = warp_wait(&bar->tmem_ready, 0, bar, a.status) && ok;
+    ok = tile_wait(&bar->tmem_ready, 0, bar, a.status) && ok;
     const uint32_t lanes = bar->tmem_base + ((uint32_t)(wq * 32) << 16);
     const uint32_t tS = lanes + (uint32_t)(t * kBN), tO = lanes + kColO + (uint32_t)(t * D);
     auto known = [&] {
@@ -562,7 +585,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       return n;
     };
     int n_info = 0;                                 // tiles whose numbers are known to be there
-    if (nt > 0) ok = warp_wait(&bar->info_ready, 0, bar, a.status) && ok;
+    if (nt > 0) ok = tile_wait(&bar->info_ready, 0, bar, a.status) && ok;
     for (int it = 0; ok; ++it) {
       const int j = kOne ? 2 * it + t : it;         // kOne: this warpgroup's key set is every other tile
       if (j >= nt) break;
@@ -571,17 +594,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       if (j >= n_info) {
         n_info = known();
         if (j >= n_info) {
-          if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
+          if (!tile_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
           n_info = known();
         }
       }
       const ChunkInfo& ti = info[j & (kInfo - 1)];
       const bool wild = ti.wild != 0;
-      float rs = 1.0f;                              // what O has to be scaled by for the tile's reference
-      if (!wild && ti.r != r) {
-        if (it > 0) rs = pow2_any(r - ti.r);
-        r = ti.r;
-      }
+      if (it == 0 && !wild) r = ti.r;
       // of 32 keys: factor and summand of the exponent S + e_v - r + 7 - m, and what the row sum takes of theirs
       float fc[4];
 #pragma unroll
@@ -600,9 +619,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       };
       const int key0 = ti.key0;
       const bool full = trow1 < 0 || (key0 + kBN <= full_hi && (key0 >= full_lo || key0 + kBN <= a.mask.sinks));
-      const bool keeps = it > 0 && rs == 1.0f && !wild;   // uniform over the warpgroup
-      bool direct = full && keeps;
-      if (!warp_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
+      bool direct = !wild && __all_sync(0xffffffffu, r == ti.r);   // the rows go together, at the tile's reference
+      if (!tile_wait(&bar->s_full[t], it & 1, bar, a.status)) { ok = false; break; }
       tc_fence_after();
       uint32_t ca[32], cb[32], ov = 0;
       if (!full) {                                  // masked keys' logits become -inf, in place
@@ -620,7 +638,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           FK_TMEM_ST32(tS + c * 32, ca);
         }
         tmem_wait_st();
-        direct = keeps;
       }
       if (it == 0 && !wild) {                       // the first tile: m from 32 of its keys, at its end where a window begins in it
         const int c = key0 >= full_lo || key0 < a.mask.sinks ? 0 : 3;
@@ -630,107 +647,97 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
 #pragma unroll
         for (int i = 0; i < 32; ++i) mxa[i & 3] = fmaxf(mxa[i & 3], __uint_as_float(ca[i]));
         m = fmaxf(fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * factor_at(c), kNoMax);
-        direct = true;
       }
       // A tile goes in two parts, keys 0-95 and 96-127 (a wild one 32 keys at a time).  P is
       // computed with the running max m straight away; a part with a weight beyond 2^8 (2^15 as stored) is
-      // done again with a max pass, which raises m.  One copy of that general path serves all parts: with one for each,
-      // the loop outgrew the instruction cache (a copy for wild tiles alone cost a sixth).
+      // done again after a max pass, which raises m and moves the rows' references.  Rows that do not go together afterwards take
+      // the loop at its end.  (Few instructions beside those: the loop is at the size of the instruction cache, and
+      // some hundred more of them cost a tenth.)
       const int parts = wild ? 4 : 2;
 #pragma unroll 1
       for (int part = 0; part < parts; ++part) {
-        bool general = true;
-        if (direct) {
-          if (part == 0) {
-            uint32_t pk[48];
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+          if (direct) {
             float plain = 0.0f, dl = 0.0f;
-            auto chunk = [&](const uint32_t* x, int c) {
+            bool fits;
+            auto chunk = [&](const uint32_t* x, int c, uint32_t* pk) {
               float2 ah[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
-              exp_chunk<PFormat::kF16>(x, factor(c), summand(c), ah, pk + 16 * c, ov);
+              exp_chunk<PFormat::kF16>(x, factor(c), summand(c), ah, pk, ov);
               dl += weighted(ah, c, plain);
             };
-            FK_TMEM_LD32(tS, ca);
-            FK_TMEM_WAIT_LD32(ca);
-            FK_TMEM_LD32(tS + 32, cb);
-            chunk(ca, 0);
-            FK_TMEM_WAIT_LD32(cb);
-            FK_TMEM_LD32(tS + 64, ca);
-            chunk(cb, 1);
-            FK_TMEM_WAIT_LD32(ca);
-            FK_TMEM_LD32(tS + 96, cb);
-            chunk(ca, 2);
-            FK_TMEM_WAIT_LD32(cb);
-            general = __any_sync(0xffffffffu, plain > 32768.0f);   // (no numerator exceeds the sum) warp-uniform
-            if (!general) {
-              FK_TMEM_ST32(tS, pk);
-              FK_TMEM_ST16(tS + 32, (pk + 32));
-              l += dl;
+            if (part == 0) {
+              uint32_t pk[48];
+              FK_TMEM_LD32(tS, ca);
+              FK_TMEM_WAIT_LD32(ca);
+              FK_TMEM_LD32(tS + 32, cb);
+              chunk(ca, 0, pk);
+              FK_TMEM_WAIT_LD32(cb);
+              FK_TMEM_LD32(tS + 64, ca);
+              chunk(cb, 1, pk + 16);
+              FK_TMEM_WAIT_LD32(ca);
+              FK_TMEM_LD32(tS + 96, cb);
+              chunk(ca, 2, pk + 32);
+              FK_TMEM_WAIT_LD32(cb);
+              fits = again || !__any_sync(0xffffffffu, plain > 32768.0f);   // (no numerator exceeds the sum) warp-uniform
+              if (fits) {
+                FK_TMEM_ST32(tS, pk);
+                FK_TMEM_ST16(tS + 32, (pk + 32));
+              }
+            } else {
+              uint32_t pk[16];
+              if (again) {                           // (not kept across what follows)
+                FK_TMEM_LD32(tS + 96, cb);
+                FK_TMEM_WAIT_LD32(cb);
+              }
+              chunk(cb, 3, pk);
+              fits = again || !__any_sync(0xffffffffu, plain > 32768.0f);
+              if (fits) FK_TMEM_ST16(tS + 48, pk);
             }
-          } else {
-            uint32_t pk[16];
-            float2 ah[4];
-            float plain = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ah[i] = make_float2(0.0f, 0.0f);
-            exp_chunk<PFormat::kF16>(cb, factor(3), summand(3), ah, pk, ov);
-            const float dl = weighted(ah, 3, plain);
-            general = __any_sync(0xffffffffu, plain > 32768.0f);
-            if (!general) {
-              FK_TMEM_ST16(tS + 48, pk);
+            if (fits) {
               l += dl;
+              break;
             }
           }
-        }
-        if (general) {
           const int c0 = wild ? part : 3 * part, c1 = wild ? part + 1 : 3 + part;   // chunks of 32 keys
-          if (wild) {                                // at their own reference
-            const int e = chunk_exp(ti.ve, part), rn = e == kZeroExp ? r : e + kRefRoom;
-            rs = pow2_any(r - rn);
-            r = rn;
-          } else if (part > 0) {
-            rs = 1.0f;
-          }
-          auto load_chunk = [&](int c) {             // logits of a chunk
-            FK_TMEM_LD32(tS + c * 32, ca);
-            FK_TMEM_WAIT_LD32(ca);
-          };
+          const int e0 = chunk_exp(ti.ve, part);
+          const int to = !wild ? ti.r : e0 != kZeroExp ? e0 + kRefRoom : l == 0.0f ? kNoRef : r;   // reference asked for
           float mx = -INFINITY;
 #pragma unroll 1
           for (int c = c0; c < c1; ++c) {
-            load_chunk(c);
+            FK_TMEM_LD32(tS + c * 32, ca);
+            FK_TMEM_WAIT_LD32(ca);
             float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int i = 0; i < 32; ++i) mxa[i & 3] = fmaxf(mxa[i & 3], __uint_as_float(ca[i]));
             mx = fmaxf(mx, fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * factor_at(c));
           }
           const float m_new = fmaxf(m, mx);
-          const bool raise = __any_sync(0xffffffffu, m_new > m + kRescaleThreshold);   // warp-uniform
-          if (raise) {
-            const float al = fast_exp2(m - m_new);   // 0 when m = kNoMax
-            l *= al;
-            rs *= al;
+          float rs = 1.0f, less = held[threadIdx.x]; // what O has to be scaled by; |O| <= 2^9 l + less
+          if (__any_sync(0xffffffffu, m_new > m + kRescaleThreshold)) {   // warp-uniform
+            rs = fast_exp2(m - m_new);               // 0 when m = kNoMax
+            l *= rs;
+            less *= rs;
             m = m_new;
           }
-#pragma unroll 1
-          for (int c = c0; c < c1; ++c) {            // (P's columns lie over logits already read)
-            load_chunk(c);
-            uint32_t pk[16];
-            float2 ac[4];
-            float plain = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ac[i] = make_float2(0.0f, 0.0f);
-            const float f = factor_at(c);
-            exp_chunk<PFormat::kF16>(ca, make_float2(f, f), summand(c), ac, pk, ov);
-            FK_TMEM_ST16(tS + c * 16, pk);
-            l += weighted(ac, c, plain);
+          // The row's reference.  One that holds nothing takes any, one that does not see the part keeps its own.
+          if (__any_sync(0xffffffffu, to != r)) {
+            const bool none = l == 0.0f || r == kNoRef;
+            float most = none ? 0.0f : fmaxf(fmaf(512.0f, l, less), 1e-37f);   // |O|, at most
+            int want = none ? to : r;
+            if (want != to && mx > -INFINITY) want = follow(r, to, mx - m, above2(most));
+            const float f = pow2_any(r - want);
+            less = fmaf(-512.0f, l, most * f);
+            rs *= f;
+            r = want;
           }
           const bool rescale = __any_sync(0xffffffffu, rs != 1.0f) && (it > 0 || c0 > 0);   // O holds every key before chunk c0 ...
-          if (c0 > 0 && (rescale || wild)) {         // ... once pva_done says so
-            // (A wild tile's parts all go over pa_full: no warp hands one over before all four have handed over the one before,
-            // or a fast warp's arrival would stand for a slow one's.)
-            if (!warp_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) { ok = false; break; }
+          // ... once pva_done says so.  (A wild tile's parts all go over pa_full: no warp hands one over before all four have
+          // handed over the one before, or a fast warp's arrival would stand for a slow one's.)
+          if (c0 > 0 && (rescale || wild)) {
+            if (!tile_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) { ok = false; break; }
             tc_fence_after();
           }
           if (rescale) {
@@ -743,11 +750,32 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
               FK_TMEM_ST32(tO + c * 32, ca);
             }
           }
-          if (direct && part == 0) {                 // (not kept across the general path)
-            FK_TMEM_LD32(tS + 96, cb);
-            FK_TMEM_WAIT_LD32(cb);
+          held[threadIdx.x] = less;
+          direct = !wild && __all_sync(0xffffffffu, r == ti.r);
+          if (direct) continue;
+          // numerators, and then the block's size relative to the row's reference, which l does not know
+#pragma unroll 1
+          for (int x = 2 * c0; x < 2 * c1; ++x) {    // 16 keys (P's columns lie over logits already read)
+            const int c = x >> 1, e = chunk_exp(ti.ve, c);
+            const float f = factor_at(c), below = kShiftP - m, size = e == kZeroExp ? 0.0f : pow2_any(e - r);
+            float sum = 0.0f;
+            uint32_t v[16], pk[8];
+            FK_TMEM_LD16(tS + x * 16, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float y0 = fast_exp2(fmaf(__uint_as_float(v[2 * i]), f, below));
+              const float y1 = fast_exp2(fmaf(__uint_as_float(v[2 * i + 1]), f, below));
+              sum += y0 + y1;
+              pk[i] = pack_f16(y0 * size, y1 * size);
+            }
+            FK_TMEM_ST8(tS + x * 8, pk);
+            l += sum;
+            less = fmaf(512.0f * sum, size - 1.0f, less);
           }
+          held[threadIdx.x] = less;
+          break;
         }
+        if (!ok) break;
         // P in TMEM -> the MMA warp
         const bool more = wild || part == 0;
         tmem_wait_st();
@@ -764,7 +792,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     }
     // ---------------------------------------------------------------- epilogue
     // This accumulator's last MMA is done, and with it every MMA that reads Q: that shared memory is free.
-    ok = ok && warp_wait(&bar->o_done[t], 0, bar, a.status);
+    ok = ok && tile_wait(&bar->o_done[t], 0, bar, a.status);
     tc_fence_after();
     const bool has = kOne ? t < nt : nt > 0;        // this accumulator was written
     const int row0 = bar->row0, rows = bar->rows, kvh = bar->kvh, n_splits = bar->n_splits;
@@ -773,7 +801,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       const int q = row0 + r, tok = a.by_g.div(q);
       return a.O + (q0 + tok) * a.ostride + (int64_t)(kvh * a.G + q - tok * a.G) * D;
     };
-    // (r is that of the last tile, or of the tile's last block: the same for all threads of an accumulator)
     if (!kOne && n_splits == 1) {
       // normalise; a thread writes its row, a whole 32-byte sector at a time where rows are aligned to that (through shared
       // memory to coalesced rows, side by side: 228.7 us for the prompts; 16 bytes at a time 228.3; 32: 221.4)
@@ -799,7 +826,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         }
       }
     } else {
-      ok = ok && warp_wait(&bar->o_done[t ^ 1], 0, bar, a.status);   // all operand tiles are free
+      ok = ok && tile_wait(&bar->o_done[t ^ 1], 0, bar, a.status);   // all operand tiles are free
       // both accumulators to shared memory, [t][row][D] with 16-byte run c of a row at c ^ (row & 7), and their (m, l, r)
       float* so = reinterpret_cast<float*>(smem) + (t * kBM + row) * D;
       float4* ml = reinterpret_cast<float4*>(smem + 2 * kBM * D * 4);
@@ -829,8 +856,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         if constexpr (kOne) {                        // the two key sets
           const float4 o = ml[kBM + r];
           const float4 y = *reinterpret_cast<const float4*>(base + (kBM + r) * D + ((c ^ (r & 7)) << 2));
-          const float M2 = fmaxf(M, o.x), R2 = fmaxf(R, o.z), w0 = fast_exp2(M - M2), w1 = fast_exp2(o.x - M2);
-          const float v0 = w0 * pow2_any((int)(R - R2)), v1 = w1 * pow2_any((int)(o.z - R2));
+          const float M2 = fmaxf(M, o.x), R2 = floorf(fmaxf((M - M2) + R, (o.x - M2) + o.z));   // (as join_ref)
+          const float w0 = fast_exp2(M - M2), w1 = fast_exp2(o.x - M2);
+          const float v0 = fast_exp2((M - M2) + (R - R2)), v1 = fast_exp2((o.x - M2) + (o.z - R2));
           x = make_float4(fmaf(x.x, v0, y.x * v1), fmaf(x.y, v0, y.y * v1), fmaf(x.z, v0, y.z * v1), fmaf(x.w, v0, y.w * v1));
           L = fmaf(L, w0, o.y * w1);
           M = M2;
@@ -856,7 +884,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
 }
 
 // Joins the key splits of the chunk kernel: a warp for a row.  (A kernel of its own: the last of 18 splits took 27 us to join
-// 128 rows by itself.)  With M = max m, R = max r: O = 2^R sum 2^(m - M) 2^(r - R) O_s / sum 2^(m - M) l_s.
+// 128 rows by itself.)  With M = max m, R from join_ref: O = 2^R sum 2^(m - M) 2^(r - R) O_s / sum 2^(m - M) l_s.
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ PagedAttnArgs a, int tiles) {
   constexpr int kRuns = D / 4, kFly = 4;
@@ -893,14 +921,14 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Paged
     M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
     R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, off));
   }
+  R = join_ref(M, R, e0, n_splits, [&](int sp) { return __ldcg(mls + first + sp * next); });
   float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   for (int s0 = 0; s0 < n_splits; s0 += 32) {        // weights of 32 splits, a lane each
     float w = 0.0f;
     if (s0 + lane < n_splits) {
       const float4 e = s0 == 0 ? e0 : __ldcg(mls + first + (s0 + lane) * next);
-      const float f = fast_exp2(e.x - M);
-      L = fmaf(f, e.y, L);
-      w = f * pow2_any((int)(e.z - R));
+      L = fmaf(fast_exp2(e.x - M), e.y, L);
+      w = fast_exp2((e.x - M) + (e.z - R));
     }
     const int n = min(32, n_splits - s0);
     for (int k0 = 0; k0 < n; k0 += kFly) {

@@ -17,7 +17,10 @@
 //             quarter warp then meet in a bank, neither for keys (4 lanes on a row) nor for values (2 runs of 4 rows).
 //   scales    e_k is in the factor of the exponent and e_v - r in its summand (r: see kRefWindow), so no key or value
 //             is scaled.  m is raised only when a row outgrows it by 2^4: a vote finds that no row does, without a maximum
-//             over lanes, and O is seldom rescaled.
+//             over lanes, and O is seldom rescaled.  r is one for a warp's rows: it goes with a block outside its window if all rows hold
+//             nothing yet, or see large p there, or it is near, and if O has room.  Where that does not hold (blocks of values that
+//             differ by 2^40 and more, or by less with rows that give the larger next to nothing) the CTA does its rows again by
+//             exact_rows.  (References of the rows' own, held in shared memory, cost every call 4-7%.)
 // What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 50 us, 5.3 TB/s, where
 // reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 82.3 us, 5.9 TB/s (76.4).  With
 // little to read the launch and the join do: one token of 12 heads over 1561 keys 6.7 us.  At 16 rows its products and
@@ -35,8 +38,8 @@ constexpr int kFewThreads = (kWarps + 1) * 32;
 constexpr int kStages = 4;
 constexpr float kLowest = -3.402823466e38f;           // m before any key: finite, so that 2^(-inf - m) is 0
 constexpr float kRaise = 4.0f;                        // log2 units by which a row may outgrow m
+constexpr int kApart = 1 << 20, kCloseRefs = 40, kRaised = 74;   // see few_kernel
 constexpr float kShiftP = 8.0f;                       // p is stored times 2^8: at most 2^12 in f16
-constexpr int kNoRef = -1000;                         // r before any block but zeros
 
 template <int D>
 struct FewLayout {
@@ -67,10 +70,101 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+// 2^k in 64 bits, k in [-1022, 1023]
+__device__ __forceinline__ double pow2_double(int k) { return __hiloint2double((1023 + k) << 20, 0); }
 // byte offset of 16-byte run c of row `row` in a tile (TMA swizzle of the row length)
 template <int D>
 __device__ __forceinline__ int run_at(int row, int c) {
   return D == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+}
+
+// A CTA's rows over its key tiles once more, O in 64 bits and without references: where the blocks of values of its keys differ by more
+// than the rows can go through together.  A warp to a row, 32 keys (of one block) at a time.  Writes what the tensor-core path would: O, or O and (m, l, r) to part and mls.
+template <int D>
+__device__ __forceinline__ void exact_rows(const PagedAttnArgs& a, int s, int kvh, int row0, int rows, TileRange tr, int i0, int i1,
+                                        float* part, float4* mls, uint8_t* smem) {
+  constexpr int kC = D / 32;                            // channels of a lane
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_keys = a.seqs.n_keys[s], p_first = n_keys - a.seqs.n_q[s], last_page = max(n_keys - 1, 0) / a.P;
+  const int* table = a.table + (int64_t)a.seqs.slot[s] * a.max_pages;
+  float* q = reinterpret_cast<float*>(smem) + warp * D;
+#pragma unroll 1
+  for (int row = warp; row < rows; row += kWarps + 1) {
+    const int rr = row0 + row, tok = a.by_g.div(rr), pos = p_first + tok;
+    const int64_t at = (int64_t)(kvh * a.G + rr - tok * a.G) * D + kC * lane;
+    const bf16* src = a.Q + ((int64_t)a.seqs.q0[s] + tok) * a.qstride + at;
+    const int limit = a.mask.causal ? min(pos + 1, n_keys) : n_keys, lower = a.mask.window > 0 ? pos - a.mask.window + 1 : 0;
+    float top = 0.0f;
+    bool fine = true;
+    for (int c = 0; c < kC; ++c) {
+      const float x = __bfloat162float(src[c]);
+      fine = fine && fabsf(x) <= 3.402823466e38f;
+      top = fmaxf(top, fabsf(x));
+    }
+    for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    fine = __all_sync(0xffffffffu, fine);
+    const int eq = fine ? e4m3_row_exponent(top) : 0;
+    __syncwarp();
+    for (int c = 0; c < kC; ++c) q[kC * lane + c] = fine ? __bfloat162float(src[c]) * pow2f(-eq) : 0.0f;
+    __syncwarp();
+    double o[kC] = {}, l = 0.0;
+    float m = kLowest;
+#pragma unroll 1
+    for (int i = 2 * i0; i < 2 * i1; ++i) {
+      const int key = tr.at(i >> 1) * kPagedFewTile + (i & 1) * 32 + lane;
+      const int64_t block = (int64_t)__ldg(table + min(key / a.P, last_page)) * a.Hkv + kvh, place = (block * a.P + key % a.P) * D;
+      const bool seen = key < limit && (key >= lower || key < a.mask.sinks);
+      float x = -INFINITY;
+      if (seen) {
+        float dot = 0.0f;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 4) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(a.k + place + c);
+          const uint32_t h0 = f16x2_of_e4m3x2((uint16_t)w), h1 = f16x2_of_e4m3x2((uint16_t)(w >> 16));
+          const float2 k0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), k1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+          dot = fmaf(q[c], k0.x, fmaf(q[c + 1], k0.y, fmaf(q[c + 2], k1.x, fmaf(q[c + 3], k1.y, dot))));
+        }
+        x = (float)fmin(fmax((double)dot * a.scale_log2 * pow2_double(eq + a.ke[block]), -3e38), 3e38);
+      }
+      float mx = x;
+      for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+      if (!(mx > -INFINITY)) continue;
+      if (mx > m) {
+        const double al = exp2((double)m - mx);
+        m = mx;
+        l *= al;
+        for (int c = 0; c < kC; ++c) o[c] *= al;
+      }
+      const float p = seen ? exp2f(x - m) : 0.0f;
+      l += p;
+      float sum[kC] = {};
+#pragma unroll 1
+      for (int k = 0; k < 32; ++k) {
+        const float w = __shfl_sync(0xffffffffu, p, k);
+        const int64_t pk = __shfl_sync(0xffffffffu, place, k);
+        for (int c = 0; c < kC; c += 2) {
+          const uint32_t h = f16x2_of_e4m3x2(*reinterpret_cast<const uint16_t*>(a.v + pk + kC * lane + c));
+          const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+          sum[c] = fmaf(w, v.x, sum[c]);
+          sum[c + 1] = fmaf(w, v.y, sum[c + 1]);
+        }
+      }
+      const double size = pow2_double(a.ve[block]);       // (of one block)
+      for (int c = 0; c < kC; ++c) o[c] = fma((double)sum[c], size, o[c]);
+    }
+    for (int off = 16; off >= 1; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+    if (!part) {                                        // no visible key: 0; infinities or NaN in the query: NaN
+      bf16* out = a.O + ((int64_t)a.seqs.q0[s] + tok) * a.ostride + at;
+      for (int c = 0; c < kC; ++c) out[c] = __float2bfloat16_rn(!fine ? NAN : l > 0.0 ? (float)(o[c] / l) : 0.0f);
+      continue;
+    }
+    double most = 0.0;                                  // r: the exponent of the largest |O|
+    for (int c = 0; c < kC; ++c) most = fmax(most, fabs(o[c]));
+    for (int off = 16; off >= 1; off >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, off));
+    const int r = most > 0.0 ? min(max(ilogb(most), -110), 110) : kNoRef;
+    for (int c = 0; c < kC; ++c) part[(int64_t)row * D + kC * lane + c] = r == kNoRef ? 0.0f : (float)(o[c] * pow2_double(-r)) * (1 << (int)kShiftP);
+    if (lane == 0) mls[row] = make_float4(m, fine ? (float)(l * (1 << (int)kShiftP)) : NAN, (float)r, 0.0f);
+  }
 }
 
 template <int D, int kN>
@@ -130,7 +224,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     m[j][0] = m[j][1] = kLowest;
     l[j][0] = l[j][1] = 0.0f;
   }
-  int r = kNoRef;
+  int r = kNoRef, raised = 0;                           // reference of the warp's O, and by how much moves down have lifted O
+  bool zeros = false, edge = false, apart = false;      // see below
   const int g = lane >> 2, t = lane & 3;
 
   if (warp == kWarps) {
@@ -296,9 +391,12 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           grows |= fmaxf(sv[j][h], sv[j][2 + h]) > m[j][h] + kRaise;
         }
       const bool move = ev != kZeroExp && (ev > r || ev < r - kRefWindow);   // warp-uniform
+      zeros |= ev == kZeroExp;
+      edge |= move && !full;
       if (__any_sync(0xffffffffu, grows || move)) {
-        const float fr = move ? pow2_any(r - (ev + kRefRoom)) : 1.0f;
-        if (move) r = ev + kRefRoom;
+        const int to = ev + kRefRoom;
+        bool seen = false, go = raised + r - to <= kRaised;
+        float al[kN][2];
 #pragma unroll
         for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -306,17 +404,37 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             float mx = fmaxf(sv[j][h], sv[j][2 + h]);    // over the 16 keys
 #pragma unroll
             for (int off = 4; off <= 16; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-            const float mn = fmaxf(m[j][h], mx), al = fast_exp2(m[j][h] - mn);
+            const float mn = fmaxf(m[j][h], mx);
+            seen |= mx > -INFINITY;
+            go &= r == kNoRef || m[j][h] == kLowest || 8 * j + 2 * t + h >= rows || to <= r + kAbove || mx - mn >= kAskPast;
+            al[j][h] = fast_exp2(m[j][h] - mn);
             m[j][h] = mn;
-            l[j][h] *= al;
+            l[j][h] *= al[j][h];
+          }
+        if (move && __any_sync(0xffffffffu, seen)) {     // the rows go together, or not at all
+          apart |= !__all_sync(0xffffffffu, go);
+          const float f = pow2_any(r - to);
+          raised = r == kNoRef ? 0 : max(0, raised + r - to);
+          r = to;
 #pragma unroll
-            for (int c = 0; c < kRowTiles; ++c) {
-              o[j][c][h] *= al * fr;
-              o[j][c][2 + h] *= al * fr;
-            }
+          for (int j = 0; j < kN; ++j) {
+            al[j][0] *= f;
+            al[j][1] *= f;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kN; ++j)
+#pragma unroll
+          for (int c = 0; c < kRowTiles; ++c) {
+            o[j][c][0] *= al[j][0];
+            o[j][c][1] *= al[j][1];
+            o[j][c][2] *= al[j][0];
+            o[j][c][3] *= al[j][1];
           }
       }
-      const float we = kShiftP + (ev == kZeroExp ? 0.0f : (float)(ev - r)), fl = ev == kZeroExp ? 1.0f : pow2f(r - ev);
+      // (a block of which no row sees a key may still be far from r: its numerators are 0)
+      const int d = ev == kZeroExp ? 0 : min(max(ev - r, -kRefWindow), 0);
+      const float we = kShiftP + (float)d, fl = pow2f(-d);
       uint32_t p0[kN], p1[kN];
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
@@ -360,7 +478,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   // ---- the warps' (m, l, r) and O
   float* sO = reinterpret_cast<float*>(smem);           // [warp][row][D], 16-byte run c of row at c ^ (row & 7)
   __shared__ float sm[kWarps][kRows], sl[kWarps][kRows];
-  __shared__ int sr[kWarps];
+  __shared__ int sr[kWarps];                            // reference (kApart: what the warp holds is of no use)
   if (warp < kWarps) {
 #pragma unroll
     for (int j = 0; j < kN; ++j)
@@ -379,11 +497,18 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           sl[warp][row] = l[j][h];
         }
       }
-    if (lane == 0) sr[warp] = r;
+    // (A row that took a block's reference without seeing it, and then saw blocks of zeros, holds nothing of that size.)
+    apart |= zeros && edge;
+    if (lane == 0) sr[warp] = apart ? kApart : r;
   }
   __syncthreads();
   // O of the CTA relative to (M, 2^R): weights 2^(m_w - M) 2^(r_w - R)
-  const int R = max(max(sr[0], sr[1]), max(sr[2], sr[3]));
+  int r_low = INT_MAX, R = kNoRef;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    R = max(R, sr[w]);
+    if (sr[w] != kNoRef) r_low = min(r_low, sr[w]);
+  }
   const int cta = a.seqs.part0[s] + kvh * (a.seqs.item0[s + 1] - a.seqs.item0[s]) + item;   // workspace slot
   constexpr int kRuns = D / 4;
   auto out_row = [&](int row) {
@@ -392,8 +517,14 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   };
   float4* part = reinterpret_cast<float4*>(a.part);                     // [slot][row][run]
   float4* mls = part + (int64_t)kPartSlots * kPagedFewRows * kRuns;     // [slot][row]: m, l, r
+  const bool together = R < kApart && R - r_low <= kCloseRefs;
+  if (!together) {
+    __syncthreads();                                    // (the numbers above have been read)
+    exact_rows<D>(a, s, kvh, row0, rows, tr, i0, i1, n_splits > 1 ? a.part + (int64_t)cta * kPagedFewRows * D : nullptr,
+                  mls + cta * kPagedFewRows, smem);
+  }
 #pragma unroll 1
-  for (int i = threadIdx.x; i < rows * kRuns; i += kFewThreads) {
+  for (int i = threadIdx.x; together && i < rows * kRuns; i += kFewThreads) {
     const int row = i / kRuns, c = i % kRuns;
     float M = kLowest, L = 0.0f;
 #pragma unroll
@@ -432,7 +563,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
   __syncthreads();
   if (!bar->last) return;
-  // each row's weights 2^(m - M) 2^(r - RR), first (row by row, a warp each), then the sums.  What both need of the workspace
+  // each row's weights (join_ref), first (row by row, a warp each), then the sums.  What both need of the workspace
   // is asked for at once: its numbers of the first 32 splits, and the first twelve runs of a thread's sum.
   float* wts = reinterpret_cast<float*>(smem);          // [row][split]
   constexpr int kRowsEach = (kRows + kWarps) / (kWarps + 1), kFly = 12;
@@ -470,11 +601,11 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
       RR = fmaxf(RR, __shfl_xor_sync(0xffffffffu, RR, off));
     }
+    RR = join_ref(M, RR, e0[k], n_splits, [&](int sp) { return __ldcg(mls + (first + sp) * kPagedFewRows + row); });
     for (int sp = lane; sp < n_splits; sp += 32) {
       const float4 e = sp == lane ? e0[k] : __ldcg(mls + (first + sp) * kPagedFewRows + row);
-      const float f = fast_exp2(e.x - M);
-      L = fmaf(f, e.y, L);
-      wts[row * n_splits + sp] = f * pow2_any((int)(e.z - RR));
+      L = fmaf(fast_exp2(e.x - M), e.y, L);
+      wts[row * n_splits + sp] = fast_exp2((e.x - M) + (e.z - RR));
     }
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
@@ -555,11 +686,12 @@ __global__ void __launch_bounds__(512) few_join_kernel(const __grid_constant__ P
     M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
     R = fmaxf(R, __shfl_xor_sync(0xffffffffu, R, off));
   }
+  R = join_ref(M, R, e0, n_splits, [&](int sp) { return __ldcg(mls + sp * kPagedFewRows); });
   float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   for (int s0 = 0; s0 < n_splits; s0 += 32) {           // weights of 32 splits, a lane each
     const float4 e = s0 == 0 ? e0 : s0 + lane < n_splits ? __ldcg(mls + (s0 + lane) * kPagedFewRows) : none;
-    const float f = s0 + lane < n_splits ? fast_exp2(e.x - M) : 0.0f, w = f * pow2_any((int)(e.z - R));
-    L = fmaf(f, e.y, L);
+    const float w = s0 + lane < n_splits ? fast_exp2((e.x - M) + (e.z - R)) : 0.0f;
+    L = fmaf(s0 + lane < n_splits ? fast_exp2(e.x - M) : 0.0f, e.y, L);
     const int n = min(32, n_splits - s0);
     for (int k0 = 0; k0 < n; k0 += kFly) {
       float4 x[kFly];

@@ -664,6 +664,8 @@ fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_strid
     if (!rows_ok(h, Q, q_stride, c.n_q_heads) || !rows_ok(h, O, o_stride, c.n_q_heads)) return FK_ERR_ARG;
     std::unique_ptr<PagedAttnArgs> a(new PagedAttnArgs);
     a->table = h->table;
+    a->k = h->pools[layer].k;
+    a->v = h->pools[layer].v;
     a->ke = h->pools[layer].ke;
     a->ve = h->pools[layer].ve;
     a->max_pages = h->max_pages;
