@@ -18,8 +18,10 @@ constexpr int kPartSlots = 4096;      // CTAs of a launch that share their rows 
 constexpr int kZeroExp = -126;
 // The attention folds a value block's 2^e into the softmax numerators, w = p 2^(e - r), as f16, relative to a
 // reference r that O (fp32) is kept to: e - r stays in [-kRefWindow, 0] where the rows go together, and a block outside asks for
-// r = e + kRefRoom: O moves by a power of two, as far as what it holds allows.
-constexpr int kRefWindow = 16, kRefRoom = 2;
+// r = e + kRefRoom: O moves by a power of two, as far as what it holds allows.  f16 has 2^-24 and up, so that p = 2^-24 is the
+// smallest that counts at the window's end, and 2^-13 the smallest that keeps all 11 bits (a window of 16 lost all p below 2^-17 there, which
+// l counts: thousands of keys of small weight gave 0).
+constexpr int kRefWindow = 8, kRefRoom = 2;
 constexpr int kNoRef = -1000;         // r before any block but zeros
 constexpr int kAskPast = -8;          // log2 of a block's largest p from which on a row simply takes a larger block's reference
 

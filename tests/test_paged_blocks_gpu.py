@@ -190,3 +190,25 @@ def test_steps_and_slices_over_blocks_far_apart(nq):
                 assert (np.abs(got[qat: qat + m, 3:11] - want) <= bound).all(), (n, mask)
                 at, qat = at + n, qat + m
         assert cache.sync_status() == 0
+
+
+@pytest.mark.parametrize("heads,D,nq", [((4, 2), 128, 1), ((8, 1), 64, 2), ((8, 2), 128, 64), ((8, 2), 64, 70)])
+@pytest.mark.parametrize("ratio", [2.0 ** 6, 2.0 ** 9, 2.0 ** 13])
+def test_many_keys_of_small_weight_in_small_blocks(heads, D, nq, ratio):
+    """One key of 16 holds nearly all the weight and a value of 0, the others share the rest, and the first value is larger than
+    theirs: whatever page the numerators go by, those of 2^-20 have to count.  (As many sequences as fill the device, so that no keys are split.)"""
+    n, B = 1500, 160
+    r = np.random.default_rng(88)
+    u = np.sign(r.standard_normal(D))
+    K, V = np.zeros((n, heads[1], D)), 1.0 + 0.1 * r.random((n, heads[1], D))
+    K[5::16] = 20 * np.log(2) / np.sqrt(D) * u
+    V[5::16] = 0
+    V[0] *= ratio
+    K, V, Q = (P.to_bf16(np.ascontiguousarray(x, dtype=np.float32)) for x in (K, V, np.broadcast_to(u, (nq, heads[0], D))))
+    with T._cache(n_q_heads=heads[0], n_kv_heads=heads[1], head_dim=D, page_tokens=64, max_seqs=B, n_pages=24 * B, max_seq_tokens=n) as cache:
+        cache.step(range(B), [n] * B, [nq] * B)
+        cache.append(0, T._bf16(K).repeat(B, 1, 1), T._bf16(V).repeat(B, 1, 1))
+        for mask in (dict(), dict(causal=False), dict(window=700, sinks=1)):
+            got = T._np(cache.attend(0, T._bf16(Q).repeat(B, 1, 1), **mask))
+            want, bound = exact(Q, P.held(K, 64), P.held(V, 64), 64, **mask)
+            assert (np.abs(got[:nq] - want) <= bound).all() and np.array_equal(got[:nq], got[-nq:]), mask
