@@ -140,7 +140,8 @@ __device__ __forceinline__ void rotate_row(const AppendArgs& a, int pos, int j, 
   rotate16(x, cs, sn, a.interleaved);
 }
 
-// Largest finite magnitude of 16 values; `bad` when one is not finite.
+// Largest finite magnitude of 16 values; `bad` when one is not finite.  (Beside an infinity at least the smallest number, which has the
+// exponent of zeros, -120, but is not one: a block of zeros and infinities holds 448 2^-120, and kZeroExp says that it holds nothing.)
 __device__ __forceinline__ float largest16(const float* x, bool& bad) {
   float m = 0.0f;
   float2 z = make_float2(0.0f, 0.0f);
@@ -153,7 +154,7 @@ __device__ __forceinline__ float largest16(const float* x, bool& bad) {
     m = 0.0f;
 #pragma unroll
     for (int c = 0; c < 16; ++c)
-      if (fabsf(x[c]) <= 3.402823466e38f) m = fmaxf(m, fabsf(x[c]));
+      if (x[c] == x[c]) m = fmaxf(m, fabsf(x[c]) <= 3.402823466e38f ? fabsf(x[c]) : __uint_as_float(1u));
   }
   return m;
 }

@@ -212,3 +212,26 @@ def test_many_keys_of_small_weight_in_small_blocks(heads, D, nq, ratio):
             got = T._np(cache.attend(0, T._bf16(Q).repeat(B, 1, 1), **mask))
             want, bound = exact(Q, P.held(K, 64), P.held(V, 64), 64, **mask)
             assert (np.abs(got[:nq] - want) <= bound).all() and np.array_equal(got[:nq], got[-nq:]), mask
+
+
+@pytest.mark.parametrize("D,page,news", [(128, 64, [3, 5, 40]), (64, 32, [70, 1]), (128, 32, [1, 1, 1, 20, 8])])
+def test_infinities_among_zeros(D, page, news):
+    """A page whose finite values are all 0 holds an infinity as its largest magnitude, 448 2^-120, as any page does: what `read` gives is
+    what the attention sees, however the tokens came, and until a token of ordinary size joins the page."""
+    n = sum(news)
+    K, V = np.zeros((n, 2, D), np.float32), np.zeros((n, 2, D), np.float32)
+    K[0, 0, 3], K[1 % n, 1, 5], V[0, 0, 1], V[2 % n, 1, 7], V[2 % n, 1, 9] = np.inf, -np.inf, -np.inf, np.inf, np.nan
+    K[n - 3, 0] = 1.5                                      # (in the last page)
+    Q = P.to_bf16(np.random.default_rng(89).standard_normal((n, 4, D)).astype(np.float32))
+    with T._cache(head_dim=D, page_tokens=page) as cache:
+        at = 0
+        for b in news:
+            cache.step([0], [b])
+            cache.append(0, T._bf16(K[at: at + b]), T._bf16(V[at: at + b]))
+            at += b
+            hk, hv = cache.read(0, whole=True)
+            assert np.array_equal(T._np(hk), P.held(K[:at], page)) and np.array_equal(T._np(hv), P.held(V[:at], page))
+            got = T._np(cache.attend(0, T._bf16(Q[at - b: at])))
+            want, bound = exact(Q[at - b: at], P.held(K[:at], page), P.held(V[:at], page), page)
+            assert (np.abs(got - want) <= bound).all()
+        assert cache.sync_status() == 5
