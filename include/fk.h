@@ -465,8 +465,9 @@ FK_API int64_t fk_paged_free_pages(const fk_paged* h);
 FK_API size_t fk_paged_reserved_bytes(const fk_paged* h);
 FK_API int64_t fk_paged_launch_count(const fk_paged* h);
 
-/* Synchronize `stream` and report (then clear) device-side conditions: FK_ERR_TIMEOUT (a bounded wait
- * expired), FK_ERR_RANGE (an appended key or value that was not finite, a position outside the tables), FK_OK. */
+/* Synchronize `stream` and report (then clear, in the stream's order) device-side conditions of the work it waited for:
+ * FK_ERR_TIMEOUT (a bounded wait expired), FK_ERR_RANGE (an appended key or value that was not finite, a position outside the
+ * tables; after a timeout it is the next call's), FK_OK. */
 FK_API fk_status fk_paged_sync_status(fk_paged* h, void* stream);
 
 /* Static text for a status code. */

@@ -110,6 +110,9 @@ struct TableArgs {                    // table[index[i]] = page[i]
 };
 cudaError_t launch_paged_table(const TableArgs& a, cudaStream_t s);
 
+// *report = what is to be reported of *status, which is cleared of it
+cudaError_t launch_paged_status(int* status, int* report, cudaStream_t s);
+
 // Visible keys of the query at position p of a sequence of n keys: j < (causal ? p + 1 : n), and under a window W
 // also j > p - W or j < sinks.
 struct PagedMask {

@@ -435,6 +435,13 @@ __global__ void table_kernel(const __grid_constant__ TableArgs a) {
   if (i < a.n) a.table[a.index[i]] = a.page[i];
 }
 
+// The status word's report: a timeout by itself, else all there is; only what is reported is cleared.
+__global__ void status_kernel(int* status, int* report) {
+  const int word = atomicOr(status, 0), told = word & kStatusTimeout ? kStatusTimeout : word;
+  atomicAnd(status, ~told);
+  *report = told;
+}
+
 }  // namespace
 
 cudaError_t launch_paged_append(int D, const AppendArgs& a, cudaStream_t s) {
@@ -466,6 +473,11 @@ cudaError_t launch_paged_read(int D, const ReadArgs& a, cudaStream_t s) {
 cudaError_t launch_paged_table(const TableArgs& a, cudaStream_t s) {
   if (a.n == 0) return cudaSuccess;
   table_kernel<<<(a.n + 127) / 128, 128, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_paged_status(int* status, int* report, cudaStream_t s) {
+  status_kernel<<<1, 1, 0, s>>>(status, report);
   return cudaGetLastError();
 }
 

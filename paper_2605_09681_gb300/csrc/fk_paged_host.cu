@@ -69,7 +69,7 @@ struct fk_paged {
   float* part_chunk = nullptr;
   int part_tiles = 0;                 // query tiles that part_chunk holds
   int* arrived = nullptr;
-  int* status = nullptr;
+  int* status = nullptr;              // the status word, and a report of it
   int sms = 0;
   std::vector<void*> allocs;
   size_t reserved = 0;
@@ -500,7 +500,7 @@ fk_status fk_paged_create(const fk_paged_config* cfg, fk_paged** out) {
     h->part_tiles = std::min(4 * h->sms, kPartSlots);
     get((size_t)h->part_tiles * kAttnBM * (D + 4) * sizeof(float), &h->part_chunk);
     get(kPartSlots * sizeof(int), &h->arrived);
-    get(sizeof(int), &h->status);
+    get(2 * sizeof(int), &h->status);
     if (e != FK_OK) return e;
     if (paged_few_prepare((int)D) != cudaSuccess || paged_chunk_prepare((int)D) != cudaSuccess) return FK_ERR_CUDA;
     if (cudaDeviceSynchronize() != cudaSuccess) return FK_ERR_CUDA;
@@ -778,10 +778,11 @@ fk_status fk_paged_sync_status(fk_paged* h, void* stream) {
   if (dev.err != cudaSuccess) return FK_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int word = 0;
-  if (cudaMemcpyAsync(&word, h->status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+  // (cleared by a kernel of the same stream: a memset of the legacy one would come whenever that has time, and take later reports with it)
+  if (done(h, launch_paged_status(h->status, h->status + 1, s)) != FK_OK ||
+      cudaMemcpyAsync(&word, h->status + 1, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
       cudaStreamSynchronize(s) != cudaSuccess)
     return FK_ERR_CUDA;
-  if (word && cudaMemset(h->status, 0, sizeof(int)) != cudaSuccess) return FK_ERR_CUDA;
   if (word & kStatusTimeout) return FK_ERR_TIMEOUT;
   if (word & (kStatusNonFinite | kStatusPosition)) return FK_ERR_RANGE;
   return FK_OK;

@@ -1,0 +1,51 @@
+"""What the paged cache's calls owe beside their values: reports that are neither lost nor given twice, whatever the streams."""
+import pytest
+import torch
+
+import test_paged_gpu as T
+
+pytestmark = pytest.mark.gpu
+
+RANGE = 5                                                  # FK_ERR_RANGE
+
+
+def _busy(ms=60):
+    """Keep the current stream busy for a while."""
+    torch.cuda._sleep(int(ms * 2e6))
+
+
+def test_a_report_is_cleared_on_its_own_stream():
+    """A report read on a side stream is cleared there and then: not when the legacy stream, busy with other work, comes to it, which
+    would give it twice and take a later one with it."""
+    side = torch.cuda.Stream()
+    good = torch.ones((3, 2, 128), dtype=torch.bfloat16, device="cuda")
+    bad = torch.full((3, 2, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    with T._cache() as cache, torch.cuda.stream(side):
+        cache.step([0], [3])
+        cache.append(0, bad, good)
+        side.synchronize()
+        with torch.cuda.stream(torch.cuda.default_stream()):
+            _busy()
+        assert cache.sync_status() == RANGE
+        assert cache.sync_status() == 0                    # (while the default stream is still busy)
+        cache.append(0, good, bad)
+        side.synchronize()
+        torch.cuda.default_stream().synchronize()
+        assert cache.sync_status() == RANGE and cache.sync_status() == 0
+
+
+def test_reports_of_two_streams():
+    """What one stream reports and clears leaves what another sets afterwards."""
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    good = torch.ones((3, 2, 128), dtype=torch.bfloat16, device="cuda")
+    bad = torch.full((3, 2, 128), float("inf"), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    with T._cache() as cache:
+        cache.step([0], [3], stream=one)
+        cache.append(0, good, bad, stream=one)
+        assert cache.sync_status(stream=one) == RANGE
+        cache.append(0, bad, good, stream=two)
+        assert cache.sync_status(stream=two) == RANGE and cache.sync_status(stream=one) == 0
+        cache.append(0, good, good, stream=two)
+        assert cache.sync_status(stream=two) == 0
