@@ -316,8 +316,9 @@ class PagedKVCache:
 
     Tensors are bf16 CUDA tensors [tokens, heads, head_dim], the step's sequences one after the other in its order;
     they may be slices of wider rows (a fused projection's output).  Calls are asynchronous on `stream`
-    (default: torch's current stream of the cache's device).  The step's tokens belong to their sequences from the
-    next step on; until then append may be called again with other keys and values, which take their place."""
+    (default: torch's current stream of the cache's device), and tensors that they make are that stream's.  The step's
+    tokens belong to their sequences from the next step on; until then append may be called again with other keys and
+    values, which take their place."""
 
     def __init__(self, *, n_layers, n_q_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs,
                  max_seq_tokens, rope="half", device=0):
@@ -360,6 +361,17 @@ class PagedKVCache:
             except AttributeError:
                 return torch.cuda.current_stream(self.device).cuda_stream
         return getattr(stream, "cuda_stream", stream)
+
+    def _made(self, shape, stream):
+        """An output tensor, of the memory of the stream that is to write it: the current stream may still have work
+        queued on memory that it has given back."""
+        import torch
+        raw = self._on(stream)
+        if raw == self._on(None):
+            return torch.empty(shape, dtype=self._bf16, device=self._dev)
+        own = torch.cuda.ExternalStream(raw, device=self._dev) if raw else torch.cuda.default_stream(self._dev)
+        with torch.cuda.stream(own):
+            return torch.empty(shape, dtype=self._bf16, device=self._dev)
 
     def _rows(self, x, tokens, heads, name):
         """(address, elements from token to token) of a [tokens, heads, head_dim] tensor.  (Few tensor properties are
@@ -413,8 +425,8 @@ class PagedKVCache:
         if Q is not None:
             q, qs = self._rows(Q, self._new, self.n_q_heads, "Q")
             if Q_out is None:
-                import torch
-                Q_out = torch.empty_like(Q)          # (dense: rows of a wider tensor are not kept apart)
+                import torch                         # (dense: rows of a wider tensor are not kept apart)
+                Q_out = torch.empty_like(Q) if stream is None else self._made(Q.shape, stream)
                 o, os = Q_out.data_ptr(), self.n_q_heads * self.head_dim
             else:
                 o, os = self._rows(Q_out, self._new, self.n_q_heads, "Q_out")
@@ -433,7 +445,7 @@ class PagedKVCache:
         q, qs = self._rows(Q, self._queries, self.n_q_heads, "Q")
         if O is None:
             import torch
-            O = torch.empty_like(Q)
+            O = torch.empty_like(Q) if stream is None else self._made(Q.shape, stream)
             o, os = O.data_ptr(), self.n_q_heads * self.head_dim
         else:
             o, os = self._rows(O, self._queries, self.n_q_heads, "O")
@@ -456,11 +468,9 @@ class PagedKVCache:
                 self._rows(x, n, self.n_kv_heads, "K, V")
                 if not x.is_contiguous():
                     raise ValueError("K, V: expected contiguous tensors")
-        if K is None or V is None:
-            import torch
-            shape = (n, self.n_kv_heads, self.head_dim)
-            K = torch.empty(shape, dtype=self._bf16, device=self._dev) if K is None else K
-            V = torch.empty(shape, dtype=self._bf16, device=self._dev) if V is None else V
+        shape = (n, self.n_kv_heads, self.head_dim)
+        K = self._made(shape, stream) if K is None else K
+        V = self._made(shape, stream) if V is None else V
         k, v = K.data_ptr(), V.data_ptr()
         _check(self._lib.fk_paged_read(self._h, layer, 1 if whole else 0, k, v, n, self._count, self._on(stream)),
                "fk_paged_read")

@@ -49,3 +49,47 @@ def test_reports_of_two_streams():
         assert cache.sync_status(stream=two) == RANGE and cache.sync_status(stream=one) == 0
         cache.append(0, good, good, stream=two)
         assert cache.sync_status(stream=two) == 0
+
+
+@pytest.mark.parametrize("call", ["append", "attend", "read"])
+def test_outputs_made_for_another_stream(call):
+    """A tensor that the current stream has given back while its work on it is still queued is not written by another one."""
+    side, n = torch.cuda.Stream(), 64
+    kv = torch.ones((n, 4, 128), dtype=torch.bfloat16, device="cuda")
+    cos, sin = torch.ones((n, 64), device="cuda"), torch.zeros((n, 64), device="cuda")
+    torch.cuda.synchronize()
+    for other in (side, side.cuda_stream):
+        with T._cache(n_kv_heads=4, n_q_heads=4) as cache:
+            cache.step([0], [n], stream=other)
+            cache.append(0, kv, kv, stream=other)
+            side.synchronize()
+            mine = [torch.full((n, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+            seen = [torch.empty_like(x) for x in mine]
+            places = {x.data_ptr() for x in mine}
+            _busy()
+            for x, y in zip(mine, seen):
+                y.copy_(x)
+            del mine, x
+            if call == "append":
+                out = (cache.append(0, kv, kv, cos, sin, Q=kv, stream=other),)
+            elif call == "attend":
+                out = (cache.attend(0, kv, stream=other),)
+            else:
+                out = cache.read(0, stream=other)
+            assert not places & {x.data_ptr() for x in out}
+            side.synchronize()
+            assert all((x == 1).all() for x in out)
+            torch.cuda.synchronize()
+            assert all((y == 7).all() for y in seen)
+            del out
+
+
+def test_the_default_stream_by_its_number():
+    with T._cache() as cache, torch.cuda.stream(torch.cuda.Stream()):
+        kv = torch.ones((3, 2, 128), dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        cache.step([0], [3], stream=0)
+        cache.append(0, kv, kv, stream=0)
+        k, v = cache.read(0, stream=0)
+        torch.cuda.synchronize()
+        assert (k == 1).all() and (v == 1).all()
