@@ -438,8 +438,8 @@ class PagedKVCache:
         """Attention of the step's queries over what their sequences hold: query at position p sees key j when
         j <= p (causal) or any j, and under window > 0 only j > p - window or j < sinks; a query that sees
         none gives 0.  scale: default 1 / sqrt(head_dim)."""
-        if scale is not None and not scale > 0:
-            raise ValueError("scale must be positive")
+        if scale is not None and not ctypes.c_float(scale).value > 0:      # (0 asks for the default)
+            raise ValueError("scale must be positive in fp32")
         if window >= 2 ** 31 or sinks >= 2 ** 31:
             raise ValueError("window, sinks: at most 2^31 - 1")
         q, qs = self._rows(Q, self._queries, self.n_q_heads, "Q")

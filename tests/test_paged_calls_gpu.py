@@ -93,3 +93,19 @@ def test_the_default_stream_by_its_number():
         k, v = cache.read(0, stream=0)
         torch.cuda.synchronize()
         assert (k == 1).all() and (v == 1).all()
+
+
+def test_scales_that_fp32_does_not_hold_are_refused():
+    """A positive scale that is 0 in fp32 is not the default."""
+    from paper_2605_09681_gb300 import FkError
+    kv = torch.ones((3, 2, 128), dtype=torch.bfloat16, device="cuda")
+    with T._cache(n_q_heads=2) as cache:
+        cache.step([0], [3])
+        cache.append(0, kv, kv)
+        for scale in (1e-50, 1e-46, 5e-324, float("nan"), -1.0, 0.0):
+            with pytest.raises(ValueError):
+                cache.attend(0, kv, scale=scale)
+        for scale in (1e39, float("inf")):
+            with pytest.raises(FkError):
+                cache.attend(0, kv, scale=scale)
+        assert (cache.attend(0, kv, scale=1e-40) == 1).all()
