@@ -422,9 +422,9 @@ FK_API void fk_paged_destroy(fk_paged* h);
 
 /* Begin a step of n_seqs different sequences (host arrays): sequence seqs[i] appends n_new[i] >= 0 tokens and asks
  * n_query[i] >= 0 queries (n_query NULL: as many as new tokens), which stand at its last positions.
- * Takes the pages that the new tokens need.  FK_ERR_FULL when too few are free or a sequence would exceed
- * max_seq_tokens, FK_ERR_STATE when the step before was appended to some layers and not to others; a
- * refused step leaves the one before current. */
+ * Queries times n_q_heads are below 2^30, new tokens below 2^31 (FK_ERR_ARG).  Takes the pages that the new
+ * tokens need.  FK_ERR_FULL when too few are free or a sequence would exceed max_seq_tokens, FK_ERR_STATE when
+ * the step before was appended to some layers and not to others; a refused step leaves the one before current. */
 FK_API fk_status fk_paged_step(fk_paged* h, int n_seqs, const int32_t* seqs, const int32_t* n_new,
                                const int32_t* n_query, void* stream);
 

@@ -530,7 +530,8 @@ fk_status fk_paged_step(fk_paged* h, int n_seqs, const int32_t* seqs, const int3
       total += n_new[i];
       queries += n_query ? n_query[i] : n_new[i];
     }
-    if (total >= ((int64_t)1 << 31) || queries * h->cfg.n_q_heads >= ((int64_t)1 << 31)) return FK_ERR_ARG;
+    // (rows and positions are 32-bit numbers in the kernels, where a tile and a window go beside them)
+    if (total >= ((int64_t)1 << 31) || queries * h->cfg.n_q_heads >= ((int64_t)1 << 30)) return FK_ERR_ARG;
     DeviceGuard dev(h->cfg.device);
     if (dev.err != cudaSuccess) return FK_ERR_CUDA;
     // lengths and pages as they are once the current step has ended: a refusal leaves it as it is

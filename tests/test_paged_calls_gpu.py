@@ -109,3 +109,16 @@ def test_scales_that_fp32_does_not_hold_are_refused():
             with pytest.raises(FkError):
                 cache.attend(0, kv, scale=scale)
         assert (cache.attend(0, kv, scale=1e-40) == 1).all()
+
+
+@pytest.mark.parametrize("heads,asks", [(1, 2 ** 31 - 1), (1, 2 ** 30), (8, 2 ** 27), (64, 2 ** 24 + 5)])
+def test_steps_of_more_query_rows_than_the_kernels_count_are_refused(heads, asks):
+    """Rows (queries times heads) and positions are counted in 32 bits, with room for a tile and a window beside them: below 2^30."""
+    from paper_2605_09681_gb300 import FkError
+    with T._cache(n_q_heads=heads, n_kv_heads=1) as cache:
+        for seqs, nq in (([0], [asks]), ([0, 1], [asks - 7, 7])):
+            with pytest.raises(FkError) as e:
+                cache.step(seqs, [1] * len(seqs), nq)
+            assert e.value.name == "FK_ERR_ARG"
+        cache.step([0], [1], [2 ** 30 // heads - 1])
+        assert cache.length(0) == 1
