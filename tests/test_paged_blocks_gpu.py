@@ -235,3 +235,21 @@ def test_infinities_among_zeros(D, page, news):
             want, bound = exact(Q[at - b: at], P.held(K[:at], page), P.held(V[:at], page), page)
             assert (np.abs(got - want) <= bound).all()
         assert cache.sync_status() == 5
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,page,lens,nq", T.ATTEND)
+@pytest.mark.parametrize("spread", [1.0, 5.0])
+def test_every_query_by_what_it_sees(Hq, Hkv, D, page, lens, nq, spread):
+    r = np.random.default_rng(90)
+    K, V, Q = T._normal(r, (sum(lens), Hkv, D), 0.3), T._normal(r, (sum(lens), Hkv, D), spread), T._normal(r, (sum(nq), Hq, D), 0.5)
+    with T._cache(n_q_heads=Hq, n_kv_heads=Hkv, head_dim=D, page_tokens=page, n_pages=sum(-(-n // page) for n in lens) + 1,
+                  max_seqs=len(lens), max_seq_tokens=max(max(lens), 1)) as cache:
+        cache.step(range(len(lens)), lens, nq)
+        cache.append(0, T._bf16(K), T._bf16(V))
+        for mask in T.ALL:
+            got, at, qat = T._np(cache.attend(0, T._bf16(Q), **mask)), 0, 0
+            for n, m in zip(lens, nq):
+                want, bound = exact(Q[qat: qat + m], P.held(K[at: at + n], page), P.held(V[at: at + n], page), page, **mask)
+                assert (np.abs(got[qat: qat + m] - want) <= bound).all(), (mask, n)
+                at, qat = at + n, qat + m
+        assert cache.sync_status() == 0
