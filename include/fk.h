@@ -424,7 +424,9 @@ FK_API void fk_paged_destroy(fk_paged* h);
  * n_query[i] >= 0 queries (n_query NULL: as many as new tokens), which stand at its last positions.
  * Queries times n_q_heads are below 2^30, new tokens below 2^31 (FK_ERR_ARG).  Takes the pages that the new
  * tokens need.  FK_ERR_FULL when too few are free or a sequence would exceed max_seq_tokens, FK_ERR_STATE when
- * the step before was appended to some layers and not to others; a refused step leaves the one before current. */
+ * the step before was appended to some layers and not to others; a refused step leaves the one before current.
+ * Tokens appended to every layer stay (no call takes a step's last tokens back, but fk_paged_drop all of a sequence's); a step that ended
+ * halfway is finished by appending to the layers that are left, whatever it is if its sequences are to be dropped then. */
 FK_API fk_status fk_paged_step(fk_paged* h, int n_seqs, const int32_t* seqs, const int32_t* n_new,
                                const int32_t* n_query, void* stream);
 
@@ -440,7 +442,9 @@ FK_API fk_status fk_paged_append(fk_paged* h, int layer, const void* K, int64_t 
  * (causal = 0), and under window > 0 only j > p - window or j < sinks.  A query that sees no key gives 0.  scale = 0:
  * 1 / sqrt(head_dim).  Logits, softmax and sums are in fp32; products are of the held values and the bf16
  * queries, exact but for query elements below 2^-9 of their row's largest, which may be rounded to 2^-17 of it;
- * softmax numerators are rounded to f16 before they multiply the values.  A query with an infinity or NaN gives NaN
+ * softmax numerators are rounded to f16 before they multiply the values: 11 bits down to 2^-13 of a row's largest, and to 2^-24
+ * of it below.  Pages may differ in size by any amount: what a row does not see does not reach it, and of what it sees only what
+ * lies 2^-100 below the largest value of a page that it sees a key of may be lost.  A query with an infinity or NaN gives NaN
  * in that head and nowhere else.
  * FK_ERR_STATE without a step, or when the layer was not appended to in it. */
 FK_API fk_status fk_paged_attend(fk_paged* h, int layer, const void* Q, int64_t q_stride, void* O,

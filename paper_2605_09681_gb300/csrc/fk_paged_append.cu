@@ -14,8 +14,9 @@
 // tokens are touched.  A step's append may be repeated with other keys and values: nothing it reads is what it wrote.
 // Threads: P D / 32, in rows of D / 16; a thread holds 16 channels (two runs of 8, the two halves of its pairs) of
 // 2 tokens, so that a page is loaded at once and never read again.  Steps of a few tokens: append_few_kernel.
-// What bounds it: bytes move at half the copy rate, for the instructions of rotation, maximum and rounding (issue slots 51%
-// busy) between waits for loads.  4680 tokens of 12 + 12 + 12 heads of 128, pages of 128: 21.2 us (75 MB, 3.5 TB/s);
+// What bounds it: latency.  Bytes move at half the copy rate: a CTA loads, reduces and stores once, two of 512 threads fit an SM, its rotation
+// factors are asked for when its rows are there, and nothing is in flight from one page to the next (issue slots 51% busy, loads
+// the first reason to wait).  4680 tokens of 12 + 12 + 12 heads of 128, pages of 128: 21.0 us (75 MB, 3.6 TB/s);
 // reading the 37 pages back as bf16 9.3 us (43 MB, 4.6 TB/s).  Keys, values and queries in CTAs of their own, so that registers hold one tensor's
 // rows (all three in one CTA: 25.6 us).
 #include "fk_paged.h"

@@ -21,10 +21,10 @@
 //             nothing yet, or see large p there, or it is near, and if O has room.  Where that does not hold (blocks of values that
 //             differ by 2^40 and more, or by less with rows that give the larger next to nothing) the CTA does its rows again by
 //             exact_rows.  (References of the rows' own, held in shared memory, cost every call 4-7%.)
-// What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 50 us, 5.3 TB/s, where
-// reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 82.3 us, 5.9 TB/s (76.4).  With
-// little to read the launch and the join do: one token of 12 heads over 1561 keys 6.7 us.  At 16 rows its products and
-// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.1 us).
+// What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 51 us, 5.2 TB/s, where
+// reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 83 us, 5.9 TB/s (76.4).  With
+// little to read the launch and the join do: one token of 12 heads over 1561 keys 6.5-6.9 us.  At 16 rows its products and
+// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.3 us).
 // Splits leave (m, l, r, O) in a workspace; the last one to arrive (8 rows) or a kernel of its own (16) joins them in the order of
 // the splits (no atomics on values: results do not change from run to run).
 #include "fk_paged.h"
@@ -652,8 +652,8 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 }
 
 // The same join by a kernel of its own, a warp for a row, for 16-row CTAs: one CTA would take long over the rows of many splits
-// (two queries of 64 heads over 20000 keys of 8: 30.3 us, this 22.6; 16 streams' drafts 17.1, 16.4; without the early
-// launch 24.6 and 18.6: launched one after the other).  For 8 rows or fewer the last
+// (two queries of 64 heads over 20000 keys of 8, one call after the other: 30.3 us, this 22.9; 16 streams' drafts 17.1, 16.5;
+// without the early launch 24.6 and 18.6).  For 8 rows or fewer the last
 // CTA is as good or better (two rows: 9.9 us, a kernel of its own 15.1).
 template <int D>
 __global__ void __launch_bounds__(512) few_join_kernel(const __grid_constant__ PagedAttnArgs a) {
