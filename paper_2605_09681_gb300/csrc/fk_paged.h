@@ -189,30 +189,6 @@ cudaError_t paged_chunk_prepare(int D);
 // exponent e of x > 0, 2^e > x (below 2^-126: -126)
 __device__ __forceinline__ int above2(float x) { return (int)(__float_as_uint(x) >> 23) - 126; }
 
-// Where a row's reference r goes when a block that it sees asks for `to`.  p: log2 of the row's largest numerator in the block; 2^top > |O|
-// relative to r (a numerator of 1 in a block of reference r is 2^kRowTop there at most).  Not lower than leaves O room, which then grows, and
-// no higher above what the row holds or the block adds than leaves the bits of both.
-constexpr int kRowTop = 16, kRoom = 110, kAbove = 8;
-__device__ __forceinline__ int follow(int r, int to, float p, int top) {
-  const int most = max(r + top - kRowTop, to + (int)fmaxf(p, -1000.0f));
-  return max(min(to, most + kAbove), max(r + top - kRoom, r - 127));
-}
-
-// Parts of a row's keys, each with its maximum m, its l and its reference r, joined by a warp: weights 2^(m - M) of l, M = max m, and
-// 2^((m - M) + (r - R)) of O.  R: the largest r, unless no part holds nearly 2^R (then that of what they hold).  e0: part `lane`.
-template <class Part>
-__device__ __forceinline__ float join_ref(float M, float R, const float4& e0, int n, Part part) {
-  float most = (e0.x - M) + e0.z;
-  if (__any_sync(0xffffffffu, most >= R - 40.0f)) return R;
-  for (int i = (threadIdx.x & 31) + 32; i < n; i += 32) {
-    const float4 e = part(i);
-    most = fmaxf(most, (e.x - M) + e.z);
-  }
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
-  return floorf(most);
-}
-
 // A join's launch may come while the kernel before it in the stream still runs (that one allows it, once all its CTAs have
 // started): the join waits for its end, and its writes, before it reads anything.
 __device__ __forceinline__ void allow_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -30,8 +30,7 @@
 // two-pass path for masked tiles (prompts 244, window 33.8), a thread's query row from global memory into registers (64 channels and kOne
 // 2-3% faster, 128 channels 3-4% slower: the instruction cache again, which every wait's polling inline also overran: 705 us).
 // The pipeline, its barriers and the lazily raised running maximum are those of the chunk attention over packed views.
-#include "fk_paged.h"
-#include "fk_tc.h"
+#include "fk_paged_rows.h"
 
 namespace fk {
 namespace {
@@ -715,7 +714,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
             mx = fmaxf(mx, fmaxf(fmaxf(mxa[0], mxa[1]), fmaxf(mxa[2], mxa[3])) * factor_at(c));
           }
           const float m_new = fmaxf(m, mx);
-          float rs = 1.0f, less = held[threadIdx.x]; // what O has to be scaled by; |O| <= 2^9 l + less
+          float rs = 1.0f, less = held[threadIdx.x]; // what O has to be scaled by: rs 2^d; |O| <= 2^9 l + less
+          int d = 0;
           if (__any_sync(0xffffffffu, m_new > m + kRescaleThreshold)) {   // warp-uniform
             rs = fast_exp2(m - m_new);               // 0 when m = kNoMax
             l *= rs;
@@ -728,19 +728,23 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
             float most = none ? 0.0f : fmaxf(fmaf(512.0f, l, less), 1e-37f);   // |O|, at most
             int want = none ? to : r;
             if (want != to && mx > -INFINITY) want = follow(r, to, mx - m, above2(most));
-            const float f = pow2_any(r - want);
-            less = fmaf(-512.0f, l, most * f);
-            rs *= f;
+            d = r - want;
+            less = fmaf(-512.0f, l, most * pow2_any(max(d, -100)) * pow2_any(min(d + 100, 0)));
             r = want;
           }
-          const bool rescale = __any_sync(0xffffffffu, rs != 1.0f) && (it > 0 || c0 > 0);   // O holds every key before chunk c0 ...
+          const bool rescale = __any_sync(0xffffffffu, rs != 1.0f || d != 0) && (it > 0 || c0 > 0);   // O holds every key before chunk c0 ...
           // ... once pva_done says so.  (A wild tile's parts all go over pa_full: no warp hands one over before all four have
           // handed over the one before, or a fast warp's arrival would stand for a slow one's.)
           if (c0 > 0 && (rescale || wild)) {
             if (!tile_wait(&bar->pva_done[t], (n_pa - 1) & 1, bar, a.status)) { ok = false; break; }
             tc_fence_after();
           }
-          if (rescale) {
+          // (in turns where a factor by itself would be too small for fp32, and what O holds in the end is not)
+#pragma unroll 1
+          for (bool more = rescale, first = true; more; first = false) {
+            const int step = first && d < -20 ? 0 : max(d, -100);
+            rs *= pow2_any(step);
+            d -= step;
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
               FK_TMEM_LD32(tO + c * 32, ca);
@@ -749,6 +753,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
               for (int e = 0; e < 32; ++e) ca[e] = __float_as_uint(__uint_as_float(ca[e]) * rs);
               FK_TMEM_ST32(tO + c * 32, ca);
             }
+            rs = 1.0f;
+            more = __any_sync(0xffffffffu, d != 0);
+            if (more) tmem_wait_st();
           }
           held[threadIdx.x] = less;
           direct = !wild && __all_sync(0xffffffffu, r == ti.r);
@@ -804,7 +811,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     if (!kOne && n_splits == 1) {
       // normalise; a thread writes its row, a whole 32-byte sector at a time where rows are aligned to that (through shared
       // memory to coalesced rows, side by side: 228.7 us for the prompts; 16 bytes at a time 228.3; 32: 221.4)
-      const float inv = l > 0.0f || l != l ? pow2_any(r) / l : 0.0f;    // no visible key: 0
+      const Normal to(l, max(r, -60));
+      const float inv = to.by_l * to.size, low = pow2_any(min(r + 60, 0));
+      const bool tiny = __any_sync(0xffffffffu, r < -60);                // (inv by itself would lose bits)
       const int cr = (kOne ? 0 : t * kBM) + row;
       if (ok) {
         bf16* dst = out_row(min(cr, rows - 1));
@@ -813,6 +822,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           uint32_t o[32], v[16];
           FK_TMEM_LD32(tO + c * 32, o);
           FK_TMEM_WAIT_LD32(o);
+          if (tiny) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * low);
+          }
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[e] = has ? pack_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
           if (cr >= rows) continue;
@@ -830,12 +843,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       // both accumulators to shared memory, [t][row][D] with 16-byte run c of a row at c ^ (row & 7), and their (m, l, r)
       float* so = reinterpret_cast<float*>(smem) + (t * kBM + row) * D;
       float4* ml = reinterpret_cast<float4*>(smem + 2 * kBM * D * 4);
+      // a part goes out at the reference of what it holds (O may have been lifted), or the joins' factors could not hold it
+      const int lift = max(above2(fmaxf(fmaf(512.0f, l, held[threadIdx.x]), 1e-37f)) - 24, 0);
+      const float down = pow2_any(-lift);
+      r += lift;
       if (ok) {
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
           FK_TMEM_LD32(tO + c * 32, o);
           FK_TMEM_WAIT_LD32(o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * down);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             *reinterpret_cast<uint4*>(so + (((c * 8 + e) ^ (row & 7)) << 2)) =
@@ -865,8 +884,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           R = R2;
         }
         if (n_splits == 1) {
-          const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;
-          *reinterpret_cast<uint2*>(out_row(r) + 4 * c) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+          *reinterpret_cast<uint2*>(out_row(r) + 4 * c) = Normal(L, (int)R).bf16x4(x);
         } else {
           part[((int64_t)slot0 * kBM + r) * kRuns + c] = x;
           if (c == 0) mls[(int64_t)slot0 * kBM + r] = make_float4(M, L, R, 0.0f);
@@ -945,11 +963,10 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Paged
   }
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
-  const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;      // no visible key: 0
   const int tok = a.by_g.div(row);
   bf16* o = a.O + ((int64_t)a.seqs.q0[s] + tok) * a.ostride + (int64_t)(kvh * a.G + row - tok * a.G) * D;
   if (lane < kRuns)
-    *reinterpret_cast<uint2*>(o + 4 * lane) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    *reinterpret_cast<uint2*>(o + 4 * lane) = Normal(L, (int)R).bf16x4(acc);
 }
 
 }  // namespace

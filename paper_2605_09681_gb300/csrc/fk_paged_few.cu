@@ -27,8 +27,7 @@
 // conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.3 us).
 // Splits leave (m, l, r, O) in a workspace; the last one to arrive (8 rows) or a kernel of its own (16) joins them in the order of
 // the splits (no atomics on values: results do not change from run to run).
-#include "fk_paged.h"
-#include "fk_tc.h"
+#include "fk_paged_rows.h"
 
 namespace fk {
 namespace {
@@ -38,7 +37,9 @@ constexpr int kFewThreads = (kWarps + 1) * 32;
 constexpr int kStages = 4;
 constexpr float kLowest = -3.402823466e38f;           // m before any key: finite, so that 2^(-inf - m) is 0
 constexpr float kRaise = 4.0f;                        // log2 units by which a row may outgrow m
-constexpr int kApart = 1 << 20, kCloseRefs = 40, kRaised = 74;   // see few_kernel
+// A warp whose rows did not go together; how far the warps' references may lie apart, and O be lifted at the end; how far moves down may lift O in
+// all (log2: at most 2^(9 + kRaised) l), and one move up press it
+constexpr int kApart = 1 << 20, kCloseRefs = 40, kRaised = 74, kFall = 100;
 constexpr float kShiftP = 8.0f;                       // p is stored times 2^8: at most 2^12 in f16
 
 template <int D>
@@ -395,8 +396,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       edge |= move && !full;
       if (__any_sync(0xffffffffu, grows || move)) {
         const int to = ev + kRefRoom;
-        bool seen = false, go = raised + r - to <= kRaised;
-        float al[kN][2];
+        bool seen = false, go = raised + r - to <= kRaised && (to - r <= kFall || r == kNoRef);
 #pragma unroll
         for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -407,9 +407,14 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             const float mn = fmaxf(m[j][h], mx);
             seen |= mx > -INFINITY;
             go &= r == kNoRef || m[j][h] == kLowest || 8 * j + 2 * t + h >= rows || to <= r + kAbove || mx - mn >= kAskPast;
-            al[j][h] = fast_exp2(m[j][h] - mn);
+            const float al = fast_exp2(m[j][h] - mn);
             m[j][h] = mn;
-            l[j][h] *= al[j][h];
+            l[j][h] *= al;
+#pragma unroll
+            for (int c = 0; c < kRowTiles; ++c) {
+              o[j][c][h] *= al;
+              o[j][c][2 + h] *= al;
+            }
           }
         if (move && __any_sync(0xffffffffu, seen)) {     // the rows go together, or not at all
           apart |= !__all_sync(0xffffffffu, go);
@@ -417,20 +422,12 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           raised = r == kNoRef ? 0 : max(0, raised + r - to);
           r = to;
 #pragma unroll
-          for (int j = 0; j < kN; ++j) {
-            al[j][0] *= f;
-            al[j][1] *= f;
-          }
+          for (int j = 0; j < kN; ++j)
+#pragma unroll
+            for (int c = 0; c < kRowTiles; ++c)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) o[j][c][x] *= f;
         }
-#pragma unroll
-        for (int j = 0; j < kN; ++j)
-#pragma unroll
-          for (int c = 0; c < kRowTiles; ++c) {
-            o[j][c][0] *= al[j][0];
-            o[j][c][1] *= al[j][1];
-            o[j][c][2] *= al[j][0];
-            o[j][c][3] *= al[j][1];
-          }
       }
       // (a block of which no row sees a key may still be far from r: its numerators are 0)
       const int d = ev == kZeroExp ? 0 : min(max(ev - r, -kRefWindow), 0);
@@ -478,7 +475,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   // ---- the warps' (m, l, r) and O
   float* sO = reinterpret_cast<float*>(smem);           // [warp][row][D], 16-byte run c of row at c ^ (row & 7)
   __shared__ float sm[kWarps][kRows], sl[kWarps][kRows];
-  __shared__ int sr[kWarps];                            // reference (kApart: what the warp holds is of no use)
+  __shared__ int sr[kWarps], su[kWarps];                // reference (kApart: what the warp holds is of no use), raised
   if (warp < kWarps) {
 #pragma unroll
     for (int j = 0; j < kN; ++j)
@@ -499,7 +496,10 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       }
     // (A row that took a block's reference without seeing it, and then saw blocks of zeros, holds nothing of that size.)
     apart |= zeros && edge;
-    if (lane == 0) sr[warp] = apart ? kApart : r;
+    if (lane == 0) {
+      sr[warp] = apart || raised > kCloseRefs ? kApart : r + raised;
+      su[warp] = raised;
+    }
   }
   __syncthreads();
   // O of the CTA relative to (M, 2^R): weights 2^(m_w - M) 2^(r_w - R)
@@ -532,7 +532,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float f = fast_exp2(sm[w][row] - M), fo = f * pow2_any(sr[w] - R);
+      const float f = fast_exp2(sm[w][row] - M), fo = f * pow2_any(sr[w] - su[w] - R);
       const float4 x = *reinterpret_cast<const float4*>(sO + (w * kRows + row) * D + ((c ^ (row & 7)) << 2));
       L = fmaf(f, sl[w][row], L);
       acc.x = fmaf(fo, x.x, acc.x);
@@ -541,9 +541,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       acc.w = fmaf(fo, x.w, acc.w);
     }
     if (n_splits == 1) {
-      const float inv = L > 0.0f || L != L ? pow2_any(R) / L : 0.0f;   // no visible key: 0
-      *reinterpret_cast<uint2*>(out_row(row) + 4 * c) =
-          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+      *reinterpret_cast<uint2*>(out_row(row) + 4 * c) = Normal(L, R).bf16x4(acc);
     } else {
       part[((int64_t)cta * kPagedFewRows + row) * kRuns + c] = acc;
       if (c == 0) mls[cta * kPagedFewRows + row] = make_float4(M, L, (float)R, 0.0f);
@@ -609,7 +607,10 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     }
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
-    if (lane == 0) sl[0][row] = L > 0.0f || L != L ? pow2_any((int)RR) / L : 0.0f;
+    if (lane == 0) {
+      sl[0][row] = L;
+      sm[0][row] = RR;
+    }
   }
   __syncthreads();
   float4* sums = reinterpret_cast<float4*>(smem + kMaxFewSplits * kPagedFewRows * 4);     // [set][place]
@@ -644,9 +645,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         }
     }
     if (mine && set == 0) {
-      const float inv = sl[0][row];
-      *reinterpret_cast<uint2*>(out_row(row) + 4 * c) =
-          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+      *reinterpret_cast<uint2*>(out_row(row) + 4 * c) = Normal(sl[0][row], (int)sm[0][row]).bf16x4(acc);
     }
   }
 }
@@ -707,11 +706,10 @@ __global__ void __launch_bounds__(512) few_join_kernel(const __grid_constant__ P
   }
 #pragma unroll
   for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
-  const float inv = L > 0.0f || L != L ? pow2_any((int)R) / L : 0.0f;      // no visible key: 0
   const int tok = a.by_g.div(row);
   bf16* o = a.O + ((int64_t)a.seqs.q0[s] + tok) * a.ostride + (int64_t)(kvh * a.G + row - tok * a.G) * D;
   if (lane < kRuns)
-    *reinterpret_cast<uint2*>(o + 4 * lane) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    *reinterpret_cast<uint2*>(o + 4 * lane) = Normal(L, (int)R).bf16x4(acc);
 }
 
 using FewKern = void (*)(const CUtensorMap, const CUtensorMap, const PagedAttnArgs);

@@ -253,3 +253,21 @@ def test_every_query_by_what_it_sees(Hq, Hkv, D, page, lens, nq, spread):
                 assert (np.abs(got[qat: qat + m] - want) <= bound).all(), (mask, n)
                 at, qat = at + n, qat + m
         assert cache.sync_status() == 0
+
+
+@pytest.mark.parametrize("heads,D,page,n,nq", SHAPES)
+@pytest.mark.parametrize("down,up,bits", [(30, 60, 0), (60, 40, 0), (60, 90, 0), (56, 90, 22), (90, 60, 10), (40, 85, 40)])
+def test_what_has_been_lifted_outlasts_a_large_block(heads, D, page, n, nq, down, up, bits):
+    """Ordinary pages, then tiny ones of most of the weight, for which O is lifted, then large ones that hold one channel only, at a weight of
+    2^-bits: in the other channels the ordinary pages' sums remain, in one CTA's keys and across key splits."""
+    r = np.random.default_rng(87)
+    u = np.sign(r.standard_normal(D))
+    Q = u * (1 + 0.1 * r.random((nq, heads[0], D)))
+    Q *= np.sqrt(D) / (Q * u).sum(-1, keepdims=True) * np.sqrt(D)
+    for block in (page, n // 6 + 1, n // 3 + 1):
+        kind = np.arange(n) // block % 3
+        K = 0.02 * r.standard_normal((n, heads[1], D)) - (np.array([5.0, 0.0, bits])[kind] * np.log(2) / np.sqrt(D))[:, None, None] * u
+        V = r.standard_normal((n, heads[1], D)) * np.array([1.0, 2.0 ** -down, 2.0 ** up])[kind][:, None, None]
+        V[kind == 2, :, 1:] = 0
+        check(heads, D, page, V, nq, [dict(), dict(causal=False), dict(window=n // 2)],
+              K=P.to_bf16(K.astype(np.float32)), Q=P.to_bf16(Q.astype(np.float32)))
