@@ -18,12 +18,12 @@
 // tile whose own pages differ by more than the window allows, or has one of zeros ("wild"), is handed over 32 keys at a time,
 // which ask for their own, O rescaled in between.
 // Key splits leave (m, l, r, O) in a workspace; join_kernel joins them.
-// What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 626-637 us, 1480-1505 TFLOP/s.  A key tile takes the two query tiles
+// What bounds it: 4680 queries over 32760 keys, 12 heads of 128, take 626-641 us, 1470-1505 TFLOP/s.  A key tile takes the two query tiles
 // 2950 cycles, 2048 of them products at their nominal rate: a query tile's softmax (1600) and the wait for its next S take turns, since
 // P lies over S and tensor memory is full (S, O of two tiles), and Q K^T wants 128 bytes of shared memory a cycle, all there is, beside
 // the conversion's.  A CTA starts and ends in ~15000 cycles (queries copied 3300, their codes 3500, first S 1450, first tile
-// 2000 more than the others, rows out 3000), which is what causal prompts (6 of 63 to 4001 tokens, 32 heads of 128: 220-224 us)
-// and windows (2048 queries, window 1024: 28.8 us) pay for.  kOne (8 sequences of 16000 keys, 12 kv heads, 30 rows: 99.5 us, the
+// 2000 more than the others, rows out 3000), which is what causal prompts (6 of 63 to 4001 tokens, 32 heads of 128: 220-228 us)
+// and windows (2048 queries, window 1024: 29.0 us) pay for.  kOne (8 sequences of 16000 keys, 12 kv heads, 30 rows: 100 us, the
 // codes' bytes 58) is bound by its products' operands.
 // Measured and left: an MMA warp for each query tile (their products then interleave: 821 us), looking for the next hand-over
 // between products (712), four converting warps at 88 registers (677; kOne 105.8), keys handed over as 112 + 16 (701), the

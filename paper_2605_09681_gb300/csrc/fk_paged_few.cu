@@ -24,7 +24,7 @@
 // What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 51 us, 5.2 TB/s, where
 // reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 83 us, 5.9 TB/s (76.4).  With
 // little to read the launch and the join do: one token of 12 heads over 1561 keys 6.5-6.9 us.  At 16 rows its products and
-// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.3 us).
+// conversions bound it (16 sequences of up to 96 rows of 64 channels, 200 to 4000 keys: 14.5 us).
 // Splits leave (m, l, r, O) in a workspace; the last one to arrive (8 rows) or a kernel of its own (16) joins them in the order of
 // the splits (no atomics on values: results do not change from run to run).
 #include "fk_paged_rows.h"
