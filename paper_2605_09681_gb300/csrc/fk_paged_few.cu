@@ -20,7 +20,8 @@
 //             over lanes, and O is seldom rescaled.  r is one for a warp's rows: it goes with a block outside its window if all rows hold
 //             nothing yet, or see large p there, or it is near, and if O has room.  Where that does not hold (blocks of values that
 //             differ by 2^40 and more, or by less with rows that give the larger next to nothing) the CTA does its rows again by
-//             exact_rows.  (References of the rows' own, held in shared memory, cost every call 4-7%.)
+//             exact_rows, 30 times as slowly (131072 keys in pages 10^20 apart: 1.5 ms).  (References of the rows' own, held in
+//             shared memory, cost every call 4-7%.)
 // What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 51 us, 5.2 TB/s, where
 // reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 83 us, 5.9 TB/s (76.4).  With
 // little to read the launch and the join do: one token of 12 heads over 1561 keys 6.5-6.9 us.  At 16 rows its products and
