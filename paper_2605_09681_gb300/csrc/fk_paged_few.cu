@@ -19,8 +19,8 @@
 //             is scaled.  m is raised only when a row outgrows it by 2^4: a vote finds that no row does, without a maximum
 //             over lanes, and O is seldom rescaled.  r is one for a warp's rows: it goes with a block outside its window if all rows hold
 //             nothing yet, or see large p there, or it is near, and if O has room.  Where that does not hold (blocks of values that
-//             differ by 2^40 and more, or by less with rows that give the larger next to nothing) the CTA does its rows again by
-//             exact_rows, 30 times as slowly (131072 keys in pages 10^20 apart: 1.5 ms).  (References of the rows' own, held in
+//             differ by 2^74 and more, or by less with rows that give the larger next to nothing) the CTA does its rows again by
+//             exact_rows, 30 times as slowly (131072 keys in pages 10^50 apart: 1.6 ms).  (References of the rows' own, held in
 //             shared memory, cost every call 4-7%.)
 // What bounds it: the cache's bytes.  One token of 32 heads over 131072 keys of 8 kv heads (268 MB of codes) 51 us, 5.2 TB/s, where
 // reading those bytes and nothing else takes 42.8; 64 streams of 500 to 7000 keys (489 MB) 83 us, 5.9 TB/s (76.4).  With
@@ -38,9 +38,9 @@ constexpr int kFewThreads = (kWarps + 1) * 32;
 constexpr int kStages = 4;
 constexpr float kLowest = -3.402823466e38f;           // m before any key: finite, so that 2^(-inf - m) is 0
 constexpr float kRaise = 4.0f;                        // log2 units by which a row may outgrow m
-// A warp whose rows did not go together; how far the warps' references may lie apart, and O be lifted at the end; how far moves down may lift O in
-// all (log2: at most 2^(9 + kRaised) l), and one move up press it
-constexpr int kApart = 1 << 20, kCloseRefs = 40, kRaised = 74, kFall = 100;
+// A warp whose rows did not go together; how far the warps' references may lie apart; how far moves down may lift O in all (log2: at most
+// 2^(9 + kRaised) l), and one move up press it
+constexpr int kApart = 1 << 20, kCloseRefs = 100, kRaised = 74, kFall = 100;
 constexpr float kShiftP = 8.0f;                       // p is stored times 2^8: at most 2^12 in f16
 
 template <int D>
@@ -476,8 +476,18 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   // ---- the warps' (m, l, r) and O
   float* sO = reinterpret_cast<float*>(smem);           // [warp][row][D], 16-byte run c of row at c ^ (row & 7)
   __shared__ float sm[kWarps][kRows], sl[kWarps][kRows];
-  __shared__ int sr[kWarps], su[kWarps];                // reference (kApart: what the warp holds is of no use), raised
+  __shared__ int sr[kWarps];                            // reference (kApart: what the warp holds is of no use)
   if (warp < kWarps) {
+    if (raised > 0) {                                   // back to the reference of what O holds
+      const float f = pow2_any(-raised);
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (int c = 0; c < kRowTiles; ++c)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][c][x] *= f;
+      r += raised;
+    }
 #pragma unroll
     for (int j = 0; j < kN; ++j)
 #pragma unroll
@@ -498,8 +508,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     // (A row that took a block's reference without seeing it, and then saw blocks of zeros, holds nothing of that size.)
     apart |= zeros && edge;
     if (lane == 0) {
-      sr[warp] = apart || raised > kCloseRefs ? kApart : r + raised;
-      su[warp] = raised;
+      sr[warp] = apart ? kApart : r;
     }
   }
   __syncthreads();
@@ -533,7 +542,7 @@ few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float f = fast_exp2(sm[w][row] - M), fo = f * pow2_any(sr[w] - su[w] - R);
+      const float f = fast_exp2(sm[w][row] - M), fo = f * pow2_any(sr[w] - R);
       const float4 x = *reinterpret_cast<const float4*>(sO + (w * kRows + row) * D + ((c ^ (row & 7)) << 2));
       L = fmaf(f, sl[w][row], L);
       acc.x = fmaf(fo, x.x, acc.x);
