@@ -350,6 +350,76 @@ FK_API fk_status fk_quantize_e4m3(const void* X, int64_t rows, int dim, int row_
                                   void* q8, int8_t* exps, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Rotary positions (no counterpart in the paper, whose queries and keys come rotated): queries and keys turned by
+ * their positions, for every cache of this library, and tables of the angles for fk_paged_append.
+ *
+ * Pair i of axis a turns by positions[token][a] * f_i: y = m (x_j cos - x_k sin), m (x_k cos + x_j sin).  The frequencies
+ * are taken as fractions of a turn in 64-bit fixed point and a position times one is exact modulo whole turns: an angle
+ * is as good at position 2^31 - 1 as at 1 (2^-24 of a turn or better).  Rotations are in fp32, rounded once.
+ * --------------------------------------------------------------------------------------------- */
+enum {
+  FK_ROPE_HALF = 0,        /* channel pairs (i, i + dim/2)  */
+  FK_ROPE_INTERLEAVED = 1  /* channel pairs (2i, 2i + 1)    */
+};
+
+/* How frequencies are scaled for contexts longer than a model was trained on.  f_i = base^(-2 i / d), d the channels
+ * of the pair's axis. */
+enum {
+  FK_ROPE_SCALE_NONE = 0,
+  FK_ROPE_SCALE_LINEAR = 1, /* f_i / factor (position interpolation, arXiv 2306.15595)                    */
+  FK_ROPE_SCALE_BASE = 2,   /* base * factor^(d / (d - 2)): the slowest pair as LINEAR, the fastest as it is */
+  FK_ROPE_SCALE_RAMP = 3    /* by the turns t of a pair in original_tokens positions: f_i for t >= fast_turns, f_i / factor for
+                               t <= slow_turns, linear in t between; m = 0.1 ln(factor) + 1 (arXiv 2309.00071) */
+};
+
+/* Types of rotated tensors. */
+enum { FK_TYPE_BF16 = 0, FK_TYPE_F16 = 1, FK_TYPE_F32 = 2 };
+
+typedef struct fk_rotary_config {
+  int32_t head_dim;        /* a multiple of 8, 16..256                                            */
+  int32_t dim;             /* rotated channels, the first of a head: a multiple of 16, at most head_dim */
+  int32_t style;           /* FK_ROPE_*                                                           */
+  int32_t n_axes;          /* position axes, 1..4 (a video's: frame, row, column)                 */
+  int32_t pairs[4];        /* channel pairs of each axis, in order, at least 1 each, dim / 2 together */
+  int32_t scaling;         /* FK_ROPE_SCALE_* (BASE: axes of at least 2 pairs)                    */
+  int32_t original_tokens; /* RAMP: at least 1                                                    */
+  double base;             /* above 1                                                             */
+  double factor;           /* LINEAR, BASE, RAMP: at least 1                                      */
+  double slow_turns;       /* RAMP: 0 <= slow_turns < fast_turns                                  */
+  double fast_turns;
+  double magnitude;        /* m; 0: 1, and RAMP's own                                             */
+  const double* frequencies; /* host [dim / 2], radians a position, each of magnitude below pi; or NULL:
+                              from base and scaling                                               */
+} fk_rotary_config;
+
+/* A rotation: plain data (copy it, keep it), made by fk_rotary_make. */
+typedef struct fk_rotary {
+  uint64_t turns[128];     /* fraction of a turn a position, in 2^-64                             */
+  float magnitude;
+  int32_t head_dim, dim, style, n_axes;
+  int32_t first[4];        /* first pair of each axis (dim / 2 behind the last)                   */
+} fk_rotary;
+
+/* Host only: FK_OK, FK_ERR_CONFIG or FK_ERR_ARG. */
+FK_API fk_status fk_rotary_make(const fk_rotary_config* cfg, fk_rotary* out);
+
+/* Rotate X [tokens][x_heads][head_dim] into Y and, in the same launch, X2 into Y2 (X2 NULL, x2_heads 0: none), by
+ * positions (device int32 [tokens][n_axes], any values); inverse = 1: by the opposite angles (the gradient of the rotation).  Channels
+ * behind `dim` are copied.  Y may be X (then with the same stride); otherwise outputs overlap nothing.  Tensors of
+ * `type`, 16-byte aligned, tokens `stride` elements apart (a multiple of 16 bytes, at least heads * head_dim; heads and
+ * channels contiguous).  heads 1..1024 each, tokens below 2^31.
+ * FK_ERR_ARG for null, unaligned or host pointers, short strides; FK_ERR_CONFIG for sizes out of range or a rotation
+ * that fk_rotary_make did not make.  Asynchronous on `stream`; allocates nothing; uses the current device. */
+FK_API fk_status fk_rotate(const fk_rotary* r, int64_t tokens, const int32_t* positions, int inverse, int type,
+                           const void* X, int64_t x_stride, int x_heads, void* Y, int64_t y_stride,
+                           const void* X2, int64_t x2_stride, int x2_heads, void* Y2, int64_t y2_stride, void* stream);
+
+/* m cos and m sin of the tokens' angles, cos, sin: device fp32 [tokens][dim / 2], 16-byte aligned: tables of
+ * fk_rope (then `positions` there is the row of a token).  Otherwise as fk_rotate. */
+FK_API fk_status fk_rotary_tables(const fk_rotary* r, int64_t tokens, const int32_t* positions, float* cos, float* sin,
+                                  void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Paged 8-bit cache: keys and values of many sequences in pages, held as OCP FP8 E4M3 codes with one
  * power-of-two scale for each page and head, and the attention that reads it (no counterpart in the
  * paper, whose cache holds one video).  For the parts of a generator that are language models: prompt
@@ -374,11 +444,6 @@ FK_API fk_status fk_quantize_e4m3(const void* X, int64_t rows, int dim, int row_
  * caller, as is the work of one handle's attentions among themselves (they share a workspace).  The current
  * device is left as it was.
  * --------------------------------------------------------------------------------------------- */
-enum {
-  FK_ROPE_HALF = 0,        /* channel pairs (i, i + dim/2)  */
-  FK_ROPE_INTERLEAVED = 1  /* channel pairs (2i, 2i + 1)    */
-};
-
 typedef struct fk_paged_config {
   int32_t n_layers;        /* 1..256; pages are taken for all layers at once                       */
   int32_t n_q_heads;       /* a multiple of n_kv_heads, at most 1024: head h reads kv head
@@ -473,6 +538,90 @@ FK_API int64_t fk_paged_launch_count(const fk_paged* h);
  * FK_ERR_TIMEOUT (a bounded wait expired), FK_ERR_RANGE (an appended key or value that was not finite, a position outside the
  * tables; after a timeout it is the next call's), FK_OK. */
 FK_API fk_status fk_paged_sync_status(fk_paged* h, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Linear attention with a decay for each head (no counterpart in the paper): each sequence keeps, for each layer and kv
+ * head, one state S [head_dim][head_dim] in fp32 instead of its keys and values,
+ *   S_t = exp(g_t) S_(t-1) + k_t v_t^T,   o_t = scale q_t^T S_t,
+ * whatever its length: for layers of a generator (language model or video) that would otherwise hold a cache.
+ *
+ * Use: fk_linear_step names the sequences of a step and how many tokens each has; then, layer by layer,
+ * fk_linear_attend on [tokens][heads][head_dim] bf16 tensors that hold the sequences' tokens one after the other in the
+ * step's order.  The states are memory of the handle that the caller may read and write (fk_linear_states); all
+ * start as zeros.  A few tokens (drafts, single tokens) go through the recurrence in fp32; longer runs are computed in chunks on the
+ * tensor cores, where decayed keys multiply values in three bf16 parts (2^-24 of them) for the states, and for
+ * o the decayed products q k and the states before a chunk are rounded to bf16.
+ *
+ * All calls: device tensors only (FK_ERR_ARG for host memory or memory of another device), 16-byte aligned, tokens
+ * `stride` elements apart (a multiple of 8, at least heads * head_dim; heads and channels contiguous).  Asynchronous on
+ * `stream`; nothing is allocated or waited for after fk_linear_create, and calls can be captured in a graph, whose
+ * replays go on from the states that they find.  Calls that use different streams are ordered by the caller (calls of
+ * one handle share its states and a workspace).  The current device is left as it was.
+ * --------------------------------------------------------------------------------------------- */
+typedef struct fk_linear_config {
+  int32_t n_layers;        /* 1..256                                                              */
+  int32_t n_q_heads;       /* a multiple of n_kv_heads, at most 1024: head h reads the state of kv head
+                              h / (n_q_heads / n_kv_heads)                                        */
+  int32_t n_kv_heads;      /* 1..128                                                              */
+  int32_t head_dim;        /* 64 or 128                                                           */
+  int32_t max_seqs;        /* sequences 0..max_seqs-1, at most 65536                              */
+  int32_t device;          /* CUDA device ordinal                                                 */
+} fk_linear_config;
+
+typedef struct fk_linear fk_linear;
+
+/* What becomes of the states that a step's sequences hold. */
+enum {
+  FK_LINEAR_ADVANCE = 0,   /* they take the step's tokens in                                      */
+  FK_LINEAR_STAY = 1       /* they stay: the step's tokens are tried only (drafts to be verified, a chunk that
+                              is denoised again)                                                  */
+};
+
+/* Host-only validation (no CUDA call): FK_OK, FK_ERR_CONFIG or FK_ERR_ARG. */
+FK_API fk_status fk_linear_validate_config(const fk_linear_config* cfg);
+
+/* Create the states on cfg->device, all zero: n_layers * max_seqs * n_kv_heads * head_dim^2 * 4 bytes, and a workspace for
+ * splits of long runs, one for all layers.  Errors as fk_create. */
+FK_API fk_status fk_linear_create(const fk_linear_config* cfg, fk_linear** out);
+
+/* Release the handle and its device memory (synchronizes the device first).  NULL is a no-op. */
+FK_API void fk_linear_destroy(fk_linear* h);
+
+/* Begin a step of n_seqs different sequences (host arrays): sequence seqs[i] has n_new[i] >= 0 tokens.  Host only.  The
+ * step stands until the next one.  Tokens times n_q_heads are below 2^31 (FK_ERR_ARG; a refused step leaves the one before). */
+FK_API fk_status fk_linear_step(fk_linear* h, int n_seqs, const int32_t* seqs, const int32_t* n_new);
+
+/* One layer's attention over the step's tokens: Q, O [tokens][n_q_heads][head_dim], K, V [tokens][n_kv_heads][head_dim].
+ * decay: device fp32, g as it stands in exp(g): [tokens][n_kv_heads] with decay_stride elements (at least n_kv_heads) from token to
+ * token, or, decay_stride = 0, [n_kv_heads] for all tokens.  g <= 0 decays (-inf: the state starts anew); g > 0 grows.
+ * scale = 0: 1 / sqrt(head_dim).
+ * mode FK_LINEAR_ADVANCE: the states held become those after the step (calling again takes the tokens in again).
+ * FK_LINEAR_STAY: they stay, and with state_out (device fp32 [n_seqs][n_kv_heads][head_dim][head_dim], 16-byte aligned, not
+ * memory of the handle) those after the step go there, in the step's order; NULL with FK_LINEAR_ADVANCE.
+ * Infinities and NaN reach the tokens from their own on, and no other sequence.  O overlaps no input (FK_ERR_ARG).
+ * FK_ERR_STATE without a step. */
+FK_API fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_stride, const void* K,
+                                  int64_t k_stride, const void* V, int64_t v_stride, const float* decay,
+                                  int64_t decay_stride, void* O, int64_t o_stride, float scale, int mode,
+                                  float* state_out, void* stream);
+
+/* The states of a layer: *states = device memory [max_seqs][n_kv_heads][head_dim (of k)][head_dim (of v)], which the
+ * caller may read and write in the order of the stream (checkpoints, forks, accepted drafts). */
+FK_API fk_status fk_linear_states(const fk_linear* h, int layer, float** states);
+
+/* Zero the states of sequence `seq`, all layers, on `stream` (a new sequence takes its number). */
+FK_API fk_status fk_linear_drop(fk_linear* h, int seq, void* stream);
+
+/* Sequence dst's states become copies of sequence src's, all layers, on `stream` (a fork). */
+FK_API fk_status fk_linear_fork(fk_linear* h, int dst, int src, void* stream);
+
+/* Device memory that the handle allocated, kernels launched so far. */
+FK_API size_t fk_linear_reserved_bytes(const fk_linear* h);
+FK_API int64_t fk_linear_launch_count(const fk_linear* h);
+
+/* Synchronize `stream` and report (then clear, in the stream's order) device-side conditions of the work it waited for:
+ * FK_ERR_TIMEOUT (a bounded wait expired: outputs and states are undefined) or FK_OK. */
+FK_API fk_status fk_linear_sync_status(fk_linear* h, void* stream);
 
 /* Static text for a status code. */
 FK_API const char* fk_status_str(fk_status s);

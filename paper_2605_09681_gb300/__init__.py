@@ -1,6 +1,7 @@
 """Forcing-KV hot path on GB300: hybrid KV-cache compression (static structural pruning,
-segment-similarity pruning) and chunk attention over the compressed cache; and a paged 8-bit cache of
-many sequences (PagedKVCache) with the attention that reads it.
+segment-similarity pruning) and chunk attention over the compressed cache; a paged 8-bit cache of
+many sequences (PagedKVCache) with the attention that reads it; rotary positions (Rotary); and linear
+attention with decays over states of a fixed size (LinearStateCache).
 
 Every step runs in the CUDA kernels of libfk.so behind the C ABI of include/fk.h; this
 module only marshals arguments (torch tensors for device memory and streams).
@@ -14,7 +15,7 @@ import numpy as np
 from . import _lib as L
 from ._lib import FkError, KERNEL_KINDS, STATUS_NAMES
 
-__all__ = ["ForcingKVCache", "PagedKVCache", "FkError", "KERNEL_KINDS", "STATUS_NAMES", "load_library",
+__all__ = ["ForcingKVCache", "PagedKVCache", "Rotary", "LinearStateCache", "FkError", "KERNEL_KINDS", "STATUS_NAMES", "load_library",
            "head_profile", "classify_heads", "quantize_e4m3", "stream_read"]
 
 
@@ -498,3 +499,256 @@ class PagedKVCache:
     def sync_status(self, stream=None) -> int:
         """Synchronize and return the device status (FK_OK, FK_ERR_RANGE, FK_ERR_TIMEOUT)."""
         return int(self._lib.fk_paged_sync_status(self._h, self._on(stream)))
+
+
+class Rotary:
+    """Rotary positions (fk_rotary_*): queries and keys turned by their positions, for any of the caches.
+
+        rotary = Rotary(head_dim=128, layout="interleaved", axes=(22, 21, 21))   # a video's frame, row, column
+        Q, K = rotary.rotate(positions, Q, K)                # positions: int32 [tokens, axes]
+        cos, sin = rotary.tables(positions)                  # for PagedKVCache.append
+
+    dim: rotated channels, the first of a head (default: all); layout "half" (pairs i, i + dim / 2) or "interleaved" (2i,
+    2i + 1); axes: channel pairs of each position axis (default: one axis).  Pair i of an axis of d channels turns by
+    base^(-2i / d) radians a position, scaled for long contexts by `scaling`: "linear" (positions / factor), "base" (base *
+    factor^(d / (d - 2))) or "ramp" (pairs of at least fast_turns turns in original_tokens positions as they are, of at
+    most slow_turns by 1 / factor, in proportion between; cos and sin times `magnitude`, default 0.1 ln(factor) + 1); or
+    give the `frequencies` themselves (radians a position, one a pair)."""
+
+    def __init__(self, *, head_dim, dim=None, layout="half", axes=None, base=10000.0, scaling="none", factor=1.0,
+                 original_tokens=0, slow_turns=1.0, fast_turns=32.0, magnitude=None, frequencies=None):
+        self._lib, self._r = L.load(), L.FkRotary()
+        dim = head_dim if dim is None else dim
+        axes = [int(x) for x in (axes if axes else [dim // 2])]
+        if len(axes) > 4:
+            raise ValueError("axes: at most 4")
+        freq = None
+        if frequencies is not None:
+            freq = [float(x) for x in frequencies]
+            if len(freq) != dim // 2:
+                raise ValueError("frequencies: expected %d, one for each pair" % (dim // 2))
+            freq = (ctypes.c_double * len(freq))(*freq)
+        if magnitude is not None and not magnitude > 0:                    # (0 asks for the default)
+            raise ValueError("magnitude must be positive")
+        cfg = L.FkRotaryConfig(head_dim, dim, L.FK_ROPE[layout], len(axes), (ctypes.c_int32 * 4)(*axes),
+                               L.FK_ROPE_SCALE[scaling or "none"], original_tokens, base, factor, slow_turns, fast_turns,
+                               0.0 if magnitude is None else magnitude, freq)
+        _check(self._lib.fk_rotary_make(ctypes.byref(cfg), ctypes.byref(self._r)), "fk_rotary_make")
+        self.head_dim, self.dim, self.n_axes = head_dim, dim, len(axes)
+        self._ref = ctypes.byref(self._r)
+        import torch
+        self._types = {torch.bfloat16: L.FK_TYPE_BF16, torch.float16: L.FK_TYPE_F16, torch.float32: L.FK_TYPE_F32}
+        self._i32 = torch.int32
+
+    def _at(self, positions, tokens):
+        n = self.n_axes
+        if positions.dtype is not self._i32 or not positions.is_cuda or not positions.is_contiguous() or \
+                not (positions.shape == (tokens, n) or (n == 1 and positions.shape == (tokens,))):
+            raise ValueError("positions: expected a contiguous int32 CUDA tensor [%d, %d]" % (tokens, n))
+        return positions.data_ptr()
+
+    def _rows(self, x, dtype, tokens, name):
+        """(address, elements from token to token, heads) of a [tokens, heads, head_dim] tensor."""
+        D = self.head_dim
+        if x.dtype is not dtype or not x.is_cuda or x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != D:
+            raise ValueError("%s: expected a CUDA tensor [%d, heads, %d] of %s, not %s %s"
+                             % (name, tokens, D, dtype, x.dtype, list(x.shape)))
+        row, head, channel = x.stride()
+        heads = x.shape[1]
+        if tokens and (channel != 1 or (heads > 1 and head != D)):
+            raise ValueError("%s: the heads of a token must lie contiguously" % name)
+        return x.data_ptr(), row if tokens > 1 else heads * D, heads
+
+    def _call(self, device, stream, call):
+        """call(raw stream) with the tensors' device as the current one."""
+        import torch
+        if torch.cuda.current_device() == device.index:
+            return call(_stream(stream))
+        with torch.cuda.device(device):
+            return call(_stream(stream))
+
+    def rotate(self, positions, Q, K=None, inverse=False, Q_out=None, K_out=None, stream=None):
+        """Q (and K, in the same launch) [tokens, heads, head_dim] in bf16, fp16 or fp32, which may be slices of wider rows,
+        turned by `positions` (int32 [tokens, axes], or [tokens]); inverse: the other way (the rotation's gradient).
+        Returns the rotated Q, or Q and K, in new tensors or in Q_out, K_out (which may be Q, K)."""
+        dtype = Q.dtype
+        if dtype not in self._types:
+            raise ValueError("Q: expected bf16, fp16 or fp32, not %s" % dtype)
+        if K is None and K_out is not None:
+            raise ValueError("K_out needs K")
+        tokens = Q.shape[0]
+        p = self._at(positions, tokens)
+        q, qs, hq = self._rows(Q, dtype, tokens, "Q")
+        k = o2 = None
+        ks = os2 = hk = 0
+        if K is not None:
+            k, ks, hk = self._rows(K, dtype, tokens, "K")
+
+        def call(s):
+            nonlocal Q_out, K_out, o2, os2
+            if Q_out is None:
+                Q_out = _made(Q.shape, dtype, Q.device, stream, s)
+            o1, os1, _ = self._rows(Q_out, dtype, tokens, "Q_out")
+            if Q_out.shape != Q.shape or (K_out is not None and K_out.shape != K.shape):
+                raise ValueError("Q_out, K_out: expected the shapes of Q and K")
+            if K is not None:
+                if K_out is None:
+                    K_out = _made(K.shape, dtype, K.device, stream, s)
+                o2, os2, _ = self._rows(K_out, dtype, tokens, "K_out")
+            _check(self._lib.fk_rotate(self._ref, tokens, p, 1 if inverse else 0, self._types[dtype], q, qs, hq, o1, os1,
+                                       k, ks, hk, o2, os2, s), "fk_rotate")
+
+        self._call(Q.device, stream, call)
+        return Q_out if K is None else (Q_out, K_out)
+
+    def tables(self, positions, cos=None, sin=None, stream=None):
+        """cos and sin of the angles at `positions`, fp32 [tokens, dim / 2] (rows of PagedKVCache.append's tables)."""
+        import torch
+        tokens = positions.shape[0]
+        p = self._at(positions, tokens)
+        shape = (tokens, self.dim // 2)
+        for x in (cos, sin):
+            if x is not None and (x.dtype is not torch.float32 or x.shape != shape or not x.is_cuda or not x.is_contiguous()):
+                raise ValueError("cos, sin: expected contiguous fp32 CUDA tensors [%d, %d]" % shape)
+
+        def call(s):
+            nonlocal cos, sin
+            cos = _made(shape, torch.float32, positions.device, stream, s) if cos is None else cos
+            sin = _made(shape, torch.float32, positions.device, stream, s) if sin is None else sin
+            _check(self._lib.fk_rotary_tables(self._ref, tokens, p, cos.data_ptr(), sin.data_ptr(), s), "fk_rotary_tables")
+
+        self._call(positions.device, stream, call)
+        return cos, sin
+
+
+def _made(shape, dtype, device, stream, raw):
+    """An output tensor, of the memory of the stream that is to write it (`raw`; `stream` None: the current one): the current
+    stream may still have work queued on memory that it has given back."""
+    import torch
+    if stream is None or raw == torch.cuda.current_stream(device).cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    own = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    with torch.cuda.stream(own):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class LinearStateCache:
+    """Linear attention with a decay for each head (fk_linear_*): each sequence keeps one fp32 state [head_dim, head_dim] a
+    layer and kv head, S_t = exp(g_t) S_(t-1) + k_t v_t^T, o_t = scale q_t^T S_t, however long it gets.
+
+        cache.step(seqs, n_new)                              # which sequences have how many tokens
+        for layer in range(n_layers):
+            O = cache.attend(layer, Q, K, V, decay)          # decay: g, fp32 [tokens, n_kv_heads] or [n_kv_heads]
+
+    Tensors are bf16 CUDA tensors [tokens, heads, head_dim], the step's sequences one after the other in its order;
+    they may be slices of wider rows (a fused projection's output).  Calls are asynchronous on `stream` (default:
+    torch's current stream of the cache's device), and tensors that they make are that stream's.  A graph that captured a
+    step's calls goes on from the states that it finds at each replay."""
+
+    def __init__(self, *, n_layers, n_q_heads, n_kv_heads, head_dim, max_seqs, device=0):
+        self._lib = L.load()
+        self._h = ctypes.c_void_p()
+        self.cfg = L.FkLinearConfig(n_layers, n_q_heads, n_kv_heads, head_dim, max_seqs, device)
+        self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
+        self.max_seqs, self.device = max_seqs, device
+        import torch
+        self._bf16, self._f32 = torch.bfloat16, torch.float32
+        self._dev = torch.device("cuda", device)
+        self._tokens = self._seqs = 0
+        _check(self._lib.fk_linear_create(ctypes.byref(self.cfg), ctypes.byref(self._h)), "fk_linear_create")
+
+    # ---- lifetime
+    def close(self):
+        if getattr(self, "_h", None) and self._h.value:
+            self._lib.fk_linear_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    _on, _rows = PagedKVCache._on, PagedKVCache._rows
+
+    # ---- steps
+    def step(self, seqs, n_new):
+        """Begin a step: sequence seqs[i] has n_new[i] tokens."""
+        s = _ints(seqs)
+        n = _ints(n_new, len(s))
+        _check(self._lib.fk_linear_step(self._h, len(s), s, n), "fk_linear_step")
+        self._tokens, self._seqs = sum(n), len(s)
+
+    def attend(self, layer, Q, K, V, decay, O=None, scale=None, advance=True, state_out=None, stream=None):
+        """Linear attention of the step's tokens in a layer; the states held take them in.  advance=False, or state_out given
+        (fp32 [sequences of the step, n_kv_heads, head_dim, head_dim], gets the states after the step): the states
+        held stay.  decay: g <= 0 for each token and kv head (fp32 [tokens, n_kv_heads]) or each kv head.  scale:
+        default 1 / sqrt(head_dim)."""
+        if scale is not None and not ctypes.c_float(scale).value > 0:      # (0 asks for the default)
+            raise ValueError("scale must be positive in fp32")
+        T, H, D = self._tokens, self.n_kv_heads, self.head_dim
+        q, qs = self._rows(Q, T, self.n_q_heads, "Q")
+        k, ks = self._rows(K, T, H, "K")
+        v, vs = self._rows(V, T, H, "V")
+        if decay.dtype is not self._f32 or not decay.is_cuda or decay.shape not in ((T, H), (H,)) or \
+                (H > 1 and decay.stride(-1) != 1):
+            raise ValueError("decay: expected an fp32 CUDA tensor [%d, %d] or [%d]" % (T, H, H))
+        gs = 0
+        if decay.dim() == 2:
+            gs = decay.stride(0) if T > 1 else H
+        s1 = None
+        if state_out is not None:
+            if state_out.dtype is not self._f32 or state_out.shape != (self._seqs, H, D, D) or not state_out.is_cuda or \
+                    not state_out.is_contiguous():
+                raise ValueError("state_out: expected a contiguous fp32 CUDA tensor [%d, %d, %d, %d]" % (self._seqs, H, D, D))
+            s1 = state_out.data_ptr()
+        raw = self._on(stream)
+        if O is None:
+            O = _made(Q.shape, self._bf16, self._dev, stream, raw)
+            o, os = O.data_ptr(), self.n_q_heads * D
+        else:
+            o, os = self._rows(O, T, self.n_q_heads, "O")
+        mode = L.FK_LINEAR_ADVANCE if advance and state_out is None else L.FK_LINEAR_STAY
+        _check(self._lib.fk_linear_attend(self._h, layer, q, qs, k, ks, v, vs, decay.data_ptr(), gs, o, os,
+                                          0.0 if scale is None else scale, mode, s1, raw), "fk_linear_attend")
+        return O
+
+    def states(self, layer):
+        """The states of a layer, fp32 [max_seqs, n_kv_heads, head_dim of k, head_dim of v]: the cache's own memory, to be read
+        and written on the stream that the layer's calls use, while the cache lives."""
+        p = ctypes.c_void_p()
+        _check(self._lib.fk_linear_states(self._h, layer, ctypes.byref(p)), "fk_linear_states")
+        import torch
+        D = self.head_dim
+
+        class View:
+            cache = self                             # (a view keeps its cache)
+            __cuda_array_interface__ = {"shape": (self.max_seqs, self.n_kv_heads, D, D), "typestr": "<f4",
+                                        "data": (p.value, False), "version": 3}
+
+        return torch.as_tensor(View(), device=self._dev)
+
+    def drop(self, seq, stream=None):
+        """Zero a sequence's states: a new sequence may take its number."""
+        _check(self._lib.fk_linear_drop(self._h, seq, self._on(stream)), "fk_linear_drop")
+
+    def fork(self, dst, src, stream=None):
+        """Sequence dst's states become copies of sequence src's."""
+        _check(self._lib.fk_linear_fork(self._h, dst, src, self._on(stream)), "fk_linear_fork")
+
+    # ---- inspection
+    def reserved_bytes(self) -> int:
+        return int(self._lib.fk_linear_reserved_bytes(self._h))
+
+    def launch_count(self) -> int:
+        return int(self._lib.fk_linear_launch_count(self._h))
+
+    def sync_status(self, stream=None) -> int:
+        """Synchronize and return the device status (FK_OK, FK_ERR_TIMEOUT)."""
+        return int(self._lib.fk_linear_sync_status(self._h, self._on(stream)))

@@ -18,6 +18,9 @@ FK_SCORE_PER_HEAD, FK_SCORE_LAYER0_POOLED = 0, 1
 FK_SELECT = {"similarity": 0, "all": 1, "uniform": 2, "random": 3}
 FK_ATTN = {"bf16": 0, "fp8_qk": 1, "fp8": 2}
 FK_ROPE = {"half": 0, "interleaved": 1}
+FK_ROPE_SCALE = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+FK_TYPE_BF16, FK_TYPE_F16, FK_TYPE_F32 = 0, 1, 2
+FK_LINEAR_ADVANCE, FK_LINEAR_STAY = 0, 1
 KERNEL_KINDS = {"append": 0, "score": 1, "select": 2, "compact": 3, "attend": 4}
 
 EXPORTS = [
@@ -30,6 +33,10 @@ EXPORTS = [
     "fk_paged_validate_config", "fk_paged_create", "fk_paged_destroy", "fk_paged_step", "fk_paged_append",
     "fk_paged_attend", "fk_paged_read", "fk_paged_drop", "fk_paged_length", "fk_paged_free_pages",
     "fk_paged_reserved_bytes", "fk_paged_launch_count", "fk_paged_sync_status",
+    "fk_rotary_make", "fk_rotate", "fk_rotary_tables",
+    "fk_linear_validate_config", "fk_linear_create", "fk_linear_destroy", "fk_linear_step", "fk_linear_attend",
+    "fk_linear_states", "fk_linear_drop", "fk_linear_fork", "fk_linear_reserved_bytes", "fk_linear_launch_count",
+    "fk_linear_sync_status",
 ]
 
 
@@ -56,6 +63,25 @@ class FkPagedConfig(ctypes.Structure):
 class FkRope(ctypes.Structure):
     _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("rows", ctypes.c_int32), ("dim", ctypes.c_int32)]
+
+
+class FkRotaryConfig(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("dim", ctypes.c_int32), ("style", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4), ("scaling", ctypes.c_int32),
+                ("original_tokens", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("slow_turns", ctypes.c_double), ("fast_turns", ctypes.c_double), ("magnitude", ctypes.c_double),
+                ("frequencies", ctypes.POINTER(ctypes.c_double))]
+
+
+class FkRotary(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_uint64 * 128), ("magnitude", ctypes.c_float), ("head_dim", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("style", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("first", ctypes.c_int32 * 4)]
+
+
+class FkLinearConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("n_layers", "n_q_heads", "n_kv_heads", "head_dim", "max_seqs", "device")]
 
 
 class FkError(RuntimeError):
@@ -124,6 +150,20 @@ def load(path: str | None = None) -> ctypes.CDLL:
         "fk_paged_reserved_bytes": (ctypes.c_size_t, [vp]),
         "fk_paged_launch_count": (i64, [vp]),
         "fk_paged_sync_status": (st, [vp, vp]),
+        "fk_rotary_make": (st, [ctypes.POINTER(FkRotaryConfig), ctypes.POINTER(FkRotary)]),
+        "fk_rotate": (st, [ctypes.POINTER(FkRotary), i64, vp, i32, i32, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp]),
+        "fk_rotary_tables": (st, [ctypes.POINTER(FkRotary), i64, vp, vp, vp, vp]),
+        "fk_linear_validate_config": (st, [ctypes.POINTER(FkLinearConfig)]),
+        "fk_linear_create": (st, [ctypes.POINTER(FkLinearConfig), ctypes.POINTER(vp)]),
+        "fk_linear_destroy": (None, [vp]),
+        "fk_linear_step": (st, [vp, i32, vp, vp]),
+        "fk_linear_attend": (st, [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, ctypes.c_float, i32, vp, vp]),
+        "fk_linear_states": (st, [vp, i32, ctypes.POINTER(vp)]),
+        "fk_linear_drop": (st, [vp, i32, vp]),
+        "fk_linear_fork": (st, [vp, i32, i32, vp]),
+        "fk_linear_reserved_bytes": (ctypes.c_size_t, [vp]),
+        "fk_linear_launch_count": (i64, [vp]),
+        "fk_linear_sync_status": (st, [vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

@@ -1,0 +1,163 @@
+// Linear attention with decays, token by token: S = exp(g) S + k v^T, o = scale q^T S in fp32.
+//
+// For single tokens and drafts, where nothing but the state's bytes counts: D^2 floats of each head are read and
+// written once, whatever the number of tokens.  A CTA holds 32 columns (channels of v) of one head's state in its registers:
+// thread (r, c) rows r D/16 .. and columns 4c .. 4c + 3.  A token's k and q come straight from global memory (16 or
+// 8 bytes a thread, the same for the 8 threads of a row group), the next token's while this one is computed; o is a sum
+// over the 16 row groups: by shuffles in a warp, then over the 4 warps through shared memory.
+#include "fk_linear.h"
+
+namespace fk {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kCols = 32;             // of a CTA
+constexpr int kSums = 32;             // rows of o that are collected before the warps' parts are added
+
+template <int N>
+struct Row {                          // N bf16 in registers
+  uint32_t w[N / 2];
+  __device__ __forceinline__ void load(const bf16* p) {
+    if constexpr (N == 8) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+      w[0] = v.x, w[1] = v.y;
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 8) linear_few_kernel(const __grid_constant__ LinearArgs a) {
+  constexpr int kRows = D / 16;       // of a thread
+  constexpr int kSlices = D / kCols;
+  __shared__ __align__(16) float sums[kSums][4][kCols];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = tid & 7, r = tid >> 3;
+  const int slice = blockIdx.x % kSlices, rest = blockIdx.x / kSlices;
+  const int h = rest % a.Hkv, k = rest / a.Hkv;
+  const int n = a.seqs.len[k];
+  const int64_t tok0 = a.seqs.tok0[k];
+  const int64_t at = (int64_t)(r * kRows) * D + slice * kCols + c * 4;
+  const float* s0 = a.state + ((int64_t)a.seqs.slot[k] * a.Hkv + h) * (D * D) + at;
+  float4 s[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) s[i] = *reinterpret_cast<const float4*>(s0 + i * D);
+
+  const bf16* K = a.K + tok0 * a.kstride + h * D + r * kRows;
+  const bf16* V = a.V + tok0 * a.vstride + h * D + slice * kCols + c * 4;
+  const bf16* Q = a.Q + tok0 * a.qstride + (int64_t)h * a.G * D + r * kRows;
+  const float* decay = a.decay + tok0 * a.dstride + h;
+  Row<kRows> kk, qq;
+  Row<4> vv;
+  float g = 0.0f;
+  auto load = [&](int t) {
+    kk.load(K + t * a.kstride);
+    vv.load(V + t * a.vstride);
+    qq.load(Q + t * a.qstride);
+    g = __ldg(decay + t * a.dstride);
+  };
+  // rows [first, first + m) of o, numbered token by token and query head by query head
+  auto flush = [&](int64_t first, int m) {
+    __syncthreads();
+    for (int i = tid; i < m * (kCols / 2); i += kThreads) {
+      const int p = i / (kCols / 2), x = 2 * (i % (kCols / 2));
+      float2 o = make_float2(0.0f, 0.0f);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float2 y = *reinterpret_cast<const float2*>(&sums[p][w][x]);
+        o.x += y.x;
+        o.y += y.y;
+      }
+      const int64_t row = first + p, t = row / a.G;
+      *reinterpret_cast<__nv_bfloat162*>(a.O + (tok0 + t) * a.ostride + ((int64_t)h * a.G + (row - t * a.G)) * D +
+                                         slice * kCols + x) = __floats2bfloat162_rn(o.x * a.scale, o.y * a.scale);
+    }
+    __syncthreads();
+  };
+  if (n > 0) load(0);
+  int64_t row = 0;
+  int held = 0;
+  for (int t = 0; t < n; ++t) {
+    const Row<kRows> kt = kk;
+    const Row<4> vt = vv;
+    Row<kRows> q = qq;
+    const float e = expf(g), less = expm1f(g);
+    if (t + 1 < n) load(t + 1);
+    // exp(g) rounded is off by up to 2^-24 at every token alike, and a slow decay takes thousands of them: there what the
+    // state loses, S (exp(g) - 1), is added
+    if (e > 0.5f) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const float x = kt.get(i);
+        s[i].x = fmaf(less, s[i].x, fmaf(x, vt.get(0), s[i].x));
+        s[i].y = fmaf(less, s[i].y, fmaf(x, vt.get(1), s[i].y));
+        s[i].z = fmaf(less, s[i].z, fmaf(x, vt.get(2), s[i].z));
+        s[i].w = fmaf(less, s[i].w, fmaf(x, vt.get(3), s[i].w));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const float x = kt.get(i);
+        s[i].x = fmaf(e, s[i].x, x * vt.get(0));
+        s[i].y = fmaf(e, s[i].y, x * vt.get(1));
+        s[i].z = fmaf(e, s[i].z, x * vt.get(2));
+        s[i].w = fmaf(e, s[i].w, x * vt.get(3));
+      }
+    }
+    for (int j = 0; j < a.G; ++j) {
+      Row<kRows> next = q;
+      if (j + 1 < a.G) next.load(Q + t * a.qstride + (j + 1) * D);
+      float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const float x = q.get(i);
+        o.x = fmaf(x, s[i].x, o.x);
+        o.y = fmaf(x, s[i].y, o.y);
+        o.z = fmaf(x, s[i].z, o.z);
+        o.w = fmaf(x, s[i].w, o.w);
+      }
+#pragma unroll
+      for (int m = 8; m < 32; m *= 2) {
+        o.x += __shfl_xor_sync(0xffffffffu, o.x, m);
+        o.y += __shfl_xor_sync(0xffffffffu, o.y, m);
+        o.z += __shfl_xor_sync(0xffffffffu, o.z, m);
+        o.w += __shfl_xor_sync(0xffffffffu, o.w, m);
+      }
+      if (lane < 8) *reinterpret_cast<float4*>(&sums[held][warp][4 * lane]) = o;
+      if (++held == kSums) {
+        flush(row, held);
+        row += held;
+        held = 0;
+      }
+      q = next;
+    }
+  }
+  if (a.state_new) {
+    float* s1 = a.state_new + ((int64_t)(a.to_out ? a.seqs.out[k] : a.seqs.slot[k]) * a.Hkv + h) * (D * D) + at;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4*>(s1 + i * D) = s[i];
+  }
+  if (held > 0) flush(row, held);
+}
+
+__global__ void linear_status_kernel(int* status, int* report) { *report = atomicExch(status, 0); }
+
+}  // namespace
+
+cudaError_t launch_linear_few(int D, const LinearArgs& a, cudaStream_t s) {
+  const unsigned grid = (unsigned)a.seqs.n * a.Hkv * (D / kCols);
+  if (D == 128) linear_few_kernel<128><<<grid, kThreads, 0, s>>>(a);
+  else linear_few_kernel<64><<<grid, kThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_linear_status(int* status, int* report, cudaStream_t s) {
+  linear_status_kernel<<<1, 1, 0, s>>>(status, report);
+  return cudaGetLastError();
+}
+
+}  // namespace fk

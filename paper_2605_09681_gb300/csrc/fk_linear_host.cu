@@ -1,0 +1,307 @@
+// Host side of linear attention with decays: states, steps, and the C ABI (fk_linear_*).
+//
+// The host knows every length, so it hands the kernels their sequences by value (kLinearSeqs to a launch).  Nothing is
+// allocated or waited for after fk_linear_create, so that a step's attentions can be captured in a graph; which states
+// a launch reads depends on the step alone, so that a graph's replays go on from one another.
+#include "fk_linear.h"
+
+#include <algorithm>
+#include <cmath>
+#include <memory>
+#include <new>
+
+using namespace fk;
+
+namespace {
+
+struct StepSeq {
+  int seq, n_new;
+};
+
+// the caller's current device comes back when a call ends
+struct DeviceGuard {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceGuard(int dev) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != dev) err = cudaSetDevice(dev);
+    else if (err == cudaSuccess) before = -1;
+  }
+  ~DeviceGuard() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+
+}  // namespace
+
+struct fk_linear {
+  fk_linear_config cfg{};
+  std::vector<StepSeq> step;
+  bool in_step = false;
+  int64_t tokens = 0;                 // of the step
+  float* states = nullptr;            // [layers][max_seqs][Hkv][D][D]
+  size_t per_seq = 0, per_layer = 0;  // floats
+  int* status = nullptr;              // the status word, and a report of it
+  std::vector<void*> allocs;
+  size_t reserved = 0;
+  int64_t launches = 0;
+  ~fk_linear() {
+    for (void* p : allocs) cudaFree(p);
+    cudaGetLastError();
+  }
+};
+
+namespace {
+
+// No C++ exception leaves a C entry: the only ones here are failed host allocations.
+template <class F>
+fk_status guarded(F&& f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return FK_ERR_NOMEM;
+  } catch (...) {
+    return FK_ERR_STATE;
+  }
+}
+
+bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+bool on_device(const void* p, int dev) {
+  cudaPointerAttributes at{};
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev);
+}
+
+fk_status done(fk_linear* h, cudaError_t e) {
+  h->launches++;
+  return e == cudaSuccess ? FK_OK : FK_ERR_CUDA;
+}
+
+fk_status alloc(fk_linear* h, size_t bytes, void** out) {
+  void* p = nullptr;
+  cudaError_t e = cudaMalloc(&p, bytes);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return e == cudaErrorMemoryAllocation ? FK_ERR_NOMEM : FK_ERR_CUDA;
+  }
+  h->allocs.push_back(p);
+  h->reserved += bytes;
+  *out = p;
+  return cudaMemset(p, 0, bytes) == cudaSuccess ? FK_OK : FK_ERR_CUDA;
+}
+
+// `tokens` rows of `width` bytes, `stride` bytes apart
+struct Rows {
+  uintptr_t p;
+  int64_t stride, width;
+};
+// Whether rows of one meet rows of the other.  With one stride, slices of the same wide rows are told apart; else whole
+// extents are compared.
+bool meet(const Rows& a, const Rows& b, int64_t tokens) {
+  const int64_t la = (tokens - 1) * a.stride + a.width, lb = (tokens - 1) * b.stride + b.width;
+  if (a.p + (uintptr_t)la <= b.p || b.p + (uintptr_t)lb <= a.p) return false;
+  if (a.stride != b.stride || tokens == 1) return true;
+  const int64_t d = (int64_t)(a.p < b.p ? b.p - a.p : a.p - b.p) % a.stride;
+  const int64_t low = a.p < b.p ? a.width : b.width, high = a.p < b.p ? b.width : a.width;
+  return d < low || a.stride - d < high;
+}
+
+}  // namespace
+
+extern "C" {
+
+fk_status fk_linear_validate_config(const fk_linear_config* c) {
+  if (!c) return FK_ERR_ARG;
+  if (c->n_layers < 1 || c->n_layers > kMaxLayers) return FK_ERR_CONFIG;
+  if (c->n_kv_heads < 1 || c->n_kv_heads > kMaxHeads || c->n_q_heads < c->n_kv_heads || c->n_q_heads > 1024 ||
+      c->n_q_heads % c->n_kv_heads)
+    return FK_ERR_CONFIG;
+  if (c->head_dim != 64 && c->head_dim != 128) return FK_ERR_CONFIG;
+  if (c->max_seqs < 1 || c->max_seqs > 65536) return FK_ERR_CONFIG;
+  return FK_OK;
+}
+
+fk_status fk_linear_create(const fk_linear_config* cfg, fk_linear** out) {
+  if (!out) return FK_ERR_ARG;
+  *out = nullptr;
+  fk_status st = fk_linear_validate_config(cfg);
+  if (st != FK_OK) return st;
+  return guarded([&]() -> fk_status {
+    int n_dev = 0;
+    if (cudaGetDeviceCount(&n_dev) != cudaSuccess || cfg->device < 0 || cfg->device >= n_dev) {
+      cudaGetLastError();
+      return FK_ERR_CUDA;
+    }
+    DeviceGuard dev(cfg->device);
+    if (dev.err != cudaSuccess) return FK_ERR_CUDA;
+    std::unique_ptr<fk_linear> h(new fk_linear());
+    h->cfg = *cfg;
+    h->per_seq = (size_t)cfg->n_kv_heads * cfg->head_dim * cfg->head_dim;
+    h->per_layer = h->per_seq * cfg->max_seqs;
+    void* p = nullptr;
+    if ((st = alloc(h.get(), h->per_layer * cfg->n_layers * sizeof(float), &p)) != FK_OK) return st;
+    h->states = static_cast<float*>(p);
+    if ((st = alloc(h.get(), 2 * sizeof(int), &p)) != FK_OK) return st;
+    h->status = static_cast<int*>(p);
+    if (cudaDeviceSynchronize() != cudaSuccess) return FK_ERR_CUDA;
+    *out = h.release();
+    return FK_OK;
+  });
+}
+
+void fk_linear_destroy(fk_linear* h) {
+  if (!h) return;
+  DeviceGuard dev(h->cfg.device);
+  cudaDeviceSynchronize();
+  delete h;
+}
+
+fk_status fk_linear_step(fk_linear* h, int n_seqs, const int32_t* seqs, const int32_t* n_new) {
+  if (!h || n_seqs < 0 || (n_seqs > 0 && (!seqs || !n_new))) return FK_ERR_ARG;
+  if (n_seqs > h->cfg.max_seqs) return FK_ERR_ARG;
+  return guarded([&]() -> fk_status {
+    std::vector<uint8_t> seen(h->cfg.max_seqs, 0);
+    std::vector<StepSeq> step(n_seqs);
+    int64_t total = 0;
+    for (int i = 0; i < n_seqs; ++i) {
+      if (seqs[i] < 0 || seqs[i] >= h->cfg.max_seqs || seen[seqs[i]] || n_new[i] < 0) return FK_ERR_ARG;
+      seen[seqs[i]] = 1;
+      step[i] = {seqs[i], n_new[i]};
+      total += n_new[i];
+    }
+    if (total * h->cfg.n_q_heads >= ((int64_t)1 << 31)) return FK_ERR_ARG;
+    h->step.swap(step);
+    h->tokens = total;
+    h->in_step = true;
+    return FK_OK;
+  });
+}
+
+fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                           const void* V, int64_t v_stride, const float* decay, int64_t decay_stride, void* O, int64_t o_stride,
+                           float scale, int mode, float* state_out, void* stream) {
+  if (!h || layer < 0 || layer >= h->cfg.n_layers) return FK_ERR_ARG;
+  if ((mode != FK_LINEAR_ADVANCE && mode != FK_LINEAR_STAY) || !(scale >= 0.0f) || std::isinf(scale)) return FK_ERR_CONFIG;
+  if (mode == FK_LINEAR_ADVANCE && state_out) return FK_ERR_ARG;
+  if (!h->in_step) return FK_ERR_STATE;
+  const fk_linear_config& c = h->cfg;
+  if (h->step.empty() || (h->tokens == 0 && !state_out)) return FK_OK;
+  return guarded([&]() -> fk_status {
+    DeviceGuard dev(c.device);
+    if (dev.err != cudaSuccess) return FK_ERR_CUDA;
+    if (state_out) {
+      const size_t bytes = h->step.size() * h->per_seq * sizeof(float);
+      const uintptr_t p = reinterpret_cast<uintptr_t>(state_out), own = reinterpret_cast<uintptr_t>(h->states);
+      if (!aligned(state_out, 16) || !on_device(state_out, c.device)) return FK_ERR_ARG;
+      if (p < own + h->per_layer * c.n_layers * sizeof(float) && own < p + bytes) return FK_ERR_ARG;
+    }
+    if (h->tokens > 0) {
+      const int64_t wq = (int64_t)c.n_q_heads * c.head_dim, wk = (int64_t)c.n_kv_heads * c.head_dim;
+      auto rows_ok = [&](const void* p, int64_t stride, int64_t width) {
+        return p && aligned(p, 16) && stride >= width && stride % 8 == 0 && on_device(p, c.device);
+      };
+      if (!rows_ok(Q, q_stride, wq) || !rows_ok(O, o_stride, wq) || !rows_ok(K, k_stride, wk) || !rows_ok(V, v_stride, wk))
+        return FK_ERR_ARG;
+      if (!decay || !aligned(decay, 4) || (decay_stride != 0 && decay_stride < c.n_kv_heads) || !on_device(decay, c.device))
+        return FK_ERR_ARG;
+      auto rows = [](const void* p, int64_t stride, int64_t width) {
+        return Rows{reinterpret_cast<uintptr_t>(p), stride * 2, width * 2};
+      };
+      const Rows o = rows(O, o_stride, wq);
+      if (meet(o, rows(Q, q_stride, wq), h->tokens) || meet(o, rows(K, k_stride, wk), h->tokens) ||
+          meet(o, rows(V, v_stride, wk), h->tokens))
+        return FK_ERR_ARG;
+    }
+    auto a = std::make_unique<LinearArgs>();
+    a->Q = static_cast<const bf16*>(Q);
+    a->K = static_cast<const bf16*>(K);
+    a->V = static_cast<const bf16*>(V);
+    a->O = static_cast<bf16*>(O);
+    a->qstride = q_stride;
+    a->kstride = k_stride;
+    a->vstride = v_stride;
+    a->ostride = o_stride;
+    a->decay = decay;
+    a->dstride = decay_stride;
+    a->scale = scale > 0.0f ? scale : (float)(1.0 / std::sqrt((double)c.head_dim));
+    a->Hkv = c.n_kv_heads;
+    a->G = c.n_q_heads / c.n_kv_heads;
+    a->state = h->states + h->per_layer * layer;
+    a->state_new = mode == FK_LINEAR_ADVANCE ? h->states + h->per_layer * layer : state_out;
+    a->to_out = mode != FK_LINEAR_ADVANCE;
+    a->status = h->status;
+    int64_t tok = 0;
+    for (size_t i = 0; i < h->step.size();) {
+      a->seqs.n = 0;
+      for (; i < h->step.size() && a->seqs.n < kLinearSeqs; ++i) {
+        const StepSeq& s = h->step[i];
+        if (s.n_new > 0 || state_out) {
+          const int k = a->seqs.n++;
+          a->seqs.slot[k] = s.seq;
+          a->seqs.out[k] = (int)i;
+          a->seqs.tok0[k] = (int)tok;
+          a->seqs.len[k] = s.n_new;
+        }
+        tok += s.n_new;
+      }
+      if (a->seqs.n == 0) continue;
+      const fk_status st = done(h, launch_linear_few(c.head_dim, *a, static_cast<cudaStream_t>(stream)));
+      if (st != FK_OK) return st;
+    }
+    return FK_OK;
+  });
+}
+
+fk_status fk_linear_states(const fk_linear* h, int layer, float** states) {
+  if (!h || layer < 0 || layer >= h->cfg.n_layers || !states) return FK_ERR_ARG;
+  *states = h->states + h->per_layer * layer;
+  return FK_OK;
+}
+
+fk_status fk_linear_drop(fk_linear* h, int seq, void* stream) {
+  if (!h || seq < 0 || seq >= h->cfg.max_seqs) return FK_ERR_ARG;
+  DeviceGuard dev(h->cfg.device);
+  if (dev.err != cudaSuccess) return FK_ERR_CUDA;
+  for (int l = 0; l < h->cfg.n_layers; ++l)
+    if (cudaMemsetAsync(h->states + h->per_layer * l + h->per_seq * seq, 0, h->per_seq * sizeof(float),
+                        static_cast<cudaStream_t>(stream)) != cudaSuccess)
+      return FK_ERR_CUDA;
+  return FK_OK;
+}
+
+fk_status fk_linear_fork(fk_linear* h, int dst, int src, void* stream) {
+  if (!h || dst < 0 || dst >= h->cfg.max_seqs || src < 0 || src >= h->cfg.max_seqs) return FK_ERR_ARG;
+  if (dst == src) return FK_OK;
+  DeviceGuard dev(h->cfg.device);
+  if (dev.err != cudaSuccess) return FK_ERR_CUDA;
+  for (int l = 0; l < h->cfg.n_layers; ++l) {
+    float* s = h->states + h->per_layer * l;
+    if (cudaMemcpyAsync(s + h->per_seq * dst, s + h->per_seq * src, h->per_seq * sizeof(float), cudaMemcpyDeviceToDevice,
+                        static_cast<cudaStream_t>(stream)) != cudaSuccess)
+      return FK_ERR_CUDA;
+  }
+  return FK_OK;
+}
+
+size_t fk_linear_reserved_bytes(const fk_linear* h) { return h ? h->reserved : 0; }
+
+int64_t fk_linear_launch_count(const fk_linear* h) { return h ? h->launches : 0; }
+
+fk_status fk_linear_sync_status(fk_linear* h, void* stream) {
+  if (!h) return FK_ERR_ARG;
+  DeviceGuard dev(h->cfg.device);
+  if (dev.err != cudaSuccess) return FK_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int word = 0;
+  if (done(h, launch_linear_status(h->status, h->status + 1, s)) != FK_OK ||
+      cudaMemcpyAsync(&word, h->status + 1, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+      cudaStreamSynchronize(s) != cudaSuccess)
+    return FK_ERR_CUDA;
+  return word & kStatusTimeout ? FK_ERR_TIMEOUT : FK_OK;
+}
+
+}  // extern "C"

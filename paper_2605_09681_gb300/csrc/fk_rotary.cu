@@ -1,0 +1,380 @@
+// Rotary positions: queries and keys turned by their positions, and tables of the angles.
+//
+// A pair's angle is position * f modulo a turn.  f is kept as a 64-bit fraction of a turn, so that the 64-bit product
+// with the position, taken modulo 2^64, is the angle modulo whole turns without any error: an fp32 product of
+// a position and a frequency is off by a radian and more at position 10^7.  Its upper bits are cut to fp32
+// (2^-25 of a turn) for sincospi.
+//
+// Both kernels move each byte once and should be bound by DRAM.  The angles are the expensive part (a sine and a
+// cosine of a pair cost as much as the rotation of several heads), so a thread turns the same 8 pairs of several heads.
+#include "fk_internal.h"
+
+#include <cuda_fp16.h>
+
+#include <cmath>
+
+namespace fk {
+namespace {
+
+constexpr int kMaxPairs = 128;
+constexpr int kThreads = 256;
+
+struct Angles {
+  uint64_t turns[kMaxPairs];
+  const int* positions;               // [tokens][axes]
+  int axes;
+  int first[4];                       // first pair of each axis
+  float magnitude;
+};
+
+struct RotateArgs {
+  Angles a;
+  int64_t tokens;
+  int dim, units, rotated;            // units of a head: 8 pairs each, then 8 channels each that are copied
+  int per_block, per_group;           // tokens of a block, heads of a thread
+  int heads1, heads;                  // of the first tensor, of both
+  int head_dim;
+  const char* x[2];
+  char* y[2];
+  int64_t xs[2], ys[2];               // bytes from token to token
+  int inverse;
+};
+
+struct TableArgs {
+  Angles a;
+  int64_t tokens;
+  int pairs, per_block;
+  float* cos;
+  float* sin;
+};
+
+// The fractions in shared memory (every thread reads others) and a pair's angle from there.
+__device__ __forceinline__ void stage(const Angles& a, int pairs, uint64_t* s) {
+  for (int i = threadIdx.x; i < pairs; i += blockDim.x) s[i] = a.turns[i];
+  __syncthreads();
+}
+
+// cos and sin of the angle `pos * turns` (times m, sin with the sign of `dir`)
+__device__ __forceinline__ void angle(uint64_t turns, int pos, float m, float dir, float* c, float* s) {
+  const uint64_t t = turns * (uint64_t)(int64_t)pos;
+  // the fraction as a signed number of half turns in [-1, 1)
+  const float x = fmaf((float)(uint32_t)t, 0x1p-63f, (float)(int32_t)(uint32_t)(t >> 32) * 0x1p-31f);
+  float sn, cs;
+  sincospif(x, &sn, &cs);
+  *c = cs * m;
+  *s = sn * dir;
+}
+
+__device__ __forceinline__ int axis_of(const Angles& a, int pair) {
+  return (a.axes > 1 && pair >= a.first[1]) + (a.axes > 2 && pair >= a.first[2]) + (a.axes > 3 && pair >= a.first[3]);
+}
+
+// eight channels in memory <-> fp32
+template <class T>
+struct Eight;
+template <>
+struct Eight<float> {
+  float4 v[2];
+  __device__ __forceinline__ void load(const char* p) {
+    v[0] = reinterpret_cast<const float4*>(p)[0];
+    v[1] = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void store(char* p) const {
+    reinterpret_cast<float4*>(p)[0] = v[0];
+    reinterpret_cast<float4*>(p)[1] = v[1];
+  }
+  __device__ __forceinline__ void get(float* x) const {
+    x[0] = v[0].x, x[1] = v[0].y, x[2] = v[0].z, x[3] = v[0].w;
+    x[4] = v[1].x, x[5] = v[1].y, x[6] = v[1].z, x[7] = v[1].w;
+  }
+  __device__ __forceinline__ void set(const float* x) {
+    v[0] = make_float4(x[0], x[1], x[2], x[3]);
+    v[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+};
+template <class T, class T2>
+struct EightHalves {
+  uint4 v;
+  __device__ __forceinline__ void load(const char* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void store(char* p) const { *reinterpret_cast<uint4*>(p) = v; }
+};
+template <>
+struct Eight<bf16> : EightHalves<bf16, __nv_bfloat162> {
+  __device__ __forceinline__ void get(float* x) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+  __device__ __forceinline__ void set(const float* x) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Eight<__half> : EightHalves<__half, __half2> {
+  __device__ __forceinline__ void get(float* x) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      x[2 * i] = f.x, x[2 * i + 1] = f.y;
+    }
+  }
+  __device__ __forceinline__ void set(const float* x) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 p = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// One thread: a unit of a token, in the heads of one group.  kHalf: pairs (i, i + dim / 2).
+template <class T, bool kHalf>
+__global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant__ RotateArgs a) {
+  __shared__ uint64_t turns[kMaxPairs];
+  stage(a.a, a.dim / 2, turns);
+  const int tb = threadIdx.x / a.units, u = threadIdx.x - tb * a.units;
+  const int64_t t = (int64_t)blockIdx.x * a.per_block + tb;
+  if (tb >= a.per_block || t >= a.tokens) return;
+  const int h0 = blockIdx.y * a.per_group, h1 = min(h0 + a.per_group, a.heads);
+  const bool turn = u < a.rotated;
+  // byte offsets in a head of the unit's two blocks of 8 channels (one block where channels are copied)
+  const int c0 = turn ? (kHalf ? 8 * u : 16 * u) : a.dim + 8 * (u - a.rotated);
+  const int c1 = kHalf ? c0 + a.dim / 2 : c0 + 8;
+  float cs[8], sn[8];
+  if (turn) {
+    const int* pos = a.a.positions + t * a.a.axes;
+    const float dir = a.inverse ? -a.a.magnitude : a.a.magnitude;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = 8 * u + i;
+      angle(turns[p], __ldg(pos + axis_of(a.a, p)), a.a.magnitude, dir, &cs[i], &sn[i]);
+    }
+  }
+#pragma unroll 2
+  for (int h = h0; h < h1; ++h) {
+    const int k = h >= a.heads1, hh = k ? h - a.heads1 : h;
+    const char* x = a.x[k] + t * a.xs[k] + (int64_t)hh * a.head_dim * sizeof(T);
+    char* y = a.y[k] + t * a.ys[k] + (int64_t)hh * a.head_dim * sizeof(T);
+    Eight<T> p, q;
+    p.load(x + c0 * sizeof(T));
+    if (!turn) {
+      p.store(y + c0 * sizeof(T));
+      continue;
+    }
+    q.load(x + c1 * sizeof(T));
+    float f[16];
+    p.get(f);
+    q.get(f + 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float& u0 = kHalf ? f[i] : f[2 * i];
+      float& u1 = kHalf ? f[8 + i] : f[2 * i + 1];
+      const float v0 = fmaf(u0, cs[i], -(u1 * sn[i])), v1 = fmaf(u1, cs[i], u0 * sn[i]);
+      u0 = v0;
+      u1 = v1;
+    }
+    p.set(f);
+    q.set(f + 8);
+    p.store(y + c0 * sizeof(T));
+    q.store(y + c1 * sizeof(T));
+  }
+}
+
+// One thread: 4 pairs of a token.
+__global__ void __launch_bounds__(kThreads) tables_kernel(const __grid_constant__ TableArgs a) {
+  __shared__ uint64_t turns[kMaxPairs];
+  stage(a.a, a.pairs, turns);
+  const int quads = a.pairs / 4, tb = threadIdx.x / quads, p = 4 * (threadIdx.x - tb * quads);
+  const int64_t t = (int64_t)blockIdx.x * a.per_block + tb;
+  if (tb >= a.per_block || t >= a.tokens) return;
+  const int* pos = a.a.positions + t * a.a.axes;
+  float c[4], s[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    angle(turns[p + i], __ldg(pos + axis_of(a.a, p + i)), a.a.magnitude, a.a.magnitude, &c[i], &s[i]);
+  *reinterpret_cast<float4*>(a.cos + t * a.pairs + p) = make_float4(c[0], c[1], c[2], c[3]);
+  *reinterpret_cast<float4*>(a.sin + t * a.pairs + p) = make_float4(s[0], s[1], s[2], s[3]);
+}
+
+bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+bool on_current_device(const void* p) {
+  cudaPointerAttributes at{};
+  int dev = -1;
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess || cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev);
+}
+
+// what fk_rotary_make makes
+bool made(const fk_rotary& r) {
+  if (r.head_dim < 16 || r.head_dim > 256 || r.head_dim % 8 || r.dim < 16 || r.dim > r.head_dim || r.dim % 16) return false;
+  if (r.style != FK_ROPE_HALF && r.style != FK_ROPE_INTERLEAVED) return false;
+  if (r.n_axes < 1 || r.n_axes > 4 || r.first[0] != 0) return false;
+  for (int i = 1; i < 4; ++i)
+    if (i < r.n_axes ? r.first[i] <= r.first[i - 1] || r.first[i] >= r.dim / 2 : r.first[i] != r.dim / 2) return false;
+  return std::isfinite(r.magnitude);
+}
+
+void fill(const fk_rotary& r, const int32_t* positions, Angles* a) {
+  for (int i = 0; i < kMaxPairs; ++i) a->turns[i] = r.turns[i];
+  a->positions = positions;
+  a->axes = r.n_axes;
+  for (int i = 0; i < 4; ++i) a->first[i] = r.first[i];
+  a->magnitude = r.magnitude;
+}
+
+// a frequency in radians a position -> the fraction of a turn in 2^-64 (its sign goes into the two's complement)
+uint64_t turns_of(double f) {
+  const double t = std::fabs(f) / 6.283185307179586476925286766559;   // below 1/2
+  const double hi = std::floor(std::ldexp(t, 32));
+  const uint64_t u = ((uint64_t)hi << 32) + (uint64_t)std::ldexp(std::ldexp(t, 32) - hi, 32);
+  return f < 0 ? 0 - u : u;
+}
+
+template <class T>
+cudaError_t launch_rotate(const RotateArgs& a, int style, dim3 grid, cudaStream_t s) {
+  if (style == FK_ROPE_HALF) rotate_kernel<T, true><<<grid, kThreads, 0, s>>>(a);
+  else rotate_kernel<T, false><<<grid, kThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+}  // namespace fk
+
+using namespace fk;
+
+extern "C" {
+
+fk_status fk_rotary_make(const fk_rotary_config* c, fk_rotary* out) {
+  if (!c || !out) return FK_ERR_ARG;
+  fk_rotary r{};
+  r.head_dim = c->head_dim;
+  r.dim = c->dim;
+  r.style = c->style;
+  r.n_axes = c->n_axes;
+  if (c->n_axes < 1 || c->n_axes > 4) return FK_ERR_CONFIG;
+  if (c->scaling < FK_ROPE_SCALE_NONE || c->scaling > FK_ROPE_SCALE_RAMP) return FK_ERR_CONFIG;
+  if (!std::isfinite(c->magnitude) || c->magnitude < 0.0) return FK_ERR_CONFIG;
+  int n = 0;
+  for (int a = 0; a < 4; ++a) {
+    r.first[a] = n;
+    if (a >= c->n_axes) continue;
+    if (c->pairs[a] < 1 || c->pairs[a] > kMaxPairs) return FK_ERR_CONFIG;
+    n += c->pairs[a];
+  }
+  r.magnitude = c->magnitude > 0.0 ? (float)c->magnitude : 1.0f;
+  if (2 * n != c->dim || !made(r)) return FK_ERR_CONFIG;
+  if (c->frequencies) {
+    for (int i = 0; i < n; ++i) {
+      if (!(std::fabs(c->frequencies[i]) < 3.14159265358979)) return FK_ERR_CONFIG;
+      r.turns[i] = turns_of(c->frequencies[i]);
+    }
+    *out = r;
+    return FK_OK;
+  }
+  if (!(c->base > 1.0) || std::isinf(c->base)) return FK_ERR_CONFIG;
+  if (c->scaling != FK_ROPE_SCALE_NONE && (!(c->factor >= 1.0) || std::isinf(c->factor))) return FK_ERR_CONFIG;
+  if (c->scaling == FK_ROPE_SCALE_RAMP) {
+    if (c->original_tokens < 1 || !(c->slow_turns >= 0.0) || !(c->fast_turns > c->slow_turns) || std::isinf(c->fast_turns))
+      return FK_ERR_CONFIG;
+    if (!(c->magnitude > 0.0)) r.magnitude = (float)(0.1 * std::log(c->factor) + 1.0);
+  }
+  for (int a = 0; a < c->n_axes; ++a) {
+    const double d = 2.0 * c->pairs[a];
+    if (c->scaling == FK_ROPE_SCALE_BASE && c->pairs[a] < 2) return FK_ERR_CONFIG;
+    const double base = c->scaling == FK_ROPE_SCALE_BASE ? c->base * std::pow(c->factor, d / (d - 2.0)) : c->base;
+    for (int i = 0; i < c->pairs[a]; ++i) {
+      double f = std::pow(base, -2.0 * i / d);
+      if (c->scaling == FK_ROPE_SCALE_LINEAR) f /= c->factor;
+      if (c->scaling == FK_ROPE_SCALE_RAMP) {
+        const double t = c->original_tokens * f / 6.283185307179586476925286766559;
+        const double keep = std::fmin(1.0, std::fmax(0.0, (t - c->slow_turns) / (c->fast_turns - c->slow_turns)));
+        f = f * keep + f / c->factor * (1.0 - keep);
+      }
+      r.turns[r.first[a] + i] = turns_of(f);
+    }
+  }
+  *out = r;
+  return FK_OK;
+}
+
+fk_status fk_rotate(const fk_rotary* r, int64_t tokens, const int32_t* positions, int inverse, int type, const void* X,
+                    int64_t x_stride, int x_heads, void* Y, int64_t y_stride, const void* X2, int64_t x2_stride, int x2_heads,
+                    void* Y2, int64_t y2_stride, void* stream) {
+  if (!r) return FK_ERR_ARG;
+  if (!made(*r) || (inverse != 0 && inverse != 1) || type < FK_TYPE_BF16 || type > FK_TYPE_F32) return FK_ERR_CONFIG;
+  if (tokens < 0 || tokens >= ((int64_t)1 << 31)) return FK_ERR_CONFIG;
+  if (x_heads < 1 || x_heads > 1024 || x2_heads < 0 || x2_heads > 1024) return FK_ERR_CONFIG;
+  if (!X2 != !Y2 || !X2 != (x2_heads == 0)) return FK_ERR_ARG;
+  if (tokens == 0) return FK_OK;
+  const int size = type == FK_TYPE_F32 ? 4 : 2;
+  auto rows_ok = [&](const void* p, int64_t stride, int heads) {
+    return p && aligned(p, 16) && stride >= (int64_t)heads * r->head_dim && stride * size % 16 == 0 && on_current_device(p);
+  };
+  if (!positions || !aligned(positions, 4) || !on_current_device(positions)) return FK_ERR_ARG;
+  if (!rows_ok(X, x_stride, x_heads) || !rows_ok(Y, y_stride, x_heads) || (X == Y && x_stride != y_stride)) return FK_ERR_ARG;
+  if (X2 && (!rows_ok(X2, x2_stride, x2_heads) || !rows_ok(Y2, y2_stride, x2_heads) || (X2 == Y2 && x2_stride != y2_stride)))
+    return FK_ERR_ARG;
+  RotateArgs a;
+  fill(*r, positions, &a.a);
+  a.tokens = tokens;
+  a.dim = r->dim;
+  a.rotated = r->dim / 16;
+  a.units = a.rotated + (r->head_dim - r->dim) / 8;
+  a.heads1 = x_heads;
+  a.heads = x_heads + x2_heads;
+  a.head_dim = r->head_dim;
+  a.inverse = inverse;
+  a.x[0] = static_cast<const char*>(X);
+  a.x[1] = static_cast<const char*>(X2);
+  a.y[0] = static_cast<char*>(Y);
+  a.y[1] = static_cast<char*>(Y2);
+  a.xs[0] = x_stride * size;
+  a.xs[1] = x2_stride * size;
+  a.ys[0] = y_stride * size;
+  a.ys[1] = y2_stride * size;
+  // heads of a thread: as many as leave the device full of threads
+  a.per_group = 1;
+  while (a.per_group < 8 && a.per_group < a.heads && tokens * a.units * a.heads / (2 * a.per_group) >= (int64_t)152 * 1024)
+    a.per_group *= 2;
+  a.per_block = kThreads / a.units;
+  const dim3 grid((unsigned)((tokens + a.per_block - 1) / a.per_block), (unsigned)((a.heads + a.per_group - 1) / a.per_group));
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (type == FK_TYPE_BF16) e = launch_rotate<bf16>(a, r->style, grid, s);
+  else if (type == FK_TYPE_F16) e = launch_rotate<__half>(a, r->style, grid, s);
+  else e = launch_rotate<float>(a, r->style, grid, s);
+  return e == cudaSuccess ? FK_OK : FK_ERR_CUDA;
+}
+
+fk_status fk_rotary_tables(const fk_rotary* r, int64_t tokens, const int32_t* positions, float* cos, float* sin, void* stream) {
+  if (!r) return FK_ERR_ARG;
+  if (!made(*r) || tokens < 0 || tokens >= ((int64_t)1 << 31)) return FK_ERR_CONFIG;
+  if (tokens == 0) return FK_OK;
+  if (!positions || !aligned(positions, 4) || !on_current_device(positions)) return FK_ERR_ARG;
+  for (const float* p : {cos, sin})
+    if (!p || !aligned(p, 16) || !on_current_device(p)) return FK_ERR_ARG;
+  TableArgs a;
+  fill(*r, positions, &a.a);
+  a.tokens = tokens;
+  a.pairs = r->dim / 2;
+  a.cos = cos;
+  a.sin = sin;
+  a.per_block = kThreads / (a.pairs / 4);
+  tables_kernel<<<(unsigned)((tokens + a.per_block - 1) / a.per_block), kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  return cudaGetLastError() == cudaSuccess ? FK_OK : FK_ERR_CUDA;
+}
+
+}  // extern "C"
