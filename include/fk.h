@@ -615,6 +615,11 @@ FK_API fk_status fk_linear_drop(fk_linear* h, int seq, void* stream);
 /* Sequence dst's states become copies of sequence src's, all layers, on `stream` (a fork). */
 FK_API fk_status fk_linear_fork(fk_linear* h, int dst, int src, void* stream);
 
+/* Fix how steps from the next one on are computed, for tests and measurements: sequences of up to `few` tokens by the
+ * recurrence, the others in chunks, each sequence split into `segments` runs of chunks (fewer where it has fewer chunks or the
+ * workspace is too small).  0: chosen by the lengths (the default).  FK_ERR_CONFIG for negative numbers. */
+FK_API fk_status fk_linear_force_plan(fk_linear* h, int few, int segments);
+
 /* Device memory that the handle allocated, kernels launched so far. */
 FK_API size_t fk_linear_reserved_bytes(const fk_linear* h);
 FK_API int64_t fk_linear_launch_count(const fk_linear* h);

@@ -742,6 +742,11 @@ class LinearStateCache:
         """Sequence dst's states become copies of sequence src's."""
         _check(self._lib.fk_linear_fork(self._h, dst, src, self._on(stream)), "fk_linear_fork")
 
+    def force_plan(self, few: int = 0, segments: int = 0) -> None:
+        """Fix up to how many tokens a sequence goes through the recurrence and into how many segments others are split, for
+        tests and measurements (fk_linear_force_plan); 0: chosen by the lengths."""
+        _check(self._lib.fk_linear_force_plan(self._h, int(few), int(segments)), "fk_linear_force_plan")
+
     # ---- inspection
     def reserved_bytes(self) -> int:
         return int(self._lib.fk_linear_reserved_bytes(self._h))

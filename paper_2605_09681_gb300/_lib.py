@@ -35,7 +35,7 @@ EXPORTS = [
     "fk_paged_reserved_bytes", "fk_paged_launch_count", "fk_paged_sync_status",
     "fk_rotary_make", "fk_rotate", "fk_rotary_tables",
     "fk_linear_validate_config", "fk_linear_create", "fk_linear_destroy", "fk_linear_step", "fk_linear_attend",
-    "fk_linear_states", "fk_linear_drop", "fk_linear_fork", "fk_linear_reserved_bytes", "fk_linear_launch_count",
+    "fk_linear_states", "fk_linear_force_plan", "fk_linear_drop", "fk_linear_fork", "fk_linear_reserved_bytes", "fk_linear_launch_count",
     "fk_linear_sync_status",
 ]
 
@@ -159,6 +159,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
         "fk_linear_step": (st, [vp, i32, vp, vp]),
         "fk_linear_attend": (st, [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, ctypes.c_float, i32, vp, vp]),
         "fk_linear_states": (st, [vp, i32, ctypes.POINTER(vp)]),
+        "fk_linear_force_plan": (st, [vp, i32, i32]),
         "fk_linear_drop": (st, [vp, i32, vp]),
         "fk_linear_fork": (st, [vp, i32, i32, vp]),
         "fk_linear_reserved_bytes": (ctypes.c_size_t, [vp]),

@@ -16,7 +16,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libfk.so")
 SOURCES = ["fk_host.cu", "fk_copy.cu", "fk_score.cu", "fk_attn.cu", "fk_quant.cu",
            "fk_paged_host.cu", "fk_paged_append.cu", "fk_paged_few.cu", "fk_paged_chunk.cu",
-           "fk_rotary.cu", "fk_linear_host.cu", "fk_linear_few.cu"]
+           "fk_rotary.cu", "fk_linear_host.cu", "fk_linear_few.cu", "fk_linear_chunk.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]

@@ -34,6 +34,45 @@ struct LinearArgs {
   LinearSeqs seqs;
 };
 
+// Chunks of kLinearChunk tokens on the tensor cores; a work item is a segment (a run of chunks) of one kv head of a sequence.
+constexpr int kLinearChunk = 128;
+struct LinearChunkSeqs {
+  int n;
+  int slot[kLinearSeqs];
+  int out[kLinearSeqs];
+  int tok0[kLinearSeqs];
+  int len[kLinearSeqs];               // at least 1
+  int segs[kLinearSeqs];              // segments of a head
+  int place0[kLinearSeqs];            // its states' places in the workspace, where segs > 1: place0 + head * segs + segment
+  int item0[kLinearSeqs + 1];         // items before the sequence's first one
+};
+struct LinearChunkArgs {
+  bf16* O;
+  const bf16* Q;                      // (the tiles come by tensor maps: for values that are not finite)
+  const bf16* K;
+  const bf16* V;
+  int64_t ostride, qstride, kstride, vstride;
+  int wide_o;                         // rows of O are 32-byte aligned
+  const float* decay;
+  int64_t dstride;
+  float scale;
+  int Hkv, G;
+  const float* state;
+  float* state_new;
+  int to_out;
+  float* place;                       // [places][D][D]: the state before a segment
+  float* place_decay;                 // [places]: what the segment before it leaves of a state
+  int* status;
+  LinearChunkSeqs seqs;
+};
+cudaError_t linear_chunk_prepare(int D);
+// With segments: first what each adds to a state that starts at zero (all but the last), then the states before each.
+cudaError_t launch_linear_chunk(int D, bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                                const LinearChunkArgs& a, cudaStream_t s);
+
+// [rows][cols] bf16, `stride` elements from row to row: tiles of 128 rows of 64 columns, 128-byte swizzle.
+bool encode_bf16_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride);
+
 // The recurrence, token by token.
 cudaError_t launch_linear_few(int D, const LinearArgs& a, cudaStream_t s);
 

@@ -18,6 +18,15 @@ struct StepSeq {
   int seq, n_new;
 };
 
+constexpr int kPlaces = 512;          // states of segments that the workspace holds
+
+// One launch of a step's plan (the same for every layer): sequences of few tokens, or in chunks.
+struct Launch {
+  bool chunk, split;
+  LinearSeqs few;
+  LinearChunkSeqs seqs;
+};
+
 // the caller's current device comes back when a call ends
 struct DeviceGuard {
   int before = -1;
@@ -39,6 +48,11 @@ struct fk_linear {
   std::vector<StepSeq> step;
   bool in_step = false;
   int64_t tokens = 0;                 // of the step
+  std::vector<Launch> plan;           // of the step's sequences that have tokens
+  int force_few = 0, force_segments = 0;
+  float* place = nullptr;             // [kPlaces][D][D], and what segments leave of a state
+  float* place_decay = nullptr;
+  int sms = 0;
   float* states = nullptr;            // [layers][max_seqs][Hkv][D][D]
   size_t per_seq = 0, per_layer = 0;  // floats
   int* status = nullptr;              // the status word, and a report of it
@@ -110,6 +124,62 @@ bool meet(const Rows& a, const Rows& b, int64_t tokens) {
   return d < low || a.stride - d < high;
 }
 
+// Tokens up to which a sequence goes through the recurrence.
+constexpr int kFewTokens = 32;
+
+int segments_of(const fk_linear* h, int chunks, int64_t items) {
+  if (h->force_segments > 0) return std::min(h->force_segments, chunks);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(chunks / 2, h->sms / items));
+}
+
+// The launches of a step: sequences of few tokens, then the others, kLinearSeqs of them to a launch.
+void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<Launch>* plan) {
+  const int upto = h->force_few > 0 ? h->force_few : kFewTokens, H = h->cfg.n_kv_heads;
+  int64_t items = 0;
+  for (const StepSeq& s : step) items += s.n_new > upto ? H : 0;
+  for (const bool chunk : {false, true}) {
+    Launch l{};
+    int64_t tok = 0;
+    int places = 0;
+    auto push = [&] {
+      if (chunk ? l.seqs.n : l.few.n) plan->push_back(l);
+      l = Launch{};
+      places = 0;
+    };
+    l.chunk = chunk;
+    for (size_t i = 0; i < step.size(); tok += step[i++].n_new) {
+      const StepSeq& s = step[i];
+      if (s.n_new == 0 || (s.n_new > upto) != chunk) continue;
+      if ((chunk ? l.seqs.n : l.few.n) == kLinearSeqs) push();
+      l.chunk = chunk;
+      if (!chunk) {
+        const int k = l.few.n++;
+        l.few.slot[k] = s.seq;
+        l.few.out[k] = (int)i;
+        l.few.tok0[k] = (int)tok;
+        l.few.len[k] = s.n_new;
+        continue;
+      }
+      const int k = l.seqs.n++;
+      int segs = segments_of(h, (s.n_new + kLinearChunk - 1) / kLinearChunk, items);
+      segs = std::min(segs, (kPlaces - places) / H);
+      if (segs < 2) segs = 1;
+      l.seqs.slot[k] = s.seq;
+      l.seqs.out[k] = (int)i;
+      l.seqs.tok0[k] = (int)tok;
+      l.seqs.len[k] = s.n_new;
+      l.seqs.segs[k] = segs;
+      l.seqs.place0[k] = places;
+      l.seqs.item0[k + 1] = l.seqs.item0[k] + segs * H;
+      if (segs > 1) {
+        places += segs * H;
+        l.split = true;
+      }
+    }
+    push();
+  }
+}
+
 }  // namespace
 
 extern "C" {
@@ -147,6 +217,12 @@ fk_status fk_linear_create(const fk_linear_config* cfg, fk_linear** out) {
     h->states = static_cast<float*>(p);
     if ((st = alloc(h.get(), 2 * sizeof(int), &p)) != FK_OK) return st;
     h->status = static_cast<int*>(p);
+    if ((st = alloc(h.get(), (size_t)kPlaces * cfg->head_dim * cfg->head_dim * sizeof(float), &p)) != FK_OK) return st;
+    h->place = static_cast<float*>(p);
+    if ((st = alloc(h.get(), kPlaces * sizeof(float), &p)) != FK_OK) return st;
+    h->place_decay = static_cast<float*>(p);
+    if (cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess) return FK_ERR_CUDA;
+    if (linear_chunk_prepare(cfg->head_dim) != cudaSuccess) return FK_ERR_CUDA;
     if (cudaDeviceSynchronize() != cudaSuccess) return FK_ERR_CUDA;
     *out = h.release();
     return FK_OK;
@@ -174,6 +250,9 @@ fk_status fk_linear_step(fk_linear* h, int n_seqs, const int32_t* seqs, const in
       total += n_new[i];
     }
     if (total * h->cfg.n_q_heads >= ((int64_t)1 << 31)) return FK_ERR_ARG;
+    std::vector<Launch> plan;
+    make_plan(h, step, &plan);
+    h->plan.swap(plan);
     h->step.swap(step);
     h->tokens = total;
     h->in_step = true;
@@ -216,44 +295,79 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
           meet(o, rows(V, v_stride, wk), h->tokens))
         return FK_ERR_ARG;
     }
-    auto a = std::make_unique<LinearArgs>();
-    a->Q = static_cast<const bf16*>(Q);
-    a->K = static_cast<const bf16*>(K);
-    a->V = static_cast<const bf16*>(V);
-    a->O = static_cast<bf16*>(O);
-    a->qstride = q_stride;
-    a->kstride = k_stride;
-    a->vstride = v_stride;
-    a->ostride = o_stride;
-    a->decay = decay;
-    a->dstride = decay_stride;
-    a->scale = scale > 0.0f ? scale : (float)(1.0 / std::sqrt((double)c.head_dim));
-    a->Hkv = c.n_kv_heads;
-    a->G = c.n_q_heads / c.n_kv_heads;
-    a->state = h->states + h->per_layer * layer;
-    a->state_new = mode == FK_LINEAR_ADVANCE ? h->states + h->per_layer * layer : state_out;
-    a->to_out = mode != FK_LINEAR_ADVANCE;
-    a->status = h->status;
-    int64_t tok = 0;
-    for (size_t i = 0; i < h->step.size();) {
-      a->seqs.n = 0;
-      for (; i < h->step.size() && a->seqs.n < kLinearSeqs; ++i) {
-        const StepSeq& s = h->step[i];
-        if (s.n_new > 0 || state_out) {
-          const int k = a->seqs.n++;
-          a->seqs.slot[k] = s.seq;
-          a->seqs.out[k] = (int)i;
-          a->seqs.tok0[k] = (int)tok;
-          a->seqs.len[k] = s.n_new;
-        }
-        tok += s.n_new;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const float sc = scale > 0.0f ? scale : (float)(1.0 / std::sqrt((double)c.head_dim));
+    const float* held = h->states + h->per_layer * layer;
+    float* state_new = mode == FK_LINEAR_ADVANCE ? h->states + h->per_layer * layer : state_out;
+    auto fill = [&](auto& a) {
+      a.Q = static_cast<const bf16*>(Q);
+      a.K = static_cast<const bf16*>(K);
+      a.V = static_cast<const bf16*>(V);
+      a.O = static_cast<bf16*>(O);
+      a.qstride = q_stride;
+      a.kstride = k_stride;
+      a.vstride = v_stride;
+      a.ostride = o_stride;
+      a.decay = decay;
+      a.dstride = decay_stride;
+      a.scale = sc;
+      a.Hkv = c.n_kv_heads;
+      a.G = c.n_q_heads / c.n_kv_heads;
+      a.state = held;
+      a.state_new = state_new;
+      a.to_out = mode != FK_LINEAR_ADVANCE;
+      a.status = h->status;
+    };
+    LinearArgs f;
+    fill(f);
+    for (const Launch& l : h->plan) {
+      if (!l.chunk) {
+        f.seqs = l.few;
+        const fk_status e = done(h, launch_linear_few(c.head_dim, f, st));
+        if (e != FK_OK) return e;
+        continue;
       }
-      if (a->seqs.n == 0) continue;
-      const fk_status st = done(h, launch_linear_few(c.head_dim, *a, static_cast<cudaStream_t>(stream)));
-      if (st != FK_OK) return st;
+      LinearChunkArgs a;
+      fill(a);
+      a.wide_o = aligned(O, 32) && o_stride % 16 == 0;
+      a.place = h->place;
+      a.place_decay = h->place_decay;
+      a.seqs = l.seqs;
+      CUtensorMap tmQ, tmK, tmV;
+      if (!encode_bf16_rows(&tmQ, Q, h->tokens, (int64_t)c.n_q_heads * c.head_dim, q_stride) ||
+          !encode_bf16_rows(&tmK, K, h->tokens, (int64_t)c.n_kv_heads * c.head_dim, k_stride) ||
+          !encode_bf16_rows(&tmV, V, h->tokens, (int64_t)c.n_kv_heads * c.head_dim, v_stride))
+        return FK_ERR_CUDA;
+      h->launches += l.split ? 2 : 0;
+      const fk_status e = done(h, launch_linear_chunk(c.head_dim, l.split, tmQ, tmK, tmV, a, st));
+      if (e != FK_OK) return e;
+    }
+    if (!state_out || !std::any_of(h->step.begin(), h->step.end(), [](const StepSeq& s) { return s.n_new == 0; })) return FK_OK;
+    // sequences without tokens: their states as they are
+    f.seqs.n = 0;
+    for (size_t i = 0; i < h->step.size(); ++i) {
+      if (h->step[i].n_new == 0) {
+        const int k = f.seqs.n++;
+        f.seqs.slot[k] = h->step[i].seq;
+        f.seqs.out[k] = (int)i;
+        f.seqs.tok0[k] = f.seqs.len[k] = 0;
+      }
+      if (f.seqs.n == kLinearSeqs || (i + 1 == h->step.size() && f.seqs.n > 0)) {
+        const fk_status e = done(h, launch_linear_few(c.head_dim, f, st));
+        if (e != FK_OK) return e;
+        f.seqs.n = 0;
+      }
     }
     return FK_OK;
   });
+}
+
+fk_status fk_linear_force_plan(fk_linear* h, int few, int segments) {
+  if (!h) return FK_ERR_ARG;
+  if (few < 0 || segments < 0) return FK_ERR_CONFIG;
+  h->force_few = few;
+  h->force_segments = segments;
+  return FK_OK;
 }
 
 fk_status fk_linear_states(const fk_linear* h, int layer, float** states) {
