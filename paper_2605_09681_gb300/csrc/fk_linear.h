@@ -52,7 +52,7 @@ struct LinearChunkArgs {
   const bf16* K;
   const bf16* V;
   int64_t ostride, qstride, kstride, vstride;
-  int wide_o;                         // rows of O are 32-byte aligned
+  float log2_scale;
   const float* decay;
   int64_t dstride;
   float scale;
@@ -68,10 +68,10 @@ struct LinearChunkArgs {
 cudaError_t linear_chunk_prepare(int D);
 // With segments: first what each adds to a state that starts at zero (all but the last), then the states before each.
 cudaError_t launch_linear_chunk(int D, bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                                const LinearChunkArgs& a, cudaStream_t s);
+                                const CUtensorMap& tmO, const LinearChunkArgs& a, cudaStream_t s);
 
-// [rows][cols] bf16, `stride` elements from row to row: tiles of 128 rows of 64 columns, 128-byte swizzle.
-bool encode_bf16_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride);
+// [rows][cols] bf16, `stride` elements from row to row: tiles of box_rows rows of 64 columns, 128-byte swizzle.
+bool encode_bf16_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows);
 
 // The recurrence, token by token.
 cudaError_t launch_linear_few(int D, const LinearArgs& a, cudaStream_t s);

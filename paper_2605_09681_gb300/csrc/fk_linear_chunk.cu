@@ -7,19 +7,23 @@
 // tensor cores run at their measured rate alone.  All exponents are of sums that are <= 0 where decays are.
 //
 // One CTA takes a segment of one kv head's chunks in turn, for all query heads that share it:
-//   warp 0        TMA: K and V of a chunk, Q of a chunk and query head, two stages each, 128-byte swizzle
-//   warp 1        tcgen05.mma, one elected lane: A = Q K^T, X = Q S, Y = P V, dS = K'^T V
-//   warp 2        the chunk's running sums G (two fp32 numbers, log2 domain) and what follows from them alone
-//   warps 4-7     K' = exp(G_C - G_j) k_j, transposed by ldmatrix into tensor memory (the A operand of dS), in three bf16 parts: the
-//                 state is kept to fp32 (two parts: 2^-17 of each term).  Half a chunk at a time.  Between the halves
-//                 P_ij = exp(G_i - G_j) A_ij for j <= i as bf16, over A's columns.
-//   warps 8-11    the state: thread r keeps row r (channel r of k) in registers, S' = exp(G_C) S + dS, and writes it as bf16 to
+//   warp 3        TMA: K and V of a chunk, Q of a chunk and query head, two stages each, 128-byte swizzle
+//   warp 1        tcgen05.mma, one elected lane: A = Q K^T, X = Q S, Y = exp(G_i) X + P V, dS = K'^T V
+//   warp 2        the chunk's running sums G (log2 domain) and what follows from them alone
+//   warp 0        whether V holds values that are not finite
+//   warps 4-11    two warpgroups.  K' = exp(G_C - G_j) k_j, transposed by ldmatrix into tensor memory (the A operand of dS), in
+//                 three bf16 parts, which is exact (two: 2^-17 of each term, and the state is kept to fp32): 32 tokens at a
+//                 time, taking turns, each into its own buffer.  Then P_ij = exp(G_i - G_j) A_ij for j <= i as bf16, 32 columns
+//                 at a time, taking turns, over the columns of A that it came from.
+//   warps 12-15   the state: thread r keeps row r (channel r of k) in registers, S' = exp(G_C) S + dS, and writes it as bf16 to
 //                 shared memory, the B operand of X
-//   warps 12-15   o: thread i reads row i of X, then of Y (the same columns), and writes its row
-// Tensor memory columns: A and P 0-127, X and Y 128.., dS 256.., K' 384-479.
+//   warps 16-19   o: thread i scales row i of X where it is, and writes row i of Y
+// Tensor memory columns: A and P 0-127, X and Y 128.., dS 256.., K' 384-479 (two buffers; kLocal: four from 0).
 //
 // kLocal: the state alone, from zero (what a segment adds), without Q and o.
 // Every wait is bounded; when one expires the CTA records it, drains its copies and products, and ends.
+// Loops over columns are rolled where registers are not indexed: the roles' code together has to stay in the instruction
+// cache (unrolled, P of a chunk took 2400 cycles, and 4800 with all SMs fetching).
 #include "fk_linear.h"
 #include "fk_tc.h"
 
@@ -27,39 +31,59 @@ namespace fk {
 namespace {
 
 constexpr int C = kLinearChunk;
-constexpr int kThreads = 512;
-constexpr uint32_t kColA = 0, kColX = 128, kColS = 256, kColK = 384;
+constexpr int kThreads = 640;
+// Registers of a thread of each warpgroup: together no more than the launch gives them (raising a count waits for registers
+// that others gave back: without an end where there are too few).
+constexpr int kRegsStart = 65536 / kThreads / 8 * 8;
+constexpr int kRegsIssue = 72, kRegsConvert = 80, kRegsState = 176, kRegsOut = 72;
+static_assert(kRegsIssue + 2 * kRegsConvert + kRegsState + kRegsOut <= kThreads / 128 * kRegsStart, "registers of the CTA");
+static_assert(kRegsIssue <= kRegsStart && kRegsConvert <= kRegsStart && kRegsOut <= kRegsStart && kRegsState >= kRegsStart, "who gives, who takes");
+constexpr uint32_t kColA = 0, kColX = 128, kColS = 256, kColK = 384;   // kLocal: K' from 0
 
+// Many of the roles' steps are a few hundred cycles long, and so are a product's way to a barrier and a warp's way from
+// one: what can share a barrier does.
 struct Barriers {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], q_empty[2];
-  uint64_t g_full[2], g_empty[2];
-  uint64_t a_full, p_full, kp_full, kp_empty, ds_full, ds_empty;
-  uint64_t s_full, s_empty, x_full, x_empty, y_full, y_empty;
+  uint64_t kv_full[3], kv_empty[3], q_full[2], q_empty[2];
+  uint64_t g_full[2], g_empty[2];     // the chunk's sums
+  uint64_t odd_full[2], odd_empty[2];
+  uint64_t kp_full[4], kp_empty[4];   // K' buffers: written, multiplied
+  uint64_t ds_full, ds_empty;         // all of dS is there, is read
+  uint64_t a_full;                    // A is there
+  uint64_t x_ready, x_full;           // S is written, the Y before it read; X is there
+  uint64_t y_ready, y_full;           // P is written, X scaled; Y is there
   uint64_t fin;
   uint32_t tmem_base;
   volatile int abort;
+  int odd[2];                         // V of the chunk holds values that are not finite
+};
+
+// What follows from the decays of a chunk alone, G in the log2 domain.
+struct alignas(16) Sums {
+  float g[C];                         // G_j
+  float u[C];                         // exp(R - G_j), R the sum at the end of j's 32 tokens; `grow`: exp(G_C - G_j)
+  float w[4];                         // exp(G_C - R) of each 32 tokens; `grow`: 1
+  float e;                            // exp(G_C)
+  int grow;                           // some g > 0: the factors could overflow where their product does not
 };
 
 template <int D>
 struct Layout {
   static constexpr int kTile = C * D * 2;         // bytes of a tile of Q, K or V: D / 64 panels of 128-byte rows
-  static constexpr int kOffK = 0, kOffV = 2 * kTile, kOffQ = 4 * kTile;
+  static constexpr int kOffQ = 4 * kTile;
   static constexpr int kOffS = 6 * kTile;         // S: D / 64 panels of D 128-byte rows
-  static constexpr int kOffG = kOffS + D * D * 2; // [2][C] G (log2), [2][C] exp(G_C - G_j)
-  static constexpr int kOffBar = kOffG + 4 * C * 4;
-  static constexpr int kUsed = kOffBar + (int)sizeof(Barriers) + 16;   // exp(G_C) of two chunks behind the barriers
+  static constexpr int kOffG = kOffS + D * D * 2;
+  static constexpr int kOffBar = kOffG + 2 * (int)sizeof(Sums);
+  static constexpr int kUsed = kOffBar + (int)sizeof(Barriers);
   // at least ~116 KB, so that one CTA occupies an SM (its 512 tensor memory columns are then free)
   static constexpr int kSmem = kUsed > 118 * 1024 ? kUsed : 118 * 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
-// 16 lanes x 32 columns of tensor memory from transposed 8 x 8 tiles (ldmatrix): register 2 b + s is lane 8 s + t / 4, column
+// 16 lanes x 16 columns of tensor memory from transposed 8 x 8 tiles (ldmatrix): register 2 b + s is lane 8 s + t / 4, column
 // 4 b + t % 4 of thread t
 __device__ __forceinline__ void tmem_st_tiles(uint32_t taddr, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-      :: "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
-      "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               :: "r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t* v) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -67,77 +91,88 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t* v) {
 }
 __device__ __forceinline__ void fence_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // Warp-uniform bounded wait for the phase of parity `parity`; false when the CTA is aborting or the limit expired (which
-// starts the abort).  (fk_tc.h's counts in 64 bits; out of line it is a call, which warps of fewer registers cannot make.)
-__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Barriers* bar, int* status) {
-  if (__all_sync(0xffffffffu, mbar_test(b, parity))) return true;
-  uint32_t t0;
-  asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t0));
-  while (true) {
+// starts the abort; the CTA records it at its end).  As short as it gets: there are thirty of them, and in C++ each took
+// 670 bytes of the instruction cache.
+__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Barriers* bar) {
+  uint32_t done;
+  asm volatile(
+      "{\n .reg .pred p, q;\n .reg .b32 t0, t;\n"
+      " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      " @p bra DONE%=;\n"
+      " mov.u32 t0, %%globaltimer_lo;\n"
+      "AGAIN%=:\n"
+      " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x4E20;\n"
+      " @p bra DONE%=;\n"
+      " mov.u32 t, %%globaltimer_lo;\n"
+      " sub.u32 t, t, t0;\n"
+      " setp.gt.u32 q, t, %4;\n"
+      " @q st.volatile.shared.u32 [%3], 1;\n"
+      " ld.volatile.shared.u32 t, [%3];\n"
+      " setp.eq.u32 q, t, 0;\n"
+      " @q bra AGAIN%=;\n"
+      "DONE%=:\n"
+      " selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(done)
+      : "r"(su32(b)), "r"(parity & 1), "r"(su32(const_cast<const int*>(&bar->abort))), "n"((uint32_t)kWaitLimitNs) : "memory");
+  return __all_sync(0xffffffffu, done);
+}
+// The same for what is to be over before the CTA ends, aborting or not.
+__device__ __forceinline__ void drain(uint64_t* b, uint32_t parity, Barriers* bar) {
+  const uint64_t t0 = now_ns();
 #pragma unroll 1
-    for (int i = 0; i < 16; ++i)
-      if (__all_sync(0xffffffffu, mbar_test(b, parity))) return true;
-    uint32_t t;
-    asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
-    bool stop = bar->abort;
-    if (t - t0 > (uint32_t)kWaitLimitNs) {
+  while (!mbar_test(b, parity))
+    if (now_ns() - t0 > kWaitLimitNs) {
       bar->abort = 1;
-      atomicOr(status, kStatusTimeout);
-      stop = true;
+      break;
     }
-    if (__any_sync(0xffffffffu, stop)) return false;
-  }
 }
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n"
+      " mul.rn.f32x2 rd, ra, rb;\n mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// 0 x + z of bf16 pairs
+__device__ __forceinline__ uint32_t zero_times(uint32_t x, uint32_t z) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(0u), "r"(z));
+  return d;
+}
+// not 0 where a bf16 pair holds an infinity or NaN: an exponent of ones
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+// x less a bf16 pair (exact where the pair is x rounded)
+__device__ __forceinline__ float2 less(float2 x, uint32_t y) {
+  float2 d;
+  asm("{\n .reg .b16 l, h, m;\n mov.b32 {l, h}, %4;\n mov.b16 m, 0xBF80;\n fma.rn.f32.bf16 %0, l, m, %2;\n fma.rn.f32.bf16 %1, h, m, %3;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "r"(y));
+  return d;
+}
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-// a sum kept as two numbers
-struct Two {
-  float h, l;
-};
-__device__ __forceinline__ Two add(Two a, Two b) {
-  const float s = a.h + b.h, v = s - a.h;
-  const float e = (a.h - (s - v)) + (b.h - v) + (a.l + b.l);
-  const float h = s + e;
-  return {h, e - (h - s)};
-}
-
-// Eight columns of a row of sum_(j <= i) P_ij v_j by themselves, in fp32: the product P V multiplies the zeros of P with
-// what later tokens of the chunk hold, and gives NaN where that is not finite.
-template <int D>
-__device__ __noinline__ void row_alone(const LinearChunkArgs& a, const float* g, int64_t tok0, int i, int head, int kvh, int col, float* y) {
-  float acc[8] = {};
-  const bf16* q = a.Q + (tok0 + i) * a.qstride + (int64_t)head * D;
-  for (int j = 0; j <= i; ++j) {
-    const bf16* k = a.K + (tok0 + j) * a.kstride + (int64_t)kvh * D;
-    float s = 0.0f;
-    for (int c = 0; c < D; ++c) s = fmaf(__bfloat162float(q[c]), __bfloat162float(k[c]), s);
-    const float p = s * exp2f(g[i] - g[j]);
-    const bf16* v = a.V + (tok0 + j) * a.vstride + (int64_t)kvh * D + col;
-    for (int c = 0; c < 8; ++c) acc[c] = fmaf(p, __bfloat162float(v[c]), acc[c]);
-  }
-  for (int c = 0; c < 8; ++c) y[c] = acc[c];
-}
 
 template <int D, bool kLocal>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ LinearChunkArgs a) {
+                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
+                    const __grid_constant__ LinearChunkArgs a) {
   using Lay = Layout<D>;
-  constexpr int kPanels = D / 64;
+  constexpr int kStages = kLocal ? 3 : 2;         // of K and V: tiles 2 b and 2 b + 1; Q: tiles 4 and 5 (kLocal: the third stage)
+  constexpr int kPanels = D / 64, kBufs = kLocal ? 4 : 2;    // K' buffers, a chunk's quarters in turn
+  constexpr uint32_t kColKp = kLocal ? 0 : kColK;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t* sK = smem + Lay::kOffK;
-  uint8_t* sV = smem + Lay::kOffV;
+  uint8_t* sK = smem;                             // (2 kTile from stage to stage)
+  uint8_t* sV = smem + Lay::kTile;
   uint8_t* sQ = smem + Lay::kOffQ;
   uint8_t* sS = smem + Lay::kOffS;
-  float* sG = reinterpret_cast<float*>(smem + Lay::kOffG);   // [2][C]
-  float* sW = sG + 2 * C;                                    // [2][C]
+  Sums* sums = reinterpret_cast<Sums*>(smem + Lay::kOffG);   // of two chunks
   Barriers* bar = reinterpret_cast<Barriers*>(smem + Lay::kOffBar);
-  volatile float* sE = reinterpret_cast<volatile float*>(smem + Lay::kOffBar + sizeof(Barriers));   // [2]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (the compiler takes what a shuffle or a vote gives for the same in all lanes: branches by it stay plain branches)
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   // ---- this CTA's segment
   int s = 0;
@@ -160,27 +195,28 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&bar->k_full[i], 1);
-      mbar_init(&bar->k_empty[i], kLocal ? 4 : 5);           // the converting warps, and Q K^T
-      mbar_init(&bar->v_full[i], 1);
-      mbar_init(&bar->v_empty[i], 1);
       mbar_init(&bar->q_full[i], 1);
-      mbar_init(&bar->q_empty[i], 1);
+      mbar_init(&bar->q_empty[i], 4);                        // O's rows, put in the tile's place, are on their way
       mbar_init(&bar->g_full[i], 1);
-      mbar_init(&bar->g_empty[i], kLocal ? 8 : 12);
+      mbar_init(&bar->g_empty[i], kLocal ? 12 : 16);
+      mbar_init(&bar->odd_full[i], 1);
+      mbar_init(&bar->odd_empty[i], 4);
     }
-    mbar_init(&bar->a_full, 1);
-    mbar_init(&bar->p_full, 4);
-    mbar_init(&bar->kp_full, 4);
-    mbar_init(&bar->kp_empty, 1);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&bar->kv_full[i], 1);
+      mbar_init(&bar->kv_empty[i], kLocal ? 1 : 2);          // the products, and the check
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&bar->kp_full[i], 4);
+      mbar_init(&bar->kp_empty[i], 1);
+    }
     mbar_init(&bar->ds_full, 1);
     mbar_init(&bar->ds_empty, 4);
-    mbar_init(&bar->s_full, 4);
-    mbar_init(&bar->s_empty, 1);
+    mbar_init(&bar->a_full, 1);
+    mbar_init(&bar->x_ready, 8);
     mbar_init(&bar->x_full, 1);
-    mbar_init(&bar->x_empty, 4);
+    mbar_init(&bar->y_ready, 12);
     mbar_init(&bar->y_full, 1);
-    mbar_init(&bar->y_empty, 4);
     mbar_init(&bar->fin, 1);
     bar->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -194,153 +230,141 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = bar->tmem_base;
-  const int wq = warp & 3, row = wq * 32 + lane;             // tensor memory lane of a thread of warps 4-15
+  // All of the tensor memory is this CTA's, so that it starts at 0: the products then take constants (with the number read
+  // from shared memory an instruction took 130 cycles to issue).
+  if (bar->tmem_base != 0) bar->abort = 1;
+  constexpr uint32_t tmem = 0;
+  const int wq = warp & 3, row = wq * 32 + lane;             // tensor memory lane of a thread of warps 4-19
   const uint32_t lanes = tmem + ((uint32_t)(wq * 32) << 16);
-  auto wait_for = [&](uint64_t* b, uint32_t parity) { return wait(b, parity, bar, a.status); };
+  auto wait_for = [&](uint64_t* b, uint32_t parity) { return wait(b, parity, bar); };
   auto arrive = [&](uint64_t* b) {                           // of a warp
     __syncwarp();
     if (lane == 0) mbar_arrive(b);
   };
 
   if (warp < 4) {
-    fewer_registers<56>();
-    if (warp == 0) {
+    fewer_registers<kRegsIssue>();
+    if (warp == 3) {
       // ------------------------------------------------------------------ TMA
       bool ok = true;
-      int ik = -1, iv = -1, iq = -1;                         // last tiles issued
-      auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int n) {
+      int ikv = -1, iq = -1;                                 // last tiles issued
+      auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int n) {   // one lane
+        for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)(tok0 + n * C));
+      };
+#pragma unroll 1
+      for (int n = 0; n < nc && ok; ++n) {
+        const int b = n % kStages, u = n / kStages;
+        if (u > 0 && !(ok = wait_for(&bar->kv_empty[b], u - 1))) break;
         if (lane == 0) {
-          mbar_expect_tx(b, Lay::kTile);
-          for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)(tok0 + n * C));
+          mbar_expect_tx(&bar->kv_full[b], 2 * Lay::kTile);
+          load(&tmK, sK + b * (2 * Lay::kTile), &bar->kv_full[b], kvh, n);
+          load(&tmV, sV + b * (2 * Lay::kTile), &bar->kv_full[b], kvh, n);
         }
         __syncwarp();
-      };
-      for (int n = 0; n < nc && ok; ++n) {
-        const int b = n & 1, u = n >> 1;
-        if (u > 0 && !(ok = wait_for(&bar->k_empty[b], (u - 1) & 1))) break;
-        load(&tmK, sK + b * Lay::kTile, &bar->k_full[b], kvh, n);
-        ik = n;
-        for (int g = 0; g < G; ++g) {
-          if (!kLocal) {
-            const int m = n * G + g, qb = m & 1, qu = m >> 1;
-            if (qu > 0 && !(ok = wait_for(&bar->q_empty[qb], (qu - 1) & 1))) break;
+        ikv = n;
+#pragma unroll 1
+        for (int g = 0; g < G && !kLocal; ++g) {
+          const int m = n * G + g, qb = m & 1, qu = m >> 1;
+          if (qu > 0 && !(ok = wait_for(&bar->q_empty[qb], qu - 1))) break;
+          if (lane == 0) {
+            mbar_expect_tx(&bar->q_full[qb], Lay::kTile);
             load(&tmQ, sQ + qb * Lay::kTile, &bar->q_full[qb], kvh * G + g, n);
-            iq = m;
           }
-          if (g == 0) {
-            if (u > 0 && !(ok = wait_for(&bar->v_empty[b], (u - 1) & 1))) break;
-            load(&tmV, sV + b * Lay::kTile, &bar->v_full[b], kvh, n);
-            iv = n;
-          }
+          __syncwarp();
+          iq = m;
         }
       }
       if (!ok) {                                             // what was issued lands before the CTA ends
-        for (int i = max(0, ik - 1); i <= ik; ++i) wait_phase(&bar->k_full[i & 1], (i >> 1) & 1, bar, a.status, false);
-        for (int i = max(0, iv - 1); i <= iv; ++i) wait_phase(&bar->v_full[i & 1], (i >> 1) & 1, bar, a.status, false);
-        for (int i = max(0, iq - 1); i <= iq; ++i) wait_phase(&bar->q_full[i & 1], (i >> 1) & 1, bar, a.status, false);
+#pragma unroll 1
+        for (int i = 0; i < kStages; ++i) {
+          if (ikv >= i) drain(&bar->kv_full[(ikv - i) % kStages], ((ikv - i) / kStages) & 1, bar);
+          if (iq >= i && i < 2) drain(&bar->q_full[(iq - i) & 1], ((iq - i) >> 1) & 1, bar);
+        }
       }
       __syncwarp();
     } else if (warp == 1) {
       // ------------------------------------------------------------------ MMA issuer
-      // Operations of one thread complete in issue order.
-      constexpr uint32_t kIdA = idesc_bf16(C, C, 0), kIdD = idesc_bf16(C, D, 1);
+      // Operations of one thread complete in issue order.  Of a chunk (one query head): the first half of dS, X, the other half,
+      // Y, the next chunk's A.  While the last two run, S' is formed from dS and the next K' are made; P and X's scaling
+      // are done while the second half of dS runs.  (X, dS, Y, A one after the other in any other order leave the tensor cores
+      // waiting for S' or for K'.)
+      constexpr uint32_t kIdA = idesc_bf16(C, C, 0), kIdD = idesc_bf16(C, D, 1), kTile16 = Lay::kTile >> 4;
       const uint64_t dQ = sdesc(su32(sQ), 16, 1024), dK = sdesc(su32(sK), 16, 1024);
-      const uint64_t dV = sdesc(su32(sV), 16384, 1024), dS = sdesc(su32(sS), D * 128, 1024);
-      bool ok = true;
+      const uint64_t dV = sdesc(su32(sV), 16384, 1024), dS = sdesc(su32(sS), 16384, 1024);
+      // K = 16 steps of an operand: rows of 128-byte panels (channels along K), or 16 rows of panels (tokens or channels of k)
+      auto along = [](int kk) { return (uint32_t)((kk >> 2) * 1024 + (kk & 3) * 2); };
       auto q_k = [&](int m, int n) {                         // A = Q K^T
+        const uint64_t x = dQ + (m & 1) * kTile16, y = dK + (n & 1) * (2 * kTile16);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = (uint32_t)((kk >> 2) * 1024 + (kk & 3) * 2);
-          umma(tmem + kColA, dQ + (uint32_t)((m & 1) * (Lay::kTile >> 4)) + off,
-               dK + (uint32_t)((n & 1) * (Lay::kTile >> 4)) + off, kIdA, kk > 0 ? 1u : 0u);
-        }
+        for (int kk = 0; kk < D / 16; ++kk) umma(kColA, x + along(kk), y + along(kk), kIdA, kk > 0 ? 1u : 0u);
         umma_commit(&bar->a_full);
       };
-      auto ds = [&](int n, int half) {                       // dS += K'^T V of 64 tokens
-        const uint64_t db = dV + (uint32_t)((n & 1) * (Lay::kTile >> 4)) + (uint32_t)(half * 4 * 128);
-#pragma unroll
-        for (int part = 0; part < 3; ++part)
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            umma_ts(tmem + kColS, tmem + kColK + part * 32 + kk * 8, db + kk * 128, kIdD, half + part + kk > 0 ? 1u : 0u);
-        umma_commit(&bar->kp_empty);
-      };
-      if (!kLocal) {
-        ok = wait_for(&bar->k_full[0], 0) && wait_for(&bar->q_full[0], 0);
-        if (ok) {
+      auto half_ds = [&](int n, int q0) {                    // dS += K'^T V of 64 tokens
+#pragma unroll 1
+        for (int q = q0; q < q0 + 2; ++q) {
+          if (!wait_for(&bar->kp_full[q % kBufs], n * (4 / kBufs) + q / kBufs)) return false;
           tc_fence_after();
           if (elect_one()) {
-            q_k(0, 0);
-            if (G == 1) umma_commit(&bar->k_empty[0]);
+            const uint64_t y = dV + (uint32_t)(n % kStages * (2 * kTile16) + q * 256);
+            const uint32_t kp = kColKp + (q % kBufs) * 48;
+#pragma unroll
+            for (int i = 0; i < 6; ++i)                      // part, 16 tokens
+              umma_ts(kColS, kp + i * 8, y + (i & 1) * 128, kIdD, q + i > 0 ? 1u : 0u);
+            umma_commit(&bar->kp_empty[q % kBufs]);
+            if (q == 3) umma_commit(&bar->ds_full);
+            if (q == 3 && kLocal) umma_commit(&bar->kv_empty[n % kStages]);
           }
           __syncwarp();
         }
+        return true;
+      };
+      bool ok = wait_for(&bar->kv_full[0], 0);
+      if (!kLocal && ok && (ok = wait_for(&bar->q_full[0], 0))) {
+        tc_fence_after();
+        if (elect_one()) q_k(0, 0);
+        __syncwarp();
       }
+#pragma unroll 1
       for (int n = 0; n < nc && ok; ++n) {
-        const int b = n & 1, u = n >> 1;
-        for (int g = 0; g < G && ok; ++g) {
+        if (kLocal && n > 0 && !(ok = wait_for(&bar->kv_full[n % kStages], n / kStages))) break;
+        if (n > 0 && !(ok = wait_for(&bar->ds_empty, n - 1))) break;
+        if (!(ok = half_ds(n, 0))) break;
+        if (kLocal) ok = half_ds(n, 2);
+#pragma unroll 1
+        for (int g = 0; g < G && !kLocal; ++g) {
           const int m = n * G + g;
-          if (!kLocal) {                                     // X = Q S
-            if (g == 0 && !(ok = wait_for(&bar->s_full, n & 1))) break;
-            if (m > 0 && !(ok = wait_for(&bar->y_empty, (m - 1) & 1))) break;
-            tc_fence_after();
-            if (elect_one()) {
-              const uint64_t da = dQ + (uint32_t)((m & 1) * (Lay::kTile >> 4));
+          if (!(ok = wait_for(&bar->x_ready, m))) break;
+          tc_fence_after();
+          if (elect_one()) {                                 // X = Q S
+            const uint64_t x = dQ + (m & 1) * kTile16;
 #pragma unroll
-              for (int kk = 0; kk < D / 16; ++kk)
-                umma(tmem + kColX, da + (uint32_t)((kk >> 2) * 1024 + (kk & 3) * 2), dS + kk * 128, kIdD, kk > 0 ? 1u : 0u);
-              umma_commit(&bar->x_full);
-              umma_commit(&bar->q_empty[m & 1]);
-              if (g == G - 1) umma_commit(&bar->s_empty);
-            }
-            __syncwarp();
+            for (int kk = 0; kk < D / 16; ++kk) umma(kColX, x + along(kk), dS + kk * 128, kIdD, kk > 0 ? 1u : 0u);
+            umma_commit(&bar->x_full);
           }
-          if (g == 0) {
-            if (!(ok = wait_for(&bar->kp_full, 0) && wait_for(&bar->v_full[b], u & 1))) break;
-            if (n > 0 && !(ok = wait_for(&bar->ds_empty, (n - 1) & 1))) break;
-            tc_fence_after();
-            if (elect_one()) ds(n, 0);
-            __syncwarp();
-          }
-          if (!kLocal) {                                     // Y = P V, and the next A
-            if (!(ok = wait_for(&bar->p_full, m & 1) && wait_for(&bar->x_empty, m & 1))) break;
-            tc_fence_after();
-            if (elect_one()) {
-              const uint64_t db = dV + (uint32_t)(b * (Lay::kTile >> 4));
+          __syncwarp();
+          if (g == 0 && !(ok = half_ds(n, 2))) break;
+          if (!(ok = wait_for(&bar->y_ready, m))) break;
+          tc_fence_after();
+          if (elect_one()) {                                 // Y = exp(G_i) X + P V
+            const uint64_t y = dV + (uint32_t)((n & 1) * (2 * kTile16));
 #pragma unroll
-              for (int kk = 0; kk < C / 16; ++kk)
-                umma_ts(tmem + kColX, tmem + kColA + kk * 8, db + kk * 128, kIdD, kk > 0 ? 1u : 0u);
-              umma_commit(&bar->y_full);
-              if (G > 1 && g == G - 1) umma_commit(&bar->v_empty[b]);
-            }
-            __syncwarp();
-            if (m + 1 < nc * G) {
-              const int n1 = g + 1 < G ? n : n + 1;
-              if (n1 > n && !(ok = wait_for(&bar->k_full[n1 & 1], (n1 >> 1) & 1))) break;
-              if (!(ok = wait_for(&bar->q_full[(m + 1) & 1], ((m + 1) >> 1) & 1))) break;
-              tc_fence_after();
-              if (elect_one()) {
-                q_k(m + 1, n1);
-                if ((m + 1) % G == G - 1) umma_commit(&bar->k_empty[n1 & 1]);
-              }
-              __syncwarp();
-            }
+            for (int kk = 0; kk < C / 16; ++kk) umma_ts(kColX, kColA + (kk >> 1) * 32 + (kk & 1) * 8, y + kk * 128, kIdD, 1u);
+            umma_commit(&bar->y_full);
+            if (g == G - 1) umma_commit(&bar->kv_empty[n & 1]);
           }
-          if (g == 0) {
-            if (!(ok = wait_for(&bar->kp_full, 1))) break;
+          __syncwarp();
+          if (m + 1 < nc * G) {                              // the next A
+            const int n1 = g + 1 < G ? n : n + 1;
+            if (n1 > n && !(ok = wait_for(&bar->kv_full[n1 & 1], n1 >> 1))) break;
+            if (!(ok = wait_for(&bar->q_full[(m + 1) & 1], (m + 1) >> 1))) break;
             tc_fence_after();
-            if (elect_one()) {
-              ds(n, 1);
-              umma_commit(&bar->ds_full);
-              if (G == 1) umma_commit(&bar->v_empty[b]);
-            }
+            if (elect_one()) q_k(m + 1, n1);
             __syncwarp();
           }
         }
       }
       if (elect_one()) umma_commit(&bar->fin);               // completes once every product above is done
-      wait_phase(&bar->fin, 0, bar, a.status, false);
+      drain(&bar->fin, 0, bar);
       __syncwarp();
     } else if (warp == 2) {
       // ------------------------------------------------------------------ running sums of a chunk: lane's tokens 4 lane .. + 3
@@ -356,147 +380,191 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       fetch(0);
       for (int n = 0; n < nc; ++n) {
         const int b = n & 1, u = n >> 1;
-        Two sum[4];
+        // (in fp64: a dozen additions a chunk, and the sums' differences keep fp32's relative precision however far they run)
+        double sum[4];
+        bool grows = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float y = at_least(x[i], kLeastDecay);
-          const float h = y * 1.4426950408889634f;           // log2(e) in two numbers
-          const Two z{h, fmaf(y, 1.4426950408889634f, -h) + y * 1.925963033500e-8f};
-          sum[i] = i == 0 ? z : add(sum[i - 1], z);
+          grows |= !(y <= 0.0f);
+          sum[i] = (i == 0 ? 0.0 : sum[i - 1]) + (double)y * 1.4426950408889634;
         }
-        Two all = sum[3];
+        double all = sum[3];
+#pragma unroll 1
         for (int o = 1; o < 32; o *= 2) {
-          const Two z{__shfl_up_sync(0xffffffffu, all.h, o), __shfl_up_sync(0xffffffffu, all.l, o)};
-          if (lane >= o) all = add(z, all);
+          const double z = __shfl_up_sync(0xffffffffu, all, o);
+          if (lane >= o) all += z;
         }
-        const Two before{__shfl_up_sync(0xffffffffu, all.h, 1), __shfl_up_sync(0xffffffffu, all.l, 1)};
-        const Two end{__shfl_sync(0xffffffffu, all.h, 31), __shfl_sync(0xffffffffu, all.l, 31)};
+        const double before = __shfl_up_sync(0xffffffffu, all, 1), end = __shfl_sync(0xffffffffu, all, 31);
         if (n + 1 < nc) fetch(n + 1);
-        if (u > 0 && !wait_for(&bar->g_empty[b], (u - 1) & 1)) break;
-        float w[4];
+        // the sum at the end of this lane's 32 tokens, unless the chunk grows
+        const double r = __shfl_sync(0xffffffffu, all, lane | 7);
+        const bool grow = __any_sync(0xffffffffu, grows);
+        const double from = grow ? end : r;
+        float v[4], gg[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (lane > 0) sum[i] = add(before, sum[i]);
-          w[i] = n * C + 4 * lane + i < tokens ? exp2f((end.h - sum[i].h) + (end.l - sum[i].l)) : 0.0f;
+          if (lane > 0) sum[i] += before;
+          gg[i] = (float)sum[i];
+          v[i] = exp2f((float)(from - sum[i]));
         }
-        *reinterpret_cast<float4*>(sG + b * C + 4 * lane) = make_float4(sum[0].h, sum[1].h, sum[2].h, sum[3].h);
-        *reinterpret_cast<float4*>(sW + b * C + 4 * lane) = make_float4(w[0], w[1], w[2], w[3]);
-        if (lane == 0) sE[b] = exp2f(end.h + end.l);
+        if (u > 0 && !wait_for(&bar->g_empty[b], u - 1)) break;
+        Sums& out = sums[b];
+        *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(gg[0], gg[1], gg[2], gg[3]);
+        *reinterpret_cast<float4*>(out.u + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
+        if ((lane & 7) == 7) out.w[lane >> 3] = grow ? 1.0f : exp2f((float)(end - r));
+        if (lane == 0) {
+          out.e = exp2f((float)end);
+          out.grow = grow;
+        }
         arrive(&bar->g_full[b]);
       }
-    }
-  } else if (warp < 8) {
-    fewer_registers<120>();
-    // ------------------------------------------------------------------ K' and P
-    // K' of 64 tokens: channels 32 wq .. + 31 of this warp, 16 at a time
-    auto convert = [&](int n, int half, int valid) {
-      const uint32_t tile = su32(sK) + (uint32_t)((n & 1) * Lay::kTile);
-      const float* w = sW + (n & 1) * C + half * 64 + 2 * (lane & 3);
-      const int r = lane & 7, mat = lane >> 3;
-#pragma unroll 1
-      for (int hf = 0; hf < 2; ++hf) {
-        const int c = 32 * wq + 16 * hf + (mat & 1) * 8;     // channel of the row that this lane gives ldmatrix
-        const uint32_t at = tile + (uint32_t)((c >> 6) * (C * 128) + (half * 64 + (mat >> 1) * 8 + r) * 128 + ((((c & 63) >> 3) ^ r) << 4));
-        uint32_t x[16], hi[16], mid[16], lo[16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ldmatrix4t(at + i * (16 * 128), x + 4 * i);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int t = 8 * (i >> 1);                        // token of the pair, less 2 (lane & 3)
-          const float2 ww = *reinterpret_cast<const float2*>(w + t);
-          uint32_t v = x[i];
-          if (valid < C) {                                   // (tokens of others: any values)
-            const int j = half * 64 + t + 2 * (lane & 3);
-            v = j + 1 < valid ? v : j < valid ? v & 0xFFFFu : 0u;
-          }
-          float p = low(v) * ww.x, q = high(v) * ww.y;
-          hi[i] = pack_bf16(p, q);
-          p -= low(hi[i]);
-          q -= high(hi[i]);
-          mid[i] = pack_bf16(p, q);
-          p -= low(mid[i]);
-          q -= high(mid[i]);
-          lo[i] = pack_bf16(p, q);
+    } else if (!kLocal) {
+      // ------------------------------------------------------------------ is V finite
+      for (int n = 0; n < nc; ++n) {
+        const int b = n & 1, u = n >> 1, valid = min(C, tokens - n * C);
+        if (!wait_for(&bar->kv_full[b], u)) break;
+        // 0 times a value is NaN where it is not finite; 8 runs of 16 bytes to a row of a panel
+        uint32_t z[4] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int i = lane; i < Lay::kTile / 16; i += 32) {
+          uint4 v = *reinterpret_cast<const uint4*>(sV + b * (2 * Lay::kTile) + i * 16);
+          if (valid < C && (i >> 3) % C >= valid) v = make_uint4(0, 0, 0, 0);
+          z[0] = zero_times(v.x, z[0]);
+          z[1] = zero_times(v.y, z[1]);
+          z[2] = zero_times(v.z, z[2]);
+          z[3] = zero_times(v.w, z[3]);
         }
-        const uint32_t to = lanes + kColK + ((uint32_t)(16 * hf) << 16);
-        tmem_st_tiles(to, hi);
-        tmem_st_tiles(to + 32, mid);
-        tmem_st_tiles(to + 64, lo);
+        if (u > 0 && !wait_for(&bar->odd_empty[b], u - 1)) break;
+        const bool odd = __any_sync(0xffffffffu, ((z[0] | z[1] | z[2] | z[3]) & 0x7FFF7FFFu) != 0);
+        if (lane == 0) bar->odd[b] = (int)odd;
+        arrive(&bar->odd_full[b]);
+        arrive(&bar->kv_empty[b]);
       }
-      tmem_wait_st();
-      tc_fence_before();
-      arrive(&bar->kp_full);
-    };
-    for (int n = 0; n < nc; ++n) {
+    }
+  } else if (warp < 12) {
+    fewer_registers<kRegsConvert>();
+    // ------------------------------------------------------------------ K' and P
+    const int w2 = (warp >> 2) - 1;                          // which of the two warpgroups
+    const bool mine = 32 * wq < D;                           // D = 64: lanes 64-127 of dS are not used
+    bool ok = true;
+    for (int n = 0; n < nc && ok; ++n) {
       const int b = n & 1, u = n >> 1, valid = min(C, tokens - n * C);
-      if (!wait_for(&bar->k_full[b], u & 1) || !wait_for(&bar->g_full[b], u & 1)) break;
-      if (n > 0 && !wait_for(&bar->kp_empty, 1)) break;      // the chunk before's second half
-      tc_fence_after();
+      const Sums& sm = sums[b];
+      const int bk = n % kStages;                            // stage of K and V
+      if (!(ok = wait_for(&bar->kv_full[bk], n / kStages) && wait_for(&bar->g_full[b], u))) break;
       if (valid < C) {                                       // rows of others: zeros for the products with V
-        if (!wait_for(&bar->v_full[b], u & 1)) break;
-        if (row >= valid) {
-#pragma unroll
-          for (int p = 0; p < kPanels; ++p)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              *reinterpret_cast<uint4*>(sV + b * Lay::kTile + p * (C * 128) + row * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+        const int p = wq >> 1, r = 64 * (wq & 1) + 32 * w2 + lane;   // panel, token of this warpgroup's
+        if (r >= valid && p < kPanels) {
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(sV + bk * (2 * Lay::kTile) + p * (C * 128) + r * 128 + i * 16) = make_uint4(0, 0, 0, 0);
         }
         fence_to_async();
       }
-      const bool mine = 32 * wq < D;                         // D = 64: lanes 64-127 of dS are not used
-      if (mine) convert(n, 0, valid);
-      else arrive(&bar->kp_full);
-      bool ok = true;
-      for (int g = 0; g < G && ok; ++g) {
-        if (!kLocal) {
-          const int m = n * G + g;
-          if (!(ok = wait_for(&bar->a_full, m & 1))) break;
+      const float gi = kLocal ? 0.0f : sm.g[row] + a.log2_scale;
+      const bool grow = !kLocal && __any_sync(0xffffffffu, sm.grow);
+      // K' of this warpgroup's two quarters, then P of each query head
+#pragma unroll 1
+      for (int step = 0; step < (kLocal ? 2 : G + 2) && ok; ++step) {
+        if (step < 2) {
+          const int q = w2 + 2 * step, buf = q % kBufs, use = n * (4 / kBufs) + q / kBufs;
+          if (use > 0 && !(ok = wait_for(&bar->kp_empty[buf], use - 1))) break;
           tc_fence_after();
-          const float gi = sG[b * C + row];
-          const float4* gj = reinterpret_cast<const float4*>(sG + b * C);
+          if (mine) {
+            // channels 32 wq .. + 31 of this warp, 16 at a time
+            const int t0 = 32 * q + 2 * (lane & 3);          // first token of this thread's pairs, 8 apart
+            float2 w[4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t p[16];
-            if (q <= wq) {
-              uint32_t x[32];
-              FK_TMEM_LD32(lanes + kColA + 32 * q, x);
+            for (int k = 0; k < 4; ++k) w[k] = fmul2(*reinterpret_cast<const float2*>(sm.u + t0 + 8 * k), make_float2(sm.w[q], sm.w[q]));
+            const int r = lane & 7, mat = lane >> 3;
+#pragma unroll 1
+            for (int hf = 0; hf < 2; ++hf) {
+              const int c = 32 * wq + 16 * hf + (mat & 1) * 8;   // channel of the row that this lane gives ldmatrix
+              const uint32_t at = su32(sK) + (uint32_t)(bk * (2 * Lay::kTile) + (c >> 6) * (C * 128) + (32 * q + (mat >> 1) * 8 + r) * 128 +
+                                                        ((((c & 63) >> 3) ^ r) << 4));
+              uint32_t x[8], hi[8], mid[8], lo[8];
+              ldmatrix4t(at, x);
+              ldmatrix4t(at + 16 * 128, x + 4);
+              if (valid < C) {                               // (tokens of others: any values)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const int j = t0 + 8 * (k >> 1);
+                  x[k] = j + 1 < valid ? x[k] : j < valid ? x[k] & 0xFFFFu : 0u;
+                }
+              }
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                float2 p = fmul2(make_float2(low(x[k]), high(x[k])), w[k >> 1]);
+                hi[k] = pack_bf16(p.x, p.y);
+                p = less(p, hi[k]);
+                mid[k] = pack_bf16(p.x, p.y);
+                p = less(p, mid[k]);
+                lo[k] = pack_bf16(p.x, p.y);
+              }
+              const uint32_t to = lanes + kColKp + buf * 48 + ((uint32_t)(16 * hf) << 16);
+              tmem_st_tiles(to, hi);
+              tmem_st_tiles(to + 16, mid);
+              tmem_st_tiles(to + 32, lo);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+          }
+          arrive(&bar->kp_full[buf]);
+          continue;
+        }
+        if (!(ok = wait_for(&bar->a_full, n * G + step - 2))) break;
+        tc_fence_after();
+        // below the diagonal A f u_j with f of the row, on it A exp(G_i - G_j), scaled
+#pragma unroll 1
+        for (int q = w2; q < 4; q += 2) {
+          uint32_t x[32];
+          if (q > wq) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = 0;
+          } else {
+            FK_TMEM_LD32(lanes + kColA + 32 * q, x);
+            if (q == wq || grow) {
+              const float4* y = reinterpret_cast<const float4*>(sm.g + 32 * q);
               FK_TMEM_WAIT_LD32(x);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                const float4 y = gj[8 * q + i];
-                const float yy[4] = {y.x, y.y, y.z, y.w};
+                const float4 v = y[i];
+                const float vv[4] = {v.x, v.y, v.z, v.w};
                 float e[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                  e[c] = __uint_as_float(x[4 * i + c]) * fast_exp2(gi - yy[c]);
+                  e[c] = __uint_as_float(x[4 * i + c]) * fast_exp2(gi - vv[c]);
                   if (q == wq && 4 * i + c > lane) e[c] = 0.0f;
                 }
-                p[2 * i] = pack_bf16(e[0], e[1]);
-                p[2 * i + 1] = pack_bf16(e[2], e[3]);
+                x[2 * i] = pack_bf16(e[0], e[1]);
+                x[2 * i + 1] = pack_bf16(e[2], e[3]);
               }
             } else {
+              const float4* y = reinterpret_cast<const float4*>(sm.u + 32 * q);
+              const float f1 = fast_exp2(gi - sm.g[32 * q + 31]);
+              const float2 f = make_float2(f1, f1);
+              FK_TMEM_WAIT_LD32(x);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) p[i] = 0;
+              for (int i = 0; i < 8; ++i) {
+                const float4 v = y[i];
+                const float2 s0 = fmul2(fmul2(make_float2(__uint_as_float(x[4 * i]), __uint_as_float(x[4 * i + 1])), make_float2(v.x, v.y)), f);
+                const float2 s1 = fmul2(fmul2(make_float2(__uint_as_float(x[4 * i + 2]), __uint_as_float(x[4 * i + 3])), make_float2(v.z, v.w)), f);
+                x[2 * i] = pack_bf16(s0.x, s0.y);
+                x[2 * i + 1] = pack_bf16(s1.x, s1.y);
+              }
             }
-            FK_TMEM_ST16(lanes + kColA + 16 * q, p);
           }
-          tmem_wait_st();
-          tc_fence_before();
-          arrive(&bar->p_full);
+          FK_TMEM_ST16(lanes + kColA + 32 * q, x);
         }
-        if (g == 0) {
-          if (!(ok = wait_for(&bar->kp_empty, 0))) break;
-          tc_fence_after();
-          if (mine) convert(n, 1, valid);
-          else arrive(&bar->kp_full);
-          arrive(&bar->k_empty[b]);
-        }
+        tmem_wait_st();
+        tc_fence_before();
+        arrive(&bar->y_ready);
       }
-      if (!ok) break;
-      arrive(&bar->g_empty[b]);
+      if (ok) arrive(&bar->g_empty[b]);
     }
-  } else if (warp < 12) {
-    more_registers<168>();
+  } else if (warp < 16) {
+    more_registers<kRegsState>();
     // ------------------------------------------------------------------ the state
     const bool mine = 32 * wq < D;
     float st[D];
@@ -512,40 +580,59 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         st[i] = v.x, st[i + 1] = v.y, st[i + 2] = v.z, st[i + 3] = v.w;
       }
     }
+    // State n is formed from dS of chunk n - 1 and written, 32 columns at a time.
     bool ok = true;
-    for (int n = 0; n < nc; ++n) {
-      const int b = n & 1, u = n >> 1;
-      if (!kLocal) {
-        if (n > 0 && !(ok = wait_for(&bar->s_empty, (n - 1) & 1))) break;
-        if (mine) {
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            const uint4 v = make_uint4(pack_bf16(st[8 * i], st[8 * i + 1]), pack_bf16(st[8 * i + 2], st[8 * i + 3]),
-                                       pack_bf16(st[8 * i + 4], st[8 * i + 5]), pack_bf16(st[8 * i + 6], st[8 * i + 7]));
-            *reinterpret_cast<uint4*>(sS + (i >> 3) * (D * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = v;
-          }
-          fence_to_async();
+#pragma unroll 1
+    for (int n = 0; n <= nc; ++n) {
+      float e = 1.0f;
+      if (n > 0) {
+        const int b = (n - 1) & 1;
+        if (!(ok = wait_for(&bar->g_full[b], (n - 1) >> 1))) break;
+        e = sums[b].e;
+        arrive(&bar->g_empty[b]);
+        left *= e;
+        // every X of the chunk (each phase is seen): S's place is free, and further query heads' X may follow
+#pragma unroll 1
+        for (int g = 0; g < G && !kLocal && ok; ++g) {
+          if (g > 0) arrive(&bar->x_ready);
+          ok = wait_for(&bar->x_full, (n - 1) * G + g);
         }
-        arrive(&bar->s_full);
+        if (!ok || !(ok = wait_for(&bar->ds_full, n - 1))) break;
+        tc_fence_after();
       }
-      if (!(ok = wait_for(&bar->g_full[b], u & 1))) break;
-      const float e = sE[b];
-      arrive(&bar->g_empty[b]);
-      left *= e;
-      if (!(ok = wait_for(&bar->ds_full, n & 1))) break;
-      tc_fence_after();
       if (mine) {
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
-          uint32_t x[32];
-          FK_TMEM_LD32(lanes + kColS + 32 * q, x);
-          FK_TMEM_WAIT_LD32(x);
+          if (n > 0) {
+            uint32_t x[32];
+            FK_TMEM_LD32(lanes + kColS + 32 * q, x);
+            FK_TMEM_WAIT_LD32(x);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) st[32 * q + i] = fmaf(st[32 * q + i], e, __uint_as_float(x[i]));
+            for (int i = 0; i < 32; i += 2) {
+              const float2 y = ffma2(make_float2(st[32 * q + i], st[32 * q + i + 1]), make_float2(e, e),
+                                     make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+              st[32 * q + i] = y.x;
+              st[32 * q + i + 1] = y.y;
+            }
+          }
+          if (!kLocal) {
+#pragma unroll
+            for (int i = 4 * q; i < 4 * q + 4; ++i) {
+              const uint4 v = make_uint4(pack_bf16(st[8 * i], st[8 * i + 1]), pack_bf16(st[8 * i + 2], st[8 * i + 3]),
+                                         pack_bf16(st[8 * i + 4], st[8 * i + 5]), pack_bf16(st[8 * i + 6], st[8 * i + 7]));
+              *reinterpret_cast<uint4*>(sS + (i >> 3) * (D * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = v;
+            }
+          }
         }
       }
-      tc_fence_before();
-      arrive(&bar->ds_empty);
+      if (n > 0) {
+        tc_fence_before();
+        arrive(&bar->ds_empty);
+      }
+      if (!kLocal && n < nc) {
+        fence_to_async();
+        arrive(&bar->x_ready);
+      }
     }
     float* to = nullptr;
     if (kLocal) to = a.place + (place + 1) * (D * D);
@@ -557,84 +644,151 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       if (kLocal && row == 0) a.place_decay[place + 1] = left;
     }
   } else {
-    more_registers<168>();
+    fewer_registers<kRegsOut>();
     // ------------------------------------------------------------------ o
-    bool ok = !kLocal;
+    bool ok = !kLocal, any_odd = false;
+    if (!kLocal) arrive(&bar->x_ready);                      // no Y before the first X
+#pragma unroll 1
     for (int n = 0; n < nc && ok; ++n) {
       const int b = n & 1, u = n >> 1, t = n * C + row;
-      if (!(ok = wait_for(&bar->g_full[b], u & 1))) break;
-      const float e = a.scale * exp2f(sG[b * C + row]);
+      if (!(ok = wait_for(&bar->g_full[b], u) && wait_for(&bar->odd_full[b], u))) break;
+      const float e = exp2f(sums[b].g[row] + a.log2_scale);
+      const bool odd = __any_sync(0xffffffffu, bar->odd[b]);
       for (int g = 0; g < G; ++g) {
-        const int m = n * G + g;
-        float o[D];
-        if (!(ok = wait_for(&bar->x_full, m & 1))) break;
+        const int m = n * G + g, head = kvh * G + g;
+        bf16* to = a.O + (tok0 + t) * a.ostride + (int64_t)head * D;
+        if (!(ok = wait_for(&bar->x_full, m))) break;
         tc_fence_after();
+        if (!odd) {
+#pragma unroll 1
+          for (int q = 0; q < D / 32; ++q) {
+            uint32_t x[32];
+            FK_TMEM_LD32(lanes + kColX + 32 * q, x);
+            FK_TMEM_WAIT_LD32(x);
 #pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
-          uint32_t x[32];
-          FK_TMEM_LD32(lanes + kColX + 32 * q, x);
-          FK_TMEM_WAIT_LD32(x);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[32 * q + i] = e * __uint_as_float(x[i]);
+            for (int i = 0; i < 32; i += 2) {
+              const float2 y = fmul2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), make_float2(e, e));
+              x[i] = __float_as_uint(y.x);
+              x[i + 1] = __float_as_uint(y.y);
+            }
+            FK_TMEM_ST32(lanes + kColX + 32 * q, x);
+          }
+          tmem_wait_st();
+        } else {
+          // P V multiplies the zeros of P with what later tokens hold, and gives NaN where that is not finite: X alone is
+          // written, and the rest of o added to it at the end, token by token.
+          any_odd = true;
+#pragma unroll 1
+          for (int q = 0; q < D / 8; ++q) {
+            float x[8];
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                         : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+                         : "r"(lanes + kColX + 8 * q));
+            asm volatile("tcgen05.wait::ld.sync.aligned;"
+                         : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]) :: "memory");
+            if (t < tokens)
+              *reinterpret_cast<uint4*>(to + 8 * q) = make_uint4(pack_bf16(e * x[0], e * x[1]), pack_bf16(e * x[2], e * x[3]),
+                                                                 pack_bf16(e * x[4], e * x[5]), pack_bf16(e * x[6], e * x[7]));
+          }
+          __syncwarp();
         }
         tc_fence_before();
-        arrive(&bar->x_empty);
-        if (!(ok = wait_for(&bar->y_full, m & 1))) break;
+        arrive(&bar->y_ready);
+        if (!(ok = wait_for(&bar->y_full, m))) break;
         tc_fence_after();
-        bf16* to = a.O + (tok0 + t) * a.ostride + (int64_t)(kvh * G + g) * D;
-#pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
+        const bool whole = n * C + 32 * wq + 32 <= tokens;   // all rows of this warp
+        uint8_t* tile = sQ + (m & 1) * Lay::kTile;
+#pragma unroll 1
+        for (int q = 0; q < D / 32 && !odd; ++q) {
           uint32_t y[32];
           FK_TMEM_LD32(lanes + kColX + 32 * q, y);
           FK_TMEM_WAIT_LD32(y);
-          if (q == D / 32 - 1) {                             // the last of Y is read
-            tc_fence_before();
-            arrive(&bar->y_empty);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y[i] = pack_bf16(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1]));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int c = 4 * q + i;                         // run of 16 bytes
+            *reinterpret_cast<uint4*>(tile + (c >> 3) * (C * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+                make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
           }
-          float z = 0.0f;                                    // NaN if any of Y is not finite
+        }
+        tc_fence_before();
+        arrive(&bar->x_ready);
+        if (whole && !odd) {
+          fence_to_async();
+          __syncwarp();
+          if (lane == 0) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) z = fmaf(__uint_as_float(y[i]), 0.0f, z);
-          if (z != z && t < tokens) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              float x = 0.0f, f[8];
-#pragma unroll
-              for (int c = 0; c < 8; ++c) x = fmaf(__uint_as_float(y[i + c]), 0.0f, x);
-              if (x == x) continue;
-              row_alone<D>(a, sG + b * C, tok0 + n * C, row, kvh * G + g, kvh, 32 * q + i, f);
-#pragma unroll
-              for (int c = 0; c < 8; ++c) y[i + c] = __float_as_uint(f[c]);
-            }
+            for (int p = 0; p < kPanels; ++p)
+              asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+                           :: "l"(&tmO), "r"(su32(tile + p * (C * 128) + wq * (32 * 128))), "r"(head * D + p * 64),
+                           "r"((int)(tok0 + n * C) + 32 * wq) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
           }
-          uint32_t v[16];
+        }
+        if (!whole && !odd && t < tokens) {                  // (the last chunk's last rows)
+#pragma unroll 1
+          for (int c = 0; c < D / 8; ++c)
+            *reinterpret_cast<uint4*>(to + 8 * c) =
+                *reinterpret_cast<const uint4*>(tile + (c >> 3) * (C * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+        }
+        arrive(&bar->q_empty[m & 1]);
+      }
+      if (!ok) break;
+      arrive(&bar->odd_empty[b]);
+      arrive(&bar->g_empty[b]);
+    }
+    if (!kLocal && any_odd) {
+      // o's terms of a chunk's own tokens, where V of the chunk is not all finite, in fp32 (a millisecond a chunk: this is for
+      // inputs that went wrong)
+#pragma unroll 1
+      for (int n = 0; n < nc; ++n) {
+        const int t = n * C + row, valid = min(C, tokens - n * C);
+        bool odd = false;
+        uint32_t tile_odd;
+        for (int i = row; i < valid * (D / 8); i += 128) {
+          const uint4 v = *reinterpret_cast<const uint4*>(a.V + (tok0 + n * C + i / (D / 8)) * a.vstride + (int64_t)kvh * D + i % (D / 8) * 8);
+          odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+        }
+        asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
+                     : "=r"(tile_odd) : "r"((uint32_t)odd) : "memory");
+        if (!tile_odd || t >= tokens) continue;
+#pragma unroll 1
+        for (int g = 0; g < G; ++g) {
+          const bf16* q = a.Q + (tok0 + t) * a.qstride + (int64_t)(kvh * G + g) * D;
+          bf16* to = a.O + (tok0 + t) * a.ostride + (int64_t)(kvh * G + g) * D;
+#pragma unroll 1
+          for (int c = 0; c < D; c += 8) {
+            float o[8], d = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            v[i] = pack_bf16(fmaf(a.scale, __uint_as_float(y[2 * i]), o[32 * q + 2 * i]),
-                             fmaf(a.scale, __uint_as_float(y[2 * i + 1]), o[32 * q + 2 * i + 1]));
-          if (t < tokens) {
-            if (a.wide_o) {
+            for (int i = 0; i < 8; ++i) o[i] = __bfloat162float(to[c + i]);
+#pragma unroll 1
+            for (int j = row; j >= 0; --j) {
+              const bf16* k = a.K + (tok0 + n * C + j) * a.kstride + (int64_t)kvh * D;
+              const bf16* v = a.V + (tok0 + n * C + j) * a.vstride + (int64_t)kvh * D + c;
+              float p = 0.0f;
+#pragma unroll 1
+              for (int i = 0; i < D; ++i) p = fmaf(__bfloat162float(q[i]), __bfloat162float(k[i]), p);
+              p *= a.scale * expf(d);
 #pragma unroll
-              for (int i = 0; i < 2; ++i)
-                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                             :: "l"(to + 32 * q + 16 * i), "r"(v[8 * i]), "r"(v[8 * i + 1]), "r"(v[8 * i + 2]), "r"(v[8 * i + 3]),
-                             "r"(v[8 * i + 4]), "r"(v[8 * i + 5]), "r"(v[8 * i + 6]), "r"(v[8 * i + 7]) : "memory");
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<uint4*>(to + 32 * q + 8 * i) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+              for (int i = 0; i < 8; ++i) o[i] = fmaf(p, __bfloat162float(v[i]), o[i]);
+              d += at_least(__ldg(a.decay + (tok0 + n * C + j) * a.dstride + kvh), kLeastDecay);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[c + i] = __float2bfloat16_rn(o[i]);
           }
         }
       }
-      if (ok) arrive(&bar->g_empty[b]);
     }
   }
 
   tc_fence_before();
   __syncthreads();
+  if (threadIdx.x == 0 && bar->abort) atomicOr(a.status, kStatusTimeout);
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512u) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(bar->tmem_base), "r"(512u) : "memory");
   }
 }
 
@@ -684,7 +838,8 @@ cudaError_t prepare() {
 }
 
 template <int D>
-cudaError_t launch(bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const LinearChunkArgs& a,
+cudaError_t launch(bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                   const CUtensorMap& tmO, const LinearChunkArgs& a,
                    cudaStream_t s) {
   if (split) {
     LinearChunkArgs b = a;                        // all segments but the last
@@ -694,10 +849,10 @@ cudaError_t launch(bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, c
       item += (a.seqs.segs[k] - 1) * a.Hkv;
     }
     b.seqs.item0[a.seqs.n] = item;
-    linear_chunk_kernel<D, true><<<item, kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, b);
+    linear_chunk_kernel<D, true><<<item, kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, b);
     linear_join_kernel<D><<<dim3(a.Hkv * (D * D / 1024), a.seqs.n), 256, 0, s>>>(a);
   }
-  linear_chunk_kernel<D, false><<<a.seqs.item0[a.seqs.n], kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, a);
+  linear_chunk_kernel<D, false><<<a.seqs.item0[a.seqs.n], kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, a);
   return cudaGetLastError();
 }
 
@@ -706,8 +861,8 @@ cudaError_t launch(bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, c
 cudaError_t linear_chunk_prepare(int D) { return D == 128 ? prepare<128>() : prepare<64>(); }
 
 cudaError_t launch_linear_chunk(int D, bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                                const LinearChunkArgs& a, cudaStream_t s) {
-  return D == 128 ? launch<128>(split, tmQ, tmK, tmV, a, s) : launch<64>(split, tmQ, tmK, tmV, a, s);
+                                const CUtensorMap& tmO, const LinearChunkArgs& a, cudaStream_t s) {
+  return D == 128 ? launch<128>(split, tmQ, tmK, tmV, tmO, a, s) : launch<64>(split, tmQ, tmK, tmV, tmO, a, s);
 }
 
 }  // namespace fk

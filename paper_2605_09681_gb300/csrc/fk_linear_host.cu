@@ -329,17 +329,18 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
       }
       LinearChunkArgs a;
       fill(a);
-      a.wide_o = aligned(O, 32) && o_stride % 16 == 0;
+      a.log2_scale = (float)std::log2((double)sc);
       a.place = h->place;
       a.place_decay = h->place_decay;
       a.seqs = l.seqs;
-      CUtensorMap tmQ, tmK, tmV;
-      if (!encode_bf16_rows(&tmQ, Q, h->tokens, (int64_t)c.n_q_heads * c.head_dim, q_stride) ||
-          !encode_bf16_rows(&tmK, K, h->tokens, (int64_t)c.n_kv_heads * c.head_dim, k_stride) ||
-          !encode_bf16_rows(&tmV, V, h->tokens, (int64_t)c.n_kv_heads * c.head_dim, v_stride))
+      CUtensorMap tmQ, tmK, tmV, tmO;
+      if (!encode_bf16_rows(&tmQ, Q, h->tokens, (int64_t)c.n_q_heads * c.head_dim, q_stride, kLinearChunk) ||
+          !encode_bf16_rows(&tmK, K, h->tokens, (int64_t)c.n_kv_heads * c.head_dim, k_stride, kLinearChunk) ||
+          !encode_bf16_rows(&tmV, V, h->tokens, (int64_t)c.n_kv_heads * c.head_dim, v_stride, kLinearChunk) ||
+          !encode_bf16_rows(&tmO, O, h->tokens, (int64_t)c.n_q_heads * c.head_dim, o_stride, 32))
         return FK_ERR_CUDA;
       h->launches += l.split ? 2 : 0;
-      const fk_status e = done(h, launch_linear_chunk(c.head_dim, l.split, tmQ, tmK, tmV, a, st));
+      const fk_status e = done(h, launch_linear_chunk(c.head_dim, l.split, tmQ, tmK, tmV, tmO, a, st));
       if (e != FK_OK) return e;
     }
     if (!state_out || !std::any_of(h->step.begin(), h->step.end(), [](const StepSeq& s) { return s.n_new == 0; })) return FK_OK;
