@@ -155,6 +155,18 @@ __device__ __forceinline__ float2 less(float2 x, uint32_t y) {
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// A sum kept as two numbers: sums' differences keep fp32's relative precision however far the sums run.  (A chunk's sums took 3200
+// cycles in fp64.)
+struct Two {
+  float h, l;
+};
+__device__ __forceinline__ Two add(Two a, Two b) {
+  const float s = a.h + b.h, v = s - a.h;
+  const float e = (a.h - (s - v)) + (b.h - v) + (a.l + b.l);
+  const float h = s + e;
+  return {h, e - (h - s)};
+}
+
 template <int D, bool kLocal>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -380,41 +392,42 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       fetch(0);
       for (int n = 0; n < nc; ++n) {
         const int b = n & 1, u = n >> 1;
-        // (in fp64: a dozen additions a chunk, and the sums' differences keep fp32's relative precision however far they run)
-        double sum[4];
+        Two sum[4];
         bool grows = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float y = at_least(x[i], kLeastDecay);
           grows |= !(y <= 0.0f);
-          sum[i] = (i == 0 ? 0.0 : sum[i - 1]) + (double)y * 1.4426950408889634;
+          const float h = y * 1.4426950408889634f;           // log2(e) in two numbers
+          const Two z{h, fmaf(y, 1.4426950408889634f, -h) + y * 1.925963033500e-8f};
+          sum[i] = i == 0 ? z : add(sum[i - 1], z);
         }
-        double all = sum[3];
+        Two all = sum[3];
 #pragma unroll 1
         for (int o = 1; o < 32; o *= 2) {
-          const double z = __shfl_up_sync(0xffffffffu, all, o);
-          if (lane >= o) all += z;
+          const Two z{__shfl_up_sync(0xffffffffu, all.h, o), __shfl_up_sync(0xffffffffu, all.l, o)};
+          if (lane >= o) all = add(z, all);
         }
-        const double before = __shfl_up_sync(0xffffffffu, all, 1), end = __shfl_sync(0xffffffffu, all, 31);
+        const Two before{__shfl_up_sync(0xffffffffu, all.h, 1), __shfl_up_sync(0xffffffffu, all.l, 1)};
+        const Two end{__shfl_sync(0xffffffffu, all.h, 31), __shfl_sync(0xffffffffu, all.l, 31)};
         if (n + 1 < nc) fetch(n + 1);
         // the sum at the end of this lane's 32 tokens, unless the chunk grows
-        const double r = __shfl_sync(0xffffffffu, all, lane | 7);
+        const Two r{__shfl_sync(0xffffffffu, all.h, lane | 7), __shfl_sync(0xffffffffu, all.l, lane | 7)};
         const bool grow = __any_sync(0xffffffffu, grows);
-        const double from = grow ? end : r;
-        float v[4], gg[4];
+        const Two from = grow ? end : r;
+        float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (lane > 0) sum[i] += before;
-          gg[i] = (float)sum[i];
-          v[i] = exp2f((float)(from - sum[i]));
+          if (lane > 0) sum[i] = add(before, sum[i]);
+          v[i] = exp2f((from.h - sum[i].h) + (from.l - sum[i].l));
         }
         if (u > 0 && !wait_for(&bar->g_empty[b], u - 1)) break;
         Sums& out = sums[b];
-        *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(gg[0], gg[1], gg[2], gg[3]);
+        *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(sum[0].h, sum[1].h, sum[2].h, sum[3].h);
         *reinterpret_cast<float4*>(out.u + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
-        if ((lane & 7) == 7) out.w[lane >> 3] = grow ? 1.0f : exp2f((float)(end - r));
+        if ((lane & 7) == 7) out.w[lane >> 3] = grow ? 1.0f : exp2f((end.h - r.h) + (end.l - r.l));
         if (lane == 0) {
-          out.e = exp2f((float)end);
+          out.e = exp2f(end.h + end.l);
           out.grow = grow;
         }
         arrive(&bar->g_full[b]);
@@ -464,11 +477,12 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       }
       const float gi = kLocal ? 0.0f : sm.g[row] + a.log2_scale;
       const bool grow = !kLocal && __any_sync(0xffffffffu, sm.grow);
-      // K' of this warpgroup's two quarters, then P of each query head
+      // K' of this warpgroup's first quarter, P of the first query head while that is multiplied, K' of the other quarter, P of
+      // further query heads
 #pragma unroll 1
       for (int step = 0; step < (kLocal ? 2 : G + 2) && ok; ++step) {
-        if (step < 2) {
-          const int q = w2 + 2 * step, buf = q % kBufs, use = n * (4 / kBufs) + q / kBufs;
+        if (step == 0 || step == (kLocal ? 1 : 2)) {
+          const int q = step == 0 ? w2 : w2 + 2, buf = q % kBufs, use = n * (4 / kBufs) + q / kBufs;
           if (use > 0 && !(ok = wait_for(&bar->kp_empty[buf], use - 1))) break;
           tc_fence_after();
           if (mine) {
@@ -513,7 +527,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           arrive(&bar->kp_full[buf]);
           continue;
         }
-        if (!(ok = wait_for(&bar->a_full, n * G + step - 2))) break;
+        if (!(ok = wait_for(&bar->a_full, n * G + (step < 2 ? 0 : step - 2)))) break;
         tc_fence_after();
         // below the diagonal A f u_j with f of the row, on it A exp(G_i - G_j), scaled
 #pragma unroll 1
