@@ -43,7 +43,7 @@ constexpr uint32_t kColA = 0, kColX = 128, kColS = 256, kColK = 384;   // kLocal
 // Many of the roles' steps are a few hundred cycles long, and so are a product's way to a barrier and a warp's way from
 // one: what can share a barrier does.
 struct Barriers {
-  uint64_t kv_full[3], kv_empty[3], q_full[2], q_empty[2];
+  uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3], q_full[2], q_empty[2];
   uint64_t g_full[2], g_empty[2];     // the chunk's sums
   uint64_t odd_full[2], odd_empty[2];
   uint64_t kp_full[4], kp_empty[4];   // K' buffers: written, multiplied
@@ -215,8 +215,10 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       mbar_init(&bar->odd_empty[i], 4);
     }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(&bar->kv_full[i], 1);
-      mbar_init(&bar->kv_empty[i], kLocal ? 1 : 2);          // the products, and the check
+      mbar_init(&bar->k_full[i], 1);
+      mbar_init(&bar->k_empty[i], kLocal ? 8 : 9);           // the converting warps, and Q K^T
+      mbar_init(&bar->v_full[i], 1);
+      mbar_init(&bar->v_empty[i], kLocal ? 1 : 2);           // the products, and the check
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&bar->kp_full[i], 4);
@@ -259,37 +261,39 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     if (warp == 3) {
       // ------------------------------------------------------------------ TMA
       bool ok = true;
-      int ikv = -1, iq = -1;                                 // last tiles issued
-      auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int n) {   // one lane
-        for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)(tok0 + n * C));
+      int ik = -1, iv = -1, iq = -1;                         // last tiles issued
+      auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int n) {
+        if (lane == 0) {
+          mbar_expect_tx(b, Lay::kTile);
+          for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)(tok0 + n * C));
+        }
+        __syncwarp();
       };
 #pragma unroll 1
       for (int n = 0; n < nc && ok; ++n) {
         const int b = n % kStages, u = n / kStages;
-        if (u > 0 && !(ok = wait_for(&bar->kv_empty[b], u - 1))) break;
-        if (lane == 0) {
-          mbar_expect_tx(&bar->kv_full[b], 2 * Lay::kTile);
-          load(&tmK, sK + b * (2 * Lay::kTile), &bar->kv_full[b], kvh, n);
-          load(&tmV, sV + b * (2 * Lay::kTile), &bar->kv_full[b], kvh, n);
-        }
-        __syncwarp();
-        ikv = n;
+        if (u > 0 && !(ok = wait_for(&bar->k_empty[b], u - 1))) break;
+        load(&tmK, sK + b * (2 * Lay::kTile), &bar->k_full[b], kvh, n);
+        ik = n;
 #pragma unroll 1
-        for (int g = 0; g < G && !kLocal; ++g) {
-          const int m = n * G + g, qb = m & 1, qu = m >> 1;
-          if (qu > 0 && !(ok = wait_for(&bar->q_empty[qb], qu - 1))) break;
-          if (lane == 0) {
-            mbar_expect_tx(&bar->q_full[qb], Lay::kTile);
+        for (int g = 0; g < (kLocal ? 1 : G); ++g) {
+          if (!kLocal) {
+            const int m = n * G + g, qb = m & 1, qu = m >> 1;
+            if (qu > 0 && !(ok = wait_for(&bar->q_empty[qb], qu - 1))) break;
             load(&tmQ, sQ + qb * Lay::kTile, &bar->q_full[qb], kvh * G + g, n);
+            iq = m;
           }
-          __syncwarp();
-          iq = m;
+          if (g > 0) continue;
+          if (u > 0 && !(ok = wait_for(&bar->v_empty[b], u - 1))) break;
+          load(&tmV, sV + b * (2 * Lay::kTile), &bar->v_full[b], kvh, n);
+          iv = n;
         }
       }
       if (!ok) {                                             // what was issued lands before the CTA ends
 #pragma unroll 1
         for (int i = 0; i < kStages; ++i) {
-          if (ikv >= i) drain(&bar->kv_full[(ikv - i) % kStages], ((ikv - i) / kStages) & 1, bar);
+          if (ik >= i) drain(&bar->k_full[(ik - i) % kStages], ((ik - i) / kStages) & 1, bar);
+          if (iv >= i) drain(&bar->v_full[(iv - i) % kStages], ((iv - i) / kStages) & 1, bar);
           if (iq >= i && i < 2) drain(&bar->q_full[(iq - i) & 1], ((iq - i) >> 1) & 1, bar);
         }
       }
@@ -310,6 +314,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) umma(kColA, x + along(kk), y + along(kk), kIdA, kk > 0 ? 1u : 0u);
         umma_commit(&bar->a_full);
+        if (G == 1 || m % G == G - 1) umma_commit(&bar->k_empty[n & 1]);
       };
       auto half_ds = [&](int n, int q0) {                    // dS += K'^T V of 64 tokens
 #pragma unroll 1
@@ -324,21 +329,21 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               umma_ts(kColS, kp + i * 8, y + (i & 1) * 128, kIdD, q + i > 0 ? 1u : 0u);
             umma_commit(&bar->kp_empty[q % kBufs]);
             if (q == 3) umma_commit(&bar->ds_full);
-            if (q == 3 && kLocal) umma_commit(&bar->kv_empty[n % kStages]);
+            if (q == 3 && kLocal) umma_commit(&bar->v_empty[n % kStages]);
           }
           __syncwarp();
         }
         return true;
       };
-      bool ok = wait_for(&bar->kv_full[0], 0);
-      if (!kLocal && ok && (ok = wait_for(&bar->q_full[0], 0))) {
+      bool ok = true;
+      if (!kLocal && (ok = wait_for(&bar->k_full[0], 0) && wait_for(&bar->q_full[0], 0))) {
         tc_fence_after();
         if (elect_one()) q_k(0, 0);
         __syncwarp();
       }
 #pragma unroll 1
       for (int n = 0; n < nc && ok; ++n) {
-        if (kLocal && n > 0 && !(ok = wait_for(&bar->kv_full[n % kStages], n / kStages))) break;
+        if (!(ok = wait_for(&bar->v_full[n % kStages], n / kStages))) break;
         if (n > 0 && !(ok = wait_for(&bar->ds_empty, n - 1))) break;
         if (!(ok = half_ds(n, 0))) break;
         if (kLocal) ok = half_ds(n, 2);
@@ -362,12 +367,12 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
             for (int kk = 0; kk < C / 16; ++kk) umma_ts(kColX, kColA + (kk >> 1) * 32 + (kk & 1) * 8, y + kk * 128, kIdD, 1u);
             umma_commit(&bar->y_full);
-            if (g == G - 1) umma_commit(&bar->kv_empty[n & 1]);
+            if (g == G - 1) umma_commit(&bar->v_empty[n & 1]);
           }
           __syncwarp();
           if (m + 1 < nc * G) {                              // the next A
             const int n1 = g + 1 < G ? n : n + 1;
-            if (n1 > n && !(ok = wait_for(&bar->kv_full[n1 & 1], n1 >> 1))) break;
+            if (n1 > n && !(ok = wait_for(&bar->k_full[n1 & 1], n1 >> 1))) break;
             if (!(ok = wait_for(&bar->q_full[(m + 1) & 1], (m + 1) >> 1))) break;
             tc_fence_after();
             if (elect_one()) q_k(m + 1, n1);
@@ -436,7 +441,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       // ------------------------------------------------------------------ is V finite
       for (int n = 0; n < nc; ++n) {
         const int b = n & 1, u = n >> 1, valid = min(C, tokens - n * C);
-        if (!wait_for(&bar->kv_full[b], u)) break;
+        if (!wait_for(&bar->v_full[b], u)) break;
         // 0 times a value is NaN where it is not finite; 8 runs of 16 bytes to a row of a panel
         uint32_t z[4] = {0, 0, 0, 0};
 #pragma unroll 4
@@ -452,7 +457,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const bool odd = __any_sync(0xffffffffu, ((z[0] | z[1] | z[2] | z[3]) & 0x7FFF7FFFu) != 0);
         if (lane == 0) bar->odd[b] = (int)odd;
         arrive(&bar->odd_full[b]);
-        arrive(&bar->kv_empty[b]);
+        arrive(&bar->v_empty[b]);
       }
     }
   } else if (warp < 12) {
@@ -465,8 +470,9 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       const int b = n & 1, u = n >> 1, valid = min(C, tokens - n * C);
       const Sums& sm = sums[b];
       const int bk = n % kStages;                            // stage of K and V
-      if (!(ok = wait_for(&bar->kv_full[bk], n / kStages) && wait_for(&bar->g_full[b], u))) break;
+      if (!(ok = wait_for(&bar->k_full[bk], n / kStages) && wait_for(&bar->g_full[b], u))) break;
       if (valid < C) {                                       // rows of others: zeros for the products with V
+        if (!(ok = wait_for(&bar->v_full[bk], n / kStages))) break;
         const int p = wq >> 1, r = 64 * (wq & 1) + 32 * w2 + lane;   // panel, token of this warpgroup's
         if (r >= valid && p < kPanels) {
 #pragma unroll 1
@@ -525,6 +531,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             tc_fence_before();
           }
           arrive(&bar->kp_full[buf]);
+          if (step > 0) arrive(&bar->k_empty[bk]);
           continue;
         }
         if (!(ok = wait_for(&bar->a_full, n * G + (step < 2 ? 0 : step - 2)))) break;
