@@ -155,17 +155,8 @@ __device__ __forceinline__ float2 less(float2 x, uint32_t y) {
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// A sum kept as two numbers: sums' differences keep fp32's relative precision however far the sums run.  (A chunk's sums took 3200
-// cycles in fp64.)
-struct Two {
-  float h, l;
-};
-__device__ __forceinline__ Two add(Two a, Two b) {
-  const float s = a.h + b.h, v = s - a.h;
-  const float e = (a.h - (s - v)) + (b.h - v) + (a.l + b.l);
-  const float h = s + e;
-  return {h, e - (h - s)};
-}
+// a whole number of 2^-32 as fp32
+__device__ __forceinline__ float of_fixed(int64_t x) { return fmaf((float)(uint32_t)x, 0x1p-32f, (float)(int32_t)(x >> 32)); }
 
 template <int D, bool kLocal>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -205,7 +196,14 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   const int G = kLocal ? 1 : a.G;
   const int64_t place = (int64_t)a.seqs.place0[s] + kvh * segs + seg;
 
-  if (threadIdx.x == 0) {
+  // The loading warp makes the barriers and asks for the first tiles before the CTA meets (which takes 1700 cycles: the
+  // allocation of tensor memory).
+  auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int n) {   // one lane
+    mbar_expect_tx(b, Lay::kTile);
+    for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)(tok0 + n * C));
+  };
+  if (warp == 3 && lane == 0) {
+    for (const CUtensorMap* map : {&tmK, &tmV, &tmQ, &tmO}) asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bar->q_full[i], 1);
       mbar_init(&bar->q_empty[i], 4);                        // O's rows, put in the tile's place, are on their way
@@ -234,12 +232,29 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     mbar_init(&bar->fin, 1);
     bar->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    load(&tmK, sK, &bar->k_full[0], kvh, 0);
+    if (!kLocal) load(&tmQ, sQ, &bar->q_full[0], kvh * G, 0);
+    load(&tmV, sV, &bar->v_full[0], kvh, 0);
   }
   if (warp == 1) {
     __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  :: "r"(su32(&bar->tmem_base)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // decays of a chunk (warp 2, lane's tokens 4 lane .. + 3), three chunks ahead: one chunk's time is less than a load takes
+  const float* decay = a.decay + tok0 * a.dstride + kvh;
+  float ahead[3][4];
+  auto fetch = [&](int n, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = n * C + 4 * lane + i;
+      x[i] = t < tokens ? __ldg(decay + (int64_t)t * a.dstride) : 0.0f;
+    }
+  };
+  if (warp == 2) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) fetch(i, ahead[i]);
   }
   tc_fence_before();
   __syncthreads();
@@ -261,31 +276,27 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     if (warp == 3) {
       // ------------------------------------------------------------------ TMA
       bool ok = true;
-      int ik = -1, iv = -1, iq = -1;                         // last tiles issued
-      auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int n) {
-        if (lane == 0) {
-          mbar_expect_tx(b, Lay::kTile);
-          for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)(tok0 + n * C));
-        }
-        __syncwarp();
-      };
+      int ik = 0, iv = 0, iq = kLocal ? -1 : 0;              // last tiles issued
 #pragma unroll 1
       for (int n = 0; n < nc && ok; ++n) {
         const int b = n % kStages, u = n / kStages;
         if (u > 0 && !(ok = wait_for(&bar->k_empty[b], u - 1))) break;
-        load(&tmK, sK + b * (2 * Lay::kTile), &bar->k_full[b], kvh, n);
+        if (lane == 0 && n > 0) load(&tmK, sK + b * (2 * Lay::kTile), &bar->k_full[b], kvh, n);
+        __syncwarp();
         ik = n;
 #pragma unroll 1
         for (int g = 0; g < (kLocal ? 1 : G); ++g) {
           if (!kLocal) {
             const int m = n * G + g, qb = m & 1, qu = m >> 1;
             if (qu > 0 && !(ok = wait_for(&bar->q_empty[qb], qu - 1))) break;
-            load(&tmQ, sQ + qb * Lay::kTile, &bar->q_full[qb], kvh * G + g, n);
+            if (lane == 0 && m > 0) load(&tmQ, sQ + qb * Lay::kTile, &bar->q_full[qb], kvh * G + g, n);
+            __syncwarp();
             iq = m;
           }
           if (g > 0) continue;
           if (u > 0 && !(ok = wait_for(&bar->v_empty[b], u - 1))) break;
-          load(&tmV, sV + b * (2 * Lay::kTile), &bar->v_full[b], kvh, n);
+          if (lane == 0 && n > 0) load(&tmV, sV + b * (2 * Lay::kTile), &bar->v_full[b], kvh, n);
+          __syncwarp();
           iv = n;
         }
       }
@@ -384,55 +395,55 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       drain(&bar->fin, 0, bar);
       __syncwarp();
     } else if (warp == 2) {
-      // ------------------------------------------------------------------ running sums of a chunk: lane's tokens 4 lane .. + 3
-      const float* decay = a.decay + tok0 * a.dstride + kvh;
-      float x[4];
-      auto fetch = [&](int n) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = n * C + 4 * lane + i;
-          x[i] = t < tokens ? __ldg(decay + (int64_t)t * a.dstride) : 0.0f;
-        }
-      };
-      fetch(0);
+      // ------------------------------------------------------------------ running sums of a chunk
+#pragma unroll 1
       for (int n = 0; n < nc; ++n) {
         const int b = n & 1, u = n >> 1;
-        Two sum[4];
+        // whole numbers of 2^-32: sums and their differences are exact however far they run (2^-33 a token is 2^-26 at most for a
+        // chunk, of a logarithm); what is not a number makes all sums from its token on that
+        int64_t sum[4];
         bool grows = false;
+        int lost = C;                                        // first token that is not a number
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float y = at_least(x[i], kLeastDecay);
+          const float y = ahead[0][i];
           grows |= !(y <= 0.0f);
-          const float h = y * 1.4426950408889634f;           // log2(e) in two numbers
-          const Two z{h, fmaf(y, 1.4426950408889634f, -h) + y * 1.925963033500e-8f};
-          sum[i] = i == 0 ? z : add(sum[i - 1], z);
+          if (y != y) lost = min(lost, 4 * lane + i);
+          const int64_t z = __float2ll_rn(fminf(fmaxf(y, kLeastDecay), -kLeastDecay) * (1.4426950408889634f * 0x1p32f));
+          sum[i] = i == 0 ? z : sum[i - 1] + z;
         }
-        Two all = sum[3];
-#pragma unroll 1
+        int64_t all = sum[3];
+#pragma unroll
         for (int o = 1; o < 32; o *= 2) {
-          const Two z{__shfl_up_sync(0xffffffffu, all.h, o), __shfl_up_sync(0xffffffffu, all.l, o)};
-          if (lane >= o) all = add(z, all);
+          const int64_t z = __shfl_up_sync(0xffffffffu, all, o);
+          if (lane >= o) all += z;
         }
-        const Two before{__shfl_up_sync(0xffffffffu, all.h, 1), __shfl_up_sync(0xffffffffu, all.l, 1)};
-        const Two end{__shfl_sync(0xffffffffu, all.h, 31), __shfl_sync(0xffffffffu, all.l, 31)};
-        if (n + 1 < nc) fetch(n + 1);
-        // the sum at the end of this lane's 32 tokens, unless the chunk grows
-        const Two r{__shfl_sync(0xffffffffu, all.h, lane | 7), __shfl_sync(0xffffffffu, all.l, lane | 7)};
+        const int64_t before = all - sum[3], end = __shfl_sync(0xffffffffu, all, 31);
         const bool grow = __any_sync(0xffffffffu, grows);
-        const Two from = grow ? end : r;
-        float v[4];
+        lost = __reduce_min_sync(0xffffffffu, lost);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (lane > 0) sum[i] = add(before, sum[i]);
-          v[i] = exp2f((from.h - sum[i].h) + (from.l - sum[i].l));
+          ahead[0][i] = ahead[1][i];
+          ahead[1][i] = ahead[2][i];
+        }
+        fetch(n + 3, ahead[2]);
+        // the sum at the end of this lane's 32 tokens, unless the chunk grows
+        const int64_t r = __shfl_sync(0xffffffffu, all, lane | 7), from = grow ? end : r;
+        const float nan = __int_as_float(0x7FFFFFFF);
+        float gg[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t x = before + sum[i];
+          gg[i] = 4 * lane + i >= lost ? nan : of_fixed(x);
+          v[i] = lost < C ? nan : exp2f(of_fixed(from - x));
         }
         if (u > 0 && !wait_for(&bar->g_empty[b], u - 1)) break;
         Sums& out = sums[b];
-        *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(sum[0].h, sum[1].h, sum[2].h, sum[3].h);
+        *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(gg[0], gg[1], gg[2], gg[3]);
         *reinterpret_cast<float4*>(out.u + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
-        if ((lane & 7) == 7) out.w[lane >> 3] = grow ? 1.0f : exp2f((end.h - r.h) + (end.l - r.l));
+        if ((lane & 7) == 7) out.w[lane >> 3] = grow ? 1.0f : exp2f(of_fixed(end - r));
         if (lane == 0) {
-          out.e = exp2f(end.h + end.l);
+          out.e = lost < C ? nan : exp2f(of_fixed(end));
           out.grow = grow;
         }
         arrive(&bar->g_full[b]);
