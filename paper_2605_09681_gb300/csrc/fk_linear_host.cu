@@ -124,49 +124,165 @@ bool meet(const Rows& a, const Rows& b, int64_t tokens) {
   return d < low || a.stride - d < high;
 }
 
-// Tokens up to which a sequence goes through the recurrence.
-constexpr int kFewTokens = 32;
+// ---- plan of a step
+// Estimated times in us, measured back to back on a GB300 (segments alone and with all SMs taken): a CTA's start and end, and
+// what it takes for a chunk and each further query head, of the kernel that computes o and of the one that forms
+// segments' states; the join of those; a token of the recurrence alone, and what all SMs together take for a token of one head.
+struct Times {
+  double fixed, chunk, head, fixed_local, chunk_local, join, few, few_token, few_share;
+};
+constexpr Times kTimes128{8.0, 2.7, 2.4, 7.0, 1.8, 4.0, 2.2, 0.6, 0.0042}, kTimes64{8.0, 2.4, 0.9, 6.0, 1.2, 3.5, 2.0, 0.4, 0.0012};
 
-int segments_of(const fk_linear* h, int chunks, int64_t items) {
-  if (h->force_segments > 0) return std::min(h->force_segments, chunks);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(chunks / 2, h->sms / items));
+// Time of `groups` of equally long items (length, count), longest first, on the SMs: each goes to the one that is free first.
+double fill_sms(const fk_linear* h, std::vector<std::pair<double, int64_t>>& groups) {
+  std::sort(groups.begin(), groups.end(), [](const auto& x, const auto& y) { return x.first > y.first; });
+  std::vector<double> busy(h->sms, 0.0), other(h->sms);
+  for (const auto& g : groups) {
+    int64_t left = g.second;
+    const int64_t whole = left / h->sms > 8 ? left / h->sms - 8 : 0;   // (many rounds: as much for everyone)
+    for (double& t : busy) t += (double)whole * g.first;
+    left -= whole * h->sms;
+    while (left > 0) {
+      const int n = (int)std::min<int64_t>(left, h->sms);
+      for (int i = 0; i < n; ++i) busy[i] += g.first;
+      std::merge(busy.begin(), busy.begin() + n, busy.begin() + n, busy.end(), other.begin());
+      busy.swap(other);
+      left -= n;
+    }
+  }
+  return busy.back();
 }
 
-// The launches of a step: sequences of few tokens, then the others, kLinearSeqs of them to a launch.
+int chunks_of(int tokens) { return (tokens + kLinearChunk - 1) / kLinearChunk; }
+
+// Segments of a sequence of `chunks`, of at most `per` chunks each.
+int segments_of(int chunks, int per) { return (chunks + per - 1) / per; }
+
+// Chunks of a segment, at most, that make the sequences of more than `upto` tokens the fastest.  Splitting a sequence reads its
+// keys and values twice and takes two launches more, and pays where long sequences would leave SMs idle.
+int best_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto, double* us) {
+  const Times& t = h->cfg.head_dim == 128 ? kTimes128 : kTimes64;
+  const int H = h->cfg.n_kv_heads;
+  const double chunk = t.chunk + (h->cfg.n_q_heads / H - 1) * t.head;
+  int most = 0;
+  for (const StepSeq& s : step) most = std::max(most, s.n_new > upto ? chunks_of(s.n_new) : 0);
+  *us = 0.0;
+  if (most == 0) return 1;
+  int best = most;
+  double least = 1e30;
+  std::vector<std::pair<double, int64_t>> full, local;
+  for (int parts = 1; parts <= most; parts += std::max(1, parts / 8)) {
+    const int per = (most + parts - 1) / parts;
+    full.clear();
+    local.clear();
+    int64_t places = 0;
+    for (const StepSeq& s : step) {
+      if (s.n_new <= upto) continue;
+      const int c = chunks_of(s.n_new), n = segments_of(c, per);
+      full.push_back({t.fixed + (c + n - 1) / n * chunk, (int64_t)n * H});
+      if (n > 1) {
+        local.push_back({t.fixed_local + (c + n - 1) / n * t.chunk_local, (int64_t)(n - 1) * H});
+        places += (int64_t)n * H;
+      }
+    }
+    if (places > kPlaces) break;
+    const double x = fill_sms(h, full) + (local.empty() ? 0.0 : fill_sms(h, local) + t.join);
+    if (x < least - 0.5) {
+      least = x;
+      best = per;
+    }
+    if (per <= 2) break;
+  }
+  *us = least;
+  return best;
+}
+
+// Sequences of up to how many tokens go through the recurrence: it takes longer for each token, but a chunk takes as long
+// for one as for 128.
+int best_few(const fk_linear* h, const std::vector<StepSeq>& step, int* per) {
+  const Times& t = h->cfg.head_dim == 128 ? kTimes128 : kTimes64;
+  const int G = h->cfg.n_q_heads / h->cfg.n_kv_heads;
+  int best = 0;
+  double least = 1e30;
+  for (int upto : {1, 2, 4, 8, 16, 32}) {
+    int longest = 0;
+    int64_t tokens = 0, beyond = 0;
+    for (const StepSeq& s : step) {
+      if (s.n_new > upto) {
+        ++beyond;
+      } else {
+        longest = std::max(longest, s.n_new);
+        tokens += s.n_new;
+      }
+    }
+    double us = 0.0;
+    const int p = best_split(h, step, upto, &us);
+    if (tokens > 0)
+      us += t.few + std::max(t.few_token * longest * (0.6 + 0.4 * G), t.few_share * (double)tokens * h->cfg.n_kv_heads * (0.6 + 0.4 * G));
+    if (us < least) {
+      least = us;
+      best = upto;
+      *per = p;
+    }
+    if (beyond == 0) break;
+  }
+  return best;
+}
+
+// The launches of a step: sequences of few tokens, then the others, the longest segments first; kLinearSeqs to a launch.
 void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<Launch>* plan) {
-  const int upto = h->force_few > 0 ? h->force_few : kFewTokens, H = h->cfg.n_kv_heads;
-  int64_t items = 0;
-  for (const StepSeq& s : step) items += s.n_new > upto ? H : 0;
+  const int H = h->cfg.n_kv_heads;
+  int upto = 1, per = 1;
+  if (std::all_of(step.begin(), step.end(), [](const StepSeq& s) { return s.n_new <= 1; }) && h->force_few == 0) {
+    upto = 1;                           // (a decoding step: nothing to estimate)
+  } else if (h->force_few > 0) {
+    double us;
+    upto = h->force_few;
+    per = best_split(h, step, upto, &us);
+  } else {
+    upto = best_few(h, step, &per);
+  }
+  std::vector<int> order(step.size());
+  std::vector<int64_t> tok0(step.size());
+  int64_t tok = 0;
+  for (size_t i = 0; i < step.size(); tok += step[i++].n_new) {
+    order[i] = (int)i;
+    tok0[i] = tok;
+  }
+  auto segments = [&](int tokens) {
+    const int c = chunks_of(tokens);
+    return h->force_segments > 0 ? std::min(h->force_segments, c) : segments_of(c, per);
+  };
+  auto length = [&](int i) { return (chunks_of(step[i].n_new) + segments(step[i].n_new) - 1) / std::max(1, segments(step[i].n_new)); };
   for (const bool chunk : {false, true}) {
     Launch l{};
-    int64_t tok = 0;
     int places = 0;
     auto push = [&] {
       if (chunk ? l.seqs.n : l.few.n) plan->push_back(l);
       l = Launch{};
+      l.chunk = chunk;
       places = 0;
     };
     l.chunk = chunk;
-    for (size_t i = 0; i < step.size(); tok += step[i++].n_new) {
+    if (chunk) std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return length(x) > length(y); });
+    for (const int i : order) {
       const StepSeq& s = step[i];
       if (s.n_new == 0 || (s.n_new > upto) != chunk) continue;
       if ((chunk ? l.seqs.n : l.few.n) == kLinearSeqs) push();
-      l.chunk = chunk;
       if (!chunk) {
         const int k = l.few.n++;
         l.few.slot[k] = s.seq;
-        l.few.out[k] = (int)i;
-        l.few.tok0[k] = (int)tok;
+        l.few.out[k] = i;
+        l.few.tok0[k] = (int)tok0[i];
         l.few.len[k] = s.n_new;
         continue;
       }
       const int k = l.seqs.n++;
-      int segs = segments_of(h, (s.n_new + kLinearChunk - 1) / kLinearChunk, items);
-      segs = std::min(segs, (kPlaces - places) / H);
+      int segs = std::min(segments(s.n_new), (kPlaces - places) / H);
       if (segs < 2) segs = 1;
       l.seqs.slot[k] = s.seq;
-      l.seqs.out[k] = (int)i;
-      l.seqs.tok0[k] = (int)tok;
+      l.seqs.out[k] = i;
+      l.seqs.tok0[k] = (int)tok0[i];
       l.seqs.len[k] = s.n_new;
       l.seqs.segs[k] = segs;
       l.seqs.place0[k] = places;
