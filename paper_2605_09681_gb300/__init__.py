@@ -538,98 +538,104 @@ class Rotary:
         self._ref = ctypes.byref(self._r)
         import torch
         self._types = {torch.bfloat16: L.FK_TYPE_BF16, torch.float16: L.FK_TYPE_F16, torch.float32: L.FK_TYPE_F32}
-        self._i32 = torch.int32
+        self._torch, self._i32 = torch, torch.int32
 
     def _at(self, positions, tokens):
         n = self.n_axes
         if positions.dtype is not self._i32 or not positions.is_cuda or not positions.is_contiguous() or \
-                not (positions.shape == (tokens, n) or (n == 1 and positions.shape == (tokens,))):
+                positions.shape != (tokens, n) and (n > 1 or positions.shape != (tokens,)):
             raise ValueError("positions: expected a contiguous int32 CUDA tensor [%d, %d]" % (tokens, n))
         return positions.data_ptr()
 
     def _rows(self, x, dtype, tokens, name):
-        """(address, elements from token to token, heads) of a [tokens, heads, head_dim] tensor."""
-        D = self.head_dim
-        if x.dtype is not dtype or not x.is_cuda or x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != D:
+        """(address, elements from token to token, heads) of a [tokens, heads, head_dim] tensor.  (Few tensor properties are
+        asked for: a small call is paced by the host.)"""
+        D, shape = self.head_dim, x.shape
+        if x.dtype is not dtype or not x.is_cuda or len(shape) != 3 or shape[0] != tokens or shape[2] != D:
             raise ValueError("%s: expected a CUDA tensor [%d, heads, %d] of %s, not %s %s"
-                             % (name, tokens, D, dtype, x.dtype, list(x.shape)))
+                             % (name, tokens, D, dtype, x.dtype, list(shape)))
+        heads = shape[1]
         row, head, channel = x.stride()
-        heads = x.shape[1]
         if tokens and (channel != 1 or (heads > 1 and head != D)):
             raise ValueError("%s: the heads of a token must lie contiguously" % name)
         return x.data_ptr(), row if tokens > 1 else heads * D, heads
 
-    def _call(self, device, stream, call):
-        """call(raw stream) with the tensors' device as the current one."""
-        import torch
-        if torch.cuda.current_device() == device.index:
-            return call(_stream(stream))
-        with torch.cuda.device(device):
-            return call(_stream(stream))
+    def _elsewhere(self, x):
+        """The device of x where it is not the current one."""
+        dev = x.get_device()
+        return dev if dev >= 0 and dev != self._torch.cuda.current_device() else None
 
     def rotate(self, positions, Q, K=None, inverse=False, Q_out=None, K_out=None, stream=None):
         """Q (and K, in the same launch) [tokens, heads, head_dim] in bf16, fp16 or fp32, which may be slices of wider rows,
         turned by `positions` (int32 [tokens, axes], or [tokens]); inverse: the other way (the rotation's gradient).
         Returns the rotated Q, or Q and K, in new tensors or in Q_out, K_out (which may be Q, K)."""
+        dev = self._elsewhere(Q)
+        if dev is not None:
+            with self._torch.cuda.device(dev):
+                return self.rotate(positions, Q, K, inverse, Q_out, K_out, stream)
         dtype = Q.dtype
-        if dtype not in self._types:
+        kind = self._types.get(dtype)
+        if kind is None:
             raise ValueError("Q: expected bf16, fp16 or fp32, not %s" % dtype)
         if K is None and K_out is not None:
             raise ValueError("K_out needs K")
         tokens = Q.shape[0]
         p = self._at(positions, tokens)
         q, qs, hq = self._rows(Q, dtype, tokens, "Q")
-        k = o2 = None
-        ks = os2 = hk = 0
+        raw = _stream(stream)
+        if Q_out is None:
+            Q_out = self._torch.empty_like(Q) if stream is None else _made(Q, raw)   # (dense either way)
+            q1, qs1 = Q_out.data_ptr(), hq * self.head_dim
+        else:
+            q1, qs1, h = self._rows(Q_out, dtype, tokens, "Q_out")
+            if h != hq:
+                raise ValueError("Q_out: expected the shape of Q")
+        k = k1 = None
+        ks = ks1 = hk = 0
         if K is not None:
             k, ks, hk = self._rows(K, dtype, tokens, "K")
-
-        def call(s):
-            nonlocal Q_out, K_out, o2, os2
-            if Q_out is None:
-                Q_out = _made(Q.shape, dtype, Q.device, stream, s)
-            o1, os1, _ = self._rows(Q_out, dtype, tokens, "Q_out")
-            if Q_out.shape != Q.shape or (K_out is not None and K_out.shape != K.shape):
-                raise ValueError("Q_out, K_out: expected the shapes of Q and K")
-            if K is not None:
-                if K_out is None:
-                    K_out = _made(K.shape, dtype, K.device, stream, s)
-                o2, os2, _ = self._rows(K_out, dtype, tokens, "K_out")
-            _check(self._lib.fk_rotate(self._ref, tokens, p, 1 if inverse else 0, self._types[dtype], q, qs, hq, o1, os1,
-                                       k, ks, hk, o2, os2, s), "fk_rotate")
-
-        self._call(Q.device, stream, call)
+            if K_out is None:
+                K_out = self._torch.empty_like(K) if stream is None else _made(K, raw)
+                k1, ks1 = K_out.data_ptr(), hk * self.head_dim
+            else:
+                k1, ks1, h = self._rows(K_out, dtype, tokens, "K_out")
+                if h != hk:
+                    raise ValueError("K_out: expected the shape of K")
+        _check(self._lib.fk_rotate(self._ref, tokens, p, 1 if inverse else 0, kind, q, qs, hq, q1, qs1, k, ks, hk, k1, ks1, raw),
+               "fk_rotate")
         return Q_out if K is None else (Q_out, K_out)
 
     def tables(self, positions, cos=None, sin=None, stream=None):
         """cos and sin of the angles at `positions`, fp32 [tokens, dim / 2] (rows of PagedKVCache.append's tables)."""
-        import torch
+        dev = self._elsewhere(positions)
+        if dev is not None:
+            with self._torch.cuda.device(dev):
+                return self.tables(positions, cos, sin, stream)
         tokens = positions.shape[0]
         p = self._at(positions, tokens)
-        shape = (tokens, self.dim // 2)
+        shape, f32 = (tokens, self.dim // 2), self._torch.float32
         for x in (cos, sin):
-            if x is not None and (x.dtype is not torch.float32 or x.shape != shape or not x.is_cuda or not x.is_contiguous()):
+            if x is not None and (x.dtype is not f32 or x.shape != shape or not x.is_cuda or not x.is_contiguous()):
                 raise ValueError("cos, sin: expected contiguous fp32 CUDA tensors [%d, %d]" % shape)
-
-        def call(s):
-            nonlocal cos, sin
-            cos = _made(shape, torch.float32, positions.device, stream, s) if cos is None else cos
-            sin = _made(shape, torch.float32, positions.device, stream, s) if sin is None else sin
-            _check(self._lib.fk_rotary_tables(self._ref, tokens, p, cos.data_ptr(), sin.data_ptr(), s), "fk_rotary_tables")
-
-        self._call(positions.device, stream, call)
+        raw = _stream(stream)
+        if cos is None:
+            cos = self._torch.empty(shape, dtype=f32, device=positions.device) if stream is None else _made(positions, raw, shape, f32)
+        if sin is None:
+            sin = self._torch.empty(shape, dtype=f32, device=positions.device) if stream is None else _made(positions, raw, shape, f32)
+        _check(self._lib.fk_rotary_tables(self._ref, tokens, p, cos.data_ptr(), sin.data_ptr(), raw), "fk_rotary_tables")
         return cos, sin
 
 
-def _made(shape, dtype, device, stream, raw):
-    """An output tensor, of the memory of the stream that is to write it (`raw`; `stream` None: the current one): the current
-    stream may still have work queued on memory that it has given back."""
+def _made(like, raw, shape=None, dtype=None):
+    """An output tensor beside `like` (its shape and type by default), of the memory of the stream that is to write it (`raw`):
+    the current stream may still have work queued on memory that it has given back."""
     import torch
-    if stream is None or raw == torch.cuda.current_stream(device).cuda_stream:
-        return torch.empty(shape, dtype=dtype, device=device)
-    own = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    shape, dtype = like.shape if shape is None else shape, like.dtype if dtype is None else dtype
+    if raw == torch.cuda.current_stream(like.device).cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    own = torch.cuda.ExternalStream(raw, device=like.device) if raw else torch.cuda.default_stream(like.device)
     with torch.cuda.stream(own):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 class LinearStateCache:
@@ -652,7 +658,7 @@ class LinearStateCache:
         self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
         self.max_seqs, self.device = max_seqs, device
         import torch
-        self._bf16, self._f32 = torch.bfloat16, torch.float32
+        self._torch, self._bf16, self._f32 = torch, torch.bfloat16, torch.float32
         self._dev = torch.device("cuda", device)
         self._tokens = self._seqs = 0
         _check(self._lib.fk_linear_create(ctypes.byref(self.cfg), ctypes.byref(self._h)), "fk_linear_create")
@@ -696,11 +702,11 @@ class LinearStateCache:
         q, qs = self._rows(Q, T, self.n_q_heads, "Q")
         k, ks = self._rows(K, T, H, "K")
         v, vs = self._rows(V, T, H, "V")
-        if decay.dtype is not self._f32 or not decay.is_cuda or decay.shape not in ((T, H), (H,)) or \
+        shape, gs = decay.shape, 0
+        if decay.dtype is not self._f32 or not decay.is_cuda or (shape != (T, H) and shape != (H,)) or \
                 (H > 1 and decay.stride(-1) != 1):
             raise ValueError("decay: expected an fp32 CUDA tensor [%d, %d] or [%d]" % (T, H, H))
-        gs = 0
-        if decay.dim() == 2:
+        if len(shape) == 2:
             gs = decay.stride(0) if T > 1 else H
         s1 = None
         if state_out is not None:
@@ -710,7 +716,7 @@ class LinearStateCache:
             s1 = state_out.data_ptr()
         raw = self._on(stream)
         if O is None:
-            O = _made(Q.shape, self._bf16, self._dev, stream, raw)
+            O = self._torch.empty_like(Q) if stream is None else _made(Q, raw)   # (dense either way)
             o, os = O.data_ptr(), self.n_q_heads * D
         else:
             o, os = self._rows(O, T, self.n_q_heads, "O")

@@ -131,7 +131,7 @@ bool meet(const Rows& a, const Rows& b, int64_t tokens) {
 struct Times {
   double fixed, chunk, head, fixed_local, chunk_local, join, few, few_token, few_share;
 };
-constexpr Times kTimes128{8.0, 2.7, 2.4, 7.0, 1.8, 4.0, 2.2, 0.6, 0.0042}, kTimes64{8.0, 2.4, 0.9, 6.0, 1.2, 3.5, 2.0, 0.4, 0.0012};
+constexpr Times kTimes128{8.0, 2.7, 2.4, 7.0, 1.8, 4.0, 2.2, 0.27, 0.0023}, kTimes64{8.0, 2.4, 0.9, 6.0, 1.2, 3.5, 2.0, 0.2, 0.0007};
 
 // Time of `groups` of equally long items (length, count), longest first, on the SMs: each goes to the one that is free first.
 double fill_sms(const fk_linear* h, std::vector<std::pair<double, int64_t>>& groups) {
@@ -206,19 +206,21 @@ int best_few(const fk_linear* h, const std::vector<StepSeq>& step, int* per) {
   double least = 1e30;
   for (int upto : {1, 2, 4, 8, 16, 32}) {
     int longest = 0;
-    int64_t tokens = 0, beyond = 0;
+    int64_t tokens = 0, seqs = 0, beyond = 0;
     for (const StepSeq& s : step) {
       if (s.n_new > upto) {
         ++beyond;
       } else {
         longest = std::max(longest, s.n_new);
         tokens += s.n_new;
+        seqs += s.n_new > 0;
       }
     }
     double us = 0.0;
     const int p = best_split(h, step, upto, &us);
     if (tokens > 0)
-      us += t.few + std::max(t.few_token * longest * (0.6 + 0.4 * G), t.few_share * (double)tokens * h->cfg.n_kv_heads * (0.6 + 0.4 * G));
+      us += t.few + (double)seqs * h->per_seq * 8 / 6.3e6 +      // (the states' bytes, and the tokens)
+            (0.6 + 0.4 * G) * std::max(t.few_token * longest, t.few_share * (double)tokens * h->cfg.n_kv_heads);
     if (us < least) {
       least = us;
       best = upto;

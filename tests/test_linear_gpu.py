@@ -196,8 +196,7 @@ def test_slices_of_wide_rows_and_guard_values():
     assert (O == 7.0).all()
 
 
-@pytest.mark.parametrize("where", ["q", "k", "v", "g"])
-@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("where,value", [(w, x) for w in "qkvg" for x in (np.inf, -np.inf, np.nan) if (w, x) != ("g", -np.inf)])
 @pytest.mark.parametrize("T", [6, 290])
 def test_infinities_and_nan_reach_no_token_before_them(T, value, where):
     """Tokens before one that is not finite, and other sequences, are as if it were another value; behind it the values that are
@@ -207,8 +206,6 @@ def test_infinities_and_nan_reach_no_token_before_them(T, value, where):
     q, k, v, g, _ = _inputs(n, 2, 2, 64, 15)
     g = g.copy()
     {"q": q, "k": k, "v": v, "g": g}[where][(bad, 1, 5) if where != "g" else (bad, 1)] = value
-    if where == "g" and value == -np.inf:
-        pytest.skip("a decay of its own: test_states_that_start_anew")
     with _cache(head_dim=64) as cache:
         cache.step([0, 1, 2], lens)
         o = _np(cache.attend(0, _bf16(q), _bf16(k), _bf16(v), _dev(g)))
@@ -246,6 +243,50 @@ def test_captured_steps_go_on_at_each_replay(T):
             graph.replay()
             want = plain.attend(*args)
             assert torch.equal(out, want) and torch.equal(cache.states(0), plain.states(0))
+
+
+@pytest.mark.parametrize("T,segments", [(700, 1), (700, 2), (700, 3), (700, 6), (129, 2), (1500, 0), (3000, 5)])
+@pytest.mark.parametrize("D,Hq,H", [(64, 2, 2), (128, 3, 1)])
+def test_segments(T, segments, D, Hq, H):
+    """However a sequence is split, beside others that are not, and whatever the state goes to."""
+    lens = [130, T, 40]
+    n = sum(lens)
+    q, k, v, g, s0 = _inputs(n, Hq, H, D, T + segments)
+    with _cache(head_dim=D, n_q_heads=Hq, n_kv_heads=H) as cache:
+        cache.force_plan(16, segments)
+        cache.states(0)[:3] = _dev(np.stack([s0, -s0, 3 * s0]))
+        cache.step([2, 1, 0], lens)
+        args = (0, _bf16(q), _bf16(k), _bf16(v), _dev(g))
+        new = torch.empty(3, H, D, D, device="cuda")
+        o1 = cache.attend(*args, state_out=new)
+        o2 = cache.attend(*args)
+        assert cache.sync_status() == 0
+        assert torch.equal(o1, o2) and torch.equal(new, cache.states(0)[[2, 1, 0]])
+        at = 0
+        for i, m in enumerate(lens):
+            p = slice(at, at + m)
+            _check(_np(o1)[p], _np(new[i]), q[p], k[p], v[p], g[p], [3 * s0, -s0, s0][i])
+            at += m
+
+
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 8, 9, 16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_drafts_of_every_group_size(G, D):
+    lens = [1, 2, 7, 8, 9, 17, 3]
+    n = sum(lens)
+    q, k, v, g, s0 = _inputs(n, 2 * G, 2, D, G)
+    with _cache(head_dim=D, n_q_heads=2 * G, n_kv_heads=2, max_seqs=7) as cache:
+        cache.force_plan(32)
+        cache.states(0)[:] = _dev(s0)
+        cache.step(list(range(7)), lens)
+        o = _np(cache.attend(0, _bf16(q), _bf16(k), _bf16(v), _dev(g)))
+        s, at = _np(cache.states(0)), 0
+        for i, m in enumerate(lens):
+            p = slice(at, at + m)
+            want, sw, oa, sa, e = R.attend(q[p], k[p], v[p], g[p], s0, D ** -0.5)
+            assert (np.abs(o[p] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -14 * oa).all()     # all in fp32
+            assert (np.abs(s[i] - sw) <= 1.01 * e + 2.0 ** -22 * sa).all()
+            at += m
 
 
 def test_the_same_inputs_give_the_same_bits():
