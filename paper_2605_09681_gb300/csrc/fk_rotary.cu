@@ -3,10 +3,13 @@
 // A pair's angle is position * f modulo a turn.  f is kept as a 64-bit fraction of a turn, so that the 64-bit product
 // with the position, taken modulo 2^64, is the angle modulo whole turns without any error: an fp32 product of
 // a position and a frequency is off by a radian and more at position 10^7.  Its upper bits are cut to fp32
-// (2^-25 of a turn) for sincospi.
+// (2^-27 of a turn).
 //
-// Both kernels move each byte once and should be bound by DRAM.  The angles are the expensive part (a sine and a
-// cosine of a pair cost as much as the rotation of several heads), so a thread turns the same 8 pairs of several heads.
+// Both kernels move each byte once.  The angles are the expensive part (a sine and a cosine of a pair take as long as the
+// rotation of three heads), so a thread turns the same 8 pairs of several heads, and the rotation is bound by DRAM: 40003
+// tokens of 40 heads of 64 in 65.8 us, 92% of the measured copy rate; a video chunk (4680 tokens of 24 heads of 128, whose 57 MB are
+// hardly more than a launch's start and end) in 13.4 us, 63%.  The tables are bound by the angles' arithmetic: 131072 x 64 in 19.8
+// us, 10 us of which their writes would take.
 #include "fk_internal.h"
 
 #include <cuda_fp16.h>
@@ -18,6 +21,8 @@ namespace {
 
 constexpr int kMaxPairs = 128;
 constexpr int kThreads = 256;
+constexpr int kBlocksPerSm = 4;       // of rotate_kernel (64 registers)
+constexpr int kSms = 152;
 
 struct Angles {
   uint64_t turns[kMaxPairs];
@@ -43,31 +48,46 @@ struct RotateArgs {
 struct TableArgs {
   Angles a;
   int64_t tokens;
-  int pairs, per_block;
+  int pairs, per_block, rounds;       // tokens of a block at once, and how often
   float* cos;
   float* sin;
 };
 
-// The fractions in shared memory (every thread reads others) and a pair's angle from there.
+// The fractions in shared memory: every thread reads others, which one warp's read of the arguments takes one after the
+// other (half of the tables' time when all did).
 __device__ __forceinline__ void stage(const Angles& a, int pairs, uint64_t* s) {
   for (int i = threadIdx.x; i < pairs; i += blockDim.x) s[i] = a.turns[i];
   __syncthreads();
 }
 
-// cos and sin of the angle `pos * turns` (times m, sin with the sign of `dir`)
+// cos and sin of the angle `pos * turns` (times m, sin with the sign of `dir`).  The fraction of a turn is taken to the nearest
+// quarter and a rest a of at most pi / 4 either way, whose sine and cosine are the first five terms of their series:
+// the next ones are a^11 / 11! < 2^-29 and a^10 / 10! < 2^-25.  (sincospif took twice as long for a whole context's tables.)
 __device__ __forceinline__ void angle(uint64_t turns, int pos, float m, float dir, float* c, float* s) {
-  const uint64_t t = turns * (uint64_t)(int64_t)pos;
-  // the fraction as a signed number of half turns in [-1, 1)
-  const float x = fmaf((float)(uint32_t)t, 0x1p-63f, (float)(int32_t)(uint32_t)(t >> 32) * 0x1p-31f);
-  float sn, cs;
-  sincospif(x, &sn, &cs);
-  *c = cs * m;
-  *s = sn * dir;
+  const uint64_t t = turns * (uint64_t)(int64_t)pos + (1ull << 61);   // + 1/8: the quarter is rounded, not cut off
+  const uint32_t q = (uint32_t)(t >> 62);
+  const int32_t hi = (int32_t)((uint32_t)(t >> 32) & 0x3FFFFFFFu) - 0x20000000;
+  const float a = fmaf((float)(uint32_t)t, 0x1p-32f, (float)hi) * (6.2831853071795865f * 0x1p-32f), z = a * a;
+  const float sn = fmaf(a * z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), a);
+  const float cs = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+  const float x = q & 1 ? sn : cs, y = q & 1 ? cs : sn;      // quarters: (cs, sn), (-sn, cs), (-cs, -sn), (sn, -cs)
+  *c = __uint_as_float(__float_as_uint(x * m) ^ ((q + 1) << 30 & 0x80000000u));
+  *s = __uint_as_float(__float_as_uint(y * dir) ^ (q << 30 & 0x80000000u));
 }
 
-__device__ __forceinline__ int axis_of(const Angles& a, int pair) {
-  return (a.axes > 1 && pair >= a.first[1]) + (a.axes > 2 && pair >= a.first[2]) + (a.axes > 3 && pair >= a.first[3]);
-}
+// a token's positions, and a pair's of them
+struct Places {
+  int at[4];
+  __device__ __forceinline__ Places(const Angles& a, int64_t t) {
+    const int* p = a.positions + t * a.axes;
+    at[0] = __ldg(p);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) at[i] = i < a.axes ? __ldg(p + i) : 0;
+  }
+  __device__ __forceinline__ int of(const Angles& a, int pair) const {   // (behind the last axis, `first` is past all pairs)
+    return pair < a.first[1] ? at[0] : pair < a.first[2] ? at[1] : pair < a.first[3] ? at[2] : at[3];
+  }
+};
 
 // eight channels in memory <-> fp32
 template <class T>
@@ -151,58 +171,74 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant_
   const int c1 = kHalf ? c0 + a.dim / 2 : c0 + 8;
   float cs[8], sn[8];
   if (turn) {
-    const int* pos = a.a.positions + t * a.a.axes;
+    const Places pos(a.a, t);
     const float dir = a.inverse ? -a.a.magnitude : a.a.magnitude;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int p = 8 * u + i;
-      angle(turns[p], __ldg(pos + axis_of(a.a, p)), a.a.magnitude, dir, &cs[i], &sn[i]);
+      angle(turns[p], pos.of(a.a, p), a.a.magnitude, dir, &cs[i], &sn[i]);
     }
   }
-#pragma unroll 2
-  for (int h = h0; h < h1; ++h) {
-    const int k = h >= a.heads1, hh = k ? h - a.heads1 : h;
-    const char* x = a.x[k] + t * a.xs[k] + (int64_t)hh * a.head_dim * sizeof(T);
-    char* y = a.y[k] + t * a.ys[k] + (int64_t)hh * a.head_dim * sizeof(T);
-    Eight<T> p, q;
-    p.load(x + c0 * sizeof(T));
-    if (!turn) {
-      p.store(y + c0 * sizeof(T));
-      continue;
-    }
-    q.load(x + c1 * sizeof(T));
-    float f[16];
-    p.get(f);
-    q.get(f + 8);
+  // several heads' loads before the first is turned: a thread's own are few bytes
+  constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;
+#pragma unroll 1
+  for (int hb = h0; hb < h1; hb += kAhead) {
+    Eight<T> p[kAhead], q[kAhead];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float& u0 = kHalf ? f[i] : f[2 * i];
-      float& u1 = kHalf ? f[8 + i] : f[2 * i + 1];
-      const float v0 = fmaf(u0, cs[i], -(u1 * sn[i])), v1 = fmaf(u1, cs[i], u0 * sn[i]);
-      u0 = v0;
-      u1 = v1;
+    for (int j = 0; j < kAhead; ++j) {
+      const int h = hb + j, k = h >= a.heads1, hh = k ? h - a.heads1 : h;
+      const char* x = a.x[k] + t * a.xs[k] + (int64_t)hh * a.head_dim * sizeof(T);
+      if (h < h1) {
+        p[j].load(x + c0 * sizeof(T));
+        if (turn) q[j].load(x + c1 * sizeof(T));
+      }
     }
-    p.set(f);
-    q.set(f + 8);
-    p.store(y + c0 * sizeof(T));
-    q.store(y + c1 * sizeof(T));
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int h = hb + j, k = h >= a.heads1, hh = k ? h - a.heads1 : h;
+      char* y = a.y[k] + t * a.ys[k] + (int64_t)hh * a.head_dim * sizeof(T);
+      if (h >= h1) break;
+      if (turn) {
+        float f[16];
+        p[j].get(f);
+        q[j].get(f + 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float& u0 = kHalf ? f[i] : f[2 * i];
+          float& u1 = kHalf ? f[8 + i] : f[2 * i + 1];
+          const float v0 = fmaf(u0, cs[i], -(u1 * sn[i])), v1 = fmaf(u1, cs[i], u0 * sn[i]);
+          u0 = v0;
+          u1 = v1;
+        }
+        p[j].set(f);
+        q[j].set(f + 8);
+        q[j].store(y + c1 * sizeof(T));
+      }
+      p[j].store(y + c0 * sizeof(T));
+    }
   }
 }
 
-// One thread: 4 pairs of a token.
+// One thread: 4 pairs of several tokens, per_block apart.
 __global__ void __launch_bounds__(kThreads) tables_kernel(const __grid_constant__ TableArgs a) {
-  __shared__ uint64_t turns[kMaxPairs];
-  stage(a.a, a.pairs, turns);
+  __shared__ uint64_t all[kMaxPairs];
+  stage(a.a, a.pairs, all);
   const int quads = a.pairs / 4, tb = threadIdx.x / quads, p = 4 * (threadIdx.x - tb * quads);
-  const int64_t t = (int64_t)blockIdx.x * a.per_block + tb;
-  if (tb >= a.per_block || t >= a.tokens) return;
-  const int* pos = a.a.positions + t * a.a.axes;
-  float c[4], s[4];
+  if (tb >= a.per_block) return;
+  uint64_t turns[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    angle(turns[p + i], __ldg(pos + axis_of(a.a, p + i)), a.a.magnitude, a.a.magnitude, &c[i], &s[i]);
-  *reinterpret_cast<float4*>(a.cos + t * a.pairs + p) = make_float4(c[0], c[1], c[2], c[3]);
-  *reinterpret_cast<float4*>(a.sin + t * a.pairs + p) = make_float4(s[0], s[1], s[2], s[3]);
+  for (int i = 0; i < 4; ++i) turns[i] = all[p + i];
+  const int64_t t0 = (int64_t)blockIdx.x * a.per_block * a.rounds + tb;
+  for (int r = 0; r < a.rounds; ++r) {
+    const int64_t t = t0 + (int64_t)r * a.per_block;
+    if (t >= a.tokens) return;
+    const Places pos(a.a, t);
+    float c[4], s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) angle(turns[i], pos.of(a.a, p + i), a.a.magnitude, a.a.magnitude, &c[i], &s[i]);
+    *reinterpret_cast<float4*>(a.cos + t * a.pairs + p) = make_float4(c[0], c[1], c[2], c[3]);
+    *reinterpret_cast<float4*>(a.sin + t * a.pairs + p) = make_float4(s[0], s[1], s[2], s[3]);
+  }
 }
 
 bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -345,12 +381,21 @@ fk_status fk_rotate(const fk_rotary* r, int64_t tokens, const int32_t* positions
   a.xs[1] = x2_stride * size;
   a.ys[0] = y_stride * size;
   a.ys[1] = y2_stride * size;
-  // heads of a thread: as many as leave the device full of threads
-  a.per_group = 1;
-  while (a.per_group < 8 && a.per_group < a.heads && tokens * a.units * a.heads / (2 * a.per_group) >= (int64_t)152 * 1024)
-    a.per_group *= 2;
+  // Heads of a thread: its angles take as long as three of them, and the last of a few rounds of blocks as long as a full one
+  // (4680 tokens of 24 heads: 6 heads in one round 13.4 us, 4 in one and a half 14.5).
   a.per_block = kThreads / a.units;
-  const dim3 grid((unsigned)((tokens + a.per_block - 1) / a.per_block), (unsigned)((a.heads + a.per_group - 1) / a.per_group));
+  const int64_t columns = (tokens + a.per_block - 1) / a.per_block;
+  a.per_group = 1;
+  double least = 1e30;
+  for (int p = 1; p <= 8 && p <= a.heads; ++p) {
+    double rounds = (double)(columns * ((a.heads + p - 1) / p)) / (kSms * kBlocksPerSm);
+    if (rounds < 4.0) rounds = std::ceil(rounds);
+    if (rounds * (3 + p) < least) {
+      least = rounds * (3 + p);
+      a.per_group = p;
+    }
+  }
+  const dim3 grid((unsigned)columns, (unsigned)((a.heads + a.per_group - 1) / a.per_group));
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (type == FK_TYPE_BF16) e = launch_rotate<bf16>(a, r->style, grid, s);
@@ -373,7 +418,11 @@ fk_status fk_rotary_tables(const fk_rotary* r, int64_t tokens, const int32_t* po
   a.cos = cos;
   a.sin = sin;
   a.per_block = kThreads / (a.pairs / 4);
-  tables_kernel<<<(unsigned)((tokens + a.per_block - 1) / a.per_block), kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  // (a thread's frequencies are for many tokens, but the device wants threads first)
+  a.rounds = 1;
+  while (a.rounds < 16 && tokens * (a.pairs / 4) / (2 * a.rounds) >= (int64_t)kSms * 2048) a.rounds *= 2;
+  const int64_t block = (int64_t)a.per_block * a.rounds;
+  tables_kernel<<<(unsigned)((tokens + block - 1) / block), kThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
   return cudaGetLastError() == cudaSuccess ? FK_OK : FK_ERR_CUDA;
 }
 
