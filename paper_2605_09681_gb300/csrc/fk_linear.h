@@ -43,6 +43,7 @@ struct LinearChunkSeqs {
   int tok0[kLinearSeqs];
   int len[kLinearSeqs];               // at least 1
   int segs[kLinearSeqs];              // segments of a head
+  int per[kLinearSeqs];               // chunks of a segment, rounded down
   int place0[kLinearSeqs];            // its states' places in the workspace, where segs > 1: place0 + head * segs + segment
   int item0[kLinearSeqs + 1];         // items before the sequence's first one
 };
@@ -63,6 +64,7 @@ struct LinearChunkArgs {
   float* place;                       // [places][D][D]: the state before a segment
   float* place_decay;                 // [places]: what the segment before it leaves of a state
   int* status;
+  int items, ctas;                    // work items, CTAs that take them in turn
   LinearChunkSeqs seqs;
 };
 cudaError_t linear_chunk_prepare(int D);

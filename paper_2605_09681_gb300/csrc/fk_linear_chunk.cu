@@ -27,6 +27,8 @@
 #include "fk_linear.h"
 #include "fk_tc.h"
 
+#include <algorithm>
+
 namespace fk {
 namespace {
 
@@ -158,6 +160,65 @@ __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0
 // a whole number of 2^-32 as fp32
 __device__ __forceinline__ float of_fixed(int64_t x) { return fmaf((float)(uint32_t)x, 0x1p-32f, (float)(int32_t)(x >> 32)); }
 
+// A segment of one kv head of a sequence.
+struct Item {
+  int s, seg, segs, kvh;
+  int nc, tokens;                     // chunks, at least one, and tokens
+  int64_t tok0, place;
+};
+__device__ __forceinline__ Item item_of(const LinearChunkArgs& a, int i) {
+  Item t;
+  int lo = 0, hi = a.seqs.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.seqs.item0[mid] <= i) lo = mid;
+    else hi = mid - 1;
+  }
+  t.s = lo;
+  t.segs = a.seqs.segs[lo];
+  i -= a.seqs.item0[lo];
+  t.seg = (int)((unsigned)i / (unsigned)a.Hkv);
+  t.kvh = i - t.seg * a.Hkv;
+  // per chunks to a segment, one more to the first of them
+  const int len = a.seqs.len[lo], per = a.seqs.per[lo], more = (int)((unsigned)(len + C - 1) / C) - per * t.segs;
+  const int c0 = t.seg * per + min(t.seg, more);
+  t.nc = per + (t.seg < more);
+  t.tok0 = (int64_t)a.seqs.tok0[lo] + (int64_t)c0 * C;
+  t.tokens = min(len - c0 * C, t.nc * C);
+  t.place = (int64_t)a.seqs.place0[lo] + t.kvh * t.segs + t.seg;
+  return t;
+}
+// The items of a CTA: one of each round of gridDim.x, forth and back, so that the longest of one round meets the shortest of the
+// next (they come longest first).
+__device__ __forceinline__ int item_at(int round) {
+  const int g = gridDim.x, b = blockIdx.x;
+  return round * g + (round & 1 ? g - 1 - b : b);
+}
+
+// A warp's 32 rows of D floats, row r of lane r, from and to rows that lie one after the other in memory: 128 bytes of 4 rows
+// at a time there, turned through 4 KB of shared memory.  (With each lane at its own row an access touches 32 lines: 4 us for
+// both ways of a state of 64 KB.)
+template <int D>
+__device__ __forceinline__ void turn(float* st, uint8_t* tile, int lane, bool to_rows) {
+  float4* v = reinterpret_cast<float4*>(st);
+#pragma unroll
+  for (int q = 0; q < D / 32; ++q) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = to_rows ? 4 * i + (lane >> 3) : lane, c = to_rows ? lane & 7 : i;
+      *reinterpret_cast<float4*>(tile + r * 128 + ((c ^ (r & 7)) << 4)) = v[8 * q + i];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = to_rows ? lane : 4 * i + (lane >> 3), c = to_rows ? i : lane & 7;
+      v[8 * q + i] = *reinterpret_cast<const float4*>(tile + r * 128 + ((c ^ (r & 7)) << 4));
+    }
+  }
+  __syncwarp();
+}
+
 template <int D, bool kLocal>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -177,30 +238,16 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
   // (the compiler takes what a shuffle or a vote gives for the same in all lanes: branches by it stay plain branches)
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
-  // ---- this CTA's segment
-  int s = 0;
-  {
-    int hi = a.seqs.n - 1;
-    while (s < hi) {
-      const int mid = (s + hi + 1) >> 1;
-      if (a.seqs.item0[mid] <= (int)blockIdx.x) s = mid;
-      else hi = mid - 1;
-    }
-  }
-  const int segs = a.seqs.segs[s], item = (int)blockIdx.x - a.seqs.item0[s];
-  const int seg = item / a.Hkv, kvh = item - seg * a.Hkv;
-  const int len = a.seqs.len[s], chunks = (len + C - 1) / C;
-  const int c0 = (int)((int64_t)chunks * seg / segs), nc = (int)((int64_t)chunks * (seg + 1) / segs) - c0;   // nc >= 1
-  const int64_t tok0 = (int64_t)a.seqs.tok0[s] + (int64_t)c0 * C;   // of the segment
-  const int tokens = min(len - c0 * C, nc * C);
   const int G = kLocal ? 1 : a.G;
-  const int64_t place = (int64_t)a.seqs.place0[s] + kvh * segs + seg;
+  // Every role takes the CTA's items one after the other, and their chunks: chunk c, and c G + g its products with query head g, count
+  // on from item to item, and so do the barriers' phases; nothing waits for an item to end.
+  const Item first = item_of(a, blockIdx.x);
 
   // The loading warp makes the barriers and asks for the first tiles before the CTA meets (which takes 1700 cycles: the
   // allocation of tensor memory).
-  auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int n) {   // one lane
+  auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* b, int head, int64_t tok) {   // one lane
     mbar_expect_tx(b, Lay::kTile);
-    for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)(tok0 + n * C));
+    for (int p = 0; p < kPanels; ++p) tma_load_2d(dst + p * (C * 128), map, b, head * D + p * 64, (int)tok);
   };
   if (warp == 3 && lane == 0) {
     for (const CUtensorMap* map : {&tmK, &tmV, &tmQ, &tmO}) asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
@@ -232,9 +279,9 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     mbar_init(&bar->fin, 1);
     bar->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    load(&tmK, sK, &bar->k_full[0], kvh, 0);
-    if (!kLocal) load(&tmQ, sQ, &bar->q_full[0], kvh * G, 0);
-    load(&tmV, sV, &bar->v_full[0], kvh, 0);
+    load(&tmK, sK, &bar->k_full[0], first.kvh, first.tok0);
+    if (!kLocal) load(&tmQ, sQ, &bar->q_full[0], first.kvh * G, first.tok0);
+    load(&tmV, sV, &bar->v_full[0], first.kvh, first.tok0);
   }
   if (warp == 1) {
     __syncwarp();
@@ -243,18 +290,18 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   // decays of a chunk (warp 2, lane's tokens 4 lane .. + 3), three chunks ahead: one chunk's time is less than a load takes
-  const float* decay = a.decay + tok0 * a.dstride + kvh;
   float ahead[3][4];
-  auto fetch = [&](int n, float* x) {
+  auto fetch = [&](const Item& it, int n, float* x) {
+    const float* decay = a.decay + it.tok0 * a.dstride + it.kvh;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = n * C + 4 * lane + i;
-      x[i] = t < tokens ? __ldg(decay + (int64_t)t * a.dstride) : 0.0f;
+      x[i] = t < it.tokens ? __ldg(decay + (int64_t)t * a.dstride) : 0.0f;
     }
   };
   if (warp == 2) {
 #pragma unroll
-    for (int i = 0; i < 3; ++i) fetch(i, ahead[i]);
+    for (int i = 0; i < 3; ++i) fetch(first, i, ahead[i]);
   }
   tc_fence_before();
   __syncthreads();
@@ -277,28 +324,35 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       // ------------------------------------------------------------------ TMA
       bool ok = true;
       int ik = 0, iv = 0, iq = kLocal ? -1 : 0;              // last tiles issued
+      int base = 0;                                          // chunks of the items before
 #pragma unroll 1
-      for (int n = 0; n < nc && ok; ++n) {
-        const int b = n % kStages, u = n / kStages;
-        if (u > 0 && !(ok = wait_for(&bar->k_empty[b], u - 1))) break;
-        if (lane == 0 && n > 0) load(&tmK, sK + b * (2 * Lay::kTile), &bar->k_full[b], kvh, n);
-        __syncwarp();
-        ik = n;
+      for (int round = 0; ok && item_at(round) < a.items; ++round) {
+        const Item it = item_of(a, item_at(round));
 #pragma unroll 1
-        for (int g = 0; g < (kLocal ? 1 : G); ++g) {
-          if (!kLocal) {
-            const int m = n * G + g, qb = m & 1, qu = m >> 1;
-            if (qu > 0 && !(ok = wait_for(&bar->q_empty[qb], qu - 1))) break;
-            if (lane == 0 && m > 0) load(&tmQ, sQ + qb * Lay::kTile, &bar->q_full[qb], kvh * G + g, n);
-            __syncwarp();
-            iq = m;
-          }
-          if (g > 0) continue;
-          if (u > 0 && !(ok = wait_for(&bar->v_empty[b], u - 1))) break;
-          if (lane == 0 && n > 0) load(&tmV, sV + b * (2 * Lay::kTile), &bar->v_full[b], kvh, n);
+        for (int n = 0; n < it.nc && ok; ++n) {
+          const int c = base + n, b = c % kStages, u = c / kStages;
+          const int64_t tok = it.tok0 + n * C;
+          if (u > 0 && !(ok = wait_for(&bar->k_empty[b], u - 1))) break;
+          if (lane == 0 && c > 0) load(&tmK, sK + b * (2 * Lay::kTile), &bar->k_full[b], it.kvh, tok);
           __syncwarp();
-          iv = n;
+          ik = c;
+#pragma unroll 1
+          for (int g = 0; g < (kLocal ? 1 : G); ++g) {
+            if (!kLocal) {
+              const int m = c * G + g, qb = m & 1, qu = m >> 1;
+              if (qu > 0 && !(ok = wait_for(&bar->q_empty[qb], qu - 1))) break;
+              if (lane == 0 && m > 0) load(&tmQ, sQ + qb * Lay::kTile, &bar->q_full[qb], it.kvh * G + g, tok);
+              __syncwarp();
+              iq = m;
+            }
+            if (g > 0) continue;
+            if (u > 0 && !(ok = wait_for(&bar->v_empty[b], u - 1))) break;
+            if (lane == 0 && c > 0) load(&tmV, sV + b * (2 * Lay::kTile), &bar->v_full[b], it.kvh, tok);
+            __syncwarp();
+            iv = c;
+          }
         }
+        base += it.nc;
       }
       if (!ok) {                                             // what was issued lands before the CTA ends
 #pragma unroll 1
@@ -346,6 +400,9 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
         return true;
       };
+      int chunks = 0;                                        // of all items
+#pragma unroll 1
+      for (int round = 0; item_at(round) < a.items; ++round) chunks += item_of(a, item_at(round)).nc;
       bool ok = true;
       if (!kLocal && (ok = wait_for(&bar->k_full[0], 0) && wait_for(&bar->q_full[0], 0))) {
         tc_fence_after();
@@ -353,7 +410,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         __syncwarp();
       }
 #pragma unroll 1
-      for (int n = 0; n < nc && ok; ++n) {
+      for (int n = 0; n < chunks && ok; ++n) {
         if (!(ok = wait_for(&bar->v_full[n % kStages], n / kStages))) break;
         if (n > 0 && !(ok = wait_for(&bar->ds_empty, n - 1))) break;
         if (!(ok = half_ds(n, 0))) break;
@@ -381,7 +438,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             if (g == G - 1) umma_commit(&bar->v_empty[n & 1]);
           }
           __syncwarp();
-          if (m + 1 < nc * G) {                              // the next A
+          if (m + 1 < chunks * G) {                          // the next A
             const int n1 = g + 1 < G ? n : n + 1;
             if (n1 > n && !(ok = wait_for(&bar->k_full[n1 & 1], n1 >> 1))) break;
             if (!(ok = wait_for(&bar->q_full[(m + 1) & 1], (m + 1) >> 1))) break;
@@ -396,9 +453,18 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       __syncwarp();
     } else if (warp == 2) {
       // ------------------------------------------------------------------ running sums of a chunk
+      int base = 0;
+      bool ok = true;
 #pragma unroll 1
-      for (int n = 0; n < nc; ++n) {
-        const int b = n & 1, u = n >> 1;
+      for (int round = 0; ok && item_at(round) < a.items; ++round) {
+      const Item it = item_of(a, item_at(round));
+      if (round > 0) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) fetch(it, i, ahead[i]);
+      }
+#pragma unroll 1
+      for (int n = 0; n < it.nc; ++n) {
+        const int c = base + n, b = c & 1, u = c >> 1;
         // whole numbers of 2^-32: sums and their differences are exact however far they run (2^-33 a token is 2^-26 at most for a
         // chunk, of a logarithm); what is not a number makes all sums from its token on that
         int64_t sum[4];
@@ -426,7 +492,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           ahead[0][i] = ahead[1][i];
           ahead[1][i] = ahead[2][i];
         }
-        fetch(n + 3, ahead[2]);
+        fetch(it, n + 3, ahead[2]);
         // the sum at the end of this lane's 32 tokens, unless the chunk grows
         const int64_t r = __shfl_sync(0xffffffffu, all, lane | 7), from = grow ? end : r;
         const float nan = __int_as_float(0x7FFFFFFF);
@@ -437,7 +503,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           gg[i] = 4 * lane + i >= lost ? nan : of_fixed(x);
           v[i] = lost < C ? nan : exp2f(of_fixed(from - x));
         }
-        if (u > 0 && !wait_for(&bar->g_empty[b], u - 1)) break;
+        if (u > 0 && !(ok = wait_for(&bar->g_empty[b], u - 1))) break;
         Sums& out = sums[b];
         *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(gg[0], gg[1], gg[2], gg[3]);
         *reinterpret_cast<float4*>(out.u + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
@@ -448,11 +514,19 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
         arrive(&bar->g_full[b]);
       }
+      base += it.nc;
+      }
     } else if (!kLocal) {
       // ------------------------------------------------------------------ is V finite
-      for (int n = 0; n < nc; ++n) {
-        const int b = n & 1, u = n >> 1, valid = min(C, tokens - n * C);
-        if (!wait_for(&bar->v_full[b], u)) break;
+      int base = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (int round = 0; ok && item_at(round) < a.items; ++round) {
+      const Item it = item_of(a, item_at(round));
+#pragma unroll 1
+      for (int n = 0; n < it.nc; ++n) {
+        const int c = base + n, b = c & 1, u = c >> 1, valid = min(C, it.tokens - n * C);
+        if (!(ok = wait_for(&bar->v_full[b], u))) break;
         // 0 times a value is NaN where it is not finite; 8 runs of 16 bytes to a row of a panel
         uint32_t z[4] = {0, 0, 0, 0};
 #pragma unroll 4
@@ -464,11 +538,13 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           z[2] = zero_times(v.z, z[2]);
           z[3] = zero_times(v.w, z[3]);
         }
-        if (u > 0 && !wait_for(&bar->odd_empty[b], u - 1)) break;
+        if (u > 0 && !(ok = wait_for(&bar->odd_empty[b], u - 1))) break;
         const bool odd = __any_sync(0xffffffffu, ((z[0] | z[1] | z[2] | z[3]) & 0x7FFF7FFFu) != 0);
         if (lane == 0) bar->odd[b] = (int)odd;
         arrive(&bar->odd_full[b]);
         arrive(&bar->v_empty[b]);
+      }
+      base += it.nc;
       }
     }
   } else if (warp < 12) {
@@ -477,13 +553,18 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     const int w2 = (warp >> 2) - 1;                          // which of the two warpgroups
     const bool mine = 32 * wq < D;                           // D = 64: lanes 64-127 of dS are not used
     bool ok = true;
-    for (int n = 0; n < nc && ok; ++n) {
-      const int b = n & 1, u = n >> 1, valid = min(C, tokens - n * C);
+    int base = 0;
+#pragma unroll 1
+    for (int round = 0; ok && item_at(round) < a.items; ++round) {
+    const Item it = item_of(a, item_at(round));
+#pragma unroll 1
+    for (int n = 0; n < it.nc && ok; ++n) {
+      const int c = base + n, b = c & 1, u = c >> 1, valid = min(C, it.tokens - n * C);
       const Sums& sm = sums[b];
-      const int bk = n % kStages;                            // stage of K and V
-      if (!(ok = wait_for(&bar->k_full[bk], n / kStages) && wait_for(&bar->g_full[b], u))) break;
+      const int bk = c % kStages;                            // stage of K and V
+      if (!(ok = wait_for(&bar->k_full[bk], c / kStages) && wait_for(&bar->g_full[b], u))) break;
       if (valid < C) {                                       // rows of others: zeros for the products with V
-        if (!(ok = wait_for(&bar->v_full[bk], n / kStages))) break;
+        if (!(ok = wait_for(&bar->v_full[bk], c / kStages))) break;
         const int p = wq >> 1, r = 64 * (wq & 1) + 32 * w2 + lane;   // panel, token of this warpgroup's
         if (r >= valid && p < kPanels) {
 #pragma unroll 1
@@ -499,7 +580,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll 1
       for (int step = 0; step < (kLocal ? 2 : G + 2) && ok; ++step) {
         if (step == 0 || step == (kLocal ? 1 : 2)) {
-          const int q = step == 0 ? w2 : w2 + 2, buf = q % kBufs, use = n * (4 / kBufs) + q / kBufs;
+          const int q = step == 0 ? w2 : w2 + 2, buf = q % kBufs, use = c * (4 / kBufs) + q / kBufs;
           if (use > 0 && !(ok = wait_for(&bar->kp_empty[buf], use - 1))) break;
           tc_fence_after();
           if (mine) {
@@ -511,9 +592,9 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             const int r = lane & 7, mat = lane >> 3;
 #pragma unroll 1
             for (int hf = 0; hf < 2; ++hf) {
-              const int c = 32 * wq + 16 * hf + (mat & 1) * 8;   // channel of the row that this lane gives ldmatrix
-              const uint32_t at = su32(sK) + (uint32_t)(bk * (2 * Lay::kTile) + (c >> 6) * (C * 128) + (32 * q + (mat >> 1) * 8 + r) * 128 +
-                                                        ((((c & 63) >> 3) ^ r) << 4));
+              const int ch = 32 * wq + 16 * hf + (mat & 1) * 8;  // channel of the row that this lane gives ldmatrix
+              const uint32_t at = su32(sK) + (uint32_t)(bk * (2 * Lay::kTile) + (ch >> 6) * (C * 128) + (32 * q + (mat >> 1) * 8 + r) * 128 +
+                                                        ((((ch & 63) >> 3) ^ r) << 4));
               uint32_t x[8], hi[8], mid[8], lo[8];
               ldmatrix4t(at, x);
               ldmatrix4t(at + 16 * 128, x + 4);
@@ -545,7 +626,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (step > 0) arrive(&bar->k_empty[bk]);
           continue;
         }
-        if (!(ok = wait_for(&bar->a_full, n * G + (step < 2 ? 0 : step - 2)))) break;
+        if (!(ok = wait_for(&bar->a_full, c * G + (step < 2 ? 0 : step - 2)))) break;
         tc_fence_after();
         // below the diagonal A f u_j with f of the row, on it A exp(G_i - G_j), scaled
 #pragma unroll 1
@@ -595,100 +676,125 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       }
       if (ok) arrive(&bar->g_empty[b]);
     }
+    base += it.nc;
+    }
   } else if (warp < 16) {
     more_registers<kRegsState>();
     // ------------------------------------------------------------------ the state
     const bool mine = 32 * wq < D;
-    float st[D];
-    float left = 1.0f;                                       // what the segment leaves of a state
-    if (kLocal || !mine) {
-#pragma unroll
-      for (int i = 0; i < D; ++i) st[i] = 0.0f;
-    } else {
-      const float* from = (segs > 1 ? a.place + place * (D * D) : a.state + ((int64_t)a.seqs.slot[s] * a.Hkv + kvh) * (D * D)) + row * D;
-#pragma unroll
-      for (int i = 0; i < D; i += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(from + i);
-        st[i] = v.x, st[i + 1] = v.y, st[i + 2] = v.z, st[i + 3] = v.w;
-      }
-    }
-    // State n is formed from dS of chunk n - 1 and written, 32 columns at a time.
+    const int at = (32 * wq + (lane >> 3)) * D + (lane & 7) * 4;   // of a state, in memory: rows 4 i + lane / 8 of the warp's
     bool ok = true;
+    int base = 0;
 #pragma unroll 1
-    for (int n = 0; n <= nc; ++n) {
-      float e = 1.0f;
-      if (n > 0) {
-        const int b = (n - 1) & 1;
-        if (!(ok = wait_for(&bar->g_full[b], (n - 1) >> 1))) break;
-        e = sums[b].e;
-        arrive(&bar->g_empty[b]);
-        left *= e;
-        // every X of the chunk (each phase is seen): S's place is free, and further query heads' X may follow
-#pragma unroll 1
-        for (int g = 0; g < G && !kLocal && ok; ++g) {
-          if (g > 0) arrive(&bar->x_ready);
-          ok = wait_for(&bar->x_full, (n - 1) * G + g);
+    for (int round = 0; ok && item_at(round) < a.items; ++round) {
+      const Item it = item_of(a, item_at(round));
+      auto from = [&](const Item& t) {
+        return (t.segs > 1 ? a.place + t.place * (D * D) : a.state + ((int64_t)a.seqs.slot[t.s] * a.Hkv + t.kvh) * (D * D)) + at;
+      };
+      alignas(16) float st[D];
+      float left = 1.0f;                                     // what the segment leaves of a state
+      if (kLocal || !mine) {
+#pragma unroll
+        for (int i = 0; i < D; ++i) st[i] = 0.0f;
+      } else {
+        const float* x = from(it);
+#pragma unroll
+        for (int i = 0; i < D / 4; ++i) {                    // 4 rows of 32 columns at a time
+          const float4 v = *reinterpret_cast<const float4*>(x + (i >> 3) * 32 + (i & 7) * (4 * D));
+          st[4 * i] = v.x, st[4 * i + 1] = v.y, st[4 * i + 2] = v.z, st[4 * i + 3] = v.w;
         }
-        if (!ok || !(ok = wait_for(&bar->ds_full, n - 1))) break;
-        tc_fence_after();
-      }
-      if (mine) {
+        turn<D>(st, sS + wq * 4096, lane, true);             // (S's place: no X is on its way)
+        if (item_at(round + 1) < a.items) {                  // the next item's state on its way to L2
+          const float* y = from(item_of(a, item_at(round + 1)));
 #pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
-          if (n > 0) {
-            uint32_t x[32];
-            FK_TMEM_LD32(lanes + kColS + 32 * q, x);
-            FK_TMEM_WAIT_LD32(x);
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const float2 y = ffma2(make_float2(st[32 * q + i], st[32 * q + i + 1]), make_float2(e, e),
-                                     make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
-              st[32 * q + i] = y.x;
-              st[32 * q + i + 1] = y.y;
-            }
-          }
-          if (!kLocal) {
-#pragma unroll
-            for (int i = 4 * q; i < 4 * q + 4; ++i) {
-              const uint4 v = make_uint4(pack_bf16(st[8 * i], st[8 * i + 1]), pack_bf16(st[8 * i + 2], st[8 * i + 3]),
-                                         pack_bf16(st[8 * i + 4], st[8 * i + 5]), pack_bf16(st[8 * i + 6], st[8 * i + 7]));
-              *reinterpret_cast<uint4*>(sS + (i >> 3) * (D * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = v;
-            }
-          }
+          for (int i = 0; i < D / 4; ++i)
+            if ((lane & 7) == 0) asm volatile("prefetch.global.L2 [%0];" :: "l"(y + (i >> 3) * 32 + (i & 7) * (4 * D)));
         }
       }
-      if (n > 0) {
-        tc_fence_before();
-        arrive(&bar->ds_empty);
-      }
-      if (!kLocal && n < nc) {
-        fence_to_async();
-        arrive(&bar->x_ready);
-      }
-    }
-    float* to = nullptr;
-    if (kLocal) to = a.place + (place + 1) * (D * D);
-    else if (a.state_new && seg == segs - 1)
-      to = a.state_new + ((int64_t)(a.to_out ? a.seqs.out[s] : a.seqs.slot[s]) * a.Hkv + kvh) * (D * D);
-    if (ok && to && mine) {
+      // State n is formed from dS of chunk n - 1 and written, 32 columns at a time.
+#pragma unroll 1
+      for (int n = 0; n <= it.nc; ++n) {
+        const int c = base + n - 1;
+        float e = 1.0f;
+        if (n > 0) {
+          if (!(ok = wait_for(&bar->g_full[c & 1], c >> 1))) break;
+          e = sums[c & 1].e;
+          arrive(&bar->g_empty[c & 1]);
+          left *= e;
+          // every X of the chunk (each phase is seen): S's place is free, and further query heads' X may follow
+#pragma unroll 1
+          for (int g = 0; g < G && !kLocal && ok; ++g) {
+            if (g > 0) arrive(&bar->x_ready);
+            ok = wait_for(&bar->x_full, c * G + g);
+          }
+          if (!ok || !(ok = wait_for(&bar->ds_full, c))) break;
+          tc_fence_after();
+        }
+        if (mine) {
 #pragma unroll
-      for (int i = 0; i < D; i += 4) *reinterpret_cast<float4*>(to + row * D + i) = make_float4(st[i], st[i + 1], st[i + 2], st[i + 3]);
-      if (kLocal && row == 0) a.place_decay[place + 1] = left;
+          for (int q = 0; q < D / 32; ++q) {
+            if (n > 0) {
+              uint32_t x[32];
+              FK_TMEM_LD32(lanes + kColS + 32 * q, x);
+              FK_TMEM_WAIT_LD32(x);
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                const float2 y = ffma2(make_float2(st[32 * q + i], st[32 * q + i + 1]), make_float2(e, e),
+                                       make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])));
+                st[32 * q + i] = y.x;
+                st[32 * q + i + 1] = y.y;
+              }
+            }
+            if (!kLocal && n < it.nc) {
+#pragma unroll
+              for (int i = 4 * q; i < 4 * q + 4; ++i) {
+                const uint4 v = make_uint4(pack_bf16(st[8 * i], st[8 * i + 1]), pack_bf16(st[8 * i + 2], st[8 * i + 3]),
+                                           pack_bf16(st[8 * i + 4], st[8 * i + 5]), pack_bf16(st[8 * i + 6], st[8 * i + 7]));
+                *reinterpret_cast<uint4*>(sS + (i >> 3) * (D * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4)) = v;
+              }
+            }
+          }
+        }
+        if (n > 0) {
+          tc_fence_before();
+          arrive(&bar->ds_empty);
+        }
+        if (!kLocal && n < it.nc) {
+          fence_to_async();
+          arrive(&bar->x_ready);
+        }
+      }
+      float* to = nullptr;
+      if (kLocal) to = a.place + (it.place + 1) * (D * D);
+      else if (a.state_new && it.seg == it.segs - 1)
+        to = a.state_new + ((int64_t)(a.to_out ? a.seqs.out[it.s] : a.seqs.slot[it.s]) * a.Hkv + it.kvh) * (D * D);
+      if (ok && to && mine) {
+        turn<D>(st, sS + wq * 4096, lane, false);
+#pragma unroll
+        for (int i = 0; i < D / 4; ++i)
+          *reinterpret_cast<float4*>(to + at + (i >> 3) * 32 + (i & 7) * (4 * D)) = make_float4(st[4 * i], st[4 * i + 1], st[4 * i + 2], st[4 * i + 3]);
+        if (kLocal && row == 0) a.place_decay[it.place + 1] = left;
+      }
+      base += it.nc;
     }
   } else {
     fewer_registers<kRegsOut>();
     // ------------------------------------------------------------------ o
     bool ok = !kLocal, any_odd = false;
     if (!kLocal) arrive(&bar->x_ready);                      // no Y before the first X
+    int base = 0;
 #pragma unroll 1
-    for (int n = 0; n < nc && ok; ++n) {
-      const int b = n & 1, u = n >> 1, t = n * C + row;
+    for (int round = 0; ok && item_at(round) < a.items; ++round) {
+    const Item it = item_of(a, item_at(round));
+#pragma unroll 1
+    for (int n = 0; n < it.nc && ok; ++n) {
+      const int c = base + n, b = c & 1, u = c >> 1, t = n * C + row;
       if (!(ok = wait_for(&bar->g_full[b], u) && wait_for(&bar->odd_full[b], u))) break;
       const float e = exp2f(sums[b].g[row] + a.log2_scale);
       const bool odd = __any_sync(0xffffffffu, bar->odd[b]);
       for (int g = 0; g < G; ++g) {
-        const int m = n * G + g, head = kvh * G + g;
-        bf16* to = a.O + (tok0 + t) * a.ostride + (int64_t)head * D;
+        const int m = c * G + g, head = it.kvh * G + g;
+        bf16* to = a.O + (it.tok0 + t) * a.ostride + (int64_t)head * D;
         if (!(ok = wait_for(&bar->x_full, m))) break;
         tc_fence_after();
         if (!odd) {
@@ -718,7 +824,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                          : "r"(lanes + kColX + 8 * q));
             asm volatile("tcgen05.wait::ld.sync.aligned;"
                          : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]) :: "memory");
-            if (t < tokens)
+            if (t < it.tokens)
               *reinterpret_cast<uint4*>(to + 8 * q) = make_uint4(pack_bf16(e * x[0], e * x[1]), pack_bf16(e * x[2], e * x[3]),
                                                                  pack_bf16(e * x[4], e * x[5]), pack_bf16(e * x[6], e * x[7]));
           }
@@ -728,7 +834,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         arrive(&bar->y_ready);
         if (!(ok = wait_for(&bar->y_full, m))) break;
         tc_fence_after();
-        const bool whole = n * C + 32 * wq + 32 <= tokens;   // all rows of this warp
+        const bool whole = n * C + 32 * wq + 32 <= it.tokens;   // all rows of this warp
         uint8_t* tile = sQ + (m & 1) * Lay::kTile;
 #pragma unroll 1
         for (int q = 0; q < D / 32 && !odd; ++q) {
@@ -739,8 +845,8 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           for (int i = 0; i < 16; ++i) y[i] = pack_bf16(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1]));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int c = 4 * q + i;                         // run of 16 bytes
-            *reinterpret_cast<uint4*>(tile + (c >> 3) * (C * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+            const int k = 4 * q + i;                         // run of 16 bytes
+            *reinterpret_cast<uint4*>(tile + (k >> 3) * (C * 128) + row * 128 + (((k & 7) ^ (row & 7)) << 4)) =
                 make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
           }
         }
@@ -754,16 +860,16 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             for (int p = 0; p < kPanels; ++p)
               asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
                            :: "l"(&tmO), "r"(su32(tile + p * (C * 128) + wq * (32 * 128))), "r"(head * D + p * 64),
-                           "r"((int)(tok0 + n * C) + 32 * wq) : "memory");
+                           "r"((int)(it.tok0 + n * C) + 32 * wq) : "memory");
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
           }
         }
-        if (!whole && !odd && t < tokens) {                  // (the last chunk's last rows)
+        if (!whole && !odd && t < it.tokens) {               // (the last chunk's last rows)
 #pragma unroll 1
-          for (int c = 0; c < D / 8; ++c)
-            *reinterpret_cast<uint4*>(to + 8 * c) =
-                *reinterpret_cast<const uint4*>(tile + (c >> 3) * (C * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+          for (int k = 0; k < D / 8; ++k)
+            *reinterpret_cast<uint4*>(to + 8 * k) =
+                *reinterpret_cast<const uint4*>(tile + (k >> 3) * (C * 128) + row * 128 + (((k & 7) ^ (row & 7)) << 4));
         }
         arrive(&bar->q_empty[m & 1]);
       }
@@ -771,45 +877,50 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       arrive(&bar->odd_empty[b]);
       arrive(&bar->g_empty[b]);
     }
-    if (!kLocal && any_odd) {
+    base += it.nc;
+    }
+    if (!kLocal && any_odd && ok) {
       // o's terms of a chunk's own tokens, where V of the chunk is not all finite, in fp32 (a millisecond a chunk: this is for
       // inputs that went wrong)
 #pragma unroll 1
-      for (int n = 0; n < nc; ++n) {
-        const int t = n * C + row, valid = min(C, tokens - n * C);
-        bool odd = false;
-        uint32_t tile_odd;
-        for (int i = row; i < valid * (D / 8); i += 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(a.V + (tok0 + n * C + i / (D / 8)) * a.vstride + (int64_t)kvh * D + i % (D / 8) * 8);
-          odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
-        }
-        asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
-                     : "=r"(tile_odd) : "r"((uint32_t)odd) : "memory");
-        if (!tile_odd || t >= tokens) continue;
+      for (int round = 0; item_at(round) < a.items; ++round) {
+        const Item it = item_of(a, item_at(round));
 #pragma unroll 1
-        for (int g = 0; g < G; ++g) {
-          const bf16* q = a.Q + (tok0 + t) * a.qstride + (int64_t)(kvh * G + g) * D;
-          bf16* to = a.O + (tok0 + t) * a.ostride + (int64_t)(kvh * G + g) * D;
-#pragma unroll 1
-          for (int c = 0; c < D; c += 8) {
-            float o[8], d = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = __bfloat162float(to[c + i]);
-#pragma unroll 1
-            for (int j = row; j >= 0; --j) {
-              const bf16* k = a.K + (tok0 + n * C + j) * a.kstride + (int64_t)kvh * D;
-              const bf16* v = a.V + (tok0 + n * C + j) * a.vstride + (int64_t)kvh * D + c;
-              float p = 0.0f;
-#pragma unroll 1
-              for (int i = 0; i < D; ++i) p = fmaf(__bfloat162float(q[i]), __bfloat162float(k[i]), p);
-              p *= a.scale * expf(d);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] = fmaf(p, __bfloat162float(v[i]), o[i]);
-              d += at_least(__ldg(a.decay + (tok0 + n * C + j) * a.dstride + kvh), kLeastDecay);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) to[c + i] = __float2bfloat16_rn(o[i]);
+        for (int n = 0; n < it.nc; ++n) {
+          const int t = n * C + row, valid = min(C, it.tokens - n * C);
+          const int64_t tok = it.tok0 + n * C;
+          bool odd = false;
+          for (int i = lane; i < valid * (D / 8); i += 32) {
+            const uint4 v = *reinterpret_cast<const uint4*>(a.V + (tok + i / (D / 8)) * a.vstride + (int64_t)it.kvh * D + i % (D / 8) * 8);
+            odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
           }
+          if (!__any_sync(0xffffffffu, odd)) continue;
+#pragma unroll 1
+          for (int g = 0; g < G && t < it.tokens; ++g) {
+            const bf16* q = a.Q + (tok + row) * a.qstride + (int64_t)(it.kvh * G + g) * D;
+            bf16* to = a.O + (tok + row) * a.ostride + (int64_t)(it.kvh * G + g) * D;
+#pragma unroll 1
+            for (int k0 = 0; k0 < D; k0 += 8) {
+              float o[8], d = 0.0f;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] = __bfloat162float(to[k0 + i]);
+#pragma unroll 1
+              for (int j = row; j >= 0; --j) {
+                const bf16* k = a.K + (tok + j) * a.kstride + (int64_t)it.kvh * D;
+                const bf16* v = a.V + (tok + j) * a.vstride + (int64_t)it.kvh * D + k0;
+                float p = 0.0f;
+#pragma unroll 1
+                for (int i = 0; i < D; ++i) p = fmaf(__bfloat162float(q[i]), __bfloat162float(k[i]), p);
+                p *= a.scale * expf(d);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = fmaf(p, __bfloat162float(v[i]), o[i]);
+                d += at_least(__ldg(a.decay + (tok + j) * a.dstride + it.kvh), kLeastDecay);
+              }
+#pragma unroll
+              for (int i = 0; i < 8; ++i) to[k0 + i] = __float2bfloat16_rn(o[i]);
+            }
+          }
+          __syncwarp();
         }
       }
     }
@@ -880,11 +991,11 @@ cudaError_t launch(bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, c
       b.seqs.item0[k] = item;
       item += (a.seqs.segs[k] - 1) * a.Hkv;
     }
-    b.seqs.item0[a.seqs.n] = item;
-    linear_chunk_kernel<D, true><<<item, kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, b);
+    b.seqs.item0[a.seqs.n] = b.items = item;
+    linear_chunk_kernel<D, true><<<std::min(item, a.ctas), kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, b);
     linear_join_kernel<D><<<dim3(a.Hkv * (D * D / 1024), a.seqs.n), 256, 0, s>>>(a);
   }
-  linear_chunk_kernel<D, false><<<a.seqs.item0[a.seqs.n], kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, a);
+  linear_chunk_kernel<D, false><<<std::min(a.items, a.ctas), kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, a);
   return cudaGetLastError();
 }
 

@@ -287,6 +287,7 @@ void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector
       l.seqs.tok0[k] = (int)tok0[i];
       l.seqs.len[k] = s.n_new;
       l.seqs.segs[k] = segs;
+      l.seqs.per[k] = chunks_of(s.n_new) / segs;
       l.seqs.place0[k] = places;
       l.seqs.item0[k + 1] = l.seqs.item0[k] + segs * H;
       if (segs > 1) {
@@ -451,6 +452,8 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
       a.place = h->place;
       a.place_decay = h->place_decay;
       a.seqs = l.seqs;
+      a.items = l.seqs.item0[l.seqs.n];
+      a.ctas = h->sms;
       CUtensorMap tmQ, tmK, tmV, tmO;
       if (!encode_bf16_rows(&tmQ, Q, h->tokens, (int64_t)c.n_q_heads * c.head_dim, q_stride, kLinearChunk) ||
           !encode_bf16_rows(&tmK, K, h->tokens, (int64_t)c.n_kv_heads * c.head_dim, k_stride, kLinearChunk) ||
