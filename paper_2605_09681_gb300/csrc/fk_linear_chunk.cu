@@ -28,6 +28,7 @@
 #include "fk_tc.h"
 
 #include <algorithm>
+#include <utility>
 
 namespace fk {
 namespace {
@@ -683,6 +684,8 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     // ------------------------------------------------------------------ the state
     const bool mine = 32 * wq < D;
     const int at = (32 * wq + (lane >> 3)) * D + (lane & 7) * 4;   // of a state, in memory: rows 4 i + lane / 8 of the warp's
+    // Where segments are joined, this kernel starts while the join still runs: its states alone come from there.
+    if (!kLocal) asm volatile("griddepcontrol.wait;" ::: "memory");
     bool ok = true;
     int base = 0;
 #pragma unroll 1
@@ -939,6 +942,9 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 template <int D>
 __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant__ LinearChunkArgs a) {
   constexpr int kBlocks = D * D / 4 / 256;        // of a head
+  // (launched while the kernel before still ends, and lets the next one start)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int k = blockIdx.y, segs = a.seqs.segs[k];
   if (segs < 2) return;
   const int h = blockIdx.x / kBlocks, at = (blockIdx.x % kBlocks) * 256 + threadIdx.x;
@@ -980,6 +986,22 @@ cudaError_t prepare() {
   return e;
 }
 
+// A launch that may come before the end of the kernel before it in the stream.
+template <class... Params, class... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, Args&&... args) {
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
 template <int D>
 cudaError_t launch(bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                    const CUtensorMap& tmO, const LinearChunkArgs& a,
@@ -993,7 +1015,11 @@ cudaError_t launch(bool split, const CUtensorMap& tmQ, const CUtensorMap& tmK, c
     }
     b.seqs.item0[a.seqs.n] = b.items = item;
     linear_chunk_kernel<D, true><<<std::min(item, a.ctas), kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, b);
-    linear_join_kernel<D><<<dim3(a.Hkv * (D * D / 1024), a.seqs.n), 256, 0, s>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch_early(linear_join_kernel<D>, dim3(a.Hkv * (D * D / 1024), a.seqs.n), 256, 0, s, a);
+    if (e == cudaSuccess)
+      e = launch_early(linear_chunk_kernel<D, false>, dim3(std::min(a.items, a.ctas)), kThreads, Layout<D>::kSmem, s, tmQ, tmK, tmV, tmO, a);
+    return e;
   }
   linear_chunk_kernel<D, false><<<std::min(a.items, a.ctas), kThreads, Layout<D>::kSmem, s>>>(tmQ, tmK, tmV, tmO, a);
   return cudaGetLastError();
