@@ -254,7 +254,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     for (const CUtensorMap* map : {&tmK, &tmV, &tmQ, &tmO}) asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bar->q_full[i], 1);
-      mbar_init(&bar->q_empty[i], 4);                        // O's rows, put in the tile's place, are on their way
+      mbar_init(&bar->q_empty[i], 4);
       mbar_init(&bar->g_full[i], 1);
       mbar_init(&bar->g_empty[i], kLocal ? 12 : 16);
       mbar_init(&bar->odd_full[i], 1);
@@ -264,7 +264,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       mbar_init(&bar->k_full[i], 1);
       mbar_init(&bar->k_empty[i], kLocal ? 8 : 9);           // the converting warps, and Q K^T
       mbar_init(&bar->v_full[i], 1);
-      mbar_init(&bar->v_empty[i], kLocal ? 1 : 2);           // the products, and the check
+      mbar_init(&bar->v_empty[i], kLocal ? 1 : 5);           // the products; the check, and O's rows on their way
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&bar->kp_full[i], 4);
@@ -436,7 +436,6 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
             for (int kk = 0; kk < C / 16; ++kk) umma_ts(kColX, kColA + (kk >> 1) * 32 + (kk & 1) * 8, y + kk * 128, kIdD, 1u);
             umma_commit(&bar->y_full);
-            if (g == G - 1) umma_commit(&bar->v_empty[n & 1]);
           }
           __syncwarp();
           if (m + 1 < chunks * G) {                          // the next A
@@ -800,6 +799,10 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         bf16* to = a.O + (it.tok0 + t) * a.ostride + (int64_t)head * D;
         if (!(ok = wait_for(&bar->x_full, m))) break;
         tc_fence_after();
+        // O goes out from the place of a tile that all products are done with: Q of this query head, or V after the last one (Q can
+        // then be loaded anew by now: the next but one is wanted soon)
+        const bool last = g == G - 1;
+        if (last) arrive(&bar->q_empty[m & 1]);
         if (!odd) {
 #pragma unroll 1
           for (int q = 0; q < D / 32; ++q) {
@@ -838,7 +841,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         if (!(ok = wait_for(&bar->y_full, m))) break;
         tc_fence_after();
         const bool whole = n * C + 32 * wq + 32 <= it.tokens;   // all rows of this warp
-        uint8_t* tile = sQ + (m & 1) * Lay::kTile;
+        uint8_t* tile = last ? sV + b * (2 * Lay::kTile) : sQ + (m & 1) * Lay::kTile;
 #pragma unroll 1
         for (int q = 0; q < D / 32 && !odd; ++q) {
           uint32_t y[32];
@@ -874,7 +877,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             *reinterpret_cast<uint4*>(to + 8 * k) =
                 *reinterpret_cast<const uint4*>(tile + (k >> 3) * (C * 128) + row * 128 + (((k & 7) ^ (row & 7)) << 4));
         }
-        arrive(&bar->q_empty[m & 1]);
+        arrive(last ? &bar->v_empty[b] : &bar->q_empty[m & 1]);
       }
       if (!ok) break;
       arrive(&bar->odd_empty[b]);
