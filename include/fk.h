@@ -598,8 +598,8 @@ FK_API fk_status fk_linear_step(fk_linear* h, int n_seqs, const int32_t* seqs, c
  * mode FK_LINEAR_ADVANCE: the states held become those after the step (calling again takes the tokens in again).
  * FK_LINEAR_STAY: they stay, and with state_out (device fp32 [n_seqs][n_kv_heads][head_dim][head_dim], 16-byte aligned, not
  * memory of the handle) those after the step go there, in the step's order; NULL with FK_LINEAR_ADVANCE.
- * Infinities and NaN reach the tokens from their own on, and no other sequence.  O overlaps no input (FK_ERR_ARG).
- * FK_ERR_STATE without a step. */
+ * Infinities and NaN reach the tokens from their own on, and no other sequence.  O and state_out overlap no input, not
+ * each other and no memory of the handle (FK_ERR_ARG).  FK_ERR_STATE without a step. */
 FK_API fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_stride, const void* K,
                                   int64_t k_stride, const void* V, int64_t v_stride, const float* decay,
                                   int64_t decay_stride, void* O, int64_t o_stride, float scale, int mode,

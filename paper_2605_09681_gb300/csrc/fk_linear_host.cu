@@ -124,14 +124,20 @@ bool meet(const Rows& a, const Rows& b, int64_t tokens) {
   return d < low || a.stride - d < high;
 }
 
+// All that rows extend over, as one.
+Rows whole(const Rows& a, int64_t tokens) {
+  const int64_t n = (tokens - 1) * a.stride + a.width;
+  return Rows{a.p, n, n};
+}
+
 // ---- plan of a step
-// Estimated times in us, measured back to back on a GB300 (segments alone and with all SMs taken): a CTA's start and end, and
-// what it takes for a chunk and each further query head, of the kernel that computes o and of the one that forms
-// segments' states; the join of those; a token of the recurrence alone, and what all SMs together take for a token of one head.
+// Estimated times in us, measured back to back on a GB300: a launch's start and end; an item, and its chunks and each
+// further query head of them, of the kernel that computes o and of the one that forms segments' states; the join of those; of the
+// recurrence, a launch, a token of one sequence, and what all SMs together take for a token of one head.
 struct Times {
-  double fixed, chunk, head, fixed_local, chunk_local, join, few, few_token, few_share;
+  double start, item, chunk, head, item_local, chunk_local, join, few, few_token, few_share;
 };
-constexpr Times kTimes128{8.0, 2.7, 2.4, 7.0, 1.8, 4.0, 2.2, 0.27, 0.0023}, kTimes64{8.0, 2.4, 0.9, 6.0, 1.2, 3.5, 2.0, 0.2, 0.0007};
+constexpr Times kTimes128{4.5, 3.0, 2.8, 2.3, 2.0, 1.8, 1.0, 2.2, 0.27, 0.0023}, kTimes64{4.5, 2.5, 2.5, 1.2, 1.5, 1.3, 1.0, 2.0, 0.2, 0.0007};
 
 // Time of `groups` of equally long items (length, count), longest first, on the SMs: each goes to the one that is free first.
 double fill_sms(const fk_linear* h, std::vector<std::pair<double, int64_t>>& groups) {
@@ -179,19 +185,19 @@ int best_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto, d
     for (const StepSeq& s : step) {
       if (s.n_new <= upto) continue;
       const int c = chunks_of(s.n_new), n = segments_of(c, per);
-      full.push_back({t.fixed + (c + n - 1) / n * chunk, (int64_t)n * H});
+      full.push_back({t.item + (c + n - 1) / n * chunk, (int64_t)n * H});
       if (n > 1) {
-        local.push_back({t.fixed_local + (c + n - 1) / n * t.chunk_local, (int64_t)(n - 1) * H});
+        local.push_back({t.item_local + (c + n - 1) / n * t.chunk_local, (int64_t)(n - 1) * H});
         places += (int64_t)n * H;
       }
     }
     if (places > kPlaces) break;
-    const double x = fill_sms(h, full) + (local.empty() ? 0.0 : fill_sms(h, local) + t.join);
+    const double x = t.start + fill_sms(h, full) + (local.empty() ? 0.0 : t.start + fill_sms(h, local) + t.join);
     if (x < least - 0.5) {
       least = x;
       best = per;
     }
-    if (per <= 2) break;
+    if (per <= 1) break;
   }
   *us = least;
   return best;
@@ -391,11 +397,13 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
   return guarded([&]() -> fk_status {
     DeviceGuard dev(c.device);
     if (dev.err != cudaSuccess) return FK_ERR_CUDA;
+    Rows taken{};                       // state_out
     if (state_out) {
       const size_t bytes = h->step.size() * h->per_seq * sizeof(float);
       const uintptr_t p = reinterpret_cast<uintptr_t>(state_out), own = reinterpret_cast<uintptr_t>(h->states);
       if (!aligned(state_out, 16) || !on_device(state_out, c.device)) return FK_ERR_ARG;
       if (p < own + h->per_layer * c.n_layers * sizeof(float) && own < p + bytes) return FK_ERR_ARG;
+      taken = Rows{p, (int64_t)bytes, (int64_t)bytes};
     }
     if (h->tokens > 0) {
       const int64_t wq = (int64_t)c.n_q_heads * c.head_dim, wk = (int64_t)c.n_kv_heads * c.head_dim;
@@ -409,10 +417,14 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
       auto rows = [](const void* p, int64_t stride, int64_t width) {
         return Rows{reinterpret_cast<uintptr_t>(p), stride * 2, width * 2};
       };
-      const Rows o = rows(O, o_stride, wq);
-      if (meet(o, rows(Q, q_stride, wq), h->tokens) || meet(o, rows(K, k_stride, wk), h->tokens) ||
-          meet(o, rows(V, v_stride, wk), h->tokens))
-        return FK_ERR_ARG;
+      const int64_t T = h->tokens;
+      const Rows o = rows(O, o_stride, wq), own = whole(Rows{reinterpret_cast<uintptr_t>(h->states), (int64_t)(h->per_layer * 4), (int64_t)(h->per_layer * 4)}, c.n_layers);
+      const Rows g{reinterpret_cast<uintptr_t>(decay), decay_stride * 4, (int64_t)c.n_kv_heads * 4};
+      for (const Rows& in : {rows(Q, q_stride, wq), rows(K, k_stride, wk), rows(V, v_stride, wk), g}) {
+        if (in.stride ? meet(o, in, T) : meet(whole(o, T), in, 1)) return FK_ERR_ARG;
+        if (state_out && meet(taken, whole(in, T), 1)) return FK_ERR_ARG;
+      }
+      if (meet(whole(o, T), own, 1) || (state_out && meet(taken, whole(o, T), 1))) return FK_ERR_ARG;
     }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const float sc = scale > 0.0f ? scale : (float)(1.0 / std::sqrt((double)c.head_dim));
