@@ -621,7 +621,7 @@ class Rotary:
         if cos is None:
             cos = self._torch.empty(shape, dtype=f32, device=positions.device) if stream is None else _made(positions, raw, shape, f32)
         if sin is None:
-            sin = self._torch.empty(shape, dtype=f32, device=positions.device) if stream is None else _made(positions, raw, shape, f32)
+            sin = self._torch.empty_like(cos) if stream is None else _made(positions, raw, shape, f32)
         _check(self._lib.fk_rotary_tables(self._ref, tokens, p, cos.data_ptr(), sin.data_ptr(), raw), "fk_rotary_tables")
         return cos, sin
 

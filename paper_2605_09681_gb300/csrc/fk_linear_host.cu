@@ -161,55 +161,89 @@ double fill_sms(const fk_linear* h, std::vector<std::pair<double, int64_t>>& gro
 
 int chunks_of(int tokens) { return (tokens + kLinearChunk - 1) / kLinearChunk; }
 
-// Segments of a sequence of `chunks`, of at most `per` chunks each.
+// ... of at most `per` each.
 int segments_of(int chunks, int per) { return (chunks + per - 1) / per; }
 
-// Chunks of a segment, at most, that make the sequences of more than `upto` tokens the fastest.  Splitting a sequence reads its
-// keys and values twice and takes two launches more, and pays where long sequences would leave SMs idle.
-int best_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto, double* us) {
+// Estimated time of the sequences of more than `upto` tokens, sequence i split into segs[i]; huge where the workspace is too small.
+double time_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto, const std::vector<int>& segs) {
   const Times& t = h->cfg.head_dim == 128 ? kTimes128 : kTimes64;
   const int H = h->cfg.n_kv_heads;
   const double chunk = t.chunk + (h->cfg.n_q_heads / H - 1) * t.head;
-  int most = 0;
-  for (const StepSeq& s : step) most = std::max(most, s.n_new > upto ? chunks_of(s.n_new) : 0);
-  *us = 0.0;
-  if (most == 0) return 1;
-  int best = most;
-  double least = 1e30;
   std::vector<std::pair<double, int64_t>> full, local;
+  int64_t places = 0;
+  for (size_t i = 0; i < step.size(); ++i) {
+    if (step[i].n_new <= upto) continue;
+    const int c = chunks_of(step[i].n_new), n = segs[i], per = c / n, more = c % n;
+    if (more) full.push_back({t.item + (per + 1) * chunk, (int64_t)more * H});
+    full.push_back({t.item + per * chunk, (int64_t)(n - more) * H});
+    if (n > 1) {
+      if (more) local.push_back({t.item_local + (per + 1) * t.chunk_local, (int64_t)more * H});
+      if (n - 1 > more) local.push_back({t.item_local + per * t.chunk_local, (int64_t)(n - 1 - more) * H});
+      places += (int64_t)n * H;
+    }
+  }
+  if (places > kPlaces) return 1e30;
+  return t.start + fill_sms(h, full) + (local.empty() ? 0.0 : t.start + fill_sms(h, local) + t.join);
+}
+
+// Into how many segments each sequence of more than `upto` tokens is split.  Splitting a sequence reads its keys and values twice and
+// takes two launches more, and pays where long sequences would leave SMs idle.  First segments of the same length for all, then
+// one more or less for single sequences, as long as it helps: the last round of items is what it evens out (prompts of
+// 4001, 2500, 1777 and five shorter of 16 heads: from 14 to 16 segments, FIGURE us).
+double best_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto, std::vector<int>* segs) {
+  int most = 0;
+  segs->assign(step.size(), 1);
+  std::vector<int> longest;
+  for (size_t i = 0; i < step.size(); ++i)
+    if (step[i].n_new > upto) {
+      most = std::max(most, chunks_of(step[i].n_new));
+      if (step[i].n_new > kLinearChunk) longest.push_back((int)i);
+    }
+  if (most == 0) return 0.0;
+  double least = 1e30;
+  std::vector<int> n(step.size(), 1);
   for (int parts = 1; parts <= most; parts += std::max(1, parts / 8)) {
     const int per = (most + parts - 1) / parts;
-    full.clear();
-    local.clear();
-    int64_t places = 0;
-    for (const StepSeq& s : step) {
-      if (s.n_new <= upto) continue;
-      const int c = chunks_of(s.n_new), n = segments_of(c, per);
-      full.push_back({t.item + (c + n - 1) / n * chunk, (int64_t)n * H});
-      if (n > 1) {
-        local.push_back({t.item_local + (c + n - 1) / n * t.chunk_local, (int64_t)(n - 1) * H});
-        places += (int64_t)n * H;
-      }
-    }
-    if (places > kPlaces) break;
-    const double x = t.start + fill_sms(h, full) + (local.empty() ? 0.0 : t.start + fill_sms(h, local) + t.join);
-    if (x < least - 0.5) {
-      least = x;
-      best = per;
+    for (const int i : longest) n[i] = segments_of(chunks_of(step[i].n_new), per);
+    const double us = time_split(h, step, upto, n);
+    if (us > 1e29) break;
+    if (us < least - 0.5) {
+      least = us;
+      *segs = n;
     }
     if (per <= 1) break;
   }
-  *us = least;
-  return best;
+  if (longest.size() < 2) return least;
+  std::stable_sort(longest.begin(), longest.end(), [&](int x, int y) { return step[x].n_new > step[y].n_new; });
+  if (longest.size() > 8) longest.resize(8);
+  bool better = true;
+  for (int pass = 0; pass < 3 && better; ++pass) {
+    better = false;
+    for (const int i : longest)
+      for (const int d : {1, -1}) {
+        n = *segs;
+        n[i] += d;
+        if (n[i] < 1 || n[i] > chunks_of(step[i].n_new)) continue;
+        const double us = time_split(h, step, upto, n);
+        if (us < least - 0.3) {
+          least = us;
+          *segs = n;
+          better = true;
+          break;
+        }
+      }
+  }
+  return least;
 }
 
 // Sequences of up to how many tokens go through the recurrence: it takes longer for each token, but a chunk takes as long
 // for one as for 128.
-int best_few(const fk_linear* h, const std::vector<StepSeq>& step, int* per) {
+int best_few(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<int>* segs) {
   const Times& t = h->cfg.head_dim == 128 ? kTimes128 : kTimes64;
   const int G = h->cfg.n_q_heads / h->cfg.n_kv_heads;
   int best = 0;
   double least = 1e30;
+  std::vector<int> n;
   for (int upto : {1, 2, 4, 8, 16, 32}) {
     int longest = 0;
     int64_t tokens = 0, seqs = 0, beyond = 0;
@@ -222,15 +256,14 @@ int best_few(const fk_linear* h, const std::vector<StepSeq>& step, int* per) {
         seqs += s.n_new > 0;
       }
     }
-    double us = 0.0;
-    const int p = best_split(h, step, upto, &us);
+    double us = best_split(h, step, upto, &n);
     if (tokens > 0)
       us += t.few + (double)seqs * h->per_seq * 8 / 6.3e6 +      // (the states' bytes, and the tokens)
             (0.6 + 0.4 * G) * std::max(t.few_token * longest, t.few_share * (double)tokens * h->cfg.n_kv_heads);
     if (us < least) {
       least = us;
       best = upto;
-      *per = p;
+      segs->swap(n);
     }
     if (beyond == 0) break;
   }
@@ -240,15 +273,15 @@ int best_few(const fk_linear* h, const std::vector<StepSeq>& step, int* per) {
 // The launches of a step: sequences of few tokens, then the others, the longest segments first; kLinearSeqs to a launch.
 void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<Launch>* plan) {
   const int H = h->cfg.n_kv_heads;
-  int upto = 1, per = 1;
+  int upto = 1;
+  std::vector<int> segs_of(step.size(), 1);
   if (std::all_of(step.begin(), step.end(), [](const StepSeq& s) { return s.n_new <= 1; }) && h->force_few == 0) {
     upto = 1;                           // (a decoding step: nothing to estimate)
   } else if (h->force_few > 0) {
-    double us;
     upto = h->force_few;
-    per = best_split(h, step, upto, &us);
+    best_split(h, step, upto, &segs_of);
   } else {
-    upto = best_few(h, step, &per);
+    upto = best_few(h, step, &segs_of);
   }
   std::vector<int> order(step.size());
   std::vector<int64_t> tok0(step.size());
@@ -257,11 +290,8 @@ void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector
     order[i] = (int)i;
     tok0[i] = tok;
   }
-  auto segments = [&](int tokens) {
-    const int c = chunks_of(tokens);
-    return h->force_segments > 0 ? std::min(h->force_segments, c) : segments_of(c, per);
-  };
-  auto length = [&](int i) { return (chunks_of(step[i].n_new) + segments(step[i].n_new) - 1) / std::max(1, segments(step[i].n_new)); };
+  auto segments = [&](int i) { return h->force_segments > 0 ? std::min(h->force_segments, chunks_of(step[i].n_new)) : segs_of[i]; };
+  auto length = [&](int i) { return segments_of(chunks_of(step[i].n_new), std::max(1, segments(i))); };
   for (const bool chunk : {false, true}) {
     Launch l{};
     int places = 0;
@@ -286,7 +316,7 @@ void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector
         continue;
       }
       const int k = l.seqs.n++;
-      int segs = std::min(segments(s.n_new), (kPlaces - places) / H);
+      int segs = std::min(segments(i), (kPlaces - places) / H);
       if (segs < 2) segs = 1;
       l.seqs.slot[k] = s.seq;
       l.seqs.out[k] = i;
