@@ -3,6 +3,8 @@
 
 #include "fk_internal.h"
 
+#include <utility>
+
 namespace fk {
 
 constexpr int kLinearSeqs = 256;      // sequences of one launch (their numbers travel by value)
@@ -75,13 +77,30 @@ cudaError_t launch_linear_chunk(int D, bool split, const CUtensorMap& tmQ, const
 // [rows][cols] bf16, `stride` elements from row to row: tiles of box_rows rows of 64 columns, 128-byte swizzle.
 bool encode_bf16_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows);
 
-// The recurrence, token by token.
-cudaError_t launch_linear_few(int D, const LinearArgs& a, cudaStream_t s);
+// The recurrence, token by token.  beside: it may run beside the chunks' launch before it (of other sequences).
+cudaError_t launch_linear_few(int D, const LinearArgs& a, bool beside, cudaStream_t s);
 
 // *report = *status, which is cleared
 cudaError_t launch_linear_status(int* status, int* report, cudaStream_t s);
 
 #ifdef __CUDACC__
+// A launch that may come before the end of the kernel before it in the stream.  It, or what it waits for, waits for that one's end
+// before it ends itself, so that the stream's order holds behind it.
+template <class... Params, class... Args>
+inline cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, Args&&... args) {
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
 __device__ __forceinline__ float at_least(float g, float least) { return g < least ? least : g; }   // (NaN stays)
 #endif
 

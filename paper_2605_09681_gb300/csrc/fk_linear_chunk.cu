@@ -28,7 +28,6 @@
 #include "fk_tc.h"
 
 #include <algorithm>
-#include <utility>
 
 namespace fk {
 namespace {
@@ -283,6 +282,8 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     load(&tmK, sK, &bar->k_full[0], first.kvh, first.tok0);
     if (!kLocal) load(&tmQ, sQ, &bar->q_full[0], first.kvh * G, first.tok0);
     load(&tmV, sV, &bar->v_full[0], first.kvh, first.tok0);
+    // sequences of few tokens may take the SMs that this launch leaves idle
+    if (!kLocal) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   }
   if (warp == 1) {
     __syncwarp();
@@ -987,22 +988,6 @@ cudaError_t prepare() {
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(linear_chunk_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<D>::kSmem);
   return e;
-}
-
-// A launch that may come before the end of the kernel before it in the stream.
-template <class... Params, class... Args>
-cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, Args&&... args) {
-  cudaLaunchAttribute early{};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = &early;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
 
 template <int D>

@@ -46,6 +46,11 @@ struct Row {                          // N bf16 in registers
   }
 };
 
+// This launch ends no earlier than the one before it in the stream, beside which it may run: one block, the last to start, stays.
+__device__ __forceinline__ void end_behind() {
+  if (blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 8) linear_one_kernel(const __grid_constant__ LinearArgs a) {
   constexpr int kRows = D / 16;       // of a thread
@@ -157,6 +162,7 @@ __global__ void __launch_bounds__(kThreads, 8) linear_one_kernel(const __grid_co
     for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4*>(s1 + i * D) = s[i];
   }
   if (held > 0) flush(row, held);
+  end_behind();
 }
 
 constexpr int kMostHeads = 8;         // query heads of a group
@@ -278,23 +284,21 @@ __global__ void __launch_bounds__(kThreads) linear_few_kernel(const __grid_const
       s1[(2 * i + 1) * D] = s[i].y;
     }
   }
+  end_behind();
 }
 
 __global__ void linear_status_kernel(int* status, int* report) { *report = atomicExch(status, 0); }
 
 }  // namespace
 
-cudaError_t launch_linear_few(int D, const LinearArgs& a, cudaStream_t s) {
+cudaError_t launch_linear_few(int D, const LinearArgs& a, bool beside, cudaStream_t s) {
   const unsigned grid = (unsigned)a.seqs.n * a.Hkv * (D / kCols);
   int most = 0;
   for (int k = 0; k < a.seqs.n; ++k) most = most > a.seqs.len[k] ? most : a.seqs.len[k];
-  if (most <= 1 || a.G > kMostHeads) {
-    if (D == 128) linear_one_kernel<128><<<grid, kThreads, 0, s>>>(a);
-    else linear_one_kernel<64><<<grid, kThreads, 0, s>>>(a);
-  } else {
-    if (D == 128) linear_few_kernel<128><<<grid, kThreads, 0, s>>>(a);
-    else linear_few_kernel<64><<<grid, kThreads, 0, s>>>(a);
-  }
+  const bool one = most <= 1 || a.G > kMostHeads;
+  const auto kernel = D == 128 ? (one ? linear_one_kernel<128> : linear_few_kernel<128>) : (one ? linear_one_kernel<64> : linear_few_kernel<64>);
+  if (beside) return launch_early(kernel, dim3(grid), kThreads, 0, s, a);
+  kernel<<<grid, kThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
 

@@ -137,7 +137,7 @@ Rows whole(const Rows& a, int64_t tokens) {
 struct Times {
   double start, item, chunk, head, item_local, chunk_local, join, few, few_token, few_share;
 };
-constexpr Times kTimes128{4.5, 3.0, 2.8, 2.3, 2.0, 1.8, 1.0, 2.2, 0.27, 0.0023}, kTimes64{4.5, 2.5, 2.5, 1.2, 1.5, 1.3, 1.0, 2.0, 0.2, 0.0007};
+constexpr Times kTimes128{4.5, 3.0, 2.8, 2.3, 2.0, 1.8, 1.0, 2.2, 0.28, 0.0031}, kTimes64{3.0, 2.5, 2.0, 1.3, 1.5, 1.3, 1.0, 2.0, 0.22, 0.00105};
 
 // Time of `groups` of equally long items (length, count), longest first, on the SMs: each goes to the one that is free first.
 double fill_sms(const fk_linear* h, std::vector<std::pair<double, int64_t>>& groups) {
@@ -189,7 +189,7 @@ double time_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto
 // Into how many segments each sequence of more than `upto` tokens is split.  Splitting a sequence reads its keys and values twice and
 // takes two launches more, and pays where long sequences would leave SMs idle.  First segments of the same length for all, then
 // one more or less for single sequences, as long as it helps: the last round of items is what it evens out (prompts of
-// 4001, 2500, 1777 and five shorter of 16 heads: from 14 to 16 segments, FIGURE us).
+// 4001, 2500, 1777 and five shorter of 16 heads: 92.7 us with equal lengths alone, 89.8 so).
 double best_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto, std::vector<int>* segs) {
   int most = 0;
   segs->assign(step.size(), 1);
@@ -243,10 +243,11 @@ int best_few(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<i
   const int G = h->cfg.n_q_heads / h->cfg.n_kv_heads;
   int best = 0;
   double least = 1e30;
+  int64_t before = -1;
   std::vector<int> n;
   for (int upto : {1, 2, 4, 8, 16, 32}) {
     int longest = 0;
-    int64_t tokens = 0, seqs = 0, beyond = 0;
+    int64_t tokens = 0, seqs = 0, beyond = 0, items = 0;
     for (const StepSeq& s : step) {
       if (s.n_new > upto) {
         ++beyond;
@@ -256,10 +257,18 @@ int best_few(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<i
         seqs += s.n_new > 0;
       }
     }
-    double us = best_split(h, step, upto, &n);
+    if (beyond == before) continue;     // the same sequences as with the number before
+    before = beyond;
+    const double chunks_us = best_split(h, step, upto, &n);
+    double few_us = 0.0;
     if (tokens > 0)
-      us += t.few + (double)seqs * h->per_seq * 8 / 6.3e6 +      // (the states' bytes, and the tokens)
-            (0.6 + 0.4 * G) * std::max(t.few_token * longest, t.few_share * (double)tokens * h->cfg.n_kv_heads);
+      few_us = t.few + (double)seqs * h->per_seq * 8 / 6.3e6 +   // (the states' bytes, and the tokens)
+               (0.65 + 0.36 * G) * std::max(t.few_token * longest, t.few_share * (double)tokens * h->cfg.n_kv_heads);
+    // they run beside one another where there are SMs for both: of the recurrence, four blocks of 32 columns keep an SM busy
+    for (size_t i = 0; i < step.size(); ++i) items += step[i].n_new > upto ? (int64_t)n[i] * h->cfg.n_kv_heads : 0;
+    const double blocks = (double)seqs * h->cfg.n_kv_heads * h->cfg.head_dim / 32;
+    const double both = std::min(1.0, (double)items / h->sms) + std::min(1.0, blocks / (4.0 * h->sms)) - 1.0;
+    const double us = std::max(few_us, chunks_us) + (0.2 + 0.8 * std::max(0.0, both)) * std::min(few_us, chunks_us);
     if (us < least) {
       least = us;
       best = upto;
@@ -270,7 +279,8 @@ int best_few(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<i
   return best;
 }
 
-// The launches of a step: sequences of few tokens, then the others, the longest segments first; kLinearSeqs to a launch.
+// The launches of a step: sequences in chunks, the longest segments first, then those of few tokens, which fill the SMs that the
+// chunks leave idle; kLinearSeqs to a launch.
 void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector<Launch>* plan) {
   const int H = h->cfg.n_kv_heads;
   int upto = 1;
@@ -292,7 +302,7 @@ void make_plan(const fk_linear* h, const std::vector<StepSeq>& step, std::vector
   }
   auto segments = [&](int i) { return h->force_segments > 0 ? std::min(h->force_segments, chunks_of(step[i].n_new)) : segs_of[i]; };
   auto length = [&](int i) { return segments_of(chunks_of(step[i].n_new), std::max(1, segments(i))); };
-  for (const bool chunk : {false, true}) {
+  for (const bool chunk : {true, false}) {
     Launch l{};
     int places = 0;
     auto push = [&] {
@@ -481,10 +491,12 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
     };
     LinearArgs f;
     fill(f);
+    bool beside = false;
     for (const Launch& l : h->plan) {
       if (!l.chunk) {
         f.seqs = l.few;
-        const fk_status e = done(h, launch_linear_few(c.head_dim, f, st));
+        const fk_status e = done(h, launch_linear_few(c.head_dim, f, beside, st));
+        beside = false;
         if (e != FK_OK) return e;
         continue;
       }
@@ -503,6 +515,7 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
           !encode_bf16_rows(&tmO, O, h->tokens, (int64_t)c.n_q_heads * c.head_dim, o_stride, 32))
         return FK_ERR_CUDA;
       h->launches += l.split ? 2 : 0;
+      beside = true;
       const fk_status e = done(h, launch_linear_chunk(c.head_dim, l.split, tmQ, tmK, tmV, tmO, a, st));
       if (e != FK_OK) return e;
     }
@@ -517,7 +530,7 @@ fk_status fk_linear_attend(fk_linear* h, int layer, const void* Q, int64_t q_str
         f.seqs.tok0[k] = f.seqs.len[k] = 0;
       }
       if (f.seqs.n == kLinearSeqs || (i + 1 == h->step.size() && f.seqs.n > 0)) {
-        const fk_status e = done(h, launch_linear_few(c.head_dim, f, st));
+        const fk_status e = done(h, launch_linear_few(c.head_dim, f, false, st));
         if (e != FK_OK) return e;
         f.seqs.n = 0;
       }

@@ -348,3 +348,41 @@ def test_overlaps_are_refused():
             with pytest.raises(FkError):
                 cache.force_plan(*plan)
         assert cache.sync_status() == 0
+
+
+@pytest.mark.parametrize("D,Hq,H", [(64, 6, 6), (128, 8, 4)])
+def test_captured_steps_of_chunks_and_single_tokens(D, Hq, H):
+    """Prompts, drafts and single tokens of one step run beside one another: replays, calls of several layers in a row and what
+    follows them in the stream find all of it done."""
+    lens = [1, 900, 3, 1, 200, 1, 0, 131] + [1] * 30
+    q, k, v, g = _tensors(sum(lens), Hq, H, D, D)
+    seqs = list(range(len(lens)))
+    kw = dict(n_layers=3, n_q_heads=Hq, n_kv_heads=H, head_dim=D, max_seqs=len(lens))
+    with _cache(**kw) as cache, _cache(**kw) as plain:
+        for c in (cache, plain):
+            c.step(seqs, lens)
+        out = [torch.empty_like(q) for _ in range(3)]
+        after = [torch.empty_like(q) for _ in range(3)]
+        copies = [torch.empty_like(plain.states(0)) for _ in range(3)]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for layer in range(3):
+                cache.attend(layer, q, k, v, g, O=out[layer])
+                after[layer].copy_(out[layer])
+                copies[layer].copy_(cache.states(layer))
+        for _ in range(3):
+            graph.replay()
+            for layer in range(3):
+                want = torch.empty_like(q)
+                for i, at in zip(seqs, np.concatenate(([0], np.cumsum(lens)))):
+                    if lens[i] > 0:                      # each by itself
+                        p = slice(int(at), int(at) + lens[i])
+                        plain.force_plan(8 if lens[i] < 8 else 1, 3 if lens[i] > 500 else 1)
+                        plain.step([i], [lens[i]])
+                        want[p] = plain.attend(layer, q[p], k[p], v[p], g[p])
+                # (a prompt may be split another way: two results, each within 2^-8 and 2^-20 of the exact ones)
+                assert (after[layer].float() - want.float()).norm() <= 2.0 ** -7 * want.float().norm()
+                assert (copies[layer] - plain.states(layer)).norm() <= 2.0 ** -18 * plain.states(layer).norm()
+                assert torch.equal(after[layer], out[layer])
+        assert cache.sync_status() == 0 and plain.sync_status() == 0
