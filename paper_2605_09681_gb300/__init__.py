@@ -62,6 +62,21 @@ def _stream(stream) -> int | None:
     return getattr(stream, "cuda_stream", stream)
 
 
+def _fast_calls():
+    """(new tensor of (shape, strides, dtype) on the current device, the current device, the current stream of a device), as short as torch
+    has them: between launches torch.empty_like takes 4 us a call and torch's own allocation of strided tensors 2."""
+    import torch
+    try:
+        from torch._C._dynamo.guards import _empty_strided_cuda as new
+    except ImportError:
+        def new(shape, strides, dtype):
+            return torch.empty_strided(shape, strides, dtype=dtype, device="cuda")
+    try:
+        return new, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    except AttributeError:
+        return new, torch.cuda.current_device, lambda dev: torch.cuda.current_stream(dev).cuda_stream
+
+
 def head_profile(Q, K, n_generate: int, n_sink: int, n_transition: int, mass=None, status=None,
                  stream=None):
     """Offline head profiling (Sec. 4.1, Eq. 1) through fk_head_profile.
@@ -538,7 +553,8 @@ class Rotary:
         self._ref = ctypes.byref(self._r)
         import torch
         self._types = {torch.bfloat16: L.FK_TYPE_BF16, torch.float16: L.FK_TYPE_F16, torch.float32: L.FK_TYPE_F32}
-        self._torch, self._i32 = torch, torch.int32
+        self._torch, self._i32, self._f32 = torch, torch.int32, torch.float32
+        self._new, self._current, self._queue = _fast_calls()
 
     def _at(self, positions, tokens):
         n = self.n_axes
@@ -560,20 +576,15 @@ class Rotary:
             raise ValueError("%s: the heads of a token must lie contiguously" % name)
         return x.data_ptr(), row if tokens > 1 else heads * D, heads
 
-    def _elsewhere(self, x):
-        """The device of x where it is not the current one."""
-        dev = x.get_device()
-        return dev if dev >= 0 and dev != self._torch.cuda.current_device() else None
-
     def rotate(self, positions, Q, K=None, inverse=False, Q_out=None, K_out=None, stream=None):
         """Q (and K, in the same launch) [tokens, heads, head_dim] in bf16, fp16 or fp32, which may be slices of wider rows,
         turned by `positions` (int32 [tokens, axes], or [tokens]); inverse: the other way (the rotation's gradient).
         Returns the rotated Q, or Q and K, in new tensors or in Q_out, K_out (which may be Q, K)."""
-        dev = self._elsewhere(Q)
-        if dev is not None:
+        dev = Q.get_device()
+        if dev >= 0 and dev != self._current():
             with self._torch.cuda.device(dev):
                 return self.rotate(positions, Q, K, inverse, Q_out, K_out, stream)
-        dtype = Q.dtype
+        dtype, D = Q.dtype, self.head_dim
         kind = self._types.get(dtype)
         if kind is None:
             raise ValueError("Q: expected bf16, fp16 or fp32, not %s" % dtype)
@@ -582,10 +593,10 @@ class Rotary:
         tokens = Q.shape[0]
         p = self._at(positions, tokens)
         q, qs, hq = self._rows(Q, dtype, tokens, "Q")
-        raw = _stream(stream)
+        raw = self._queue(dev) if stream is None else _stream(stream)
         if Q_out is None:
-            Q_out = self._torch.empty_like(Q) if stream is None else _made(Q, raw)   # (dense either way)
-            q1, qs1 = Q_out.data_ptr(), hq * self.head_dim
+            Q_out = self._new((tokens, hq, D), (hq * D, D, 1), dtype) if stream is None else _made(Q, raw)
+            q1, qs1 = Q_out.data_ptr(), hq * D
         else:
             q1, qs1, h = self._rows(Q_out, dtype, tokens, "Q_out")
             if h != hq:
@@ -595,8 +606,8 @@ class Rotary:
         if K is not None:
             k, ks, hk = self._rows(K, dtype, tokens, "K")
             if K_out is None:
-                K_out = self._torch.empty_like(K) if stream is None else _made(K, raw)
-                k1, ks1 = K_out.data_ptr(), hk * self.head_dim
+                K_out = self._new((tokens, hk, D), (hk * D, D, 1), dtype) if stream is None else _made(K, raw)
+                k1, ks1 = K_out.data_ptr(), hk * D
             else:
                 k1, ks1, h = self._rows(K_out, dtype, tokens, "K_out")
                 if h != hk:
@@ -607,21 +618,22 @@ class Rotary:
 
     def tables(self, positions, cos=None, sin=None, stream=None):
         """cos and sin of the angles at `positions`, fp32 [tokens, dim / 2] (rows of PagedKVCache.append's tables)."""
-        dev = self._elsewhere(positions)
-        if dev is not None:
+        dev = positions.get_device()
+        if dev >= 0 and dev != self._current():
             with self._torch.cuda.device(dev):
                 return self.tables(positions, cos, sin, stream)
         tokens = positions.shape[0]
         p = self._at(positions, tokens)
-        shape, f32 = (tokens, self.dim // 2), self._torch.float32
+        n, f32 = self.dim // 2, self._f32
+        shape = (tokens, n)
         for x in (cos, sin):
             if x is not None and (x.dtype is not f32 or x.shape != shape or not x.is_cuda or not x.is_contiguous()):
                 raise ValueError("cos, sin: expected contiguous fp32 CUDA tensors [%d, %d]" % shape)
-        raw = _stream(stream)
+        raw = self._queue(dev) if stream is None else _stream(stream)
         if cos is None:
-            cos = self._torch.empty(shape, dtype=f32, device=positions.device) if stream is None else _made(positions, raw, shape, f32)
+            cos = self._new(shape, (n, 1), f32) if stream is None else _made(positions, raw, shape, f32)
         if sin is None:
-            sin = self._torch.empty_like(cos) if stream is None else _made(positions, raw, shape, f32)
+            sin = self._new(shape, (n, 1), f32) if stream is None else _made(positions, raw, shape, f32)
         _check(self._lib.fk_rotary_tables(self._ref, tokens, p, cos.data_ptr(), sin.data_ptr(), raw), "fk_rotary_tables")
         return cos, sin
 
@@ -661,6 +673,7 @@ class LinearStateCache:
         self._torch, self._bf16, self._f32 = torch, torch.bfloat16, torch.float32
         self._dev = torch.device("cuda", device)
         self._tokens = self._seqs = 0
+        self._new, self._current, self._queue = _fast_calls()
         _check(self._lib.fk_linear_create(ctypes.byref(self.cfg), ctypes.byref(self._h)), "fk_linear_create")
 
     # ---- lifetime
@@ -714,10 +727,14 @@ class LinearStateCache:
                     not state_out.is_contiguous():
                 raise ValueError("state_out: expected a contiguous fp32 CUDA tensor [%d, %d, %d, %d]" % (self._seqs, H, D, D))
             s1 = state_out.data_ptr()
-        raw = self._on(stream)
+        raw = self._queue(self.device) if stream is None else self._on(stream)
         if O is None:
-            O = self._torch.empty_like(Q) if stream is None else _made(Q, raw)   # (dense either way)
-            o, os = O.data_ptr(), self.n_q_heads * D
+            n = self.n_q_heads
+            if stream is None and self._current() == self.device:
+                O = self._new((T, n, D), (n * D, D, 1), self._bf16)
+            else:
+                O = _made(Q, raw)
+            o, os = O.data_ptr(), n * D
         else:
             o, os = self._rows(O, T, self.n_q_heads, "O")
         mode = L.FK_LINEAR_ADVANCE if advance and state_out is None else L.FK_LINEAR_STAY

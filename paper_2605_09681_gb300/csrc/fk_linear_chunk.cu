@@ -3,10 +3,12 @@
 // With G_i the sum of the decays' logarithms from a chunk's start through token i, and S the state before the chunk,
 //   o_i = scale (exp(G_i) q_i S + sum_(j <= i) exp(G_i - G_j) (q_i k_j) v_j),
 //   S'  = exp(G_C) S + sum_j exp(G_C - G_j) k_j v_j^T:
-// four matrix products of 128 x 128 x D a chunk and head (six: see K'), 1.3 times the time of its 1 KB a token from DRAM if the
-// tensor cores run at their measured rate alone.  All exponents are of sums that are <= 0 where decays are.
+// four matrix products of 128 x 128 x D a chunk and head, six with K' in three parts: 1.6 us of the tensor cores at their rate, for
+// 128 KB of q, k, v and o (D = 128), 2.9 us of an SM's share of the memory.  All exponents are of sums that are <= 0 where
+// decays are.
 //
-// One CTA takes a segment of one kv head's chunks in turn, for all query heads that share it:
+// A CTA takes items (segments of one kv head's chunks, with all query heads that share it) one after the other, without a break
+// between them:
 //   warp 3        TMA: K and V of a chunk, Q of a chunk and query head, two stages each, 128-byte swizzle
 //   warp 1        tcgen05.mma, one elected lane: A = Q K^T, X = Q S, Y = exp(G_i) X + P V, dS = K'^T V
 //   warp 2        the chunk's running sums G (log2 domain) and what follows from them alone
@@ -17,13 +19,22 @@
 //                 at a time, taking turns, over the columns of A that it came from.
 //   warps 12-15   the state: thread r keeps row r (channel r of k) in registers, S' = exp(G_C) S + dS, and writes it as bf16 to
 //                 shared memory, the B operand of X
-//   warps 16-19   o: thread i scales row i of X where it is, and writes row i of Y
+//   warps 16-19   o: thread i scales row i of X where it is, rounds row i of Y to bf16 over a tile of Q or V that the products are
+//                 done with, and a TMA store takes it from there (straight from registers: 16 bytes of 32 lines at a time)
 // Tensor memory columns: A and P 0-127, X and Y 128.., dS 256.., K' 384-479 (two buffers; kLocal: four from 0).
 //
 // kLocal: the state alone, from zero (what a segment adds), without Q and o.
 // Every wait is bounded; when one expires the CTA records it, drains its copies and products, and ends.
+//
+// What bounds it.  A chunk takes 2.8 us of a CTA by itself (2.3 more for each further query head; kLocal 1.8) and 3.8 with all SMs
+// loading: 24 chunks of 144 heads of 128 in 87 us, 5.1 TB/s.  By itself it is a chain: S' (and so X of the next chunk) waits for all
+// of dS, that for K', P for A and Y for P; the products are in the order that hides most of it, and the tensor pipe is active 31
+// to 38% of the time (two chunks at once would want twice the tensor memory).  An item costs 3 us besides (its first tiles, its state
+// both ways), a launch 4.5.  One sequence of few heads is therefore split (the host's plan): 4680 tokens of 12 heads in 12
+// segments 30 us, unsplit 113; what each segment adds is then formed first, which reads K and V twice.
 // Loops over columns are rolled where registers are not indexed: the roles' code together has to stay in the instruction
-// cache (unrolled, P of a chunk took 2400 cycles, and 4800 with all SMs fetching).
+// cache (unrolled, P of a chunk took 2400 cycles, and 4800 with all SMs fetching).  Roles are told apart by a warp number that comes
+// from a shuffle, so that the compiler knows branches by it to be uniform.
 #include "fk_linear.h"
 #include "fk_tc.h"
 
@@ -466,8 +477,8 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll 1
       for (int n = 0; n < it.nc; ++n) {
         const int c = base + n, b = c & 1, u = c >> 1;
-        // whole numbers of 2^-32: sums and their differences are exact however far they run (2^-33 a token is 2^-26 at most for a
-        // chunk, of a logarithm); what is not a number makes all sums from its token on that
+        // whole numbers of 2^-32: sums and their differences are exact however far they run (of g log2 e itself, 2^-33 a token is
+        // 2^-26 at most for a chunk, and its product in fp32 2^-24 of it); what is not a number makes all sums from its token on that
         int64_t sum[4];
         bool grows = false;
         int lost = C;                                        // first token that is not a number
@@ -886,16 +897,23 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     }
     base += it.nc;
     }
+    // Each thread's factors of a chunk's values go to shared memory, over the tiles: these are done with once O's warps have
+    // let go of the last two of V.
+    if (!kLocal && any_odd && ok) ok = wait_for(&bar->v_empty[(base - 1) & 1], (base - 1) >> 1);
+    if (!kLocal && any_odd && ok && base > 1) ok = wait_for(&bar->v_empty[base & 1], (base - 2) >> 1);
     if (!kLocal && any_odd && ok) {
-      // o's terms of a chunk's own tokens, where V of the chunk is not all finite, in fp32 (a millisecond a chunk: this is for
-      // inputs that went wrong)
+      // o's terms of a chunk's own tokens, where V of the chunk is not all finite, in fp32 (0.5 ms a chunk and query head of 128: this
+      // is for inputs that went wrong)
+      float* factor = reinterpret_cast<float*>(smem) + row;  // [token][row]
+      static_assert(4 * Lay::kTile >= C * C * 4, "the factors' place");
 #pragma unroll 1
       for (int round = 0; item_at(round) < a.items; ++round) {
         const Item it = item_of(a, item_at(round));
 #pragma unroll 1
         for (int n = 0; n < it.nc; ++n) {
-          const int t = n * C + row, valid = min(C, it.tokens - n * C);
+          const int valid = min(C, it.tokens - n * C), own = min(row, valid - 1);   // (rows behind the last one: not written)
           const int64_t tok = it.tok0 + n * C;
+          const int newest = __reduce_max_sync(0xffffffffu, own);
           bool odd = false;
           for (int i = lane; i < valid * (D / 8); i += 32) {
             const uint4 v = *reinterpret_cast<const uint4*>(a.V + (tok + i / (D / 8)) * a.vstride + (int64_t)it.kvh * D + i % (D / 8) * 8);
@@ -903,28 +921,39 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           }
           if (!__any_sync(0xffffffffu, odd)) continue;
 #pragma unroll 1
-          for (int g = 0; g < G && t < it.tokens; ++g) {
-            const bf16* q = a.Q + (tok + row) * a.qstride + (int64_t)(it.kvh * G + g) * D;
-            bf16* to = a.O + (tok + row) * a.ostride + (int64_t)(it.kvh * G + g) * D;
+          for (int g = 0; g < G; ++g) {
+            const uint4* q = reinterpret_cast<const uint4*>(a.Q + (tok + own) * a.qstride + (int64_t)(it.kvh * G + g) * D);
+            float d = 0.0f;
+#pragma unroll 1
+            for (int j = newest; j >= 0; --j) {
+              const uint4* k = reinterpret_cast<const uint4*>(a.K + (tok + j) * a.kstride + (int64_t)it.kvh * D);
+              float p = 0.0f;
+#pragma unroll 4
+              for (int i = 0; i < D / 8; ++i) {
+                const uint4 x = q[i], y = k[i];
+                const uint32_t xx[4] = {x.x, x.y, x.z, x.w}, yy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p = fmaf(high(xx[e]), high(yy[e]), fmaf(low(xx[e]), low(yy[e]), p));
+              }
+              factor[j * C] = p * a.scale * expf(d);
+              if (j <= own) d += at_least(__ldg(a.decay + (tok + j) * a.dstride + it.kvh), kLeastDecay);
+            }
+            bf16* to = a.O + (tok + own) * a.ostride + (int64_t)(it.kvh * G + g) * D;
 #pragma unroll 1
             for (int k0 = 0; k0 < D; k0 += 8) {
-              float o[8], d = 0.0f;
+              uint4 x = *reinterpret_cast<const uint4*>(to + k0);
+              float o[8] = {low(x.x), high(x.x), low(x.y), high(x.y), low(x.z), high(x.z), low(x.w), high(x.w)};
+#pragma unroll 2
+              for (int j = newest; j >= 0; --j) {
+                x = *reinterpret_cast<const uint4*>(a.V + (tok + j) * a.vstride + (int64_t)it.kvh * D + k0);
+                const float v[8] = {low(x.x), high(x.x), low(x.y), high(x.y), low(x.z), high(x.z), low(x.w), high(x.w)};
+                if (j > own) continue;
+                const float p = factor[j * C];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] = __bfloat162float(to[k0 + i]);
-#pragma unroll 1
-              for (int j = row; j >= 0; --j) {
-                const bf16* k = a.K + (tok + j) * a.kstride + (int64_t)it.kvh * D;
-                const bf16* v = a.V + (tok + j) * a.vstride + (int64_t)it.kvh * D + k0;
-                float p = 0.0f;
-#pragma unroll 1
-                for (int i = 0; i < D; ++i) p = fmaf(__bfloat162float(q[i]), __bfloat162float(k[i]), p);
-                p *= a.scale * expf(d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = fmaf(p, __bfloat162float(v[i]), o[i]);
-                d += at_least(__ldg(a.decay + (tok + j) * a.dstride + it.kvh), kLeastDecay);
+                for (int i = 0; i < 8; ++i) o[i] = fmaf(p, v[i], o[i]);
               }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) to[k0 + i] = __float2bfloat16_rn(o[i]);
+              if (row < valid)
+                *reinterpret_cast<uint4*>(to + k0) = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
             }
           }
           __syncwarp();

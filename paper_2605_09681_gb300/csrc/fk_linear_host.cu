@@ -4,6 +4,7 @@
 // allocated or waited for after fk_linear_create, so that a step's attentions can be captured in a graph; which states
 // a launch reads depends on the step alone, so that a graph's replays go on from one another.
 #include "fk_linear.h"
+#include "fk_rows.h"
 
 #include <algorithm>
 #include <cmath>
@@ -108,28 +109,6 @@ fk_status alloc(fk_linear* h, size_t bytes, void** out) {
   return cudaMemset(p, 0, bytes) == cudaSuccess ? FK_OK : FK_ERR_CUDA;
 }
 
-// `tokens` rows of `width` bytes, `stride` bytes apart
-struct Rows {
-  uintptr_t p;
-  int64_t stride, width;
-};
-// Whether rows of one meet rows of the other.  With one stride, slices of the same wide rows are told apart; else whole
-// extents are compared.
-bool meet(const Rows& a, const Rows& b, int64_t tokens) {
-  const int64_t la = (tokens - 1) * a.stride + a.width, lb = (tokens - 1) * b.stride + b.width;
-  if (a.p + (uintptr_t)la <= b.p || b.p + (uintptr_t)lb <= a.p) return false;
-  if (a.stride != b.stride || tokens == 1) return true;
-  const int64_t d = (int64_t)(a.p < b.p ? b.p - a.p : a.p - b.p) % a.stride;
-  const int64_t low = a.p < b.p ? a.width : b.width, high = a.p < b.p ? b.width : a.width;
-  return d < low || a.stride - d < high;
-}
-
-// All that rows extend over, as one.
-Rows whole(const Rows& a, int64_t tokens) {
-  const int64_t n = (tokens - 1) * a.stride + a.width;
-  return Rows{a.p, n, n};
-}
-
 // ---- plan of a step
 // Estimated times in us, measured back to back on a GB300: a launch's start and end; an item, and its chunks and each
 // further query head of them, of the kernel that computes o and of the one that forms segments' states; the join of those; of the
@@ -142,6 +121,12 @@ constexpr Times kTimes128{4.5, 3.0, 2.8, 2.3, 2.0, 1.8, 1.0, 2.2, 0.28, 0.0031},
 // Time of `groups` of equally long items (length, count), longest first, on the SMs: each goes to the one that is free first.
 double fill_sms(const fk_linear* h, std::vector<std::pair<double, int64_t>>& groups) {
   std::sort(groups.begin(), groups.end(), [](const auto& x, const auto& y) { return x.first > y.first; });
+  size_t kinds = 0;
+  for (size_t i = 0; i < groups.size(); ++i) {       // those of one length as one group
+    if (kinds > 0 && groups[kinds - 1].first == groups[i].first) groups[kinds - 1].second += groups[i].second;
+    else groups[kinds++] = groups[i];
+  }
+  groups.resize(kinds);
   std::vector<double> busy(h->sms, 0.0), other(h->sms);
   for (const auto& g : groups) {
     int64_t left = g.second;
@@ -149,7 +134,8 @@ double fill_sms(const fk_linear* h, std::vector<std::pair<double, int64_t>>& gro
     for (double& t : busy) t += (double)whole * g.first;
     left -= whole * h->sms;
     while (left > 0) {
-      const int n = (int)std::min<int64_t>(left, h->sms);
+      const auto again = std::lower_bound(busy.begin() + 1, busy.end(), busy[0] + g.first);   // (the first SM is free before it)
+      const int n = (int)std::min<int64_t>(left, again - busy.begin());
       for (int i = 0; i < n; ++i) busy[i] += g.first;
       std::merge(busy.begin(), busy.begin() + n, busy.begin() + n, busy.end(), other.begin());
       busy.swap(other);
@@ -200,6 +186,10 @@ double best_split(const fk_linear* h, const std::vector<StepSeq>& step, int upto
       if (step[i].n_new > kLinearChunk) longest.push_back((int)i);
     }
   if (most == 0) return 0.0;
+  // where all SMs are busy for longer than the longest sequence takes, there is nothing to gain
+  int64_t chunks = 0;
+  for (const StepSeq& s : step) chunks += s.n_new > upto ? chunks_of(s.n_new) : 0;
+  if (chunks * h->cfg.n_kv_heads >= 2 * (int64_t)most * h->sms) return time_split(h, step, upto, *segs);
   double least = 1e30;
   std::vector<int> n(step.size(), 1);
   for (int parts = 1; parts <= most; parts += std::max(1, parts / 8)) {

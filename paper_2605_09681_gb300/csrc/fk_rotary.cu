@@ -11,6 +11,7 @@
 // hardly more than a launch's start and end) in 13.4 us, 63%.  The tables are bound by the angles' arithmetic: 131072 x 64 in 19.8
 // us, 10 us of which their writes would take.
 #include "fk_internal.h"
+#include "fk_rows.h"
 
 #include <cuda_fp16.h>
 
@@ -243,10 +244,15 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(const __grid_constant_
 
 bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-bool on_current_device(const void* p) {
-  cudaPointerAttributes at{};
+int current_device() {
   int dev = -1;
-  if (cudaPointerGetAttributes(&at, p) != cudaSuccess || cudaGetDevice(&dev) != cudaSuccess) {
+  if (cudaGetDevice(&dev) != cudaSuccess) cudaGetLastError();
+  return dev;
+}
+
+bool on_device(const void* p, int dev) {
+  cudaPointerAttributes at{};
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
     cudaGetLastError();
     return false;
   }
@@ -356,13 +362,25 @@ fk_status fk_rotate(const fk_rotary* r, int64_t tokens, const int32_t* positions
   if (!X2 != !Y2 || !X2 != (x2_heads == 0)) return FK_ERR_ARG;
   if (tokens == 0) return FK_OK;
   const int size = type == FK_TYPE_F32 ? 4 : 2;
+  const int dev = current_device();
   auto rows_ok = [&](const void* p, int64_t stride, int heads) {
-    return p && aligned(p, 16) && stride >= (int64_t)heads * r->head_dim && stride * size % 16 == 0 && on_current_device(p);
+    return p && aligned(p, 16) && stride >= (int64_t)heads * r->head_dim && stride * size % 16 == 0 && on_device(p, dev);
   };
-  if (!positions || !aligned(positions, 4) || !on_current_device(positions)) return FK_ERR_ARG;
-  if (!rows_ok(X, x_stride, x_heads) || !rows_ok(Y, y_stride, x_heads) || (X == Y && x_stride != y_stride)) return FK_ERR_ARG;
-  if (X2 && (!rows_ok(X2, x2_stride, x2_heads) || !rows_ok(Y2, y2_stride, x2_heads) || (X2 == Y2 && x2_stride != y2_stride)))
-    return FK_ERR_ARG;
+  if (!positions || !aligned(positions, 4) || !on_device(positions, dev)) return FK_ERR_ARG;
+  if (!rows_ok(X, x_stride, x_heads) || !rows_ok(Y, y_stride, x_heads)) return FK_ERR_ARG;
+  if (X2 && (!rows_ok(X2, x2_stride, x2_heads) || !rows_ok(Y2, y2_stride, x2_heads))) return FK_ERR_ARG;
+  // outputs meet nothing but their own input, row for row
+  auto rows = [&](const void* p, int64_t stride, int heads) {
+    return Rows{reinterpret_cast<uintptr_t>(p), stride * size, (int64_t)heads * r->head_dim * size};
+  };
+  const Rows at{reinterpret_cast<uintptr_t>(positions), r->n_axes * 4, r->n_axes * 4};
+  const Rows x = rows(X, x_stride, x_heads), y = rows(Y, y_stride, x_heads);
+  auto apart = [&](const Rows& in, const Rows& out) { return in.p == out.p ? in.stride == out.stride : !meet(in, out, tokens); };
+  if (!apart(x, y) || meet(at, y, tokens)) return FK_ERR_ARG;
+  if (X2) {
+    const Rows x2 = rows(X2, x2_stride, x2_heads), y2 = rows(Y2, y2_stride, x2_heads);
+    if (!apart(x2, y2) || meet(at, y2, tokens) || meet(x, y2, tokens) || meet(x2, y, tokens) || meet(y, y2, tokens)) return FK_ERR_ARG;
+  }
   RotateArgs a;
   fill(*r, positions, &a.a);
   a.tokens = tokens;
@@ -408,9 +426,13 @@ fk_status fk_rotary_tables(const fk_rotary* r, int64_t tokens, const int32_t* po
   if (!r) return FK_ERR_ARG;
   if (!made(*r) || tokens < 0 || tokens >= ((int64_t)1 << 31)) return FK_ERR_CONFIG;
   if (tokens == 0) return FK_OK;
-  if (!positions || !aligned(positions, 4) || !on_current_device(positions)) return FK_ERR_ARG;
+  const int dev = current_device();
+  if (!positions || !aligned(positions, 4) || !on_device(positions, dev)) return FK_ERR_ARG;
   for (const float* p : {cos, sin})
-    if (!p || !aligned(p, 16) || !on_current_device(p)) return FK_ERR_ARG;
+    if (!p || !aligned(p, 16) || !on_device(p, dev)) return FK_ERR_ARG;
+  auto all = [&](const void* p, int64_t width) { return Rows{reinterpret_cast<uintptr_t>(p), width, tokens * width}; };
+  const Rows at = all(positions, r->n_axes * 4), c = all(cos, r->dim * 2), n = all(sin, r->dim * 2);
+  if (meet(at, c, 1) || meet(at, n, 1) || meet(c, n, 1)) return FK_ERR_ARG;
   TableArgs a;
   fill(*r, positions, &a.a);
   a.tokens = tokens;

@@ -386,3 +386,50 @@ def test_captured_steps_of_chunks_and_single_tokens(D, Hq, H):
                 assert (copies[layer] - plain.states(layer)).norm() <= 2.0 ** -18 * plain.states(layer).norm()
                 assert torch.equal(after[layer], out[layer])
         assert cache.sync_status() == 0 and plain.sync_status() == 0
+
+
+def test_rotations_that_overlap_are_refused():
+    from paper_2605_09681_gb300 import FkError, Rotary
+    rotary = Rotary(head_dim=64)
+    T = 8
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    wide = torch.randn(T, 6 * 64, device="cuda").bfloat16()
+    q, k, v = (wide[:, a * 64: (a + 2) * 64].unflatten(1, (2, 64)) for a in (0, 2, 4))
+    want = rotary.rotate(pos, q, k)
+    got = rotary.rotate(pos, q, k, Q_out=v, K_out=k)         # other slices of the rows, or the input itself
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    near = wide[:, 64: 3 * 64].unflatten(1, (2, 64))
+    flat = wide.flatten()
+    ints = flat.view(torch.int32)[:T]
+    dense = flat[: T * 128].view(T, 2, 64)
+    for bad in (dict(Q_out=k), dict(Q_out=near), dict(K_out=q), dict(Q_out=v, K_out=v), dict(Q_out=dense), dict(Q_out=q, K_out=near)):
+        with pytest.raises(FkError):
+            rotary.rotate(pos, q, k, **bad)
+    for bad in (dict(Q_out=q), dict(K_out=dense)):
+        with pytest.raises(FkError):
+            rotary.rotate(ints, q, k.clone(), **bad)
+    cos, sin = (torch.empty(T, 32, device="cuda") for _ in range(2))
+    with pytest.raises(FkError):
+        rotary.tables(pos, cos=cos, sin=cos)
+    with pytest.raises(FkError):
+        rotary.tables(cos.view(torch.int32).flatten()[:T], cos=cos, sin=sin)
+
+
+@pytest.mark.parametrize("D,G", [(64, 3), (128, 2)])
+def test_values_not_finite_in_every_chunk(D, G):
+    """NaN in one channel of all values from a token on, in a long run that is not split: the other channels as without."""
+    T = 700
+    q, k, v, g = _tensors(T, 2 * G, 2, D, G)
+    with _cache(n_q_heads=2 * G, head_dim=D) as cache:
+        cache.force_plan(8, 1)
+        cache.step([0], [T])
+        w = v.clone()
+        w[5:, 1, 3] = float("nan")
+        o, fine = cache.attend(0, q, k, w, g, advance=False), cache.attend(0, q, k, v, g, advance=False)
+        assert cache.sync_status() == 0
+        assert torch.equal(o[:, :G], fine[:, :G])
+        assert o[5:, G:, 3].isnan().all() and o[:5, G:].isfinite().all()
+        keep = [d for d in range(D) if d != 3]
+        want, _, oa, _, _ = R.attend(_np(q[:, G:]), _np(k[:, 1:]), _np(v[:, 1:]), _np(g[:, 1:]), np.zeros((1, D, D)), D ** -0.5)
+        lim = 2.0 ** -8 * np.abs(want) + (2.0 ** -7 + 2.0 ** -13) * oa
+        assert (np.abs(_np(o[:, G:]) - want) <= lim)[..., keep].all()
