@@ -550,7 +550,8 @@ FK_API fk_status fk_paged_sync_status(fk_paged* h, void* stream);
  * step's order.  The states are memory of the handle that the caller may read and write (fk_linear_states); all
  * start as zeros.  A few tokens (drafts, single tokens) go through the recurrence in fp32; longer runs are computed in chunks on the
  * tensor cores, where decayed keys multiply values in three bf16 parts (2^-24 of them) for the states, and for
- * o the decayed products q k and the states before a chunk are rounded to bf16.
+ * o the decayed products q k and the states before a chunk are rounded to bf16 (in a chunk whose values are not all finite, what
+ * comes from the state once more).
  *
  * All calls: device tensors only (FK_ERR_ARG for host memory or memory of another device), 16-byte aligned, tokens
  * `stride` elements apart (a multiple of 8, at least heads * head_dim; heads and channels contiguous).  Asynchronous on

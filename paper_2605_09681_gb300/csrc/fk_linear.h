@@ -8,7 +8,8 @@
 namespace fk {
 
 constexpr int kLinearSeqs = 256;      // sequences of one launch (their numbers travel by value)
-// g below this is taken as this: exp of it is 0 in fp32, and differences of sums stay numbers when a state starts anew
+// g below this is taken as this: exp of it is 0 in fp32 (the least positive number is exp(-103.3)), and differences of sums stay
+// numbers when a state starts anew
 constexpr float kLeastDecay = -110.0f;
 
 struct LinearSeqs {

@@ -29,9 +29,9 @@
 // What bounds it.  A chunk takes 2.8 us of a CTA by itself (2.3 more for each further query head; kLocal 1.8) and 3.8 with all SMs
 // loading: 24 chunks of 144 heads of 128 in 87 us, 5.1 TB/s.  By itself it is a chain: S' (and so X of the next chunk) waits for all
 // of dS, that for K', P for A and Y for P; the products are in the order that hides most of it, and the tensor pipe is active 31
-// to 38% of the time (two chunks at once would want twice the tensor memory).  An item costs 3 us besides (its first tiles, its state
+// to 43% of the time (two chunks at once would want twice the tensor memory).  An item costs 3 us besides (its first tiles, its state
 // both ways), a launch 4.5.  One sequence of few heads is therefore split (the host's plan): 4680 tokens of 12 heads in 12
-// segments 30 us, unsplit 113; what each segment adds is then formed first, which reads K and V twice.
+// segments 30 us, unsplit 104; what each segment adds is then formed first, which reads K and V twice.
 // Loops over columns are rolled where registers are not indexed: the roles' code together has to stay in the instruction
 // cache (unrolled, P of a chunk took 2400 cycles, and 4800 with all SMs fetching).  Roles are told apart by a warp number that comes
 // from a shuffle, so that the compiler knows branches by it to be uniform.
@@ -293,8 +293,8 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     load(&tmK, sK, &bar->k_full[0], first.kvh, first.tok0);
     if (!kLocal) load(&tmQ, sQ, &bar->q_full[0], first.kvh * G, first.tok0);
     load(&tmV, sV, &bar->v_full[0], first.kvh, first.tok0);
-    // sequences of few tokens may take the SMs that this launch leaves idle
-    if (!kLocal) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // (the join's blocks, or those of sequences of few tokens, may take the SMs that this launch leaves idle)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   }
   if (warp == 1) {
     __syncwarp();
@@ -975,16 +975,14 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 template <int D>
 __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant__ LinearChunkArgs a) {
   constexpr int kBlocks = D * D / 4 / 256;        // of a head
-  // (launched while the kernel before still ends, and lets the next one start)
+  // (launched while the kernel before still runs, and lets the next one start)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int k = blockIdx.y, segs = a.seqs.segs[k];
-  if (segs < 2) return;
   const int h = blockIdx.x / kBlocks, at = (blockIdx.x % kBlocks) * 256 + threadIdx.x;
   const int64_t place = (int64_t)a.seqs.place0[k] + h * segs;
-  float4 s = reinterpret_cast<const float4*>(a.state + ((int64_t)a.seqs.slot[k] * a.Hkv + h) * (D * D))[at];
-  float4* p = reinterpret_cast<float4*>(a.place + place * (D * D)) + at;
-  p[0] = s;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f), *p = reinterpret_cast<float4*>(a.place + place * (D * D)) + at;
+  if (segs > 1) p[0] = s = reinterpret_cast<const float4*>(a.state + ((int64_t)a.seqs.slot[k] * a.Hkv + h) * (D * D))[at];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   p += D * D / 4;
   const float* decay = a.place_decay + place + 1;
   constexpr int kAhead = 8;
