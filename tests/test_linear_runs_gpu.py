@@ -1,5 +1,5 @@
 """Linear attention and rotary positions as a generator uses them: many sequences of all lengths at once, hybrid layers over
-two kinds of cache, drafts that are verified, captured steps, rows far apart, a fixed memory budget.
+two kinds of cache, drafts that are verified, captured steps, rows far apart, memory held.
 
 A sequence's results depend on its own tokens, state and split alone, so beside others they are, bit for bit, what they are
 by themselves; against float64 the bounds are those of test_linear_gpu.py.
