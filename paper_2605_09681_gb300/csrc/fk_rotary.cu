@@ -7,8 +7,8 @@
 //
 // Both kernels move each byte once.  The angles are the expensive part (a sine and a cosine of a pair take as long as the
 // rotation of three heads), so a thread turns the same 8 pairs of several heads, and the rotation is bound by DRAM: 40003
-// tokens of 40 heads of 64 in 65.8 us, 92% of the measured copy rate; a video chunk (4680 tokens of 24 heads of 128, whose 57 MB are
-// hardly more than a launch's start and end) in 13.4 us, 63%.  The tables are bound by the angles' arithmetic: 131072 x 64 in 19.8
+// tokens of 40 heads of 64 in 65.2 us, 93% of the measured copy rate; a video chunk (4680 tokens of 24 heads of 128, whose 57 MB are
+// hardly more than a launch's start and end) in 13.4 us, 63%.  The tables are bound by the angles' arithmetic: 131072 x 64 in 16.8
 // us, 10 us of which their writes would take.
 #include "fk_internal.h"
 #include "fk_rows.h"
@@ -62,18 +62,39 @@ __device__ __forceinline__ void stage(const Angles& a, int pairs, uint64_t* s) {
 }
 
 // cos and sin of the angle `pos * turns` (times m, sin with the sign of `dir`).  The fraction of a turn is taken to the nearest
-// quarter and a rest a of at most pi / 4 either way, whose sine and cosine are the first five terms of their series:
-// the next ones are a^11 / 11! < 2^-29 and a^10 / 10! < 2^-25.  (sincospif took twice as long for a whole context's tables.)
-__device__ __forceinline__ void angle(uint64_t turns, int pos, float m, float dir, float* c, float* s) {
-  const uint64_t t = turns * (uint64_t)(int64_t)pos + (1ull << 61);   // + 1/8: the quarter is rounded, not cut off
-  const uint32_t q = (uint32_t)(t >> 62);
-  const int32_t hi = (int32_t)((uint32_t)(t >> 32) & 0x3FFFFFFFu) - 0x20000000;
-  const float a = fmaf((float)(uint32_t)t, 0x1p-32f, (float)hi) * (6.2831853071795865f * 0x1p-32f), z = a * a;
-  const float sn = fmaf(a * z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), a);
-  const float cs = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
-  const float x = q & 1 ? sn : cs, y = q & 1 ? cs : sn;      // quarters: (cs, sn), (-sn, cs), (-cs, -sn), (sn, -cs)
-  *c = __uint_as_float(__float_as_uint(x * m) ^ ((q + 1) << 30 & 0x80000000u));
-  *s = __uint_as_float(__float_as_uint(y * dir) ^ (q << 30 & 0x80000000u));
+// half and a rest a of at most pi / 2 either way, whose sine and cosine are the first seven terms of their series:
+// the next ones are a^15 / 15! < 2^-30 and a^14 / 14! < 2^-27; with the roundings 2^-23.  (The device is busier with integers and signs
+// than with products: to the nearest quarter, five terms and more to choose from, a whole context's tables took 19.7 us, so 18.1, 17.3 with
+// positions of several axes taken by address and not by choice, 16.8 with two pairs' products in one; with sincospif 40.)
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rc, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mov.b64 rc, {%6, %7};\n"
+      " fma.rn.f32x2 rd, ra, rb, rc;\n mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return fma2(a, b, two(-0.0f)); }
+
+// the rest of an angle in radians, and its odd half turn in the highest bit
+__device__ __forceinline__ float rest(uint64_t turns, int pos, uint32_t* odd) {
+  const uint64_t t = turns * (uint64_t)(int64_t)pos + (1ull << 62);   // + 1/4: the half is rounded, not cut off
+  const uint32_t top = (uint32_t)(t >> 32);
+  *odd = top & 0x80000000u;
+  return fmaf((float)(uint32_t)t, 0x1p-32f, (float)((int32_t)(top & 0x7FFFFFFFu) - 0x40000000)) * (6.2831853071795865f * 0x1p-32f);
+}
+// of two pairs
+__device__ __forceinline__ void angles(const uint64_t* turns, int pos0, int pos1, float m, float dir, float* c, float* s) {
+  uint32_t odd[2];
+  const float2 a = make_float2(rest(turns[0], pos0, &odd[0]), rest(turns[1], pos1, &odd[1])), z = mul2(a, a);
+  float2 sn = fma2(z, two(1.0f / 6227020800), two(-1.0f / 39916800)), cs = fma2(z, two(1.0f / 479001600), two(-1.0f / 3628800));
+  for (const float x : {1.0f / 362880, -1.0f / 5040, 1.0f / 120, -1.0f / 6}) sn = fma2(z, sn, two(x));
+  for (const float x : {1.0f / 40320, -1.0f / 720, 1.0f / 24, -0.5f, 1.0f}) cs = fma2(z, cs, two(x));
+  sn = fma2(mul2(a, z), sn, a);
+  c[0] = cs.x * __uint_as_float(__float_as_uint(m) ^ odd[0]);
+  c[1] = cs.y * __uint_as_float(__float_as_uint(m) ^ odd[1]);
+  s[0] = sn.x * __uint_as_float(__float_as_uint(dir) ^ odd[0]);
+  s[1] = sn.y * __uint_as_float(__float_as_uint(dir) ^ odd[1]);
 }
 
 // a token's positions, and a pair's of them
@@ -175,9 +196,9 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const __grid_constant_
     const Places pos(a.a, t);
     const float dir = a.inverse ? -a.a.magnitude : a.a.magnitude;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; i += 2) {
       const int p = 8 * u + i;
-      angle(turns[p], pos.of(a.a, p), a.a.magnitude, dir, &cs[i], &sn[i]);
+      angles(turns + p, pos.of(a.a, p), pos.of(a.a, p + 1), a.a.magnitude, dir, cs + i, sn + i);
     }
   }
   // several heads' loads before the first is turned: a thread's own are few bytes
@@ -227,16 +248,21 @@ __global__ void __launch_bounds__(kThreads) tables_kernel(const __grid_constant_
   const int quads = a.pairs / 4, tb = threadIdx.x / quads, p = 4 * (threadIdx.x - tb * quads);
   if (tb >= a.per_block) return;
   uint64_t turns[4];
+  int axis[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) turns[i] = all[p + i];
+  for (int i = 0; i < 4; ++i) {
+    turns[i] = all[p + i];
+    axis[i] = (p + i >= a.a.first[1]) + (p + i >= a.a.first[2]) + (p + i >= a.a.first[3]);
+  }
   const int64_t t0 = (int64_t)blockIdx.x * a.per_block * a.rounds + tb;
   for (int r = 0; r < a.rounds; ++r) {
     const int64_t t = t0 + (int64_t)r * a.per_block;
     if (t >= a.tokens) return;
-    const Places pos(a.a, t);
+    const int* pos = a.a.positions + t * a.a.axes;
     float c[4], s[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) angle(turns[i], pos.of(a.a, p + i), a.a.magnitude, a.a.magnitude, &c[i], &s[i]);
+    for (int i = 0; i < 4; i += 2)
+      angles(turns + i, __ldg(pos + axis[i]), __ldg(pos + axis[i + 1]), a.a.magnitude, a.a.magnitude, c + i, s + i);
     *reinterpret_cast<float4*>(a.cos + t * a.pairs + p) = make_float4(c[0], c[1], c[2], c[3]);
     *reinterpret_cast<float4*>(a.sin + t * a.pairs + p) = make_float4(s[0], s[1], s[2], s[3]);
   }

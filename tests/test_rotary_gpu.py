@@ -1,7 +1,7 @@
 """Rotary positions on the GPU against float64.
 
-Bound: an angle is off by at most 2^-24 half turns (pi 2^-24) by its rounding to fp32, sine and cosine by 2 steps (2^-22), each
-product and the sum by 2^-24, so a rotated channel by (|a| + |b|) m (pi + 4 + 2) 2^-24 < (|a| + |b|) m 2^-20, and by half a
+Bound: an angle of up to a quarter turn is off by three roundings to fp32 (1.5 pi 2^-24), sine and cosine by 2 steps (2^-22), each
+product and the sum by 2^-24, so a rotated channel by (|a| + |b|) m (1.5 pi + 4 + 2) 2^-24 < (|a| + |b|) m 2^-20, and by half a
 step of its type.  Frequencies in double precision: 2^-52 of an angle, 2^31 2^-52 at the farthest position (below
 2^-20 too); both go into 2^-19.
 """
