@@ -407,7 +407,7 @@ FK_API fk_status fk_rotary_make(const fk_rotary_config* cfg, fk_rotary* out);
  * positions (device int32 [tokens][n_axes], any values); inverse = 1: by the opposite angles (the gradient of the rotation).  Channels
  * behind `dim` are copied.  Y may be X (then with the same stride); otherwise outputs overlap nothing (FK_ERR_ARG).  Tensors of
  * `type`, 16-byte aligned, tokens `stride` elements apart (a multiple of 16 bytes, at least heads * head_dim; heads and
- * channels contiguous).  heads 1..1024 each, tokens below 2^31.
+ * channels contiguous).  heads 1..1024 each, tokens below 2^31; without tokens no pointer is looked at.
  * FK_ERR_ARG for null, unaligned or host pointers, short strides; FK_ERR_CONFIG for sizes out of range or a rotation
  * that fk_rotary_make did not make.  Asynchronous on `stream`; allocates nothing; uses the current device. */
 FK_API fk_status fk_rotate(const fk_rotary* r, int64_t tokens, const int32_t* positions, int inverse, int type,

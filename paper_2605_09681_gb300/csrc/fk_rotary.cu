@@ -385,8 +385,8 @@ fk_status fk_rotate(const fk_rotary* r, int64_t tokens, const int32_t* positions
   if (!made(*r) || (inverse != 0 && inverse != 1) || type < FK_TYPE_BF16 || type > FK_TYPE_F32) return FK_ERR_CONFIG;
   if (tokens < 0 || tokens >= ((int64_t)1 << 31)) return FK_ERR_CONFIG;
   if (x_heads < 1 || x_heads > 1024 || x2_heads < 0 || x2_heads > 1024) return FK_ERR_CONFIG;
+  if (tokens == 0) return FK_OK;        // (tensors of no tokens may have no address)
   if (!X2 != !Y2 || !X2 != (x2_heads == 0)) return FK_ERR_ARG;
-  if (tokens == 0) return FK_OK;
   const int size = type == FK_TYPE_F32 ? 4 : 2;
   const int dev = current_device();
   auto rows_ok = [&](const void* p, int64_t stride, int heads) {
