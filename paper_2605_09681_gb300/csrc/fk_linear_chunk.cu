@@ -74,6 +74,7 @@ struct Barriers {
 struct alignas(16) Sums {
   float g[C];                         // G_j
   float u[C];                         // exp(R - G_j), R the sum at the end of j's 32 tokens; `grow`: exp(G_C - G_j)
+  __half rest[C];                     // G_j less g[j]: sums run to 2^15 where states start anew, and fp32 has steps of 2^-9 there
   float w[4];                         // exp(G_C - R) of each 32 tokens; `grow`: 1
   float e;                            // exp(G_C)
   int grow;                           // some g > 0: the factors could overflow where their product does not
@@ -165,11 +166,14 @@ __device__ __forceinline__ float2 less(float2 x, uint32_t y) {
       : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "r"(y));
   return d;
 }
+__device__ __forceinline__ float2 of_f16(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// a whole number of 2^-32 as fp32
-__device__ __forceinline__ float of_fixed(int64_t x) { return fmaf((float)(uint32_t)x, 0x1p-32f, (float)(int32_t)(x >> 32)); }
+// a whole number of 2^-32, less what fp32 holds of it already
+__device__ __forceinline__ float of_fixed(int64_t x, float held = 0.0f) {
+  return fmaf((float)(uint32_t)x, 0x1p-32f, (float)(int32_t)(x >> 32) - held);
+}
 
 // A segment of one kv head of a sequence.
 struct Item {
@@ -478,7 +482,8 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       for (int n = 0; n < it.nc; ++n) {
         const int c = base + n, b = c & 1, u = c >> 1;
         // whole numbers of 2^-32: sums and their differences are exact however far they run (of g log2 e itself, 2^-33 a token is
-        // 2^-26 at most for a chunk, and its product in fp32 2^-24 of it); what is not a number makes all sums from its token on that
+        // 2^-26 at most for a chunk, and its product in fp32 2^-24 of it), and P's from two parts of them to 2^-20; what is not a
+        // number makes all sums from its token on that
         int64_t sum[4];
         bool grows = false;
         int lost = C;                                        // first token that is not a number
@@ -508,17 +513,20 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         // the sum at the end of this lane's 32 tokens, unless the chunk grows
         const int64_t r = __shfl_sync(0xffffffffu, all, lane | 7), from = grow ? end : r;
         const float nan = __int_as_float(0x7FFFFFFF);
-        float gg[4], v[4];
+        float gg[4], rest[4], v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int64_t x = before + sum[i];
-          gg[i] = 4 * lane + i >= lost ? nan : of_fixed(x);
+          gg[i] = of_fixed(x);
+          rest[i] = of_fixed(x, gg[i]);
+          if (4 * lane + i >= lost) gg[i] = nan;
           v[i] = lost < C ? nan : exp2f(of_fixed(from - x));
         }
         if (u > 0 && !(ok = wait_for(&bar->g_empty[b], u - 1))) break;
         Sums& out = sums[b];
         *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(gg[0], gg[1], gg[2], gg[3]);
         *reinterpret_cast<float4*>(out.u + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
+        if (!kLocal) *reinterpret_cast<uint2*>(out.rest + 4 * lane) = make_uint2(pack_f16(rest[0], rest[1]), pack_f16(rest[2], rest[3]));
         if ((lane & 7) == 7) out.w[lane >> 3] = grow ? 1.0f : exp2f(of_fixed(end - r));
         if (lane == 0) {
           out.e = lost < C ? nan : exp2f(of_fixed(end));
@@ -585,7 +593,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         }
         fence_to_async();
       }
-      const float gi = kLocal ? 0.0f : sm.g[row] + a.log2_scale;
+      const float gi = kLocal ? 0.0f : sm.g[row], ri = kLocal ? 0.0f : __half2float(sm.rest[row]) + a.log2_scale;
       const bool grow = !kLocal && __any_sync(0xffffffffu, sm.grow);
       // K' of this warpgroup's first quarter, P of the first query head while that is multiplied, K' of the other quarter, P of
       // further query heads
@@ -651,15 +659,21 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
             FK_TMEM_LD32(lanes + kColA + 32 * q, x);
             if (q == wq || grow) {
               const float4* y = reinterpret_cast<const float4*>(sm.g + 32 * q);
+              const uint2* z = reinterpret_cast<const uint2*>(sm.rest + 32 * q);
               FK_TMEM_WAIT_LD32(x);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const float4 v = y[i];
-                const float vv[4] = {v.x, v.y, v.z, v.w};
+                const uint2 w = z[i];
+                // (the difference of the fp32 parts is exact where it is small)
+                const float2 minus = make_float2(-1.0f, -1.0f), g2 = make_float2(gi, gi), r2 = make_float2(ri, ri);
+                const float2 d0 = fadd2(ffma2(make_float2(v.x, v.y), minus, g2), ffma2(of_f16(w.x), minus, r2));
+                const float2 d1 = fadd2(ffma2(make_float2(v.z, v.w), minus, g2), ffma2(of_f16(w.y), minus, r2));
+                const float vv[4] = {d0.x, d0.y, d1.x, d1.y};
                 float e[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                  e[c] = __uint_as_float(x[4 * i + c]) * fast_exp2(gi - vv[c]);
+                  e[c] = __uint_as_float(x[4 * i + c]) * fast_exp2(vv[c]);
                   if (q == wq && 4 * i + c > lane) e[c] = 0.0f;
                 }
                 x[2 * i] = pack_bf16(e[0], e[1]);
@@ -667,7 +681,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
               }
             } else {
               const float4* y = reinterpret_cast<const float4*>(sm.u + 32 * q);
-              const float f1 = fast_exp2(gi - sm.g[32 * q + 31]);
+              const float f1 = fast_exp2((gi - sm.g[32 * q + 31]) + (ri - __half2float(sm.rest[32 * q + 31])));
               const float2 f = make_float2(f1, f1);
               FK_TMEM_WAIT_LD32(x);
 #pragma unroll
@@ -804,7 +818,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
     for (int n = 0; n < it.nc && ok; ++n) {
       const int c = base + n, b = c & 1, u = c >> 1, t = n * C + row;
       if (!(ok = wait_for(&bar->g_full[b], u) && wait_for(&bar->odd_full[b], u))) break;
-      const float e = exp2f(sums[b].g[row] + a.log2_scale);
+      const float e = exp2f(sums[b].g[row] + (__half2float(sums[b].rest[row]) + a.log2_scale));
       const bool odd = __any_sync(0xffffffffu, bar->odd[b]);
       for (int g = 0; g < G; ++g) {
         const int m = c * G + g, head = it.kvh * G + g;
