@@ -594,7 +594,8 @@ FK_API fk_status fk_linear_step(fk_linear* h, int n_seqs, const int32_t* seqs, c
 
 /* One layer's attention over the step's tokens: Q, O [tokens][n_q_heads][head_dim], K, V [tokens][n_kv_heads][head_dim].
  * decay: device fp32, g as it stands in exp(g): [tokens][n_kv_heads] with decay_stride elements (at least n_kv_heads) from token to
- * token, or, decay_stride = 0, [n_kv_heads] for all tokens.  g <= 0 decays (-inf: the state starts anew); g > 0 grows.
+ * token, or, decay_stride = 0, [n_kv_heads] for all tokens.  g <= 0 decays (-inf: the state starts anew); g > 0 grows,
+ * as far as fp32 goes: from a token on whose exp(g) passes it nothing is finite, and need not be where growth over 128 tokens does.
  * scale = 0: 1 / sqrt(head_dim).
  * mode FK_LINEAR_ADVANCE: the states held become those after the step (calling again takes the tokens in again).
  * FK_LINEAR_STAY: they stay, and with state_out (device fp32 [n_seqs][n_kv_heads][head_dim][head_dim], 16-byte aligned, not

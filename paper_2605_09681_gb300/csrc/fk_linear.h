@@ -9,8 +9,10 @@ namespace fk {
 
 constexpr int kLinearSeqs = 256;      // sequences of one launch (their numbers travel by value)
 // g below this is taken as this: exp of it is 0 in fp32 (the least positive number is exp(-103.3)), and differences of sums stay
-// numbers when a state starts anew
-constexpr float kLeastDecay = -110.0f;
+// numbers when a state starts anew.  Among tokens that grow the least is lower, since 127 of them may multiply by exp(11268).
+constexpr float kLeastDecay = -110.0f, kLeastAmongGrowth = -12000.0f;
+// exp of more is no fp32 number: nothing is from there on
+constexpr float kMostGrowth = 88.72283f;
 
 struct LinearSeqs {
   int n;

@@ -74,7 +74,8 @@ struct Barriers {
 struct alignas(16) Sums {
   float g[C];                         // G_j
   float u[C];                         // exp(R - G_j), R the sum at the end of j's 32 tokens; `grow`: exp(G_C - G_j)
-  __half rest[C];                     // G_j less g[j]: sums run to 2^15 where states start anew, and fp32 has steps of 2^-9 there
+  __half rest[C];                     // G_j less g[j]: sums run to 2^15 where states start anew (2^22 in a chunk that grows), and
+                                      // fp32 has steps of 2^-9 there
   float w[4];                         // exp(G_C - R) of each 32 tokens; `grow`: 1
   float e;                            // exp(G_C)
   int grow;                           // some g > 0: the factors could overflow where their product does not
@@ -482,17 +483,21 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
       for (int n = 0; n < it.nc; ++n) {
         const int c = base + n, b = c & 1, u = c >> 1;
         // whole numbers of 2^-32: sums and their differences are exact however far they run (of g log2 e itself, 2^-33 a token is
-        // 2^-26 at most for a chunk, and its product in fp32 2^-24 of it), and P's from two parts of them to 2^-20; what is not a
-        // number makes all sums from its token on that
+        // 2^-26 at most for a chunk, and its product in fp32 2^-24 of it), and P's from two parts of them to 2^-20 (2^-14 in a
+        // chunk that grows); where exp(g) is not a number, nothing is from that token on
         int64_t sum[4];
         bool grows = false;
-        int lost = C;                                        // first token that is not a number
+        int lost = C;                                        // first token whose exp(g) is not a number
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float y = ahead[0][i];
-          grows |= !(y <= 0.0f);
-          if (y != y) lost = min(lost, 4 * lane + i);
-          const int64_t z = __float2ll_rn(fminf(fmaxf(y, kLeastDecay), -kLeastDecay) * (1.4426950408889634f * 0x1p32f));
+          grows |= !(ahead[0][i] <= 0.0f);
+          if (!(ahead[0][i] <= kMostGrowth)) lost = min(lost, 4 * lane + i);
+        }
+        const bool grow = __any_sync(0xffffffffu, grows);
+        const float least = grow ? kLeastAmongGrowth : kLeastDecay;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t z = __float2ll_rn(fminf(fmaxf(ahead[0][i], least), kMostGrowth) * (1.4426950408889634f * 0x1p32f));
           sum[i] = i == 0 ? z : sum[i - 1] + z;
         }
         int64_t all = sum[3];
@@ -502,7 +507,6 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (lane >= o) all += z;
         }
         const int64_t before = all - sum[3], end = __shfl_sync(0xffffffffu, all, 31);
-        const bool grow = __any_sync(0xffffffffu, grows);
         lost = __reduce_min_sync(0xffffffffu, lost);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -950,7 +954,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                 for (int e = 0; e < 4; ++e) p = fmaf(high(xx[e]), high(yy[e]), fmaf(low(xx[e]), low(yy[e]), p));
               }
               factor[j * C] = p * a.scale * expf(d);
-              if (j <= own) d += at_least(__ldg(a.decay + (tok + j) * a.dstride + it.kvh), kLeastDecay);
+              if (j <= own) d += at_least(__ldg(a.decay + (tok + j) * a.dstride + it.kvh), kLeastAmongGrowth);
             }
             bf16* to = a.O + (tok + own) * a.ostride + (int64_t)(it.kvh * G + g) * D;
 #pragma unroll 1
