@@ -67,7 +67,7 @@ struct LinearChunkArgs {
   float* state_new;
   int to_out;
   float* place;                       // [places][D][D]: the state before a segment
-  float* place_decay;                 // [places]: what the segment before it leaves of a state
+  float2* place_decay;                // [places]: what the segment before it leaves of a state, in two parts
   int* status;
   int items, ctas;                    // work items, CTAs that take them in turn
   LinearChunkSeqs seqs;

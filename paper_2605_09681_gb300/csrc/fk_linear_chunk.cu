@@ -78,6 +78,7 @@ struct alignas(16) Sums {
                                       // fp32 has steps of 2^-9 there
   float w[4];                         // exp(G_C - R) of each 32 tokens; `grow`: 1
   float e;                            // exp(G_C)
+  float2 left;                        // kLocal: what the segment leaves of a state by the chunk's end, in two parts
   int grow;                           // some g > 0: the factors could overflow where their product does not
 };
 
@@ -171,9 +172,19 @@ __device__ __forceinline__ float2 of_f16(uint32_t w) { return __half22float2(*re
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// a whole number of 2^-32, less what fp32 holds of it already
+// a whole number of 2^-40 (to 2^-25), less what fp32 holds of it already
 __device__ __forceinline__ float of_fixed(int64_t x, float held = 0.0f) {
-  return fmaf((float)(uint32_t)x, 0x1p-32f, (float)(int32_t)(x >> 32) - held);
+  return fmaf((float)(uint32_t)(x >> 8), 0x1p-32f, (float)(int32_t)(x >> 40) - held);
+}
+// Factors whose error is made up for.  (One by itself is off by up to 2^-23, at every chunk the same way where the decay is the same,
+// and slow decays take hundreds of them; what decays faster is forgotten in four.)
+__device__ __forceinline__ bool near_one(float e) { return e >= 0.78f && e <= 1.28f; }
+// 2^x less such a factor, its fp32 rounding or nearly that.  Of exp(y) - 1, |y| < 1/4; the series' next term is 4^-8 / 8! < 2^-31.
+__device__ __forceinline__ float exp_rest(int64_t x, float held) {
+  const float y = (float)x * (0.69314718055994531f * 0x1p-40f);
+  float t = 1.0f / 5040;
+  for (const float c : {1.0f / 720, 1.0f / 120, 1.0f / 24, 1.0f / 6, 0.5f}) t = fmaf(t, y, c);
+  return fmaf(y * y, t, y) - (held - 1.0f);
 }
 
 // A segment of one kv head of a sequence.
@@ -479,11 +490,14 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
 #pragma unroll
         for (int i = 0; i < 3; ++i) fetch(it, i, ahead[i]);
       }
+      int64_t total = 0;                                     // of the segment's chunks
+      bool total_lost = false;
+      float owed = 0.0f;                                     // what their factors so far, as rounded, lack of their product
 #pragma unroll 1
       for (int n = 0; n < it.nc; ++n) {
         const int c = base + n, b = c & 1, u = c >> 1;
-        // whole numbers of 2^-32: sums and their differences are exact however far they run (of g log2 e itself, 2^-33 a token is
-        // 2^-26 at most for a chunk, and its product in fp32 2^-24 of it), and P's from two parts of them to 2^-20 (2^-14 in a
+        // whole numbers of 2^-40: sums and their differences are exact however far they run (of g log2 e itself, 2^-41 a token, and its
+        // product in fp32 2^-24 of it), and P's from two parts of them to 2^-20 (2^-14 in a
         // chunk that grows); where exp(g) is not a number, nothing is from that token on
         int64_t sum[4];
         bool grows = false;
@@ -497,7 +511,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         const float least = grow ? kLeastAmongGrowth : kLeastDecay;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int64_t z = __float2ll_rn(fminf(fmaxf(ahead[0][i], least), kMostGrowth) * (1.4426950408889634f * 0x1p32f));
+          const int64_t z = __float2ll_rn(fminf(fmaxf(ahead[0][i], least), kMostGrowth) * (1.4426950408889634f * 0x1p40f));
           sum[i] = i == 0 ? z : sum[i - 1] + z;
         }
         int64_t all = sum[3];
@@ -526,17 +540,32 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
           if (4 * lane + i >= lost) gg[i] = nan;
           v[i] = lost < C ? nan : exp2f(of_fixed(from - x));
         }
+        const float w = grow ? 1.0f : exp2f(of_fixed(end - r));
+        float e = exp2f(of_fixed(end));
+        e = lost < C ? nan : fmaf(e, owed, e);
+        float2 left = make_float2(1.0f, 0.0f);
+        if (kLocal) {
+          // (what passes 2^21 stays there: it is 0 or infinite)
+          constexpr int64_t kMost = (int64_t)1 << 61;
+          total = min(max(total + end, -kMost), kMost);
+          total_lost |= lost < C;
+          left.x = total_lost ? nan : exp2f(of_fixed(total));
+          if (near_one(left.x)) left.y = exp_rest(total, left.x);
+        }
+        // (all but the stores is done by now: the chunk may be waited for)
         if (u > 0 && !(ok = wait_for(&bar->g_empty[b], u - 1))) break;
         Sums& out = sums[b];
         *reinterpret_cast<float4*>(out.g + 4 * lane) = make_float4(gg[0], gg[1], gg[2], gg[3]);
         *reinterpret_cast<float4*>(out.u + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
         if (!kLocal) *reinterpret_cast<uint2*>(out.rest + 4 * lane) = make_uint2(pack_f16(rest[0], rest[1]), pack_f16(rest[2], rest[3]));
-        if ((lane & 7) == 7) out.w[lane >> 3] = grow ? 1.0f : exp2f(of_fixed(end - r));
+        if ((lane & 7) == 7) out.w[lane >> 3] = w;
         if (lane == 0) {
-          out.e = lost < C ? nan : exp2f(of_fixed(end));
+          out.e = e;
+          if (kLocal) out.left = left;
           out.grow = grow;
         }
         arrive(&bar->g_full[b]);
+        owed = near_one(e) ? owed + exp_rest(end, e) : 0.0f;
       }
       base += it.nc;
       }
@@ -724,7 +753,7 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         return (t.segs > 1 ? a.place + t.place * (D * D) : a.state + ((int64_t)a.seqs.slot[t.s] * a.Hkv + t.kvh) * (D * D)) + at;
       };
       alignas(16) float st[D];
-      float left = 1.0f;                                     // what the segment leaves of a state
+      float2 left = make_float2(1.0f, 0.0f);                 // what the segment leaves of a state
       if (kLocal || !mine) {
 #pragma unroll
         for (int i = 0; i < D; ++i) st[i] = 0.0f;
@@ -751,8 +780,8 @@ linear_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
         if (n > 0) {
           if (!(ok = wait_for(&bar->g_full[c & 1], c >> 1))) break;
           e = sums[c & 1].e;
+          if (kLocal && n == it.nc) left = sums[c & 1].left;
           arrive(&bar->g_empty[c & 1]);
-          left *= e;
           // every X of the chunk (each phase is seen): S's place is free, and further query heads' X may follow
 #pragma unroll 1
           for (int g = 0; g < G && !kLocal && ok; ++g) {
@@ -1002,11 +1031,11 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
   if (segs > 1) p[0] = s = reinterpret_cast<const float4*>(a.state + ((int64_t)a.seqs.slot[k] * a.Hkv + h) * (D * D))[at];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   p += D * D / 4;
-  const float* decay = a.place_decay + place + 1;
+  const float2* decay = a.place_decay + place + 1;
   constexpr int kAhead = 8;
   for (int i0 = 1; i0 < segs; i0 += kAhead) {
     float4 x[kAhead];
-    float e[kAhead];
+    float2 e[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       if (i0 + i < segs) {
@@ -1016,10 +1045,10 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       if (i0 + i < segs) {
-        s.x = fmaf(s.x, e[i], x[i].x);
-        s.y = fmaf(s.y, e[i], x[i].y);
-        s.z = fmaf(s.z, e[i], x[i].z);
-        s.w = fmaf(s.w, e[i], x[i].w);
+        s.x = fmaf(s.x, e[i].x, fmaf(s.x, e[i].y, x[i].x));
+        s.y = fmaf(s.y, e[i].x, fmaf(s.y, e[i].y, x[i].y));
+        s.z = fmaf(s.z, e[i].x, fmaf(s.z, e[i].y, x[i].z));
+        s.w = fmaf(s.w, e[i].x, fmaf(s.w, e[i].y, x[i].w));
         p[i * (D * D / 4)] = s;
       }
     p += kAhead * (D * D / 4);

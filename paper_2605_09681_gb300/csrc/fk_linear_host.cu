@@ -52,7 +52,7 @@ struct fk_linear {
   std::vector<Launch> plan;           // of the step's sequences that have tokens
   int force_few = 0, force_segments = 0;
   float* place = nullptr;             // [kPlaces][D][D], and what segments leave of a state
-  float* place_decay = nullptr;
+  float2* place_decay = nullptr;
   int sms = 0;
   float* states = nullptr;            // [layers][max_seqs][Hkv][D][D]
   size_t per_seq = 0, per_layer = 0;  // floats
@@ -374,8 +374,8 @@ fk_status fk_linear_create(const fk_linear_config* cfg, fk_linear** out) {
     h->status = static_cast<int*>(p);
     if ((st = alloc(h.get(), (size_t)kPlaces * cfg->head_dim * cfg->head_dim * sizeof(float), &p)) != FK_OK) return st;
     h->place = static_cast<float*>(p);
-    if ((st = alloc(h.get(), kPlaces * sizeof(float), &p)) != FK_OK) return st;
-    h->place_decay = static_cast<float*>(p);
+    if ((st = alloc(h.get(), kPlaces * sizeof(float2), &p)) != FK_OK) return st;
+    h->place_decay = static_cast<float2*>(p);
     if (cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess) return FK_ERR_CUDA;
     if (linear_chunk_prepare(cfg->head_dim) != cudaSuccess) return FK_ERR_CUDA;
     if (cudaDeviceSynchronize() != cudaSuccess) return FK_ERR_CUDA;
