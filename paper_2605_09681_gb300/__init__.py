@@ -66,11 +66,22 @@ def _fast_calls():
     """(new tensor of (shape, strides, dtype) on the current device, the current device, the current stream of a device), as short as torch
     has them: between launches torch.empty_like takes 4 us a call and torch's own allocation of strided tensors 2."""
     import torch
+
+    def new(shape, strides, dtype):
+        return torch.empty_strided(shape, strides, dtype=dtype, device="cuda")
+
     try:
-        from torch._C._dynamo.guards import _empty_strided_cuda as new
+        from torch._C._dynamo.guards import _empty_strided_cuda as short
     except ImportError:
+        pass
+    else:
+        plain = new
+
         def new(shape, strides, dtype):
-            return torch.empty_strided(shape, strides, dtype=dtype, device="cuda")
+            try:
+                return short(shape, strides, dtype)
+            except TypeError:                                # (no public function: a torch to come may want other arguments)
+                return plain(shape, strides, dtype)
     try:
         return new, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     except AttributeError:
