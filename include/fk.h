@@ -353,9 +353,10 @@ FK_API fk_status fk_quantize_e4m3(const void* X, int64_t rows, int dim, int row_
  * Rotary positions (no counterpart in the paper, whose queries and keys come rotated): queries and keys turned by
  * their positions, for every cache of this library, and tables of the angles for fk_paged_append.
  *
- * Pair i of axis a turns by positions[token][a] * f_i: y = m (x_j cos - x_k sin), m (x_k cos + x_j sin).  The frequencies
- * are taken as fractions of a turn in 64-bit fixed point and a position times one is exact modulo whole turns: an angle
- * is as good at position 2^31 - 1 as at 1 (2^-24 of a turn or better).  Rotations are in fp32, rounded once.
+ * Pair i of axis a turns by positions[token][a] * f_i: y = m (x_j cos - x_k sin), m (x_k cos + x_j sin).  f_i is a double
+ * (from base and scaling: 2^-51 of itself), taken as a fraction of a turn to 2^-64, and a position times that is exact modulo whole
+ * turns: at position 2^31 - 1 an angle is off by 2^-33 of a turn from f_i's, and everywhere by its roundings to fp32, under 2^-24
+ * of a turn.  Rotations are in fp32, rounded once.
  * --------------------------------------------------------------------------------------------- */
 enum {
   FK_ROPE_HALF = 0,        /* channel pairs (i, i + dim/2)  */

@@ -2,8 +2,8 @@
 //
 // A pair's angle is position * f modulo a turn.  f is kept as a 64-bit fraction of a turn, so that the 64-bit product
 // with the position, taken modulo 2^64, is the angle modulo whole turns without any error: an fp32 product of
-// a position and a frequency is off by a radian and more at position 10^7.  Its upper bits are cut to fp32
-// (2^-27 of a turn).
+// a position and a frequency is off by a radian and more at position 10^7.  It is then rounded to fp32 (three roundings of at
+// most a quarter turn: under 2^-24 of a turn).
 //
 // Both kernels move each byte once.  The angles are the expensive part (a sine and a cosine of a pair take as long as the
 // rotation of three heads), so a thread turns the same 8 pairs of several heads, and the rotation is bound by DRAM: 40003
@@ -303,11 +303,13 @@ void fill(const fk_rotary& r, const int32_t* positions, Angles* a) {
   a->magnitude = r.magnitude;
 }
 
-// a frequency in radians a position -> the fraction of a turn in 2^-64 (its sign goes into the two's complement)
+// A frequency in radians a position -> the fraction of a turn in 2^-64 (its sign goes into the two's complement).  f / 2 pi as two
+// doubles: one alone is off by up to 2^-54 of a turn, which 2^31 positions make 2^-23.
 uint64_t turns_of(double f) {
-  const double t = std::fabs(f) / 6.283185307179586476925286766559;   // below 1/2
-  const double hi = std::floor(std::ldexp(t, 32));
-  const uint64_t u = ((uint64_t)hi << 32) + (uint64_t)std::ldexp(std::ldexp(t, 32) - hi, 32);
+  constexpr double kInverse = 0.15915494309189535, kRest = -9.839338337591243e-18;   // of 2 pi
+  const double x = std::fabs(f), t = x * kInverse, rest = std::fma(x, kInverse, -t) + x * kRest;   // t below 1/2
+  const double hi = std::floor(std::ldexp(t, 32)), lo = std::ldexp(std::ldexp(t, 32) - hi, 32);
+  const uint64_t u = ((uint64_t)hi << 32) + (uint64_t)(int64_t)std::floor(lo + std::ldexp(rest, 64));
   return f < 0 ? 0 - u : u;
 }
 
