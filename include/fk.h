@@ -549,10 +549,12 @@ FK_API fk_status fk_paged_sync_status(fk_paged* h, void* stream);
  * Use: fk_linear_step names the sequences of a step and how many tokens each has; then, layer by layer,
  * fk_linear_attend on [tokens][heads][head_dim] bf16 tensors that hold the sequences' tokens one after the other in the
  * step's order.  The states are memory of the handle that the caller may read and write (fk_linear_states); all
- * start as zeros.  A few tokens (drafts, single tokens) go through the recurrence in fp32; longer runs are computed in chunks on the
- * tensor cores, where decayed keys multiply values in three bf16 parts (2^-24 of them) for the states, and for
- * o the decayed products q k and the states before a chunk are rounded to bf16 (in a chunk whose values are not all finite, what
- * comes from the state once more).
+ * start as zeros.  Single tokens go through the recurrence in fp32.  A longer run goes through it too, or in chunks on the tensor
+ * cores, where decayed keys multiply values in three bf16 parts (2^-24 of them) for the states, and for o the decayed
+ * products q k and the states before a chunk are rounded to bf16 (in a chunk whose values are not all finite, what comes from
+ * the state once more): whichever is estimated to be faster for the step as a whole.  So of 2 to 32 tokens (drafts) the lengths of
+ * the other sequences decide whether o has those roundings, and of a longer run into how many segments it is split, whose
+ * states are joined in fp32.
  *
  * All calls: device tensors only (FK_ERR_ARG for host memory or memory of another device), 16-byte aligned, tokens
  * `stride` elements apart (a multiple of 8, at least heads * head_dim; heads and channels contiguous).  Asynchronous on

@@ -589,8 +589,9 @@ class Rotary:
 
     def rotate(self, positions, Q, K=None, inverse=False, Q_out=None, K_out=None, stream=None):
         """Q (and K, in the same launch) [tokens, heads, head_dim] in bf16, fp16 or fp32, which may be slices of wider rows,
-        turned by `positions` (int32 [tokens, axes], or [tokens]); inverse: the other way (the rotation's gradient).
-        Returns the rotated Q, or Q and K, in new tensors or in Q_out, K_out (which may be Q, K)."""
+        turned by `positions` (int32 [tokens, axes], or [tokens]); inverse: the other way (of the outputs' gradients: the
+        inputs' ones, which no call here records by itself).  Returns the rotated Q, or Q and K, in new tensors or in
+        Q_out, K_out (which may be Q, K)."""
         dev = Q.get_device()
         if dev >= 0 and dev != self._current():
             with self._torch.cuda.device(dev):
