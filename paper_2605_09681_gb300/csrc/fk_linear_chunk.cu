@@ -3,8 +3,8 @@
 // With G_i the sum of the decays' logarithms from a chunk's start through token i, and S the state before the chunk,
 //   o_i = scale (exp(G_i) q_i S + sum_(j <= i) exp(G_i - G_j) (q_i k_j) v_j),
 //   S'  = exp(G_C) S + sum_j exp(G_C - G_j) k_j v_j^T:
-// four matrix products of 128 x 128 x D a chunk and head, six with K' in three parts: 1.6 us of the tensor cores at their rate, for
-// 128 KB of q, k, v and o (D = 128), 2.9 us of an SM's share of the memory.  All exponents are of sums that are <= 0 where
+// four matrix products of 128 x 128 x D a chunk and head, six with K' in three parts: 2.0 us of an SM's tensor cores at the measured rate of
+// large products, for 128 KB of q, k, v and o (D = 128), 2.9 us of an SM's share of the memory.  All exponents are of sums that are <= 0 where
 // decays are.
 //
 // A CTA takes items (segments of one kv head's chunks, with all query heads that share it) one after the other, without a break
@@ -21,17 +21,20 @@
 //                 shared memory, the B operand of X
 //   warps 16-19   o: thread i scales row i of X where it is, rounds row i of Y to bf16 over a tile of Q or V that the products are
 //                 done with, and a TMA store takes it from there (straight from registers: 16 bytes of 32 lines at a time)
+// P and the S of X are rounded to bf16 (half a step, up to 2^-8 of a term): a product's operands have one type, Q's and V's range
+// wants bf16, and o is rounded to bf16 itself (0.0017 of it in the 2-norm, 0.0023 so).  Second parts would double two of the products, and
+// S's has no room in shared memory at D = 128.
 // Tensor memory columns: A and P 0-127, X and Y 128.., dS 256.., K' 384-479 (two buffers; kLocal: four from 0).
 //
 // kLocal: the state alone, from zero (what a segment adds), without Q and o.
 // Every wait is bounded; when one expires the CTA records it, drains its copies and products, and ends.
 //
 // What bounds it.  A chunk takes 2.8 us of a CTA by itself (2.3 more for each further query head; kLocal 1.8) and 3.8 with all SMs
-// loading: 24 chunks of 144 heads of 128 in 87 us, 5.1 TB/s.  By itself it is a chain: S' (and so X of the next chunk) waits for all
+// loading: 24 chunks of 144 heads of 128 in 85 us, 5.3 TB/s.  By itself it is a chain: S' (and so X of the next chunk) waits for all
 // of dS, that for K', P for A and Y for P; the products are in the order that hides most of it, and the tensor pipe is active 31
 // to 43% of the time (two chunks at once would want twice the tensor memory).  An item costs 3 us besides (its first tiles, its state
 // both ways), a launch 4.5.  One sequence of few heads is therefore split (the host's plan): 4680 tokens of 12 heads in 12
-// segments 30 us, unsplit 104; what each segment adds is then formed first, which reads K and V twice.
+// segments 31 us, unsplit 105; what each segment adds is then formed first, which reads K and V twice.
 // Loops over columns are rolled where registers are not indexed: the roles' code together has to stay in the instruction
 // cache (unrolled, P of a chunk took 2400 cycles, and 4800 with all SMs fetching).  Roles are told apart by a warp number that comes
 // from a shuffle, so that the compiler knows branches by it to be uniform.

@@ -7,9 +7,9 @@
 //
 // Both kernels move each byte once.  The angles are the expensive part (a sine and a cosine of a pair take as long as the
 // rotation of three heads), so a thread turns the same 8 pairs of several heads, and the rotation is bound by DRAM: 40003
-// tokens of 40 heads of 64 in 65.2 us, 93% of the measured copy rate; a video chunk (4680 tokens of 24 heads of 128, whose 57 MB are
-// hardly more than a launch's start and end) in 13.4 us, 63%.  The tables are bound by the angles' arithmetic: 131072 x 64 in 16.8
-// us, 10 us of which their writes would take.
+// tokens of 40 heads of 64 in fp16 in 65.6 us, 92% of the measured copy rate, in fp32 in 126 us, 96%; a video chunk (4680 tokens of 24
+// heads of 128, 57 MB, where loads wait for the angles and there is one round of blocks) in 13.6 us, 63%.  The tables are bound by the
+// angles' arithmetic: 131072 x 64 in 15.3 us (14.6 where they stay in L2), 10 us of which their writes would take.
 #include "fk_internal.h"
 #include "fk_rows.h"
 
