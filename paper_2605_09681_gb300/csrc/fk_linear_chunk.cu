@@ -29,10 +29,10 @@
 // kLocal: the state alone, from zero (what a segment adds), without Q and o.
 // Every wait is bounded; when one expires the CTA records it, drains its copies and products, and ends.
 //
-// What bounds it.  A chunk takes 2.8 us of a CTA by itself (2.3 more for each further query head; kLocal 1.8) and 3.8 with all SMs
+// What bounds it.  A chunk takes 2.8 us of a CTA by itself (2.3 more for each further query head; kLocal 1.8) and 3.2 with all SMs
 // loading: 24 chunks of 144 heads of 128 in 85 us, 5.3 TB/s.  By itself it is a chain: S' (and so X of the next chunk) waits for all
 // of dS, that for K', P for A and Y for P; the products are in the order that hides most of it, and the tensor pipe is active 31
-// to 43% of the time (two chunks at once would want twice the tensor memory).  An item costs 3 us besides (its first tiles, its state
+// to 43% of the time (two chunks at once would want twice the tensor memory at D = 128).  An item costs 3 us besides (its first tiles, its state
 // both ways), a launch 4.5.  One sequence of few heads is therefore split (the host's plan): 4680 tokens of 12 heads in 12
 // segments 31 us, unsplit 105; what each segment adds is then formed first, which reads K and V twice.
 // Loops over columns are rolled where registers are not indexed: the roles' code together has to stay in the instruction
